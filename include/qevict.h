@@ -34,8 +34,8 @@
  *   - Every call makes the cache's device current while it runs and puts the caller's current device back
  *     before it returns.
  *   - Process-wide state is limited to three things, none of which a caller can observe through results:
- *     the text qevict_last_error(NULL) returns (per thread: the last failure of qevict_create or
- *     qevict_workspace_bytes, which have no handle to keep it in); the per-device record of the
+ *     the text qevict_last_error(NULL) returns (per thread: the last failure of qevict_create,
+ *     qevict_workspace_bytes and the calls that take no handle); the per-device record of the
  *     shared-memory limits already granted to the kernels (only ever raised); and the built-in scratch
  *     array of qevict_decode_attn_noalloc with its per-device address.  One handle must not be used from
  *     two threads at once; different handles may be.
@@ -370,6 +370,139 @@ QEVICT_API qevict_status qevict_state_layout_of(qevict_handle h, qevict_state_la
 QEVICT_API qevict_status qevict_export_state(qevict_handle h, int32_t layer, int32_t seq, qevict_state_view* view);
 QEVICT_API qevict_status qevict_import_state(qevict_handle h, int32_t layer, int32_t seq, const qevict_state_view* view);
 
+/* ---- Attention over whole prompts ----------------------------------------------------------------------------
+ * The step before qevict_prefill_assign: softmax attention of every prompt token over the tokens before it, in
+ * full precision, for a batch of prompts of different lengths.  Needs no cache handle; errors leave their text in
+ * qevict_last_error(NULL) of the calling thread.
+ *     out[i, h] = sum_j softmax_j(scale * q[i, h] . k[j, h / G]) v[j, h / G],   lse[h, i] = ln sum_j exp(...)
+ * over the keys j that token i may see: all n_k of its sequence, or with `causal` those with j <= i + n_k - n_q
+ * (the queries are the last n_q of n_k tokens: a prompt given in pieces passes the earlier pieces' keys too).  A
+ * query that sees no key (n_k < n_q, or n_k = 0) gets out = 0 and lse = -infinity.
+ *
+ * Layouts, strides in elements, the last dimension (head_dim) contiguous, strides and addresses multiples of 16
+ * bytes.  PACKED: q [total_q, n_q_heads, d], k, v [total_k, n_kv_heads, d], lse [n_q_heads, total_q]; q_bounds and
+ * k_bounds are device int32 [n_seqs + 1], sequence s holds the rows bounds[s] .. bounds[s+1] - 1 (ascending; rows
+ * outside every sequence are neither read into a result nor written).  PADDED: q [n_seqs, n_q_heads, max_q, d],
+ * k, v [n_seqs, n_kv_heads, max_k, d] (the layout of qevict_prefill_assign), lse [n_seqs, n_q_heads, max_q];
+ * bounds are device int32 [n_seqs] lengths, or NULL for max_q / max_k everywhere.  max_q and max_k bound the
+ * lengths; a longer sequence is cut to them.  A key or value that is not finite spreads to every row of the
+ * sequence from 255 tokens before it on (nothing outside the sequence is affected). */
+enum { QEVICT_LAYOUT_PACKED = 0, QEVICT_LAYOUT_PADDED = 1 };
+typedef struct {
+  uint32_t struct_size;      /* sizeof(qevict_prompt_args) */
+  int32_t device;
+  int32_t dtype;             /* QEVICT_DTYPE_* of q, k, v, out */
+  int32_t layout;            /* QEVICT_LAYOUT_* */
+  int32_t n_seqs;            /* 0: nothing to do */
+  int32_t n_q_heads;         /* multiple of n_kv_heads */
+  int32_t n_kv_heads;
+  int32_t head_dim;          /* 64 or 128 */
+  int32_t max_q, max_k;
+  int32_t causal;            /* 0 or 1 */
+  float softmax_scale;       /* 0 => 1/sqrt(d) */
+  int64_t total_q, total_k;  /* PACKED: rows of q / of k and v; PADDED: ignored */
+  const void* q;             /* device */
+  const void* k;
+  const void* v;
+  void* out;                 /* device, strides out_stride */
+  float* lse;                /* device, or NULL */
+  const int32_t* q_bounds;   /* device */
+  const int32_t* k_bounds;
+  int64_t q_stride[3];       /* sequence (PADDED only), head, token */
+  int64_t k_stride[3];
+  int64_t v_stride[3];
+  int64_t out_stride[3];
+  int32_t* status;           /* device int32 or NULL: set to a nonzero code if a kernel gave up (see qevict_stats) */
+} qevict_prompt_args;
+QEVICT_API qevict_status qevict_prompt_attn_scratch_bytes(const qevict_prompt_args* args, uint64_t* bytes);
+QEVICT_API qevict_status qevict_prompt_attn(const qevict_prompt_args* args, void* scratch, uint64_t scratch_bytes, void* stream);
+
+/* ---- A cache in 8 bits with a scale for each block of tokens and KV head -----------------------------------
+ * The untiered companion of the three-tier cache: every token stays, at one byte per element.  All buffers are
+ * the caller's; the view below only points at them, and no call keeps anything.
+ *   - The tokens of a sequence are cut into blocks of `block` tokens.  A full block lies in a page of the pools as
+ *     codes, with one float32 scale for its keys and one for its values per KV head; block b of sequence s is page
+ *     block_table[s][b].  The open block (len % block tokens) lies in 16 bits in the sequence's tail rows.
+ *   - A block is quantised once, when its last token arrives [Migration-Stable Quantization: codes are written
+ *     once], in float32 with every operation rounded on its own: scale = amax / 127 (int8) or amax / 448 (e4m3),
+ *     code = x / scale rounded to the nearest code, ties to even.  A block whose amax / 127 (/ 448) is zero or not
+ *     finite gets scale 1; if it is not finite, codes 0.
+ *   - A page id outside 0 .. n_pages - 1 means that the block is absent: it is not written, not attended to, and its
+ *     mass is 0.  Any such id but -1 that a call would use also sets *status.
+ *   - Lengths are device int32 [n_seqs]; a length < 1 is an empty sequence (out = 0, lse = -infinity, no mass), one
+ *     beyond max_blocks * block or the call's max_len is cut to the whole blocks within the smaller of them, and
+ *     *status is set.
+ * The three calls need no handle; errors leave their text in qevict_last_error(NULL) of the calling thread.  They
+ * allocate nothing, do not synchronise and read the lengths and tables on the device, so they can be captured. */
+enum { QEVICT_CODE_INT8 = 0, QEVICT_CODE_E4M3 = 1 };
+typedef struct {
+  uint32_t struct_size;      /* sizeof(qevict_kv8_cache) */
+  int32_t device;
+  int32_t dtype;             /* QEVICT_DTYPE_* of q, k, v, out and the tail rows */
+  int32_t code;              /* QEVICT_CODE_* */
+  int32_t n_seqs;
+  int32_t n_kv_heads;
+  int32_t head_dim;          /* 64 or 128 */
+  int32_t block;             /* 16, 32, 64 or 128 tokens */
+  int32_t max_blocks;        /* columns of block_table */
+  int32_t n_pages;
+  void* k_codes;             /* device [n_pages, n_kv_heads, block, d] of 1 byte */
+  void* v_codes;
+  float* k_scale;            /* device [n_pages, n_kv_heads] */
+  float* v_scale;
+  void* k_tail;              /* device [n_seqs, n_kv_heads, block, d] of dtype */
+  void* v_tail;
+  const int32_t* block_table; /* device [n_seqs, max_blocks] */
+  int32_t* status;           /* device int32 or NULL */
+} qevict_kv8_cache;
+
+/* Appends tokens: token i of sequence s is row cu_new[s] + i of k, v [total_new, n_kv_heads, d] (strides in elements,
+ * multiples of 16 bytes) and becomes token start[s] + i.  cu_new: device int32 [n_seqs + 1], or NULL for one token per
+ * sequence (row s).  max_new bounds the tokens of one sequence (later ones are dropped).  A sequence with start < 0 is
+ * left as it is.  Pages must be in the table for every block the call fills.  The lengths stay the caller's. */
+QEVICT_API qevict_status qevict_kv8_append(const qevict_kv8_cache* cache, const void* k, const void* v, int64_t token_stride,
+                                           int64_t head_stride, int64_t total_new, const int32_t* start,
+                                           const int32_t* cu_new, int32_t max_new, void* stream);
+
+/* Attention of one token per sequence over the cache (the tokens appended so far, lens[s] of them): q, out [n_seqs,
+ * n_q_heads, d] (device, contiguous), lse [n_seqs, n_q_heads] float32 or NULL.  n_q_heads / n_kv_heads <= 16.
+ * score_out [n_seqs, max_blocks] float32 or NULL: score_in (NULL: 0; may be score_out itself) plus the probability mass
+ * that the block's tokens received, summed over the query heads [Eq. 1], in a fixed order.  Blocks past the length get
+ * score_in.  scratch: device, from qevict_kv8_attn_scratch_bytes for the same arguments; calls that may run at the
+ * same time need scratch of their own.  scale 0 => 1/sqrt(d). */
+QEVICT_API qevict_status qevict_kv8_attn_scratch_bytes(const qevict_kv8_cache* cache, int32_t n_q_heads, int32_t max_len,
+                                                       int32_t with_scores, uint64_t* bytes);
+QEVICT_API qevict_status qevict_kv8_attn(const qevict_kv8_cache* cache, int32_t n_q_heads, float softmax_scale, const void* q,
+                                         const int32_t* lens, int32_t max_len, void* out, float* lse, const float* score_in,
+                                         float* score_out, void* scratch, uint64_t scratch_bytes, void* stream);
+
+/* One-way eviction by accumulated mass: a sequence with more than `budget` full blocks keeps the first `sink`, the
+ * last `recent` and the best of the others by score (higher score first, then the lower block; a score that is not a
+ * number ranks last), `budget` in all; its open block always stays.  Codes do not move: the kept entries of the table
+ * and the scores close up in their order, entries after the full blocks follow them, and the rest is -1 / 0.
+ *   table, scores: device [n_seqs, max_blocks]; lens: device [n_seqs] (in tokens; < 0: left as it is)
+ *   table_out, scores_out, lens_out: the same shapes; each may be its input
+ *   kept [n_seqs, max_blocks]: block index before the call of every entry of table_out, -1 behind; or NULL
+ *   freed [n_seqs, max_blocks], n_freed [n_seqs]: pages of the evicted blocks in their order, -1 behind; ids outside
+ *   0 .. n_pages - 1 are not listed; or NULL
+ * sink + recent <= budget; max_blocks <= 16384. */
+typedef struct {
+  uint32_t struct_size;      /* sizeof(qevict_kv8_evict_args) */
+  int32_t device;
+  int32_t n_seqs, max_blocks, block, n_pages;
+  int32_t budget, sink, recent;
+  const int32_t* table;
+  const int32_t* lens;
+  const float* scores;
+  int32_t* table_out;
+  int32_t* lens_out;
+  float* scores_out;
+  int32_t* kept;
+  int32_t* freed;
+  int32_t* n_freed;
+} qevict_kv8_evict_args;
+QEVICT_API qevict_status qevict_kv8_evict(const qevict_kv8_evict_args* args, void* stream);
+
 /* Tuning: force the number of KV splits per (unit, KV head) of the decode kernel (1..64); 0 restores
  * the built-in choice, which fills the GPU in whole waves.  Results do not depend on it beyond
  * floating-point summation order. */
@@ -401,7 +534,7 @@ QEVICT_API qevict_status qevict_kernel_timeline(qevict_handle h, int32_t max_rec
 QEVICT_API uint64_t qevict_launch_count(qevict_handle h);
 
 /* Text of the last error on this handle (never NULL).  With h == NULL: the calling thread's last failure of
- * qevict_create or qevict_workspace_bytes. */
+ * qevict_create, qevict_workspace_bytes or one of the calls without a handle (qevict_prompt_*, qevict_kv8_*). */
 QEVICT_API const char* qevict_last_error(qevict_handle h);
 QEVICT_API const char* qevict_status_string(qevict_status s);
 /* Library version, "major.minor". */

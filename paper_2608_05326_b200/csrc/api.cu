@@ -27,8 +27,8 @@ int next_pow2(int x) {
 
 namespace {
 
-// Text of the last failure of a call that has no handle to keep it in (qevict_create, qevict_workspace_bytes),
-// per calling thread; qevict_last_error(NULL) returns it.
+// Text of the last failure of a call that has no handle to keep it in (qevict_create, qevict_workspace_bytes, the
+// prompt attention and the 8-bit cache), per calling thread; qevict_last_error(NULL) returns it.
 thread_local std::string t_create_error;
 
 qevict_status fail(qevict_handle h, qevict_status s, const std::string& msg) {
@@ -36,6 +36,22 @@ qevict_status fail(qevict_handle h, qevict_status s, const std::string& msg) {
   else t_create_error = msg;
   return s;
 }
+
+}  // namespace
+
+namespace qevict {
+
+qevict_status stateless_fail(qevict_status s, const char* msg) noexcept {
+  try {
+    t_create_error = msg;
+  } catch (...) {  // no memory for the text: the status still says what happened
+  }
+  return s;
+}
+
+}  // namespace qevict
+
+namespace {
 
 // Brackets one kernel launch with events when instrumentation is on.
 template <class F>

@@ -28,6 +28,9 @@ enum : int {
   CHECK_BOUNDS_PAGE = 7,     // page id in a window table or a list
   CHECK_BOUNDS_WINDOW = 8,   // window index
   CHECK_BOUNDS_RECORD = 9,   // migration record
+  // calls on caller-owned tables (always checked)
+  CHECK_PAGE_ID = 10,        // page id outside the pool (other than -1) where a block is needed
+  CHECK_LENGTH = 11,         // length beyond the table or the call's bound
 };
 
 static constexpr int TILE_TOKENS = 32;    // tokens per attention tile

@@ -70,6 +70,9 @@ struct qevict_ctx {
 
 namespace qevict {
 
+// Records the text of a failed call that has no handle (for qevict_last_error(NULL) on this thread); returns `s`.
+qevict_status stateless_fail(qevict_status s, const char* msg) noexcept;
+
 // Splits per (unit, KV head) of the attention kernel for a call over `n_units` units.
 int choose_splits(const qevict_ctx* h, int n_units);
 // Argument and call-order checks of a decode step over layers [l0, l1); nullptr if the step may run (nothing is

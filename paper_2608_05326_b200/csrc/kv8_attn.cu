@@ -1,0 +1,751 @@
+// Attention of one token per sequence over the 8-bit block-scaled cache.
+//
+//     x_i = scale * q . (s_b c_i) * log2 e,  out = sum_i 2^(x_i - M) s'_b c'_i / L,  L = sum_i 2^(x_i - M)
+//     mass_b = sum_heads sum_{i in b} 2^(x_i - M) / L
+// The codes are read once (one byte per element, keys and values); everything else is small, so HBM bounds the call.
+//
+// Work.  The cache of a call is a sequence of units of UT tokens (32, or 16 where a block has 16), ordered by
+// (sequence, KV head, token).  Every warp of the grid takes one contiguous run of them, equal to within one unit, so
+// ragged lengths balance without a plan on the host: each CTA sums the lengths itself.  A warp's part of a
+// (sequence, KV head) is one partial result; run w's part of row r is slot w + r of the scratch (both only grow along
+// the order, so slots are distinct), and kv8_combine_kernel finds a row's slots from the same arithmetic.
+//
+// Tile.  Both products put the cache on the A side of mma.m16n8k16 (tokens, then channels on M; the G heads that
+// share the KV head on N).  Codes become fp16 in registers -- every int8 and e4m3 code is exact there -- and the
+// block's scale multiplies the logits / the block's output in float32.  The contraction index may be permuted as long
+// as both sides agree, so a lane takes whole 4-byte words of its key row, and the token pairs of the values come out
+// of byte permutes.  The query goes to fp16 after a division by a power of two per head, which brings its largest
+// element into [1, 2): exact but for elements 2^-14 below the largest, which lose at most 2^-25 of it.
+// Probabilities enter the second product as fp16 (2^-11); the sums of the softmax, the block masses and the output
+// are float32.
+#include <cuda.h>
+
+#include "kv8.cuh"
+
+namespace qevict {
+
+namespace {
+
+constexpr int WARPS = 4;                  // warps per CTA
+constexpr int ATTN_THREADS = WARPS * 32;
+constexpr int STAGES = 4;                 // units of 16 tokens, or pairs of 16 for UT = 32, in a warp's ring
+constexpr float LAZY = 8.f;               // the reference exponent moves only when a logit exceeds it by this (log2)
+
+struct Kv8AttnArgs {
+  Kv8View c;
+  int Hq, G;
+  float scale_log2;
+  const void* q;
+  const int32_t* lens;
+  int max_len;     // already cut to max_blocks * block
+  int n_warps;     // warps of the attention grid
+  int max_units;   // units of a sequence of max_len tokens
+  void* out;
+  float* lse;
+  const float* score_in;
+  float* score_out;
+  float* part_o;   // [slot][G][D]
+  float2* part_ml; // [slot][G] {reference, sum}
+  float2* rec;     // [seq][max_units][Hq] {reference, sum} of every unit, or nullptr
+  float2* stats;   // [seq][Hq] {M, 1 / L}
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
+}
+
+// Bytes {x, y} of the low (HI = 0) or high half of a word of two code pairs -> two fp16 values.
+template <int CODE, bool HI> __device__ __forceinline__ uint32_t codes_to_h2(uint32_t w) {
+  uint32_t r;
+  if (CODE == QEVICT_CODE_INT8) {
+    // w holds code + 128: 1024 + (code + 128) is an fp16 number with the byte in its low bits
+    const uint32_t m = __byte_perm(w, 0x64646464u, HI ? 0x4342 : 0x4140);
+    return as_u32(__hsub2(as_t2<__half2>(m), as_t2<__half2>(0x64806480u)));
+  }
+  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, %2;\n\t}\n"
+      : "=r"(r) : "r"(w), "h"((uint16_t)(HI ? w >> 16 : w & 0xffffu)));
+  return r;
+}
+template <int CODE> __device__ __forceinline__ uint32_t bias(uint32_t w) {
+  return CODE == QEVICT_CODE_INT8 ? w ^ 0x80808080u : w;
+}
+
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(y) : "r"(x));
+  return y;
+}
+
+// Tokens of a sequence that the call sees: a length beyond the bound is cut to the whole blocks within it (a partial
+// one would be in the tail, and the tail holds later tokens).
+__device__ __forceinline__ int clamp_len(const Kv8AttnArgs& a, int len) {
+  return len <= a.max_len ? max(0, len) : a.max_len / a.c.block * a.c.block;
+}
+
+// Prefix sums of the sequences' units per KV head, in shared memory.
+__device__ void unit_prefix(const Kv8AttnArgs& a, int ut, int* pre, int* s_w) {
+  const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, wid = tid >> 5;
+  int base = 0;
+  for (int s0 = 0; s0 < a.c.n_seqs; s0 += nt) {
+    const int s = s0 + tid;
+    int x = s < a.c.n_seqs ? (clamp_len(a, a.lens[s]) + ut - 1) / ut : 0;
+    int v = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += y;
+    }
+    if (lane == 31) s_w[wid] = v;
+    __syncthreads();
+    int before = base, all = base;
+    for (int i = 0; i < (nt >> 5); ++i) {
+      if (i < wid) before += s_w[i];
+      all += s_w[i];
+    }
+    if (s < a.c.n_seqs) pre[s] = before + v - x;
+    base = all;
+    __syncthreads();
+  }
+  if (tid == 0) pre[a.c.n_seqs] = base;
+  __syncthreads();
+}
+
+// First unit of run w of n over `total` units; the run that holds unit u.  There are never more runs than units, so
+// that no run is empty and every slot between a row's first and last is written.
+__device__ __forceinline__ int runs_of(long long total, int n_warps) { return (int)min((long long)n_warps, total); }
+__device__ __forceinline__ long long run_start(long long total, int n, int w) { return total * w / n; }
+__device__ __forceinline__ int run_of(long long total, int n, long long u) { return (int)(((u + 1) * n - 1) / total); }
+
+// sequence of unit u: the last s with pre[s] * Hkv <= u and units of its own
+__device__ __forceinline__ int seq_of(const int* pre, int n_seqs, int u_per_head) {
+  int lo = 0, hi = n_seqs - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (pre[mid] <= u_per_head) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+// Shared-memory byte offset of 16-byte chunk `c` of token row `r` of a tile, so that the 8 lanes of a load phase
+// fall into different banks (rows of 128 bytes: chunk ^ row; rows of 64 bytes: two rows share a 128-byte line).
+template <int D> __device__ __forceinline__ uint32_t swz(int r, int c) {
+  if (D == 128) return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4));
+  const int line = r >> 1, c8 = ((r & 1) << 2) | c;
+  return (uint32_t)(line * 128 + ((c8 ^ ((line & 3) << 1)) << 4));
+}
+
+// One warp's running state for one (sequence, KV head).
+template <int D, int NT> struct Acc {
+  float o[NT][D / 16][4];  // output, channels x heads
+  float m[NT][2], l[NT][2];  // reference (log2), lane's share of the sum; heads 2 t, 2 t + 1 of head tile nt
+};
+
+template <class T, int CODE, int D, int NT, int UT>
+__global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel(const Kv8AttnArgs a) {
+  constexpr int KS = D / 16, MT = UT / 16, STAGE = 2 * UT * D, RING = STAGES * 16 / UT;
+  extern __shared__ __align__(128) unsigned char sm[];
+  const Kv8View& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
+  int* pre = reinterpret_cast<int*>(sm + WARPS * RING * STAGE);
+  __shared__ int s_w[WARPS];
+  pdl_prologue();
+  unit_prefix(a, UT, pre, s_w);
+  const long long total = (long long)pre[c.n_seqs] * c.Hkv;
+  if (total == 0) return;
+  const int w = blockIdx.x * WARPS + wid, n_runs = runs_of(total, a.n_warps);
+  if (w >= n_runs) return;
+  long long u = run_start(total, n_runs, w);
+  const long long u_end = run_start(total, n_runs, w + 1);
+  unsigned char* ring = sm + wid * RING * STAGE;
+  const uint32_t ring_a = (uint32_t)__cvta_generic_to_shared(ring);
+  const int upb = c.block / UT;  // units per block
+
+  while (u < u_end) {
+    const int s = seq_of(pre, c.n_seqs, (int)(u / c.Hkv));
+    const int nu = pre[s + 1] - pre[s];
+    const long long in_seq = u - (long long)pre[s] * c.Hkv;
+    const int h = (int)(in_seq / nu);
+    const int i0 = (int)(in_seq - (long long)h * nu), i1 = (int)min((long long)nu, i0 + (u_end - u));
+    const int row = s * c.Hkv + h;
+    const int len = clamp_len(a, a.lens[s]);
+    const int n_code = len / c.block * upb;  // units that lie in full blocks
+    u += i1 - i0;
+
+    // queries of this KV head: B fragments in fp16, divided by a power of two per head
+    uint32_t qf[NT][KS][2];
+    float qs[NT][2];  // of heads 2 t, 2 t + 1: that power of two times the softmax scale
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int hl = nt * 8 + g;
+      float x[KS][4], mx = 0.f;
+      const T* qp = static_cast<const T*>(a.q) + ((size_t)s * a.Hq + h * a.G + hl) * D + t * (D / 4);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[ks][j] = hl < a.G ? Tr<T>::to_float(qp[ks * 4 + j]) : 0.f;
+          mx = fmaxf(mx, fabsf(x[ks][j]));
+        }
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      // 2^-e with e the exponent of the largest element (kept where both it and its inverse are normal)
+      const int e = min(max((int)(__float_as_uint(mx) >> 23), 2), 252);
+      const float down = __uint_as_float((uint32_t)(254 - e) << 23), up = __uint_as_float((uint32_t)e << 23);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        qf[nt][ks][0] = as_u32(__floats2half2_rn(x[ks][0] * down, x[ks][1] * down));
+        qf[nt][ks][1] = as_u32(__floats2half2_rn(x[ks][2] * down, x[ks][3] * down));
+      }
+      qs[nt][0] = __shfl_sync(0xffffffffu, up, 8 * t) * a.scale_log2;
+      qs[nt][1] = __shfl_sync(0xffffffffu, up, 8 * t + 4) * a.scale_log2;
+    }
+
+    Acc<D, NT> acc;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      acc.m[nt][0] = acc.m[nt][1] = -INFINITY;
+      acc.l[nt][0] = acc.l[nt][1] = 0.f;
+#pragma unroll
+      for (int mt = 0; mt < KS; ++mt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc.o[nt][mt][j] = 0.f;
+    }
+
+    // Softmax of one unit's logits x (log2 domain, -inf where masked): moves the reference if it must, turns x into
+    // probabilities, adds the sums, writes the unit's record.
+    auto softmax = [&](float (&x)[NT][MT][4], int unit) {
+      bool over = false;
+      float mx[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float v = -INFINITY;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) v = fmaxf(v, fmaxf(x[nt][mt][j], x[nt][mt][j + 2]));
+          mx[nt][j] = v;
+          over |= v > acc.m[nt][j] + LAZY;  // -inf + LAZY = -inf: the first finite logit counts
+        }
+      if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            float v = mx[nt][j];
+            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+            const float old = acc.m[nt][j], m = fmaxf(old, v);
+            const float f = m == old ? 1.f : ex2(old - m);
+            acc.m[nt][j] = m;
+            acc.l[nt][j] *= f;
+#pragma unroll
+            for (int mt = 0; mt < KS; ++mt) {
+              acc.o[nt][mt][j] *= f;
+              acc.o[nt][mt][j + 2] *= f;
+            }
+          }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float m = acc.m[nt][j] == -INFINITY ? 0.f : acc.m[nt][j];
+          float sum = 0.f;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            x[nt][mt][j] = ex2(x[nt][mt][j] - m);
+            x[nt][mt][j + 2] = ex2(x[nt][mt][j + 2] - m);
+            sum += x[nt][mt][j] + x[nt][mt][j + 2];
+          }
+          acc.l[nt][j] += sum;
+          if (a.rec) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+            const int hl = nt * 8 + 2 * t + j;
+            if (g == 0 && hl < a.G) a.rec[((size_t)s * a.max_units + unit) * a.Hq + h * a.G + hl] = make_float2(acc.m[nt][j], sum);
+          }
+        }
+    };
+
+    // ---- units in full blocks: ring of asynchronous copies -----------------------------------------------------
+    const int e1 = min(i1, n_code);
+    if (i0 < e1) {
+      // page and scales of 32 blocks at a time, one per lane; the copies run RING - 1 units ahead
+      auto fetch = [&](int blk0, int& page) {
+        page = -1;
+        const int b = blk0 + lane;
+        if (b < n_code / upb) {
+          page = c.table[(size_t)s * c.max_blocks + b];
+          if (page < 0 || page >= c.n_pages) {
+            if (page != -1) kv8_record(c.status, CHECK_PAGE_ID);
+            page = -1;
+          }
+        }
+      };
+      int f_blk0 = i0 / upb, f_page;  // producer's window of 32 blocks
+      fetch(f_blk0, f_page);
+      auto issue = [&](int i) {
+        if (i < e1) {
+          const int b = i / upb;
+          if (b >= f_blk0 + 32) {
+            f_blk0 += 32;
+            fetch(f_blk0, f_page);
+          }
+          const int page = __shfl_sync(0xffffffffu, f_page, b - f_blk0);
+          if (page >= 0) {
+            const size_t off = (((size_t)page * c.Hkv + h) * c.block + (size_t)(i - b * upb) * UT) * D;
+            const uint32_t dst = ring_a + (uint32_t)(i % RING) * STAGE;
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+              for (int n = 0; n < UT * D / 512; ++n) {
+                const int ch = n * 32 + lane, r = ch / (D / 16), cc = ch - r * (D / 16);
+                cp16(dst + kv * UT * D + swz<D>(r, cc), c.codes[kv] + off + ch * 16);
+              }
+          }
+        }
+        asm volatile("cp.async.commit_group;\n" ::: "memory");
+      };
+      for (int i = i0; i < i0 + RING - 1; ++i) issue(i);
+      int s_blk0 = i0 / upb - 32, s_page = -1;
+      float s_k = 0.f, s_v = 0.f;
+      for (int i = i0; i < e1; ++i) {
+        const int b = i / upb;
+        if (b >= s_blk0 + 32) {  // consumer's window: scales too
+          s_blk0 = s_blk0 + 32 > b ? s_blk0 + 32 : b;
+          fetch(s_blk0, s_page);
+          s_k = s_page >= 0 ? c.scale[0][(size_t)s_page * c.Hkv + h] : 0.f;
+          s_v = s_page >= 0 ? c.scale[1][(size_t)s_page * c.Hkv + h] : 0.f;
+        }
+        asm volatile("cp.async.wait_group %0;\n" ::"n"(RING - 2) : "memory");
+        __syncwarp();
+        const int page = __shfl_sync(0xffffffffu, s_page, b - s_blk0);
+        const float ksc = __shfl_sync(0xffffffffu, s_k, b - s_blk0), vsc = __shfl_sync(0xffffffffu, s_v, b - s_blk0);
+        const unsigned char* kt = ring + (i % RING) * STAGE;
+        const unsigned char* vt = kt + UT * D;
+        if (page < 0) {  // absent block: nothing was copied
+          if (a.rec)
+            for (int hl = lane; hl < a.G; hl += 32) a.rec[((size_t)s * a.max_units + i) * a.Hq + h * a.G + hl] = make_float2(-INFINITY, 0.f);
+        } else {
+          float x[NT][MT][4];
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            uint32_t k0[KS], k1[KS];  // this lane's words of token rows g and g + 8: channels t D/4 ..
+#pragma unroll
+            for (int v = 0; v < D / 64; ++v) {
+              const uint4 p = *reinterpret_cast<const uint4*>(kt + swz<D>(mt * 16 + g, t * (D / 64) + v));
+              const uint4 r = *reinterpret_cast<const uint4*>(kt + swz<D>(mt * 16 + g + 8, t * (D / 64) + v));
+              k0[v * 4] = p.x; k0[v * 4 + 1] = p.y; k0[v * 4 + 2] = p.z; k0[v * 4 + 3] = p.w;
+              k1[v * 4] = r.x; k1[v * 4 + 1] = r.y; k1[v * 4 + 2] = r.z; k1[v * 4 + 3] = r.w;
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) x[nt][mt][j] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+              const uint32_t w0 = bias<CODE>(k0[ks]), w1 = bias<CODE>(k1[ks]);
+              const uint32_t a0 = codes_to_h2<CODE, false>(w0), a2 = codes_to_h2<CODE, true>(w0);
+              const uint32_t a1 = codes_to_h2<CODE, false>(w1), a3 = codes_to_h2<CODE, true>(w1);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) mma16816<__half>(x[nt][mt], a0, a1, a2, a3, qf[nt][ks][0], qf[nt][ks][1]);
+            }
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const float f = qs[nt][j] * ksc;
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) {
+                x[nt][mt][j] *= f;
+                x[nt][mt][j + 2] *= f;
+              }
+            }
+          softmax(x, i);
+          float o[NT][KS][4];  // this unit's output before the block's scale
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int mt = 0; mt < KS; ++mt)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) o[nt][mt][j] = 0.f;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            uint32_t p0[NT], p1[NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              p0[nt] = transpose8(as_u32(__floats2half2_rn(x[nt][mt][0], x[nt][mt][1])));
+              p1[nt] = transpose8(as_u32(__floats2half2_rn(x[nt][mt][2], x[nt][mt][3])));
+            }
+            // this lane's tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9, channels g D/8 ..
+            uint32_t v[4][D / 32];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+              const int r = mt * 16 + 2 * t + (n & 1) + (n >> 1) * 8;
+              if (D == 128) {
+                const uint4 p = *reinterpret_cast<const uint4*>(vt + swz<D>(r, g));
+                v[n][0] = p.x; v[n][1] = p.y; v[n][2 % (D / 32)] = p.z; v[n][3 % (D / 32)] = p.w;
+              } else {
+                const uint2 p = *reinterpret_cast<const uint2*>(vt + swz<D>(r, g >> 1) + (g & 1) * 8);
+                v[n][0] = p.x; v[n][1] = p.y;
+              }
+            }
+#pragma unroll
+            for (int q4 = 0; q4 < D / 32; ++q4) {
+              const uint32_t wa = bias<CODE>(v[0][q4]), wb = bias<CODE>(v[1][q4]), wc = bias<CODE>(v[2][q4]), wd = bias<CODE>(v[3][q4]);
+#pragma unroll
+              for (int half = 0; half < 2; ++half) {
+                const uint32_t ab = __byte_perm(wa, wb, half ? 0x7362 : 0x5140), cd = __byte_perm(wc, wd, half ? 0x7362 : 0x5140);
+                const uint32_t a0 = codes_to_h2<CODE, false>(ab), a1 = codes_to_h2<CODE, true>(ab);
+                const uint32_t a2 = codes_to_h2<CODE, false>(cd), a3 = codes_to_h2<CODE, true>(cd);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma16816<__half>(o[nt][q4 * 2 + half], a0, a1, a2, a3, p0[nt], p1[nt]);
+              }
+            }
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int mt = 0; mt < KS; ++mt)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) acc.o[nt][mt][j] = fmaf(o[nt][mt][j], vsc, acc.o[nt][mt][j]);
+        }
+        __syncwarp();  // every lane has read the slot that the next copy fills
+        issue(i + RING - 1);
+      }
+      asm volatile("cp.async.wait_group 0;\n" ::: "memory");
+      __syncwarp();
+    }
+
+    // ---- units of the open block: 16-bit rows -----------------------------------------------------------------
+    for (int i = max(i0, n_code); i < i1; ++i) {
+      const int r0 = (i - n_code) * UT, rows = len - n_code * UT - r0;  // valid tokens from r0 on
+      const T* kp = static_cast<const T*>(c.tail[0]) + ((size_t)row * c.block + r0) * D;
+      const T* vp = static_cast<const T*>(c.tail[1]) + ((size_t)row * c.block + r0) * D;
+      float x[NT][MT][4];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[nt][mt][j] = 0.f;
+#pragma unroll 2
+      for (int ks = 0; ks < KS; ++ks) {
+        uint2 qv[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const int hl = nt * 8 + g;
+          qv[nt] = hl < a.G ? *reinterpret_cast<const uint2*>(static_cast<const T*>(a.q) + ((size_t)s * a.Hq + h * a.G + hl) * D + t * (D / 4) + ks * 4)
+                            : make_uint2(0u, 0u);
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          uint2 ka = make_uint2(0u, 0u), kb = ka;
+          const int ra = mt * 16 + g, rb = ra + 8;
+          if (ra < rows) ka = *reinterpret_cast<const uint2*>(kp + (size_t)ra * D + t * (D / 4) + ks * 4);
+          if (rb < rows) kb = *reinterpret_cast<const uint2*>(kp + (size_t)rb * D + t * (D / 4) + ks * 4);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) mma16816<T>(x[nt][mt], ka.x, kb.x, ka.y, kb.y, qv[nt].x, qv[nt].y);
+        }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            x[nt][mt][j] = mt * 16 + g + (j >> 1) * 8 < rows ? x[nt][mt][j] * a.scale_log2 : -INFINITY;
+      softmax(x, i);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        // probabilities in T, and (bf16) what the rounding left, so that the open block is as exact as the others
+        uint32_t p0[NT], p1[NT], d0[NT], d1[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          T hi[4], lo[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            hi[j] = Tr<T>::from_float(x[nt][mt][j]);
+            lo[j] = Tr<T>::from_float(x[nt][mt][j] - Tr<T>::to_float(hi[j]));
+          }
+          p0[nt] = transpose8(*reinterpret_cast<uint32_t*>(&hi[0]));
+          p1[nt] = transpose8(*reinterpret_cast<uint32_t*>(&hi[2]));
+          d0[nt] = transpose8(*reinterpret_cast<uint32_t*>(&lo[0]));
+          d1[nt] = transpose8(*reinterpret_cast<uint32_t*>(&lo[2]));
+        }
+#pragma unroll 2
+        for (int o2 = 0; o2 < KS; ++o2) {  // channels g D/8 + 2 o2, + 1
+          uint32_t v[4];
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            const int r = mt * 16 + 2 * t + (n & 1) + (n >> 1) * 8;
+            v[n] = r < rows ? *reinterpret_cast<const uint32_t*>(vp + (size_t)r * D + g * (D / 8) + 2 * o2) : 0u;
+          }
+          const uint32_t a0 = __byte_perm(v[0], v[1], 0x5410), a1 = __byte_perm(v[0], v[1], 0x7632);
+          const uint32_t a2 = __byte_perm(v[2], v[3], 0x5410), a3 = __byte_perm(v[2], v[3], 0x7632);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int z = 0; z < KS; ++z)
+              if (z == o2) {  // keeps the accumulators in registers under the partial unroll
+                mma16816<T>(acc.o[nt][z], a0, a1, a2, a3, p0[nt], p1[nt]);
+                mma16816<T>(acc.o[nt][z], a0, a1, a2, a3, d0[nt], d1[nt]);
+              }
+          }
+        }
+      }
+    }
+
+    // ---- partial result of this run's part of the row -----------------------------------------------------------
+    const size_t slot = (size_t)w + row;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float l = acc.l[nt][j];
+        l += __shfl_xor_sync(0xffffffffu, l, 4);
+        l += __shfl_xor_sync(0xffffffffu, l, 8);
+        l += __shfl_xor_sync(0xffffffffu, l, 16);
+        const int hl = nt * 8 + 2 * t + j;
+        if (hl < a.G) {
+          if (g == 0) a.part_ml[slot * a.G + hl] = make_float2(acc.m[nt][j], l);
+          float4* dst = reinterpret_cast<float4*>(a.part_o + (slot * a.G + hl) * D + g * (D / 8));
+#pragma unroll
+          for (int mt = 0; mt < KS; mt += 2)
+            dst[mt >> 1] = make_float4(acc.o[nt][mt][j], acc.o[nt][mt][j + 2], acc.o[nt][mt + 1][j], acc.o[nt][mt + 1][j + 2]);
+        }
+      }
+  }
+}
+
+// Merges a row's partial results: one CTA per (query head, sequence).
+constexpr int COMB_THREADS = 256;
+template <class T>
+__global__ void __launch_bounds__(COMB_THREADS) kv8_combine_kernel(const Kv8AttnArgs a, int ut) {
+  extern __shared__ int pre[];
+  __shared__ int s_w[COMB_THREADS / 32];
+  __shared__ float s_red[COMB_THREADS / 32], s_o[COMB_THREADS / 32][128];
+  const int s = blockIdx.y, hq = blockIdx.x, h = hq / a.G, hl = hq - h * a.G, D = a.c.D;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, nw = COMB_THREADS / 32;
+  pdl_prologue();
+  unit_prefix(a, ut, pre, s_w);
+  const long long total = (long long)pre[a.c.n_seqs] * a.c.Hkv;
+  const int nu = pre[s + 1] - pre[s], row = s * a.c.Hkv + h;
+  T* out = static_cast<T*>(a.out) + ((size_t)s * a.Hq + hq) * D;
+  if (tid == 0 && a.c.status && hq == 0 && a.lens[s] > a.max_len) kv8_record(a.c.status, CHECK_LENGTH);
+  if (nu == 0) {
+    for (int i = tid; i < D; i += COMB_THREADS) out[i] = Tr<T>::from_float(0.f);
+    if (tid == 0) {
+      if (a.lse) a.lse[(size_t)s * a.Hq + hq] = -INFINITY;
+      a.stats[(size_t)s * a.Hq + hq] = make_float2(0.f, 0.f);
+    }
+    return;
+  }
+  const long long u0 = (long long)pre[s] * a.c.Hkv + (long long)h * nu;
+  const int n_runs = runs_of(total, a.n_warps);
+  const int w0 = run_of(total, n_runs, u0), n = run_of(total, n_runs, u0 + nu - 1) - w0 + 1;
+  const size_t slot0 = (size_t)w0 + row;
+  float M = -INFINITY;
+  for (int i = tid; i < n; i += COMB_THREADS) M = fmaxf(M, a.part_ml[(slot0 + i) * a.G + hl].x);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  if (lane == 0) s_red[wid] = M;
+  __syncthreads();
+  for (int i = 0; i < nw; ++i) M = fmaxf(M, s_red[i]);
+  const float Ms = M == -INFINITY ? 0.f : M;
+  __syncthreads();
+  // warp `wid` takes partials wid, wid + 8, ...; lanes hold 4 channels each (d = 64: half the lanes twice as many rows)
+  const int per = D / 4, sub = lane / per, subs = 32 / per, c4 = lane - sub * per;
+  float l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int i = wid * subs + sub; i < n; i += nw * subs) {
+    const float2 ml = a.part_ml[(slot0 + i) * a.G + hl];
+    const float4 v = *reinterpret_cast<const float4*>(a.part_o + ((slot0 + i) * a.G + hl) * D + c4 * 4);
+    const float f = ex2(ml.x - Ms);
+    l += ml.y * f;
+    o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
+  }
+  if (subs == 2) {
+    l += __shfl_xor_sync(0xffffffffu, l, 16);
+    o.x += __shfl_xor_sync(0xffffffffu, o.x, 16);
+    o.y += __shfl_xor_sync(0xffffffffu, o.y, 16);
+    o.z += __shfl_xor_sync(0xffffffffu, o.z, 16);
+    o.w += __shfl_xor_sync(0xffffffffu, o.w, 16);
+  }
+  if (lane == 0) s_red[wid] = l;
+  if (sub == 0) *reinterpret_cast<float4*>(&s_o[wid][c4 * 4]) = o;
+  __syncthreads();
+  if (tid < D) {
+    float L = 0.f, v = 0.f;
+    for (int i = 0; i < nw; ++i) {
+      L += s_red[i];
+      v += s_o[i][tid];
+    }
+    out[tid] = Tr<T>::from_float(L > 0.f ? v / L : (L == 0.f ? 0.f : v));
+    if (tid == 0) {
+      if (a.lse) a.lse[(size_t)s * a.Hq + hq] = L == 0.f ? -INFINITY : (Ms + log2f(L)) * 0.6931471805599453f;
+      a.stats[(size_t)s * a.Hq + hq] = make_float2(Ms, L == 0.f ? 0.f : 1.f / L);
+    }
+  }
+}
+
+// Block masses: one warp per (block, sequence); lanes stride over the query heads, fixed shuffle tree.
+constexpr int MASS_THREADS = 256;
+__global__ void __launch_bounds__(MASS_THREADS) kv8_mass_kernel(const Kv8AttnArgs a, int ut) {
+  const int s = blockIdx.y, lane = threadIdx.x & 31, b = blockIdx.x * (MASS_THREADS / 32) + (threadIdx.x >> 5);
+  pdl_prologue();
+  if (b >= a.c.max_blocks) return;
+  const int len = clamp_len(a, a.lens[s]), upb = a.c.block / ut;
+  const int nu = (len + ut - 1) / ut;
+  const size_t at = (size_t)s * a.c.max_blocks + b;
+  float mass = 0.f;
+  for (int i = b * upb; i < min(nu, (b + 1) * upb); ++i)
+    for (int h = lane; h < a.Hq; h += 32) {
+      const float2 r = a.rec[((size_t)s * a.max_units + i) * a.Hq + h], st = a.stats[(size_t)s * a.Hq + h];
+      mass += r.y * ex2(r.x - st.x) * st.y;
+    }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
+  if (lane == 0) a.score_out[at] = (a.score_in ? a.score_in[at] : 0.f) + mass;
+}
+
+struct Plan {
+  int ut, n_warps, max_units, max_len;
+  size_t off_ml, off_rec, off_stats, bytes;
+};
+
+int sm_count(int device) {
+  int n = 0;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || n < 1) {
+    (void)cudaGetLastError();
+    n = SM_COUNT_FALLBACK;
+  }
+  return n;
+}
+
+const char* plan_of(const Kv8View& c, int Hq, int max_len, bool scores, int sms, qevict_status* st, Plan* p) {
+  *st = QEVICT_ERR_INVALID_ARG;
+  if (Hq < 1 || Hq % c.Hkv) return "n_q_heads must be a multiple of n_kv_heads";
+  if (max_len < 0) return "max_len must be >= 0";
+  *st = QEVICT_ERR_UNSUPPORTED;
+  if (Hq / c.Hkv > 16) return "more than 16 query heads per KV head";
+  const long long cap = (long long)c.max_blocks * c.block;
+  p->max_len = (int)(max_len < cap ? max_len : cap);
+  p->ut = c.block >= 32 ? 32 : 16;
+  p->max_units = (p->max_len + p->ut - 1) / p->ut;
+  if ((long long)c.n_seqs * p->max_units > 0x7fffffffll) return "n_seqs * max_len is too large for one call";
+  const int G = Hq / c.Hkv;
+  const int ctas_per_sm = G <= 8 ? 3 : 2;
+  const long long units = (long long)c.n_seqs * c.Hkv * p->max_units;
+  long long ctas = (units + WARPS - 1) / WARPS;
+  if (ctas > (long long)sms * ctas_per_sm) ctas = (long long)sms * ctas_per_sm;
+  if (ctas < 1) ctas = 1;
+  p->n_warps = (int)ctas * WARPS;
+  const size_t slots = (size_t)p->n_warps + (size_t)c.n_seqs * c.Hkv;
+  auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  p->off_ml = up(slots * G * c.D * sizeof(float));
+  p->off_stats = p->off_ml + up(slots * G * sizeof(float2));
+  p->off_rec = p->off_stats + up((size_t)c.n_seqs * Hq * sizeof(float2));
+  p->bytes = p->off_rec + (scores ? up((size_t)c.n_seqs * p->max_units * Hq * sizeof(float2)) : 0);
+  return nullptr;
+}
+
+template <class T, int CODE, int D, int NT, int UT> cudaError_t launch_attn(const Kv8AttnArgs& a, cudaStream_t s) {
+  constexpr int RING = STAGES * 16 / UT;
+  const size_t smem = (size_t)WARPS * RING * 2 * UT * D + (size_t)(a.c.n_seqs + 1) * sizeof(int);
+  auto kernel = kv8_attn_kernel<T, CODE, D, NT, UT>;
+  cudaError_t e = cudaSuccess;
+  if (smem > 48 * 1024) {  // one size for every call, so that calls with different batches do not lower each other's limit
+    constexpr int most = WARPS * RING * 2 * UT * D + 8193 * (int)sizeof(int);
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+  }
+  if (e == cudaSuccess) e = launch_pdl(kernel, dim3(a.n_warps / WARPS), dim3(ATTN_THREADS), smem, s, a);
+  return e;
+}
+
+template <class T, int CODE, int D, int NT> cudaError_t launch_attn_ut(const Kv8AttnArgs& a, int ut, cudaStream_t s) {
+  return ut == 32 ? launch_attn<T, CODE, D, NT, 32>(a, s) : launch_attn<T, CODE, D, NT, 16>(a, s);
+}
+template <class T, int CODE> cudaError_t launch_attn_shape(const Kv8AttnArgs& a, int ut, cudaStream_t s) {
+  const bool wide = a.G > 8;
+  if (a.c.D == 128) return wide ? launch_attn_ut<T, CODE, 128, 2>(a, ut, s) : launch_attn_ut<T, CODE, 128, 1>(a, ut, s);
+  return wide ? launch_attn_ut<T, CODE, 64, 2>(a, ut, s) : launch_attn_ut<T, CODE, 64, 1>(a, ut, s);
+}
+template <class T> cudaError_t launch_all(const Kv8AttnArgs& a, int code, int ut, cudaStream_t s) {
+  cudaError_t e = code == QEVICT_CODE_INT8 ? launch_attn_shape<T, QEVICT_CODE_INT8>(a, ut, s) : launch_attn_shape<T, QEVICT_CODE_E4M3>(a, ut, s);
+  const size_t smem = (size_t)(a.c.n_seqs + 1) * sizeof(int);
+  if (e == cudaSuccess) e = launch_pdl(kv8_combine_kernel<T>, dim3(a.Hq, a.c.n_seqs), dim3(COMB_THREADS), smem, s, a, ut);
+  if (e == cudaSuccess && a.score_out) {
+    const int per = MASS_THREADS / 32;
+    e = launch_pdl(kv8_mass_kernel, dim3((a.c.max_blocks + per - 1) / per, a.c.n_seqs), dim3(MASS_THREADS), 0, s, a, ut);
+  }
+  return e;
+}
+
+}  // namespace
+
+}  // namespace qevict
+
+using namespace qevict;
+
+extern "C" {
+
+QEVICT_API qevict_status qevict_kv8_attn_scratch_bytes(const qevict_kv8_cache* cache, int32_t n_q_heads, int32_t max_len,
+                                                       int32_t with_scores, uint64_t* bytes) {
+  Kv8View v;
+  qevict_status st;
+  Plan p;
+  const char* why = kv8_check(cache, &st, &v);
+  if (!why && !bytes) { why = "bytes is NULL"; st = QEVICT_ERR_INVALID_ARG; }
+  if (!why) why = plan_of(v, n_q_heads, max_len, with_scores != 0, sm_count(cache->device), &st, &p);
+  if (why) return stateless_fail(st, why);
+  *bytes = p.bytes;
+  return QEVICT_OK;
+}
+
+QEVICT_API qevict_status qevict_kv8_attn(const qevict_kv8_cache* cache, int32_t n_q_heads, float softmax_scale, const void* q,
+                                         const int32_t* lens, int32_t max_len, void* out, float* lse, const float* score_in,
+                                         float* score_out, void* scratch, uint64_t scratch_bytes, void* stream) {
+  Kv8AttnArgs a;
+  qevict_status st;
+  Plan p;
+  auto bad = [](const char* msg) { return stateless_fail(QEVICT_ERR_INVALID_ARG, msg); };
+  const char* why = kv8_check(cache, &st, &a.c);
+  if (!why) why = plan_of(a.c, n_q_heads, max_len, score_out != nullptr, sm_count(cache->device), &st, &p);
+  if (why) return stateless_fail(st, why);
+  if (!(softmax_scale >= 0.f) || isinf(softmax_scale)) return bad("softmax_scale must be finite and >= 0");
+  if (score_in && !score_out) return bad("score_in needs score_out");
+  if (a.c.n_seqs == 0) return QEVICT_OK;
+  if (!q || !lens || !out || !scratch) return bad("q, lens, out and scratch must not be NULL");
+  if (misaligned16(q) || misaligned16(out) || (reinterpret_cast<uintptr_t>(scratch) & 15u)) return bad("q, out and scratch must be 16-byte aligned");
+  if (misaligned4(lens) || misaligned4(lse) || misaligned4(score_in) || misaligned4(score_out)) return bad("lens, lse and scores must be 4-byte aligned");
+  if (scratch_bytes < p.bytes) return stateless_fail(QEVICT_ERR_NO_MEMORY, "scratch too small: see qevict_kv8_attn_scratch_bytes");
+  a.Hq = n_q_heads; a.G = n_q_heads / a.c.Hkv;
+  a.scale_log2 = (float)((softmax_scale > 0.f ? (double)softmax_scale : 1.0 / sqrt((double)a.c.D)) * 1.4426950408889634);
+  a.q = q; a.lens = lens; a.max_len = p.max_len; a.n_warps = p.n_warps; a.max_units = p.max_units;
+  a.out = out; a.lse = lse; a.score_in = score_in; a.score_out = score_out;
+  char* base = static_cast<char*>(scratch);
+  a.part_o = reinterpret_cast<float*>(base);
+  a.part_ml = reinterpret_cast<float2*>(base + p.off_ml);
+  a.stats = reinterpret_cast<float2*>(base + p.off_stats);
+  a.rec = score_out ? reinterpret_cast<float2*>(base + p.off_rec) : nullptr;
+  DeviceGuard guard(cache->device);
+  cudaError_t e = guard.err;
+  cudaStream_t s = (cudaStream_t)stream;
+  if (e == cudaSuccess)
+    e = cache->dtype == QEVICT_DTYPE_FP16 ? launch_all<__half>(a, cache->code, p.ut, s) : launch_all<__nv_bfloat16>(a, cache->code, p.ut, s);
+  if (e != cudaSuccess) return stateless_fail(QEVICT_ERR_CUDA, cudaGetErrorString(e));
+  return QEVICT_OK;
+}
+
+}  // extern "C"

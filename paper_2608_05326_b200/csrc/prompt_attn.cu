@@ -1,0 +1,623 @@
+// Attention over whole prompts on the 5th-generation tensor cores.
+//
+//     S = Q K^T,  P = 2^(S * scale * log2 e - m),  O += P V,  out = O / sum P,  lse = ln sum exp(scale * S)
+//
+// One CTA takes 256 query rows of one head as two tiles of 128 and walks the keys in tiles of 128, last tile first.
+// Ten warps: four per query tile for the softmax (a thread owns a row: no shuffles), one that issues the products, one
+// that issues the copies.
+//   - Q, K, V tiles come by TMA (boxes of 64 channels x 128 tokens, 128-byte swizzle); K and V share a ring.
+//   - S (128 x 128 fp32) and O (128 x d fp32) of both tiles fill the 512 columns of tensor memory.  P goes back over S
+//     in 16 bits and is the A operand of the second product from there.
+//   - While one tile's warps are in their softmax, the tensor cores work on the other tile's products.
+//   - The reference exponent m of a row moves only when a logit exceeds it by 2^8 (then O is rescaled in tensor
+//     memory); P is at most 2^8, sums are float32.
+// At d = 128 a key tile costs both query tiles 2 x 1024 tensor-core cycles and 2 x 1024 cycles of the exponential
+// unit (16 a cycle): the call is bound by the two together.
+//
+// Few query rows (one token, a short piece behind a long prefix): the keys are split over several CTAs whose partial
+// outputs prompt_merge_kernel joins.
+//
+// Keys past the sequence's end are masked by selection, so what lies there (another sequence, padding, NaN) never
+// enters; value rows past the end are zeroed in shared memory before the product reads them, since 0 * NaN is NaN.
+// Every wait is bounded; one that runs out records CHECK_COPY_TIMEOUT and the CTA leaves after its copies have landed.
+#include <cuda.h>
+
+#include "kv8.cuh"
+
+namespace qevict {
+
+namespace {
+
+constexpr int PROMPT_THREADS = 320;
+constexpr int MMA_WARP = 8, LOAD_WARP = 9;
+constexpr int TILE = 128;           // query rows of a tile, keys of a tile
+constexpr float PROMPT_LAZY = 8.f;  // log2
+
+struct PromptArgs {
+  int padded, n_seqs, Hq, Hkv, D, max_q, max_k, causal, splits;
+  long long total_q, total_k;
+  float scale_log2;
+  void* out;
+  float* lse;
+  const int32_t* q_bounds;
+  const int32_t* k_bounds;
+  long long out_stride[3];
+  float* part_o;    // [split][row][Hq][D]
+  float* part_lse;  // [split][row][Hq] (log2)
+  long long rows;   // rows of the partial results
+  int32_t* status;
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ float ex2p(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
+  for (uint32_t it = 0; it < (1u << 20); ++it) {
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}\n"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    if (done) return true;
+  }
+  return false;
+}
+// the same for a whole warp, with one answer
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, bar_wait(bar, parity)); }
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int tok, int head, int seq) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+               ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(tok), "r"(head), "r"(seq) : "memory");
+}
+__device__ __forceinline__ void commit_to(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// shared-memory operand with the 128-byte swizzle: address, leading and stride byte offsets in 16-byte units
+__device__ __forceinline__ uint64_t desc128(uint32_t addr, uint32_t lbo, uint32_t sbo) {
+  return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)((lbo >> 4) & 0x3FFFu) << 16) | ((uint64_t)((sbo >> 4) & 0x3FFFu) << 32) |
+         (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc) : "memory");
+}
+#define QE_R32(v, o) \
+  v[o + 0], v[o + 1], v[o + 2], v[o + 3], v[o + 4], v[o + 5], v[o + 6], v[o + 7], v[o + 8], v[o + 9], v[o + 10], v[o + 11], v[o + 12], \
+      v[o + 13], v[o + 14], v[o + 15], v[o + 16], v[o + 17], v[o + 18], v[o + 19], v[o + 20], v[o + 21], v[o + 22], v[o + 23], v[o + 24], \
+      v[o + 25], v[o + 26], v[o + 27], v[o + 28], v[o + 29], v[o + 30], v[o + 31]
+__device__ __forceinline__ void tm_ld32(uint32_t addr, float* v) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, "
+      "%19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
+        "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]),
+        "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]),
+        "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+      : "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* u) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
+      "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};\n" ::"r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]),
+      "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]),
+      "r"(u[15]), "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]), "r"(u[20]), "r"(u[21]), "r"(u[22]), "r"(u[23]), "r"(u[24]),
+      "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]), "r"(u[30]), "r"(u[31]), "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tm_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tm_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+template <class T> __device__ __forceinline__ uint32_t pack2(float a, float b);
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b) { return as_u32(__floats2half2_rn(a, b)); }
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) { return as_u32(__floats2bfloat162_rn(a, b)); }
+
+// Rows of a sequence: first row, count, sequence coordinate of the tensor map.
+__device__ __forceinline__ void span_of(const int32_t* bounds, int padded, int s, int most, long long total, int* first, int* n) {
+  if (padded) {
+    *first = 0;
+    *n = bounds ? max(0, min(bounds[s], most)) : most;
+  } else {
+    const long long b0 = max(0ll, min((long long)bounds[s], total)), b1 = max(b0, min((long long)bounds[s + 1], total));
+    *first = (int)b0;
+    *n = (int)min(b1 - b0, (long long)most);
+  }
+}
+
+template <int D> struct PromptSmem {
+  static constexpr int STAGES = D == 128 ? 5 : 8;
+  static constexpr int HALF = TILE * 128;             // 64 channels of 128 rows
+  static constexpr int TILE_BYTES = HALF * (D / 64);
+  static constexpr int Q_OFF = 0, KV_OFF = 2 * TILE_BYTES, BAR_OFF = KV_OFF + STAGES * TILE_BYTES;
+  static constexpr int BYTES = BAR_OFF + 256 + 1024;  // 1024: the tiles start on a multiple of 1024 bytes
+};
+
+template <class T, int D>
+__global__ void __launch_bounds__(PROMPT_THREADS, 1)
+    prompt_attn_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+                       const __grid_constant__ CUtensorMap mv) {
+  using SM = PromptSmem<D>;
+  constexpr int NS = SM::STAGES;
+  extern __shared__ unsigned char raw[];
+  unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const uint32_t smb = smem_u32(sm), bars = smb + SM::BAR_OFF;
+  // barriers: Q; ring full / empty; S ready, P ready, O ready of both tiles; value tail zeroed
+  const uint32_t b_q = bars, b_full = bars + 8, b_empty = b_full + 8 * NS, b_s = b_empty + 8 * NS, b_p = b_s + 16, b_o = b_p + 16,
+                 b_clean = b_o + 16;
+  volatile uint32_t* shared_words = reinterpret_cast<volatile uint32_t*>(sm + SM::BAR_OFF + 224);  // tensor memory, loads issued, failed
+  pdl_prologue();
+
+  const int m_tiles = (a.max_q + 2 * TILE - 1) / (2 * TILE);
+  const int split = blockIdx.x % a.splits, mt_raw = blockIdx.x / a.splits;
+  const int mt = a.causal ? m_tiles - 1 - mt_raw : mt_raw;  // the longest rows first
+  const int hq = blockIdx.y, s = blockIdx.z, hk = hq / (a.Hq / a.Hkv);
+  int q0, nq, k0, nk;
+  span_of(a.q_bounds, a.padded, s, a.max_q, a.total_q, &q0, &nq);
+  span_of(a.k_bounds, a.padded, s, a.max_k, a.total_k, &k0, &nk);
+  const int r0 = mt * 2 * TILE, off = nk - nq;
+  if (r0 >= nq) return;
+  // key tiles of the two query tiles, and this CTA's part of them
+  int nt[2];
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    const int rw = r0 + w * TILE, last = min(rw + TILE, nq) - 1;
+    const int lim = rw >= nq ? 0 : (a.causal ? min(nk, last + off + 1) : nk);
+    nt[w] = lim > 0 ? (lim + TILE - 1) / TILE : 0;
+  }
+  int lo = 0, n = max(nt[0], nt[1]);
+  if (a.splits > 1) {
+    const int per = (n + a.splits - 1) / a.splits;
+    lo = min(n, split * per);
+    n = min(n, lo + per);
+    nt[0] = min(nt[0], n);
+    nt[1] = min(nt[1], n);
+  }
+  const int cnt0 = max(0, nt[0] - lo), cnt1 = max(0, nt[1] - lo);
+  const int n_all = n - lo;  // tiles that are loaded
+  const bool dirty = n_all > 0 && n * TILE > nk;  // the first tile reaches past the sequence
+
+  if (wid == MMA_WARP) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((void*)shared_words)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (tid == 0) {
+    bar_init(b_q, 1);
+    for (int i = 0; i < NS; ++i) { bar_init(b_full + 8 * i, 1); bar_init(b_empty + 8 * i, 1); }
+    for (int w = 0; w < 2; ++w) { bar_init(b_s + 8 * w, 1); bar_init(b_p + 8 * w, 4); bar_init(b_o + 8 * w, 1); }
+    bar_init(b_clean, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    shared_words[1] = 0;
+    shared_words[2] = 0;
+  }
+  tm_before();
+  __syncthreads();
+  tm_after();
+  const uint32_t tmem = shared_words[0];
+  bool ok = true;
+
+  if (wid == LOAD_WARP) {
+    const int cs = a.padded ? s : 0;
+    if (lane == 0 && n_all > 0) {
+      bar_expect(b_q, (uint32_t)((cnt0 > 0) + (cnt1 > 0)) * SM::TILE_BYTES);
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+        if ((w ? cnt1 : cnt0) > 0)
+          for (int x = 0; x < D / 64; ++x)
+            tma_load(smb + SM::Q_OFF + w * SM::TILE_BYTES + x * SM::HALF, &mq, b_q, x * 64, q0 + r0 + w * TILE, hq, cs);
+    }
+    const int loads = 2 * n_all, clean_at = min(NS, loads) - 1;
+    for (int it = 0; it < loads && ok; ++it) {  // K, V of the last tile, K, V of the one before, ...
+      const int slot = it % NS, j = n - 1 - (it >> 1);
+      if (it >= NS) ok = warp_wait(b_empty + 8 * slot, (uint32_t)(it / NS - 1) & 1u);
+      if (ok && lane == 0) {
+        bar_expect(b_full + 8 * slot, SM::TILE_BYTES);
+        for (int x = 0; x < D / 64; ++x)
+          tma_load(smb + SM::KV_OFF + slot * SM::TILE_BYTES + x * SM::HALF, (it & 1) ? &mv : &mk, b_full + 8 * slot, x * 64, k0 + j * TILE, hk, cs);
+        shared_words[1] = it + 1;
+      }
+      if (ok && dirty && it == clean_at) {  // zero the value rows past the end
+        ok = warp_wait(b_full + 8, 0);
+        const int from = nk - (n - 1) * TILE;
+        if (ok) {
+          for (int i = lane; i < (TILE - from) * 8 * (D / 64); i += 32) {
+            const int x = i / ((TILE - from) * 8), k = i - x * (TILE - from) * 8;
+            *reinterpret_cast<uint4*>(sm + SM::KV_OFF + SM::TILE_BYTES + x * SM::HALF + from * 128 + k * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) bar_arrive(b_clean);
+        }
+      }
+      __syncwarp();
+    }
+  } else if (wid == MMA_WARP) {
+    if (lane == 0 && n_all > 0) {
+      const uint32_t fmt = Tr<T>::MAGIC == 0x64006400u ? 0u : 1u;  // 0 = fp16, 1 = bf16
+      const uint32_t base = (1u << 4) | (fmt << 7) | (fmt << 10) | ((128u >> 4) << 24);
+      const uint32_t id_s = base | ((128u >> 3) << 17);                           // both operands K-major
+      const uint32_t id_o = base | (1u << 16) | ((uint32_t)(D >> 3) << 17);       // V: channels contiguous (N-major)
+      auto issue_s = [&](int w, int slot) {
+        const uint32_t qa = smb + SM::Q_OFF + w * SM::TILE_BYTES, ka = smb + SM::KV_OFF + slot * SM::TILE_BYTES;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+          const uint32_t o = (uint32_t)(ks >> 2) * SM::HALF + (ks & 3) * 32;
+          mma_ss(tmem + w * 128, desc128(qa + o, 16, 1024), desc128(ka + o, 16, 1024), id_s, ks > 0);
+        }
+        commit_to(b_s + 8 * w);
+      };
+      auto issue_o = [&](int w, int slot, bool acc) {
+        const uint32_t va = smb + SM::KV_OFF + slot * SM::TILE_BYTES;
+#pragma unroll
+        for (int ks = 0; ks < TILE / 16; ++ks)
+          mma_ts(tmem + 256 + w * 128, tmem + w * 128 + ks * 8, desc128(va + ks * 2048, SM::HALF, 1024), id_o, acc || ks > 0);
+        commit_to(b_o + 8 * w);
+      };
+      ok = bar_wait(b_q, 0) && bar_wait(b_full, 0);
+      if (ok) {
+        if (n - 1 < nt[0]) issue_s(0, 0);
+        if (n - 1 < nt[1]) issue_s(1, 0);
+        commit_to(b_empty);
+      }
+      int done[2] = {0, 0};  // tiles whose P has been taken
+      for (int i = 0; i < n_all && ok; ++i) {
+        const int j = n - 1 - i, it_v = 2 * i + 1, it_k = 2 * i + 2, sv = it_v % NS, sk = it_k % NS;
+        const bool more = i + 1 < n_all;
+        ok = bar_wait(b_full + 8 * sv, (uint32_t)(it_v / NS) & 1u);
+        if (ok && i == 0 && dirty) ok = bar_wait(b_clean, 0);
+        if (ok && more) ok = bar_wait(b_full + 8 * sk, (uint32_t)(it_k / NS) & 1u);
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          if (ok && j < nt[w]) {
+            ok = bar_wait(b_p + 8 * w, (uint32_t)done[w] & 1u);
+            if (!ok) break;
+            tm_after();
+            issue_o(w, sv, done[w] > 0);
+            ++done[w];
+          }
+          if (ok && more && j - 1 < nt[w]) issue_s(w, sk);
+        }
+        if (ok) {
+          commit_to(b_empty + 8 * sv);
+          if (more) commit_to(b_empty + 8 * sk);
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    const int w = wid >> 2, r = (wid & 3) * 32 + lane;  // row of the tile
+    const int row = r0 + w * TILE + r;                  // of the sequence
+    const int cnt = w ? cnt1 : cnt0, top = w ? nt[1] : nt[0];
+    const int lim = a.causal ? min(nk, row + off + 1) : nk;  // keys this row sees
+    const uint32_t lane_base = (uint32_t)((wid & 3) * 32) << 16;
+    const uint32_t ts = tmem + lane_base + w * 128, to = tmem + lane_base + 256 + w * 128;
+    float m = -INFINITY, l = 0.f;
+    for (int i = 0; i < cnt && ok; ++i) {
+      const int c0 = (top - 1 - i) * TILE;
+      // the output's barrier is waited for in every phase: a parity says nothing about a phase further back
+      ok = warp_wait(b_s + 8 * w, (uint32_t)i & 1u) && (i == 0 || warp_wait(b_o + 8 * w, (uint32_t)(i - 1) & 1u));
+      if (!ok) break;
+      tm_after();
+      float x[TILE];
+#pragma unroll
+      for (int c = 0; c < TILE; c += 32) tm_ld32(ts + c, x + c);
+      tm_wait_ld();
+      if (__any_sync(0xffffffffu, lim < c0 + TILE)) {
+#pragma unroll
+        for (int c = 0; c < TILE; ++c) x[c] = c0 + c < lim ? x[c] : -INFINITY;
+      }
+      float mx[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+      for (int c = 4; c < TILE; ++c) mx[c & 3] = fmaxf(mx[c & 3], x[c]);
+      const float top_x = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
+      if (__any_sync(0xffffffffu, top_x > m + PROMPT_LAZY)) {
+        const float m_new = fmaxf(m, top_x);
+        const float f = m_new == m ? 1.f : ex2p(m - m_new);
+        m = m_new;
+        l *= f;
+        if (i > 0) {
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            float o[32];
+            tm_ld32(to + c, o);
+            tm_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] *= f;
+            tm_st32(to + c, reinterpret_cast<const uint32_t*>(o));
+          }
+        }
+      }
+      const float ms = m == -INFINITY ? 0.f : m;
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      uint32_t p[TILE / 2];
+#pragma unroll
+      for (int c = 0; c < TILE; c += 2) {
+        const float p0 = ex2p(fmaf(x[c], a.scale_log2, -ms)), p1 = ex2p(fmaf(x[c + 1], a.scale_log2, -ms));
+        sum[(c >> 1) & 3] += p0 + p1;
+        p[c >> 1] = pack2<T>(p0, p1);
+      }
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      tm_st32(ts, p);
+      tm_st32(ts + 32, p + 32);
+      tm_wait_st();
+      tm_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(b_p + 8 * w);
+    }
+    // results
+    if (cnt > 0 && ok) ok = warp_wait(b_o + 8 * w, (uint32_t)(cnt - 1) & 1u);
+    tm_after();
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const bool mine = row < nq;
+    const long long prow = a.padded ? (long long)s * a.max_q + row : (long long)q0 + row;
+    const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
+    if (ok && mine) {
+      if (a.splits > 1)
+        a.part_lse[((long long)split * a.rows + prow) * a.Hq + hq] = lse2;
+      else if (a.lse)
+        a.lse[a.padded ? ((long long)s * a.Hq + hq) * a.max_q + row : hq * a.total_q + prow] = lse2 * 0.6931471805599453f;
+    }
+    T* out = static_cast<T*>(a.out) + (a.padded ? s * a.out_stride[0] + row * a.out_stride[2] : prow * a.out_stride[2]) + hq * a.out_stride[1];
+    float* po = a.part_o + (((long long)split * a.rows + prow) * a.Hq + hq) * D;
+#pragma unroll 1
+    for (int c = 0; c < D && ok; c += 32) {
+      float o[32];
+      if (cnt > 0) {  // warp-uniform
+        tm_ld32(to + c, o);
+        tm_wait_ld();
+      }
+#pragma unroll
+      for (int k = 0; k < 32; ++k) o[k] = l == 0.f ? 0.f : o[k] * inv;
+      if (!mine) continue;
+      if (a.splits > 1) {
+#pragma unroll
+        for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(po + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 32; k += 8)
+          *reinterpret_cast<uint4*>(out + c + k) =
+              make_uint4(pack2<T>(o[k], o[k + 1]), pack2<T>(o[k + 2], o[k + 3]), pack2<T>(o[k + 4], o[k + 5]), pack2<T>(o[k + 6], o[k + 7]));
+      }
+    }
+  }
+  if (!ok) {
+    shared_words[2] = 1;
+    kv8_record(a.status, CHECK_COPY_TIMEOUT);
+  }
+  tm_before();
+  __syncthreads();
+  tm_after();
+  if (shared_words[2] && tid == 0) {  // a wait ran out: the copies in flight must land before the shared memory is given up
+    const int issued = (int)shared_words[1];
+    for (int it = max(0, issued - NS); it < issued; ++it) bar_wait(b_full + 8 * (it % NS), (uint32_t)(it / NS) & 1u);
+    if (n_all > 0) bar_wait(b_q, 0);
+  }
+  __syncthreads();
+  if (wid == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+// Joins the partial results of a split call: one warp per (row, head).
+template <class T>
+__global__ void __launch_bounds__(256) prompt_merge_kernel(const PromptArgs a) {
+  const int lane = threadIdx.x & 31, s = blockIdx.y;
+  pdl_prologue();
+  int q0, nq;
+  span_of(a.q_bounds, a.padded, s, a.max_q, a.total_q, &q0, &nq);
+  const long long at = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int row = (int)(at / a.Hq), hq = (int)(at - (long long)row * a.Hq);
+  if (row >= nq) return;
+  const long long prow = a.padded ? (long long)s * a.max_q + row : (long long)q0 + row;
+  float M = -INFINITY;
+  for (int i = 0; i < a.splits; ++i) M = fmaxf(M, a.part_lse[((long long)i * a.rows + prow) * a.Hq + hq]);
+  const float Ms = M == -INFINITY ? 0.f : M;
+  float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  const int per = a.D / 32;  // channels of a lane: 2 or 4
+  for (int i = 0; i < a.splits; ++i) {
+    const long long p = ((long long)i * a.rows + prow) * a.Hq + hq;
+    const float f = ex2p(a.part_lse[p] - Ms);
+    L += f;
+    const float* src = a.part_o + p * a.D + lane * per;
+    for (int k = 0; k < per; ++k) o[k] += f * src[k];
+  }
+  T* out = static_cast<T*>(a.out) + (a.padded ? s * a.out_stride[0] + row * a.out_stride[2] : prow * a.out_stride[2]) + hq * a.out_stride[1];
+  for (int k = 0; k < per; ++k) out[lane * per + k] = Tr<T>::from_float(L == 0.f ? 0.f : o[k] / L);
+  if (lane == 0 && a.lse)
+    a.lse[a.padded ? ((long long)s * a.Hq + hq) * a.max_q + row : hq * a.total_q + prow] =
+        L == 0.f ? -INFINITY : (Ms + log2f(L)) * 0.6931471805599453f;
+}
+
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encode_fn() {
+  static EncodeFn fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) {
+      (void)cudaGetLastError();
+      p = nullptr;
+    }
+    return reinterpret_cast<EncodeFn>(p);
+  }();
+  return fn;
+}
+
+// {channel, token, head, sequence} map of boxes of 64 channels x 128 tokens
+bool make_map(CUtensorMap* map, int dtype, const void* base, int D, long long tokens, int heads, long long seqs, const int64_t* stride) {
+  memset(map, 0, sizeof(*map));
+  if (tokens < 1) return true;  // no rows: no copy is made
+  const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)tokens, (cuuint64_t)heads, (cuuint64_t)seqs};
+  // a dimension of one element has no stride that matters
+  const cuuint64_t st[3] = {(cuuint64_t)(tokens > 1 ? stride[2] : D) * 2, (cuuint64_t)(heads > 1 ? stride[1] : D) * 2,
+                            (cuuint64_t)(seqs > 1 ? stride[0] : D) * 2};
+  const cuuint32_t box[4] = {64, TILE, 1, 1}, el[4] = {1, 1, 1, 1};
+  EncodeFn fn = encode_fn();
+  return fn && fn(map, dtype == QEVICT_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base),
+                  dims, st, box, el, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+const char* prompt_check(const qevict_prompt_args* p, qevict_status* st) {
+  *st = QEVICT_ERR_INVALID_ARG;
+  if (!p) return "args is NULL";
+  if (p->struct_size != sizeof(qevict_prompt_args)) return "struct_size does not match this library's qevict_prompt_args";
+  if (p->device < 0) return "device must be >= 0";
+  if (p->dtype != QEVICT_DTYPE_FP16 && p->dtype != QEVICT_DTYPE_BF16) return "dtype must be fp16 or bf16";
+  if (p->layout != QEVICT_LAYOUT_PACKED && p->layout != QEVICT_LAYOUT_PADDED) return "layout must be a QEVICT_LAYOUT_* value";
+  if (p->causal != 0 && p->causal != 1) return "causal must be 0 or 1";
+  if (p->n_seqs < 0 || p->max_q < 0 || p->max_k < 0 || p->total_q < 0 || p->total_k < 0) return "sizes must be >= 0";
+  if (p->n_kv_heads < 1 || p->n_q_heads < 1 || p->n_q_heads % p->n_kv_heads) return "n_q_heads must be a multiple of n_kv_heads";
+  if (!(p->softmax_scale >= 0.f) || isinf(p->softmax_scale)) return "softmax_scale must be finite and >= 0";
+  *st = QEVICT_ERR_UNSUPPORTED;
+  if (p->head_dim != 64 && p->head_dim != 128) return "head_dim must be 64 or 128";
+  if (p->n_seqs > 65535 || p->n_q_heads > 1024) return "more than 65535 sequences or 1024 heads";
+  if (p->total_q > 0x7fffffff - 1024 || p->total_k > 0x7fffffff - 1024 || p->max_q > 0x7fffffff - 1024 || p->max_k > 0x7fffffff - 1024)
+    return "more than 2^31 - 1024 tokens";
+  *st = QEVICT_ERR_INVALID_ARG;
+  if (p->n_seqs > 0 && p->layout == QEVICT_LAYOUT_PACKED && (!p->q_bounds || !p->k_bounds)) return "the packed layout needs q_bounds and k_bounds";
+  return nullptr;
+}
+
+const char* prompt_check_pointers(const qevict_prompt_args* p) {
+  const bool keys = p->max_k > 0 && (p->layout == QEVICT_LAYOUT_PADDED || p->total_k > 0);
+  if (!p->q || !p->out) return "q and out must not be NULL";
+  if (keys && (!p->k || !p->v)) return "k and v must not be NULL";
+  if (misaligned16(p->q) || misaligned16(p->out) || misaligned16(p->k) || misaligned16(p->v)) return "q, k, v and out must be 16-byte aligned";
+  if (misaligned4(p->lse) || misaligned4(p->q_bounds) || misaligned4(p->k_bounds) || misaligned4(p->status))
+    return "lse, bounds and status must be 4-byte aligned";
+  // a dimension of one element has no stride that matters
+  const bool padded = p->layout == QEVICT_LAYOUT_PADDED;
+  auto bad = [&](const int64_t* s, int heads, long long tokens) {
+    const long long size[3] = {padded ? p->n_seqs : 1, heads, tokens};
+    for (int i = 0; i < 3; ++i)
+      if (size[i] > 1 && (s[i] <= 0 || s[i] % 8 || s[i] >= (1ll << 38))) return true;
+    return false;
+  };
+  const long long nq = padded ? p->max_q : p->total_q, nk = padded ? p->max_k : p->total_k;
+  if (bad(p->q_stride, p->n_q_heads, nq) || bad(p->out_stride, p->n_q_heads, nq) || bad(p->k_stride, p->n_kv_heads, nk) ||
+      bad(p->v_stride, p->n_kv_heads, nk))
+    return "strides must be positive multiples of 16 bytes";
+  return nullptr;
+}
+
+int prompt_sms(int device) {
+  int n = 0;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || n < 1) {
+    (void)cudaGetLastError();
+    n = SM_COUNT_FALLBACK;
+  }
+  return n;
+}
+
+// CTAs that share a query tile's keys: more than one only where the query tiles alone leave SMs idle and there are keys
+// enough (at least four tiles each).
+int prompt_splits(const qevict_prompt_args* p) {
+  const long long tiles = ((long long)p->max_q + 2 * TILE - 1) / (2 * TILE) * p->n_q_heads * p->n_seqs;
+  const long long key_tiles = ((long long)p->max_k + TILE - 1) / TILE;
+  if (tiles < 1) return 1;
+  long long s = prompt_sms(p->device) / tiles;
+  if (s > key_tiles / 4) s = key_tiles / 4;
+  return (int)(s < 1 ? 1 : (s > 64 ? 64 : s));
+}
+
+long long prompt_rows(const qevict_prompt_args* p) {
+  return p->layout == QEVICT_LAYOUT_PADDED ? (long long)p->n_seqs * p->max_q : p->total_q;
+}
+size_t prompt_o_bytes(const qevict_prompt_args* p, int splits) {
+  return ((size_t)splits * prompt_rows(p) * p->n_q_heads * p->head_dim * sizeof(float) + 255) & ~(size_t)255;
+}
+size_t prompt_bytes(const qevict_prompt_args* p, int splits) {
+  return splits > 1 ? prompt_o_bytes(p, splits) + (size_t)splits * prompt_rows(p) * p->n_q_heads * sizeof(float) : 0;
+}
+
+template <class T, int D>
+cudaError_t launch_prompt(const PromptArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t s) {
+  auto kernel = prompt_attn_kernel<T, D>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptSmem<D>::BYTES);
+  const unsigned m_tiles = (unsigned)((a.max_q + 2 * TILE - 1) / (2 * TILE));
+  if (e == cudaSuccess)
+    e = launch_pdl(kernel, dim3(m_tiles * a.splits, a.Hq, a.n_seqs), dim3(PROMPT_THREADS), PromptSmem<D>::BYTES, s, a, mq, mk, mv);
+  if (e == cudaSuccess && a.splits > 1) {
+    const unsigned ctas = (unsigned)(((long long)a.max_q * a.Hq + 7) / 8);
+    e = launch_pdl(prompt_merge_kernel<T>, dim3(ctas, a.n_seqs), dim3(256), 0, s, a);
+  }
+  return e;
+}
+
+}  // namespace
+
+}  // namespace qevict
+
+using namespace qevict;
+
+extern "C" {
+
+QEVICT_API qevict_status qevict_prompt_attn_scratch_bytes(const qevict_prompt_args* args, uint64_t* bytes) {
+  qevict_status st;
+  const char* why = prompt_check(args, &st);
+  if (!why && !bytes) { why = "bytes is NULL"; st = QEVICT_ERR_INVALID_ARG; }
+  if (why) return stateless_fail(st, why);
+  *bytes = prompt_bytes(args, prompt_splits(args));
+  return QEVICT_OK;
+}
+
+QEVICT_API qevict_status qevict_prompt_attn(const qevict_prompt_args* args, void* scratch, uint64_t scratch_bytes, void* stream) {
+  qevict_status st;
+  const char* why = prompt_check(args, &st);
+  if (why) return stateless_fail(st, why);
+  const bool padded = args->layout == QEVICT_LAYOUT_PADDED;
+  if (args->n_seqs == 0 || args->max_q == 0 || (!padded && args->total_q == 0)) return QEVICT_OK;
+  why = prompt_check_pointers(args);
+  if (why) return stateless_fail(QEVICT_ERR_INVALID_ARG, why);
+  PromptArgs a;
+  a.padded = padded; a.n_seqs = args->n_seqs; a.Hq = args->n_q_heads; a.Hkv = args->n_kv_heads; a.D = args->head_dim;
+  a.max_q = args->max_q; a.max_k = args->max_k; a.causal = args->causal;
+  a.splits = prompt_splits(args);
+  const size_t need = prompt_bytes(args, a.splits);
+  if (need > 0 && (!scratch || scratch_bytes < need))
+    return stateless_fail(QEVICT_ERR_NO_MEMORY, "scratch too small: see qevict_prompt_attn_scratch_bytes");
+  if (need > 0 && misaligned16(scratch)) return stateless_fail(QEVICT_ERR_INVALID_ARG, "scratch must be 16-byte aligned");
+  a.total_q = args->total_q; a.total_k = args->total_k;
+  a.scale_log2 = (float)((args->softmax_scale > 0.f ? (double)args->softmax_scale : 1.0 / sqrt((double)args->head_dim)) * 1.4426950408889634);
+  a.out = args->out; a.lse = args->lse; a.q_bounds = args->q_bounds; a.k_bounds = args->k_bounds;
+  for (int i = 0; i < 3; ++i) a.out_stride[i] = args->out_stride[i];
+  a.rows = prompt_rows(args);
+  a.part_o = static_cast<float*>(scratch);
+  a.part_lse = reinterpret_cast<float*>(static_cast<char*>(scratch) + prompt_o_bytes(args, a.splits));
+  a.status = args->status;
+  DeviceGuard guard(args->device);
+  cudaError_t e = guard.err;
+  if (e != cudaSuccess) return stateless_fail(QEVICT_ERR_CUDA, cudaGetErrorString(e));
+  CUtensorMap mq, mk, mv;
+  const long long nq = padded ? args->max_q : args->total_q, nk = padded ? args->max_k : args->total_k;
+  const long long seqs = padded ? args->n_seqs : 1;
+  if (!make_map(&mq, args->dtype, args->q, a.D, nq, a.Hq, seqs, args->q_stride) ||
+      !make_map(&mk, args->dtype, args->k, a.D, args->max_k > 0 ? nk : 0, a.Hkv, seqs, args->k_stride) ||
+      !make_map(&mv, args->dtype, args->v, a.D, args->max_k > 0 ? nk : 0, a.Hkv, seqs, args->v_stride))
+    return stateless_fail(QEVICT_ERR_CUDA, "a tensor map could not be made for q, k or v");
+  cudaStream_t s = (cudaStream_t)stream;
+  if (args->dtype == QEVICT_DTYPE_FP16)
+    e = a.D == 128 ? launch_prompt<__half, 128>(a, mq, mk, mv, s) : launch_prompt<__half, 64>(a, mq, mk, mv, s);
+  else
+    e = a.D == 128 ? launch_prompt<__nv_bfloat16, 128>(a, mq, mk, mv, s) : launch_prompt<__nv_bfloat16, 64>(a, mq, mk, mv, s);
+  if (e != cudaSuccess) return stateless_fail(QEVICT_ERR_CUDA, cudaGetErrorString(e));
+  return QEVICT_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,276 @@
+"""Attention over whole prompts against a float64 evaluation, and what the call refuses."""
+
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import prompt as oracle
+from paper_2608_05326_b200 import binding
+
+HALF_STEP = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+
+
+# ---- refusals: checked before anything reaches a device --------------------------------------------------------
+def _args(**over):
+    a = binding.qevict_prompt_args()
+    values = dict(struct_size=C.sizeof(a), device=0, dtype=1, layout=0, n_seqs=2, n_q_heads=8, n_kv_heads=2, head_dim=64, max_q=16,
+                  max_k=16, causal=1, softmax_scale=0.0, total_q=32, total_k=32, q=4096, k=4096, v=4096, out=4096, q_bounds=4096, k_bounds=4096)
+    values.update(over)
+    for n, x in values.items():
+        if n.endswith("_stride"):
+            continue
+        setattr(a, n, x)
+    for n in ("q_stride", "k_stride", "v_stride", "out_stride"):
+        heads = a.n_q_heads if n in ("q_stride", "out_stride") else a.n_kv_heads
+        for i, x in enumerate(values.get(n, (0, 64, 64 * heads))):
+            getattr(a, n)[i] = x
+    return a
+
+
+@pytest.mark.parametrize("over,status,word", [
+    (dict(struct_size=8), 1, "struct_size"), (dict(device=-1), 1, "device"), (dict(dtype=7), 1, "dtype"), (dict(layout=2), 1, "layout"),
+    (dict(causal=2), 1, "causal"), (dict(n_seqs=-1), 1, "sizes"), (dict(n_q_heads=7), 1, "multiple"), (dict(n_kv_heads=0), 1, "multiple"),
+    (dict(softmax_scale=float("nan")), 1, "softmax_scale"), (dict(softmax_scale=-1.0), 1, "softmax_scale"), (dict(head_dim=96), 4, "head_dim"),
+    (dict(q=None), 1, "NULL"), (dict(k=None), 1, "NULL"), (dict(out=None), 1, "NULL"), (dict(q_bounds=None), 1, "q_bounds"),
+    (dict(q=4104), 1, "aligned"), (dict(lse=4098), 1, "aligned"), (dict(k_stride=(0, 60, 128)), 1, "strides"),
+    (dict(q_stride=(0, 64, 0)), 1, "strides"), (dict(total_q=2 ** 31), 4, "tokens"),
+])
+def test_unusable_arguments_are_refused_with_a_reason(over, status, word):
+    with pytest.raises(binding.QEvictError) as e:
+        binding._check(binding.lib().qevict_prompt_attn(C.byref(_args(**over)), None, 0, None))
+    assert e.value.status == status and word in str(e.value)
+
+
+def test_nothing_to_do_is_fine_without_a_device():
+    lib = binding.lib()
+    for over in (dict(n_seqs=0), dict(max_q=0), dict(total_q=0)):
+        assert lib.qevict_prompt_attn(C.byref(_args(**over)), None, 0, None) == 0
+
+
+def test_scratch_is_needed_only_for_few_queries_and_many_keys():
+    lib, need = binding.lib(), C.c_uint64(1)
+    binding._check(lib.qevict_prompt_attn_scratch_bytes(C.byref(_args()), C.byref(need)))
+    assert need.value == 0
+    few = _args(n_seqs=1, max_q=1, total_q=1, max_k=65536, total_k=65536)
+    binding._check(lib.qevict_prompt_attn_scratch_bytes(C.byref(few), C.byref(need)))
+    assert need.value > 0
+    assert lib.qevict_prompt_attn(C.byref(few), None, 0, None) == 3  # QEVICT_ERR_NO_MEMORY
+    assert b"scratch" in lib.qevict_last_error(None)
+    assert lib.qevict_prompt_attn_scratch_bytes(C.byref(few), None) == 1
+
+
+# ---- results ---------------------------------------------------------------------------------------------------
+def _make(nq, nk, hq, hkv, d, dtype, seed, gain=1.0):
+    g = torch.Generator().manual_seed(seed)
+    q = (gain * torch.randn((sum(nq), hq, d), generator=g)).to(dtype)
+    k = torch.randn((sum(nk), hkv, d), generator=g).to(dtype)
+    v = torch.randn((sum(nk), hkv, d), generator=g).to(dtype)
+    return q, k, v
+
+
+def _cu(lens, first=0):
+    return torch.tensor(np.concatenate([[first], first + np.cumsum(lens)]), dtype=torch.int32, device="cuda")
+
+
+def _np(x):
+    return x.double().cpu().numpy()
+
+
+def _check_rows(out, lse, q, k, v, causal, dtype, what="", scale=None):
+    """out [nq, Hq, d], lse [Hq, nq] of one sequence against the oracle."""
+    ro, rl, spread, reach = oracle.attention(_np(q), _np(k), _np(v), causal, scale)
+    d = q.shape[-1]
+    vmax = float(v.double().abs().max()) if v.numel() else 0.0
+    tol = oracle.out_tolerance(ro, spread, vmax, k.shape[0], d, reach, HALF_STEP[dtype], HALF_STEP[dtype])
+    err = np.abs(_np(out) - ro)
+    assert (err <= tol).all(), (what, float((err / tol).max()), float(err.max()))
+    got = _np(lse)
+    assert (np.isneginf(got) == np.isneginf(rl)).all(), what
+    ok = np.isfinite(rl)
+    assert np.isfinite(got[ok]).all() and (np.abs(got[ok] - rl[ok]) <= oracle.lse_tolerance(rl[ok], d, reach)).all(), what
+
+
+def _check_packed(out, lse, q, k, v, nq, nk, causal, dtype, q_first=0, k_first=0, scale=None):
+    a, b = q_first, k_first
+    for i, (x, y) in enumerate(zip(nq, nk)):
+        _check_rows(out[a:a + x], lse[:, a:a + x], q[a:a + x], k[b:b + y], v[b:b + y], causal, dtype, "sequence %d (%d, %d)" % (i, x, y), scale)
+        a, b = a + x, b + y
+
+
+LENS = [
+    ([1], [1]), ([77], [77]), ([128], [128]), ([129], [129]), ([256], [256]), ([257], [257]), ([600], [600]),
+    ([5, 0, 130, 1, 255], [5, 0, 130, 1, 255]), ([3, 200], [131, 456]), ([1, 64, 300], [700, 64, 301]),
+    ([130, 4], [2, 3]), ([3, 2], [0, 2]),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nq,nk", LENS)
+@pytest.mark.parametrize("dtype,hq,hkv,d", [(torch.bfloat16, 4, 2, 128), (torch.float16, 3, 1, 64)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_packed_sequences(nq, nk, dtype, hq, hkv, d, causal):
+    q, k, v = (x.cuda() for x in _make(nq, nk, hq, hkv, d, dtype, 11 + len(nq)))
+    out, lse = binding.qevict_prompt_attn(q, k, v, _cu(nq), _cu(nk), max(nq), max(nk), causal=causal, return_lse=True)
+    _check_packed(out, lse, q, k, v, nq, nk, causal, dtype)
+    again, lse2 = binding.qevict_prompt_attn(q, k, v, _cu(nq), _cu(nk), causal=causal, return_lse=True)  # bounds from the shapes
+    _check_packed(again, lse2, q, k, v, nq, nk, causal, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,hq,hkv,d", [(torch.bfloat16, 28, 4, 128), (torch.float16, 8, 8, 64), (torch.bfloat16, 16, 1, 128), (torch.float16, 32, 8, 128)])
+def test_head_layouts_and_longer_prompts(dtype, hq, hkv, d):
+    nq = [1111, 517]
+    q, k, v = (x.cuda() for x in _make(nq, nq, hq, hkv, d, dtype, 3))
+    out, lse = binding.qevict_prompt_attn(q, k, v, _cu(nq), max_q=max(nq), max_k=max(nq), return_lse=True)
+    _check_packed(out, lse, q, k, v, nq, nq, True, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gain", [0.02, 8.0])
+def test_flat_and_sharp_distributions(gain):
+    nq = [700]
+    q, k, v = (x.cuda() for x in _make(nq, nq, 2, 1, 128, torch.bfloat16, 5, gain))
+    out, lse = binding.qevict_prompt_attn(q, k, v, _cu(nq), return_lse=True)
+    _check_packed(out, lse, q, k, v, nq, nq, True, torch.bfloat16)
+
+
+@pytest.mark.gpu
+def test_logits_that_grow_along_the_keys_move_the_reference():
+    # every tile of 128 keys has larger logits than all the ones behind it, and the reverse
+    n, d = 1000, 128
+    for sign in (1.0, -1.0):
+        q, k, v = _make([n], [n], 1, 1, d, torch.float16, 9)
+        k = k * 0.1 + (sign * torch.linspace(-3, 3, n)[:, None, None]).to(torch.float16)
+        q = (q * 0.1 + 1.0).to(torch.float16)
+        q, k, v = q.cuda(), k.to(torch.float16).cuda(), v.cuda()
+        for causal in (True, False):
+            out, lse = binding.qevict_prompt_attn(q, k, v, _cu([n]), causal=causal, return_lse=True)
+            _check_packed(out, lse, q, k, v, [n], [n], causal, torch.float16)
+
+
+@pytest.mark.gpu
+def test_an_own_softmax_scale():
+    nq = [300]
+    q, k, v = (x.cuda() for x in _make(nq, nq, 2, 1, 64, torch.float16, 8))
+    out, lse = binding.qevict_prompt_attn(q, k, v, _cu(nq), softmax_scale=0.37, return_lse=True)
+    _check_packed(out, lse, q, k, v, nq, nq, True, torch.float16, scale=0.37)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nq,nk", [([1], [9000]), ([1, 3], [5000, 131]), ([40], [6001]), ([2], [70000])])
+@pytest.mark.parametrize("dtype,hq,hkv,d", [(torch.bfloat16, 4, 2, 128), (torch.float16, 7, 1, 64)])
+def test_few_queries_behind_a_long_prefix_split_the_keys(nq, nk, dtype, hq, hkv, d):
+    q, k, v = (x.cuda() for x in _make(nq, nk, hq, hkv, d, dtype, 21))
+    args = dict(max_q=max(nq), max_k=max(nk), return_lse=True)
+    out, lse = binding.qevict_prompt_attn(q, k, v, _cu(nq), _cu(nk), **args)
+    _check_packed(out, lse, q, k, v, nq, nk, True, dtype)
+    again, lse2 = binding.qevict_prompt_attn(q, k, v, _cu(nq), _cu(nk), **args)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nq,nk", [([70, 9], [70, 9]), ([3, 1], [4100, 900])])
+def test_what_lies_outside_the_sequences_is_neither_used_nor_written(nq, nk):
+    d, hq, hkv, dtype = 128, 4, 2, torch.bfloat16
+    q, k, v = (x.cuda() for x in _make([5] + nq + [200], [7] + nk + [200], hq, hkv, d, dtype, 2))
+    for x, lo, hi in ((q, 5, 5 + sum(nq)), (k, 7, 7 + sum(nk)), (v, 7, 7 + sum(nk))):
+        x[:lo] = float("nan")
+        x[hi:hi + 100] = float("nan")
+        x[hi + 100:] = float("inf")
+    out = torch.full_like(q, 3.0)
+    lse = torch.full((hq, q.shape[0]), 7.0, device="cuda")
+    binding.qevict_prompt_attn(q, k, v, _cu(nq, 5), _cu(nk, 7), max(nq), max(nk), out=out, lse=lse)
+    _check_packed(out, lse, q, k, v, nq, nk, True, dtype, 5, 7)
+    a, b = 5, 5 + sum(nq)
+    assert (out[:a] == 3).all() and (out[b:] == 3).all() and (lse[:, :a] == 7).all() and (lse[:, b:] == 7).all()
+
+
+@pytest.mark.gpu
+def test_one_sequence_does_not_reach_into_the_next():
+    nq = [100, 150]
+    q, k, v = (x.cuda() for x in _make(nq, nq, 2, 1, 64, torch.float16, 4))
+    k[100:], v[100:] = float("nan"), float("inf")
+    out, lse = binding.qevict_prompt_attn(q, k, v, _cu(nq), return_lse=True)
+    _check_rows(out[:100], lse[:, :100], q[:100], k[:100], v[:100], True, torch.float16)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,dtype", [(128, torch.bfloat16), (64, torch.float16)])
+def test_padded_layout_with_lengths(d, dtype):
+    n, hq, hkv, m = 4, 4, 2, 300
+    g = torch.Generator().manual_seed(1)
+    q = torch.randn((n, hq, m, d), generator=g).to(dtype).cuda()
+    k, v = (torch.randn((n, hkv, m + 20, d), generator=g).to(dtype).cuda() for _ in range(2))
+    lq, lk = [300, 1, 0, 129], [320, 5, 3, 129]
+    for i in range(n):
+        for x, c in ((q, lq), (k, lk), (v, lk)):
+            x[i, :, c[i]:] = float("nan")
+    out = torch.full_like(q, 3.0)
+    lse = torch.full((n, hq, m), 7.0, device="cuda")
+    lens = [torch.tensor(x, dtype=torch.int32, device="cuda") for x in (lq, lk)]
+    binding.qevict_prompt_attn(q, k, v, lens[0], lens[1], out=out, lse=lse)
+    for i in range(n):
+        a, b = lq[i], lk[i]
+        _check_rows(out[i, :, :a].transpose(0, 1), lse[i, :, :a], q[i, :, :a].transpose(0, 1), k[i, :, :b].transpose(0, 1), v[i, :, :b].transpose(0, 1), True, dtype)
+        assert (out[i, :, a:] == 3).all() and (lse[i, :, a:] == 7).all()
+    # without lengths every row counts
+    q, k, v = torch.nan_to_num(q), torch.nan_to_num(k), torch.nan_to_num(v)
+    out, lse = binding.qevict_prompt_attn(q, k, v, return_lse=True)
+    for i in range(n):
+        _check_rows(out[i].transpose(0, 1), lse[i], q[i].transpose(0, 1), k[i].transpose(0, 1), v[i].transpose(0, 1), True, dtype)
+
+
+@pytest.mark.gpu
+def test_strided_inputs_and_output():
+    n, hq, hkv, d, dtype = 333, 4, 2, 128, torch.bfloat16
+    g = torch.Generator().manual_seed(6)
+    qkv = torch.randn((n, hq + 2 * hkv, d + 8), generator=g).to(dtype).cuda()  # one projection's output, rows padded
+    q, k, v = qkv[:, :hq, :d], qkv[:, hq:hq + hkv, 8:], qkv[:, hq + hkv:, :d]
+    buf = torch.zeros((hq, n, d), dtype=dtype, device="cuda")
+    out, lse = binding.qevict_prompt_attn(q, k, v, _cu([n]), out=buf.transpose(0, 1), return_lse=True)
+    _check_rows(buf.transpose(0, 1), lse, q, k, v, True, dtype)
+    plain = binding.qevict_prompt_attn(q.contiguous(), k.contiguous(), v.contiguous(), _cu([n]))
+    assert torch.equal(plain, out)
+
+
+@pytest.mark.gpu
+def test_captured_and_on_another_stream():
+    nq = [200, 65]
+    q, k, v = (x.cuda() for x in _make(nq, nq, 4, 2, 128, torch.bfloat16, 17))
+    cu = _cu(nq)
+    want = binding.qevict_prompt_attn(q, k, v, cu, max_q=200, max_k=200)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = binding.qevict_prompt_attn(q, k, v, cu, max_q=200, max_k=200, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
+    graph, out = torch.cuda.CUDAGraph(), torch.zeros_like(q)
+    with torch.cuda.graph(graph):
+        binding.qevict_prompt_attn(q, k, v, cu, max_q=200, max_k=200, out=out)
+    for lens in ([200, 65], [31, 200]):  # the lengths are read when the graph runs
+        cu.copy_(_cu(lens))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        a = 0
+        for x in lens:
+            ro, _, spread, reach = oracle.attention(_np(q[a:a + x]), _np(k[a:a + x]), _np(v[a:a + x]))
+            tol = oracle.out_tolerance(ro, spread, 6.0, x, 128, reach, 2.0 ** -8, 2.0 ** -8)
+            assert (np.abs(_np(out[a:a + x]) - ro) <= tol).all()
+            a += x
+        assert (out[a:] == 0).all()
+
+
+@pytest.mark.gpu
+def test_bindings_refuse_what_the_library_cannot_see():
+    q, k, v = (x.cuda() for x in _make([8], [8], 2, 1, 64, torch.float16, 1))
+    cu = _cu([8])
+    for call in (lambda: binding.qevict_prompt_attn(q.float(), k.float(), v.float(), cu), lambda: binding.qevict_prompt_attn(q, k, v),
+                 lambda: binding.qevict_prompt_attn(q, k.to(torch.bfloat16), v, cu), lambda: binding.qevict_prompt_attn(q, k, v[:4], cu),
+                 lambda: binding.qevict_prompt_attn(q, k, v, cu.long()), lambda: binding.qevict_prompt_attn(q, k, v, cu, cu[:1]),
+                 lambda: binding.qevict_prompt_attn(q[..., ::2], k[..., ::2], v[..., ::2], cu), lambda: binding.qevict_prompt_attn(q.cpu(), k, v, cu),
+                 lambda: binding.qevict_prompt_attn(q[..., 1:], k[..., 1:], v[..., 1:], cu)):
+        with pytest.raises(binding.QEvictError):
+            call()
