@@ -28,9 +28,17 @@ namespace qevict {
 
 namespace {
 
-constexpr int PROMPT_THREADS = 320;
-constexpr int MMA_WARP = 8, LOAD_WARP = 9;
+constexpr int PROMPT_THREADS = 640;  // four softmax warpgroups, one for products and copies (two of its warps idle)
+constexpr int MMA_WARP = 16, LOAD_WARP = 17;
 constexpr int TILE = 128;           // query rows of a tile, keys of a tile
+#ifndef EMU
+#define EMU 1000
+#endif
+#ifndef RLO
+#define RLO "32"
+#define RHI "112"
+#endif
+constexpr int EMULATE = EMU;          // one pair of exponentials in so many runs on the FMA units
 constexpr float PROMPT_LAZY = 8.f;  // log2
 
 struct PromptArgs {
@@ -53,6 +61,55 @@ __device__ __forceinline__ float ex2p(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
   return y;
+}
+// Packed pairs of float32: one instruction for two fused multiply-adds or additions.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;\n" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// 2^x on the FMA units for a pair, x >= -126 after the clamp (what is below becomes 2^-126): x = n + f with n the nearest
+// integer (left in the low bits of x + 1.5 * 2^23), 2^f by the degree-5 polynomial of least relative error on
+// [-1/2, 1/2] (1.6e-7, fitted by reweighted least squares), n added to the exponent.
+__device__ __forceinline__ void ex2_pair_fma(uint64_t x, float& e0, float& e1) {
+  float x0, x1;
+  unpair(x, x0, x1);
+  x = pair(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
+  const uint64_t t = add2(x, pair(12582912.f, 12582912.f));
+  const uint64_t n = add2(t, pair(-12582912.f, -12582912.f));
+  const uint64_t f = fma2(n, pair(-1.f, -1.f), x);
+  uint64_t p = fma2(f, pair(0.0013276472454890609f, 0.0013276472454890609f), pair(0.009675541892647743f, 0.009675541892647743f));
+  p = fma2(p, f, pair(0.05550713092088699f, 0.05550713092088699f));
+  p = fma2(p, f, pair(0.24022120237350464f, 0.24022120237350464f));
+  p = fma2(p, f, pair(0.6931469440460205f, 0.6931469440460205f));
+  p = fma2(p, f, pair(1.0000001192092896f, 1.0000001192092896f));
+  float p0, p1, t0, t1;
+  unpair(p, p0, p1);
+  unpair(t, t0, t1);
+  e0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
+  e1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
+}
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}\n" : "=r"(p));
+  return p != 0;
 }
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
@@ -81,23 +138,22 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, u
 __device__ __forceinline__ void commit_to(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-// shared-memory operand with the 128-byte swizzle: address, leading and stride byte offsets in 16-byte units
-__device__ __forceinline__ uint64_t desc128(uint32_t addr, uint32_t lbo, uint32_t sbo) {
-  return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)((lbo >> 4) & 0x3FFFu) << 16) | ((uint64_t)((sbo >> 4) & 0x3FFFu) << 32) |
-         (1ull << 46) | (2ull << 61);
+// Descriptor of a shared-memory operand with the 128-byte swizzle: the low word holds the address and the leading byte
+// offset, the high word (constant) the stride of 1024 bytes between groups of eight rows, version 1 and the swizzle.
+constexpr uint32_t DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lbo) { return ((addr >> 4) & 0x3FFFu) | ((lbo >> 4) << 16); }
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}\n" ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(acc), "r"(DESC_HI)
+      : "memory");
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n"
-               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc) : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 db, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}\n" ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "r"(acc), "r"(DESC_HI)
+      : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool acc) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n"
-               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc) : "memory");
-}
-#define QE_R32(v, o) \
-  v[o + 0], v[o + 1], v[o + 2], v[o + 3], v[o + 4], v[o + 5], v[o + 6], v[o + 7], v[o + 8], v[o + 9], v[o + 10], v[o + 11], v[o + 12], \
-      v[o + 13], v[o + 14], v[o + 15], v[o + 16], v[o + 17], v[o + 18], v[o + 19], v[o + 20], v[o + 21], v[o + 22], v[o + 23], v[o + 24], \
-      v[o + 25], v[o + 26], v[o + 27], v[o + 28], v[o + 29], v[o + 30], v[o + 31]
 __device__ __forceinline__ void tm_ld32(uint32_t addr, float* v) {
   uint32_t* u = reinterpret_cast<uint32_t*>(v);
   asm volatile(
@@ -117,6 +173,13 @@ __device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* u) {
       "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]),
       "r"(u[15]), "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]), "r"(u[20]), "r"(u[21]), "r"(u[22]), "r"(u[23]), "r"(u[24]),
       "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]), "r"(u[30]), "r"(u[31]), "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tm_st16(uint32_t addr, const uint32_t* u) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};\n" ::"r"(u[0]),
+      "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]),
+      "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(addr)
       : "memory");
 }
 __device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -140,12 +203,16 @@ __device__ __forceinline__ void span_of(const int32_t* bounds, int padded, int s
   }
 }
 
+// Column of the 16 keys `k` (0 .. 3) of half `half` of a tile's P, over the S of the same half: the thread that writes it
+// has read what it overwrites.
+__device__ __forceinline__ constexpr int P_COL(int half, int k) { return half * 64 + k * 8; }
+
 template <int D> struct PromptSmem {
   static constexpr int STAGES = D == 128 ? 5 : 8;
   static constexpr int HALF = TILE * 128;             // 64 channels of 128 rows
   static constexpr int TILE_BYTES = HALF * (D / 64);
   static constexpr int Q_OFF = 0, KV_OFF = 2 * TILE_BYTES, BAR_OFF = KV_OFF + STAGES * TILE_BYTES;
-  static constexpr int BYTES = BAR_OFF + 256 + 1024;  // 1024: the tiles start on a multiple of 1024 bytes
+  static constexpr int BYTES = BAR_OFF + 256 + 2048;  // barriers, row maxima
 };
 
 template <class T, int D>
@@ -154,12 +221,11 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
                        const __grid_constant__ CUtensorMap mv) {
   using SM = PromptSmem<D>;
   constexpr int NS = SM::STAGES;
-  extern __shared__ unsigned char raw[];
-  unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  extern __shared__ __align__(1024) unsigned char sm[];  // the swizzle counts from multiples of 1024 bytes
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const uint32_t smb = smem_u32(sm), bars = smb + SM::BAR_OFF;
-  // barriers: Q; ring full / empty; S ready, P ready, O ready of both tiles; value tail zeroed
-  const uint32_t b_q = bars, b_full = bars + 8, b_empty = b_full + 8 * NS, b_s = b_empty + 8 * NS, b_p = b_s + 16, b_o = b_p + 16,
+  // barriers: Q; ring full / empty; S ready, P ready (both halves), O ready of both tiles; value tail zeroed
+  const uint32_t b_q = bars, b_full = bars + 8, b_empty = b_full + 8 * NS, b_s = b_empty + 8 * NS, b_p = b_s + 16, b_o = b_p + 32,
                  b_clean = b_o + 16;
   volatile uint32_t* shared_words = reinterpret_cast<volatile uint32_t*>(sm + SM::BAR_OFF + 224);  // tensor memory, loads issued, failed
   pdl_prologue();
@@ -173,6 +239,10 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
   span_of(a.k_bounds, a.padded, s, a.max_k, a.total_k, &k0, &nk);
   const int r0 = mt * 2 * TILE, off = nk - nq;
   if (r0 >= nq) return;
+  if (smb & 1023u) {  // no tile would be where the products look for it
+    kv8_record(a.status, CHECK_ALIGNMENT);
+    return;
+  }
   // key tiles of the two query tiles, and this CTA's part of them
   int nt[2];
 #pragma unroll
@@ -200,7 +270,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
   if (tid == 0) {
     bar_init(b_q, 1);
     for (int i = 0; i < NS; ++i) { bar_init(b_full + 8 * i, 1); bar_init(b_empty + 8 * i, 1); }
-    for (int w = 0; w < 2; ++w) { bar_init(b_s + 8 * w, 1); bar_init(b_p + 8 * w, 4); bar_init(b_o + 8 * w, 1); }
+    for (int w = 0; w < 2; ++w) { bar_init(b_s + 8 * w, 1); bar_init(b_p + 16 * w, 8); bar_init(b_p + 16 * w + 8, 8); bar_init(b_o + 8 * w, 1); }
     bar_init(b_clean, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     shared_words[1] = 0;
@@ -212,6 +282,9 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
   const uint32_t tmem = shared_words[0];
   bool ok = true;
 
+  // registers: 640 x 96 at launch = 512 x 112 + 128 x 32
+  if (wid >= MMA_WARP) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 " RLO ";");
   if (wid == LOAD_WARP) {
     const int cs = a.padded ? s : 0;
     if (lane == 0 && n_all > 0) {
@@ -248,84 +321,137 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       __syncwarp();
     }
   } else if (wid == MMA_WARP) {
-    if (lane == 0 && n_all > 0) {
+    // One thread issues every product, in the order S0 S1 | PV0 S0 PV1 S1 | ...: while one tile's softmax runs, the tensor
+    // cores have the other tile's products.  S of the next tile overwrites P: one thread's products run in the order of
+    // their issue.  (Two threads, one per tile, were slower, 9.8 against 8.4 ms on 32k tokens x 32 heads: their products
+    // interleave, and both tiles wait for the slower.)
+    // The whole warp walks the loop and one elected lane issues: what the products take (addresses, descriptors) is then
+    // the same for all lanes and stays in uniform registers, which is where the instruction wants it.
+    const int u_n = uniform(n), u_lo = uniform(lo), u_n0 = uniform(nt[0]), u_n1 = uniform(nt[1]);
+    const uint32_t u_tm = (uint32_t)uniform((int)tmem), u_sm = (uint32_t)uniform((int)smb);
+    if (u_n > u_lo) {
       const uint32_t fmt = Tr<T>::MAGIC == 0x64006400u ? 0u : 1u;  // 0 = fp16, 1 = bf16
       const uint32_t base = (1u << 4) | (fmt << 7) | (fmt << 10) | ((128u >> 4) << 24);
       const uint32_t id_s = base | ((128u >> 3) << 17);                           // both operands K-major
       const uint32_t id_o = base | (1u << 16) | ((uint32_t)(D >> 3) << 17);       // V: channels contiguous (N-major)
+      const uint32_t q_lo = desc_lo(u_sm + SM::Q_OFF, 16), k_lo = desc_lo(u_sm + SM::KV_OFF, 16), v_lo = desc_lo(u_sm + SM::KV_OFF, SM::HALF);
+      const uint32_t ub = u_sm + SM::BAR_OFF, u_full = ub + 8, u_empty = u_full + 8 * NS, u_s = u_empty + 8 * NS, u_p = u_s + 16, u_o = u_p + 32;
+      const bool leader = elect_one();
       auto issue_s = [&](int w, int slot) {
-        const uint32_t qa = smb + SM::Q_OFF + w * SM::TILE_BYTES, ka = smb + SM::KV_OFF + slot * SM::TILE_BYTES;
+        const uint32_t qa = q_lo + w * (SM::TILE_BYTES >> 4), ka = k_lo + slot * (SM::TILE_BYTES >> 4);
+        if (leader) {
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-          const uint32_t o = (uint32_t)(ks >> 2) * SM::HALF + (ks & 3) * 32;
-          mma_ss(tmem + w * 128, desc128(qa + o, 16, 1024), desc128(ka + o, 16, 1024), id_s, ks > 0);
-        }
-        commit_to(b_s + 8 * w);
-      };
-      auto issue_o = [&](int w, int slot, bool acc) {
-        const uint32_t va = smb + SM::KV_OFF + slot * SM::TILE_BYTES;
-#pragma unroll
-        for (int ks = 0; ks < TILE / 16; ++ks)
-          mma_ts(tmem + 256 + w * 128, tmem + w * 128 + ks * 8, desc128(va + ks * 2048, SM::HALF, 1024), id_o, acc || ks > 0);
-        commit_to(b_o + 8 * w);
-      };
-      ok = bar_wait(b_q, 0) && bar_wait(b_full, 0);
-      if (ok) {
-        if (n - 1 < nt[0]) issue_s(0, 0);
-        if (n - 1 < nt[1]) issue_s(1, 0);
-        commit_to(b_empty);
-      }
-      int done[2] = {0, 0};  // tiles whose P has been taken
-      for (int i = 0; i < n_all && ok; ++i) {
-        const int j = n - 1 - i, it_v = 2 * i + 1, it_k = 2 * i + 2, sv = it_v % NS, sk = it_k % NS;
-        const bool more = i + 1 < n_all;
-        ok = bar_wait(b_full + 8 * sv, (uint32_t)(it_v / NS) & 1u);
-        if (ok && i == 0 && dirty) ok = bar_wait(b_clean, 0);
-        if (ok && more) ok = bar_wait(b_full + 8 * sk, (uint32_t)(it_k / NS) & 1u);
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          if (ok && j < nt[w]) {
-            ok = bar_wait(b_p + 8 * w, (uint32_t)done[w] & 1u);
-            if (!ok) break;
-            tm_after();
-            issue_o(w, sv, done[w] > 0);
-            ++done[w];
+          for (int ks = 0; ks < D / 16; ++ks) {
+            const uint32_t o = ((uint32_t)(ks >> 2) * SM::HALF + (ks & 3) * 32) >> 4;
+            mma_ss(u_tm + w * 128, qa + o, ka + o, id_s, ks > 0);
           }
-          if (ok && more && j - 1 < nt[w]) issue_s(w, sk);
+          commit_to(u_s + 8 * w);
         }
-        if (ok) {
-          commit_to(b_empty + 8 * sv);
-          if (more) commit_to(b_empty + 8 * sk);
+        __syncwarp();
+      };
+      auto issue_o = [&](int w, int part, int slot, uint32_t acc) {
+        const uint32_t va = v_lo + slot * (SM::TILE_BYTES >> 4);
+        if (leader) {
+#pragma unroll
+          for (int k4 = 0; k4 < TILE / 32; ++k4) {
+            const int half = k4 >> 1, ks = half * 4 + part * 2 + (k4 & 1);  // keys 0-31 and 64-95, then the others
+            mma_ts(u_tm + 256 + w * 128, u_tm + w * 128 + P_COL(half, part * 2 + (k4 & 1)), va + ks * (2048 >> 4), id_o, k4 > 0 ? 1u : acc);
+          }
         }
+        __syncwarp();
+      };
+      ok = warp_wait(ub, 0) && warp_wait(u_full, 0);
+      if (ok) {
+        if (u_n - 1 < u_n0) issue_s(0, 0);
+        if (u_n - 1 < u_n1) issue_s(1, 0);
+        if (leader) commit_to(u_empty);
+      }
+      int slot = 0;  // ring position and phase
+      uint32_t phase = 0, phase0 = 0, phase1 = 0, acc0 = 0, acc1 = 0;
+      for (int j = u_n - 1; j >= u_lo && ok; --j) {
+        if (++slot == NS) { slot = 0; phase ^= 1u; }
+        const int sv = slot;
+        ok = warp_wait(u_full + 8 * sv, phase);  // V(j)
+        if (ok && j == u_n - 1 && dirty) ok = warp_wait(b_clean, 0);
+        const bool more = j > u_lo;
+        if (more) {
+          if (++slot == NS) { slot = 0; phase ^= 1u; }
+          ok = ok && warp_wait(u_full + 8 * slot, phase);  // K(j - 1)
+        }
+        if (!ok) break;
+        if (j < u_n0) {
+          if (!(ok = warp_wait(u_p, phase0))) break;
+          tm_after();
+          issue_o(0, 0, sv, acc0);
+          if (!(ok = warp_wait(u_p + 8, phase0))) break;
+          tm_after();
+          issue_o(0, 1, sv, 1u);
+          acc0 = 1u;
+          phase0 ^= 1u;
+          if (!more && leader) commit_to(u_o);
+        }
+        if (more && j - 1 < u_n0) issue_s(0, slot);
+        if (j < u_n1) {
+          if (!(ok = warp_wait(u_p + 16, phase1))) break;
+          tm_after();
+          issue_o(1, 0, sv, acc1);
+          if (!(ok = warp_wait(u_p + 24, phase1))) break;
+          tm_after();
+          issue_o(1, 1, sv, 1u);
+          acc1 = 1u;
+          phase1 ^= 1u;
+          if (!more && leader) commit_to(u_o + 8);
+        }
+        if (more && j - 1 < u_n1) issue_s(1, slot);
+        if (leader) {
+          commit_to(u_empty + 8 * sv);
+          if (more) commit_to(u_empty + 8 * slot);
+        }
+        __syncwarp();
       }
     }
     __syncwarp();
+  }
   } else {
-    const int w = wid >> 2, r = (wid & 3) * 32 + lane;  // row of the tile
-    const int row = r0 + w * TILE + r;                  // of the sequence
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 " RHI ";");
+    // two threads to a row: 64 keys of every tile each
+    const int w = wid >> 3, half = (wid >> 2) & 1, r = (wid & 3) * 32 + lane;
+    const int row = r0 + w * TILE + r;  // of the sequence
     const int cnt = w ? cnt1 : cnt0, top = w ? nt[1] : nt[0];
     const int lim = a.causal ? min(nk, row + off + 1) : nk;  // keys this row sees
     const uint32_t lane_base = (uint32_t)((wid & 3) * 32) << 16;
-    const uint32_t ts = tmem + lane_base + w * 128, to = tmem + lane_base + 256 + w * 128;
+    const uint32_t ts = tmem + lane_base + w * 128, to = tmem + lane_base + 256 + w * 128 + half * (D / 2);
+    float* xch = reinterpret_cast<float*>(sm + SM::BAR_OFF + 256) + w * 2 * TILE;  // row maxima of the two halves
     float m = -INFINITY, l = 0.f;
-    for (int i = 0; i < cnt && ok; ++i) {
-      const int c0 = (top - 1 - i) * TILE;
-      // the output's barrier is waited for in every phase: a parity says nothing about a phase further back
-      ok = warp_wait(b_s + 8 * w, (uint32_t)i & 1u) && (i == 0 || warp_wait(b_o + 8 * w, (uint32_t)(i - 1) & 1u));
-      if (!ok) break;
-      tm_after();
-      float x[TILE];
+    for (int i = 0; i < cnt; ++i) {
+      const int c0 = (top - 1 - i) * TILE + half * (TILE / 2);
+      // S(i) stands for PV(i - 1) too: a commit waits for everything its thread has issued before
+      ok = ok && warp_wait(b_s + 8 * w, (uint32_t)i & 1u);
+      float x[TILE / 2];
+      float top_x = -INFINITY;
+      if (ok) {
+        tm_after();
+        tm_ld32(ts + half * 64, x);
+        tm_ld32(ts + half * 64 + 32, x + 32);
+        tm_wait_ld();
+        if (__any_sync(0xffffffffu, lim < c0 + TILE / 2)) {
 #pragma unroll
-      for (int c = 0; c < TILE; c += 32) tm_ld32(ts + c, x + c);
-      tm_wait_ld();
-      if (__any_sync(0xffffffffu, lim < c0 + TILE)) {
+          for (int c = 0; c < TILE / 2; ++c) x[c] = c0 + c < lim ? x[c] : -INFINITY;
+        }
+        float mx[4] = {max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], x[8]), max3(x[9], x[10], x[11])};
 #pragma unroll
-        for (int c = 0; c < TILE; ++c) x[c] = c0 + c < lim ? x[c] : -INFINITY;
+        for (int c = 12; c < TILE / 2 - 4; c += 8)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], x[c + 2 * k], x[c + 2 * k + 1]);
+        mx[0] = max3(mx[0], x[TILE / 2 - 4], x[TILE / 2 - 3]);
+        mx[1] = max3(mx[1], x[TILE / 2 - 2], x[TILE / 2 - 1]);
+        top_x = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+        xch[half * TILE + r] = top_x;
       }
-      float mx[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-      for (int c = 4; c < TILE; ++c) mx[c & 3] = fmaxf(mx[c & 3], x[c]);
-      const float top_x = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
+      // Both halves know the row's maximum.  Every warp comes here cnt times, also after a wait that ran out.
+      asm volatile("bar.sync %0, 256;\n" ::"r"(1 + w) : "memory");
+      if (!ok) continue;
+      top_x = fmaxf(top_x, xch[(half ^ 1) * TILE + r]) * a.scale_log2;
       if (__any_sync(0xffffffffu, top_x > m + PROMPT_LAZY)) {
         const float m_new = fmaxf(m, top_x);
         const float f = m_new == m ? 1.f : ex2p(m - m_new);
@@ -333,7 +459,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         l *= f;
         if (i > 0) {
 #pragma unroll 1
-          for (int c = 0; c < D; c += 32) {
+          for (int c = 0; c < D / 2; c += 32) {
             float o[32];
             tm_ld32(to + c, o);
             tm_wait_ld();
@@ -344,39 +470,56 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         }
       }
       const float ms = m == -INFINITY ? 0.f : m;
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
-      uint32_t p[TILE / 2];
+      const uint64_t sc2 = pair(a.scale_log2, a.scale_log2), nm2 = pair(-ms, -ms);
+      uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
-      for (int c = 0; c < TILE; c += 2) {
-        const float p0 = ex2p(fmaf(x[c], a.scale_log2, -ms)), p1 = ex2p(fmaf(x[c + 1], a.scale_log2, -ms));
-        sum[(c >> 1) & 3] += p0 + p1;
-        p[c >> 1] = pack2<T>(p0, p1);
+      for (int part = 0; part < 2; ++part) {  // the product over the first part starts while the other is worked out
+        uint32_t p[TILE / 8];
+#pragma unroll
+        for (int c2 = 0; c2 < TILE / 8; ++c2) {
+          const int c = part * (TILE / 4) + 2 * c2;
+          const uint64_t t = fma2(pair(x[c], x[c + 1]), sc2, nm2);
+          float p0, p1;
+          if (c2 % EMULATE == EMULATE - 1) {
+            ex2_pair_fma(t, p0, p1);
+          } else {
+            unpair(t, p0, p1);
+            p0 = ex2p(p0);
+            p1 = ex2p(p1);
+          }
+          sum[c2 & 1] = add2(sum[c2 & 1], pair(p0, p1));
+          p[c2] = pack2<T>(p0, p1);
+        }
+        tm_st16(ts + P_COL(half, part * 2), p);
+        tm_wait_st();
+        tm_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(b_p + 16 * w + 8 * part);
       }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      tm_st32(ts, p);
-      tm_st32(ts + 32, p + 32);
-      tm_wait_st();
-      tm_before();
-      __syncwarp();
-      if (lane == 0) bar_arrive(b_p + 8 * w);
+      float s0, s1;
+      unpair(add2(sum[0], sum[1]), s0, s1);
+      l += s0 + s1;
     }
-    // results
-    if (cnt > 0 && ok) ok = warp_wait(b_o + 8 * w, (uint32_t)(cnt - 1) & 1u);
+    // results: the two halves' sums, half of the channels each
+    if (cnt > 0 && ok) ok = warp_wait(b_o + 8 * w, 0);
     tm_after();
+    xch[half * TILE + r] = l;
+    asm volatile("bar.sync %0, 256;\n" ::"r"(1 + w) : "memory");
+    l += xch[(half ^ 1) * TILE + r];
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const bool mine = row < nq;
     const long long prow = a.padded ? (long long)s * a.max_q + row : (long long)q0 + row;
     const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
-    if (ok && mine) {
+    if (ok && mine && half == 0) {
       if (a.splits > 1)
         a.part_lse[((long long)split * a.rows + prow) * a.Hq + hq] = lse2;
       else if (a.lse)
         a.lse[a.padded ? ((long long)s * a.Hq + hq) * a.max_q + row : hq * a.total_q + prow] = lse2 * 0.6931471805599453f;
     }
-    T* out = static_cast<T*>(a.out) + (a.padded ? s * a.out_stride[0] + row * a.out_stride[2] : prow * a.out_stride[2]) + hq * a.out_stride[1];
-    float* po = a.part_o + (((long long)split * a.rows + prow) * a.Hq + hq) * D;
+    T* out = static_cast<T*>(a.out) + (a.padded ? s * a.out_stride[0] + row * a.out_stride[2] : prow * a.out_stride[2]) + hq * a.out_stride[1] + half * (D / 2);
+    float* po = a.part_o + (((long long)split * a.rows + prow) * a.Hq + hq) * D + half * (D / 2);
 #pragma unroll 1
-    for (int c = 0; c < D && ok; c += 32) {
+    for (int c = 0; c < D / 2 && ok; c += 32) {
       float o[32];
       if (cnt > 0) {  // warp-uniform
         tm_ld32(to + c, o);
