@@ -31,14 +31,6 @@ namespace {
 constexpr int PROMPT_THREADS = 640;  // four softmax warpgroups, one for products and copies (two of its warps idle)
 constexpr int MMA_WARP = 16, LOAD_WARP = 17;
 constexpr int TILE = 128;           // query rows of a tile, keys of a tile
-#ifndef EMU
-#define EMU 1000
-#endif
-#ifndef RLO
-#define RLO "32"
-#define RHI "112"
-#endif
-constexpr int EMULATE = EMU;          // one pair of exponentials in so many runs on the FMA units
 constexpr float PROMPT_LAZY = 8.f;  // log2
 
 struct PromptArgs {
@@ -84,27 +76,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// 2^x on the FMA units for a pair, x >= -126 after the clamp (what is below becomes 2^-126): x = n + f with n the nearest
-// integer (left in the low bits of x + 1.5 * 2^23), 2^f by the degree-5 polynomial of least relative error on
-// [-1/2, 1/2] (1.6e-7, fitted by reweighted least squares), n added to the exponent.
-__device__ __forceinline__ void ex2_pair_fma(uint64_t x, float& e0, float& e1) {
-  float x0, x1;
-  unpair(x, x0, x1);
-  x = pair(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
-  const uint64_t t = add2(x, pair(12582912.f, 12582912.f));
-  const uint64_t n = add2(t, pair(-12582912.f, -12582912.f));
-  const uint64_t f = fma2(n, pair(-1.f, -1.f), x);
-  uint64_t p = fma2(f, pair(0.0013276472454890609f, 0.0013276472454890609f), pair(0.009675541892647743f, 0.009675541892647743f));
-  p = fma2(p, f, pair(0.05550713092088699f, 0.05550713092088699f));
-  p = fma2(p, f, pair(0.24022120237350464f, 0.24022120237350464f));
-  p = fma2(p, f, pair(0.6931469440460205f, 0.6931469440460205f));
-  p = fma2(p, f, pair(1.0000001192092896f, 1.0000001192092896f));
-  float p0, p1, t0, t1;
-  unpair(p, p0, p1);
-  unpair(t, t0, t1);
-  e0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
-  e1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
-}
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 __device__ __forceinline__ bool elect_one() {
   uint32_t p;
@@ -128,6 +99,12 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
     if (done) return true;
   }
   return false;
+}
+__device__ __forceinline__ bool bar_peek(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}\n"
+               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  return done != 0;
 }
 // the same for a whole warp, with one answer
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, bar_wait(bar, parity)); }
@@ -224,8 +201,8 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
   extern __shared__ __align__(1024) unsigned char sm[];  // the swizzle counts from multiples of 1024 bytes
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const uint32_t smb = smem_u32(sm), bars = smb + SM::BAR_OFF;
-  // barriers: Q; ring full / empty; S ready, P ready (both halves), O ready of both tiles; value tail zeroed
-  const uint32_t b_q = bars, b_full = bars + 8, b_empty = b_full + 8 * NS, b_s = b_empty + 8 * NS, b_p = b_s + 16, b_o = b_p + 32,
+  // barriers: Q; ring full / empty; S ready, P ready, O ready of both tiles; value tail zeroed
+  const uint32_t b_q = bars, b_full = bars + 8, b_empty = b_full + 8 * NS, b_s = b_empty + 8 * NS, b_p = b_s + 16, b_o = b_p + 16,
                  b_clean = b_o + 16;
   volatile uint32_t* shared_words = reinterpret_cast<volatile uint32_t*>(sm + SM::BAR_OFF + 224);  // tensor memory, loads issued, failed
   pdl_prologue();
@@ -270,7 +247,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
   if (tid == 0) {
     bar_init(b_q, 1);
     for (int i = 0; i < NS; ++i) { bar_init(b_full + 8 * i, 1); bar_init(b_empty + 8 * i, 1); }
-    for (int w = 0; w < 2; ++w) { bar_init(b_s + 8 * w, 1); bar_init(b_p + 16 * w, 8); bar_init(b_p + 16 * w + 8, 8); bar_init(b_o + 8 * w, 1); }
+    for (int w = 0; w < 2; ++w) { bar_init(b_s + 8 * w, 1); bar_init(b_p + 8 * w, 8); bar_init(b_o + 8 * w, 1); }
     bar_init(b_clean, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     shared_words[1] = 0;
@@ -284,7 +261,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
 
   // registers: 640 x 96 at launch = 512 x 112 + 128 x 32
   if (wid >= MMA_WARP) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 " RLO ";");
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
   if (wid == LOAD_WARP) {
     const int cs = a.padded ? s : 0;
     if (lane == 0 && n_all > 0) {
@@ -335,35 +312,47 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       const uint32_t id_s = base | ((128u >> 3) << 17);                           // both operands K-major
       const uint32_t id_o = base | (1u << 16) | ((uint32_t)(D >> 3) << 17);       // V: channels contiguous (N-major)
       const uint32_t q_lo = desc_lo(u_sm + SM::Q_OFF, 16), k_lo = desc_lo(u_sm + SM::KV_OFF, 16), v_lo = desc_lo(u_sm + SM::KV_OFF, SM::HALF);
-      const uint32_t ub = u_sm + SM::BAR_OFF, u_full = ub + 8, u_empty = u_full + 8 * NS, u_s = u_empty + 8 * NS, u_p = u_s + 16, u_o = u_p + 32;
+      const uint32_t ub = u_sm + SM::BAR_OFF, u_full = ub + 8, u_empty = u_full + 8 * NS, u_s = u_empty + 8 * NS, u_p = u_s + 16, u_o = u_p + 16;
       const bool leader = elect_one();
-      auto issue_s = [&](int w, int slot) {
+      // Half of the products of S, a look at the other tile's P, the other half: the look's latency passes while the tensor
+      // cores have work.  (A wait costs this warp some 90 cycles even when there is nothing to wait for, and the queue
+      // of products is short: with the waits between the products the call took 7 % longer.)
+      bool seen = false;
+      auto issue_s = [&](int w, int slot, uint32_t other_phase) {
         const uint32_t qa = q_lo + w * (SM::TILE_BYTES >> 4), ka = k_lo + slot * (SM::TILE_BYTES >> 4);
-        if (leader) {
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) {
-            const uint32_t o = ((uint32_t)(ks >> 2) * SM::HALF + (ks & 3) * 32) >> 4;
-            mma_ss(u_tm + w * 128, qa + o, ka + o, id_s, ks > 0);
+        for (int part = 0; part < 2; ++part) {
+          if (leader) {
+#pragma unroll
+            for (int ks = part * (D / 32); ks < (part + 1) * (D / 32); ++ks) {
+              const uint32_t o = ((uint32_t)(ks >> 2) * SM::HALF + (ks & 3) * 32) >> 4;
+              mma_ss(u_tm + w * 128, qa + o, ka + o, id_s, ks > 0);
+            }
+            if (part == 1) commit_to(u_s + 8 * w);
           }
-          commit_to(u_s + 8 * w);
+          __syncwarp();
+          if (part == 0) seen = bar_peek(u_p + 8 * (w ^ 1), other_phase);
         }
-        __syncwarp();
       };
-      auto issue_o = [&](int w, int part, int slot, uint32_t acc) {
+      auto p_ready = [&](int w, uint32_t phase) {
+        const bool yes = __all_sync(0xffffffffu, seen) || warp_wait(u_p + 8 * w, phase);
+        seen = false;
+        return yes;
+      };
+      auto issue_o = [&](int w, int slot, uint32_t acc) {
         const uint32_t va = v_lo + slot * (SM::TILE_BYTES >> 4);
         if (leader) {
 #pragma unroll
-          for (int k4 = 0; k4 < TILE / 32; ++k4) {
-            const int half = k4 >> 1, ks = half * 4 + part * 2 + (k4 & 1);  // keys 0-31 and 64-95, then the others
-            mma_ts(u_tm + 256 + w * 128, u_tm + w * 128 + P_COL(half, part * 2 + (k4 & 1)), va + ks * (2048 >> 4), id_o, k4 > 0 ? 1u : acc);
-          }
+          for (int ks = 0; ks < TILE / 16; ++ks)
+            mma_ts(u_tm + 256 + w * 128, u_tm + w * 128 + P_COL(ks >> 2, ks & 3), va + ks * (2048 >> 4), id_o, ks > 0 ? 1u : acc);
         }
         __syncwarp();
       };
       ok = warp_wait(ub, 0) && warp_wait(u_full, 0);
       if (ok) {
-        if (u_n - 1 < u_n0) issue_s(0, 0);
-        if (u_n - 1 < u_n1) issue_s(1, 0);
+        if (u_n - 1 < u_n0) issue_s(0, 0, 0);
+        if (u_n - 1 < u_n1) issue_s(1, 0, 0);
+        seen = false;
         if (leader) commit_to(u_empty);
       }
       int slot = 0;  // ring position and phase
@@ -380,29 +369,23 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         }
         if (!ok) break;
         if (j < u_n0) {
-          if (!(ok = warp_wait(u_p, phase0))) break;
+          if (!(ok = p_ready(0, phase0))) break;
           tm_after();
-          issue_o(0, 0, sv, acc0);
-          if (!(ok = warp_wait(u_p + 8, phase0))) break;
-          tm_after();
-          issue_o(0, 1, sv, 1u);
+          issue_o(0, sv, acc0);
           acc0 = 1u;
           phase0 ^= 1u;
           if (!more && leader) commit_to(u_o);
         }
-        if (more && j - 1 < u_n0) issue_s(0, slot);
+        if (more && j - 1 < u_n0) issue_s(0, slot, phase1);
         if (j < u_n1) {
-          if (!(ok = warp_wait(u_p + 16, phase1))) break;
+          if (!(ok = p_ready(1, phase1))) break;
           tm_after();
-          issue_o(1, 0, sv, acc1);
-          if (!(ok = warp_wait(u_p + 24, phase1))) break;
-          tm_after();
-          issue_o(1, 1, sv, 1u);
+          issue_o(1, sv, acc1);
           acc1 = 1u;
           phase1 ^= 1u;
           if (!more && leader) commit_to(u_o + 8);
         }
-        if (more && j - 1 < u_n1) issue_s(1, slot);
+        if (more && j - 1 < u_n1) issue_s(1, slot, phase0);
         if (leader) {
           commit_to(u_empty + 8 * sv);
           if (more) commit_to(u_empty + 8 * slot);
@@ -413,7 +396,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
     __syncwarp();
   }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 " RHI ";");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
     // two threads to a row: 64 keys of every tile each
     const int w = wid >> 3, half = (wid >> 2) & 1, r = (wid & 3) * 32 + lane;
     const int row = r0 + w * TILE + r;  // of the sequence
@@ -473,29 +456,24 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       const uint64_t sc2 = pair(a.scale_log2, a.scale_log2), nm2 = pair(-ms, -ms);
       uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
-      for (int part = 0; part < 2; ++part) {  // the product over the first part starts while the other is worked out
+      for (int part = 0; part < 2; ++part) {
         uint32_t p[TILE / 8];
 #pragma unroll
         for (int c2 = 0; c2 < TILE / 8; ++c2) {
           const int c = part * (TILE / 4) + 2 * c2;
-          const uint64_t t = fma2(pair(x[c], x[c + 1]), sc2, nm2);
           float p0, p1;
-          if (c2 % EMULATE == EMULATE - 1) {
-            ex2_pair_fma(t, p0, p1);
-          } else {
-            unpair(t, p0, p1);
-            p0 = ex2p(p0);
-            p1 = ex2p(p1);
-          }
+          unpair(fma2(pair(x[c], x[c + 1]), sc2, nm2), p0, p1);
+          p0 = ex2p(p0);
+          p1 = ex2p(p1);
           sum[c2 & 1] = add2(sum[c2 & 1], pair(p0, p1));
           p[c2] = pack2<T>(p0, p1);
         }
         tm_st16(ts + P_COL(half, part * 2), p);
-        tm_wait_st();
-        tm_before();
-        __syncwarp();
-        if (lane == 0) bar_arrive(b_p + 16 * w + 8 * part);
       }
+      tm_wait_st();
+      tm_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(b_p + 8 * w);
       float s0, s1;
       unpair(add2(sum[0], sum[1]), s0, s1);
       l += s0 + s1;
