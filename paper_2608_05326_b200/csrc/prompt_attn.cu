@@ -2,17 +2,22 @@
 //
 //     S = Q K^T,  P = 2^(S * scale * log2 e - m),  O += P V,  out = O / sum P,  lse = ln sum exp(scale * S)
 //
-// One CTA takes 256 query rows of one head as two tiles of 128 and walks the keys in tiles of 128, last tile first.
-// Ten warps: four per query tile for the softmax (a thread owns a row: no shuffles), one that issues the products, one
-// that issues the copies.
+// A work item is 256 query rows of one head, as two tiles of 128, against the keys in tiles of 128, last tile first.  A CTA
+// stays on its SM and takes over grid positions that have not started (the hardware hands them out), so that one item's
+// start and results run beside another's products.  Twenty warps: eight for each query tile's softmax (two threads to a
+// row), one that issues the products, one that issues the copies, one that fetches work items.
 //   - Q, K, V tiles come by TMA (boxes of 64 channels x 128 tokens, 128-byte swizzle); K and V share a ring.
 //   - S (128 x 128 fp32) and O (128 x d fp32) of both tiles fill the 512 columns of tensor memory.  P goes back over S
 //     in 16 bits and is the A operand of the second product from there.
 //   - While one tile's warps are in their softmax, the tensor cores work on the other tile's products.
 //   - The reference exponent m of a row moves only when a logit exceeds it by 2^8 (then O is rescaled in tensor
 //     memory); P is at most 2^8, sums are float32.
-// At d = 128 a key tile costs both query tiles 2 x 1024 tensor-core cycles and 2 x 1024 cycles of the exponential
-// unit (16 a cycle): the call is bound by the two together.
+// What bounds it: at d = 128 a key tile costs both query tiles 2048 tensor-core cycles at best; with both operands of S in
+// shared memory the products alone take about 2750 (8 KB of operands for 64 cycles of products, at 128 bytes a cycle, and
+// the copies write through the same port), and a step takes about 3600 with the softmax behind it.  Measured: causal 32768
+// tokens x 32 heads 7.4 ms (1190 TFLOP/s, 0.70 of the measured burst rate, 0.84 of the sustained one).  Shares of the
+// exponentials as polynomials on the FMA units were slower at every share (1/2 to 1/16): what the softmax waits for is
+// issue and hand-over, not the exponential unit.
 //
 // Few query rows (one token, a short piece behind a long prefix): the keys are split over several CTAs whose partial
 // outputs prompt_merge_kernel joins.
@@ -28,8 +33,8 @@ namespace qevict {
 
 namespace {
 
-constexpr int PROMPT_THREADS = 640;  // four softmax warpgroups, one for products and copies (two of its warps idle)
-constexpr int MMA_WARP = 16, LOAD_WARP = 17;
+constexpr int PROMPT_THREADS = 640;  // four softmax warpgroups, one for products, copies and work items (a warp idle)
+constexpr int MMA_WARP = 16, LOAD_WARP = 17, ITEM_WARP = 18;
 constexpr int TILE = 128;           // query rows of a tile, keys of a tile
 constexpr float PROMPT_LAZY = 8.f;  // log2
 
@@ -91,8 +96,9 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar) {
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
-  for (uint32_t it = 0; it < (1u << 20); ++it) {
+// LONG: what is waited for may take as long as a whole work item.
+template <bool LONG = false> __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
+  for (uint32_t it = 0; it < (LONG ? 1u << 26 : 1u << 20); ++it) {
     uint32_t done;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}\n"
                  : "=r"(done) : "r"(bar), "r"(parity) : "memory");
@@ -107,7 +113,9 @@ __device__ __forceinline__ bool bar_peek(uint32_t bar, uint32_t parity) {
   return done != 0;
 }
 // the same for a whole warp, with one answer
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, bar_wait(bar, parity)); }
+template <bool LONG = false> __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) {
+  return __all_sync(0xffffffffu, bar_wait<LONG>(bar, parity));
+}
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int tok, int head, int seq) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
                ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(tok), "r"(head), "r"(seq) : "memory");
@@ -143,20 +151,22 @@ __device__ __forceinline__ void tm_ld32(uint32_t addr, float* v) {
       : "r"(addr)
       : "memory");
 }
-__device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* u) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
-      "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};\n" ::"r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]),
-      "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]),
-      "r"(u[15]), "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]), "r"(u[20]), "r"(u[21]), "r"(u[22]), "r"(u[23]), "r"(u[24]),
-      "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]), "r"(u[30]), "r"(u[31]), "r"(addr)
-      : "memory");
+__device__ __forceinline__ void tm_ld8(uint32_t addr, float* v) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(v);
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n"
+               : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void tm_st16(uint32_t addr, const uint32_t* u) {
+__device__ __forceinline__ void tm_st8(uint32_t addr, const uint32_t* u) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};\n" ::"r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]),
+               "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tm_ld16(uint32_t addr, float* v) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(v);
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};\n" ::"r"(u[0]),
-      "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]),
-      "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(addr)
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
+        "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+      : "r"(addr)
       : "memory");
 }
 __device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -189,8 +199,48 @@ template <int D> struct PromptSmem {
   static constexpr int HALF = TILE * 128;             // 64 channels of 128 rows
   static constexpr int TILE_BYTES = HALF * (D / 64);
   static constexpr int Q_OFF = 0, KV_OFF = 2 * TILE_BYTES, BAR_OFF = KV_OFF + STAGES * TILE_BYTES;
-  static constexpr int BYTES = BAR_OFF + 256 + 2048;  // barriers, row maxima
+  static constexpr int WORDS = 256, ITEMS = 384, ROWS = 512;  // behind the barriers: words, work items, row maxima
+  static constexpr int BYTES = BAR_OFF + ROWS + 2048;
 };
+
+// A work item: 256 query rows of one head of one sequence, or a part of their keys.
+struct PromptItem {
+  int valid, hq, s, split, r0, q0, nq, k0, nk;
+  int lo, n;       // key tiles of this item
+  int nt0, nt1;    // end of the two query tiles' key tiles
+  __device__ __forceinline__ int cnt(int w) const { return max(0, (w ? nt1 : nt0) - lo); }
+  __device__ __forceinline__ bool dirty() const { return n > lo && n * TILE > nk; }  // the first tile reaches past the sequence
+};
+
+// The item of grid position (x, y, z); not valid where the sequence has no such rows.
+__device__ __forceinline__ PromptItem item_of(const PromptArgs& a, int x, int y, int z) {
+  PromptItem it;
+  const int m_tiles = (a.max_q + 2 * TILE - 1) / (2 * TILE), mt = x / a.splits;
+  it.split = x - mt * a.splits;
+  it.r0 = (a.causal ? m_tiles - 1 - mt : mt) * 2 * TILE;  // the longest rows first
+  it.hq = y;
+  it.s = z;
+  span_of(a.q_bounds, a.padded, z, a.max_q, a.total_q, &it.q0, &it.nq);
+  span_of(a.k_bounds, a.padded, z, a.max_k, a.total_k, &it.k0, &it.nk);
+  it.valid = it.r0 < it.nq;
+  int nt[2];
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    const int rw = it.r0 + w * TILE, last = min(rw + TILE, it.nq) - 1;
+    const int lim = rw >= it.nq ? 0 : (a.causal ? min(it.nk, last + it.nk - it.nq + 1) : it.nk);
+    nt[w] = lim > 0 ? (lim + TILE - 1) / TILE : 0;
+  }
+  it.lo = 0;
+  it.n = max(nt[0], nt[1]);
+  if (a.splits > 1) {
+    const int per = (it.n + a.splits - 1) / a.splits;
+    it.lo = min(it.n, it.split * per);
+    it.n = min(it.n, it.lo + per);
+  }
+  it.nt0 = min(nt[0], it.n);
+  it.nt1 = min(nt[1], it.n);
+  return it;
+}
 
 template <class T, int D>
 __global__ void __launch_bounds__(PROMPT_THREADS, 1)
@@ -201,112 +251,157 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
   extern __shared__ __align__(1024) unsigned char sm[];  // the swizzle counts from multiples of 1024 bytes
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const uint32_t smb = smem_u32(sm), bars = smb + SM::BAR_OFF;
-  // barriers: Q; ring full / empty; S ready, P ready, O ready of both tiles; value tail zeroed
+  // barriers: Q full / empty; ring full / empty; S ready, P ready, O ready of both tiles; value tail zeroed; work items
+  // full / empty (two places); answer to the request for the next one
   const uint32_t b_q = bars, b_full = bars + 8, b_empty = b_full + 8 * NS, b_s = b_empty + 8 * NS, b_p = b_s + 16, b_o = b_p + 16,
-                 b_clean = b_o + 16;
-  volatile uint32_t* shared_words = reinterpret_cast<volatile uint32_t*>(sm + SM::BAR_OFF + 224);  // tensor memory, loads issued, failed
-  pdl_prologue();
-
-  const int m_tiles = (a.max_q + 2 * TILE - 1) / (2 * TILE);
-  const int split = blockIdx.x % a.splits, mt_raw = blockIdx.x / a.splits;
-  const int mt = a.causal ? m_tiles - 1 - mt_raw : mt_raw;  // the longest rows first
-  const int hq = blockIdx.y, s = blockIdx.z, hk = hq / (a.Hq / a.Hkv);
-  int q0, nq, k0, nk;
-  span_of(a.q_bounds, a.padded, s, a.max_q, a.total_q, &q0, &nq);
-  span_of(a.k_bounds, a.padded, s, a.max_k, a.total_k, &k0, &nk);
-  const int r0 = mt * 2 * TILE, off = nk - nq;
-  if (r0 >= nq) return;
+                 b_clean = b_o + 16, b_qe = b_clean + 8, b_item = b_qe + 8, b_taken = b_item + 16, b_next = b_taken + 16;
+  // words: 0 .. 3 the answer; 4 tensor memory; 5 loads issued; 6 failed; 8 .. 23 softmax warps that gave up
+  volatile uint32_t* words = reinterpret_cast<volatile uint32_t*>(sm + SM::BAR_OFF + SM::WORDS);
+  PromptItem* items = reinterpret_cast<PromptItem*>(sm + SM::BAR_OFF + SM::ITEMS);
+  static_assert(sizeof(PromptItem) * 2 <= 128, "two work items");
   if (smb & 1023u) {  // no tile would be where the products look for it
     kv8_record(a.status, CHECK_ALIGNMENT);
     return;
   }
-  // key tiles of the two query tiles, and this CTA's part of them
-  int nt[2];
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    const int rw = r0 + w * TILE, last = min(rw + TILE, nq) - 1;
-    const int lim = rw >= nq ? 0 : (a.causal ? min(nk, last + off + 1) : nk);
-    nt[w] = lim > 0 ? (lim + TILE - 1) / TILE : 0;
-  }
-  int lo = 0, n = max(nt[0], nt[1]);
-  if (a.splits > 1) {
-    const int per = (n + a.splits - 1) / a.splits;
-    lo = min(n, split * per);
-    n = min(n, lo + per);
-    nt[0] = min(nt[0], n);
-    nt[1] = min(nt[1], n);
-  }
-  const int cnt0 = max(0, nt[0] - lo), cnt1 = max(0, nt[1] - lo);
-  const int n_all = n - lo;  // tiles that are loaded
-  const bool dirty = n_all > 0 && n * TILE > nk;  // the first tile reaches past the sequence
-
   if (wid == MMA_WARP) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((void*)shared_words)), "r"(512u) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((void*)(words + 4))), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (tid == 0) {
     bar_init(b_q, 1);
+    bar_init(b_qe, 1);
     for (int i = 0; i < NS; ++i) { bar_init(b_full + 8 * i, 1); bar_init(b_empty + 8 * i, 1); }
-    for (int w = 0; w < 2; ++w) { bar_init(b_s + 8 * w, 1); bar_init(b_p + 8 * w, 8); bar_init(b_o + 8 * w, 1); }
+    for (int w = 0; w < 2; ++w) {
+      bar_init(b_s + 8 * w, 1);
+      bar_init(b_p + 8 * w, 8);
+      bar_init(b_o + 8 * w, 1);
+      bar_init(b_item + 8 * w, 1);
+      bar_init(b_taken + 8 * w, 18);
+    }
     bar_init(b_clean, 1);
+    bar_init(b_next, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    shared_words[1] = 0;
-    shared_words[2] = 0;
+    for (int i = 5; i < 24; ++i) words[i] = 0;
   }
   tm_before();
   __syncthreads();
   tm_after();
-  const uint32_t tmem = shared_words[0];
+  const uint32_t tmem = words[4];
+  pdl_prologue();
   bool ok = true;
+
+  // The next item, in the place that the item warp fills; the one before is given back.  No item on failure.
+  int taken = 0;
+  auto next_item = [&]() -> const PromptItem* {
+    if (taken > 0) {
+      __syncwarp();
+      if (lane == 0) bar_arrive(b_taken + 8 * ((taken - 1) & 1));
+    }
+    const int place = taken & 1;
+    ok = ok && warp_wait(b_item + 8 * place, (uint32_t)(taken >> 1) & 1u);
+    ++taken;
+    return ok && items[place].valid ? &items[place] : nullptr;
+  };
 
   // registers: 640 x 96 at launch = 512 x 112 + 128 x 32
   if (wid >= MMA_WARP) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
-  if (wid == LOAD_WARP) {
-    const int cs = a.padded ? s : 0;
-    if (lane == 0 && n_all > 0) {
-      bar_expect(b_q, (uint32_t)((cnt0 > 0) + (cnt1 > 0)) * SM::TILE_BYTES);
-#pragma unroll
-      for (int w = 0; w < 2; ++w)
-        if ((w ? cnt1 : cnt0) > 0)
-          for (int x = 0; x < D / 64; ++x)
-            tma_load(smb + SM::Q_OFF + w * SM::TILE_BYTES + x * SM::HALF, &mq, b_q, x * 64, q0 + r0 + w * TILE, hq, cs);
-    }
-    const int loads = 2 * n_all, clean_at = min(NS, loads) - 1;
-    for (int it = 0; it < loads && ok; ++it) {  // K, V of the last tile, K, V of the one before, ...
-      const int slot = it % NS, j = n - 1 - (it >> 1);
-      if (it >= NS) ok = warp_wait(b_empty + 8 * slot, (uint32_t)(it / NS - 1) & 1u);
-      if (ok && lane == 0) {
-        bar_expect(b_full + 8 * slot, SM::TILE_BYTES);
-        for (int x = 0; x < D / 64; ++x)
-          tma_load(smb + SM::KV_OFF + slot * SM::TILE_BYTES + x * SM::HALF, (it & 1) ? &mv : &mk, b_full + 8 * slot, x * 64, k0 + j * TILE, hk, cs);
-        shared_words[1] = it + 1;
-      }
-      if (ok && dirty && it == clean_at) {  // zero the value rows past the end
-        ok = warp_wait(b_full + 8, 0);
-        const int from = nk - (n - 1) * TILE;
-        if (ok) {
-          for (int i = lane; i < (TILE - from) * 8 * (D / 64); i += 32) {
-            const int x = i / ((TILE - from) * 8), k = i - x * (TILE - from) * 8;
-            *reinterpret_cast<uint4*>(sm + SM::KV_OFF + SM::TILE_BYTES + x * SM::HALF + from * 128 + k * 16) = make_uint4(0u, 0u, 0u, 0u);
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+    if (wid == ITEM_WARP) {
+      // Work items: the CTA's own grid position first, then positions that have not started, taken over one at a time
+      // while the item before is in work.  (A grid of single-item CTAs pays for start, first loads and results of every
+      // item with idle tensor cores: 12 packed prompts of up to 4001 tokens took 620 us.)
+      int x = blockIdx.x, y = blockIdx.y, z = blockIdx.z, put = 0;
+      for (uint32_t ask = 0; ok; ++ask) {
+        if (lane == 0) {
+          bar_expect(b_next, 16);
+          asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                           smem_u32((void*)words)), "r"(b_next) : "memory");
+        }
+        const PromptItem it = item_of(a, x, y, z);
+        if (it.valid) {
+          if (put >= 2) ok = warp_wait<true>(b_taken + 8 * (put & 1), (uint32_t)((put >> 1) - 1) & 1u);
+          if (ok && lane == 0) {
+            items[put & 1] = it;
+            bar_arrive(b_item + 8 * (put & 1));
           }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          ++put;
+        }
+        __syncwarp();
+        if (!warp_wait(b_next, ask & 1u)) { ok = false; break; }
+        uint32_t got;
+        asm volatile(
+            "{\n\t.reg .b128 c;\n\t.reg .pred q;\n\tld.shared.b128 c, [%4];\n\t"
+            "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 q, c;\n\tselp.u32 %0, 1, 0, q;\n\t"
+            "mov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t"
+            "@q clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, %2, %3, _}, c;\n\t}\n"
+            : "=r"(got), "=r"(x), "=r"(y), "=r"(z) : "r"(smem_u32((void*)words)) : "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the answer is read before the next one is written
+        __syncwarp();
+        if (!got) break;
+      }
+      // no more items (after a failure too: whoever still listens learns it from here or from its own limit)
+      if (put >= 2) warp_wait<true>(b_taken + 8 * (put & 1), (uint32_t)((put >> 1) - 1) & 1u);
+      if (lane == 0) {
+        items[put & 1].valid = 0;
+        bar_arrive(b_item + 8 * (put & 1));
+      }
+    } else if (wid == LOAD_WARP) {
+      int slot = 0, q_turn = 0, issued = 0;
+      uint32_t phase = 0;
+      while (const PromptItem* item = next_item()) {
+        const PromptItem& it = *item;
+        const int cs = a.padded ? it.s : 0, loads = 2 * (it.n - it.lo), hk = it.hq / (a.Hq / a.Hkv);
+        if (loads == 0) continue;
+        if (q_turn > 0) ok = warp_wait<true>(b_qe, (uint32_t)(q_turn - 1) & 1u);
+        ++q_turn;
+        if (ok && lane == 0) {
+          bar_expect(b_q, (uint32_t)((it.cnt(0) > 0) + (it.cnt(1) > 0)) * SM::TILE_BYTES);
+#pragma unroll
+          for (int w = 0; w < 2; ++w)
+            if (it.cnt(w) > 0)
+              for (int x = 0; x < D / 64; ++x)
+                tma_load(smb + SM::Q_OFF + w * SM::TILE_BYTES + x * SM::HALF, &mq, b_q, x * 64, it.q0 + it.r0 + w * TILE, it.hq, cs);
+          words[7] = 1;
+        }
+        int v_slot = 0;
+        uint32_t v_phase = 0;
+        for (int i = 0; i < loads && ok; ++i) {  // K, V of the last tile, K, V of the one before, ...
+          const int j = it.n - 1 - (i >> 1);
+          if (issued >= NS) ok = warp_wait<true>(b_empty + 8 * slot, phase ^ 1u);
+          if (ok && lane == 0) {
+            bar_expect(b_full + 8 * slot, SM::TILE_BYTES);
+            for (int x = 0; x < D / 64; ++x)
+              tma_load(smb + SM::KV_OFF + slot * SM::TILE_BYTES + x * SM::HALF, (i & 1) ? &mv : &mk, b_full + 8 * slot, x * 64, it.k0 + j * TILE, hk, cs);
+            words[5] = issued + 1;
+          }
+          ++issued;
+          if (i == 1) { v_slot = slot; v_phase = phase; }
+          if (++slot == NS) { slot = 0; phase ^= 1u; }
+          if (ok && i == min(3, loads) - 1 && it.dirty()) {  // zero the value rows past the end
+            ok = warp_wait(b_full + 8 * v_slot, v_phase);
+            const int from = it.nk - (it.n - 1) * TILE, per = (TILE - from) * 8;
+            if (ok) {
+              unsigned char* v0 = sm + SM::KV_OFF + v_slot * SM::TILE_BYTES + from * 128;
+              for (int k = lane; k < per * (D / 64); k += 32) {
+                const int x = k / per;
+                *reinterpret_cast<uint4*>(v0 + x * SM::HALF + (k - x * per) * 16) = make_uint4(0u, 0u, 0u, 0u);
+              }
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+              if (lane == 0) bar_arrive(b_clean);
+            }
+          }
           __syncwarp();
-          if (lane == 0) bar_arrive(b_clean);
         }
       }
-      __syncwarp();
-    }
-  } else if (wid == MMA_WARP) {
-    // One thread issues every product, in the order S0 S1 | PV0 S0 PV1 S1 | ...: while one tile's softmax runs, the tensor
-    // cores have the other tile's products.  S of the next tile overwrites P: one thread's products run in the order of
-    // their issue.  (Two threads, one per tile, were slower, 9.8 against 8.4 ms on 32k tokens x 32 heads: their products
-    // interleave, and both tiles wait for the slower.)
-    // The whole warp walks the loop and one elected lane issues: what the products take (addresses, descriptors) is then
-    // the same for all lanes and stays in uniform registers, which is where the instruction wants it.
-    const int u_n = uniform(n), u_lo = uniform(lo), u_n0 = uniform(nt[0]), u_n1 = uniform(nt[1]);
-    const uint32_t u_tm = (uint32_t)uniform((int)tmem), u_sm = (uint32_t)uniform((int)smb);
-    if (u_n > u_lo) {
+    } else if (wid == MMA_WARP) {
+      // One thread issues every product, in the order S0 S1 | PV0 S0 PV1 S1 | ...: while one tile's softmax runs, the tensor
+      // cores have the other tile's products.  S of the next tile overwrites P: one thread's products run in the order of
+      // their issue.  (Two threads, one per tile, were slower, 9.8 against 8.4 ms on 32k tokens x 32 heads: their products
+      // interleave, and both tiles wait for the slower.)
+      // The whole warp walks the loop and one elected lane issues: what the products take (addresses, descriptors) is then
+      // the same for all lanes and stays in uniform registers, which is where the instruction wants it.
+      const uint32_t u_tm = (uint32_t)uniform((int)tmem), u_sm = (uint32_t)uniform((int)smb);
       const uint32_t fmt = Tr<T>::MAGIC == 0x64006400u ? 0u : 1u;  // 0 = fp16, 1 = bf16
       const uint32_t base = (1u << 4) | (fmt << 7) | (fmt << 10) | ((128u >> 4) << 24);
       const uint32_t id_s = base | ((128u >> 3) << 17);                           // both operands K-major
@@ -348,186 +443,215 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         }
         __syncwarp();
       };
-      ok = warp_wait(ub, 0) && warp_wait(u_full, 0);
-      if (ok) {
-        if (u_n - 1 < u_n0) issue_s(0, 0, 0);
-        if (u_n - 1 < u_n1) issue_s(1, 0, 0);
-        seen = false;
-        if (leader) commit_to(u_empty);
-      }
       int slot = 0;  // ring position and phase
-      uint32_t phase = 0, phase0 = 0, phase1 = 0, acc0 = 0, acc1 = 0;
-      for (int j = u_n - 1; j >= u_lo && ok; --j) {
-        if (++slot == NS) { slot = 0; phase ^= 1u; }
-        const int sv = slot;
-        ok = warp_wait(u_full + 8 * sv, phase);  // V(j)
-        if (ok && j == u_n - 1 && dirty) ok = warp_wait(b_clean, 0);
-        const bool more = j > u_lo;
-        if (more) {
-          if (++slot == NS) { slot = 0; phase ^= 1u; }
-          ok = ok && warp_wait(u_full + 8 * slot, phase);  // K(j - 1)
-        }
-        if (!ok) break;
-        if (j < u_n0) {
-          if (!(ok = p_ready(0, phase0))) break;
-          tm_after();
-          issue_o(0, sv, acc0);
-          acc0 = 1u;
-          phase0 ^= 1u;
-          if (!more && leader) commit_to(u_o);
-        }
-        if (more && j - 1 < u_n0) issue_s(0, slot, phase1);
-        if (j < u_n1) {
-          if (!(ok = p_ready(1, phase1))) break;
-          tm_after();
-          issue_o(1, sv, acc1);
-          acc1 = 1u;
-          phase1 ^= 1u;
-          if (!more && leader) commit_to(u_o + 8);
-        }
-        if (more && j - 1 < u_n1) issue_s(1, slot, phase0);
+      uint32_t phase = 0, phase0 = 0, phase1 = 0, q_phase = 0, clean_phase = 0;
+      while (const PromptItem* item = next_item()) {
+        const PromptItem& it = *item;
+        const int u_n = uniform(it.n), u_lo = uniform(it.lo), u_n0 = uniform(it.nt0), u_n1 = uniform(it.nt1);
+        if (u_n <= u_lo) continue;
+        const bool dirty = it.dirty();
+        if (!(ok = warp_wait(ub, q_phase) && warp_wait(u_full + 8 * slot, phase))) break;
+        q_phase ^= 1u;
+        if (u_n - 1 < u_n0) issue_s(0, slot, phase1);
+        if (u_n - 1 < u_n1) issue_s(1, slot, phase0);
+        seen = false;
         if (leader) {
-          commit_to(u_empty + 8 * sv);
-          if (more) commit_to(u_empty + 8 * slot);
+          commit_to(u_empty + 8 * slot);
+          if (u_n - 1 == u_lo) commit_to(b_qe);
         }
         __syncwarp();
+        if (++slot == NS) { slot = 0; phase ^= 1u; }
+        uint32_t acc0 = 0, acc1 = 0;
+        for (int j = u_n - 1; j >= u_lo; --j) {
+          const int sv = slot;
+          ok = warp_wait(u_full + 8 * sv, phase);  // V(j)
+          if (++slot == NS) { slot = 0; phase ^= 1u; }
+          if (ok && j == u_n - 1 && dirty) {
+            ok = warp_wait(b_clean, clean_phase);
+            clean_phase ^= 1u;
+          }
+          const bool more = j > u_lo;
+          if (more) ok = ok && warp_wait(u_full + 8 * slot, phase);  // K(j - 1)
+          if (!ok) break;
+          if (j < u_n0) {
+            if (!(ok = p_ready(0, phase0))) break;
+            tm_after();
+            issue_o(0, sv, acc0);
+            acc0 = 1u;
+            phase0 ^= 1u;
+            if (!more && leader) commit_to(u_o);
+          }
+          if (more && j - 1 < u_n0) issue_s(0, slot, phase1);
+          if (j < u_n1) {
+            if (!(ok = p_ready(1, phase1))) break;
+            tm_after();
+            issue_o(1, sv, acc1);
+            acc1 = 1u;
+            phase1 ^= 1u;
+            if (!more && leader) commit_to(u_o + 8);
+          }
+          if (more && j - 1 < u_n1) issue_s(1, slot, phase0);
+          if (leader) {
+            commit_to(u_empty + 8 * sv);
+            if (more) commit_to(u_empty + 8 * slot);
+            if (j - 1 == u_lo) commit_to(b_qe);  // the last S
+          }
+          __syncwarp();
+          if (more && ++slot == NS) { slot = 0; phase ^= 1u; }
+        }
+        seen = false;
+        if (!ok) break;
       }
     }
-    __syncwarp();
-  }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
-    // two threads to a row: 64 keys of every tile each
+    // Two threads to a row: 64 keys of every tile each.  The two warps that share rows meet at a barrier of their own,
+    // where each also says whether a wait of its has run out, so that both leave at the same point.
     const int w = wid >> 3, half = (wid >> 2) & 1, r = (wid & 3) * 32 + lane;
-    const int row = r0 + w * TILE + r;  // of the sequence
-    const int cnt = w ? cnt1 : cnt0, top = w ? nt[1] : nt[0];
-    const int lim = a.causal ? min(nk, row + off + 1) : nk;  // keys this row sees
     const uint32_t lane_base = (uint32_t)((wid & 3) * 32) << 16;
     const uint32_t ts = tmem + lane_base + w * 128, to = tmem + lane_base + 256 + w * 128 + half * (D / 2);
-    float* xch = reinterpret_cast<float*>(sm + SM::BAR_OFF + 256) + w * 2 * TILE;  // row maxima of the two halves
-    float m = -INFINITY, l = 0.f;
-    for (int i = 0; i < cnt; ++i) {
-      const int c0 = (top - 1 - i) * TILE + half * (TILE / 2);
-      // S(i) stands for PV(i - 1) too: a commit waits for everything its thread has issued before
-      ok = ok && warp_wait(b_s + 8 * w, (uint32_t)i & 1u);
-      float x[TILE / 2];
-      float top_x = -INFINITY;
-      if (ok) {
-        tm_after();
-        tm_ld32(ts + half * 64, x);
-        tm_ld32(ts + half * 64 + 32, x + 32);
-        tm_wait_ld();
-        if (__any_sync(0xffffffffu, lim < c0 + TILE / 2)) {
+    float* xch = reinterpret_cast<float*>(sm + SM::BAR_OFF + SM::ROWS) + w * 2 * TILE + r;  // the two halves' values of a row
+    auto meet = [&] {
+      if (!ok) words[8 + wid] = 1;
+      asm volatile("bar.sync %0, 64;\n" ::"r"(1 + w * 4 + (wid & 3)) : "memory");
+      ok = ok && words[8 + (wid ^ 4)] == 0;
+    };
+    uint32_t s_phase = 0, o_phase = 0;
+    while (true) {
+      const PromptItem* item = next_item();
+      meet();
+      if (!ok || !item) break;
+      const PromptItem& it = *item;
+      const int cnt = it.cnt(w);
+      // keys that this row still sees from the tile's (this half's) first on; grows by a tile each time
+      int left = (a.causal ? min(it.nk, it.r0 + w * TILE + r + it.nk - it.nq + 1) : it.nk) - ((w ? it.nt1 : it.nt0) - 1) * TILE - half * (TILE / 2);
+      float m = -INFINITY, l = 0.f;
+      for (int i = cnt; i > 0; --i, left += TILE) {
+        // S(j) stands for P V of the tile before too: a commit waits for everything its thread has issued before
+        ok = warp_wait(b_s + 8 * w, s_phase);
+        s_phase ^= 1u;
+        float x[TILE / 2];
+        if (ok) {
+          tm_after();
+          tm_ld32(ts + half * 64, x);
+          tm_ld32(ts + half * 64 + 32, x + 32);
+          tm_wait_ld();
+          if (__any_sync(0xffffffffu, left < TILE / 2)) {
 #pragma unroll
-          for (int c = 0; c < TILE / 2; ++c) x[c] = c0 + c < lim ? x[c] : -INFINITY;
+            for (int c = 0; c < TILE / 2; ++c) x[c] = c < left ? x[c] : -INFINITY;
+          }
+          float mx[4] = {max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], x[8]), max3(x[9], x[10], x[11])};
+#pragma unroll
+          for (int c = 12; c < TILE / 2 - 4; c += 8)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], x[c + 2 * k], x[c + 2 * k + 1]);
+          mx[0] = max3(mx[0], x[TILE / 2 - 4], x[TILE / 2 - 3]);
+          mx[1] = max3(mx[1], x[TILE / 2 - 2], x[TILE / 2 - 1]);
+          xch[half * TILE] = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
         }
-        float mx[4] = {max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], x[8]), max3(x[9], x[10], x[11])};
-#pragma unroll
-        for (int c = 12; c < TILE / 2 - 4; c += 8)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], x[c + 2 * k], x[c + 2 * k + 1]);
-        mx[0] = max3(mx[0], x[TILE / 2 - 4], x[TILE / 2 - 3]);
-        mx[1] = max3(mx[1], x[TILE / 2 - 2], x[TILE / 2 - 1]);
-        top_x = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
-        xch[half * TILE + r] = top_x;
-      }
-      // Both halves know the row's maximum.  Every warp comes here cnt times, also after a wait that ran out.
-      asm volatile("bar.sync %0, 256;\n" ::"r"(1 + w) : "memory");
-      if (!ok) continue;
-      top_x = fmaxf(top_x, xch[(half ^ 1) * TILE + r]) * a.scale_log2;
-      if (__any_sync(0xffffffffu, top_x > m + PROMPT_LAZY)) {
-        const float m_new = fmaxf(m, top_x);
-        const float f = m_new == m ? 1.f : ex2p(m - m_new);
-        m = m_new;
-        l *= f;
-        if (i > 0) {
+        meet();
+        if (!ok) break;
+        const float top_x = fmaxf(xch[0], xch[TILE]) * a.scale_log2;
+        if (__any_sync(0xffffffffu, top_x > m + PROMPT_LAZY)) {
+          const float m_new = fmaxf(m, top_x);
+          const float f = m_new == m ? 1.f : ex2p(m - m_new);
+          m = m_new;
+          l *= f;
+          if (i < cnt) {
 #pragma unroll 1
-          for (int c = 0; c < D / 2; c += 32) {
-            float o[32];
-            tm_ld32(to + c, o);
-            tm_wait_ld();
+            for (int c = 0; c < D / 2; c += 8) {  // few at a time: the logits stay in registers
+              float o[8];
+              tm_ld8(to + c, o);
+              tm_wait_ld();
 #pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] *= f;
-            tm_st32(to + c, reinterpret_cast<const uint32_t*>(o));
+              for (int k = 0; k < 8; ++k) o[k] *= f;
+              tm_st8(to + c, reinterpret_cast<const uint32_t*>(o));
+            }
           }
         }
-      }
-      const float ms = m == -INFINITY ? 0.f : m;
-      const uint64_t sc2 = pair(a.scale_log2, a.scale_log2), nm2 = pair(-ms, -ms);
-      uint64_t sum[2] = {0ull, 0ull};
+        const float ms = m == -INFINITY ? 0.f : -m;
+        uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
-      for (int part = 0; part < 2; ++part) {
-        uint32_t p[TILE / 8];
+        for (int q = 0; q < 4; ++q) {  // P of 16 keys at a time: what else is live fits the registers (a spill here costs 30 to 60 %)
+          uint32_t p[8];
 #pragma unroll
-        for (int c2 = 0; c2 < TILE / 8; ++c2) {
-          const int c = part * (TILE / 4) + 2 * c2;
-          float p0, p1;
-          unpair(fma2(pair(x[c], x[c + 1]), sc2, nm2), p0, p1);
-          p0 = ex2p(p0);
-          p1 = ex2p(p1);
-          sum[c2 & 1] = add2(sum[c2 & 1], pair(p0, p1));
-          p[c2] = pack2<T>(p0, p1);
+          for (int c = 0; c < 8; ++c) {
+            float p0, p1;
+            unpair(fma2(pair(x[q * 16 + 2 * c], x[q * 16 + 2 * c + 1]), pair(a.scale_log2, a.scale_log2), pair(ms, ms)), p0, p1);
+            p0 = ex2p(p0);
+            p1 = ex2p(p1);
+            sum[c & 1] = add2(sum[c & 1], pair(p0, p1));
+            p[c] = pack2<T>(p0, p1);
+          }
+          tm_st8(ts + P_COL(half, q), p);
         }
-        tm_st16(ts + P_COL(half, part * 2), p);
+        tm_wait_st();
+        tm_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(b_p + 8 * w);
+        float s0, s1;
+        unpair(add2(sum[0], sum[1]), s0, s1);
+        l += s0 + s1;
       }
-      tm_wait_st();
-      tm_before();
-      __syncwarp();
-      if (lane == 0) bar_arrive(b_p + 8 * w);
-      float s0, s1;
-      unpair(add2(sum[0], sum[1]), s0, s1);
-      l += s0 + s1;
-    }
-    // results: the two halves' sums, half of the channels each
-    if (cnt > 0 && ok) ok = warp_wait(b_o + 8 * w, 0);
-    tm_after();
-    xch[half * TILE + r] = l;
-    asm volatile("bar.sync %0, 256;\n" ::"r"(1 + w) : "memory");
-    l += xch[(half ^ 1) * TILE + r];
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const bool mine = row < nq;
-    const long long prow = a.padded ? (long long)s * a.max_q + row : (long long)q0 + row;
-    const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
-    if (ok && mine && half == 0) {
-      if (a.splits > 1)
-        a.part_lse[((long long)split * a.rows + prow) * a.Hq + hq] = lse2;
-      else if (a.lse)
-        a.lse[a.padded ? ((long long)s * a.Hq + hq) * a.max_q + row : hq * a.total_q + prow] = lse2 * 0.6931471805599453f;
-    }
-    T* out = static_cast<T*>(a.out) + (a.padded ? s * a.out_stride[0] + row * a.out_stride[2] : prow * a.out_stride[2]) + hq * a.out_stride[1] + half * (D / 2);
-    float* po = a.part_o + (((long long)split * a.rows + prow) * a.Hq + hq) * D + half * (D / 2);
+      if (!ok) break;
+      // results: the two halves' sums, half of the channels each
+      if (cnt > 0) {
+        ok = warp_wait(b_o + 8 * w, o_phase);
+        o_phase ^= 1u;
+      }
+      tm_after();
+      xch[half * TILE] = l;
+      meet();
+      if (!ok) break;
+      l = xch[0] + xch[TILE];
+      const int row = it.r0 + w * TILE + r;  // of the sequence
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const bool mine = row < it.nq;
+      const long long prow = a.padded ? (long long)it.s * a.max_q + row : (long long)it.q0 + row;
+      const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
+      if (mine && half == 0) {
+        if (a.splits > 1)
+          a.part_lse[((long long)it.split * a.rows + prow) * a.Hq + it.hq] = lse2;
+        else if (a.lse)
+          a.lse[a.padded ? ((long long)it.s * a.Hq + it.hq) * a.max_q + row : it.hq * a.total_q + prow] = lse2 * 0.6931471805599453f;
+      }
+      T* out = static_cast<T*>(a.out) + (a.padded ? it.s * a.out_stride[0] + row * a.out_stride[2] : prow * a.out_stride[2]) +
+               it.hq * a.out_stride[1] + half * (D / 2);
+      float* po = a.part_o + (((long long)it.split * a.rows + prow) * a.Hq + it.hq) * D + half * (D / 2);
 #pragma unroll 1
-    for (int c = 0; c < D / 2 && ok; c += 32) {
-      float o[32];
-      if (cnt > 0) {  // warp-uniform
-        tm_ld32(to + c, o);
-        tm_wait_ld();
+      for (int c = 0; c < D / 2; c += 16) {
+        float o[16];
+        if (cnt > 0) {  // warp-uniform
+          tm_ld16(to + c, o);
+          tm_wait_ld();
+        }
+#pragma unroll
+        for (int k = 0; k < 16; ++k) o[k] = l == 0.f ? 0.f : o[k] * inv;
+        if (!mine) continue;
+        if (a.splits > 1) {
+#pragma unroll
+          for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4*>(po + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 16; k += 8)
+            *reinterpret_cast<uint4*>(out + c + k) =
+                make_uint4(pack2<T>(o[k], o[k + 1]), pack2<T>(o[k + 2], o[k + 3]), pack2<T>(o[k + 4], o[k + 5]), pack2<T>(o[k + 6], o[k + 7]));
+        }
       }
-#pragma unroll
-      for (int k = 0; k < 32; ++k) o[k] = l == 0.f ? 0.f : o[k] * inv;
-      if (!mine) continue;
-      if (a.splits > 1) {
-#pragma unroll
-        for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(po + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 32; k += 8)
-          *reinterpret_cast<uint4*>(out + c + k) =
-              make_uint4(pack2<T>(o[k], o[k + 1]), pack2<T>(o[k + 2], o[k + 3]), pack2<T>(o[k + 4], o[k + 5]), pack2<T>(o[k + 6], o[k + 7]));
-      }
+      __syncwarp();
     }
   }
   if (!ok) {
-    shared_words[2] = 1;
+    words[6] = 1;
     kv8_record(a.status, CHECK_COPY_TIMEOUT);
   }
   tm_before();
   __syncthreads();
   tm_after();
-  if (shared_words[2] && tid == 0) {  // a wait ran out: the copies in flight must land before the shared memory is given up
-    const int issued = (int)shared_words[1];
-    for (int it = max(0, issued - NS); it < issued; ++it) bar_wait(b_full + 8 * (it % NS), (uint32_t)(it / NS) & 1u);
-    if (n_all > 0) bar_wait(b_q, 0);
+  if (words[6] && tid == 0) {  // a wait ran out: the copies in flight must land before the shared memory is given up
+    const int issued = (int)words[5];
+    for (int i = max(0, issued - NS); i < issued; ++i) bar_wait(b_full + 8 * (i % NS), (uint32_t)(i / NS) & 1u);
+    if (words[7]) bar_wait(b_q, 0);
   }
   __syncthreads();
   if (wid == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
