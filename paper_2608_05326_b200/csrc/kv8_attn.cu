@@ -11,8 +11,7 @@
 // the order, so slots are distinct), and kv8_combine_kernel finds a row's slots from the same arithmetic.
 //
 // Tile.  Both products put the cache on the A side of mma.m16n8k16 (tokens, then channels on M; the G heads that
-// share the KV head on N).  Codes become fp16 in registers -- every int8 and e4m3 code is exact there -- and the
-// block's scale multiplies the logits / the block's output in float32.  The contraction index may be permuted as long
+// share the KV head on N).  Codes become fp16 operands in registers, exactly, and the block's scale multiplies the logits / the block's output in float32.  The contraction index may be permuted as long
 // as both sides agree, so a lane takes whole 4-byte words of its key row, and the token pairs of the values come out
 // of byte permutes.  The query goes to fp16 after a division by a power of two per head, which brings its largest
 // element into [1, 2): exact but for elements 2^-14 below the largest, which lose at most 2^-25 of it.
@@ -28,7 +27,7 @@ namespace {
 
 constexpr int WARPS = 4;                  // warps per CTA
 constexpr int ATTN_THREADS = WARPS * 32;
-constexpr int STAGES = 4;                 // units of 16 tokens, or pairs of 16 for UT = 32, in a warp's ring
+constexpr int RING_BYTES = 16384;         // of a warp (d = 128): stages of one unit's keys or values
 constexpr float LAZY = 8.f;               // the reference exponent moves only when a logit exceeds it by this (log2)
 
 struct Kv8AttnArgs {
@@ -46,8 +45,8 @@ struct Kv8AttnArgs {
   float* score_out;
   float* part_o;   // [slot][G][D]
   float2* part_ml; // [slot][G] {reference, sum}
+  float2* stats;
   float2* rec;     // [seq][max_units][Hq] {reference, sum} of every unit, or nullptr
-  float2* stats;   // [seq][Hq] {M, 1 / L}
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -60,20 +59,25 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
 }
 
-// Bytes {x, y} of the low (HI = 0) or high half of a word of two code pairs -> two fp16 values.
-template <int CODE, bool HI> __device__ __forceinline__ uint32_t codes_to_h2(uint32_t w) {
-  uint32_t r;
+// Codes as fp16 operands.  int8: code + 128 as a subnormal fp16, 2^-24 per unit (exact, and the tensor cores take
+// subnormals): one masking instruction for two codes, against three for code values proper.  The 128 comes off in the
+// accumulator's start value: -128 sum q for the logits, -128 sum p (a product with ones, over the same rounded p) for the
+// output.  The sums have terms of at most 255 instead of 127 units, which doubles their rounding errors (2^-24 of the
+// largest partial sum) and no more.  e4m3: the conversion instruction.
+template <int CODE> struct Unit { static constexpr float value = CODE == QEVICT_CODE_INT8 ? 0x1p24f : 1.f; };
+// a word of four codes c0 c1 c2 c3 -> operand registers for the pairs {c0, c2}, {c1, c3} (int8) or {c0, c1}, {c2, c3} (e4m3)
+template <int CODE> __device__ __forceinline__ void codes_to_h2(uint32_t w, uint32_t& lo, uint32_t& hi) {
   if (CODE == QEVICT_CODE_INT8) {
-    // w holds code + 128: 1024 + (code + 128) is an fp16 number with the byte in its low bits
-    const uint32_t m = __byte_perm(w, 0x64646464u, HI ? 0x4342 : 0x4140);
-    return as_u32(__hsub2(as_t2<__half2>(m), as_t2<__half2>(0x64806480u)));
+    asm("lop3.b32 %0, %1, 0x00ff00ff, 0x00800080, 0x6A;\n" : "=r"(lo) : "r"(w));  // (w & mask) ^ sign bits
+    asm("lop3.b32 %0, %1, 0x00ff00ff, 0x00800080, 0x6A;\n" : "=r"(hi) : "r"(w >> 8));
+  } else {
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}\n"
+        : "=r"(lo), "=r"(hi) : "r"(w));
   }
-  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, %2;\n\t}\n"
-      : "=r"(r) : "r"(w), "h"((uint16_t)(HI ? w >> 16 : w & 0xffffu)));
-  return r;
 }
-template <int CODE> __device__ __forceinline__ uint32_t bias(uint32_t w) {
-  return CODE == QEVICT_CODE_INT8 ? w ^ 0x80808080u : w;
+// which code of a lane's word meets element j of its k-step's operand (0, 1 in the first register, 2, 3 in the second)
+template <int CODE> __device__ __forceinline__ constexpr int code_at(int j) {
+  return CODE == QEVICT_CODE_INT8 ? (j & 1) * 2 + (j >> 1) : j;
 }
 
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
@@ -146,9 +150,11 @@ template <int D, int NT> struct Acc {
   float m[NT][2], l[NT][2];  // reference (log2), lane's share of the sum; heads 2 t, 2 t + 1 of head tile nt
 };
 
+__host__ __device__ constexpr int ring_of(int ut) { return RING_BYTES / (ut * 128); }  // 4 stages for units of 32 tokens, 8 for 16
+
 template <class T, int CODE, int D, int NT, int UT>
 __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel(const Kv8AttnArgs a) {
-  constexpr int KS = D / 16, MT = UT / 16, STAGE = 2 * UT * D, RING = STAGES * 16 / UT;
+  constexpr int KS = D / 16, MT = UT / 16, STAGE = UT * D, RING = ring_of(UT);
   extern __shared__ __align__(128) unsigned char sm[];
   const Kv8View& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -179,7 +185,8 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
 
     // queries of this KV head: B fragments in fp16, divided by a power of two per head
     uint32_t qf[NT][KS][2];
-    float qs[NT][2];  // of heads 2 t, 2 t + 1: that power of two times the softmax scale
+    float qs[NT][2];     // of heads 2 t, 2 t + 1: that power of two times the softmax scale
+    float q_off[NT][2];  // and where their logits start
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int hl = nt * 8 + g;
@@ -197,11 +204,21 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
       // 2^-e with e the exponent of the largest element (kept where both it and its inverse are normal)
       const int e = min(max((int)(__float_as_uint(mx) >> 23), 2), 252);
       const float down = __uint_as_float((uint32_t)(254 - e) << 23), up = __uint_as_float((uint32_t)e << 23);
+      float sum = 0.f;  // of the rounded elements
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        qf[nt][ks][0] = as_u32(__floats2half2_rn(x[ks][0] * down, x[ks][1] * down));
-        qf[nt][ks][1] = as_u32(__floats2half2_rn(x[ks][2] * down, x[ks][3] * down));
+        const __half2 p0 = __floats2half2_rn(x[ks][code_at<CODE>(0)] * down, x[ks][code_at<CODE>(1)] * down);
+        const __half2 p1 = __floats2half2_rn(x[ks][code_at<CODE>(2)] * down, x[ks][code_at<CODE>(3)] * down);
+        qf[nt][ks][0] = as_u32(p0);
+        qf[nt][ks][1] = as_u32(p1);
+        const float2 f0 = __half22float2(p0), f1 = __half22float2(p1);
+        sum += (f0.x + f0.y) + (f1.x + f1.y);
       }
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      const float off = CODE == QEVICT_CODE_INT8 ? -128.f * 0x1p-24f * sum : 0.f;
+      q_off[nt][0] = __shfl_sync(0xffffffffu, off, 8 * t);
+      q_off[nt][1] = __shfl_sync(0xffffffffu, off, 8 * t + 4);
       qs[nt][0] = __shfl_sync(0xffffffffu, up, 8 * t) * a.scale_log2;
       qs[nt][1] = __shfl_sync(0xffffffffu, up, 8 * t + 4) * a.scale_log2;
     }
@@ -278,7 +295,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
     // ---- units in full blocks: ring of asynchronous copies -----------------------------------------------------
     const int e1 = min(i1, n_code);
     if (i0 < e1) {
-      // page and scales of 32 blocks at a time, one per lane; the copies run RING - 1 units ahead
+      // page and scales of 32 blocks at a time, one per lane; the copies run RING - 1 stages ahead
       auto fetch = [&](int blk0, int& page) {
         page = -1;
         const int b = blk0 + lane;
@@ -292,29 +309,32 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
       };
       int f_blk0 = i0 / upb, f_page;  // producer's window of 32 blocks
       fetch(f_blk0, f_page);
-      auto issue = [&](int i) {
-        if (i < e1) {
-          const int b = i / upb;
+      const int e_end = 2 * (e1 - i0);
+      auto issue = [&](int e) {  // stage e: keys (even) or values of unit i0 + e / 2
+        if (e < e_end) {
+          const int i = i0 + (e >> 1), kv = e & 1, b = i / upb;
           if (b >= f_blk0 + 32) {
             f_blk0 += 32;
             fetch(f_blk0, f_page);
           }
           const int page = __shfl_sync(0xffffffffu, f_page, b - f_blk0);
           if (page >= 0) {
-            const size_t off = (((size_t)page * c.Hkv + h) * c.block + (size_t)(i - b * upb) * UT) * D;
-            const uint32_t dst = ring_a + (uint32_t)(i % RING) * STAGE;
+            const uint8_t* src = (kv ? c.codes[1] : c.codes[0]) + (((size_t)page * c.Hkv + h) * c.block + (size_t)(i - b * upb) * UT) * D;
+            const uint32_t dst = ring_a + (uint32_t)(e % RING) * STAGE;
 #pragma unroll
-            for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-              for (int n = 0; n < UT * D / 512; ++n) {
-                const int ch = n * 32 + lane, r = ch / (D / 16), cc = ch - r * (D / 16);
-                cp16(dst + kv * UT * D + swz<D>(r, cc), c.codes[kv] + off + ch * 16);
-              }
+            for (int n = 0; n < UT * D / 512; ++n) {
+              const int ch = n * 32 + lane, r = ch / (D / 16), cc = ch - r * (D / 16);
+              cp16(dst + swz<D>(r, cc), src + ch * 16);
+            }
           }
         }
         asm volatile("cp.async.commit_group;\n" ::: "memory");
       };
-      for (int i = i0; i < i0 + RING - 1; ++i) issue(i);
+      auto arrived = [&] {  // the oldest stage that has not been used
+        asm volatile("cp.async.wait_group %0;\n" ::"n"(RING - 2) : "memory");
+        __syncwarp();
+      };
+      for (int e = 0; e < RING - 1; ++e) issue(e);
       int s_blk0 = i0 / upb - 32, s_page = -1;
       float s_k = 0.f, s_v = 0.f;
       for (int i = i0; i < e1; ++i) {
@@ -325,15 +345,17 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
           s_k = s_page >= 0 ? c.scale[0][(size_t)s_page * c.Hkv + h] : 0.f;
           s_v = s_page >= 0 ? c.scale[1][(size_t)s_page * c.Hkv + h] : 0.f;
         }
-        asm volatile("cp.async.wait_group %0;\n" ::"n"(RING - 2) : "memory");
-        __syncwarp();
         const int page = __shfl_sync(0xffffffffu, s_page, b - s_blk0);
         const float ksc = __shfl_sync(0xffffffffu, s_k, b - s_blk0), vsc = __shfl_sync(0xffffffffu, s_v, b - s_blk0);
-        const unsigned char* kt = ring + (i % RING) * STAGE;
-        const unsigned char* vt = kt + UT * D;
+        const int e = 2 * (i - i0);
+        const unsigned char* kt = ring + (e % RING) * STAGE;
+        const unsigned char* vt = ring + ((e + 1) % RING) * STAGE;
+        arrived();
         if (page < 0) {  // absent block: nothing was copied
           if (a.rec)
             for (int hl = lane; hl < a.G; hl += 32) a.rec[((size_t)s * a.max_units + i) * a.Hq + h * a.G + hl] = make_float2(-INFINITY, 0.f);
+          issue(e + RING - 1);
+          arrived();
         } else {
           float x[NT][MT][4];
 #pragma unroll
@@ -349,12 +371,12 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) x[nt][mt][j] = 0.f;
+              for (int j = 0; j < 4; ++j) x[nt][mt][j] = q_off[nt][j & 1];
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-              const uint32_t w0 = bias<CODE>(k0[ks]), w1 = bias<CODE>(k1[ks]);
-              const uint32_t a0 = codes_to_h2<CODE, false>(w0), a2 = codes_to_h2<CODE, true>(w0);
-              const uint32_t a1 = codes_to_h2<CODE, false>(w1), a3 = codes_to_h2<CODE, true>(w1);
+              uint32_t a0, a1, a2, a3;
+              codes_to_h2<CODE>(k0[ks], a0, a2);
+              codes_to_h2<CODE>(k1[ks], a1, a3);
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) mma16816<__half>(x[nt][mt], a0, a1, a2, a3, qf[nt][ks][0], qf[nt][ks][1]);
             }
@@ -363,29 +385,36 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              const float f = qs[nt][j] * ksc;
+              const float f = qs[nt][j] * (ksc * Unit<CODE>::value);
 #pragma unroll
               for (int mt = 0; mt < MT; ++mt) {
                 x[nt][mt][j] *= f;
                 x[nt][mt][j + 2] *= f;
               }
             }
+          __syncwarp();  // every lane has read the keys: the next copy may go there
+          issue(e + RING - 1);
           softmax(x, i);
+          arrived();
+          uint32_t p0[NT][MT], p1[NT][MT];
           float o[NT][KS][4];  // this unit's output before the block's scale
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+          for (int nt = 0; nt < NT; ++nt) {
+            float start[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+              p0[nt][mt] = transpose8(as_u32(__floats2half2_rn(x[nt][mt][0], x[nt][mt][1])));
+              p1[nt][mt] = transpose8(as_u32(__floats2half2_rn(x[nt][mt][2], x[nt][mt][3])));
+              // -128 units for every p: the product with a matrix of -2^-17
+              if (CODE == QEVICT_CODE_INT8) mma16816<__half>(start, 0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u, p0[nt][mt], p1[nt][mt]);
+            }
 #pragma unroll
             for (int mt = 0; mt < KS; ++mt)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) o[nt][mt][j] = 0.f;
+              for (int j = 0; j < 4; ++j) o[nt][mt][j] = start[j & 1];
+          }
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt) {
-            uint32_t p0[NT], p1[NT];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              p0[nt] = transpose8(as_u32(__floats2half2_rn(x[nt][mt][0], x[nt][mt][1])));
-              p1[nt] = transpose8(as_u32(__floats2half2_rn(x[nt][mt][2], x[nt][mt][3])));
-            }
             // this lane's tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9, channels g D/8 ..
             uint32_t v[4][D / 32];
 #pragma unroll
@@ -401,26 +430,29 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
             }
 #pragma unroll
             for (int q4 = 0; q4 < D / 32; ++q4) {
-              const uint32_t wa = bias<CODE>(v[0][q4]), wb = bias<CODE>(v[1][q4]), wc = bias<CODE>(v[2][q4]), wd = bias<CODE>(v[3][q4]);
 #pragma unroll
               for (int half = 0; half < 2; ++half) {
-                const uint32_t ab = __byte_perm(wa, wb, half ? 0x7362 : 0x5140), cd = __byte_perm(wc, wd, half ? 0x7362 : 0x5140);
-                const uint32_t a0 = codes_to_h2<CODE, false>(ab), a1 = codes_to_h2<CODE, true>(ab);
-                const uint32_t a2 = codes_to_h2<CODE, false>(cd), a3 = codes_to_h2<CODE, true>(cd);
+                // two channels of two tokens in one word, in the order that codes_to_h2 takes apart into pairs of tokens
+                constexpr int lo = CODE == QEVICT_CODE_INT8 ? 0x5410 : 0x5140, hi = CODE == QEVICT_CODE_INT8 ? 0x7632 : 0x7362;
+                const uint32_t ab = __byte_perm(v[0][q4], v[1][q4], half ? hi : lo), cd = __byte_perm(v[2][q4], v[3][q4], half ? hi : lo);
+                uint32_t a0, a1, a2, a3;
+                codes_to_h2<CODE>(ab, a0, a1);
+                codes_to_h2<CODE>(cd, a2, a3);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma16816<__half>(o[nt][q4 * 2 + half], a0, a1, a2, a3, p0[nt], p1[nt]);
+                for (int nt = 0; nt < NT; ++nt) mma16816<__half>(o[nt][q4 * 2 + half], a0, a1, a2, a3, p0[nt][mt], p1[nt][mt]);
               }
             }
           }
+          const float vs = vsc * Unit<CODE>::value;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int mt = 0; mt < KS; ++mt)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) acc.o[nt][mt][j] = fmaf(o[nt][mt][j], vsc, acc.o[nt][mt][j]);
+              for (int j = 0; j < 4; ++j) acc.o[nt][mt][j] = fmaf(o[nt][mt][j], vs, acc.o[nt][mt][j]);
         }
-        __syncwarp();  // every lane has read the slot that the next copy fills
-        issue(i + RING - 1);
+        __syncwarp();
+        issue(e + RING);
       }
       asm volatile("cp.async.wait_group 0;\n" ::: "memory");
       __syncwarp();
@@ -661,12 +693,12 @@ const char* plan_of(const Kv8View& c, int Hq, int max_len, bool scores, int sms,
 }
 
 template <class T, int CODE, int D, int NT, int UT> cudaError_t launch_attn(const Kv8AttnArgs& a, cudaStream_t s) {
-  constexpr int RING = STAGES * 16 / UT;
-  const size_t smem = (size_t)WARPS * RING * 2 * UT * D + (size_t)(a.c.n_seqs + 1) * sizeof(int);
+  constexpr int RING = ring_of(UT);
+  const size_t smem = (size_t)WARPS * RING * UT * D + (size_t)(a.c.n_seqs + 1) * sizeof(int);
   auto kernel = kv8_attn_kernel<T, CODE, D, NT, UT>;
   cudaError_t e = cudaSuccess;
   if (smem > 48 * 1024) {  // one size for every call, so that calls with different batches do not lower each other's limit
-    constexpr int most = WARPS * RING * 2 * UT * D + 8193 * (int)sizeof(int);
+    constexpr int most = WARPS * RING * UT * D + 8193 * (int)sizeof(int);
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
   }
   if (e == cudaSuccess) e = launch_pdl(kernel, dim3(a.n_warps / WARPS), dim3(ATTN_THREADS), smem, s, a);
