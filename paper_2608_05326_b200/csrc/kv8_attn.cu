@@ -45,7 +45,8 @@ struct Kv8AttnArgs {
   float* score_out;
   float* part_o;   // [slot][G][D]
   float2* part_ml; // [slot][G] {reference, sum}
-  float2* stats;
+  float2* stats;   // [seq][Hq] {M, 1 / L}
+  int* pre;        // [n_seqs + 1] units per KV head before each sequence
   float2* rec;     // [seq][max_units][Hq] {reference, sum} of every unit, or nullptr
 };
 
@@ -91,6 +92,13 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
 __device__ __forceinline__ int clamp_len(const Kv8AttnArgs& a, int len) {
   return len <= a.max_len ? max(0, len) : a.max_len / a.c.block * a.c.block;
 }
+
+// The kernels of a call follow one another by programmatic launch.  The attention kernel lets the next one start only when
+// a warp has nothing left to read: its own CTAs fill the SMs, and CTAs of the next kernel that slipped in between cost a
+// second wave (16 ragged contexts: 104 us, 117 with the release at the start).  The last kernel of a call releases nothing
+// early for the same reason.
+__device__ __forceinline__ void wait_prior() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
+__device__ __forceinline__ void release_next() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
 
 // Prefix sums of the sequences' units per KV head, in shared memory.
 __device__ void unit_prefix(const Kv8AttnArgs& a, int ut, int* pre, int* s_w) {
@@ -160,8 +168,10 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
   int* pre = reinterpret_cast<int*>(sm + WARPS * RING * STAGE);
   __shared__ int s_w[WARPS];
-  pdl_prologue();
+  wait_prior();
   unit_prefix(a, UT, pre, s_w);
+  if (blockIdx.x == 0)  // for the kernels behind this one
+    for (int i = tid; i <= c.n_seqs; i += ATTN_THREADS) a.pre[i] = pre[i];
   const long long total = (long long)pre[c.n_seqs] * c.Hkv;
   if (total == 0) return;
   const int w = blockIdx.x * WARPS + wid, n_runs = runs_of(total, a.n_warps);
@@ -537,6 +547,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
       }
     }
 
+    if (u >= u_end) release_next();
     // ---- partial result of this run's part of the row -----------------------------------------------------------
     const size_t slot = (size_t)w + row;
 #pragma unroll
@@ -559,19 +570,20 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
   }
 }
 
-// Merges a row's partial results: one CTA per (query head, sequence).
+// Merges a row's partial results: one CTA per (query head, sequence).  A warp takes partials wid, wid + 8, ... with a running
+// maximum of its own, so that everything it needs is requested at once; the eight warps' results meet in shared memory.
 constexpr int COMB_THREADS = 256;
 template <class T>
-__global__ void __launch_bounds__(COMB_THREADS) kv8_combine_kernel(const Kv8AttnArgs a, int ut) {
-  extern __shared__ int pre[];
-  __shared__ int s_w[COMB_THREADS / 32];
-  __shared__ float s_red[COMB_THREADS / 32], s_o[COMB_THREADS / 32][128];
+__global__ void __launch_bounds__(COMB_THREADS) kv8_combine_kernel(const Kv8AttnArgs a) {
+  constexpr int NW = COMB_THREADS / 32;
+  __shared__ float s_m[NW], s_l[NW], s_o[NW][128];
   const int s = blockIdx.y, hq = blockIdx.x, h = hq / a.G, hl = hq - h * a.G, D = a.c.D;
-  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, nw = COMB_THREADS / 32;
-  pdl_prologue();
-  unit_prefix(a, ut, pre, s_w);
-  const long long total = (long long)pre[a.c.n_seqs] * a.c.Hkv;
-  const int nu = pre[s + 1] - pre[s], row = s * a.c.Hkv + h;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  wait_prior();
+  const int p0 = a.pre[s], p1 = a.pre[s + 1];
+  const long long total = (long long)a.pre[a.c.n_seqs] * a.c.Hkv;
+  release_next();
+  const int nu = p1 - p0;
   T* out = static_cast<T*>(a.out) + ((size_t)s * a.Hq + hq) * D;
   if (tid == 0 && a.c.status && hq == 0 && a.lens[s] > a.max_len) kv8_record(a.c.status, CHECK_LENGTH);
   if (nu == 0) {
@@ -582,46 +594,67 @@ __global__ void __launch_bounds__(COMB_THREADS) kv8_combine_kernel(const Kv8Attn
     }
     return;
   }
-  const long long u0 = (long long)pre[s] * a.c.Hkv + (long long)h * nu;
+  const long long u0 = (long long)p0 * a.c.Hkv + (long long)h * nu;
   const int n_runs = runs_of(total, a.n_warps);
   const int w0 = run_of(total, n_runs, u0), n = run_of(total, n_runs, u0 + nu - 1) - w0 + 1;
-  const size_t slot0 = (size_t)w0 + row;
-  float M = -INFINITY;
-  for (int i = tid; i < n; i += COMB_THREADS) M = fmaxf(M, a.part_ml[(slot0 + i) * a.G + hl].x);
-#pragma unroll
-  for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  if (lane == 0) s_red[wid] = M;
-  __syncthreads();
-  for (int i = 0; i < nw; ++i) M = fmaxf(M, s_red[i]);
-  const float Ms = M == -INFINITY ? 0.f : M;
-  __syncthreads();
-  // warp `wid` takes partials wid, wid + 8, ...; lanes hold 4 channels each (d = 64: half the lanes twice as many rows)
+  const size_t slot0 = (size_t)w0 + (size_t)s * a.c.Hkv + h;
+  // lanes hold 4 channels each (d = 64: half the lanes, twice as many partials at a time)
   const int per = D / 4, sub = lane / per, subs = 32 / per, c4 = lane - sub * per;
-  float l = 0.f;
+  float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int i = wid * subs + sub; i < n; i += nw * subs) {
-    const float2 ml = a.part_ml[(slot0 + i) * a.G + hl];
-    const float4 v = *reinterpret_cast<const float4*>(a.part_o + ((slot0 + i) * a.G + hl) * D + c4 * 4);
-    const float f = ex2(ml.x - Ms);
-    l += ml.y * f;
-    o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
+  constexpr int AT_ONCE = 8;
+  for (int i0 = wid * subs + sub; i0 < n; i0 += AT_ONCE * NW * subs) {
+    float2 ml[AT_ONCE];
+    float4 v[AT_ONCE];
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {
+      const int i = i0 + k * NW * subs;
+      ml[k] = i < n ? a.part_ml[(slot0 + i) * a.G + hl] : make_float2(-INFINITY, 0.f);
+      v[k] = i < n ? *reinterpret_cast<const float4*>(a.part_o + ((slot0 + i) * a.G + hl) * D + c4 * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    float top = m;
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) top = fmaxf(top, ml[k].x);
+    const float ref = top == -INFINITY ? 0.f : top, f0 = ex2(m - ref);  // m = -inf: 0
+    l *= f0;
+    o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+    m = top;
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {
+      const float f = ex2(ml[k].x - ref);
+      l += ml[k].y * f;
+      o.x += v[k].x * f; o.y += v[k].y * f; o.z += v[k].z * f; o.w += v[k].w * f;
+    }
   }
   if (subs == 2) {
+    const float m2 = __shfl_xor_sync(0xffffffffu, m, 16), top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
+    const float f = ex2(m - ref);
+    l *= f;
     l += __shfl_xor_sync(0xffffffffu, l, 16);
+    o.x *= f; o.y *= f; o.z *= f; o.w *= f;
     o.x += __shfl_xor_sync(0xffffffffu, o.x, 16);
     o.y += __shfl_xor_sync(0xffffffffu, o.y, 16);
     o.z += __shfl_xor_sync(0xffffffffu, o.z, 16);
     o.w += __shfl_xor_sync(0xffffffffu, o.w, 16);
+    m = top;
   }
-  if (lane == 0) s_red[wid] = l;
+  if (lane == 0) {
+    s_m[wid] = m;
+    s_l[wid] = l;
+  }
   if (sub == 0) *reinterpret_cast<float4*>(&s_o[wid][c4 * 4]) = o;
   __syncthreads();
   if (tid < D) {
+    float M = s_m[0];
+#pragma unroll
+    for (int i = 1; i < NW; ++i) M = fmaxf(M, s_m[i]);
+    const float Ms = M == -INFINITY ? 0.f : M;
     float L = 0.f, v = 0.f;
-    for (int i = 0; i < nw; ++i) {
-      L += s_red[i];
-      v += s_o[i][tid];
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      const float f = ex2(s_m[i] - Ms);
+      L += s_l[i] * f;
+      v += s_o[i][tid] * f;
     }
     out[tid] = Tr<T>::from_float(L > 0.f ? v / L : (L == 0.f ? 0.f : v));
     if (tid == 0) {
@@ -631,29 +664,37 @@ __global__ void __launch_bounds__(COMB_THREADS) kv8_combine_kernel(const Kv8Attn
   }
 }
 
-// Block masses: one warp per (block, sequence); lanes stride over the query heads, fixed shuffle tree.
+// Block masses: one warp per (block, sequence), a lane per head, every load requested at once, fixed shuffle tree.  (As a part
+// of the merge -- each of its CTAs working out all heads' statistics for itself -- the two took longer than apart: 18
+// against 14 us at one sequence of 2048 tokens.)
 constexpr int MASS_THREADS = 256;
 __global__ void __launch_bounds__(MASS_THREADS) kv8_mass_kernel(const Kv8AttnArgs a, int ut) {
   const int s = blockIdx.y, lane = threadIdx.x & 31, b = blockIdx.x * (MASS_THREADS / 32) + (threadIdx.x >> 5);
-  pdl_prologue();
+  wait_prior();
   if (b >= a.c.max_blocks) return;
-  const int len = clamp_len(a, a.lens[s]), upb = a.c.block / ut;
-  const int nu = (len + ut - 1) / ut;
+  const int nu = a.pre[s + 1] - a.pre[s], upb = a.c.block / ut;
   const size_t at = (size_t)s * a.c.max_blocks + b;
+  const float before = a.score_in ? a.score_in[at] : 0.f;
   float mass = 0.f;
-  for (int i = b * upb; i < min(nu, (b + 1) * upb); ++i)
-    for (int h = lane; h < a.Hq; h += 32) {
-      const float2 r = a.rec[((size_t)s * a.max_units + i) * a.Hq + h], st = a.stats[(size_t)s * a.Hq + h];
-      mass += r.y * ex2(r.x - st.x) * st.y;
-    }
+  for (int h = lane; h < a.Hq; h += 32) {
+    const float2 st = a.stats[(size_t)s * a.Hq + h];
+    const float2* rec = a.rec + ((size_t)s * a.max_units + (size_t)b * upb) * a.Hq + h;
+    float2 r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)  // a block has at most 8 units (16 tokens: one, 128: four)
+      r[i] = i < upb && b * upb + i < a.max_units ? rec[(size_t)i * a.Hq] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (b * upb + i < nu) mass += r[i].y * ex2(r[i].x - st.x) * st.y;  // what lies behind the length was never written
+  }
 #pragma unroll
   for (int o = 16; o; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
-  if (lane == 0) a.score_out[at] = (a.score_in ? a.score_in[at] : 0.f) + mass;
+  if (lane == 0) a.score_out[at] = before + mass;
 }
 
 struct Plan {
   int ut, n_warps, max_units, max_len;
-  size_t off_ml, off_rec, off_stats, bytes;
+  size_t off_ml, off_rec, off_stats, off_pre, bytes;
 };
 
 int sm_count(int device) {
@@ -687,7 +728,8 @@ const char* plan_of(const Kv8View& c, int Hq, int max_len, bool scores, int sms,
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   p->off_ml = up(slots * G * c.D * sizeof(float));
   p->off_stats = p->off_ml + up(slots * G * sizeof(float2));
-  p->off_rec = p->off_stats + up((size_t)c.n_seqs * Hq * sizeof(float2));
+  p->off_pre = p->off_stats + up((size_t)c.n_seqs * Hq * sizeof(float2));
+  p->off_rec = p->off_pre + up(((size_t)c.n_seqs + 1) * sizeof(int));
   p->bytes = p->off_rec + (scores ? up((size_t)c.n_seqs * p->max_units * Hq * sizeof(float2)) : 0);
   return nullptr;
 }
@@ -715,8 +757,10 @@ template <class T, int CODE> cudaError_t launch_attn_shape(const Kv8AttnArgs& a,
 }
 template <class T> cudaError_t launch_all(const Kv8AttnArgs& a, int code, int ut, cudaStream_t s) {
   cudaError_t e = code == QEVICT_CODE_INT8 ? launch_attn_shape<T, QEVICT_CODE_INT8>(a, ut, s) : launch_attn_shape<T, QEVICT_CODE_E4M3>(a, ut, s);
-  const size_t smem = (size_t)(a.c.n_seqs + 1) * sizeof(int);
-  if (e == cudaSuccess) e = launch_pdl(kv8_combine_kernel<T>, dim3(a.Hq, a.c.n_seqs), dim3(COMB_THREADS), smem, s, a, ut);
+  // the same split of the SM's memory as the attention kernel's: an SM has to drain before it changes it
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kv8_combine_kernel<T>, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kv8_mass_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
+  if (e == cudaSuccess) e = launch_pdl(kv8_combine_kernel<T>, dim3(a.Hq, a.c.n_seqs), dim3(COMB_THREADS), 0, s, a);
   if (e == cudaSuccess && a.score_out) {
     const int per = MASS_THREADS / 32;
     e = launch_pdl(kv8_mass_kernel, dim3((a.c.max_blocks + per - 1) / per, a.c.n_seqs), dim3(MASS_THREADS), 0, s, a, ut);
@@ -770,6 +814,7 @@ QEVICT_API qevict_status qevict_kv8_attn(const qevict_kv8_cache* cache, int32_t 
   a.part_o = reinterpret_cast<float*>(base);
   a.part_ml = reinterpret_cast<float2*>(base + p.off_ml);
   a.stats = reinterpret_cast<float2*>(base + p.off_stats);
+  a.pre = reinterpret_cast<int*>(base + p.off_pre);
   a.rec = score_out ? reinterpret_cast<float2*>(base + p.off_rec) : nullptr;
   DeviceGuard guard(cache->device);
   cudaError_t e = guard.err;
