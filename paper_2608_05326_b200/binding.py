@@ -4,6 +4,7 @@ CUDA kernels of the library; there is no fallback of any kind."""
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -134,15 +135,15 @@ _SIGNATURES = {
     "qevict_export_tables": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32] + [C.c_void_p] * 7),
     "qevict_export_last_mass": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]),
     "qevict_export_fp_page": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]),
-    "qevict_prompt_attn_scratch_bytes": (C.c_int, [C.POINTER(qevict_prompt_args), C.POINTER(C.c_uint64)]),
-    "qevict_prompt_attn": (C.c_int, [C.POINTER(qevict_prompt_args), C.c_void_p, C.c_uint64, C.c_void_p]),
-    "qevict_kv8_append": (C.c_int, [C.POINTER(qevict_kv8_cache), C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int64,
+    "qevict_prompt_attn_scratch_bytes": (C.c_int, [C.c_void_p, C.POINTER(C.c_uint64)]),
+    "qevict_prompt_attn": (C.c_int, [C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]),
+    "qevict_kv8_append": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int64,
                                     C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]),
-    "qevict_kv8_attn_scratch_bytes": (C.c_int, [C.POINTER(qevict_kv8_cache), C.c_int32, C.c_int32, C.c_int32,
+    "qevict_kv8_attn_scratch_bytes": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
                                                 C.POINTER(C.c_uint64)]),
-    "qevict_kv8_attn": (C.c_int, [C.POINTER(qevict_kv8_cache), C.c_int32, C.c_float, C.c_void_p, C.c_void_p, C.c_int32,
+    "qevict_kv8_attn": (C.c_int, [C.c_void_p, C.c_int32, C.c_float, C.c_void_p, C.c_void_p, C.c_int32,
                                   C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]),
-    "qevict_kv8_evict": (C.c_int, [C.POINTER(qevict_kv8_evict_args), C.c_void_p]),
+    "qevict_kv8_evict": (C.c_int, [C.c_void_p, C.c_void_p]),
     "qevict_export_q_page": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32] + [C.c_void_p] * 5),
 }
 
@@ -322,8 +323,18 @@ def qevict_kernel_time(h):
 
 
 # --- calls without a cache handle: prompt attention, the 8-bit block-scaled cache ---------------------------------
+# These are made once per layer and token, so what they cost on the host counts: argument structures are packed in one go
+# (struct.Struct in place of a ctypes structure filled field by field), a check that passes is one expression, and the
+# stream is read as a raw handle.
 _DTYPES = {torch.float16: DTYPE_FP16, torch.bfloat16: DTYPE_BF16}
 _CODES = {torch.int8: CODE_INT8, torch.float8_e4m3fn: CODE_E4M3}
+_PROMPT_PACK = struct.Struct("@I10if2q7P12qP")
+_KV8_PACK = struct.Struct("@I9i8P")
+_EVICT_PACK = struct.Struct("@I8i9P")
+for _pack, _cls in ((_PROMPT_PACK, qevict_prompt_args), (_KV8_PACK, qevict_kv8_cache), (_EVICT_PACK, qevict_kv8_evict_args)):
+    assert _pack.size == C.sizeof(_cls), _cls
+
+_i32, _f32, _u8 = torch.int32, torch.float32, torch.uint8
 
 
 def _refuse(msg):
@@ -331,41 +342,35 @@ def _refuse(msg):
 
 
 def _want(t, name, device, dtype, shape=None):
-    """Checks a tensor argument: type, device, shape, contiguity (what the C side cannot see)."""
+    """Address of a tensor argument after checking what the C side cannot see: type, device, shape, contiguity."""
+    try:
+        if t.dtype is dtype and t.device == device and (shape is None or t.shape == shape) and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
     if not isinstance(t, torch.Tensor):
         _refuse("%s must be a tensor" % name)
     if t.dtype != dtype:
         _refuse("%s must be %s, got %s" % (name, dtype, t.dtype))
     if t.device != device:
         _refuse("%s must be on %s, got %s" % (name, device, t.device))
-    if shape is not None and t.shape != shape:
+    if shape is not None and t.shape != torch.Size(shape):
         _refuse("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-    if not t.is_contiguous():
-        _refuse("%s must be contiguous" % name)
-    return t.data_ptr()
+    _refuse("%s must be contiguous" % name)
 
 
-class _OnStream:
-    """The stream of a call on `device` (the caller's, or the device's current one), current while buffers of the call
-    are allocated, so that the allocator hands them out again in that stream's order."""
-
-    def __init__(self, device, stream):
-        self.current = torch.cuda.current_stream(device)
-        self.stream = self.current if stream is None else stream
-        self.guard = None if self.stream == self.current else torch.cuda.stream(self.stream)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.stream.cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _current_stream(device):
+    """Raw handle of the current stream of a device."""
+    try:
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    except AttributeError:  # a torch without that shortcut
+        return torch.cuda.current_stream(device).cuda_stream
 
 
-def _bounds(t, name, device, n):
-    return None if t is None else _want(t, name, device, torch.int32, (n,))
+def _cuda(t, name):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        _refuse("%s must be a tensor on a CUDA device" % name)
+    return t.device
 
 
 def qevict_prompt_attn(q, k, v, cu_q=None, cu_k=None, max_q=None, max_k=None, causal=True, softmax_scale=0.0, out=None, lse=None,
@@ -379,86 +384,100 @@ def qevict_prompt_attn(q, k, v, cu_q=None, cu_k=None, max_q=None, max_k=None, ca
     Any strides that keep d contiguous and are multiples of 16 bytes.  Returns out, or (out, lse) with return_lse; rows
     of no sequence are not written.
     """
-    dev = q.device
-    if dev.type != "cuda":
-        _refuse("q must be on a CUDA device")
-    if q.dtype not in _DTYPES:
+    if stream is not None:  # its buffers come from the allocator in that stream's order
+        with torch.cuda.stream(stream):
+            return qevict_prompt_attn(q, k, v, cu_q, cu_k, max_q, max_k, causal, softmax_scale, out, lse, return_lse, status)
+    dev = _cuda(q, "q")
+    dtype, shape, kshape = q.dtype, q.shape, k.shape
+    if dtype not in _DTYPES:
         _refuse("q must be float16 or bfloat16")
-    padded = q.dim() == 4
-    for name, x in (("q", q), ("k", k), ("v", v)):
-        if x.dim() != (4 if padded else 3) or x.dtype != q.dtype or x.device != dev or x.shape[-1] != q.shape[-1] or x.stride(-1) != 1:
-            _refuse("q, k, v must be [tokens, heads, d] or [n_seqs, heads, tokens, d] of one type on one device, d contiguous (%s)" % name)
-    if k.shape != v.shape:
+    padded = len(shape) == 4
+    sq, sk, sv = q.stride(), k.stride(), v.stride()
+    if len(shape) != (4 if padded else 3) or len(kshape) != len(shape) or k.dtype is not dtype or v.dtype is not dtype or \
+            k.device != dev or v.device != dev or kshape[-1] != shape[-1] or sq[-1] != 1 or sk[-1] != 1 or sv[-1] != 1:
+        _refuse("q, k, v must be [tokens, heads, d] or [n_seqs, heads, tokens, d] of one type on one device, d contiguous")
+    if kshape != v.shape:
         _refuse("k and v must have the same shape")
     if padded:
-        n, hq, mq, d = q.shape
-        hkv, mk = k.shape[1], k.shape[2]
-        if k.shape[0] != n:
+        n, hq, mq, d = shape
+        _, hkv, mk, _ = kshape
+        if kshape[0] != n:
             _refuse("q and k must have the same number of sequences")
         if (max_q is not None and max_q != mq) or (max_k is not None and max_k != mk):
             _refuse("the padded layout has its bounds in the shapes: max_q and max_k must be None")
-        p_cq, p_ck, total_q, total_k = _bounds(cu_q, "cu_q", dev, n), _bounds(cu_k, "cu_k", dev, n), 0, 0
+        p_cq = 0 if cu_q is None else _want(cu_q, "cu_q", dev, _i32, (n,))
+        p_ck = 0 if cu_k is None else _want(cu_k, "cu_k", dev, _i32, (n,))
+        total_q = total_k = 0
         lse_shape = (n, hq, mq)
-        strides = [(C.c_int64 * 3)(*x.stride()[:3]) for x in (q, k, v)]
+        sq, sk, sv = sq[:3], sk[:3], sv[:3]
     else:
-        total_q, hq, d = q.shape
-        total_k, hkv = k.shape[0], k.shape[1]
+        total_q, hq, d = shape
+        total_k, hkv, _ = kshape
         if cu_q is None:
             _refuse("the packed layout needs cu_q")
-        if cu_k is None:
-            cu_k = cu_q
-        n = cu_q.shape[0] - 1
+        n = cu_q.numel() - 1
         if n < 0:
             _refuse("cu_q must hold n_seqs + 1 bounds")
-        p_cq, p_ck = _bounds(cu_q, "cu_q", dev, n + 1), _bounds(cu_k, "cu_k", dev, n + 1)
+        p_cq = _want(cu_q, "cu_q", dev, _i32, (n + 1,))
+        p_ck = p_cq if cu_k is None else _want(cu_k, "cu_k", dev, _i32, (n + 1,))
         mq, mk = total_q if max_q is None else max_q, total_k if max_k is None else max_k
         lse_shape = (hq, total_q)
-        strides = [(C.c_int64 * 3)(0, x.stride(1), x.stride(0)) for x in (q, k, v)]
-    with _OnStream(dev, stream) as s:
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-        elif out.shape != q.shape or out.dtype != q.dtype or out.device != dev or out.stride(-1) != 1:
-            _refuse("out must be like q")
-        if lse is None and return_lse:
-            lse = torch.empty(lse_shape, dtype=torch.float32, device=dev)
-        p_lse = None if lse is None else _want(lse, "lse", dev, torch.float32, lse_shape)
-        so = (C.c_int64 * 3)(*out.stride()[:3]) if padded else (C.c_int64 * 3)(0, out.stride(1), out.stride(0))
-        args = qevict_prompt_args(
-            C.sizeof(qevict_prompt_args), dev.index, _DTYPES[q.dtype], LAYOUT_PADDED if padded else LAYOUT_PACKED, n, hq, hkv, d,
-            mq, mk, int(causal), softmax_scale, total_q, total_k, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), p_lse,
-            p_cq, p_ck, strides[0], strides[1], strides[2], so,
-            None if status is None else _want(status, "status", dev, torch.int32, (1,)))
-        need = C.c_uint64()
-        _check(lib().qevict_prompt_attn_scratch_bytes(C.byref(args), C.byref(need)))
-        scratch = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
-        _check(lib().qevict_prompt_attn(C.byref(args), None if scratch is None else scratch.data_ptr(), need.value, s))
+        sq, sk, sv = (0, sq[1], sq[0]), (0, sk[1], sk[0]), (0, sv[1], sv[0])
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    elif out.shape != shape or out.dtype is not dtype or out.device != dev or out.stride(-1) != 1:
+        _refuse("out must be like q")
+    if lse is None:
+        if return_lse:
+            lse = q.new_empty(lse_shape, dtype=_f32)
+    so = out.stride()
+    so = so[:3] if padded else (0, so[1], so[0])
+    try:
+        args = _PROMPT_PACK.pack(
+            C.sizeof(qevict_prompt_args), dev.index, _DTYPES[dtype], padded, n, hq, hkv, d, mq, mk, bool(causal), softmax_scale, total_q,
+            total_k, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+            0 if lse is None else _want(lse, "lse", dev, _f32, lse_shape), p_cq, p_ck, *sq, *sk, *sv, *so,
+            0 if status is None else _want(status, "status", dev, _i32, (1,)))
+    except struct.error as e:
+        _refuse("an argument does not fit its field (%s)" % e)
+    need = C.c_uint64()
+    library = lib()
+    _check(library.qevict_prompt_attn_scratch_bytes(args, C.byref(need)))
+    scratch = None if need.value == 0 else q.new_empty(need.value, dtype=_u8)
+    _check(library.qevict_prompt_attn(args, None if scratch is None else scratch.data_ptr(), need.value, _current_stream(dev)))
     return (out, lse) if return_lse else out
 
 
 def qevict_kv8_evict(block_table, lens, scores, block, n_pages, budget, sink=0, recent=0, in_place=False, stream=None):
     """Keeps the `budget` best full blocks of every sequence (the first `sink` and last `recent` always).  Returns a dict:
     block_table, lens, scores (new tensors, or the given ones with in_place), kept, freed, n_freed."""
-    dev = block_table.device
-    if dev.type != "cuda":
-        _refuse("block_table must be on a CUDA device")
-    if block_table.dim() != 2:
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return qevict_kv8_evict(block_table, lens, scores, block, n_pages, budget, sink, recent, in_place)
+    dev = _cuda(block_table, "block_table")
+    shape = block_table.shape
+    if len(shape) != 2:
         _refuse("block_table must be [n_seqs, max_blocks]")
-    n, mb = block_table.shape
-    p_table = _want(block_table, "block_table", dev, torch.int32)
-    p_lens = _want(lens, "lens", dev, torch.int32, (n,))
-    p_scores = _want(scores, "scores", dev, torch.float32, (n, mb))
-    with _OnStream(dev, stream) as s:
-        if in_place:
-            out = {"block_table": block_table, "lens": lens, "scores": scores}
-        else:
-            out = {"block_table": torch.empty_like(block_table), "lens": torch.empty_like(lens), "scores": torch.empty_like(scores)}
-        out["kept"], out["freed"], out["n_freed"] = torch.empty_like(block_table), torch.empty_like(block_table), torch.empty_like(lens)
-        args = qevict_kv8_evict_args(
-            C.sizeof(qevict_kv8_evict_args), dev.index, n, mb, block, n_pages, budget, sink, recent, p_table, p_lens, p_scores,
-            out["block_table"].data_ptr(), out["lens"].data_ptr(), out["scores"].data_ptr(), out["kept"].data_ptr(),
-            out["freed"].data_ptr(), out["n_freed"].data_ptr())
-        _check(lib().qevict_kv8_evict(C.byref(args), s))
-    return out
+    n, mb = shape
+    p_table = _want(block_table, "block_table", dev, _i32)
+    p_lens = _want(lens, "lens", dev, _i32, (n,))
+    p_scores = _want(scores, "scores", dev, _f32, shape)
+    if in_place:
+        table_out, scores_out, lens_out = block_table, scores, lens
+        kept, freed = block_table.new_empty((2, n, mb)).unbind(0)
+        n_freed = torch.empty_like(lens)
+    else:
+        table_out, kept, freed = block_table.new_empty((3, n, mb)).unbind(0)
+        scores_out = torch.empty_like(scores)
+        lens_out, n_freed = lens.new_empty((2, n)).unbind(0)
+    try:
+        args = _EVICT_PACK.pack(C.sizeof(qevict_kv8_evict_args), dev.index, n, mb, block, n_pages, budget, sink, recent, p_table, p_lens, p_scores,
+                                table_out.data_ptr(), lens_out.data_ptr(), scores_out.data_ptr(), kept.data_ptr(), freed.data_ptr(),
+                                n_freed.data_ptr())
+    except struct.error as e:
+        _refuse("an argument does not fit its field (%s)" % e)
+    _check(lib().qevict_kv8_evict(args, _current_stream(dev)))
+    return {"block_table": table_out, "lens": lens_out, "scores": scores_out, "kept": kept, "freed": freed, "n_freed": n_freed}
 
 
 class Kv8Cache:
@@ -470,25 +489,23 @@ class Kv8Cache:
     """
 
     def __init__(self, k_codes, v_codes, k_scale, v_scale, k_tail, v_tail, block_table, status=None):
-        dev = k_codes.device
-        if dev.type != "cuda":
-            _refuse("k_codes must be on a CUDA device")
-        if k_codes.dtype not in _CODES or k_tail.dtype not in _DTYPES:
+        dev = _cuda(k_codes, "k_codes")
+        code, dtype, shape, grid = k_codes.dtype, k_tail.dtype, k_codes.shape, block_table.shape
+        if code not in _CODES or dtype not in _DTYPES:
             _refuse("codes must be int8 or float8_e4m3fn and tails float16 or bfloat16")
-        if k_codes.dim() != 4 or block_table.dim() != 2:
+        if len(shape) != 4 or len(grid) != 2:
             _refuse("k_codes must be [n_pages, H_kv, block, d] and block_table [n_seqs, max_blocks]")
-        n_pages, h_kv, block, d = shape = k_codes.shape
-        n, mb = block_table.shape
-        self.device, self.dtype, self.n_seqs, self.max_blocks, self.block = dev, k_tail.dtype, n, mb, block
+        n_pages, h_kv, block, d = shape
+        n, mb = grid
+        tail, scale = (n, h_kv, block, d), (n_pages, h_kv)
+        self.device, self.dtype, self.n_seqs, self.max_blocks, self.block = dev, dtype, n, mb, block
         self.n_pages, self.n_kv_heads, self.head_dim = n_pages, h_kv, d
-        tail = (n, h_kv, block, d)
-        self._view = qevict_kv8_cache(
-            C.sizeof(qevict_kv8_cache), dev.index, _DTYPES[k_tail.dtype], _CODES[k_codes.dtype], n, h_kv, d, block, mb, n_pages,
-            _want(k_codes, "k_codes", dev, k_codes.dtype), _want(v_codes, "v_codes", dev, k_codes.dtype, shape),
-            _want(k_scale, "k_scale", dev, torch.float32, (n_pages, h_kv)), _want(v_scale, "v_scale", dev, torch.float32, (n_pages, h_kv)),
-            _want(k_tail, "k_tail", dev, k_tail.dtype, tail), _want(v_tail, "v_tail", dev, k_tail.dtype, tail),
-            _want(block_table, "block_table", dev, torch.int32),
-            None if status is None else _want(status, "status", dev, torch.int32, (1,)))
+        self._view = _KV8_PACK.pack(
+            C.sizeof(qevict_kv8_cache), dev.index, _DTYPES[dtype], _CODES[code], n, h_kv, d, block, mb, n_pages,
+            _want(k_codes, "k_codes", dev, code), _want(v_codes, "v_codes", dev, code, shape),
+            _want(k_scale, "k_scale", dev, _f32, scale), _want(v_scale, "v_scale", dev, _f32, scale),
+            _want(k_tail, "k_tail", dev, dtype, tail), _want(v_tail, "v_tail", dev, dtype, tail),
+            _want(block_table, "block_table", dev, _i32), 0 if status is None else _want(status, "status", dev, _i32, (1,)))
         self._tensors = (k_codes, v_codes, k_scale, v_scale, k_tail, v_tail, block_table, status)
 
     @classmethod
@@ -499,11 +516,11 @@ class Kv8Cache:
         if dev.index is None:
             dev = torch.device(dev.type, torch.cuda.current_device())
         pool, tail = (n_pages, n_kv_heads, block, head_dim), (n_seqs, n_kv_heads, block, head_dim)
-        t = {"k_codes": torch.zeros(pool, dtype=torch.uint8, device=dev).view(code), "v_codes": torch.zeros(pool, dtype=torch.uint8, device=dev).view(code),
+        t = {"k_codes": torch.zeros(pool, dtype=_u8, device=dev).view(code), "v_codes": torch.zeros(pool, dtype=_u8, device=dev).view(code),
              "k_scale": torch.ones((n_pages, n_kv_heads), device=dev), "v_scale": torch.ones((n_pages, n_kv_heads), device=dev),
              "k_tail": torch.zeros(tail, dtype=dtype, device=dev), "v_tail": torch.zeros(tail, dtype=dtype, device=dev),
-             "block_table": torch.full((n_seqs, max_blocks), -1, dtype=torch.int32, device=dev),
-             "status": torch.zeros(1, dtype=torch.int32, device=dev)}
+             "block_table": torch.full((n_seqs, max_blocks), -1, dtype=_i32, device=dev),
+             "status": torch.zeros(1, dtype=_i32, device=dev)}
         cache = cls(**t)
         for name, x in t.items():
             setattr(cache, name, x)
@@ -512,47 +529,53 @@ class Kv8Cache:
     def append(self, k, v, start, cu_new=None, max_new=1, stream=None):
         """k, v [total, H_kv, d] (any strides that keep d contiguous): token i of sequence s is row cu_new[s] + i (without
         cu_new: one token each, row s) and becomes token start[s] + i.  start < 0: the sequence is left as it is."""
-        n, dev = self.n_seqs, self.device
-        for name, x in (("k", k), ("v", v)):
-            if x.dtype != self.dtype or x.device != dev or x.dim() != 3 or x.shape[1:] != (self.n_kv_heads, self.head_dim):
-                _refuse("%s must be [tokens, %d, %d] %s on %s" % (name, self.n_kv_heads, self.head_dim, self.dtype, dev))
-        if k.shape != v.shape or k.stride() != v.stride() or k.stride(2) != 1:
+        n, dev, dtype, shape, st = self.n_seqs, self.device, self.dtype, k.shape, k.stride()
+        if k.dtype is not dtype or v.dtype is not dtype or k.device != dev or v.device != dev or len(shape) != 3 or \
+                shape[1] != self.n_kv_heads or shape[2] != self.head_dim:
+            _refuse("k and v must be [tokens, %d, %d] %s on %s" % (self.n_kv_heads, self.head_dim, dtype, dev))
+        if shape != v.shape or st != v.stride() or st[2] != 1:
             _refuse("k and v must have the same shape and strides, the last dimension contiguous")
-        p_start = _want(start, "start", dev, torch.int32, (n,))
-        p_cu = None if cu_new is None else _want(cu_new, "cu_new", dev, torch.int32, (n + 1,))
-        _check(lib().qevict_kv8_append(C.byref(self._view), k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.shape[0],
-                                       p_start, p_cu, max_new,
-                                       torch.cuda.current_stream(dev).cuda_stream if stream is None else stream.cuda_stream))
+        p_start = _want(start, "start", dev, _i32, (n,))
+        p_cu = None if cu_new is None else _want(cu_new, "cu_new", dev, _i32, (n + 1,))
+        _check(lib().qevict_kv8_append(self._view, k.data_ptr(), v.data_ptr(), st[0], st[1], shape[0], p_start, p_cu, max_new,
+                                       _current_stream(dev) if stream is None else stream.cuda_stream))
 
     def attn(self, q, lens, max_len=None, scores=None, scores_out=None, softmax_scale=0.0, out=None, return_lse=False, stream=None):
         """Attention of one token per sequence, q [n_seqs, H_q, d], over the first lens[s] tokens of each.  Returns out, or
         (out[, lse][, scores_out]): scores [n_seqs, max_blocks] plus the probability mass of every block, in a new tensor
         or in scores_out (which may be scores).  max_len: bound of lens (default: what the table can hold)."""
-        n, dev = self.n_seqs, self.device
-        if q.dim() != 3 or q.shape[0] != n or q.shape[2] != self.head_dim:
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.attn(q, lens, max_len, scores, scores_out, softmax_scale, out, return_lse)
+        n, dev, dtype, shape = self.n_seqs, self.device, self.dtype, q.shape
+        if len(shape) != 3 or shape[0] != n or shape[2] != self.head_dim:
             _refuse("q must be [%d, H_q, %d]" % (n, self.head_dim))
-        p_q, hq = _want(q, "q", dev, self.dtype), q.shape[1]
-        p_lens = _want(lens, "lens", dev, torch.int32, (n,))
+        p_q, hq = _want(q, "q", dev, dtype), shape[1]
+        p_lens = _want(lens, "lens", dev, _i32, (n,))
         if max_len is None:
             max_len = self.max_blocks * self.block
         grid = (n, self.max_blocks)
-        p_in = None if scores is None else _want(scores, "scores", dev, torch.float32, grid)
-        with _OnStream(dev, stream) as s:
-            if out is None:
-                out = torch.empty_like(q)
-            p_out = _want(out, "out", dev, self.dtype, q.shape)
-            lse = torch.empty((n, hq), dtype=torch.float32, device=dev) if return_lse else None
-            if scores_out is None and scores is not None:
-                scores_out = torch.empty(grid, dtype=torch.float32, device=dev)
-            p_so = None if scores_out is None else _want(scores_out, "scores_out", dev, torch.float32, grid)
-            need = C.c_uint64()
-            view = C.byref(self._view)
-            _check(lib().qevict_kv8_attn_scratch_bytes(view, hq, max_len, p_so is not None, C.byref(need)))
-            scratch = torch.empty(need.value, dtype=torch.uint8, device=dev)
-            _check(lib().qevict_kv8_attn(view, hq, softmax_scale, p_q, p_lens, max_len, p_out, None if lse is None else lse.data_ptr(),
-                                         p_in, p_so, scratch.data_ptr(), need.value, s))
-        rest = ((lse,) if return_lse else ()) + (() if scores_out is None else (scores_out,))
-        return (out,) + rest if rest else out
+        p_in = p_so = None
+        if scores is not None:
+            p_in = _want(scores, "scores", dev, _f32, grid)
+            if scores_out is None:
+                scores_out = torch.empty_like(scores)
+        if scores_out is not None:
+            p_so = _want(scores_out, "scores_out", dev, _f32, grid)
+        if out is None:
+            out = torch.empty_like(q)
+            p_out = out.data_ptr()
+        else:
+            p_out = _want(out, "out", dev, dtype, shape)
+        lse = q.new_empty((n, hq), dtype=_f32) if return_lse else None
+        need, view, library = C.c_uint64(), self._view, lib()
+        _check(library.qevict_kv8_attn_scratch_bytes(view, hq, max_len, p_so is not None, C.byref(need)))
+        scratch = q.new_empty(need.value, dtype=_u8)
+        _check(library.qevict_kv8_attn(view, hq, softmax_scale, p_q, p_lens, max_len, p_out, None if lse is None else lse.data_ptr(),
+                                       p_in, p_so, scratch.data_ptr(), need.value, _current_stream(dev)))
+        if lse is None:
+            return out if scores_out is None else (out, scores_out)
+        return (out, lse) if scores_out is None else (out, lse, scores_out)
 
 
 KERNEL_NAMES = ("append", "decode_attn", "combine", "route", "migrate")

@@ -1,6 +1,8 @@
 // Shared pieces of the 8-bit block-scaled cache: argument checks, code conversions.
 #pragma once
 
+#include <atomic>
+
 #include "ctx.h"
 
 namespace qevict {
@@ -35,6 +37,15 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
   return r;
+}
+
+// Runs `set` (function attributes of a kernel) once for each device; `done` has a bit per device and is the kernel's own.
+template <class F> inline cudaError_t once_per_device(std::atomic<uint64_t>& done, int device, F set) {
+  const uint64_t bit = device < 64 ? 1ull << device : 0ull;
+  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  const cudaError_t e = set();
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+  return e;
 }
 
 inline bool misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }

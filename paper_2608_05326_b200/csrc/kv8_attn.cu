@@ -734,32 +734,35 @@ const char* plan_of(const Kv8View& c, int Hq, int max_len, bool scores, int sms,
   return nullptr;
 }
 
-template <class T, int CODE, int D, int NT, int UT> cudaError_t launch_attn(const Kv8AttnArgs& a, cudaStream_t s) {
+template <class T, int CODE, int D, int NT, int UT> cudaError_t launch_attn(const Kv8AttnArgs& a, int device, cudaStream_t s) {
   constexpr int RING = ring_of(UT);
   const size_t smem = (size_t)WARPS * RING * UT * D + (size_t)(a.c.n_seqs + 1) * sizeof(int);
   auto kernel = kv8_attn_kernel<T, CODE, D, NT, UT>;
-  cudaError_t e = cudaSuccess;
-  if (smem > 48 * 1024) {  // one size for every call, so that calls with different batches do not lower each other's limit
-    constexpr int most = WARPS * RING * UT * D + 8193 * (int)sizeof(int);
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-  }
+  static std::atomic<uint64_t> done{0};
+  cudaError_t e = once_per_device(done, device, [&] {  // the largest batch that is taken
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, WARPS * RING * UT * D + 8193 * (int)sizeof(int));
+  });
   if (e == cudaSuccess) e = launch_pdl(kernel, dim3(a.n_warps / WARPS), dim3(ATTN_THREADS), smem, s, a);
   return e;
 }
 
-template <class T, int CODE, int D, int NT> cudaError_t launch_attn_ut(const Kv8AttnArgs& a, int ut, cudaStream_t s) {
-  return ut == 32 ? launch_attn<T, CODE, D, NT, 32>(a, s) : launch_attn<T, CODE, D, NT, 16>(a, s);
+template <class T, int CODE, int D, int NT> cudaError_t launch_attn_ut(const Kv8AttnArgs& a, int ut, int device, cudaStream_t s) {
+  return ut == 32 ? launch_attn<T, CODE, D, NT, 32>(a, device, s) : launch_attn<T, CODE, D, NT, 16>(a, device, s);
 }
-template <class T, int CODE> cudaError_t launch_attn_shape(const Kv8AttnArgs& a, int ut, cudaStream_t s) {
+template <class T, int CODE> cudaError_t launch_attn_shape(const Kv8AttnArgs& a, int ut, int device, cudaStream_t s) {
   const bool wide = a.G > 8;
-  if (a.c.D == 128) return wide ? launch_attn_ut<T, CODE, 128, 2>(a, ut, s) : launch_attn_ut<T, CODE, 128, 1>(a, ut, s);
-  return wide ? launch_attn_ut<T, CODE, 64, 2>(a, ut, s) : launch_attn_ut<T, CODE, 64, 1>(a, ut, s);
+  if (a.c.D == 128) return wide ? launch_attn_ut<T, CODE, 128, 2>(a, ut, device, s) : launch_attn_ut<T, CODE, 128, 1>(a, ut, device, s);
+  return wide ? launch_attn_ut<T, CODE, 64, 2>(a, ut, device, s) : launch_attn_ut<T, CODE, 64, 1>(a, ut, device, s);
 }
-template <class T> cudaError_t launch_all(const Kv8AttnArgs& a, int code, int ut, cudaStream_t s) {
-  cudaError_t e = code == QEVICT_CODE_INT8 ? launch_attn_shape<T, QEVICT_CODE_INT8>(a, ut, s) : launch_attn_shape<T, QEVICT_CODE_E4M3>(a, ut, s);
+template <class T> cudaError_t launch_all(const Kv8AttnArgs& a, int code, int ut, int device, cudaStream_t s) {
+  cudaError_t e = code == QEVICT_CODE_INT8 ? launch_attn_shape<T, QEVICT_CODE_INT8>(a, ut, device, s) : launch_attn_shape<T, QEVICT_CODE_E4M3>(a, ut, device, s);
   // the same split of the SM's memory as the attention kernel's: an SM has to drain before it changes it
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(kv8_combine_kernel<T>, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(kv8_mass_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
+  static std::atomic<uint64_t> done{0};
+  if (e == cudaSuccess)
+    e = once_per_device(done, device, [] {
+      const cudaError_t x = cudaFuncSetAttribute(kv8_combine_kernel<T>, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
+      return x != cudaSuccess ? x : cudaFuncSetAttribute(kv8_mass_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
+    });
   if (e == cudaSuccess) e = launch_pdl(kv8_combine_kernel<T>, dim3(a.Hq, a.c.n_seqs), dim3(COMB_THREADS), 0, s, a);
   if (e == cudaSuccess && a.score_out) {
     const int per = MASS_THREADS / 32;
@@ -820,7 +823,7 @@ QEVICT_API qevict_status qevict_kv8_attn(const qevict_kv8_cache* cache, int32_t 
   cudaError_t e = guard.err;
   cudaStream_t s = (cudaStream_t)stream;
   if (e == cudaSuccess)
-    e = cache->dtype == QEVICT_DTYPE_FP16 ? launch_all<__half>(a, cache->code, p.ut, s) : launch_all<__nv_bfloat16>(a, cache->code, p.ut, s);
+    e = cache->dtype == QEVICT_DTYPE_FP16 ? launch_all<__half>(a, cache->code, p.ut, cache->device, s) : launch_all<__nv_bfloat16>(a, cache->code, p.ut, cache->device, s);
   if (e != cudaSuccess) return stateless_fail(QEVICT_ERR_CUDA, cudaGetErrorString(e));
   return QEVICT_OK;
 }

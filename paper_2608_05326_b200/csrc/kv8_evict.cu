@@ -170,8 +170,9 @@ extern "C" QEVICT_API qevict_status qevict_kv8_evict(const qevict_kv8_evict_args
   DeviceGuard guard(p->device);
   cudaError_t e = guard.err;
   const size_t smem = (size_t)p->max_blocks * 12;
+  static std::atomic<uint64_t> done{0};
   if (e == cudaSuccess && smem > 40 * 1024)
-    e = cudaFuncSetAttribute(kv8_evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, EVICT_MAX_BLOCKS * 12);
+    e = once_per_device(done, p->device, [] { return cudaFuncSetAttribute(kv8_evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, EVICT_MAX_BLOCKS * 12); });
   int nt = 128;  // a thread per entry up to 1024 threads
   while (nt < p->max_blocks && nt < EVICT_THREADS) nt <<= 1;
   if (e == cudaSuccess) e = launch_pdl(kv8_evict_kernel, dim3(p->n_seqs), dim3(nt), smem, (cudaStream_t)stream, *p);

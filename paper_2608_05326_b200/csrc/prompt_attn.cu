@@ -775,9 +775,10 @@ size_t prompt_bytes(const qevict_prompt_args* p, int splits) {
 }
 
 template <class T, int D>
-cudaError_t launch_prompt(const PromptArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t s) {
+cudaError_t launch_prompt(const PromptArgs& a, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, int device, cudaStream_t s) {
   auto kernel = prompt_attn_kernel<T, D>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptSmem<D>::BYTES);
+  static std::atomic<uint64_t> done{0};
+  cudaError_t e = once_per_device(done, device, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptSmem<D>::BYTES); });
   const unsigned m_tiles = (unsigned)((a.max_q + 2 * TILE - 1) / (2 * TILE));
   if (e == cudaSuccess)
     e = launch_pdl(kernel, dim3(m_tiles * a.splits, a.Hq, a.n_seqs), dim3(PROMPT_THREADS), PromptSmem<D>::BYTES, s, a, mq, mk, mv);
@@ -841,9 +842,9 @@ QEVICT_API qevict_status qevict_prompt_attn(const qevict_prompt_args* args, void
     return stateless_fail(QEVICT_ERR_CUDA, "a tensor map could not be made for q, k or v");
   cudaStream_t s = (cudaStream_t)stream;
   if (args->dtype == QEVICT_DTYPE_FP16)
-    e = a.D == 128 ? launch_prompt<__half, 128>(a, mq, mk, mv, s) : launch_prompt<__half, 64>(a, mq, mk, mv, s);
+    e = a.D == 128 ? launch_prompt<__half, 128>(a, mq, mk, mv, args->device, s) : launch_prompt<__half, 64>(a, mq, mk, mv, args->device, s);
   else
-    e = a.D == 128 ? launch_prompt<__nv_bfloat16, 128>(a, mq, mk, mv, s) : launch_prompt<__nv_bfloat16, 64>(a, mq, mk, mv, s);
+    e = a.D == 128 ? launch_prompt<__nv_bfloat16, 128>(a, mq, mk, mv, args->device, s) : launch_prompt<__nv_bfloat16, 64>(a, mq, mk, mv, args->device, s);
   if (e != cudaSuccess) return stateless_fail(QEVICT_ERR_CUDA, cudaGetErrorString(e));
   return QEVICT_OK;
 }
