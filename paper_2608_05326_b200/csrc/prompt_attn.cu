@@ -2,7 +2,8 @@
 //
 //     S = Q K^T,  P = 2^(S * scale * log2 e - m),  O += P V,  out = O / sum P,  lse = ln sum exp(scale * S)
 //
-// A work item is 256 query rows of one head, as two tiles of 128, against the keys in tiles of 128, last tile first.  A CTA
+// A work item is two tiles of 128 query rows (the heads that share a KV head, some tokens of each: see prompt_tile) against
+// the keys in tiles of 128, last tile first.  A CTA
 // stays on its SM and takes over grid positions that have not started (the hardware hands them out), so that one item's
 // start and results run beside another's products.  Twenty warps: eight for each query tile's softmax (two threads to a
 // row), one that issues the products, one that issues the copies, one that fetches work items.
@@ -40,6 +41,7 @@ constexpr float PROMPT_LAZY = 8.f;  // log2
 
 struct PromptArgs {
   int padded, n_seqs, Hq, Hkv, D, max_q, max_k, causal, splits;
+  int P, T;  // a tile's rows: P query heads of one KV head, T tokens each
   long long total_q, total_k;
   float scale_log2;
   void* out;
@@ -186,9 +188,9 @@ template <int D> struct PromptSmem {
   static constexpr int BYTES = BAR_OFF + ROWS + 2048;
 };
 
-// A work item: 256 query rows of one head of one sequence, or a part of their keys.
+// A work item: two tiles of T tokens of P heads of one sequence, or a part of their keys.
 struct PromptItem {
-  int valid, hq, s, split, r0, q0, nq, k0, nk;
+  int valid, h0, s, split, r0, q0, nq, k0, nk;  // h0: first query head, r0: first token
   int lo, n;       // key tiles of this item
   int nt0, nt1;    // end of the two query tiles' key tiles
   __device__ __forceinline__ int cnt(int w) const { return max(0, (w ? nt1 : nt0) - lo); }
@@ -198,10 +200,10 @@ struct PromptItem {
 // The item of grid position (x, y, z); not valid where the sequence has no such rows.
 __device__ __forceinline__ PromptItem item_of(const PromptArgs& a, int x, int y, int z) {
   PromptItem it;
-  const int m_tiles = (a.max_q + 2 * TILE - 1) / (2 * TILE), mt = x / a.splits;
+  const int m_tiles = (a.max_q + 2 * a.T - 1) / (2 * a.T), mt = x / a.splits;
   it.split = x - mt * a.splits;
-  it.r0 = (a.causal ? m_tiles - 1 - mt : mt) * 2 * TILE;  // the longest rows first
-  it.hq = y;
+  it.r0 = (a.causal ? m_tiles - 1 - mt : mt) * 2 * a.T;  // the longest rows first
+  it.h0 = y * a.P;
   it.s = z;
   span_of(a.q_bounds, a.padded, z, a.max_q, a.total_q, &it.q0, &it.nq);
   span_of(a.k_bounds, a.padded, z, a.max_k, a.total_k, &it.k0, &it.nk);
@@ -209,7 +211,7 @@ __device__ __forceinline__ PromptItem item_of(const PromptArgs& a, int x, int y,
   int nt[2];
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
-    const int rw = it.r0 + w * TILE, last = min(rw + TILE, it.nq) - 1;
+    const int rw = it.r0 + w * a.T, last = min(rw + a.T, it.nq) - 1;
     const int lim = rw >= it.nq ? 0 : (a.causal ? min(it.nk, last + it.nk - it.nq + 1) : it.nk);
     nt[w] = lim > 0 ? (lim + TILE - 1) / TILE : 0;
   }
@@ -333,17 +335,17 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       uint32_t phase = 0;
       while (const PromptItem* item = next_item()) {
         const PromptItem& it = *item;
-        const int cs = a.padded ? it.s : 0, loads = 2 * (it.n - it.lo), hk = it.hq / (a.Hq / a.Hkv);
+        const int cs = a.padded ? it.s : 0, loads = 2 * (it.n - it.lo), hk = it.h0 / (a.Hq / a.Hkv);
         if (loads == 0) continue;
         if (q_turn > 0) ok = warp_wait<true>(b_qe, (uint32_t)(q_turn - 1) & 1u);
         ++q_turn;
         if (ok && lane == 0) {
-          bar_expect(b_q, (uint32_t)((it.cnt(0) > 0) + (it.cnt(1) > 0)) * SM::TILE_BYTES);
+          bar_expect(b_q, (uint32_t)((it.cnt(0) > 0) + (it.cnt(1) > 0)) * (uint32_t)(a.T * a.P * D * 2));
 #pragma unroll
           for (int w = 0; w < 2; ++w)
             if (it.cnt(w) > 0)
               for (int x = 0; x < D / 64; ++x)
-                tma_load(smb + SM::Q_OFF + w * SM::TILE_BYTES + x * SM::HALF, &mq, b_q, x * 64, it.q0 + it.r0 + w * TILE, it.hq, cs);
+                tma_load(smb + SM::Q_OFF + w * SM::TILE_BYTES + x * SM::HALF, &mq, b_q, x * 64, it.q0 + it.r0 + w * a.T, it.h0, cs);
           words[7] = 1;
         }
         int v_slot = 0;
@@ -491,6 +493,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
     // Two threads to a row: 64 keys of every tile each.  The two warps that share rows meet at a barrier of their own,
     // where each also says whether a wait of its has run out, so that both leave at the same point.
     const int w = wid >> 3, half = (wid >> 2) & 1, r = (wid & 3) * 32 + lane;
+    const int hl = r / a.T, tok = w * a.T + r - hl * a.T;  // head and token of this row; rows past P heads are not used
     const uint32_t lane_base = (uint32_t)((wid & 3) * 32) << 16;
     const uint32_t ts = tmem + lane_base + w * 128, to = tmem + lane_base + 256 + w * 128 + half * (D / 2);
     float* xch = reinterpret_cast<float*>(sm + SM::BAR_OFF + SM::ROWS) + w * 2 * TILE + r;  // the two halves' values of a row
@@ -507,7 +510,8 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       const PromptItem& it = *item;
       const int cnt = it.cnt(w);
       // keys that this row still sees from the tile's (this half's) first on; grows by a tile each time
-      int left = (a.causal ? min(it.nk, it.r0 + w * TILE + r + it.nk - it.nq + 1) : it.nk) - ((w ? it.nt1 : it.nt0) - 1) * TILE - half * (TILE / 2);
+      int left = (a.causal ? min(it.nk, it.r0 + tok + it.nk - it.nq + 1) : it.nk) - ((w ? it.nt1 : it.nt0) - 1) * TILE - half * (TILE / 2);
+      const bool mine = it.r0 + tok < it.nq && hl < a.P;  // rows of nobody hold anything, and have no say below
       float m = -INFINITY, l = 0.f;
       for (int i = cnt; i > 0; --i, left += TILE) {
         // S(j) stands for P V of the tile before too: a commit waits for everything its thread has issued before
@@ -535,7 +539,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         meet();
         if (!ok) break;
         const float top_x = fmaxf(xch[0], xch[TILE]) * a.scale_log2;
-        if (__any_sync(0xffffffffu, top_x > m + PROMPT_LAZY)) {
+        if (__any_sync(0xffffffffu, mine && top_x > m + PROMPT_LAZY)) {
           const float m_new = fmaxf(m, top_x);
           const float f = m_new == m ? 1.f : ex2p(m - m_new);
           m = m_new;
@@ -587,20 +591,19 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       meet();
       if (!ok) break;
       l = xch[0] + xch[TILE];
-      const int row = it.r0 + w * TILE + r;  // of the sequence
+      const int row = it.r0 + tok, hq = it.h0 + hl;
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      const bool mine = row < it.nq;
       const long long prow = a.padded ? (long long)it.s * a.max_q + row : (long long)it.q0 + row;
       const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
       if (mine && half == 0) {
         if (a.splits > 1)
-          a.part_lse[((long long)it.split * a.rows + prow) * a.Hq + it.hq] = lse2;
+          a.part_lse[((long long)it.split * a.rows + prow) * a.Hq + hq] = lse2;
         else if (a.lse)
-          a.lse[a.padded ? ((long long)it.s * a.Hq + it.hq) * a.max_q + row : it.hq * a.total_q + prow] = lse2 * 0.6931471805599453f;
+          a.lse[a.padded ? ((long long)it.s * a.Hq + hq) * a.max_q + row : hq * a.total_q + prow] = lse2 * 0.6931471805599453f;
       }
       T* out = static_cast<T*>(a.out) + (a.padded ? it.s * a.out_stride[0] + row * a.out_stride[2] : prow * a.out_stride[2]) +
-               it.hq * a.out_stride[1] + half * (D / 2);
-      float* po = a.part_o + (((long long)it.split * a.rows + prow) * a.Hq + it.hq) * D + half * (D / 2);
+               hq * a.out_stride[1] + half * (D / 2);
+      float* po = a.part_o + (((long long)it.split * a.rows + prow) * a.Hq + hq) * D + half * (D / 2);
 #pragma unroll 1
       for (int c = 0; c < D / 2; c += 16) {
         float o[16];
@@ -686,15 +689,16 @@ EncodeFn encode_fn() {
   return fn;
 }
 
-// {channel, token, head, sequence} map of boxes of 64 channels x 128 tokens
-bool make_map(CUtensorMap* map, int dtype, const void* base, int D, long long tokens, int heads, long long seqs, const int64_t* stride) {
+// {channel, token, head, sequence} map of boxes of 64 channels x some tokens x some heads
+bool make_map(CUtensorMap* map, int dtype, const void* base, int D, long long tokens, int heads, long long seqs, const int64_t* stride,
+              int box_tokens, int box_heads) {
   memset(map, 0, sizeof(*map));
   if (tokens < 1) return true;  // no rows: no copy is made
   const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)tokens, (cuuint64_t)heads, (cuuint64_t)seqs};
   // a dimension of one element has no stride that matters
   const cuuint64_t st[3] = {(cuuint64_t)(tokens > 1 ? stride[2] : D) * 2, (cuuint64_t)(heads > 1 ? stride[1] : D) * 2,
                             (cuuint64_t)(seqs > 1 ? stride[0] : D) * 2};
-  const cuuint32_t box[4] = {64, TILE, 1, 1}, el[4] = {1, 1, 1, 1};
+  const cuuint32_t box[4] = {64, (cuuint32_t)box_tokens, (cuuint32_t)box_heads, 1}, el[4] = {1, 1, 1, 1};
   EncodeFn fn = encode_fn();
   return fn && fn(map, dtype == QEVICT_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base),
                   dims, st, box, el, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -753,14 +757,30 @@ int prompt_sms(int device) {
   return n;
 }
 
-// CTAs that share a query tile's keys: more than one only where the query tiles alone leave SMs idle and there are keys
-// enough (at least four tiles each).
+// Rows of a query tile: the heads that share a KV head side by side (P of them, the largest divisor of the group up to 32),
+// as many tokens of each as fit 128 rows.  Never more tiles than one head at a time, fewer for few tokens, and the
+// triangle at the causal edge is P times narrower.
+void prompt_tile(const qevict_prompt_args* p, int* P, int* T) {
+  const int G = p->n_q_heads / p->n_kv_heads;
+  *P = G < 32 ? G : 32;
+  while (G % *P) --*P;
+  *T = TILE / *P;
+}
+
+// Work items that share a query tile's keys.  Where the query tiles leave SMs idle, as many as fill them (at least four key
+// tiles each); where they make fewer than one and a half rounds of the SMs and there are keys enough (16 tiles each), as
+// many as make that: a piece of 500 tokens behind 16000 next to one of 166 behind 3714, 28 heads, 236 -> 175 us with two
+// items for each tile, 215, 183, 187 us with three, four, six.
 int prompt_splits(const qevict_prompt_args* p) {
-  const long long tiles = ((long long)p->max_q + 2 * TILE - 1) / (2 * TILE) * p->n_q_heads * p->n_seqs;
+  int P, T;
+  prompt_tile(p, &P, &T);
+  const long long tiles = ((long long)p->max_q + 2 * T - 1) / (2 * T) * (p->n_q_heads / P) * p->n_seqs;
   const long long key_tiles = ((long long)p->max_k + TILE - 1) / TILE;
   if (tiles < 1) return 1;
-  long long s = prompt_sms(p->device) / tiles;
+  const long long sms = prompt_sms(p->device), even = (3 * sms / 2 + tiles - 1) / tiles;
+  long long s = sms / tiles;
   if (s > key_tiles / 4) s = key_tiles / 4;
+  if (even > s && key_tiles / even >= 16) s = even;
   return (int)(s < 1 ? 1 : (s > 64 ? 64 : s));
 }
 
@@ -779,9 +799,9 @@ cudaError_t launch_prompt(const PromptArgs& a, const CUtensorMap& mq, const CUte
   auto kernel = prompt_attn_kernel<T, D>;
   static std::atomic<uint64_t> done{0};
   cudaError_t e = once_per_device(done, device, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptSmem<D>::BYTES); });
-  const unsigned m_tiles = (unsigned)((a.max_q + 2 * TILE - 1) / (2 * TILE));
+  const unsigned m_tiles = (unsigned)((a.max_q + 2 * a.T - 1) / (2 * a.T));
   if (e == cudaSuccess)
-    e = launch_pdl(kernel, dim3(m_tiles * a.splits, a.Hq, a.n_seqs), dim3(PROMPT_THREADS), PromptSmem<D>::BYTES, s, a, mq, mk, mv);
+    e = launch_pdl(kernel, dim3(m_tiles * a.splits, a.Hq / a.P, a.n_seqs), dim3(PROMPT_THREADS), PromptSmem<D>::BYTES, s, a, mq, mk, mv);
   if (e == cudaSuccess && a.splits > 1) {
     const unsigned ctas = (unsigned)(((long long)a.max_q * a.Hq + 7) / 8);
     e = launch_pdl(prompt_merge_kernel<T>, dim3(ctas, a.n_seqs), dim3(256), 0, s, a);
@@ -817,6 +837,7 @@ QEVICT_API qevict_status qevict_prompt_attn(const qevict_prompt_args* args, void
   PromptArgs a;
   a.padded = padded; a.n_seqs = args->n_seqs; a.Hq = args->n_q_heads; a.Hkv = args->n_kv_heads; a.D = args->head_dim;
   a.max_q = args->max_q; a.max_k = args->max_k; a.causal = args->causal;
+  prompt_tile(args, &a.P, &a.T);
   a.splits = prompt_splits(args);
   const size_t need = prompt_bytes(args, a.splits);
   if (need > 0 && (!scratch || scratch_bytes < need))
@@ -836,9 +857,9 @@ QEVICT_API qevict_status qevict_prompt_attn(const qevict_prompt_args* args, void
   CUtensorMap mq, mk, mv;
   const long long nq = padded ? args->max_q : args->total_q, nk = padded ? args->max_k : args->total_k;
   const long long seqs = padded ? args->n_seqs : 1;
-  if (!make_map(&mq, args->dtype, args->q, a.D, nq, a.Hq, seqs, args->q_stride) ||
-      !make_map(&mk, args->dtype, args->k, a.D, args->max_k > 0 ? nk : 0, a.Hkv, seqs, args->k_stride) ||
-      !make_map(&mv, args->dtype, args->v, a.D, args->max_k > 0 ? nk : 0, a.Hkv, seqs, args->v_stride))
+  if (!make_map(&mq, args->dtype, args->q, a.D, nq, a.Hq, seqs, args->q_stride, a.T, a.P) ||
+      !make_map(&mk, args->dtype, args->k, a.D, args->max_k > 0 ? nk : 0, a.Hkv, seqs, args->k_stride, TILE, 1) ||
+      !make_map(&mv, args->dtype, args->v, a.D, args->max_k > 0 ? nk : 0, a.Hkv, seqs, args->v_stride, TILE, 1))
     return stateless_fail(QEVICT_ERR_CUDA, "a tensor map could not be made for q, k or v");
   cudaStream_t s = (cudaStream_t)stream;
   if (args->dtype == QEVICT_DTYPE_FP16)

@@ -197,6 +197,23 @@ def test_one_sequence_does_not_reach_into_the_next():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(7, 1, 64, torch.float16), (6, 2, 128, torch.bfloat16), (1, 1, 128, torch.float16)])
+def test_a_sequence_has_the_same_bits_whatever_is_next_to_it(hq, hkv, d, dtype):
+    # rows of a tile that belong to nobody, or to another sequence, must not decide when a row's reference moves
+    nq, nk = [37, 3, 150], [900, 3, 150]
+    q, k, v = (x.cuda() for x in _make(nq, nk, hq, hkv, d, dtype, 33, 4.0))
+    args = dict(max_q=150, max_k=900, return_lse=True)
+    alone = binding.qevict_prompt_attn(q, k, v, _cu(nq), _cu(nk), **args)
+    for fill in (1e4, float("nan"), float("inf")):
+        q2, k2, v2 = q.clone(), k.clone(), v.clone()
+        q2[37:40], k2[900:903], v2[900:903] = fill, fill, fill
+        binding.qevict_prompt_attn(torch.full_like(q, fill), k, v, _cu(nq), _cu(nk), **args)  # leaves other values on the SMs
+        out, lse = binding.qevict_prompt_attn(q2, k2, v2, _cu(nq), _cu(nk), **args)
+        for a, b in ((0, 37), (40, 190)):
+            assert torch.equal(out[a:b], alone[0][a:b]) and torch.equal(lse[:, a:b], alone[1][:, a:b])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("d,dtype", [(128, torch.bfloat16), (64, torch.float16)])
 def test_padded_layout_with_lengths(d, dtype):
     n, hq, hkv, m = 4, 4, 2, 300
