@@ -65,6 +65,7 @@ inline const char* kv8_check(const qevict_kv8_cache* c, qevict_status* st, Kv8Vi
   if (c->head_dim != 64 && c->head_dim != 128) return "head_dim must be 64 or 128";
   if (c->block != 16 && c->block != 32 && c->block != 64 && c->block != 128) return "block must be 16, 32, 64 or 128 tokens";
   if (c->n_kv_heads > 1024 || c->n_seqs > 8192) return "more than 1024 KV heads or 8192 sequences";
+  if ((long long)c->n_pages * c->n_kv_heads > 0x7fffffffll) return "n_pages * n_kv_heads exceeds 2^31 - 1";
   if ((long long)c->max_blocks * c->block > (1ll << 30)) return "max_blocks * block exceeds 2^30 tokens";
   *st = QEVICT_ERR_INVALID_ARG;
   if (c->n_pages > 0 && (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale)) return "code pools and scales must not be NULL";

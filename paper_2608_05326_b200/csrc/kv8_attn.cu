@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
   const long long u_end = run_start(total, n_runs, w + 1);
   unsigned char* ring = sm + wid * RING * STAGE;
   const uint32_t ring_a = (uint32_t)__cvta_generic_to_shared(ring);
-  const int upb = c.block / UT;  // units per block
+  const int upb_log2 = __ffs(c.block / UT) - 1, block_log2 = __ffs(c.block) - 1;  // units of a block; both are powers of two
 
   while (u < u_end) {
     const int s = seq_of(pre, c.n_seqs, (int)(u / c.Hkv));
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
     const int i0 = (int)(in_seq - (long long)h * nu), i1 = (int)min((long long)nu, i0 + (u_end - u));
     const int row = s * c.Hkv + h;
     const int len = clamp_len(a, a.lens[s]);
-    const int n_code = len / c.block * upb;  // units that lie in full blocks
+    const int n_code = len >> block_log2 << upb_log2;  // units that lie in full blocks
     u += i1 - i0;
 
     // queries of this KV head: B fragments in fp16, divided by a power of two per head
@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
       auto fetch = [&](int blk0, int& page) {
         page = -1;
         const int b = blk0 + lane;
-        if (b < n_code / upb) {
+        if (b < n_code >> upb_log2) {
           page = c.table[(size_t)s * c.max_blocks + b];
           if (page < 0 || page >= c.n_pages) {
             if (page != -1) kv8_record(c.status, CHECK_PAGE_ID);
@@ -317,19 +317,20 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
           }
         }
       };
-      int f_blk0 = i0 / upb, f_page;  // producer's window of 32 blocks
+      int f_blk0 = i0 >> upb_log2, f_page;  // producer's window of 32 blocks
       fetch(f_blk0, f_page);
       const int e_end = 2 * (e1 - i0);
       auto issue = [&](int e) {  // stage e: keys (even) or values of unit i0 + e / 2
         if (e < e_end) {
-          const int i = i0 + (e >> 1), kv = e & 1, b = i / upb;
+          const int i = i0 + (e >> 1), kv = e & 1, b = i >> upb_log2;
           if (b >= f_blk0 + 32) {
             f_blk0 += 32;
             fetch(f_blk0, f_page);
           }
           const int page = __shfl_sync(0xffffffffu, f_page, b - f_blk0);
           if (page >= 0) {
-            const uint8_t* src = (kv ? c.codes[1] : c.codes[0]) + (((size_t)page * c.Hkv + h) * c.block + (size_t)(i - b * upb) * UT) * D;
+            const uint8_t* src = (kv ? c.codes[1] : c.codes[0]) +
+                                 (((size_t)((unsigned)page * (unsigned)c.Hkv + (unsigned)h) << block_log2) + (unsigned)((i - (b << upb_log2)) * UT)) * D;
             const uint32_t dst = ring_a + (uint32_t)(e % RING) * STAGE;
 #pragma unroll
             for (int n = 0; n < UT * D / 512; ++n) {
@@ -345,10 +346,10 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
         __syncwarp();
       };
       for (int e = 0; e < RING - 1; ++e) issue(e);
-      int s_blk0 = i0 / upb - 32, s_page = -1;
+      int s_blk0 = (i0 >> upb_log2) - 32, s_page = -1;
       float s_k = 0.f, s_v = 0.f;
       for (int i = i0; i < e1; ++i) {
-        const int b = i / upb;
+        const int b = i >> upb_log2;
         if (b >= s_blk0 + 32) {  // consumer's window: scales too
           s_blk0 = s_blk0 + 32 > b ? s_blk0 + 32 : b;
           fetch(s_blk0, s_page);
@@ -665,8 +666,7 @@ __global__ void __launch_bounds__(COMB_THREADS) kv8_combine_kernel(const Kv8Attn
 }
 
 // Block masses: one warp per (block, sequence), a lane per head, every load requested at once, fixed shuffle tree.  (As a part
-// of the merge -- each of its CTAs working out all heads' statistics for itself -- the two took longer than apart: 18
-// against 14 us at one sequence of 2048 tokens.)
+// of the merge, whose CTAs then work out all heads' statistics for themselves, the two took 2 to 4 us longer than apart.)
 constexpr int MASS_THREADS = 256;
 __global__ void __launch_bounds__(MASS_THREADS) kv8_mass_kernel(const Kv8AttnArgs a, int ut) {
   const int s = blockIdx.y, lane = threadIdx.x & 31, b = blockIdx.x * (MASS_THREADS / 32) + (threadIdx.x >> 5);

@@ -2,9 +2,11 @@
 //
 // One CTA per sequence.  Scores become 32-bit keys that order like them (NaN lowest, -0 equal to 0); the key of the
 // last block that is kept among the candidates comes from a radix selection (four 8-bit digits, histograms in shared
-// memory); blocks above it stay, and of those equal to it the first ones in block order do.  Two block-wide scans per
-// 1024 entries turn the decisions into places.  A few tens of KB per sequence: the launch and the dependent steps are
-// all the time there is.
+// memory); blocks above it stay, and of those equal to it the first ones in block order do.  A scan over the CTA for each
+// 1024 blocks turns the decisions into places (a second one where only some of the equal ones stay).  The data are a few
+// tens of KB per sequence: the launch, the dependent steps and fetching code that runs once are all the time there is, so the
+// loops stay rolled.  (16 sequences of 8192 blocks: 17 us; keys in registers with unrolled rounds and counts against
+// thresholds in place of the histograms took 23 us, a run of consecutive blocks per thread 25 us: its stores scatter.)
 #include "kv8.cuh"
 
 namespace qevict {
@@ -50,10 +52,11 @@ __global__ void __launch_bounds__(EVICT_THREADS) kv8_evict_kernel(const qevict_k
   const int mb = a.max_blocks, s = blockIdx.x, tid = threadIdx.x, nt = blockDim.x, lane = tid & 31;
   int32_t* s_page = reinterpret_cast<int32_t*>(s_key + mb);
   float* s_score = reinterpret_cast<float*>(s_page + mb);
-  __shared__ uint32_t hist[256], s_warp[32], s_pick[2];
+  __shared__ uint32_t hist[256], s_warp[32], s_pick[3];
   pdl_prologue();
   const size_t row = (size_t)s * mb;
   const int len = a.lens[s];
+#pragma unroll 4
   for (int i = tid; i < mb; i += nt) {  // everything is read before anything is written: the outputs may be the inputs
     const float x = a.scores[row + i];
     s_score[i] = x;
@@ -65,11 +68,13 @@ __global__ void __launch_bounds__(EVICT_THREADS) kv8_evict_kernel(const qevict_k
   const int c0 = a.sink, c1 = full - a.recent;                // candidates
   const int want = a.budget - a.sink - a.recent;              // of them stay
   uint32_t cut = 0xffffffffu;  // candidates with a larger key stay,
-  int ties = 0;                // and the first `ties` with this key
+  int ties = 0;                // and the first `ties` with this key,
+  bool all_ties = true;        // which may be all of them
   __syncthreads();
   if (over && want > 0) {
     uint32_t prefix = 0, mask = 0;
     int left = want;
+#pragma unroll 1
     for (int shift = 24; shift >= 0; shift -= 8) {
       for (int i = tid; i < 256; i += nt) hist[i] = 0;
       __syncthreads();
@@ -91,7 +96,11 @@ __global__ void __launch_bounds__(EVICT_THREADS) kv8_evict_kernel(const qevict_k
         uint32_t run = inc - sum;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          if (run < (uint32_t)left && run + mine[j] >= (uint32_t)left) { s_pick[0] = 255 - 8 * lane - j; s_pick[1] = run; }
+          if (run < (uint32_t)left && run + mine[j] >= (uint32_t)left) {
+            s_pick[0] = 255 - 8 * lane - j;
+            s_pick[1] = run;
+            s_pick[2] = mine[j];
+          }
           run += mine[j];
         }
       }
@@ -99,6 +108,7 @@ __global__ void __launch_bounds__(EVICT_THREADS) kv8_evict_kernel(const qevict_k
       prefix |= s_pick[0] << shift;
       mask |= 255u << shift;
       left -= (int)s_pick[1];
+      all_ties = left == (int)s_pick[2];
       __syncthreads();
     }
     cut = prefix;
@@ -106,16 +116,17 @@ __global__ void __launch_bounds__(EVICT_THREADS) kv8_evict_kernel(const qevict_k
   }
   // places, `nt` entries at a time
   int n_keep = 0, n_free = 0, n_tie = 0;
+#pragma unroll 1
   for (int base = 0; base < mb; base += nt) {
     const int i = base + tid;
     const bool in = i < mb, cand = in && over && i >= c0 && i < c1;
     const uint32_t k = cand ? s_key[i] : 0u;
     const bool tie = cand && want > 0 && k == cut;
     uint32_t total;
-    bool keep = in;
-    if (over) {
+    bool keep = in && (!cand || (want > 0 && k > cut) || (tie && all_ties));
+    if (!all_ties) {
       const uint32_t tb = block_scan(tie ? 1u : 0u, s_warp, &total);
-      if (cand) keep = want > 0 && (k > cut || (tie && n_tie + (int)tb < ties));
+      keep = keep || (tie && n_tie + (int)tb < ties);
       n_tie += (int)total;
     }
     const int page = in ? s_page[i] : -1;

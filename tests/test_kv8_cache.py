@@ -74,7 +74,7 @@ def _evict(**over):
     (dict(struct_size=4), 1, "struct_size"), (dict(device=-2), 1, "device"), (dict(dtype=5), 1, "dtype"), (dict(code=2), 1, "code"),
     (dict(n_seqs=-1), 1, "n_seqs"), (dict(head_dim=80), 4, "head_dim"), (dict(block=48), 4, "block"), (dict(n_kv_heads=0), 1, "n_kv_heads"),
     (dict(k_codes=None), 1, "NULL"), (dict(v_scale=None), 1, "NULL"), (dict(k_tail=None), 1, "NULL"), (dict(block_table=None), 1, "NULL"),
-    (dict(k_codes=4104), 1, "aligned"), (dict(v_tail=4100), 1, "aligned"), (dict(k_scale=4097), 1, "aligned"), (dict(max_blocks=1 << 30), 4, "2^30"),
+    (dict(k_codes=4104), 1, "aligned"), (dict(v_tail=4100), 1, "aligned"), (dict(k_scale=4097), 1, "aligned"), (dict(max_blocks=1 << 30), 4, "2^30"), (dict(n_pages=2 ** 30 + 1), 4, "n_pages"),
 ])
 def test_unusable_caches_are_refused_with_a_reason(over, status, word):
     for st in (_append(_view(**over)), _attn(_view(**over))):
