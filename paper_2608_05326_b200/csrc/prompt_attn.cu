@@ -197,17 +197,49 @@ struct PromptItem {
   __device__ __forceinline__ bool dirty() const { return n > lo && n * TILE > nk; }  // the first tile reaches past the sequence
 };
 
-// The item of grid position (x, y, z); not valid where the sequence has no such rows.
-__device__ __forceinline__ PromptItem item_of(const PromptArgs& a, int x, int y, int z) {
+// The item of grid position x, for a whole warp; not valid where x lies past the last sequence's.  Positions run over the
+// parts of the keys, then the tiles (the longest rows first), then the heads, then the sequences, by the sequences' own lengths,
+// so a batch of very different lengths has next to no empty positions.  *at, *before: where the last search ended (sequences
+// in groups of 32, tiles before them); positions only grow.
+__device__ __forceinline__ PromptItem item_of(const PromptArgs& a, int x, int lane, int* at, int* before) {
   PromptItem it;
-  const int m_tiles = (a.max_q + 2 * a.T - 1) / (2 * a.T), mt = x / a.splits;
-  it.split = x - mt * a.splits;
-  it.r0 = (a.causal ? m_tiles - 1 - mt : mt) * 2 * a.T;  // the longest rows first
-  it.h0 = y * a.P;
-  it.s = z;
-  span_of(a.q_bounds, a.padded, z, a.max_q, a.total_q, &it.q0, &it.nq);
-  span_of(a.k_bounds, a.padded, z, a.max_k, a.total_k, &it.k0, &it.nk);
-  it.valid = it.r0 < it.nq;
+  const int t = x / a.splits, step = 2 * a.T;
+  it.split = x - t * a.splits;
+  it.h0 = 0;
+  it.valid = 0;
+  it.s = 0;
+  const int groups = a.Hq / a.P;
+  int mt = 0;
+  for (; *at < a.n_seqs; *at += 32) {
+    const int s = *at + lane;
+    int first, n = 0;
+    if (s < a.n_seqs) span_of(a.q_bounds, a.padded, s, a.max_q, a.total_q, &first, &n);
+    const int tiles = (n + step - 1) / step;
+    int end = tiles * groups;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, end, o);
+      if (lane >= o) end += v;
+    }
+    end += *before;
+    const uint32_t past = __ballot_sync(0xffffffffu, t < end);
+    if (past) {
+      const int who = __ffs(past) - 1;
+      it.valid = 1;
+      it.s = *at + who;
+      const int who_tiles = __shfl_sync(0xffffffffu, tiles, who);
+      const int in = t - (__shfl_sync(0xffffffffu, end, who) - who_tiles * groups), head = in / who_tiles;
+      mt = in - head * who_tiles;
+      if (a.causal) mt = who_tiles - 1 - mt;
+      it.h0 = head * a.P;
+      break;
+    }
+    *before = __shfl_sync(0xffffffffu, end, 31);
+  }
+  it.r0 = mt * step;
+  if (!it.valid) return it;
+  span_of(a.q_bounds, a.padded, it.s, a.max_q, a.total_q, &it.q0, &it.nq);
+  span_of(a.k_bounds, a.padded, it.s, a.max_k, a.total_k, &it.k0, &it.nk);
   int nt[2];
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
@@ -295,14 +327,14 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       // Work items: the CTA's own grid position first, then positions that have not started, taken over one at a time
       // while the item before is in work.  (A grid of single-item CTAs pays for start, first loads and results of every
       // item with idle tensor cores: 12 packed prompts of up to 4001 tokens took 620 us.)
-      int x = blockIdx.x, y = blockIdx.y, z = blockIdx.z, put = 0;
+      int x = blockIdx.x, y, z, put = 0, at = 0, before = 0;
       for (uint32_t ask = 0; ok; ++ask) {
         if (lane == 0) {
           bar_expect(b_next, 16);
           asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
                            smem_u32((void*)words)), "r"(b_next) : "memory");
         }
-        const PromptItem it = item_of(a, x, y, z);
+        const PromptItem it = item_of(a, x, lane, &at, &before);
         if (it.valid) {
           if (put >= 2) ok = warp_wait<true>(b_taken + 8 * (put & 1), (uint32_t)((put >> 1) - 1) & 1u);
           if (ok && lane == 0) {
@@ -705,6 +737,22 @@ bool make_map(CUtensorMap* map, int dtype, const void* base, int D, long long to
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Rows of a query tile: the heads that share a KV head side by side (P of them, the largest divisor of the group up to 32),
+// as many tokens of each as fit 128 rows.  Never more tiles than one head at a time, fewer for few tokens, and the
+// triangle at the causal edge is P times narrower.
+void prompt_tile(const qevict_prompt_args* p, int* P, int* T) {
+  const int G = p->n_q_heads / p->n_kv_heads;
+  *P = G < 32 ? G : 32;
+  while (G % *P) --*P;
+  *T = TILE / *P;
+}
+
+// Most tile pairs that the sequences can have, for one group of heads: with max_q rows each, or total_q rows cut anywhere.
+long long prompt_tiles(bool padded, int n_seqs, long long max_q, long long total_q, int T) {
+  const long long each = n_seqs * ((max_q + 2 * T - 1) / (2 * T)), all = total_q / (2 * T) + n_seqs;
+  return padded || each < all ? each : all;
+}
+
 const char* prompt_check(const qevict_prompt_args* p, qevict_status* st) {
   *st = QEVICT_ERR_INVALID_ARG;
   if (!p) return "args is NULL";
@@ -721,6 +769,10 @@ const char* prompt_check(const qevict_prompt_args* p, qevict_status* st) {
   if (p->n_seqs > 65535 || p->n_q_heads > 1024) return "more than 65535 sequences or 1024 heads";
   if (p->total_q > 0x7fffffff - 1024 || p->total_k > 0x7fffffff - 1024 || p->max_q > 0x7fffffff - 1024 || p->max_k > 0x7fffffff - 1024)
     return "more than 2^31 - 1024 tokens";
+  int P, T;
+  prompt_tile(p, &P, &T);
+  if (prompt_tiles(p->layout == QEVICT_LAYOUT_PADDED, p->n_seqs, p->max_q, p->total_q, T) * (p->n_q_heads / P) > (1ll << 24))
+    return "more than 2^24 query tiles in one call";
   *st = QEVICT_ERR_INVALID_ARG;
   if (p->n_seqs > 0 && p->layout == QEVICT_LAYOUT_PACKED && (!p->q_bounds || !p->k_bounds)) return "the packed layout needs q_bounds and k_bounds";
   return nullptr;
@@ -757,36 +809,33 @@ int prompt_sms(int device) {
   return n;
 }
 
-// Rows of a query tile: the heads that share a KV head side by side (P of them, the largest divisor of the group up to 32),
-// as many tokens of each as fit 128 rows.  Never more tiles than one head at a time, fewer for few tokens, and the
-// triangle at the causal edge is P times narrower.
-void prompt_tile(const qevict_prompt_args* p, int* P, int* T) {
-  const int G = p->n_q_heads / p->n_kv_heads;
-  *P = G < 32 ? G : 32;
-  while (G % *P) --*P;
-  *T = TILE / *P;
-}
-
-// Work items that share a query tile's keys.  Where the query tiles leave SMs idle, as many as fill them (at least four key
-// tiles each); where they make fewer than one and a half rounds of the SMs and there are keys enough (16 tiles each), as
-// many as make that: a piece of 500 tokens behind 16000 next to one of 166 behind 3714, 28 heads, 236 -> 175 us with two
-// items for each tile, 215, 183, 187 us with three, four, six.
-int prompt_splits(const qevict_prompt_args* p) {
-  int P, T;
-  prompt_tile(p, &P, &T);
-  const long long tiles = ((long long)p->max_q + 2 * T - 1) / (2 * T) * (p->n_q_heads / P) * p->n_seqs;
-  const long long key_tiles = ((long long)p->max_k + TILE - 1) / TILE;
-  if (tiles < 1) return 1;
-  const long long sms = prompt_sms(p->device), even = (3 * sms / 2 + tiles - 1) / tiles;
-  long long s = sms / tiles;
-  if (s > key_tiles / 4) s = key_tiles / 4;
-  if (even > s && key_tiles / even >= 16) s = even;
-  return (int)(s < 1 ? 1 : (s > 64 ? 64 : s));
-}
-
 long long prompt_rows(const qevict_prompt_args* p) {
   return p->layout == QEVICT_LAYOUT_PADDED ? (long long)p->n_seqs * p->max_q : p->total_q;
 }
+// Work items that share a query tile's keys: the number that makes the call shortest by a model in key tiles (about 2 us).
+// An item costs its key tiles and some three more; items go to the SMs as these fall free, so the call takes the work of all
+// items over the SMs and about half an item for the uneven end, at least one item; and every part of the keys writes and reads
+// its rows' results in float32 once more.  (28 heads, a piece of 500 tokens behind 16000 next to one of 166 behind 3714: 237,
+// 174, 190, 157 us with one, two, three, five items for each tile; the model takes five.)
+int prompt_splits(const qevict_prompt_args* p) {
+  int P, T;
+  prompt_tile(p, &P, &T);
+  const double tiles = (double)prompt_tiles(p->layout == QEVICT_LAYOUT_PADDED, p->n_seqs, p->max_q, p->total_q, T) * (p->n_q_heads / P);
+  const double keys = (double)(((long long)p->max_k + TILE - 1) / TILE), sms = prompt_sms(p->device);
+  const double merge = (double)prompt_rows(p) * p->n_q_heads * p->head_dim * 8.0 / 8e6 / 2.0;  // bytes at 8 MB a us: they stay in the L2
+  int best = 1;
+  double least = 0.0;
+  for (int s = 1; s <= 64 && (s == 1 || keys / s >= 4.0); ++s) {
+    const double item = keys / s + 3.0, spread = tiles * s * item / sms + item / 2;
+    const double cost = (spread > item ? spread : item) + (s > 1 ? merge * s + 4.0 : 0.0);
+    if (s == 1 || cost < least) {
+      least = cost;
+      best = s;
+    }
+  }
+  return best;
+}
+
 size_t prompt_o_bytes(const qevict_prompt_args* p, int splits) {
   return ((size_t)splits * prompt_rows(p) * p->n_q_heads * p->head_dim * sizeof(float) + 255) & ~(size_t)255;
 }
@@ -799,9 +848,9 @@ cudaError_t launch_prompt(const PromptArgs& a, const CUtensorMap& mq, const CUte
   auto kernel = prompt_attn_kernel<T, D>;
   static std::atomic<uint64_t> done{0};
   cudaError_t e = once_per_device(done, device, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptSmem<D>::BYTES); });
-  const unsigned m_tiles = (unsigned)((a.max_q + 2 * a.T - 1) / (2 * a.T));
+  const long long tiles = prompt_tiles(a.padded, a.n_seqs, a.max_q, a.total_q, a.T);
   if (e == cudaSuccess)
-    e = launch_pdl(kernel, dim3(m_tiles * a.splits, a.Hq / a.P, a.n_seqs), dim3(PROMPT_THREADS), PromptSmem<D>::BYTES, s, a, mq, mk, mv);
+    e = launch_pdl(kernel, dim3((unsigned)(tiles * (a.Hq / a.P) * a.splits)), dim3(PROMPT_THREADS), PromptSmem<D>::BYTES, s, a, mq, mk, mv);
   if (e == cudaSuccess && a.splits > 1) {
     const unsigned ctas = (unsigned)(((long long)a.max_q * a.Hq + 7) / 8);
     e = launch_pdl(prompt_merge_kernel<T>, dim3(ctas, a.n_seqs), dim3(256), 0, s, a);
