@@ -197,44 +197,48 @@ struct PromptItem {
   __device__ __forceinline__ bool dirty() const { return n > lo && n * TILE > nk; }  // the first tile reaches past the sequence
 };
 
-// The item of grid position x, for a whole warp; not valid where x lies past the last sequence's.  Positions run over the
-// parts of the keys, then the tiles (the longest rows first), then the heads, then the sequences, by the sequences' own lengths,
-// so a batch of very different lengths has next to no empty positions.  *at, *before: where the last search ended (sequences
-// in groups of 32, tiles before them); positions only grow.
+// The item of grid position x, for a whole warp; not valid where x lies past the last sequence's.  Positions go by the
+// sequences' own lengths, so a batch of very different lengths has next to no empty positions, and by falling cost, so that the
+// SMs end together: sequences in groups of 32; in a group the tiles by falling number of keys, level by level (a level: the rows
+// of one tile more or less; a sequence's tiles have one each, from its prefix on); on a level the sequences that have it; then
+// the heads, then the parts of the keys.  *at, *before: where the last search ended (first sequence of the group, items before
+// it); positions only grow.
 __device__ __forceinline__ PromptItem item_of(const PromptArgs& a, int x, int lane, int* at, int* before) {
   PromptItem it;
-  const int t = x / a.splits, step = 2 * a.T;
+  const int t = x / a.splits, step = 2 * a.T, groups = a.Hq / a.P;
   it.split = x - t * a.splits;
   it.h0 = 0;
   it.valid = 0;
   it.s = 0;
-  const int groups = a.Hq / a.P;
   int mt = 0;
   for (; *at < a.n_seqs; *at += 32) {
     const int s = *at + lane;
-    int first, n = 0;
-    if (s < a.n_seqs) span_of(a.q_bounds, a.padded, s, a.max_q, a.total_q, &first, &n);
-    const int tiles = (n + step - 1) / step;
-    int end = tiles * groups;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, end, o);
-      if (lane >= o) end += v;
+    int first, n = 0, keys = 0;
+    if (s < a.n_seqs) {
+      span_of(a.q_bounds, a.padded, s, a.max_q, a.total_q, &first, &n);
+      span_of(a.k_bounds, a.padded, s, a.max_k, a.total_k, &first, &keys);
     }
-    end += *before;
-    const uint32_t past = __ballot_sync(0xffffffffu, t < end);
-    if (past) {
-      const int who = __ffs(past) - 1;
+    const int tiles = (n + step - 1) / step, base = (keys - n) / step, top = base + tiles;  // its levels: base .. top - 1
+    const int all = __reduce_add_sync(0xffffffffu, tiles) * groups, in = t - *before;
+    if (in < all) {
+      // the level: the largest L with more than `in` items on the levels from L on
+      auto from = [&](int level) { return __reduce_add_sync(0xffffffffu, min(tiles, max(0, top - level))) * groups; };
+      int lo = __reduce_min_sync(0xffffffffu, tiles ? base : 0x7fffffff), hi = __reduce_max_sync(0xffffffffu, tiles ? top - 1 : -0x7fffffff);
+      while (lo < hi) {
+        const int mid = lo + ((hi - lo + 1) >> 1);
+        if (from(mid) > in) lo = mid; else hi = mid - 1;
+      }
+      const int k = in - from(lo + 1), nth = k / groups;
+      uint32_t have = __ballot_sync(0xffffffffu, tiles > 0 && base <= lo && lo < top);
+      for (int i = 0; i < nth; ++i) have &= have - 1;
+      const int who = __ffs(have) - 1;
       it.valid = 1;
       it.s = *at + who;
-      const int who_tiles = __shfl_sync(0xffffffffu, tiles, who);
-      const int in = t - (__shfl_sync(0xffffffffu, end, who) - who_tiles * groups), head = in / who_tiles;
-      mt = in - head * who_tiles;
-      if (a.causal) mt = who_tiles - 1 - mt;
-      it.h0 = head * a.P;
+      it.h0 = (k - nth * groups) * a.P;
+      mt = lo - __shfl_sync(0xffffffffu, base, who);
       break;
     }
-    *before = __shfl_sync(0xffffffffu, end, 31);
+    *before += all;
   }
   it.r0 = mt * step;
   if (!it.valid) return it;
