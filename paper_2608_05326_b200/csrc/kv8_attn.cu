@@ -11,12 +11,16 @@
 // the order, so slots are distinct), and kv8_combine_kernel finds a row's slots from the same arithmetic.
 //
 // Tile.  Both products put the cache on the A side of mma.m16n8k16 (tokens, then channels on M; the G heads that
-// share the KV head on N).  Codes become fp16 operands in registers, exactly, and the block's scale multiplies the logits / the block's output in float32.  The contraction index may be permuted as long
-// as both sides agree, so a lane takes whole 4-byte words of its key row, and the token pairs of the values come out
-// of byte permutes.  The query goes to fp16 after a division by a power of two per head, which brings its largest
+// share the KV head on N).  Codes become fp16 operands in registers, exactly, and the block's scale multiplies the logits /
+// the block's output in float32.  The contraction index may be permuted as long as both sides agree, so a lane takes whole
+// 4-byte words of its key row, and the token pairs of the values come out of byte permutes.  The query goes to fp16 after a division by a power of two per head, which brings its largest
 // element into [1, 2): exact but for elements 2^-14 below the largest, which lose at most 2^-25 of it.
 // Probabilities enter the second product as fp16 (2^-11); the sums of the softmax, the block masses and the output
 // are float32.
+//
+// Measured: 16 ragged contexts of up to 32768 tokens, 32 / 8 heads of 128, int8 (472 MB): 105 us, of which this kernel 90 us
+// (5.2 TB/s; the copies without arithmetic 82 us), merge and masses the rest; 8 contexts of 65536, 28 / 4 heads, e4m3 (538 MB):
+// 109 us; one of 2048 tokens: 11 us, three dependent launches.  At 6.45 TB/s the bytes alone would take 73, 83 and 0.7 us.
 #include <cuda.h>
 
 #include "kv8.cuh"

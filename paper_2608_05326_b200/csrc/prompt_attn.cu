@@ -16,7 +16,8 @@
 // What bounds it: at d = 128 a key tile costs both query tiles 2048 tensor-core cycles at best; with both operands of S in
 // shared memory the products alone take about 2750 (8 KB of operands for 64 cycles of products, at 128 bytes a cycle, and
 // the copies write through the same port), and a step takes about 3600 with the softmax behind it.  Measured: causal 32768
-// tokens x 32 heads 7.4 ms (1190 TFLOP/s, 0.70 of the measured burst rate, 0.84 of the sustained one).  Shares of the
+// tokens x 32 heads 6.9 to 7.4 ms (1280 to 1190 TFLOP/s, 0.70 to 0.75 of the measured burst rate, 0.84 to 0.91 of the sustained
+// one; the power limit moves it); 12 packed prompts of up to 4001 tokens 506 us (997 TFLOP/s).  Shares of the
 // exponentials as polynomials on the FMA units were slower at every share (1/2 to 1/16): what the softmax waits for is
 // issue and hand-over, not the exponential unit.
 //

@@ -296,6 +296,42 @@ def test_long_and_many(n, hkv, block, code):
 
 
 @pytest.mark.gpu
+def test_hundreds_of_sequences():
+    p = Pair(300, 3, 1, 64, 16, torch.float16, "int8", 14)
+    rng = np.random.default_rng(4)
+    p.append([int(x) for x in rng.integers(0, 48, 300)])
+    p.check_state()
+    p.attend(2)
+    p.append([1] * 300, single=True)
+    p.attend(2)
+
+
+@pytest.mark.gpu
+def test_two_calls_at_once():
+    p = Pair(3, 30, 2, 128, 32, torch.bfloat16, "e4m3", 15)
+    p.append([900, 64, 333])
+    q = torch.randn((3, 8, 128), generator=p.g).to(torch.bfloat16).cuda()
+    lens = [torch.tensor(x, dtype=torch.int32, device="cuda") for x in (p.lens, [32, 0, 320])]
+    scores = torch.zeros((3, 30), device="cuda")
+    want = [p.cache.attn(q, x, scores=scores, return_lse=True) for x in lens]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[p.cache.attn(q, x, scores=scores, return_lse=True, stream=st) for x, st in zip(lens, streams)] for _ in range(10)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for pair in got for g, w in zip(pair, want) for a, b in zip(g, w))
+
+
+@pytest.mark.gpu
+def test_pages_shared_by_sequences_are_read_by_both():
+    p = Pair(2, 6, 2, 64, 16, torch.float16, "int8", 16)
+    p.append([40, 40])
+    p.o.table[1, :2] = p.o.table[0, :2]  # a common prefix of two blocks
+    p.cache.block_table.copy_(torch.from_numpy(p.o.table))
+    p.attend(4)
+    assert int(p.cache.status) == 0
+
+
+@pytest.mark.gpu
 def test_lengths_out_of_range_and_absent_blocks():
     p = Pair(5, 4, 2, 128, 32, torch.bfloat16, "int8", 4)
     p.append([128, 100, 64, 33, 128])

@@ -253,6 +253,60 @@ def test_strided_inputs_and_output():
 
 
 @pytest.mark.gpu
+def test_many_sequences_and_wide_groups():
+    rng = np.random.default_rng(3)
+    nq = [int(x) for x in rng.integers(0, 20, 150)]
+    nk = [int(x + rng.integers(0, 90)) for x in nq]
+    q, k, v = (x.cuda() for x in _make(nq, nk, 6, 3, 64, torch.float16, 12))
+    out, lse = binding.qevict_prompt_attn(q, k, v, _cu(nq), _cu(nk), max(nq), max(nk), return_lse=True)
+    _check_packed(out, lse, q, k, v, nq, nk, True, torch.float16)
+    for hq, hkv in ((40, 1), (96, 2), (37, 1)):
+        q, k, v = (x.cuda() for x in _make([70, 9], [70, 30], hq, hkv, 64, torch.bfloat16, 13))
+        out, lse = binding.qevict_prompt_attn(q, k, v, _cu([70, 9]), _cu([70, 30]), 70, 70, return_lse=True)
+        _check_packed(out, lse, q, k, v, [70, 9], [70, 30], True, torch.bfloat16)
+
+
+@pytest.mark.gpu
+def test_nothing_to_attend_to_and_nothing_to_do():
+    q, k, v = (x.cuda() for x in _make([5], [0], 2, 1, 64, torch.float16, 1))
+    out, lse = binding.qevict_prompt_attn(q, k, v, _cu([5]), _cu([0]), return_lse=True)
+    assert (out == 0).all() and torch.isneginf(lse).all()
+    out, lse = binding.qevict_prompt_attn(q[:0], k, v, _cu([0]), _cu([0]), return_lse=True)
+    assert out.shape == (0, 2, 64) and lse.shape == (2, 0)
+    assert binding.qevict_prompt_attn(q, k, v, _cu([])[:1], return_lse=False).shape == q.shape  # no sequence
+
+
+@pytest.mark.gpu
+def test_lengths_are_cut_to_the_bounds():
+    nq = [200, 90]
+    q, k, v = (x.cuda() for x in _make(nq, nq, 2, 1, 64, torch.float16, 19))
+    out = torch.full_like(q, 3.0)
+    lse = torch.full((2, 290), 7.0, device="cuda")
+    binding.qevict_prompt_attn(q, k, v, _cu(nq), max_q=150, max_k=140, causal=False, out=out, lse=lse)
+    _check_rows(out[:150], lse[:, :150], q[:150], k[:140], v[:140], False, torch.float16)
+    _check_rows(out[200:], lse[:, 200:], q[200:], k[200:], v[200:], False, torch.float16)
+    assert (out[150:200] == 3).all() and (lse[:, 150:200] == 7).all()
+
+
+@pytest.mark.gpu
+def test_two_calls_at_once():
+    a = [x.cuda() for x in _make([900], [900], 4, 2, 128, torch.bfloat16, 41)]
+    b = [x.cuda() for x in _make([3], [9000], 7, 1, 64, torch.float16, 42)]
+    cu = [_cu([900]), _cu([3]), _cu([9000])]
+    call_a = lambda **kw: binding.qevict_prompt_attn(*a, cu[0], max_q=900, max_k=900, **kw)  # noqa: E731
+    call_b = lambda **kw: binding.qevict_prompt_attn(*b, cu[1], cu[2], max_q=3, max_k=9000, **kw)  # noqa: E731
+    want_a, want_b = call_a(), call_b()
+    torch.cuda.synchronize()
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    got_a, got_b = [], []
+    for _ in range(10):
+        got_a.append(call_a(stream=one))
+        got_b.append(call_b(stream=two))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want_a) for x in got_a) and all(torch.equal(x, want_b) for x in got_b)
+
+
+@pytest.mark.gpu
 def test_captured_and_on_another_stream():
     nq = [200, 65]
     q, k, v = (x.cuda() for x in _make(nq, nq, 4, 2, 128, torch.bfloat16, 17))
