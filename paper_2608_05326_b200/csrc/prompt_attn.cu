@@ -274,9 +274,10 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const uint32_t smb = smem_u32(sm), bars = smb + SM::BAR_OFF;
   // barriers: Q full / empty; ring full / empty; S ready, P ready, O ready of both tiles; value tail zeroed; work items
-  // full / empty (two places); answer to the request for the next one
+  // full / empty (two places); answer to the request for the next one; products done after a failure
   const uint32_t b_q = bars, b_full = bars + 8, b_empty = b_full + 8 * NS, b_s = b_empty + 8 * NS, b_p = b_s + 16, b_o = b_p + 16,
-                 b_clean = b_o + 16, b_qe = b_clean + 8, b_item = b_qe + 8, b_taken = b_item + 16, b_next = b_taken + 16;
+                 b_clean = b_o + 16, b_qe = b_clean + 8, b_item = b_qe + 8, b_taken = b_item + 16, b_next = b_taken + 16,
+                 b_done = b_next + 8;
   // words: 0 .. 3 the answer; 4 tensor memory; 5 loads issued; 6 failed; 8 .. 23 softmax warps that gave up
   volatile uint32_t* words = reinterpret_cast<volatile uint32_t*>(sm + SM::BAR_OFF + SM::WORDS);
   PromptItem* items = reinterpret_cast<PromptItem*>(sm + SM::BAR_OFF + SM::ITEMS);
@@ -302,6 +303,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
     }
     bar_init(b_clean, 1);
     bar_init(b_next, 1);
+    bar_init(b_done, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     for (int i = 5; i < 24; ++i) words[i] = 0;
   }
@@ -523,6 +525,11 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         }
         seen = false;
         if (!ok) break;
+      }
+      if (!ok) {  // the tensor memory is given back below: not under products that are still running
+        if (leader) commit_to(b_done);
+        __syncwarp();
+        warp_wait(b_done, 0);
       }
     }
   } else {
@@ -768,7 +775,8 @@ const char* prompt_check(const qevict_prompt_args* p, qevict_status* st) {
   if (p->causal != 0 && p->causal != 1) return "causal must be 0 or 1";
   if (p->n_seqs < 0 || p->max_q < 0 || p->max_k < 0 || p->total_q < 0 || p->total_k < 0) return "sizes must be >= 0";
   if (p->n_kv_heads < 1 || p->n_q_heads < 1 || p->n_q_heads % p->n_kv_heads) return "n_q_heads must be a multiple of n_kv_heads";
-  if (!(p->softmax_scale >= 0.f) || isinf(p->softmax_scale)) return "softmax_scale must be finite and >= 0";
+  if (!(p->softmax_scale >= 0.f) || isinf(p->softmax_scale) || (p->softmax_scale > 0.f && p->softmax_scale < 1e-30f))
+    return "softmax_scale must be 0 or a finite number of at least 1e-30";
   *st = QEVICT_ERR_UNSUPPORTED;
   if (p->head_dim != 64 && p->head_dim != 128) return "head_dim must be 64 or 128";
   if (p->n_seqs > 65535 || p->n_q_heads > 1024) return "more than 65535 sequences or 1024 heads";

@@ -87,7 +87,7 @@ def test_unusable_caches_are_refused_with_a_reason(over, status, word):
     (lambda: _append(_view(), start=None), 1, "NULL"), (lambda: _append(_view(), ts=100), 1, "16 bytes"), (lambda: _append(_view(), hs=-64), 1, "strides"),
     (lambda: _append(_view(), cu=4097), 1, "aligned"),
     (lambda: _attn(_view(), hq=3), 1, "multiple"), (lambda: _attn(_view(), hq=34), 4, "16 query heads"), (lambda: _attn(_view(), max_len=-1), 1, "max_len"),
-    (lambda: _attn(_view(), scale=float("inf")), 1, "softmax_scale"), (lambda: _attn(_view(), q=None), 1, "NULL"), (lambda: _attn(_view(), scratch=None), 1, "NULL"),
+    (lambda: _attn(_view(), scale=float("inf")), 1, "softmax_scale"), (lambda: _attn(_view(), scale=1e-40), 1, "softmax_scale"), (lambda: _attn(_view(), q=None), 1, "NULL"), (lambda: _attn(_view(), scratch=None), 1, "NULL"),
     (lambda: _attn(_view(), n=16), 3, "scratch"), (lambda: _attn(_view(), si=4096), 1, "score_out"), (lambda: _attn(_view(), q=4100), 1, "aligned"),
     (lambda: _attn(_view(n_seqs=8192, max_blocks=1 << 24), max_len=1 << 29), 4, "too large"),
     (lambda: _evict(struct_size=3), 1, "struct_size"), (lambda: _evict(budget=1), 1, "budget"), (lambda: _evict(max_blocks=20000), 4, "16384"),
@@ -356,6 +356,32 @@ def test_blocks_of_very_different_size_and_logits_that_climb():
     v = (v * torch.cat([10.0 ** torch.linspace(-3, 3, 190), 10.0 ** torch.linspace(3, -3, 190)])[:, None, None]).half()
     p.append([190, 190], kv=[k, v])
     p.attend(4, gain=3.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("code,d", [("int8", 128), ("e4m3", 128), ("int8", 64)])
+def test_outlier_channels(code, d):
+    # four channels 30 times the others: the block's scale follows them.  int8 codes enter the products with an offset of half
+    # their range, so a logit's float32 sum has terms of up to 2 |q_c| amax: its error is bounded by that sum, not by
+    # sum |q_c| |k_c|, and the same holds for the output with the values' largest magnitude.
+    p = Pair(2, 40, 2, d, 32, torch.bfloat16, code, 17)
+    k, v = p.random(1700)
+    for x in (k, v):
+        x[:, :, [3, 17, 40, 63]] *= 30
+    p.append([1200, 500], kv=[k, v])
+    q = torch.randn((2, 8, d), generator=p.g).to(torch.bfloat16)
+    lens = torch.tensor(p.lens, dtype=torch.int32, device="cuda")
+    out, lse, so = (x.double().cpu().numpy() for x in p.cache.attn(q.cuda(), lens, scores=torch.zeros((2, 40), device="cuda"), return_lse=True))
+    res, mass = p.o.attend(q.double().numpy(), p.lens)
+    for s, (ro, rl, spread, _, n, vmax) in enumerate(res):
+        kmax = float(k.double().abs().max())
+        reach = 2 * d ** -0.5 * float(q[s].double().abs().sum(-1).max()) * kmax
+        tol = po.out_tolerance(ro, spread, vmax, n, d, reach, 2.0 ** -8, 2.0 ** -11) + 2 * 32 * 2.0 ** -24 * 2 * vmax
+        assert (np.abs(out[s] - ro) <= tol).all()
+        assert (np.abs(lse[s] - rl) <= po.lse_tolerance(rl, d, reach)).all()
+        assert (np.abs(so[s] - mass[s]) <= 2 * po.logit_error(d, reach) * mass[s] + 1e-30).all()
+        # and far inside that bound, as independent roundings are
+        assert np.abs(lse[s] - rl).max() < 2e-5 and (np.abs(so[s] - mass[s]) <= 1e-4 * mass[s]).all()
 
 
 @pytest.mark.gpu

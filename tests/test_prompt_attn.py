@@ -32,7 +32,7 @@ def _args(**over):
 @pytest.mark.parametrize("over,status,word", [
     (dict(struct_size=8), 1, "struct_size"), (dict(device=-1), 1, "device"), (dict(dtype=7), 1, "dtype"), (dict(layout=2), 1, "layout"),
     (dict(causal=2), 1, "causal"), (dict(n_seqs=-1), 1, "sizes"), (dict(n_q_heads=7), 1, "multiple"), (dict(n_kv_heads=0), 1, "multiple"),
-    (dict(softmax_scale=float("nan")), 1, "softmax_scale"), (dict(softmax_scale=-1.0), 1, "softmax_scale"), (dict(head_dim=96), 4, "head_dim"),
+    (dict(softmax_scale=float("nan")), 1, "softmax_scale"), (dict(softmax_scale=-1.0), 1, "softmax_scale"), (dict(softmax_scale=1e-40), 1, "softmax_scale"), (dict(head_dim=96), 4, "head_dim"),
     (dict(q=None), 1, "NULL"), (dict(k=None), 1, "NULL"), (dict(out=None), 1, "NULL"), (dict(q_bounds=None), 1, "q_bounds"),
     (dict(q=4104), 1, "aligned"), (dict(lse=4098), 1, "aligned"), (dict(k_stride=(0, 60, 128)), 1, "strides"),
     (dict(q_stride=(0, 64, 0)), 1, "strides"), (dict(total_q=2 ** 31), 4, "tokens"),
