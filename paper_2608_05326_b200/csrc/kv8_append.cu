@@ -18,7 +18,7 @@ namespace qevict {
 
 namespace {
 
-constexpr int APPEND_THREADS = 256;
+constexpr int APPEND_THREADS = 128;
 constexpr int APPEND_CTAS = 4096;  // a CTA takes several (head, K or V) pairs where there are more than these
 
 struct Kv8AppendArgs {
@@ -80,7 +80,7 @@ template <> __device__ __forceinline__ uint64_t floats_of<__half>(uint32_t w) {
 
 // NV: 16-byte vectors a thread holds of the block (block * D / 8 / threads).
 template <class T, int CODE, int D, int NV>
-__global__ void __launch_bounds__(APPEND_THREADS, NV <= 4 ? 5 : 3) kv8_append_kernel(const Kv8AppendArgs a) {
+__global__ void __launch_bounds__(APPEND_THREADS, NV <= 4 ? 10 : NV <= 8 ? 5 : 3) kv8_append_kernel(const Kv8AppendArgs a) {
   const Kv8View& c = a.c;
   const int tid = threadIdx.x, nt = blockDim.x;
   const int n_hw = 2 * c.Hkv, chunks = (n_hw + a.per_cta - 1) / a.per_cta;
@@ -156,8 +156,8 @@ __global__ void __launch_bounds__(APPEND_THREADS, NV <= 4 ? 5 : 3) kv8_append_ke
       __syncthreads();
       m = 0;
       if (NV > 1 || nt == APPEND_THREADS) {
-        const uint4 p = *reinterpret_cast<const uint4*>(mine), q = *reinterpret_cast<const uint4*>(mine + 4);
-        m = max(max(max(p.x, p.y), max(p.z, p.w)), max(max(q.x, q.y), max(q.z, q.w)));
+        const uint4 p = *reinterpret_cast<const uint4*>(mine);
+        m = max(max(p.x, p.y), max(p.z, p.w));
       } else {
         for (int i = 0; i < (nt >> 5); ++i) m = max(m, mine[i]);
       }
@@ -220,7 +220,8 @@ template <class T, int CODE, int D> cudaError_t launch_append(const Kv8AppendArg
     case 1: return launch_pdl(kv8_append_kernel<T, CODE, D, 1>, grid, dim3(nt), 0, s, a);
     case 2: return launch_pdl(kv8_append_kernel<T, CODE, D, 2>, grid, dim3(nt), 0, s, a);
     case 4: return launch_pdl(kv8_append_kernel<T, CODE, D, 4>, grid, dim3(nt), 0, s, a);
-    default: return launch_pdl(kv8_append_kernel<T, CODE, D, 8>, grid, dim3(nt), 0, s, a);  // 128 tokens of 128 channels
+    case 8: return launch_pdl(kv8_append_kernel<T, CODE, D, 8>, grid, dim3(nt), 0, s, a);
+    default: return launch_pdl(kv8_append_kernel<T, CODE, D, 16>, grid, dim3(nt), 0, s, a);  // 128 tokens of 128 channels
   }
 }
 template <class T, int CODE> cudaError_t launch_append_d(const Kv8AppendArgs& a, dim3 grid, cudaStream_t s) {
@@ -259,8 +260,9 @@ extern "C" QEVICT_API qevict_status qevict_kv8_append(const qevict_kv8_cache* ca
   const long long blocks = touched < a.c.max_blocks ? touched : a.c.max_blocks;
   if (blocks * 2 * a.c.Hkv > 0x7fffffffll) return stateless_fail(QEVICT_ERR_UNSUPPORTED, "max_new * n_kv_heads is too large for one call");
   // Few blocks: one pair per CTA, for the latency.  Many: several, so that the start of a CTA (lengths, page, first rows: three
-  // dependent reads) is paid less often (39k tokens x 8 heads of 128: 56 us, 0.71 of the floor, with at most 4096 CTAs; 65 us
-  // with twice or half of that; 12 pieces of 2k tokens x 4 heads: 15 us, one pair per CTA 23 us).
+  // dependent reads) is paid less often (39k tokens x 8 heads of 128: 53 us, 0.75 of the floor, with at most 4096 CTAs, 68 us
+  // with half of that, 84 us with one pair per CTA; 12 pieces of up to 2k tokens x 4 heads: 13, 17 and 23 us.  CTAs of 256
+  // threads: 56 and 15 us; of 512: 75 and 23 us).
   a.per_cta = 1;
   while (a.per_cta < 8 && a.per_cta < 2 * a.c.Hkv && blocks * a.c.n_seqs * 2 * a.c.Hkv > (long long)a.per_cta * APPEND_CTAS) a.per_cta *= 2;
   const long long chunks = (2 * a.c.Hkv + a.per_cta - 1) / a.per_cta;
