@@ -18,7 +18,6 @@ namespace qevict {
 
 namespace {
 
-constexpr int APPEND_THREADS = 128;
 constexpr int APPEND_CTAS = 4096;  // a CTA takes several (head, K or V) pairs where there are more than these
 
 struct Kv8AppendArgs {
@@ -78,16 +77,17 @@ template <> __device__ __forceinline__ uint64_t floats_of<__half>(uint32_t w) {
   return pair(f.x, f.y);
 }
 
-// NV: 16-byte vectors a thread holds of the block (block * D / 8 / threads).
-template <class T, int CODE, int D, int NV>
-__global__ void __launch_bounds__(APPEND_THREADS, NV <= 4 ? 10 : NV <= 8 ? 5 : 3) kv8_append_kernel(const Kv8AppendArgs a) {
+// NT threads, NV 16-byte vectors of the block in each: NT * NV = block * D / 8.
+template <class T, int CODE, int D, int NT, int NV>
+__global__ void __launch_bounds__(NT, NV <= 4 ? 10 : 640 / NT) kv8_append_kernel(const Kv8AppendArgs a) {
   const Kv8View& c = a.c;
-  const int tid = threadIdx.x, nt = blockDim.x;
+  constexpr int nt = NT;
+  const int tid = threadIdx.x;
   const int n_hw = 2 * c.Hkv, chunks = (n_hw + a.per_cta - 1) / a.per_cta;
   const int s = blockIdx.y, bx = blockIdx.x / chunks, hw0 = (blockIdx.x - bx * chunks) * a.per_cta, hw1 = min(n_hw, hw0 + a.per_cta);
   constexpr int VR = D / 8;  // vectors per row
   const int B = c.block;
-  __shared__ __align__(16) uint32_t red[2][APPEND_THREADS / 32];
+  __shared__ __align__(16) uint32_t red[2][NT / 32];
   pdl_prologue();
   const int st = a.start[s];
   long long row0 = s;
@@ -155,11 +155,10 @@ __global__ void __launch_bounds__(APPEND_THREADS, NV <= 4 ? 10 : NV <= 8 ? 5 : 3
       if ((tid & 31) == 0) mine[tid >> 5] = m;
       __syncthreads();
       m = 0;
-      if (NV > 1 || nt == APPEND_THREADS) {
-        const uint4 p = *reinterpret_cast<const uint4*>(mine);
-        m = max(max(p.x, p.y), max(p.z, p.w));
-      } else {
-        for (int i = 0; i < (nt >> 5); ++i) m = max(m, mine[i]);
+#pragma unroll
+      for (int i = 0; i < NT / 128; ++i) {
+        const uint4 p = reinterpret_cast<const uint4*>(mine)[i];
+        m = max(m, max(max(p.x, p.y), max(p.z, p.w)));
       }
       const uint16_t mb = (uint16_t)m;
       const float amax = Tr<T>::to_float(*reinterpret_cast<const T*>(&mb));
@@ -214,14 +213,12 @@ __global__ void __launch_bounds__(APPEND_THREADS, NV <= 4 ? 10 : NV <= 8 ? 5 : 3
 }
 
 template <class T, int CODE, int D> cudaError_t launch_append(const Kv8AppendArgs& a, dim3 grid, cudaStream_t s) {
-  const int nvec = a.c.block * D / 8;
-  const int nt = nvec < APPEND_THREADS ? nvec : APPEND_THREADS;
-  switch (nvec / nt) {
-    case 1: return launch_pdl(kv8_append_kernel<T, CODE, D, 1>, grid, dim3(nt), 0, s, a);
-    case 2: return launch_pdl(kv8_append_kernel<T, CODE, D, 2>, grid, dim3(nt), 0, s, a);
-    case 4: return launch_pdl(kv8_append_kernel<T, CODE, D, 4>, grid, dim3(nt), 0, s, a);
-    case 8: return launch_pdl(kv8_append_kernel<T, CODE, D, 8>, grid, dim3(nt), 0, s, a);
-    default: return launch_pdl(kv8_append_kernel<T, CODE, D, 16>, grid, dim3(nt), 0, s, a);  // 128 tokens of 128 channels
+  switch (a.c.block * D / 8) {  // 16 tokens of 64 channels: 128 vectors, 128 of 128: 2048
+    case 128: return launch_pdl(kv8_append_kernel<T, CODE, D, 128, 1>, grid, dim3(128), 0, s, a);
+    case 256: return launch_pdl(kv8_append_kernel<T, CODE, D, 128, 2>, grid, dim3(128), 0, s, a);
+    case 512: return launch_pdl(kv8_append_kernel<T, CODE, D, 128, 4>, grid, dim3(128), 0, s, a);
+    case 1024: return launch_pdl(kv8_append_kernel<T, CODE, D, 128, 8>, grid, dim3(128), 0, s, a);
+    default: return launch_pdl(kv8_append_kernel<T, CODE, D, 256, 8>, grid, dim3(256), 0, s, a);  // (the registers of a thread end at 8)
   }
 }
 template <class T, int CODE> cudaError_t launch_append_d(const Kv8AppendArgs& a, dim3 grid, cudaStream_t s) {
