@@ -8,7 +8,7 @@
 // (sequence, KV head, token).  Every warp of the grid takes one contiguous run of them, equal to within one unit, so
 // ragged lengths balance without a plan on the host: each CTA sums the lengths itself.  A warp's part of a
 // (sequence, KV head) is one partial result; run w's part of row r is slot w + r of the scratch (both only grow along
-// the order, so slots are distinct), and kv8_combine_kernel finds a row's slots from the same arithmetic.
+// the order, so slots are distinct); where a row's slots lie is written down for kv8_merge_kernel.
 //
 // Tile.  Both products put the cache on the A side of mma.m16n8k16 (tokens, then channels on M; the G heads that
 // share the KV head on N).  Codes become fp16 operands in registers, exactly, and the block's scale multiplies the logits /
@@ -18,9 +18,9 @@
 // Probabilities enter the second product as fp16 (2^-11); the sums of the softmax, the block masses and the output
 // are float32.
 //
-// Measured: 16 ragged contexts of up to 32768 tokens, 32 / 8 heads of 128, int8 (472 MB): 105 us, of which this kernel 90 us
+// Measured: 16 ragged contexts of up to 32768 tokens, 32 / 8 heads of 128, int8 (472 MB): 103 us, of which this kernel 90 us
 // (5.2 TB/s; the copies without arithmetic 82 us), merge and masses the rest; 8 contexts of 65536, 28 / 4 heads, e4m3 (538 MB):
-// 109 us; one of 2048 tokens: 11 us, three dependent launches.  At 6.45 TB/s the bytes alone would take 73, 83 and 0.7 us.
+// 109 us; one of 2048 tokens: 10 us, two dependent launches.  At 6.45 TB/s the bytes alone would take 73, 83 and 0.7 us.
 #include <cuda.h>
 
 #include "kv8.cuh"
@@ -49,8 +49,7 @@ struct Kv8AttnArgs {
   float* score_out;
   float* part_o;   // [slot][G][D]
   float2* part_ml; // [slot][G] {reference, sum}
-  float2* stats;   // [seq][Hq] {M, 1 / L}
-  int* pre;        // [n_seqs + 1] units per KV head before each sequence
+  int2* rows;      // [seq][Hkv] first slot and number of the row's partial results
   float2* rec;     // [seq][max_units][Hq] {reference, sum} of every unit, or nullptr
 };
 
@@ -99,8 +98,8 @@ __device__ __forceinline__ int clamp_len(const Kv8AttnArgs& a, int len) {
 
 // The kernels of a call follow one another by programmatic launch.  The attention kernel lets the next one start only when
 // a warp has nothing left to read: its own CTAs fill the SMs, and CTAs of the next kernel that slipped in between cost a
-// second wave (16 ragged contexts: 104 us, 117 with the release at the start).  The last kernel of a call releases nothing
-// early for the same reason.
+// second wave (16 ragged contexts: 104 us, 117 with the release at the start).  The merge releases nothing early for the same
+// reason.
 __device__ __forceinline__ void wait_prior() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
 __device__ __forceinline__ void release_next() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
 
@@ -174,11 +173,19 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
   __shared__ int s_w[WARPS];
   wait_prior();
   unit_prefix(a, UT, pre, s_w);
-  if (blockIdx.x == 0)  // for the kernels behind this one
-    for (int i = tid; i <= c.n_seqs; i += ATTN_THREADS) a.pre[i] = pre[i];
   const long long total = (long long)pre[c.n_seqs] * c.Hkv;
-  if (total == 0) return;
   const int w = blockIdx.x * WARPS + wid, n_runs = runs_of(total, a.n_warps);
+  // where the rows' partial results will lie, for the merge: a few rows for each thread of the grid
+  for (int r = blockIdx.x * ATTN_THREADS + tid; r < c.n_seqs * c.Hkv; r += gridDim.x * ATTN_THREADS) {
+    const int s = r / c.Hkv, h = r - s * c.Hkv, nu = pre[s + 1] - pre[s];
+    int2 v = make_int2(0, 0);
+    if (nu > 0) {
+      const long long u0 = (long long)pre[s] * c.Hkv + (long long)h * nu;
+      const int w0 = run_of(total, n_runs, u0);
+      v = make_int2(w0 + r, run_of(total, n_runs, u0 + nu - 1) - w0 + 1);
+    }
+    a.rows[r] = v;
+  }
   if (w >= n_runs) return;
   long long u = run_start(total, n_runs, w);
   const long long u_end = run_start(total, n_runs, w + 1);
@@ -575,47 +582,36 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
   }
 }
 
-// Merges a row's partial results: one CTA per (query head, sequence).  A warp takes partials wid, wid + 8, ... with a running
-// maximum of its own, so that everything it needs is requested at once; the eight warps' results meet in shared memory.
-constexpr int COMB_THREADS = 256;
-template <class T>
-__global__ void __launch_bounds__(COMB_THREADS) kv8_combine_kernel(const Kv8AttnArgs a) {
-  constexpr int NW = COMB_THREADS / 32;
-  __shared__ float s_m[NW], s_l[NW], s_o[NW][128];
-  const int s = blockIdx.y, hq = blockIdx.x, h = hq / a.G, hl = hq - h * a.G, D = a.c.D;
-  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  wait_prior();
-  const int p0 = a.pre[s], p1 = a.pre[s + 1];
-  const long long total = (long long)a.pre[a.c.n_seqs] * a.c.Hkv;
-  release_next();
-  const int nu = p1 - p0;
-  T* out = static_cast<T*>(a.out) + ((size_t)s * a.Hq + hq) * D;
+// Merges the partial results and adds up the block masses, side by side in one launch: a CTA has a (query head, sequence) or
+// MASS_BLOCKS blocks of a sequence.  The masses need every head's maximum and denominator; their CTAs work those out for
+// themselves from the {reference, sum} pairs, eight threads to a head.
+// (As a kernel of their own behind the merge the masses cost 0.4 to 3 us more and a launch; as a second task of the merge's CTAs,
+// each of which then goes through both tasks' code and statistics, 2 to 4 us more.)
+constexpr int MERGE_THREADS = 256, MERGE_WARPS = MERGE_THREADS / 32, MASS_BLOCKS = 32;
+
+// One (query head, sequence).  A warp takes partials wid, wid + 8, ... with a running maximum of its own, so that everything
+// it needs is requested at once; the eight warps' results meet in shared memory.
+template <class T> __device__ void merge_head(const Kv8AttnArgs& a, int s, int hq) {
+  __shared__ float s_m[MERGE_WARPS], s_l[MERGE_WARPS], s_o[MERGE_WARPS][128];
+  const int h = hq / a.G, hl = hq - h * a.G, D = a.c.D, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int2 where = a.rows[s * a.c.Hkv + h];
+  const int n = where.y;
   if (tid == 0 && a.c.status && hq == 0 && a.lens[s] > a.max_len) kv8_record(a.c.status, CHECK_LENGTH);
-  if (nu == 0) {
-    for (int i = tid; i < D; i += COMB_THREADS) out[i] = Tr<T>::from_float(0.f);
-    if (tid == 0) {
-      if (a.lse) a.lse[(size_t)s * a.Hq + hq] = -INFINITY;
-      a.stats[(size_t)s * a.Hq + hq] = make_float2(0.f, 0.f);
-    }
-    return;
-  }
-  const long long u0 = (long long)p0 * a.c.Hkv + (long long)h * nu;
-  const int n_runs = runs_of(total, a.n_warps);
-  const int w0 = run_of(total, n_runs, u0), n = run_of(total, n_runs, u0 + nu - 1) - w0 + 1;
-  const size_t slot0 = (size_t)w0 + (size_t)s * a.c.Hkv + h;
+  const float2* ml0 = a.part_ml + (size_t)where.x * a.G + hl;
+  const float* o0 = a.part_o + ((size_t)where.x * a.G + hl) * D;
   // lanes hold 4 channels each (d = 64: half the lanes, twice as many partials at a time)
   const int per = D / 4, sub = lane / per, subs = 32 / per, c4 = lane - sub * per;
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   constexpr int AT_ONCE = 8;
-  for (int i0 = wid * subs + sub; i0 < n; i0 += AT_ONCE * NW * subs) {
+  for (int i0 = wid * subs + sub; i0 < n; i0 += AT_ONCE * MERGE_WARPS * subs) {
     float2 ml[AT_ONCE];
     float4 v[AT_ONCE];
 #pragma unroll
     for (int k = 0; k < AT_ONCE; ++k) {
-      const int i = i0 + k * NW * subs;
-      ml[k] = i < n ? a.part_ml[(slot0 + i) * a.G + hl] : make_float2(-INFINITY, 0.f);
-      v[k] = i < n ? *reinterpret_cast<const float4*>(a.part_o + ((slot0 + i) * a.G + hl) * D + c4 * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+      const int i = i0 + k * MERGE_WARPS * subs;
+      ml[k] = i < n ? ml0[(size_t)i * a.G] : make_float2(-INFINITY, 0.f);
+      v[k] = i < n ? *reinterpret_cast<const float4*>(o0 + (size_t)i * a.G * D + c4 * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
     float top = m;
 #pragma unroll
@@ -652,53 +648,86 @@ __global__ void __launch_bounds__(COMB_THREADS) kv8_combine_kernel(const Kv8Attn
   if (tid < D) {
     float M = s_m[0];
 #pragma unroll
-    for (int i = 1; i < NW; ++i) M = fmaxf(M, s_m[i]);
+    for (int i = 1; i < MERGE_WARPS; ++i) M = fmaxf(M, s_m[i]);
     const float Ms = M == -INFINITY ? 0.f : M;
     float L = 0.f, v = 0.f;
 #pragma unroll
-    for (int i = 0; i < NW; ++i) {
+    for (int i = 0; i < MERGE_WARPS; ++i) {
       const float f = ex2(s_m[i] - Ms);
       L += s_l[i] * f;
       v += s_o[i][tid] * f;
     }
-    out[tid] = Tr<T>::from_float(L > 0.f ? v / L : (L == 0.f ? 0.f : v));
-    if (tid == 0) {
-      if (a.lse) a.lse[(size_t)s * a.Hq + hq] = L == 0.f ? -INFINITY : (Ms + log2f(L)) * 0.6931471805599453f;
-      a.stats[(size_t)s * a.Hq + hq] = make_float2(Ms, L == 0.f ? 0.f : 1.f / L);
-    }
+    static_cast<T*>(a.out)[((size_t)s * a.Hq + hq) * D + tid] = Tr<T>::from_float(L > 0.f ? v / L : (L == 0.f ? 0.f : v));
+    if (tid == 0 && a.lse) a.lse[(size_t)s * a.Hq + hq] = L == 0.f ? -INFINITY : (Ms + log2f(L)) * 0.6931471805599453f;
   }
 }
 
-// Block masses: one warp per (block, sequence), a lane per head, every load requested at once, fixed shuffle tree.  (As a part
-// of the merge, whose CTAs then work out all heads' statistics for themselves, the two took 2 to 4 us longer than apart.)
-constexpr int MASS_THREADS = 256;
-__global__ void __launch_bounds__(MASS_THREADS) kv8_mass_kernel(const Kv8AttnArgs a, int ut) {
-  const int s = blockIdx.y, lane = threadIdx.x & 31, b = blockIdx.x * (MASS_THREADS / 32) + (threadIdx.x >> 5);
-  wait_prior();
-  if (b >= a.c.max_blocks) return;
-  const int nu = a.pre[s + 1] - a.pre[s], upb = a.c.block / ut;
-  const size_t at = (size_t)s * a.c.max_blocks + b;
-  const float before = a.score_in ? a.score_in[at] : 0.f;
-  float mass = 0.f;
-  for (int h = lane; h < a.Hq; h += 32) {
-    const float2 st = a.stats[(size_t)s * a.Hq + h];
-    const float2* rec = a.rec + ((size_t)s * a.max_units + (size_t)b * upb) * a.Hq + h;
-    float2 r[8];
+// Blocks b0 .. b0 + MASS_BLOCKS - 1 of a sequence.  One warp per block, a lane per head, fixed shuffle trees.
+__device__ void block_masses(const Kv8AttnArgs& a, int s, int b0, int ut, float2* s_stat) {
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int nu = (clamp_len(a, a.lens[s]) + ut - 1) / ut, upb = a.c.block / ut;
+  if (b0 * upb < nu) {
+#pragma unroll 1
+    for (int h0 = 0; h0 < a.Hq; h0 += MERGE_THREADS / 8) {
+      const int hq = h0 + (tid >> 3), part = tid & 7;
+      float m = -INFINITY, l = 0.f;
+      if (hq < a.Hq) {
+        const int h = hq / a.G;
+        const int2 where = a.rows[s * a.c.Hkv + h];
+        const float2* ml = a.part_ml + (size_t)where.x * a.G + hq - h * a.G;
+        for (int i0 = part; i0 < where.y; i0 += 32) {
+          float2 v[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)  // a block has at most 8 units (16 tokens: one, 128: four)
-      r[i] = i < upb && b * upb + i < a.max_units ? rec[(size_t)i * a.Hq] : make_float2(-INFINITY, 0.f);
+          for (int k = 0; k < 4; ++k) v[k] = i0 + 8 * k < where.y ? ml[(size_t)(i0 + 8 * k) * a.G] : make_float2(-INFINITY, 0.f);
+          const float top = fmaxf(fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)), m), ref = top == -INFINITY ? 0.f : top;
+          l *= ex2(m - ref);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (b * upb + i < nu) mass += r[i].y * ex2(r[i].x - st.x) * st.y;  // what lies behind the length was never written
+          for (int k = 0; k < 4; ++k) l += v[k].y * ex2(v[k].x - ref);
+          m = top;
+        }
+      }
+      float M = m;
+#pragma unroll
+      for (int o = 4; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+      const float Ms = M == -INFINITY ? 0.f : M;
+      l *= ex2(m - Ms);
+#pragma unroll
+      for (int o = 4; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+      if (hq < a.Hq && part == 0) s_stat[hq] = make_float2(Ms, l == 0.f ? 0.f : 1.f / l);
+    }
   }
+  __syncthreads();
+#pragma unroll 1
+  for (int b = b0 + wid; b < min(b0 + MASS_BLOCKS, a.c.max_blocks); b += MERGE_WARPS) {
+    const size_t at = (size_t)s * a.c.max_blocks + b;
+    const float before = a.score_in ? a.score_in[at] : 0.f;
+    const int have = min(upb, nu - b * upb);  // units of this block that were read
+    float mass = 0.f;
+    for (int h = lane; h < a.Hq && have > 0; h += 32) {
+      const float2* rec = a.rec + ((size_t)s * a.max_units + (size_t)b * upb) * a.Hq + h;
+      float2 r[4];  // a block has at most four units
 #pragma unroll
-  for (int o = 16; o; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
-  if (lane == 0) a.score_out[at] = before + mass;
+      for (int i = 0; i < 4; ++i) r[i] = i < have ? rec[(size_t)i * a.Hq] : make_float2(-INFINITY, 0.f);
+      const float2 st = s_stat[h];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mass += r[i].y * ex2(r[i].x - st.x) * st.y;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
+    if (lane == 0) a.score_out[at] = before + mass;
+  }
+}
+
+template <class T> __global__ void __launch_bounds__(MERGE_THREADS) kv8_merge_kernel(const Kv8AttnArgs a, int ut) {
+  extern __shared__ float2 s_stat[];  // [Hq] {maximum, 1 / denominator}
+  wait_prior();
+  if ((int)blockIdx.x < a.Hq) merge_head<T>(a, blockIdx.y, blockIdx.x);
+  else block_masses(a, blockIdx.y, ((int)blockIdx.x - a.Hq) * MASS_BLOCKS, ut, s_stat);
 }
 
 struct Plan {
   int ut, n_warps, max_units, max_len;
-  size_t off_ml, off_rec, off_stats, off_pre, bytes;
+  size_t off_ml, off_rec, off_rows, bytes;
 };
 
 int sm_count(int device) {
@@ -731,9 +760,8 @@ const char* plan_of(const Kv8View& c, int Hq, int max_len, bool scores, int sms,
   const size_t slots = (size_t)p->n_warps + (size_t)c.n_seqs * c.Hkv;
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   p->off_ml = up(slots * G * c.D * sizeof(float));
-  p->off_stats = p->off_ml + up(slots * G * sizeof(float2));
-  p->off_pre = p->off_stats + up((size_t)c.n_seqs * Hq * sizeof(float2));
-  p->off_rec = p->off_pre + up(((size_t)c.n_seqs + 1) * sizeof(int));
+  p->off_rows = p->off_ml + up(slots * G * sizeof(float2));
+  p->off_rec = p->off_rows + up((size_t)c.n_seqs * c.Hkv * sizeof(int2));
   p->bytes = p->off_rec + (scores ? up((size_t)c.n_seqs * p->max_units * Hq * sizeof(float2)) : 0);
   return nullptr;
 }
@@ -764,14 +792,12 @@ template <class T> cudaError_t launch_all(const Kv8AttnArgs& a, int code, int ut
   static std::atomic<uint64_t> done{0};
   if (e == cudaSuccess)
     e = once_per_device(done, device, [] {
-      const cudaError_t x = cudaFuncSetAttribute(kv8_combine_kernel<T>, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
-      return x != cudaSuccess ? x : cudaFuncSetAttribute(kv8_mass_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
+      const cudaError_t x = cudaFuncSetAttribute(kv8_merge_kernel<T>, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
+      return x != cudaSuccess ? x : cudaFuncSetAttribute(kv8_merge_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 16384 * (int)sizeof(float2));
     });
-  if (e == cudaSuccess) e = launch_pdl(kv8_combine_kernel<T>, dim3(a.Hq, a.c.n_seqs), dim3(COMB_THREADS), 0, s, a);
-  if (e == cudaSuccess && a.score_out) {
-    const int per = MASS_THREADS / 32;
-    e = launch_pdl(kv8_mass_kernel, dim3((a.c.max_blocks + per - 1) / per, a.c.n_seqs), dim3(MASS_THREADS), 0, s, a, ut);
-  }
+  const int mass_ctas = a.score_out ? (a.c.max_blocks + MASS_BLOCKS - 1) / MASS_BLOCKS : 0;
+  if (e == cudaSuccess)
+    e = launch_pdl(kv8_merge_kernel<T>, dim3(a.Hq + mass_ctas, a.c.n_seqs), dim3(MERGE_THREADS), a.score_out ? (size_t)a.Hq * sizeof(float2) : 0, s, a, ut);
   return e;
 }
 
@@ -821,8 +847,7 @@ QEVICT_API qevict_status qevict_kv8_attn(const qevict_kv8_cache* cache, int32_t 
   char* base = static_cast<char*>(scratch);
   a.part_o = reinterpret_cast<float*>(base);
   a.part_ml = reinterpret_cast<float2*>(base + p.off_ml);
-  a.stats = reinterpret_cast<float2*>(base + p.off_stats);
-  a.pre = reinterpret_cast<int*>(base + p.off_pre);
+  a.rows = reinterpret_cast<int2*>(base + p.off_rows);
   a.rec = score_out ? reinterpret_cast<float2*>(base + p.off_rec) : nullptr;
   DeviceGuard guard(cache->device);
   cudaError_t e = guard.err;
