@@ -687,9 +687,11 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
   if (wid == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
-// Joins the partial results of a split call: one warp per (row, head).
-template <class T>
+// Joins the partial results of a split call: one warp per (row, head), a lane per part for the weights (at most 64 parts), then
+// per 2 or 4 channels.
+template <class T, int D>
 __global__ void __launch_bounds__(256) prompt_merge_kernel(const PromptArgs a) {
+  constexpr int PER = D / 32;
   const int lane = threadIdx.x & 31, s = blockIdx.y;
   pdl_prologue();
   int q0, nq;
@@ -698,20 +700,38 @@ __global__ void __launch_bounds__(256) prompt_merge_kernel(const PromptArgs a) {
   const int row = (int)(at / a.Hq), hq = (int)(at - (long long)row * a.Hq);
   if (row >= nq) return;
   const long long prow = a.padded ? (long long)s * a.max_q + row : (long long)q0 + row;
-  float M = -INFINITY;
-  for (int i = 0; i < a.splits; ++i) M = fmaxf(M, a.part_lse[((long long)i * a.rows + prow) * a.Hq + hq]);
+  const long long first = prow * a.Hq + hq, next = a.rows * a.Hq;  // of part 0; from part to part
+  float w0 = lane < a.splits ? a.part_lse[first + lane * next] : -INFINITY;
+  float w1 = lane + 32 < a.splits ? a.part_lse[first + (lane + 32) * next] : -INFINITY;
+  float M = fmaxf(w0, w1);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
   const float Ms = M == -INFINITY ? 0.f : M;
-  float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  const int per = a.D / 32;  // channels of a lane: 2 or 4
+  w0 = ex2p(w0 - Ms);
+  w1 = ex2p(w1 - Ms);
+  float L = w0 + w1;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+  float sum[PER] = {};
+#pragma unroll 4
   for (int i = 0; i < a.splits; ++i) {
-    const long long p = ((long long)i * a.rows + prow) * a.Hq + hq;
-    const float f = ex2p(a.part_lse[p] - Ms);
-    L += f;
-    const float* src = a.part_o + p * a.D + lane * per;
-    for (int k = 0; k < per; ++k) o[k] += f * src[k];
+    const float f = __shfl_sync(0xffffffffu, i < 32 ? w0 : w1, i & 31);
+    const float* src = a.part_o + (first + i * next) * D + lane * PER;
+    float v[PER];
+    if (PER == 4) {
+      const float4 x = *reinterpret_cast<const float4*>(src);
+      v[0] = x.x; v[1] = x.y; v[2 % PER] = x.z; v[3 % PER] = x.w;
+    } else {
+      const float2 x = *reinterpret_cast<const float2*>(src);
+      v[0] = x.x; v[1] = x.y;
+    }
+#pragma unroll
+    for (int k = 0; k < PER; ++k) sum[k] += f * v[k];
   }
-  T* out = static_cast<T*>(a.out) + (a.padded ? s * a.out_stride[0] + row * a.out_stride[2] : prow * a.out_stride[2]) + hq * a.out_stride[1];
-  for (int k = 0; k < per; ++k) out[lane * per + k] = Tr<T>::from_float(L == 0.f ? 0.f : o[k] / L);
+  T* out = static_cast<T*>(a.out) + (a.padded ? s * a.out_stride[0] + row * a.out_stride[2] : prow * a.out_stride[2]) + hq * a.out_stride[1] + lane * PER;
+#pragma unroll
+  for (int k = 0; k < PER; k += 2)
+    *reinterpret_cast<uint32_t*>(out + k) = L == 0.f ? 0u : pack2<T>(sum[k] / L, sum[k + 1] / L);
   if (lane == 0 && a.lse)
     a.lse[a.padded ? ((long long)s * a.Hq + hq) * a.max_q + row : hq * a.total_q + prow] =
         L == 0.f ? -INFINITY : (Ms + log2f(L)) * 0.6931471805599453f;
@@ -829,7 +849,7 @@ long long prompt_rows(const qevict_prompt_args* p) {
 // An item costs its key tiles and some three more; items go to the SMs as these fall free, so the call takes the work of all
 // items over the SMs and about half an item for the uneven end, at least one item; and every part of the keys writes and reads
 // its rows' results in float32 once more.  (28 heads, a piece of 500 tokens behind 16000 next to one of 166 behind 3714: 237,
-// 174, 190, 157 us with one, two, three, five items for each tile; the model takes five.)
+// 174, 190, 157 us with one, two, three, five items for each tile; the model takes five, 151 us with the present merge.)
 int prompt_splits(const qevict_prompt_args* p) {
   int P, T;
   prompt_tile(p, &P, &T);
@@ -866,7 +886,7 @@ cudaError_t launch_prompt(const PromptArgs& a, const CUtensorMap& mq, const CUte
     e = launch_pdl(kernel, dim3((unsigned)(tiles * (a.Hq / a.P) * a.splits)), dim3(PROMPT_THREADS), PromptSmem<D>::BYTES, s, a, mq, mk, mv);
   if (e == cudaSuccess && a.splits > 1) {
     const unsigned ctas = (unsigned)(((long long)a.max_q * a.Hq + 7) / 8);
-    e = launch_pdl(prompt_merge_kernel<T>, dim3(ctas, a.n_seqs), dim3(256), 0, s, a);
+    e = launch_pdl(prompt_merge_kernel<T, D>, dim3(ctas, a.n_seqs), dim3(256), 0, s, a);
   }
   return e;
 }
