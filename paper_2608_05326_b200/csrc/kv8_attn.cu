@@ -43,6 +43,7 @@ struct Kv8AttnArgs {
   int max_len;     // already cut to max_blocks * block
   int n_warps;     // warps of the attention grid
   int max_units;   // units of a sequence of max_len tokens
+  int least_run;   // units of a run, where there are runs enough
   void* out;
   float* lse;
   const float* score_in;
@@ -132,8 +133,11 @@ __device__ void unit_prefix(const Kv8AttnArgs& a, int ut, int* pre, int* s_w) {
 }
 
 // First unit of run w of n over `total` units; the run that holds unit u.  There are never more runs than units, so
-// that no run is empty and every slot between a row's first and last is written.
-__device__ __forceinline__ int runs_of(long long total, int n_warps) { return (int)min((long long)n_warps, total); }
+// that no run is empty and every slot between a row's first and last is written; and where warps are plenty a run has
+// least_run units, since every run's partial result has to be merged.
+__device__ __forceinline__ int runs_of(long long total, int n_warps, int least_run) {
+  return (int)min((long long)n_warps, (total + least_run - 1) / least_run);
+}
 __device__ __forceinline__ long long run_start(long long total, int n, int w) { return total * w / n; }
 __device__ __forceinline__ int run_of(long long total, int n, long long u) { return (int)(((u + 1) * n - 1) / total); }
 
@@ -174,7 +178,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
   wait_prior();
   unit_prefix(a, UT, pre, s_w);
   const long long total = (long long)pre[c.n_seqs] * c.Hkv;
-  const int w = blockIdx.x * WARPS + wid, n_runs = runs_of(total, a.n_warps);
+  const int w = blockIdx.x * WARPS + wid, n_runs = runs_of(total, a.n_warps, a.least_run);
   // where the rows' partial results will lie, for the merge: a few rows for each thread of the grid
   for (int r = blockIdx.x * ATTN_THREADS + tid; r < c.n_seqs * c.Hkv; r += gridDim.x * ATTN_THREADS) {
     const int s = r / c.Hkv, h = r - s * c.Hkv, nu = pre[s + 1] - pre[s];
@@ -726,7 +730,7 @@ template <class T> __global__ void __launch_bounds__(MERGE_THREADS) kv8_merge_ke
 }
 
 struct Plan {
-  int ut, n_warps, max_units, max_len;
+  int ut, n_warps, max_units, max_len, least_run;
   size_t off_ml, off_rec, off_rows, bytes;
 };
 
@@ -752,7 +756,13 @@ const char* plan_of(const Kv8View& c, int Hq, int max_len, bool scores, int sms,
   if ((long long)c.n_seqs * p->max_units > 0x7fffffffll) return "n_seqs * max_len is too large for one call";
   const int G = Hq / c.Hkv;
   const int ctas_per_sm = G <= 8 ? 3 : 2;
-  const long long units = (long long)c.n_seqs * c.Hkv * p->max_units;
+  // A unit costs a warp about 1.3 us, and the merge about 1 us for every 64 partial results of a row: r units a run take
+  // 1.3 r + units / (64 r) us on one long row, least at sqrt(units / 80) (one sequence of 29660 tokens with one KV head for 16
+  // heads: 29 us, 34 with a unit a run; one of 60000 with two KV heads for four: 18 and 22; a sequence with eight KV heads
+  // loses 1 to 2 %).
+  p->least_run = (int)(sqrt(p->max_units / 80.0) + 0.5);
+  if (p->least_run < 1) p->least_run = 1;
+  const long long units = ((long long)c.n_seqs * c.Hkv * p->max_units + p->least_run - 1) / p->least_run;
   long long ctas = (units + WARPS - 1) / WARPS;
   if (ctas > (long long)sms * ctas_per_sm) ctas = (long long)sms * ctas_per_sm;
   if (ctas < 1) ctas = 1;
@@ -842,7 +852,7 @@ QEVICT_API qevict_status qevict_kv8_attn(const qevict_kv8_cache* cache, int32_t 
   if (scratch_bytes < p.bytes) return stateless_fail(QEVICT_ERR_NO_MEMORY, "scratch too small: see qevict_kv8_attn_scratch_bytes");
   a.Hq = n_q_heads; a.G = n_q_heads / a.c.Hkv;
   a.scale_log2 = (float)((softmax_scale > 0.f ? (double)softmax_scale : 1.0 / sqrt((double)a.c.D)) * 1.4426950408889634);
-  a.q = q; a.lens = lens; a.max_len = p.max_len; a.n_warps = p.n_warps; a.max_units = p.max_units;
+  a.q = q; a.lens = lens; a.max_len = p.max_len; a.n_warps = p.n_warps; a.max_units = p.max_units; a.least_run = p.least_run;
   a.out = out; a.lse = lse; a.score_in = score_in; a.score_out = score_out;
   char* base = static_cast<char*>(scratch);
   a.part_o = reinterpret_cast<float*>(base);
