@@ -587,11 +587,11 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
 }
 
 // Merges the partial results and adds up the block masses, side by side in one launch: a CTA has a (query head, sequence) or
-// MASS_BLOCKS blocks of a sequence.  The masses need every head's maximum and denominator; their CTAs work those out for
-// themselves from the {reference, sum} pairs, eight threads to a head.
+// some blocks of a sequence.  The masses need every head's maximum and denominator; their CTAs work those out for themselves
+// from the {reference, sum} pairs, 8 to 32 threads to a head.
 // (As a kernel of their own behind the merge the masses cost 0.4 to 3 us more and a launch; as a second task of the merge's CTAs,
 // each of which then goes through both tasks' code and statistics, 2 to 4 us more.)
-constexpr int MERGE_THREADS = 256, MERGE_WARPS = MERGE_THREADS / 32, MASS_BLOCKS = 32;
+constexpr int MERGE_THREADS = 256, MERGE_WARPS = MERGE_THREADS / 32;
 
 // One (query head, sequence).  A warp takes partials wid, wid + 8, ... with a running maximum of its own, so that everything
 // it needs is requested at once; the eight warps' results meet in shared memory.
@@ -666,43 +666,45 @@ template <class T> __device__ void merge_head(const Kv8AttnArgs& a, int s, int h
   }
 }
 
-// Blocks b0 .. b0 + MASS_BLOCKS - 1 of a sequence.  One warp per block, a lane per head, fixed shuffle trees.
-__device__ void block_masses(const Kv8AttnArgs& a, int s, int b0, int ut, float2* s_stat) {
+// Blocks b0 .. b1 - 1 of a sequence.  One warp per block, a lane per head, fixed shuffle trees.
+__device__ void block_masses(const Kv8AttnArgs& a, int s, int b0, int b1, int ut, float2* s_stat) {
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int nu = (clamp_len(a, a.lens[s]) + ut - 1) / ut, upb = a.c.block / ut;
   if (b0 * upb < nu) {
+    const int per_log2 = a.Hq <= 8 ? 5 : a.Hq <= 16 ? 4 : 3, per = 1 << per_log2;  // threads to a head
 #pragma unroll 1
-    for (int h0 = 0; h0 < a.Hq; h0 += MERGE_THREADS / 8) {
-      const int hq = h0 + (tid >> 3), part = tid & 7;
+    for (int h0 = 0; h0 < a.Hq; h0 += MERGE_THREADS >> per_log2) {
+      const int hq = h0 + (tid >> per_log2), part = tid & (per - 1);
       float m = -INFINITY, l = 0.f;
       if (hq < a.Hq) {
         const int h = hq / a.G;
         const int2 where = a.rows[s * a.c.Hkv + h];
         const float2* ml = a.part_ml + (size_t)where.x * a.G + hq - h * a.G;
-        for (int i0 = part; i0 < where.y; i0 += 32) {
-          float2 v[4];
+        for (int i0 = part; i0 < where.y; i0 += 8 * per) {
+          float2 v[8];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] = i0 + 8 * k < where.y ? ml[(size_t)(i0 + 8 * k) * a.G] : make_float2(-INFINITY, 0.f);
-          const float top = fmaxf(fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)), m), ref = top == -INFINITY ? 0.f : top;
+          for (int k = 0; k < 8; ++k) v[k] = i0 + k * per < where.y ? ml[(size_t)(i0 + k * per) * a.G] : make_float2(-INFINITY, 0.f);
+          float top = m;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) top = fmaxf(top, v[k].x);
+          const float ref = top == -INFINITY ? 0.f : top;
           l *= ex2(m - ref);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) l += v[k].y * ex2(v[k].x - ref);
+          for (int k = 0; k < 8; ++k) l += v[k].y * ex2(v[k].x - ref);
           m = top;
         }
       }
       float M = m;
-#pragma unroll
-      for (int o = 4; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+      for (int o = per >> 1; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
       const float Ms = M == -INFINITY ? 0.f : M;
       l *= ex2(m - Ms);
-#pragma unroll
-      for (int o = 4; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+      for (int o = per >> 1; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
       if (hq < a.Hq && part == 0) s_stat[hq] = make_float2(Ms, l == 0.f ? 0.f : 1.f / l);
     }
   }
   __syncthreads();
 #pragma unroll 1
-  for (int b = b0 + wid; b < min(b0 + MASS_BLOCKS, a.c.max_blocks); b += MERGE_WARPS) {
+  for (int b = b0 + wid; b < b1; b += MERGE_WARPS) {
     const size_t at = (size_t)s * a.c.max_blocks + b;
     const float before = a.score_in ? a.score_in[at] : 0.f;
     const int have = min(upb, nu - b * upb);  // units of this block that were read
@@ -722,11 +724,12 @@ __device__ void block_masses(const Kv8AttnArgs& a, int s, int b0, int ut, float2
   }
 }
 
-template <class T> __global__ void __launch_bounds__(MERGE_THREADS) kv8_merge_kernel(const Kv8AttnArgs a, int ut) {
+template <class T> __global__ void __launch_bounds__(MERGE_THREADS) kv8_merge_kernel(const Kv8AttnArgs a, int ut, int mass_blocks) {
   extern __shared__ float2 s_stat[];  // [Hq] {maximum, 1 / denominator}
   wait_prior();
-  if ((int)blockIdx.x < a.Hq) merge_head<T>(a, blockIdx.y, blockIdx.x);
-  else block_masses(a, blockIdx.y, ((int)blockIdx.x - a.Hq) * MASS_BLOCKS, ut, s_stat);
+  const int b0 = ((int)blockIdx.x - a.Hq) * mass_blocks;
+  if (b0 < 0) merge_head<T>(a, blockIdx.y, blockIdx.x);
+  else block_masses(a, blockIdx.y, b0, min(b0 + mass_blocks, a.c.max_blocks), ut, s_stat);
 }
 
 struct Plan {
@@ -805,9 +808,13 @@ template <class T> cudaError_t launch_all(const Kv8AttnArgs& a, int code, int ut
       const cudaError_t x = cudaFuncSetAttribute(kv8_merge_kernel<T>, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
       return x != cudaSuccess ? x : cudaFuncSetAttribute(kv8_merge_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 16384 * (int)sizeof(float2));
     });
-  const int mass_ctas = a.score_out ? (a.c.max_blocks + MASS_BLOCKS - 1) / MASS_BLOCKS : 0;
+  // Blocks of a mass CTA: one to four for each of its warps, so that they about fill the SMs (one context of 2048 tokens 10.8 us
+  // with four, 9.0 with one; two of 8000 tokens 14.7 and 12.3, with the statistics' threads by the number of heads).
+  int mass_blocks = MERGE_WARPS;
+  while (mass_blocks < 4 * MERGE_WARPS && (long long)a.c.max_blocks * a.c.n_seqs > 148ll * mass_blocks) mass_blocks += MERGE_WARPS;
+  const int mass_ctas = a.score_out ? (a.c.max_blocks + mass_blocks - 1) / mass_blocks : 0;
   if (e == cudaSuccess)
-    e = launch_pdl(kv8_merge_kernel<T>, dim3(a.Hq + mass_ctas, a.c.n_seqs), dim3(MERGE_THREADS), a.score_out ? (size_t)a.Hq * sizeof(float2) : 0, s, a, ut);
+    e = launch_pdl(kv8_merge_kernel<T>, dim3(a.Hq + mass_ctas, a.c.n_seqs), dim3(MERGE_THREADS), a.score_out ? (size_t)a.Hq * sizeof(float2) : 0, s, a, ut, mass_blocks);
   return e;
 }
 
