@@ -432,6 +432,8 @@ QEVICT_API qevict_status qevict_prompt_attn(const qevict_prompt_args* args, void
  *   - Lengths are device int32 [n_seqs]; a length < 1 is an empty sequence (out = 0, lse = -infinity, no mass), one
  *     beyond max_blocks * block or the call's max_len is cut to the whole blocks within the smaller of them, and
  *     *status is set.
+ *   - Logits (times log2 e) and the sums of value times weight before the division by the weights' sum are float32, a
+ *     weight being at most 2^8: values up to 2^119 divided by the number of tokens cannot overflow them.
  * The three calls need no handle; errors leave their text in qevict_last_error(NULL) of the calling thread.  They
  * allocate nothing, do not synchronise and read the lengths and tables on the device, so they can be captured. */
 enum { QEVICT_CODE_INT8 = 0, QEVICT_CODE_E4M3 = 1 };

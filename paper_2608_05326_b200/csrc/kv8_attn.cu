@@ -411,7 +411,17 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              const float f = qs[nt][j] * (ksc * Unit<CODE>::value);
+              float f = qs[nt][j] * ksc;
+              // 2^24 f has to be a float32: from 2^100 on the logits take the unit first
+              if (Unit<CODE>::value != 1.f && f > 0x1p100f) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                  x[nt][mt][j] *= Unit<CODE>::value;
+                  x[nt][mt][j + 2] *= Unit<CODE>::value;
+                }
+              } else {
+                f *= Unit<CODE>::value;
+              }
 #pragma unroll
               for (int mt = 0; mt < MT; ++mt) {
                 x[nt][mt][j] *= f;
@@ -469,7 +479,16 @@ __global__ void __launch_bounds__(ATTN_THREADS, NT == 1 ? 3 : 2) kv8_attn_kernel
               }
             }
           }
-          const float vs = vsc * Unit<CODE>::value;
+          float vs = vsc * Unit<CODE>::value;
+          if (Unit<CODE>::value != 1.f && vsc > 0x1p100f) {  // the same for the block's output
+            vs = vsc;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int mt = 0; mt < KS; ++mt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[nt][mt][j] *= Unit<CODE>::value;
+          }
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll

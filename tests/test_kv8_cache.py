@@ -385,6 +385,29 @@ def test_outlier_channels(code, d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("hkv,d,block,hq", [(1, 128, 32, 8), (2, 64, 16, 4), (1, 64, 64, 12)])
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+def test_blocks_near_the_end_of_the_types_range(hkv, d, block, hq, code):
+    # |x| up to 1e34.  A running sum has at most 100 terms of at most 2^8 x 1e34: 2.6e38, a float32.
+    p = Pair(2, 8, hkv, d, block, torch.bfloat16, code, 23)
+    kv = [(1e34 * (2 * torch.rand((150, hkv, d), generator=p.g) - 1)).to(torch.bfloat16) for _ in range(2)]
+    p.append([100, 50], kv=kv)
+    p.check_state()
+    p.attend(hq, gain=2e-34)  # logits of ordinary size
+    # one key whose logits are near the end of float32, zeros beside it: all of the weight is on its token
+    p = Pair(1, 8, hkv, d, block, torch.bfloat16, code, 24)
+    k, v = torch.zeros((90, hkv, d)), torch.randn((90, hkv, d), generator=p.g)
+    k[5, :, 3] = 1e34
+    p.append([90], kv=[k.to(torch.bfloat16), v.to(torch.bfloat16)])
+    q = torch.zeros((1, hq, d), dtype=torch.bfloat16)
+    q[:, :, 3] = 1000
+    out = p.cache.attn(q.cuda(), torch.tensor([90], dtype=torch.int32, device="cuda")).double().cpu()
+    rows = torch.from_numpy(p.o.rows(0, 90)[1][5])  # [hkv, d], what the codes of token 5 stand for
+    want = rows.repeat_interleave(hq // hkv, 0)[None]
+    assert (out - want).abs().le(2.0 ** -8 * want.abs() + 2.0 ** -20).all()
+
+
+@pytest.mark.gpu
 def test_what_lies_behind_the_length_is_not_used():
     p = Pair(3, 4, 2, 64, 32, torch.float16, "e4m3", 8)
     p.append([40, 128, 97])
