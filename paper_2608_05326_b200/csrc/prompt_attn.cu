@@ -203,7 +203,7 @@ struct PromptItem {
 // SMs end together: sequences in groups of 32; in a group the tiles by falling number of keys, level by level (a level: the rows
 // of one tile more or less; a sequence's tiles have one each, from its prefix on); on a level the sequences that have it; then
 // the heads, then the parts of the keys.  *at, *before: where the last search ended (first sequence of the group, items before
-// it); positions only grow.
+// it), which is where the next one starts; positions mostly grow, but nothing promises it: a smaller one starts at the front.
 __device__ __forceinline__ PromptItem item_of(const PromptArgs& a, int x, int lane, int* at, int* before) {
   PromptItem it;
   const int t = x / a.splits, step = 2 * a.T, groups = a.Hq / a.P;
@@ -212,6 +212,10 @@ __device__ __forceinline__ PromptItem item_of(const PromptArgs& a, int x, int la
   it.valid = 0;
   it.s = 0;
   int mt = 0;
+  if (t < *before) {
+    *at = 0;
+    *before = 0;
+  }
   for (; *at < a.n_seqs; *at += 32) {
     const int s = *at + lane;
     int first, n = 0, keys = 0;
@@ -341,7 +345,11 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
           asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
                            smem_u32((void*)words)), "r"(b_next) : "memory");
         }
+#ifdef QEVICT_DEBUG_BOUNDS  // the checking build has its positions fall
+        const PromptItem it = item_of(a, (int)gridDim.x - 1 - x, lane, &at, &before);
+#else
         const PromptItem it = item_of(a, x, lane, &at, &before);
+#endif
         if (it.valid) {
           if (put >= 2) ok = warp_wait<true>(b_taken + 8 * (put & 1), (uint32_t)((put >> 1) - 1) & 1u);
           if (ok && lane == 0) {

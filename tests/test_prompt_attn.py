@@ -267,6 +267,21 @@ def test_many_sequences_and_wide_groups():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("causal", [True, False])
+def test_hundreds_of_sequences(causal):
+    # several work items for every SM, several groups of 32 sequences, empty sequences at either end
+    rng = np.random.default_rng(8)
+    nq = [0, 0] + [int(x) for x in rng.integers(0, 300, 210)] + [700] + [int(x) for x in rng.integers(0, 40, 120)] + [0] * 40
+    nk = [int(max(0, x + rng.integers(-20, 200))) for x in nq]
+    q, k, v = (x.cuda() for x in _make(nq, nk, 4, 2, 64, torch.bfloat16, 14))
+    out, lse = torch.full_like(q, 3.0), torch.full((4, sum(nq)), 7.0, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    binding.qevict_prompt_attn(q, k, v, _cu(nq), _cu(nk), max(nq), max(nk), causal=causal, out=out, lse=lse, status=status)
+    _check_packed(out, lse, q, k, v, nq, nk, causal, torch.bfloat16)
+    assert int(status) == 0
+
+
+@pytest.mark.gpu
 def test_nothing_to_attend_to_and_nothing_to_do():
     q, k, v = (x.cuda() for x in _make([5], [0], 2, 1, 64, torch.float16, 1))
     out, lse = binding.qevict_prompt_attn(q, k, v, _cu([5]), _cu([0]), return_lse=True)
