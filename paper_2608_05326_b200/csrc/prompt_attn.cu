@@ -819,6 +819,17 @@ const char* prompt_check(const qevict_prompt_args* p, qevict_status* st) {
   return nullptr;
 }
 
+// The arguments with bounds that do not pass the rows there are: a packed sequence has no more than all of them, and the plan
+// and the merge's grid (at most 2^29 CTAs with the limit on query tiles) go by the bounds.
+qevict_prompt_args prompt_cut(const qevict_prompt_args& p) {
+  qevict_prompt_args c = p;
+  if (p.layout == QEVICT_LAYOUT_PACKED) {
+    if (c.max_q > c.total_q) c.max_q = (int32_t)c.total_q;
+    if (c.max_k > c.total_k) c.max_k = (int32_t)c.total_k;
+  }
+  return c;
+}
+
 const char* prompt_check_pointers(const qevict_prompt_args* p) {
   const bool keys = p->max_k > 0 && (p->layout == QEVICT_LAYOUT_PADDED || p->total_k > 0);
   if (!p->q || !p->out) return "q and out must not be NULL";
@@ -912,14 +923,16 @@ QEVICT_API qevict_status qevict_prompt_attn_scratch_bytes(const qevict_prompt_ar
   const char* why = prompt_check(args, &st);
   if (!why && !bytes) { why = "bytes is NULL"; st = QEVICT_ERR_INVALID_ARG; }
   if (why) return stateless_fail(st, why);
-  *bytes = prompt_bytes(args, prompt_splits(args));
+  const qevict_prompt_args cut = prompt_cut(*args);
+  *bytes = prompt_bytes(&cut, prompt_splits(&cut));
   return QEVICT_OK;
 }
 
-QEVICT_API qevict_status qevict_prompt_attn(const qevict_prompt_args* args, void* scratch, uint64_t scratch_bytes, void* stream) {
+QEVICT_API qevict_status qevict_prompt_attn(const qevict_prompt_args* given, void* scratch, uint64_t scratch_bytes, void* stream) {
   qevict_status st;
-  const char* why = prompt_check(args, &st);
+  const char* why = prompt_check(given, &st);
   if (why) return stateless_fail(st, why);
+  const qevict_prompt_args cut = prompt_cut(*given), *args = &cut;
   const bool padded = args->layout == QEVICT_LAYOUT_PADDED;
   if (args->n_seqs == 0 || args->max_q == 0 || (!padded && args->total_q == 0)) return QEVICT_OK;
   why = prompt_check_pointers(args);

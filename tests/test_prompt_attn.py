@@ -303,6 +303,24 @@ def test_lengths_are_cut_to_the_bounds():
     assert (out[150:200] == 3).all() and (lse[:, 150:200] == 7).all()
 
 
+def test_packed_bounds_beyond_the_rows_plan_like_the_rows():
+    lib, need = binding.lib(), [C.c_uint64() for _ in range(2)]
+    for args, n in zip((dict(max_q=40, max_k=70000), dict(max_q=1 << 29, max_k=1 << 30)), need):
+        binding._check(lib.qevict_prompt_attn_scratch_bytes(C.byref(_args(total_q=40, total_k=70000, **args)), C.byref(n)))
+    assert need[0].value == need[1].value > 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("max_q,max_k", [(131072, 131072), (1 << 29, None), ((1 << 29) + 1, 1 << 30)])
+def test_packed_bounds_beyond_the_rows(max_q, max_k):
+    # one row in eight of 2^29 x 64 heads is 2^32 thread blocks: what a 32-bit grid cannot hold
+    nq, nk = [1, 3, 2], [5000, 131, 900]
+    q, k, v = (x.cuda() for x in _make(nq, nk, 64, 8, 64, torch.bfloat16, 51))
+    out, lse = torch.full_like(q, 3.0), torch.full((64, 6), 7.0, device="cuda")
+    binding.qevict_prompt_attn(q, k, v, _cu(nq), _cu(nk), max_q, max_k, out=out, lse=lse)
+    _check_packed(out, lse, q, k, v, nq, nk, True, torch.bfloat16)
+
+
 @pytest.mark.gpu
 def test_two_calls_at_once():
     a = [x.cuda() for x in _make([900], [900], 4, 2, 128, torch.bfloat16, 41)]
