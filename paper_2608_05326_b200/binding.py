@@ -526,15 +526,19 @@ class Kv8Cache:
             setattr(cache, name, x)
         return cache
 
-    def append(self, k, v, start, cu_new=None, max_new=1, stream=None):
+    def append(self, k, v, start, cu_new=None, max_new=None, stream=None):
         """k, v [total, H_kv, d] (any strides that keep d contiguous): token i of sequence s is row cu_new[s] + i (without
-        cu_new: one token each, row s) and becomes token start[s] + i.  start < 0: the sequence is left as it is."""
+        cu_new: one token each, row s) and becomes token start[s] + i.  start < 0: the sequence is left as it is.  max_new: bound
+        of a sequence's tokens, which sizes the launch and beyond which tokens are dropped (default: all rows, or 1 without
+        cu_new)."""
         n, dev, dtype, shape, st = self.n_seqs, self.device, self.dtype, k.shape, k.stride()
         if k.dtype is not dtype or v.dtype is not dtype or k.device != dev or v.device != dev or len(shape) != 3 or \
                 shape[1] != self.n_kv_heads or shape[2] != self.head_dim:
             _refuse("k and v must be [tokens, %d, %d] %s on %s" % (self.n_kv_heads, self.head_dim, dtype, dev))
         if shape != v.shape or st != v.stride() or st[2] != 1:
             _refuse("k and v must have the same shape and strides, the last dimension contiguous")
+        if max_new is None:
+            max_new = 1 if cu_new is None else shape[0]
         p_start = _want(start, "start", dev, _i32, (n,))
         p_cu = None if cu_new is None else _want(cu_new, "cu_new", dev, _i32, (n + 1,))
         _check(lib().qevict_kv8_append(self._view, k.data_ptr(), v.data_ptr(), st[0], st[1], shape[0], p_start, p_cu, max_new,

@@ -253,6 +253,18 @@ def test_append_to_absent_and_impossible_pages():
 
 
 @pytest.mark.gpu
+def test_append_of_prompts_without_a_bound_keeps_every_token():
+    p, r = (Pair(3, 4, 2, 64, 16, torch.float16, "int8", 27) for _ in range(2))
+    k, v = p.random(60)
+    p.append([33, 0, 27], kv=[k, v])
+    dev = dict(dtype=torch.int32, device="cuda")
+    r.cache.append(k.cuda(), v.cuda(), torch.zeros(3, **dev), torch.tensor([0, 33, 33, 60], **dev))
+    r.o, r.lens = p.o, p.lens
+    r.check_state()
+    assert int(r.cache.status) == 0
+
+
+@pytest.mark.gpu
 def test_append_takes_strided_rows():
     hkv, d, dtype = 2, 128, torch.bfloat16
     p, r = (Pair(2, 4, hkv, d, 32, dtype, "e4m3", 9) for _ in range(2))
