@@ -265,6 +265,30 @@ def test_append_of_prompts_without_a_bound_keeps_every_token():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("cu,max_new,kept", [
+    ([0, 10, 12], 7, [7, 2]),     # more tokens than the bound
+    ([0, 3, 13], 10, [3, 0]),     # rows past the input
+    ([-2, 3, 5], 10, [0, 2]),     # rows before it
+    ([0, 6, 4], 10, [6, 0]),      # falling bounds
+    ([0, 6, 4], 10, [0, 0]),      # the same for a sequence that is not to be touched: only the other one counts
+])
+def test_append_says_so_where_it_drops_rows(cu, max_new, kept):
+    p = Pair(2, 2, 1, 64, 16, torch.float16, "int8", 29)
+    k, v = p.random(12)
+    start = np.array([0 if kept[0] else -1, 0])
+    if cu[0] < 0:
+        start[0] = 0
+    p.o.append([x.double().numpy() for x in (k, v)], start, kept, [max(cu[0], 0), cu[1]])
+    p.lens = np.where(start >= 0, kept, 0)
+    dev = dict(dtype=torch.int32, device="cuda")
+    p.cache.append(k.cuda(), v.cuda(), torch.tensor(start, **dev), torch.tensor(cu, **dev), max_new)
+    p.check_state()
+    for x in (p.cache.k_tail, p.cache.v_tail):  # nothing behind them either
+        assert all(x[s, :, n:].isnan().all() for s, n in enumerate(kept))
+    assert int(p.cache.status) == 11
+
+
+@pytest.mark.gpu
 def test_append_takes_strided_rows():
     hkv, d, dtype = 2, 128, torch.bfloat16
     p, r = (Pair(2, 4, hkv, d, 32, dtype, "e4m3", 9) for _ in range(2))
