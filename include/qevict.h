@@ -426,7 +426,7 @@ QEVICT_API qevict_status qevict_prompt_attn(const qevict_prompt_args* args, void
  *   - A block is quantised once, when its last token arrives [Migration-Stable Quantization: codes are written
  *     once], in float32 with every operation rounded on its own: scale = amax / 127 (int8) or amax / 448 (e4m3),
  *     code = x / scale rounded to the nearest code, ties to even.  A block whose amax / 127 (/ 448) is zero or not
- *     finite gets scale 1; if it is not finite, codes 0.
+ *     finite gets scale 1; if it is not finite, codes 0, and *status is set.
  *   - A page id outside 0 .. n_pages - 1 means that the block is absent: it is not written, not attended to, and its
  *     mass is 0.  Any such id but -1 that a call would use also sets *status.
  *   - Lengths are device int32 [n_seqs]; a length < 1 is an empty sequence (out = 0, lse = -infinity, no mass), one

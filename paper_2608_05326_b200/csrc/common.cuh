@@ -32,6 +32,7 @@ enum : int {
   CHECK_PAGE_ID = 10,        // page id outside the pool (other than -1) where a block is needed
   CHECK_LENGTH = 11,         // length beyond the table or the call's bound
   CHECK_ALIGNMENT = 12,      // shared memory of a CTA not on a multiple of 1024 bytes
+  CHECK_NOT_FINITE = 13,     // a block to be quantised holds an infinity or not-a-number
 };
 
 static constexpr int TILE_TOKENS = 32;    // tokens per attention tile

@@ -205,7 +205,10 @@ __global__ void __launch_bounds__(NT, NV <= 4 ? 10 : 640 / NT) kv8_append_kernel
           dst[i * nt] = encode8<CODE>(y);
         }
       }
-      if (tid == 0) (w ? c.scale[1] : c.scale[0])[ph] = scale;
+      if (tid == 0) {
+        (w ? c.scale[1] : c.scale[0])[ph] = scale;
+        if (!finite) kv8_record(c.status, CHECK_NOT_FINITE);
+      }
 #pragma unroll
       for (int i = 0; i < NV; ++i) x[i] = ahead[i];
     }

@@ -289,6 +289,21 @@ def test_append_says_so_where_it_drops_rows(cu, max_new, kept):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("bad", ["nan", "inf", "-inf"])
+@pytest.mark.parametrize("code,dtype", [("int8", torch.bfloat16), ("e4m3", torch.float16)])
+def test_append_says_so_where_a_block_is_not_finite(bad, code, dtype):
+    p = Pair(2, 3, 2, 64, 16, dtype, code, 31)
+    k, v = p.random(40)
+    v[21, 1, 7] = float(bad)  # in the open block of the second sequence: kept as it is
+    p.append([16, 15], kv=[k[:31], v[:31]])
+    p.check_state()
+    assert int(p.cache.status) == 0
+    p.append([0, 1], kv=[k[31:32], v[31:32]])  # which is full now
+    p.check_state()
+    assert int(p.cache.status) == 13
+
+
+@pytest.mark.gpu
 def test_append_takes_strided_rows():
     hkv, d, dtype = 2, 128, torch.bfloat16
     p, r = (Pair(2, 4, hkv, d, 32, dtype, "e4m3", 9) for _ in range(2))
