@@ -425,7 +425,7 @@ QEVICT_API qevict_status qevict_prompt_attn(const qevict_prompt_args* args, void
  *     block_table[s][b].  The open block (len % block tokens) lies in 16 bits in the sequence's tail rows.
  *   - A block is quantised once, when its last token arrives [Migration-Stable Quantization: codes are written
  *     once], in float32 with every operation rounded on its own: scale = amax / 127 (int8) or amax / 448 (e4m3),
- *     code = x / scale rounded to the nearest code, ties to even.  A block whose amax / 127 (/ 448) is zero or not
+ *     code = x / scale rounded to the nearest code, ties to even, 0 for a zero of either sign.  A block whose amax / 127 (/ 448) is zero or not
  *     finite gets scale 1; if it is not finite, codes 0, and *status is set.
  *   - A page id outside 0 .. n_pages - 1 means that the block is absent: it is not written, not attended to, and its
  *     mass is 0.  Any such id but -1 that a call would use also sets *status.

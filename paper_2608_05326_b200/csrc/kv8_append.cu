@@ -4,7 +4,7 @@
 // quantised from its rows -- the old ones from the 16-bit tail, the new ones from the call's input -- the tokens of
 // the block that stays open go to the tail.
 //     scale = RN(amax / M), code = nearest(RN(x / scale)),  M = 127 (int8) or 448 (e4m3)
-// with IEEE float32 divisions, so the codes are a function of the values alone.
+// with IEEE float32 divisions, so the codes are a function of the values alone (a zero of either sign has code 0).
 //
 // One CTA per (block of the call, KV head and K or V, sequence): the block's rows are read once, into registers, the
 // maximum is taken over the CTA and the codes are written from the same registers.  Bandwidth bounds prompts (3 bytes
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(NT, NV <= 4 ? 10 : 640 / NT) kv8_append_kernel
           for (int k = 0; k < 4; ++k) {
             float f0, f1;
             unpair(floats_of<T>(k == 0 ? x[i].x : k == 1 ? x[i].y : k == 2 ? x[i].z : x[i].w), f0, f1);
-            y[k] = pair(__fdiv_rn(f0, scale), __fdiv_rn(f1, scale));
+            y[k] = pair(__fdiv_rn(f0 + 0.f, scale), __fdiv_rn(f1 + 0.f, scale));  // (-0 becomes 0, as in `quotient2`)
           }
           dst[i * nt] = encode8<CODE>(y);
         }

@@ -304,6 +304,26 @@ def test_append_says_so_where_a_block_is_not_finite(bad, code, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+def test_codes_of_zeros_and_of_what_rounds_to_zero(code):
+    # the same block at scales inside and outside the range in which quotients come from products
+    dev = dict(dtype=torch.int32, device="cuda")
+    x = torch.randn((16, 1, 64), generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).float()
+    x[0, 0, 0], x[3, 0, 5], x[4, 0, 6] = 5.0, -0.0, 0.0
+    got = []
+    for gain in (2.0 ** -70, 1.0, 2.0 ** 10, 2.0 ** 80):
+        c = binding.Kv8Cache.allocate(1, 1, 1, 1, 64, 16, torch.bfloat16, CODES[code])
+        c.block_table.zero_()
+        y = (x * gain).to(torch.bfloat16)
+        y[5, 0, 7], y[6, 0, 8] = -1e-39, 1e-39  # far below half a code at the larger scales, but not zeros
+        c.append(y.cuda(), y.cuda(), torch.zeros(1, **dev), torch.tensor([0, 16], **dev))
+        codes = c.k_codes.view(torch.uint8).cpu()[0, 0]
+        assert codes[3, 5] == 0 and codes[4, 6] == 0
+        got.append(codes)
+    assert all(torch.equal(got[0], z) for z in got[1:])
+
+
+@pytest.mark.gpu
 def test_append_takes_strided_rows():
     hkv, d, dtype = 2, 128, torch.bfloat16
     p, r = (Pair(2, 4, hkv, d, 32, dtype, "e4m3", 9) for _ in range(2))
