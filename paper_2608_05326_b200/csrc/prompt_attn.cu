@@ -28,6 +28,10 @@
 // enters; value rows past the end are zeroed in shared memory before the product reads them, since 0 * NaN is NaN.
 // Every wait is bounded; one that runs out records CHECK_COPY_TIMEOUT and the CTA leaves after its copies have landed.
 #include <cuda.h>
+#ifdef QEVICT_DEBUG_BOUNDS
+#include <stdio.h>
+#include <stdlib.h>
+#endif
 
 #include "kv8.cuh"
 
@@ -54,6 +58,9 @@ struct PromptArgs {
   float* part_lse;  // [split][row][Hq] (log2)
   long long rows;   // rows of the partial results
   int32_t* status;
+#ifdef QEVICT_DEBUG_BOUNDS
+  int give_up_warp, give_up_at;  // in every CTA this warp gives up at this wait of its (QEVICT_CHECK_GIVE_UP=warp:wait)
+#endif
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -82,13 +89,21 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar) {
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// LONG: what is waited for may take as long as a whole work item.
-template <bool LONG = false> __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
-  for (uint32_t it = 0; it < (LONG ? 1u << 26 : 1u << 20); ++it) {
+// Looks at a barrier until its phase is over, a number of times (a look that finds nothing takes about 1.5 us: the hardware waits).
+// ITEM: what is waited for may take as long as a whole work item; such a wait also ends when another of the CTA has given up
+// (*failed).  (A look at that word in the short waits too: 1 % slower.)
+#ifdef QEVICT_DEBUG_BOUNDS
+constexpr uint32_t LOOKS = 1u << 14, LOOKS_ITEM = 1u << 20;  // 25 ms, 1.6 s: the checking build has waits give up on purpose
+#else
+constexpr uint32_t LOOKS = 1u << 20, LOOKS_ITEM = 1u << 26;
+#endif
+template <bool ITEM = false> __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, const volatile uint32_t* failed = nullptr) {
+  for (uint32_t it = 0; it < (ITEM ? LOOKS_ITEM : LOOKS); ++it) {
     uint32_t done;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}\n"
                  : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     if (done) return true;
+    if (ITEM && *failed) return false;
   }
   return false;
 }
@@ -98,9 +113,11 @@ __device__ __forceinline__ bool bar_peek(uint32_t bar, uint32_t parity) {
                : "=r"(done) : "r"(bar), "r"(parity) : "memory");
   return done != 0;
 }
-// the same for a whole warp, with one answer
-template <bool LONG = false> __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) {
-  return __all_sync(0xffffffffu, bar_wait<LONG>(bar, parity));
+// the same for a whole warp, with one answer; says so where it gives up
+template <bool ITEM> __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* failed) {
+  const bool yes = __all_sync(0xffffffffu, bar_wait<ITEM>(bar, parity, failed));
+  if (!yes) *failed = 1;
+  return yes;
 }
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int tok, int head, int seq) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
@@ -282,7 +299,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
   const uint32_t b_q = bars, b_full = bars + 8, b_empty = b_full + 8 * NS, b_s = b_empty + 8 * NS, b_p = b_s + 16, b_o = b_p + 16,
                  b_clean = b_o + 16, b_qe = b_clean + 8, b_item = b_qe + 8, b_taken = b_item + 16, b_next = b_taken + 16,
                  b_done = b_next + 8;
-  // words: 0 .. 3 the answer; 4 tensor memory; 5 loads issued; 6 failed; 8 .. 23 softmax warps that gave up
+  // words: 0 .. 3 the answer; 4 tensor memory; 5 loads of K and V issued; 6 a wait has given up; 7 loads of Q; 8 requests for items
   volatile uint32_t* words = reinterpret_cast<volatile uint32_t*>(sm + SM::BAR_OFF + SM::WORDS);
   PromptItem* items = reinterpret_cast<PromptItem*>(sm + SM::BAR_OFF + SM::ITEMS);
   static_assert(sizeof(PromptItem) * 2 <= 128, "two work items");
@@ -309,14 +326,26 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
     bar_init(b_next, 1);
     bar_init(b_done, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    for (int i = 5; i < 24; ++i) words[i] = 0;
+    for (int i = 5; i < 9; ++i) words[i] = 0;
   }
   tm_before();
   __syncthreads();
   tm_after();
   const uint32_t tmem = words[4];
   pdl_prologue();
-  bool ok = true;
+  bool ok = true, leader = false;  // leader: the lane that issues the products
+#ifdef QEVICT_DEBUG_BOUNDS
+  int waits = 0;
+  auto gives_up = [&] {
+    if (a.give_up_warp != wid || ++waits != a.give_up_at) return false;
+    words[6] = 1;
+    return true;
+  };
+#else
+  auto gives_up = [] { return false; };
+#endif
+  auto wait = [&](uint32_t bar, uint32_t parity) { return !gives_up() && warp_wait<false>(bar, parity, words + 6); };
+  auto wait_item = [&](uint32_t bar, uint32_t parity) { return !gives_up() && warp_wait<true>(bar, parity, words + 6); };
 
   // The next item, in the place that the item warp fills; the one before is given back.  No item on failure.
   int taken = 0;
@@ -326,7 +355,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       if (lane == 0) bar_arrive(b_taken + 8 * ((taken - 1) & 1));
     }
     const int place = taken & 1;
-    ok = ok && warp_wait(b_item + 8 * place, (uint32_t)(taken >> 1) & 1u);
+    ok = ok && wait(b_item + 8 * place, (uint32_t)(taken >> 1) & 1u);
     ++taken;
     return ok && items[place].valid ? &items[place] : nullptr;
   };
@@ -341,6 +370,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       int x = blockIdx.x, y, z, put = 0, at = 0, before = 0;
       for (uint32_t ask = 0; ok; ++ask) {
         if (lane == 0) {
+          words[8] = ask + 1;
           bar_expect(b_next, 16);
           asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
                            smem_u32((void*)words)), "r"(b_next) : "memory");
@@ -351,7 +381,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         const PromptItem it = item_of(a, x, lane, &at, &before);
 #endif
         if (it.valid) {
-          if (put >= 2) ok = warp_wait<true>(b_taken + 8 * (put & 1), (uint32_t)((put >> 1) - 1) & 1u);
+          if (put >= 2) ok = wait_item(b_taken + 8 * (put & 1), (uint32_t)((put >> 1) - 1) & 1u);
           if (ok && lane == 0) {
             items[put & 1] = it;
             bar_arrive(b_item + 8 * (put & 1));
@@ -359,7 +389,11 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
           ++put;
         }
         __syncwarp();
-        if (!warp_wait(b_next, ask & 1u)) { ok = false; break; }
+        // (whatever has happened meanwhile: the answer is written to this CTA's memory)
+        if (!warp_wait<false>(b_next, ask & 1u, words + 6)) {
+          ok = false;
+          break;
+        }
         uint32_t got;
         asm volatile(
             "{\n\t.reg .b128 c;\n\t.reg .pred q;\n\tld.shared.b128 c, [%4];\n\t"
@@ -371,9 +405,9 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         __syncwarp();
         if (!got) break;
       }
-      // no more items (after a failure too: whoever still listens learns it from here or from its own limit)
-      if (put >= 2) warp_wait<true>(b_taken + 8 * (put & 1), (uint32_t)((put >> 1) - 1) & 1u);
-      if (lane == 0) {
+      // no more items
+      if (ok && put >= 2) ok = wait_item(b_taken + 8 * (put & 1), (uint32_t)((put >> 1) - 1) & 1u);
+      if (ok && lane == 0) {
         items[put & 1].valid = 0;
         bar_arrive(b_item + 8 * (put & 1));
       }
@@ -384,7 +418,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         const PromptItem& it = *item;
         const int cs = a.padded ? it.s : 0, loads = 2 * (it.n - it.lo), hk = it.h0 / (a.Hq / a.Hkv);
         if (loads == 0) continue;
-        if (q_turn > 0) ok = warp_wait<true>(b_qe, (uint32_t)(q_turn - 1) & 1u);
+        if (q_turn > 0) ok = wait_item(b_qe, (uint32_t)(q_turn - 1) & 1u);
         ++q_turn;
         if (ok && lane == 0) {
           bar_expect(b_q, (uint32_t)((it.cnt(0) > 0) + (it.cnt(1) > 0)) * (uint32_t)(a.T * a.P * D * 2));
@@ -393,13 +427,13 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
             if (it.cnt(w) > 0)
               for (int x = 0; x < D / 64; ++x)
                 tma_load(smb + SM::Q_OFF + w * SM::TILE_BYTES + x * SM::HALF, &mq, b_q, x * 64, it.q0 + it.r0 + w * a.T, it.h0, cs);
-          words[7] = 1;
+          words[7] = (uint32_t)q_turn;
         }
         int v_slot = 0;
         uint32_t v_phase = 0;
         for (int i = 0; i < loads && ok; ++i) {  // K, V of the last tile, K, V of the one before, ...
           const int j = it.n - 1 - (i >> 1);
-          if (issued >= NS) ok = warp_wait<true>(b_empty + 8 * slot, phase ^ 1u);
+          if (issued >= NS) ok = wait_item(b_empty + 8 * slot, phase ^ 1u);
           if (ok && lane == 0) {
             bar_expect(b_full + 8 * slot, SM::TILE_BYTES);
             for (int x = 0; x < D / 64; ++x)
@@ -410,7 +444,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
           if (i == 1) { v_slot = slot; v_phase = phase; }
           if (++slot == NS) { slot = 0; phase ^= 1u; }
           if (ok && i == min(3, loads) - 1 && it.dirty()) {  // zero the value rows past the end
-            ok = warp_wait(b_full + 8 * v_slot, v_phase);
+            ok = wait(b_full + 8 * v_slot, v_phase);
             const int from = it.nk - (it.n - 1) * TILE, per = (TILE - from) * 8;
             if (ok) {
               unsigned char* v0 = sm + SM::KV_OFF + v_slot * SM::TILE_BYTES + from * 128;
@@ -440,7 +474,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       const uint32_t id_o = base | (1u << 16) | ((uint32_t)(D >> 3) << 17);       // V: channels contiguous (N-major)
       const uint32_t q_lo = desc_lo(u_sm + SM::Q_OFF, 16), k_lo = desc_lo(u_sm + SM::KV_OFF, 16), v_lo = desc_lo(u_sm + SM::KV_OFF, SM::HALF);
       const uint32_t ub = u_sm + SM::BAR_OFF, u_full = ub + 8, u_empty = u_full + 8 * NS, u_s = u_empty + 8 * NS, u_p = u_s + 16, u_o = u_p + 16;
-      const bool leader = elect_one();
+      leader = elect_one();
       // Half of the products of S, a look at the other tile's P, the other half: the look's latency passes while the tensor
       // cores have work.  (A wait costs this warp some 90 cycles even when there is nothing to wait for, and the queue
       // of products is short: with the waits between the products the call took 7 % longer.)
@@ -462,7 +496,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         }
       };
       auto p_ready = [&](int w, uint32_t phase) {
-        const bool yes = __all_sync(0xffffffffu, seen) || warp_wait(u_p + 8 * w, phase);
+        const bool yes = __all_sync(0xffffffffu, seen) || wait(u_p + 8 * w, phase);
         seen = false;
         return yes;
       };
@@ -482,7 +516,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         const int u_n = uniform(it.n), u_lo = uniform(it.lo), u_n0 = uniform(it.nt0), u_n1 = uniform(it.nt1);
         if (u_n <= u_lo) continue;
         const bool dirty = it.dirty();
-        if (!(ok = warp_wait(ub, q_phase) && warp_wait(u_full + 8 * slot, phase))) break;
+        if (!(ok = wait(ub, q_phase) && wait(u_full + 8 * slot, phase))) break;
         q_phase ^= 1u;
         if (u_n - 1 < u_n0) issue_s(0, slot, phase1);
         if (u_n - 1 < u_n1) issue_s(1, slot, phase0);
@@ -496,14 +530,14 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         uint32_t acc0 = 0, acc1 = 0;
         for (int j = u_n - 1; j >= u_lo; --j) {
           const int sv = slot;
-          ok = warp_wait(u_full + 8 * sv, phase);  // V(j)
+          ok = wait(u_full + 8 * sv, phase);  // V(j)
           if (++slot == NS) { slot = 0; phase ^= 1u; }
           if (ok && j == u_n - 1 && dirty) {
-            ok = warp_wait(b_clean, clean_phase);
+            ok = wait(b_clean, clean_phase);
             clean_phase ^= 1u;
           }
           const bool more = j > u_lo;
-          if (more) ok = ok && warp_wait(u_full + 8 * slot, phase);  // K(j - 1)
+          if (more) ok = ok && wait(u_full + 8 * slot, phase);  // K(j - 1)
           if (!ok) break;
           if (j < u_n0) {
             if (!(ok = p_ready(0, phase0))) break;
@@ -534,25 +568,21 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         seen = false;
         if (!ok) break;
       }
-      if (!ok) {  // the tensor memory is given back below: not under products that are still running
-        if (leader) commit_to(b_done);
-        __syncwarp();
-        warp_wait(b_done, 0);
-      }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
-    // Two threads to a row: 64 keys of every tile each.  The two warps that share rows meet at a barrier of their own,
-    // where each also says whether a wait of its has run out, so that both leave at the same point.
+    // Two threads to a row: 64 keys of every tile each.  The two warps that share rows meet at a barrier of their own, which
+    // also gives both the same answer to whether a wait of either's has run out, so that both leave at the same point.
     const int w = wid >> 3, half = (wid >> 2) & 1, r = (wid & 3) * 32 + lane;
     const int hl = r / a.T, tok = w * a.T + r - hl * a.T;  // head and token of this row; rows past P heads are not used
     const uint32_t lane_base = (uint32_t)((wid & 3) * 32) << 16;
     const uint32_t ts = tmem + lane_base + w * 128, to = tmem + lane_base + 256 + w * 128 + half * (D / 2);
     float* xch = reinterpret_cast<float*>(sm + SM::BAR_OFF + SM::ROWS) + w * 2 * TILE + r;  // the two halves' values of a row
     auto meet = [&] {
-      if (!ok) words[8 + wid] = 1;
-      asm volatile("bar.sync %0, 64;\n" ::"r"(1 + w * 4 + (wid & 3)) : "memory");
-      ok = ok && words[8 + (wid ^ 4)] == 0;
+      uint32_t both;
+      asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}\n"
+                   : "=r"(both) : "r"((uint32_t)ok), "r"(1 + w * 4 + (wid & 3)) : "memory");
+      ok = both != 0;
     };
     uint32_t s_phase = 0, o_phase = 0;
     while (true) {
@@ -567,7 +597,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       float m = -INFINITY, l = 0.f;
       for (int i = cnt; i > 0; --i, left += TILE) {
         // S(j) stands for P V of the tile before too: a commit waits for everything its thread has issued before
-        ok = warp_wait(b_s + 8 * w, s_phase);
+        ok = wait(b_s + 8 * w, s_phase);
         s_phase ^= 1u;
         float x[TILE / 2];
         if (ok) {
@@ -635,7 +665,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       if (!ok) break;
       // results: the two halves' sums, half of the channels each
       if (cnt > 0) {
-        ok = warp_wait(b_o + 8 * w, o_phase);
+        ok = wait(b_o + 8 * w, o_phase);
         o_phase ^= 1u;
       }
       tm_after();
@@ -679,17 +709,22 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       __syncwarp();
     }
   }
-  if (!ok) {
-    words[6] = 1;
-    kv8_record(a.status, CHECK_COPY_TIMEOUT);
-  }
   tm_before();
   __syncthreads();
   tm_after();
-  if (words[6] && tid == 0) {  // a wait ran out: the copies in flight must land before the shared memory is given up
-    const int issued = (int)words[5];
-    for (int i = max(0, issued - NS); i < issued; ++i) bar_wait(b_full + 8 * (i % NS), (uint32_t)(i / NS) & 1u);
-    if (words[7]) bar_wait(b_q, 0);
+  if (words[6]) {  // a wait has given up: nothing may be under way when tensor and shared memory are given back
+    if (wid == MMA_WARP) {
+      if (leader) commit_to(b_done);
+      __syncwarp();
+      bar_wait(b_done, 0);
+    }
+    if (tid == 0) {
+      const int issued = (int)words[5], queries = (int)words[7], asked = (int)words[8];
+      for (int i = max(0, issued - NS); i < issued; ++i) bar_wait(b_full + 8 * (i % NS), (uint32_t)(i / NS) & 1u);
+      if (queries) bar_wait(b_q, (uint32_t)(queries - 1) & 1u);
+      if (asked) bar_wait(b_next, (uint32_t)(asked - 1) & 1u);
+      kv8_record(a.status, CHECK_COPY_TIMEOUT);
+    }
   }
   __syncthreads();
   if (wid == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
@@ -954,6 +989,11 @@ QEVICT_API qevict_status qevict_prompt_attn(const qevict_prompt_args* given, voi
   a.part_o = static_cast<float*>(scratch);
   a.part_lse = reinterpret_cast<float*>(static_cast<char*>(scratch) + prompt_o_bytes(args, a.splits));
   a.status = args->status;
+#ifdef QEVICT_DEBUG_BOUNDS
+  a.give_up_warp = -1;
+  a.give_up_at = 0;
+  if (const char* e = getenv("QEVICT_CHECK_GIVE_UP")) sscanf(e, "%d:%d", &a.give_up_warp, &a.give_up_at);
+#endif
   DeviceGuard guard(args->device);
   cudaError_t e = guard.err;
   if (e != cudaSuccess) return stateless_fail(QEVICT_ERR_CUDA, cudaGetErrorString(e));
