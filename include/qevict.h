@@ -412,7 +412,8 @@ typedef struct {
   int64_t k_stride[3];
   int64_t v_stride[3];
   int64_t out_stride[3];
-  int32_t* status;           /* device int32 or NULL: set to a nonzero code if a kernel gave up (see qevict_stats) */
+  int32_t* status;           /* device int32 or NULL: set to a nonzero code if a kernel gave up (see qevict_stats); the rows
+                              * without a result are not-a-number then, status or not */
 } qevict_prompt_args;
 QEVICT_API qevict_status qevict_prompt_attn_scratch_bytes(const qevict_prompt_args* args, uint64_t* bytes);
 QEVICT_API qevict_status qevict_prompt_attn(const qevict_prompt_args* args, void* scratch, uint64_t scratch_bytes, void* stream);

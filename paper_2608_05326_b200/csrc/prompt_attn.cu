@@ -26,7 +26,8 @@
 //
 // Keys past the sequence's end are masked by selection, so what lies there (another sequence, padding, NaN) never
 // enters; value rows past the end are zeroed in shared memory before the product reads them, since 0 * NaN is NaN.
-// Every wait is bounded; one that runs out records CHECK_COPY_TIMEOUT and the CTA leaves after its copies have landed.
+// Every wait is bounded; one that runs out records CHECK_COPY_TIMEOUT and the CTA leaves after its copies have landed and its
+// unfinished rows have become not-a-number.
 #include <cuda.h>
 #ifdef QEVICT_DEBUG_BOUNDS
 #include <stdio.h>
@@ -202,7 +203,7 @@ template <int D> struct PromptSmem {
   static constexpr int HALF = TILE * 128;             // 64 channels of 128 rows
   static constexpr int TILE_BYTES = HALF * (D / 64);
   static constexpr int Q_OFF = 0, KV_OFF = 2 * TILE_BYTES, BAR_OFF = KV_OFF + STAGES * TILE_BYTES;
-  static constexpr int WORDS = 256, ITEMS = 384, ROWS = 512;  // behind the barriers: words, work items, row maxima
+  static constexpr int WORDS = 256, ITEMS = 320, ROWS = 544;  // behind the barriers: words, work items, row maxima
   static constexpr int BYTES = BAR_OFF + ROWS + 2048;
 };
 
@@ -302,7 +303,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
   // words: 0 .. 3 the answer; 4 tensor memory; 5 loads of K and V issued; 6 a wait has given up; 7 loads of Q; 8 requests for items
   volatile uint32_t* words = reinterpret_cast<volatile uint32_t*>(sm + SM::BAR_OFF + SM::WORDS);
   PromptItem* items = reinterpret_cast<PromptItem*>(sm + SM::BAR_OFF + SM::ITEMS);
-  static_assert(sizeof(PromptItem) * 2 <= 128, "two work items");
+  static_assert(SM::ITEMS + sizeof(PromptItem) * 4 <= SM::ROWS, "two work items, and two that could not be handed out");
   if (smb & 1023u) {  // no tile would be where the products look for it
     kv8_record(a.status, CHECK_ALIGNMENT);
     return;
@@ -327,6 +328,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
     bar_init(b_done, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     for (int i = 5; i < 9; ++i) words[i] = 0;
+    for (int i = 0; i < 4; ++i) items[i].valid = 0;
   }
   tm_before();
   __syncthreads();
@@ -368,23 +370,28 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       // while the item before is in work.  (A grid of single-item CTAs pays for start, first loads and results of every
       // item with idle tensor cores: 12 packed prompts of up to 4001 tokens took 620 us.)
       int x = blockIdx.x, y, z, put = 0, at = 0, before = 0;
-      for (uint32_t ask = 0; ok; ++ask) {
+      auto item_at = [&] {
+#ifdef QEVICT_DEBUG_BOUNDS  // the checking build has its positions fall
+        return item_of(a, (int)gridDim.x - 1 - x, lane, &at, &before);
+#else
+        return item_of(a, x, lane, &at, &before);
+#endif
+      };
+      for (uint32_t ask = 0;; ++ask) {
         if (lane == 0) {
           words[8] = ask + 1;
           bar_expect(b_next, 16);
           asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
                            smem_u32((void*)words)), "r"(b_next) : "memory");
         }
-#ifdef QEVICT_DEBUG_BOUNDS  // the checking build has its positions fall
-        const PromptItem it = item_of(a, (int)gridDim.x - 1 - x, lane, &at, &before);
-#else
-        const PromptItem it = item_of(a, x, lane, &at, &before);
-#endif
+        const PromptItem it = item_at();
         if (it.valid) {
           if (put >= 2) ok = wait_item(b_taken + 8 * (put & 1), (uint32_t)((put >> 1) - 1) & 1u);
           if (ok && lane == 0) {
             items[put & 1] = it;
             bar_arrive(b_item + 8 * (put & 1));
+          } else if (!ok && lane == 0) {
+            items[2] = it;
           }
           ++put;
         }
@@ -404,6 +411,11 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the answer is read before the next one is written
         __syncwarp();
         if (!got) break;
+        if (!ok) {  // taken over, and nobody else's now
+          const PromptItem lost = item_at();
+          if (lane == 0) items[3] = lost;
+          break;
+        }
       }
       // no more items
       if (ok && put >= 2) ok = wait_item(b_taken + 8 * (put & 1), (uint32_t)((put >> 1) - 1) & 1u);
@@ -724,6 +736,23 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       if (queries) bar_wait(b_q, (uint32_t)(queries - 1) & 1u);
       if (asked) bar_wait(b_next, (uint32_t)(asked - 1) & 1u);
       kv8_record(a.status, CHECK_COPY_TIMEOUT);
+    }
+    // The rows of the items that may not be finished become not-a-number, for callers who do not read the status: the two that
+    // were handed out last and the two that were not.
+    for (int n = 0; n < 4; ++n) {
+      const PromptItem& it = items[n];
+      for (int i = tid; it.valid && i < 2 * a.T * a.P; i += PROMPT_THREADS) {
+        const int row = it.r0 + i / a.P, hq = it.h0 + i % a.P;
+        if (row >= it.nq) break;
+        const long long prow = a.padded ? (long long)it.s * a.max_q + row : (long long)it.q0 + row;
+        if (a.splits > 1) {
+          a.part_lse[((long long)it.split * a.rows + prow) * a.Hq + hq] = NAN;  // as a weight, it makes the merged row that
+          continue;
+        }
+        if (a.lse) a.lse[a.padded ? ((long long)it.s * a.Hq + hq) * a.max_q + row : hq * a.total_q + prow] = NAN;
+        T* out = static_cast<T*>(a.out) + (a.padded ? it.s * a.out_stride[0] + row * a.out_stride[2] : prow * a.out_stride[2]) + hq * a.out_stride[1];
+        for (int c = 0; c < D; ++c) out[c] = Tr<T>::from_float(NAN);
+      }
     }
   }
   __syncthreads();

@@ -33,7 +33,7 @@ def test_suites_pass_whatever_the_order_of_the_work_items():
     assert " passed" in r.stdout and "failed" not in r.stdout, tail
 
 
-_GIVE_UP = """
+_CALLS = """
     import os, time
     import numpy as np
     import torch
@@ -64,6 +64,9 @@ _GIVE_UP = """
         call()  # warm
         calls.append((call, call()))
         assert calls[-1][1][2] == 0
+"""
+
+_GIVE_UP = _CALLS + """
     gave_up = 0
     for warp in (0, 5, 9, 15, 16, 17, 18):  # softmax of both query tiles and halves; products; copies; work items
         for at in (1, 2, 3, 4, 7, 12, 30):
@@ -89,3 +92,27 @@ def test_a_wait_that_gives_up_ends_the_call_with_a_status():
     thread block leaves, its other warps have to leave with it and soon."""
     r = _run(_GIVE_UP)
     assert r.returncode == 0 and "gave up" in r.stdout, r.stdout[-1500:] + r.stderr[-3000:]
+
+
+_ROWS = _CALLS + """
+    lost = rows = 0
+    for warp in (0, 6, 11, 15, 16, 17, 18):
+        for at in (1, 2, 3, 5, 6, 8, 10, 14, 20):
+            for call, want in calls:
+                os.environ["QEVICT_CHECK_GIVE_UP"] = "%d:%d" % (warp, at)
+                out, lse, status = call()
+                del os.environ["QEVICT_CHECK_GIVE_UP"]
+                right = (out == want[0]).all(-1) & (lse.T == want[1].T)
+                gone = out.isnan().all(-1) & lse.T.isnan()
+                assert (right | gone).all(), (warp, at, int((~(right | gone)).sum()), out.shape)
+                assert status == (5 if gone.any() else 0) or bool(right.all()), (warp, at, status)
+                lost, rows = lost + int(gone.sum()), rows + gone.numel()
+    assert 0 < lost < rows
+    print("lost", lost, rows)
+"""
+
+
+def test_a_row_without_a_result_is_not_a_number():
+    """Whatever a call has to give up: each row and head holds its result, or not-a-number in every channel and in lse."""
+    r = _run(_ROWS)
+    assert r.returncode == 0 and "lost" in r.stdout, r.stdout[-1500:] + r.stderr[-3000:]
