@@ -385,7 +385,8 @@ QEVICT_API qevict_status qevict_import_state(qevict_handle h, int32_t layer, int
  * outside every sequence are neither read into a result nor written).  PADDED: q [n_seqs, n_q_heads, max_q, d],
  * k, v [n_seqs, n_kv_heads, max_k, d] (the layout of qevict_prefill_assign), lse [n_seqs, n_q_heads, max_q];
  * bounds are device int32 [n_seqs] lengths, or NULL for max_q / max_k everywhere.  max_q and max_k bound the
- * lengths; a longer sequence is cut to them.  A key or value that is not finite spreads to every row of the
+ * lengths; a longer sequence is cut to them, one that reaches outside the rows to these, one whose bounds fall is
+ * empty; each sets *status.  A key or value that is not finite spreads to every row of the
  * sequence from 255 tokens before it on (nothing outside the sequence is affected). */
 enum { QEVICT_LAYOUT_PACKED = 0, QEVICT_LAYOUT_PADDED = 1 };
 typedef struct {
@@ -412,8 +413,8 @@ typedef struct {
   int64_t k_stride[3];
   int64_t v_stride[3];
   int64_t out_stride[3];
-  int32_t* status;           /* device int32 or NULL: set to a nonzero code if a kernel gave up (see qevict_stats); the rows
-                              * without a result are not-a-number then, status or not */
+  int32_t* status;           /* device int32 or NULL: set to a nonzero code if a sequence was cut or a kernel gave up; the rows
+                              * without a result are not-a-number in the latter case, status or not */
 } qevict_prompt_args;
 QEVICT_API qevict_status qevict_prompt_attn_scratch_bytes(const qevict_prompt_args* args, uint64_t* bytes);
 QEVICT_API qevict_status qevict_prompt_attn(const qevict_prompt_args* args, void* scratch, uint64_t scratch_bytes, void* stream);

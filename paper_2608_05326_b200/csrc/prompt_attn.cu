@@ -194,6 +194,13 @@ __device__ __forceinline__ void span_of(const int32_t* bounds, int padded, int s
   }
 }
 
+// Whether span_of has to cut sequence s: outside the rows there are, longer than the bound, falling.
+__device__ __forceinline__ bool span_cut(const int32_t* bounds, int padded, int s, int most, long long total) {
+  if (padded) return bounds && (bounds[s] < 0 || bounds[s] > most);
+  const long long b0 = bounds[s], b1 = bounds[s + 1];
+  return b0 < 0 || b1 < b0 || b1 > total || b1 - b0 > most;
+}
+
 // Column of the 16 keys `k` (0 .. 3) of half `half` of a tile's P, over the S of the same half: the thread that writes it
 // has read what it overwrites.
 __device__ __forceinline__ constexpr int P_COL(int half, int k) { return half * 64 + k * 8; }
@@ -422,6 +429,11 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       if (ok && lane == 0) {
         items[put & 1].valid = 0;
         bar_arrive(b_item + 8 * (put & 1));
+      }
+      if (blockIdx.x == 0 && a.status) {
+        for (int s = lane; s < a.n_seqs; s += 32)
+          if (span_cut(a.q_bounds, a.padded, s, a.max_q, a.total_q) || span_cut(a.k_bounds, a.padded, s, a.max_k, a.total_k))
+            kv8_record(a.status, CHECK_LENGTH);
       }
     } else if (wid == LOAD_WARP) {
       int slot = 0, q_turn = 0, issued = 0;

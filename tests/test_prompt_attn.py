@@ -322,6 +322,50 @@ def test_packed_bounds_beyond_the_rows(max_q, max_k):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("cu_q,cu_k,max_q,max_k", [
+    ([0, 20, 60], [0, 30, 90], 40, 60),     # as they should be
+    ([0, 20, 61], [0, 30, 90], 60, 90),     # queries past the rows
+    ([0, 20, 60], [0, 30, 200], 40, 90),    # keys past the rows
+    ([-3, 20, 60], [0, 30, 90], 40, 60), ([0, 20, 60], [-1, 30, 90], 40, 60), ([0, 20, 7], [0, 30, 90], 40, 60), ([0, 20, 60], [0, 30, 9], 40, 60),
+    ([0, 20, 60], [0, 30, 90], 39, 60), ([0, 20, 60], [0, 30, 90], 40, 59),
+])
+def test_packed_bounds_that_are_cut_set_the_status(cu_q, cu_k, max_q, max_k):
+    q, _, _ = _make([60], [60], 2, 1, 64, torch.float16, 61)
+    _, k, v = _make([90], [90], 2, 1, 64, torch.float16, 62)
+    q, k, v = q.cuda(), k.cuda(), v.cuda()
+    dev = dict(dtype=torch.int32, device="cuda")
+    out, lse, status = torch.full_like(q, 3.0), torch.full((2, 60), 7.0, device="cuda"), torch.zeros(1, **dev)
+    binding.qevict_prompt_attn(q, k, v, torch.tensor(cu_q, **dev), torch.tensor(cu_k, **dev), max_q, max_k, causal=False, out=out, lse=lse, status=status)
+    cut = lambda c, most, total: [(max(0, a), min(b, total, max(0, a) + most)) for a, b in zip(c, c[1:])]  # noqa: E731
+    seqs = list(zip(cut(cu_q, max_q, 60), cut(cu_k, max_k, 90)))
+    written = torch.zeros(60, dtype=torch.bool)
+    for (a, b), (x, y) in seqs:
+        if b > a:
+            y = max(x, y)
+            _check_rows(out[a:b], lse[:, a:b], q[a:b], k[x:y], v[x:y], False, torch.float16)
+            written[a:b] = True
+    assert (out.cpu()[~written] == 3).all() and (lse.cpu()[:, ~written] == 7).all()
+    good = (cu_q, cu_k, max_q, max_k) == ([0, 20, 60], [0, 30, 90], 40, 60)
+    assert int(status) == (0 if good else 11)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lq,lk,code", [([5, 9], [9, 0], 0), ([5, 10], [9, 0], 11), ([-1, 9], [9, 9], 11), ([5, 9], [9, 12], 11), (None, None, 0)])
+def test_padded_lengths_that_are_cut_set_the_status(lq, lk, code):
+    g = torch.Generator().manual_seed(63)
+    q, k, v = (torch.randn((2, h, 9, 64), generator=g).half().cuda() for h in (2, 1, 1))
+    dev = dict(dtype=torch.int32, device="cuda")
+    out, lse, status = torch.full_like(q, 3.0), torch.full((2, 2, 9), 7.0, device="cuda"), torch.zeros(1, **dev)
+    lens = [None if x is None else torch.tensor(x, **dev) for x in (lq, lk)]
+    binding.qevict_prompt_attn(q, k, v, lens[0], lens[1], out=out, lse=lse, status=status)
+    for i in range(2):
+        a, b = (9 if x is None else min(max(x[i], 0), 9) for x in (lq, lk))
+        _check_rows(out[i, :, :a].transpose(0, 1), lse[i, :, :a], q[i, :, :a].transpose(0, 1), k[i, :, :b].transpose(0, 1), v[i, :, :b].transpose(0, 1), True, torch.float16)
+        assert (out[i, :, a:] == 3).all() and (lse[i, :, a:] == 7).all()
+    assert int(status) == code
+
+
+@pytest.mark.gpu
 def test_two_calls_at_once():
     a = [x.cuda() for x in _make([900], [900], 4, 2, 128, torch.bfloat16, 41)]
     b = [x.cuda() for x in _make([3], [9000], 7, 1, 64, torch.float16, 42)]
