@@ -400,7 +400,7 @@ typedef struct {
   int32_t head_dim;          /* 64 or 128 */
   int32_t max_q, max_k;
   int32_t causal;            /* 0 or 1 */
-  float softmax_scale;       /* 0 => 1/sqrt(d); else at least 1e-30 */
+  float softmax_scale;       /* 0 => 1/sqrt(d); else 1e-30 .. 2e38 */
   int64_t total_q, total_k;  /* PACKED: rows of q / of k and v; PADDED: ignored */
   const void* q;             /* device */
   const void* k;
@@ -475,7 +475,7 @@ QEVICT_API qevict_status qevict_kv8_append(const qevict_kv8_cache* cache, const 
  * score_out [n_seqs, max_blocks] float32 or NULL: score_in (NULL: 0; may be score_out itself) plus the probability mass
  * that the block's tokens received, summed over the query heads [Eq. 1], in a fixed order.  Blocks past the length get
  * score_in.  scratch: device, from qevict_kv8_attn_scratch_bytes for the same arguments; calls that may run at the
- * same time need scratch of their own.  softmax_scale 0 => 1/sqrt(d), else at least 1e-30. */
+ * same time need scratch of their own.  softmax_scale 0 => 1/sqrt(d), else 1e-30 .. 2e38. */
 QEVICT_API qevict_status qevict_kv8_attn_scratch_bytes(const qevict_kv8_cache* cache, int32_t n_q_heads, int32_t max_len,
                                                        int32_t with_scores, uint64_t* bytes);
 QEVICT_API qevict_status qevict_kv8_attn(const qevict_kv8_cache* cache, int32_t n_q_heads, float softmax_scale, const void* q,

@@ -48,6 +48,9 @@ template <class F> inline cudaError_t once_per_device(std::atomic<uint64_t>& don
   return e;
 }
 
+// 0, or a scale that is a float32 times log2 e too and leaves logits their bits.
+inline bool usable_scale(float s) { return s == 0.f || (s >= 1e-30f && s <= 2e38f); }
+
 inline bool misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 inline bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 

@@ -868,8 +868,7 @@ QEVICT_API qevict_status qevict_kv8_attn(const qevict_kv8_cache* cache, int32_t 
   const char* why = kv8_check(cache, &st, &a.c);
   if (!why) why = plan_of(a.c, n_q_heads, max_len, score_out != nullptr, sm_count(cache->device), &st, &p);
   if (why) return stateless_fail(st, why);
-  if (!(softmax_scale >= 0.f) || isinf(softmax_scale) || (softmax_scale > 0.f && softmax_scale < 1e-30f))
-    return bad("softmax_scale must be 0 or a finite number of at least 1e-30");
+  if (!usable_scale(softmax_scale)) return bad("softmax_scale must be 0 or between 1e-30 and 2e38");
   if (score_in && !score_out) return bad("score_in needs score_out");
   if (a.c.n_seqs == 0) return QEVICT_OK;
   if (!q || !lens || !out || !scratch) return bad("q, lens, out and scratch must not be NULL");

@@ -879,8 +879,7 @@ const char* prompt_check(const qevict_prompt_args* p, qevict_status* st) {
   if (p->causal != 0 && p->causal != 1) return "causal must be 0 or 1";
   if (p->n_seqs < 0 || p->max_q < 0 || p->max_k < 0 || p->total_q < 0 || p->total_k < 0) return "sizes must be >= 0";
   if (p->n_kv_heads < 1 || p->n_q_heads < 1 || p->n_q_heads % p->n_kv_heads) return "n_q_heads must be a multiple of n_kv_heads";
-  if (!(p->softmax_scale >= 0.f) || isinf(p->softmax_scale) || (p->softmax_scale > 0.f && p->softmax_scale < 1e-30f))
-    return "softmax_scale must be 0 or a finite number of at least 1e-30";
+  if (!usable_scale(p->softmax_scale)) return "softmax_scale must be 0 or between 1e-30 and 2e38";
   *st = QEVICT_ERR_UNSUPPORTED;
   if (p->head_dim != 64 && p->head_dim != 128) return "head_dim must be 64 or 128";
   if (p->n_seqs > 65535 || p->n_q_heads > 1024) return "more than 65535 sequences or 1024 heads";

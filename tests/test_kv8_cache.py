@@ -97,6 +97,11 @@ def test_unusable_arguments_are_refused_with_a_reason(call, status, word):
     assert call() == status and word in binding.lib().qevict_last_error(None).decode()
 
 
+@pytest.mark.parametrize("scale", [3e38, 2.5e38, float("nan"), -1e-3, 1e-31])
+def test_scales_that_are_no_float_times_log2_e_are_refused(scale):
+    assert _attn(_view(), scale=scale) == 1 and "softmax_scale" in binding.lib().qevict_last_error(None).decode()
+
+
 def test_nothing_to_do_is_fine_without_a_device():
     empty = _view(n_seqs=0, k_tail=None, v_tail=None, block_table=None)
     assert _append(empty) == 0 and _attn(empty) == 0 and _evict(n_seqs=0) == 0

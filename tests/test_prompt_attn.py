@@ -43,6 +43,15 @@ def test_unusable_arguments_are_refused_with_a_reason(over, status, word):
     assert e.value.status == status and word in str(e.value)
 
 
+@pytest.mark.parametrize("scale", [3e38, 2.5e38, float("inf"), float("nan"), -1e-3, 1e-31])
+def test_scales_that_are_no_float_times_log2_e_are_refused(scale):
+    lib, need = binding.lib(), C.c_uint64()
+    for call in (lambda: lib.qevict_prompt_attn(C.byref(_args(softmax_scale=scale)), None, 0, None),
+                 lambda: lib.qevict_prompt_attn_scratch_bytes(C.byref(_args(softmax_scale=scale)), C.byref(need))):
+        assert call() == 1 and b"softmax_scale" in lib.qevict_last_error(None)
+    assert lib.qevict_prompt_attn_scratch_bytes(C.byref(_args(softmax_scale=2e38)), C.byref(need)) == 0
+
+
 def test_nothing_to_do_is_fine_without_a_device():
     lib = binding.lib()
     for over in (dict(n_seqs=0), dict(max_q=0), dict(total_q=0)):
