@@ -3,6 +3,7 @@ class that owns the device workspace.  Argument marshalling only -- every step o
 CUDA kernels of the library; there is no fallback of any kind."""
 
 import ctypes as C
+import operator
 import os
 import struct
 
@@ -341,6 +342,17 @@ def _refuse(msg):
     raise QEvictError(QEVICT_ERR_INVALID_ARG, msg)
 
 
+def _bound(x, name):
+    """A size as the C side takes it: ctypes would cut one of more than 32 bits to its low ones."""
+    try:
+        n = operator.index(x)
+    except TypeError:
+        _refuse("%s must be an integer, got %r" % (name, x))
+    if not -0x80000000 <= n <= 0x7fffffff:
+        _refuse("%s does not fit 32 bits: %d" % (name, n))
+    return n
+
+
 def _want(t, name, device, dtype, shape=None):
     """Address of a tensor argument after checking what the C side cannot see: type, device, shape, contiguity."""
     try:
@@ -438,7 +450,7 @@ def qevict_prompt_attn(q, k, v, cu_q=None, cu_k=None, max_q=None, max_k=None, ca
             total_k, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
             0 if lse is None else _want(lse, "lse", dev, _f32, lse_shape), p_cq, p_ck, *sq, *sk, *sv, *so,
             0 if status is None else _want(status, "status", dev, _i32, (1,)))
-    except struct.error as e:
+    except (struct.error, OverflowError) as e:
         _refuse("an argument does not fit its field (%s)" % e)
     need = C.c_uint64()
     library = lib()
@@ -474,7 +486,7 @@ def qevict_kv8_evict(block_table, lens, scores, block, n_pages, budget, sink=0, 
         args = _EVICT_PACK.pack(C.sizeof(qevict_kv8_evict_args), dev.index, n, mb, block, n_pages, budget, sink, recent, p_table, p_lens, p_scores,
                                 table_out.data_ptr(), lens_out.data_ptr(), scores_out.data_ptr(), kept.data_ptr(), freed.data_ptr(),
                                 n_freed.data_ptr())
-    except struct.error as e:
+    except (struct.error, OverflowError) as e:
         _refuse("an argument does not fit its field (%s)" % e)
     _check(lib().qevict_kv8_evict(args, _current_stream(dev)))
     return {"block_table": table_out, "lens": lens_out, "scores": scores_out, "kept": kept, "freed": freed, "n_freed": n_freed}
@@ -541,7 +553,7 @@ class Kv8Cache:
             max_new = 1 if cu_new is None else shape[0]
         p_start = _want(start, "start", dev, _i32, (n,))
         p_cu = None if cu_new is None else _want(cu_new, "cu_new", dev, _i32, (n + 1,))
-        _check(lib().qevict_kv8_append(self._view, k.data_ptr(), v.data_ptr(), st[0], st[1], shape[0], p_start, p_cu, max_new,
+        _check(lib().qevict_kv8_append(self._view, k.data_ptr(), v.data_ptr(), st[0], st[1], shape[0], p_start, p_cu, _bound(max_new, "max_new"),
                                        _current_stream(dev) if stream is None else stream.cuda_stream))
 
     def attn(self, q, lens, max_len=None, scores=None, scores_out=None, softmax_scale=0.0, out=None, return_lse=False, stream=None):
@@ -556,8 +568,7 @@ class Kv8Cache:
             _refuse("q must be [%d, H_q, %d]" % (n, self.head_dim))
         p_q, hq = _want(q, "q", dev, dtype), shape[1]
         p_lens = _want(lens, "lens", dev, _i32, (n,))
-        if max_len is None:
-            max_len = self.max_blocks * self.block
+        max_len = self.max_blocks * self.block if max_len is None else _bound(max_len, "max_len")
         grid = (n, self.max_blocks)
         p_in = p_so = None
         if scores is not None:

@@ -575,6 +575,25 @@ def test_bindings_refuse_what_the_library_cannot_see():
             call()
 
 
+@pytest.mark.gpu
+def test_sizes_that_do_not_fit_their_fields_are_refused():
+    p = Pair(2, 4, 2, 64, 32, torch.float16, "int8")
+    p.append([40, 3])
+    c = p.cache
+    q, lens = torch.zeros((2, 4, 64), dtype=torch.float16, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    k = torch.zeros((2, 2, 64), dtype=torch.float16, device="cuda")
+    cu, x = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda"), torch.zeros(2, 4, device="cuda")
+    for call in (lambda: c.append(k, k, lens, cu, (1 << 32) + 1), lambda: c.append(k, k, lens, cu, 1.5), lambda: c.append(k, k, lens, cu, -(1 << 32) + 1),
+                 lambda: c.attn(q, lens, max_len=(1 << 32) + 40), lambda: c.attn(q, lens, max_len="40"),
+                 lambda: binding.qevict_kv8_evict(c.block_table, lens, x, 32, 10, (1 << 32) + 3), lambda: binding.qevict_prompt_attn(q, k, k, cu[:2], max_q=(1 << 32) + 2),
+                 lambda: binding.qevict_prompt_attn(q, k, k, cu[:2], softmax_scale=1e39)):
+        with pytest.raises(binding.QEvictError):
+            call()
+    p.check_state()  # nothing has been stored
+    c.append(k, k, torch.full_like(lens, -1), cu, np.int64(1))
+    assert torch.equal(c.attn(q, lens, max_len=np.int32(40)), c.attn(q, lens, max_len=40))
+
+
 # ---- eviction ---------------------------------------------------------------------------------------------------
 def _evict_case(n, mb, block, lens, scores, n_pages, seed=0):
     g = torch.Generator().manual_seed(seed)
