@@ -385,6 +385,12 @@ def _cuda(t, name):
     return t.device
 
 
+def _check_stream(stream, device):
+    """A stream of another device would leave the call on the current stream of the tensors' own, unordered with it."""
+    if stream.device != device:
+        _refuse("stream belongs to %s, the tensors to %s" % (stream.device, device))
+
+
 def qevict_prompt_attn(q, k, v, cu_q=None, cu_k=None, max_q=None, max_k=None, causal=True, softmax_scale=0.0, out=None, lse=None,
                        return_lse=False, status=None, stream=None):
     """Softmax attention over whole prompts (full precision, grouped heads, causal against the end of the keys).
@@ -397,6 +403,7 @@ def qevict_prompt_attn(q, k, v, cu_q=None, cu_k=None, max_q=None, max_k=None, ca
     of no sequence are not written.
     """
     if stream is not None:  # its buffers come from the allocator in that stream's order
+        _check_stream(stream, _cuda(q, "q"))
         with torch.cuda.stream(stream):
             return qevict_prompt_attn(q, k, v, cu_q, cu_k, max_q, max_k, causal, softmax_scale, out, lse, return_lse, status)
     dev = _cuda(q, "q")
@@ -464,6 +471,7 @@ def qevict_kv8_evict(block_table, lens, scores, block, n_pages, budget, sink=0, 
     """Keeps the `budget` best full blocks of every sequence (the first `sink` and last `recent` always).  Returns a dict:
     block_table, lens, scores (new tensors, or the given ones with in_place), kept, freed, n_freed."""
     if stream is not None:
+        _check_stream(stream, _cuda(block_table, "block_table"))
         with torch.cuda.stream(stream):
             return qevict_kv8_evict(block_table, lens, scores, block, n_pages, budget, sink, recent, in_place)
     dev = _cuda(block_table, "block_table")
@@ -549,6 +557,8 @@ class Kv8Cache:
             _refuse("k and v must be [tokens, %d, %d] %s on %s" % (self.n_kv_heads, self.head_dim, dtype, dev))
         if shape != v.shape or st != v.stride() or st[2] != 1:
             _refuse("k and v must have the same shape and strides, the last dimension contiguous")
+        if stream is not None:
+            _check_stream(stream, dev)
         if max_new is None:
             max_new = 1 if cu_new is None else shape[0]
         p_start = _want(start, "start", dev, _i32, (n,))
@@ -561,6 +571,7 @@ class Kv8Cache:
         (out[, lse][, scores_out]): scores [n_seqs, max_blocks] plus the probability mass of every block, in a new tensor
         or in scores_out (which may be scores).  max_len: bound of lens (default: what the table can hold)."""
         if stream is not None:
+            _check_stream(stream, self.device)
             with torch.cuda.stream(stream):
                 return self.attn(q, lens, max_len, scores, scores_out, softmax_scale, out, return_lse)
         n, dev, dtype, shape = self.n_seqs, self.device, self.dtype, q.shape

@@ -594,6 +594,24 @@ def test_sizes_that_do_not_fit_their_fields_are_refused():
     assert torch.equal(c.attn(q, lens, max_len=np.int32(40)), c.attn(q, lens, max_len=40))
 
 
+@pytest.mark.gpu
+def test_a_stream_of_another_device_is_refused():
+    class Elsewhere:  # what the check sees of a stream
+        device, device_index, stream_id, device_type, cuda_stream = torch.device("cuda", 5), 5, 0, 1, 0
+
+    p = Pair(2, 4, 2, 64, 32, torch.float16, "int8")
+    c, at = p.cache, Elsewhere()
+    q, lens = torch.zeros((2, 4, 64), dtype=torch.float16, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    k = torch.zeros((2, 2, 64), dtype=torch.float16, device="cuda")
+    cu, x = torch.tensor([0, 2], dtype=torch.int32, device="cuda"), torch.zeros(2, 4, device="cuda")
+    for call in (lambda s: c.append(k, k, lens, stream=s), lambda s: c.attn(q, lens, stream=s), lambda s: binding.qevict_prompt_attn(q, k, k, cu, stream=s),
+                 lambda s: binding.qevict_kv8_evict(c.block_table, lens, x, 32, 10, 3, stream=s)):
+        with pytest.raises(binding.QEvictError, match="stream belongs to"):
+            call(at)
+        call(torch.cuda.Stream())
+    torch.cuda.synchronize()
+
+
 # ---- eviction ---------------------------------------------------------------------------------------------------
 def _evict_case(n, mb, block, lens, scores, n_pages, seed=0):
     g = torch.Generator().manual_seed(seed)
