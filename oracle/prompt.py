@@ -47,3 +47,34 @@ def out_tolerance(out, spread, vmax, n_keys, d, reach, u_out, u_prob):
 
 def lse_tolerance(lse, d, reach):
     return logit_error(d, reach) + 2.0 ** -21 * np.maximum(1.0, np.abs(lse))
+
+
+def roundings(q, k, v, causal=True, scale=None):
+    """What independent roundings of the probabilities add up to: sum_j p_j^2 v_j^2 [nq, Hq, d], the largest probability of a row
+    [nq, Hq], sum_j v_j^2 over the keys [Hq, d]."""
+    q, k, v = (np.asarray(x, np.float64) for x in (q, k, v))
+    nq, hq, d = q.shape
+    nk, hkv = k.shape[0], k.shape[1]
+    scale = d ** -0.5 if scale is None else scale
+    s2, top, v2 = np.zeros((nq, hq, d)), np.zeros((nq, hq)), np.zeros((hq, d))
+    for h in range(hq):
+        g = h // (hq // hkv)
+        x = scale * (q[:, h] @ k[:, g].T)
+        if causal:
+            x = np.where(np.arange(nk)[None] <= np.arange(nq)[:, None] + nk - nq, x, -np.inf)
+        p = np.exp(x - x.max(axis=1, keepdims=True))
+        p /= p.sum(axis=1, keepdims=True)
+        s2[:, h], top[:, h], v2[h] = (p * p) @ (v[:, g] ** 2), p.max(axis=1), (v[:, g] ** 2).sum(axis=0)
+    return s2, top, v2
+
+
+def rms_tolerance(out, s2, top, v2, d, reach, u_out, u_prob, subnormal):
+    """Bound of the root mean square of an output's error over many elements, for values that are drawn independently of queries
+    and keys with mean zero.  A rounding to nearest is off by at most half a step u and has a mean square of at most u^2, and
+    those of different keys and elements are independent of each other, so that their squares add up; a probability that fp16
+    holds as a subnormal (`subnormal`) is off by at most 2^-25 of the row's reference, which is at most its largest probability.
+    The logits' errors depend on queries and keys alone: weighted with the values their squares add up too, and in the
+    denominator they move a row by at most their bound."""
+    rel = logit_error(d, reach)
+    low = (2.0 ** -25 * top[..., None]) ** 2 * v2[None] if subnormal else 0.0
+    return np.sqrt(np.mean(((u_out + rel) * out) ** 2 + (u_prob ** 2 + rel ** 2) * s2 + low)) + 1e-30

@@ -372,6 +372,35 @@ def test_long_and_many(n, hkv, block, code):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("hkv,hq,d,block,dtype,code", [(2, 4, 64, 32, torch.bfloat16, "int8"), (1, 16, 128, 128, torch.float16, "e4m3"), (2, 8, 128, 16, torch.float16, "int8")])
+def test_long_contexts_lose_no_part(hkv, hq, d, block, dtype, code):
+    # within what independent roundings leave, and that a sum without one in 256 of the keys is not
+    n = 50000
+    p = Pair(1, -(-n // block) + 1, hkv, d, block, dtype, code, 37)
+    k, v = (torch.randn((n, hkv, d), generator=p.g).to(dtype) for _ in range(2))
+    p.cache.append(k.cuda(), v.cuda(), torch.zeros(1, dtype=torch.int32, device="cuda"), torch.tensor([0, n], dtype=torch.int32, device="cuda"))
+    q = torch.randn((1, hq, d), generator=p.g).to(dtype)
+    out = p.cache.attn(q.cuda(), torch.tensor([n], dtype=torch.int32, device="cuda")).double().cpu().numpy()
+    full, kv = n // block, []  # what the codes on the device stand for, and the open block
+    pages = p.cache.block_table[0, :full].long()
+    for codes, scale, x in ((p.cache.k_codes, p.cache.k_scale, k), (p.cache.v_codes, p.cache.v_scale, v)):
+        y = (codes[pages].double() * scale[pages].double()[..., None, None]).transpose(1, 2).reshape(-1, hkv, d).cpu()
+        assert (y - x[:full * block].double()).abs().max() < 0.2
+        kv.append(torch.cat([y, x[full * block:].double()]).numpy())
+    qn = q.double().numpy()
+    ro, _, _, _ = po.attention(qn, *kv, False)
+    vmax = float(np.abs(kv[1]).max())
+    reach = 2 * d ** -0.5 * float(np.abs(qn).sum(-1).max()) * float(np.abs(kv[0]).max())  # codes enter with an offset: see the outliers' test
+    tol = po.rms_tolerance(ro, *po.roundings(qn, *kv, False), d, reach, HALF_STEP[dtype], 2.0 ** -11, True) + 2 * 32 * 2.0 ** -24 * 2 * vmax
+    rms = lambda x: float(np.sqrt(np.mean(x * x)))  # noqa: E731
+    assert rms(out - ro) <= tol, rms(out - ro) / tol
+    for i in (0, 100, 255):
+        less = kv[1].copy()
+        less[i * n // 256:(i + 1) * n // 256] = 0.0
+        assert rms(po.attention(qn, kv[0], less, False)[0] - ro) > 3 * tol
+
+
+@pytest.mark.gpu
 def test_hundreds_of_sequences():
     p = Pair(300, 3, 1, 64, 16, torch.float16, "int8", 14)
     rng = np.random.default_rng(4)

@@ -261,6 +261,90 @@ def test_strided_inputs_and_output():
     assert torch.equal(plain, out)
 
 
+def _rms(x):
+    return float(np.sqrt(np.mean(np.square(x))))
+
+
+def _check_rms(out, q, k, v, causal, dtype, parts):
+    """The output of a long sequence within what independent roundings leave; and that a sum without one of `parts` equal parts of
+    the keys, or with the weights of two neighbouring parts exchanged, would not be."""
+    q, k, v = _np(q), _np(k), _np(v)
+    ro, lse, _, reach = oracle.attention(q, k, v, causal)
+    u = HALF_STEP[dtype]
+    tol = oracle.rms_tolerance(ro, *oracle.roundings(q, k, v, causal), q.shape[-1], reach, u, u, dtype == torch.float16)
+    assert _rms(_np(out) - ro) <= tol, _rms(_np(out) - ro) / tol
+    n = k.shape[0] // parts
+    for i in (0, parts // 2, parts - 2):
+        a, b = slice(i * n, (i + 1) * n), slice((i + 1) * n, (i + 2) * n)
+        part = []  # what a merge joins: output and log of the denominator of a part by itself
+        for x in (a, b):
+            o, l, _, _ = oracle.attention(q, k[x], v[x], False)  # (every query sees these keys)
+            part.append((o, np.exp(l - lse).T[..., None]))
+        (oa, wa), (ob, wb) = part
+        assert _rms(oa * wa) > 3 * tol and _rms(ob * wb) > 3 * tol, i
+        assert _rms(oa * (wb - wa) + ob * (wa - wb)) > 3 * tol, i
+
+
+def _part_keys(n, hkv, d, parts, dtype, g):
+    # neighbouring parts of the keys weigh differently: logits of small and of large spread in turn
+    k = torch.randn((n, hkv, d), generator=g)
+    return (k * torch.where(torch.arange(n) * parts // n % 2 == 0, 0.3, 1.2)[:, None, None]).to(dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nq,nk,hq,hkv,d,dtype", [
+    (2, 70000, 4, 2, 128, torch.bfloat16), (1, 70000, 7, 1, 64, torch.float16), (40, 24001, 4, 1, 128, torch.float16), (300, 9000, 2, 1, 64, torch.bfloat16),
+])
+def test_split_keys_lose_and_exchange_no_part(nq, nk, hq, hkv, d, dtype):
+    g = torch.Generator().manual_seed(71)
+    q, v = torch.randn((nq, hq, d), generator=g).to(dtype), torch.randn((nk, hkv, d), generator=g).to(dtype)
+    k = _part_keys(nk, hkv, d, 64, dtype, g)
+    q, k, v = q.cuda(), k.cuda(), v.cuda()
+    out, lse = binding.qevict_prompt_attn(q, k, v, _cu([nq]), _cu([nk]), return_lse=True)
+    _check_packed(out, lse, q, k, v, [nq], [nk], True, dtype)
+    _check_rms(out, q, k, v, True, dtype, 64)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d,dtype,causal", [(4, 2, 128, torch.bfloat16, True), (7, 1, 64, torch.float16, True), (4, 1, 64, torch.bfloat16, False)])
+def test_padded_layout_with_split_keys(hq, hkv, d, dtype, causal):
+    n, mq, mk = 3, 5, 20000
+    g = torch.Generator().manual_seed(73)
+    q = torch.randn((n, hq, mq, d), generator=g).to(dtype).cuda()
+    v = torch.randn((n, hkv, mk, d), generator=g).to(dtype).cuda()
+    k = torch.stack([_part_keys(mk, hkv, d, 16, dtype, g).transpose(0, 1) for _ in range(n)]).cuda()
+    lq, lk = [5, 1, 3], [20000, 130, 11111]
+    for i in range(n):
+        for x, c in ((q, lq), (k, lk), (v, lk)):
+            x[i, :, c[i]:] = float("nan")
+    need, args = C.c_uint64(), _args(layout=1, n_seqs=n, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, max_q=mq, max_k=mk)
+    binding._check(binding.lib().qevict_prompt_attn_scratch_bytes(C.byref(args), C.byref(need)))
+    assert need.value > 0  # the keys are split
+    out, lse = torch.full_like(q, 3.0), torch.full((n, hq, mq), 7.0, device="cuda")
+    lens = [torch.tensor(x, dtype=torch.int32, device="cuda") for x in (lq, lk)]
+    binding.qevict_prompt_attn(q, k, v, lens[0], lens[1], causal=causal, out=out, lse=lse)
+    for i in range(n):
+        a, b = lq[i], lk[i]
+        row = [x[i, :, :c].transpose(0, 1) for x, c in ((out, a), (q, a), (k, b), (v, b))]
+        _check_rows(row[0], lse[i, :, :a], *row[1:], causal, dtype)
+        if b > 1000:
+            _check_rms(*row, causal, dtype, 16)
+        assert (out[i, :, a:] == 3).all() and (lse[i, :, a:] == 7).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(4, 2, 128, torch.bfloat16), (3, 1, 64, torch.float16)])
+def test_long_prompts_within_independent_roundings(hq, hkv, d, dtype):
+    n = 3001
+    q, k, v = (x.cuda() for x in _make([n], [n], hq, hkv, d, dtype, 77))
+    for causal in (True, False):
+        out = binding.qevict_prompt_attn(q, k, v, _cu([n]), causal=causal)
+        ro, _, _, reach = oracle.attention(_np(q), _np(k), _np(v), causal)
+        u = HALF_STEP[dtype]
+        tol = oracle.rms_tolerance(ro, *oracle.roundings(_np(q), _np(k), _np(v), causal), d, reach, u, u, dtype == torch.float16)
+        assert _rms(_np(out) - ro) <= tol
+
+
 @pytest.mark.gpu
 def test_many_sequences_and_wide_groups():
     rng = np.random.default_rng(3)
