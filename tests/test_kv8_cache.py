@@ -641,7 +641,65 @@ def test_a_stream_of_another_device_is_refused():
     torch.cuda.synchronize()
 
 
+@pytest.mark.gpu
+def test_masses_alone_and_an_output_in_the_queries_place():
+    p = Pair(2, 8, 2, 128, 32, torch.bfloat16, "int8", 41)
+    p.append([200, 77])
+    q = torch.randn((2, 8, 128), generator=p.g).to(torch.bfloat16).cuda()
+    lens = torch.tensor(p.lens, dtype=torch.int32, device="cuda")
+    want, so = p.cache.attn(q, lens, scores=torch.zeros((2, 8), device="cuda"))
+    got, mass = p.cache.attn(q, lens, scores_out=torch.full((2, 8), 7.0, device="cuda"))  # without scores: from zero
+    assert torch.equal(got, want) and torch.equal(mass, so)
+    got = p.cache.attn(q, lens, out=q)
+    assert got is q and torch.equal(got, want)
+
+
+@pytest.mark.gpu
+def test_empty_batches_and_a_bound_of_zero():
+    c = binding.Kv8Cache.allocate(4, 0, 2, 2, 64, 16, torch.float16)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    none = torch.zeros(0, **i32)
+    c.append(torch.zeros((0, 2, 64), device="cuda").half(), torch.zeros((0, 2, 64), device="cuda").half(), none)
+    assert c.attn(torch.zeros((0, 4, 64), device="cuda").half(), none).shape == (0, 4, 64)
+    got = binding.qevict_kv8_evict(c.block_table, none, torch.zeros((0, 2), device="cuda"), 16, 4, 1)
+    assert got["block_table"].shape == (0, 2)
+    p = Pair(2, 4, 1, 64, 16, torch.float16, "e4m3", 43)
+    p.append([40, 5])
+    p.attend(2, max_len=0, expect=[0, 0], scores=torch.rand((2, 4)).cuda())
+    assert int(p.cache.status) == 11
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hkv,hq,d,block,dtype,code", [(300, 300, 64, 16, torch.float16, "int8"), (96, 768, 64, 32, torch.bfloat16, "e4m3"), (64, 1024, 64, 16, torch.bfloat16, "int8")])
+def test_many_heads(hkv, hq, d, block, dtype, code):
+    p = Pair(2, 4, hkv, d, block, dtype, code, 45)
+    p.append([3 * block + 5, block - 1])
+    p.check_state()
+    p.attend(hq, scores=torch.rand((2, 4), generator=p.g).cuda())
+
+
+@pytest.mark.gpu
+def test_as_many_sequences_as_a_cache_takes():
+    p = Pair(8192, 3, 1, 64, 16, torch.float16, "e4m3", 47)
+    lens = np.random.default_rng(6).integers(0, 46, 8192)
+    lens[[0, 8191]] = [0, 48]
+    p.append([int(x) for x in lens])
+    p.check_state()
+    p.attend(2)
+    assert int(p.cache.status) == 0
+
+
 # ---- eviction ---------------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_equal", [0, 16384, 9000])
+def test_eviction_from_the_longest_tables(n_equal):
+    x = torch.rand((2, 16384), generator=torch.Generator().manual_seed(49))
+    x[:, :n_equal] = 0.25
+    table, lens, x = _evict_case(2, 16384, 16, [16384 * 16, 16383 * 16 + 5], x, 2 * 16384, 49)
+    want = oracle.evict(table.numpy(), lens.numpy(), x.numpy(), 16, 2 * 16384, 5000, 3, 70)
+    _check_evict(binding.qevict_kv8_evict(table.cuda(), lens.cuda(), x.cuda(), 16, 2 * 16384, 5000, 3, 70), want)
+
+
 def _evict_case(n, mb, block, lens, scores, n_pages, seed=0):
     g = torch.Generator().manual_seed(seed)
     table = torch.randperm(max(n * mb, 1), generator=g).int().view(n, mb)

@@ -459,6 +459,76 @@ def test_padded_lengths_that_are_cut_set_the_status(lq, lk, code):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("nq,nk", [([333, 1, 90], [333, 1, 90]), ([3, 2], [9000, 700])])
+def test_the_output_may_take_the_place_of_the_queries(nq, nk):
+    q, k, v = (x.cuda() for x in _make(nq, nk, 6, 2, 128, torch.bfloat16, 81))
+    want, lse = binding.qevict_prompt_attn(q, k, v, _cu(nq), _cu(nk), return_lse=True)
+    got, lse2 = binding.qevict_prompt_attn(q, k, v, _cu(nq), _cu(nk), out=q, return_lse=True)
+    assert got is q and torch.equal(got, want) and torch.equal(lse, lse2)
+
+
+@pytest.mark.gpu
+def test_padded_batch_without_keys():
+    q = torch.randn((2, 2, 5, 64), device="cuda").half()
+    k = torch.empty((2, 1, 0, 64), device="cuda").half()
+    out, lse = binding.qevict_prompt_attn(q, k, k, return_lse=True)
+    assert (out == 0).all() and torch.isneginf(lse).all()
+
+
+@pytest.mark.gpu
+def test_as_many_sequences_as_a_call_takes():
+    # 65535 sequences of 0 to 2 tokens, a longer one among them
+    n = 65535
+    nq = np.random.default_rng(5).integers(0, 3, n)
+    nq[[0, 40000, n - 1]] = [1, 150, 2]
+    q, k, v = (x.cuda() for x in _make([int(nq.sum())], [int(nq.sum())], 2, 1, 64, torch.float16, 83))
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, lse = binding.qevict_prompt_attn(q, k, v, _cu(nq), max_q=150, max_k=150, return_lse=True, status=status)
+    assert int(status) == 0
+    cu = np.concatenate([[0], np.cumsum(nq)])
+    one = torch.from_numpy(cu[:-1][nq == 1]).cuda()  # a row that sees itself alone
+    assert torch.equal(out[one], v[one].expand(-1, 2, -1))
+    for s in (40000, n - 1, 39999, 40001, 123, 65000):
+        a, b = cu[s], cu[s + 1]
+        _check_rows(out[a:b], lse[:, a:b], q[a:b], k[a:b], v[a:b], True, torch.float16)
+    two = torch.from_numpy(cu[:-1][nq == 2]).cuda()
+    x = [q[two + 1].double() * k[two + i].double() for i in range(2)]
+    reach = max(float(y.abs().sum(-1).max()) / 8 for y in x)
+    rl = torch.logaddexp(*(y.sum(-1) / 8 for y in x)).cpu().numpy()
+    assert (np.abs(_np(lse[:, two + 1].T) - rl) <= oracle.lse_tolerance(rl, 64, reach)).all()
+
+
+@pytest.mark.gpu
+def test_the_first_call_of_a_process_may_be_captured():
+    code = """
+import torch
+from paper_2608_05326_b200 import binding
+q, k = torch.randn((40, 2, 64), device="cuda").half(), torch.randn((40, 1, 64), device="cuda").half()
+i32 = dict(dtype=torch.int32, device="cuda")
+cu, out, lens = torch.tensor([0, 40], **i32), torch.zeros_like(q), torch.tensor([3], **i32)
+c = binding.Kv8Cache.allocate(4, 1, 4, 1, 64, 16, torch.float16)
+c.block_table.copy_(torch.arange(4).view(1, 4))
+acc, q1 = torch.zeros((1, 4), device="cuda"), q[:1].contiguous()
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    binding.qevict_prompt_attn(q, k, k, cu, max_q=40, max_k=40, out=out)
+    c.append(k, k, torch.zeros_like(lens), cu)
+    got = c.attn(q1, lens, scores=acc, scores_out=acc)[0]
+    ev = binding.qevict_kv8_evict(c.block_table, torch.full_like(lens, 40), acc, 16, 4, 1)
+g.replay()
+torch.cuda.synchronize()
+assert torch.equal(out, binding.qevict_prompt_attn(q, k, k, cu, max_q=40, max_k=40))
+assert torch.equal(got, c.attn(q1, lens)) and int(ev["n_freed"]) == 1 and abs(float(acc.sum()) - 2) < 1e-5
+print("captured")
+"""
+    import subprocess
+    import sys
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
+
+
+@pytest.mark.gpu
 def test_two_calls_at_once():
     a = [x.cuda() for x in _make([900], [900], 4, 2, 128, torch.bfloat16, 41)]
     b = [x.cuda() for x in _make([3], [9000], 7, 1, 64, torch.float16, 42)]
