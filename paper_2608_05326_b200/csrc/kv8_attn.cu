@@ -818,7 +818,7 @@ template <class T, int CODE> cudaError_t launch_attn_shape(const Kv8AttnArgs& a,
   if (a.c.D == 128) return wide ? launch_attn_ut<T, CODE, 128, 2>(a, ut, device, s) : launch_attn_ut<T, CODE, 128, 1>(a, ut, device, s);
   return wide ? launch_attn_ut<T, CODE, 64, 2>(a, ut, device, s) : launch_attn_ut<T, CODE, 64, 1>(a, ut, device, s);
 }
-template <class T> cudaError_t launch_all(const Kv8AttnArgs& a, int code, int ut, int device, cudaStream_t s) {
+template <class T> cudaError_t launch_all(const Kv8AttnArgs& a, int code, int ut, int sms, int device, cudaStream_t s) {
   cudaError_t e = code == QEVICT_CODE_INT8 ? launch_attn_shape<T, QEVICT_CODE_INT8>(a, ut, device, s) : launch_attn_shape<T, QEVICT_CODE_E4M3>(a, ut, device, s);
   // the same split of the SM's memory as the attention kernel's: an SM has to drain before it changes it
   static std::atomic<uint64_t> done{0};
@@ -830,7 +830,7 @@ template <class T> cudaError_t launch_all(const Kv8AttnArgs& a, int code, int ut
   // Blocks of a mass CTA: one to four for each of its warps, so that they about fill the SMs (one context of 2048 tokens 10.8 us
   // with four, 9.0 with one; two of 8000 tokens 14.7 and 12.3, with the statistics' threads by the number of heads).
   int mass_blocks = MERGE_WARPS;
-  while (mass_blocks < 4 * MERGE_WARPS && (long long)a.c.max_blocks * a.c.n_seqs > 148ll * mass_blocks) mass_blocks += MERGE_WARPS;
+  while (mass_blocks < 4 * MERGE_WARPS && (long long)a.c.max_blocks * a.c.n_seqs > (long long)sms * mass_blocks) mass_blocks += MERGE_WARPS;
   const int mass_ctas = a.score_out ? (a.c.max_blocks + mass_blocks - 1) / mass_blocks : 0;
   if (e == cudaSuccess)
     e = launch_pdl(kv8_merge_kernel<T>, dim3(a.Hq + mass_ctas, a.c.n_seqs), dim3(MERGE_THREADS), a.score_out ? (size_t)a.Hq * sizeof(float2) : 0, s, a, ut, mass_blocks);
@@ -866,7 +866,8 @@ QEVICT_API qevict_status qevict_kv8_attn(const qevict_kv8_cache* cache, int32_t 
   Plan p;
   auto bad = [](const char* msg) { return stateless_fail(QEVICT_ERR_INVALID_ARG, msg); };
   const char* why = kv8_check(cache, &st, &a.c);
-  if (!why) why = plan_of(a.c, n_q_heads, max_len, score_out != nullptr, sm_count(cache->device), &st, &p);
+  const int sms = why ? 0 : sm_count(cache->device);
+  if (!why) why = plan_of(a.c, n_q_heads, max_len, score_out != nullptr, sms, &st, &p);
   if (why) return stateless_fail(st, why);
   if (!usable_scale(softmax_scale)) return bad("softmax_scale must be 0 or between 1e-30 and 2e38");
   if (score_in && !score_out) return bad("score_in needs score_out");
@@ -888,7 +889,7 @@ QEVICT_API qevict_status qevict_kv8_attn(const qevict_kv8_cache* cache, int32_t 
   cudaError_t e = guard.err;
   cudaStream_t s = (cudaStream_t)stream;
   if (e == cudaSuccess)
-    e = cache->dtype == QEVICT_DTYPE_FP16 ? launch_all<__half>(a, cache->code, p.ut, cache->device, s) : launch_all<__nv_bfloat16>(a, cache->code, p.ut, cache->device, s);
+    e = cache->dtype == QEVICT_DTYPE_FP16 ? launch_all<__half>(a, cache->code, p.ut, sms, cache->device, s) : launch_all<__nv_bfloat16>(a, cache->code, p.ut, sms, cache->device, s);
   if (e != cudaSuccess) return stateless_fail(QEVICT_ERR_CUDA, cudaGetErrorString(e));
   return QEVICT_OK;
 }
