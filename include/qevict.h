@@ -491,6 +491,7 @@ QEVICT_API qevict_status qevict_kv8_attn(const qevict_kv8_cache* cache, int32_t 
  *   kept [n_seqs, max_blocks]: block index before the call of every entry of table_out, -1 behind; or NULL
  *   freed [n_seqs, max_blocks], n_freed [n_seqs]: pages of the evicted blocks in their order, -1 behind; ids outside
  *   0 .. n_pages - 1 are not listed; or NULL
+ * A page that several tables share is listed by each sequence that drops it: the caller counts its users.
  * sink + recent <= budget; max_blocks <= 16384. */
 typedef struct {
   uint32_t struct_size;      /* sizeof(qevict_kv8_evict_args) */

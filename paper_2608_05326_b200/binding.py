@@ -400,7 +400,8 @@ def qevict_prompt_attn(q, k, v, cu_q=None, cu_k=None, max_q=None, max_k=None, ca
     Padded: q [n_seqs, H_q, n, d], k, v [n_seqs, H_kv, m, d]; cu_q, cu_k int32 [n_seqs] lengths or None; lse is
     [n_seqs, H_q, n].
     Any strides that keep d contiguous and are multiples of 16 bytes.  Returns out, or (out, lse) with return_lse; rows
-    of no sequence are not written.
+    of no sequence are not written.  No gradient is recorded.  status: int32 tensor of one element that the kernel sets to a
+    nonzero code where a sequence was cut or it gave up.
     """
     if stream is not None:  # its buffers come from the allocator in that stream's order
         _check_stream(stream, _cuda(q, "q"))
@@ -505,7 +506,8 @@ class Kv8Cache:
 
     k_codes, v_codes [n_pages, H_kv, block, d] int8 or float8_e4m3fn; k_scale, v_scale [n_pages, H_kv] float32; k_tail,
     v_tail [n_seqs, H_kv, block, d] float16 or bfloat16; block_table [n_seqs, max_blocks] int32; status: optional int32
-    tensor of one element that kernels set to a nonzero code when a table or length is unusable.
+    tensor of one element that kernels set to a nonzero code when a table or length is unusable, rows were dropped or a block to
+    be quantised is not finite.
     """
 
     def __init__(self, k_codes, v_codes, k_scale, v_scale, k_tail, v_tail, block_table, status=None):
@@ -569,7 +571,8 @@ class Kv8Cache:
     def attn(self, q, lens, max_len=None, scores=None, scores_out=None, softmax_scale=0.0, out=None, return_lse=False, stream=None):
         """Attention of one token per sequence, q [n_seqs, H_q, d], over the first lens[s] tokens of each.  Returns out, or
         (out[, lse][, scores_out]): scores [n_seqs, max_blocks] plus the probability mass of every block, in a new tensor
-        or in scores_out (which may be scores).  max_len: bound of lens (default: what the table can hold)."""
+        or in scores_out (which may be scores).  max_len: bound of lens (default: what the table can hold).  No gradient
+        is recorded."""
         if stream is not None:
             _check_stream(stream, self.device)
             with torch.cuda.stream(stream):

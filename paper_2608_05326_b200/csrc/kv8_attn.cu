@@ -20,7 +20,7 @@
 //
 // Measured: 16 ragged contexts of up to 32768 tokens, 32 / 8 heads of 128, int8 (472 MB): 103 us, of which this kernel 90 us
 // (5.2 TB/s; the copies without arithmetic 82 us), merge and masses the rest; 8 contexts of 65536, 28 / 4 heads, e4m3 (538 MB):
-// 109 us; one of 2048 tokens: 10 us, two dependent launches.  At 6.45 TB/s the bytes alone would take 73, 83 and 0.7 us.
+// 108 us; one of 2048 tokens: 9.2 us, two dependent launches.  At 6.45 TB/s the bytes alone would take 73, 83 and 0.7 us.
 #include <cuda.h>
 
 #include "kv8.cuh"

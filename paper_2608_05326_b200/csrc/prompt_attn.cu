@@ -15,9 +15,11 @@
 //     memory); P is at most 2^8, sums are float32.
 // What bounds it: at d = 128 a key tile costs both query tiles 2048 tensor-core cycles at best; with both operands of S in
 // shared memory the products alone take about 2750 (8 KB of operands for 64 cycles of products, at 128 bytes a cycle, and
-// the copies write through the same port), and a step takes about 3600 with the softmax behind it.  Measured: causal 32768
-// tokens x 32 heads 6.9 to 7.4 ms (1280 to 1190 TFLOP/s, 0.70 to 0.75 of the measured burst rate, 0.84 to 0.91 of the sustained
-// one; the power limit moves it); 12 packed prompts of up to 4001 tokens 506 us (997 TFLOP/s).  Shares of the
+// the copies write through the same port), and a step takes about 3600 with the softmax behind it.  Measured, call after
+// call: causal 32768 tokens x 32 heads 7.97 ms (1103 TFLOP/s, 0.78 of the measured sustained rate; the power limit holds it there:
+// single calls of a cool card take 6.9 to 7.4 ms); 12 packed prompts of up to 4001 tokens 594 us (849 TFLOP/s), the best of graph
+// replays 497 to 512 us; d = 64: 16384 tokens x 32 heads 1.57 ms (702 TFLOP/s: half the products for the same exponentials).
+// Shares of the
 // exponentials as polynomials on the FMA units were slower at every share (1/2 to 1/16): what the softmax waits for is
 // issue and hand-over, not the exponential unit.
 //
@@ -943,7 +945,7 @@ long long prompt_rows(const qevict_prompt_args* p) {
 // An item costs its key tiles and some three more; items go to the SMs as these fall free, so the call takes the work of all
 // items over the SMs and about half an item for the uneven end, at least one item; and every part of the keys writes and reads
 // its rows' results in float32 once more.  (28 heads, a piece of 500 tokens behind 16000 next to one of 166 behind 3714: 237,
-// 174, 190, 157 us with one, two, three, five items for each tile; the model takes five, 151 us with the present merge.)
+// 174, 190, 157 us with one, two, three, five items for each tile; the model takes five, 152 to 169 us with the present merge.)
 int prompt_splits(const qevict_prompt_args* p) {
   int P, T;
   prompt_tile(p, &P, &T);
