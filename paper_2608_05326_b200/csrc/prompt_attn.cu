@@ -379,6 +379,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       // while the item before is in work.  (A grid of single-item CTAs pays for start, first loads and results of every
       // item with idle tensor cores: 12 packed prompts of up to 4001 tokens took 620 us.)
       int x = blockIdx.x, y, z, put = 0, at = 0, before = 0;
+      bool checks = false;  // whoever has position 0 (of its own or taken over) looks at the bounds
       auto item_at = [&] {
 #ifdef QEVICT_DEBUG_BOUNDS  // the checking build has its positions fall
         return item_of(a, (int)gridDim.x - 1 - x, lane, &at, &before);
@@ -393,6 +394,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
           asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
                            smem_u32((void*)words)), "r"(b_next) : "memory");
         }
+        checks = checks || x == 0;
         const PromptItem it = item_at();
         if (it.valid) {
           if (put >= 2) ok = wait_item(b_taken + 8 * (put & 1), (uint32_t)((put >> 1) - 1) & 1u);
@@ -421,6 +423,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         __syncwarp();
         if (!got) break;
         if (!ok) {  // taken over, and nobody else's now
+          checks = checks || x == 0;
           const PromptItem lost = item_at();
           if (lane == 0) items[3] = lost;
           break;
@@ -432,7 +435,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         items[put & 1].valid = 0;
         bar_arrive(b_item + 8 * (put & 1));
       }
-      if (blockIdx.x == 0 && a.status) {
+      if (checks && a.status) {
         for (int s = lane; s < a.n_seqs; s += 32)
           if (span_cut(a.q_bounds, a.padded, s, a.max_q, a.total_q) || span_cut(a.k_bounds, a.padded, s, a.max_k, a.total_k))
             kv8_record(a.status, CHECK_LENGTH);
