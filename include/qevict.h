@@ -462,10 +462,11 @@ typedef struct {
 
 /* Appends tokens: token i of sequence s is row cu_new[s] + i of k, v [total_new, n_kv_heads, d] (strides in elements,
  * multiples of 16 bytes) and becomes token start[s] + i.  cu_new: device int32 [n_seqs + 1], or NULL for one token per
- * sequence (row s).  max_new bounds the tokens of one sequence.  Later ones and those past the table are dropped, a sequence
- * whose rows do not lie in 0 .. total_new - 1 is left as it is; both set *status, as bounds that fall do (a call with
- * max_new or total_new 0 launches nothing).  A sequence with start < 0 is left as it is.  Pages must be in the table for every block the call fills, and no two of those may be the same page (pages
- * that are only read may be shared).  The lengths stay the caller's. */
+ * sequence (row s).  max_new bounds the tokens of one sequence.  Later ones and those past the table are dropped, a
+ * sequence whose rows do not lie in 0 .. total_new - 1 is left as it is; both set *status, as bounds that fall do (a call
+ * with max_new or total_new 0 launches nothing).  A sequence with start < 0 is left as it is.  Pages must be in the table
+ * for every block the call fills, and no two of those may be the same page (pages that are only read may be shared).  The
+ * lengths stay the caller's. */
 QEVICT_API qevict_status qevict_kv8_append(const qevict_kv8_cache* cache, const void* k, const void* v, int64_t token_stride,
                                            int64_t head_stride, int64_t total_new, const int32_t* start,
                                            const int32_t* cu_new, int32_t max_new, void* stream);
