@@ -511,6 +511,107 @@ typedef struct {
 } qevict_kv8_evict_args;
 QEVICT_API qevict_status qevict_kv8_evict(const qevict_kv8_evict_args* args, void* stream);
 
+/* ---- Rotary positions ------------------------------------------------------------------------------------------
+ * Pairs of channels turned by angles that grow with the token's position, on one axis (text) or several (time, height,
+ * width of images and video):
+ *     theta = position[axis[p]] * inv_freq[p],   (x, y) -> scale * (x cos theta - y sin theta, y cos theta + x sin theta)
+ * for the pairs p < n_pairs of every head: channels (p, p + n_pairs), or (2p, 2p + 1) where `interleaved`.  Channels from
+ * 2 * n_pairs on are copied.  Angles are reduced in 64 bits (positions may be any int32), products are float32, rounded
+ * once to the tensors' type.  (The tiered cache's rope_base rounds cosines, sines and products to that type one by one.) */
+typedef struct {
+  uint32_t struct_size;      /* sizeof(qevict_rotation) */
+  int32_t n_pairs;           /* multiple of 4, at most 128 and half of the head dimension */
+  int32_t n_axes;            /* 1 .. 8 */
+  int32_t interleaved;       /* 0 or 1 */
+  double scale;              /* factor of cosines and sines (1 unless a scheme for long contexts has another); magnitude at most 65536 */
+  double inv_freq[128];      /* magnitude at most 16 */
+  uint8_t axis[128];         /* of each pair: 0 .. n_axes - 1 */
+} qevict_rotation;
+
+/* Rotates queries and keys by themselves (for qevict_prompt_attn, say).  Strides in elements: token, head; multiples of
+ * 16 bytes, channels contiguous.  An output may be its input (same strides), else they must not overlap.  inverse: the
+ * transposed rotation (sines negated), which is the gradient of the forward one and, where scale is 1, undoes it. */
+typedef struct {
+  uint32_t struct_size;      /* sizeof(qevict_rope_args) */
+  int32_t device;
+  int32_t dtype;             /* QEVICT_DTYPE_* */
+  int32_t head_dim;          /* multiple of 8, at most 256 */
+  int32_t n_q_heads;
+  int32_t n_k_heads;         /* 0: no keys */
+  int32_t inverse;           /* 0 or 1 */
+  int32_t reserved;          /* 0 */
+  int64_t tokens;
+  const qevict_rotation* rotation; /* host; read before the call returns */
+  const int32_t* positions;  /* device [n_axes][tokens] */
+  int64_t axis_stride;       /* elements from one axis to the next */
+  const void* q;             /* device */
+  void* q_out;
+  const void* k;
+  void* k_out;
+  int64_t q_stride[2];
+  int64_t q_out_stride[2];
+  int64_t k_stride[2];
+  int64_t k_out_stride[2];
+} qevict_rope_args;
+QEVICT_API qevict_status qevict_rope(const qevict_rope_args* args, void* stream);
+
+/* ---- A paged cache in 16 bits ----------------------------------------------------------------------------------
+ * The cache in full precision next to the one in 8 bits: every token stays as it came, so that a sequence can also be cut back (a
+ * draft that was not accepted: give the shorter length to the next call).  All buffers are the caller's; the view below only
+ * points at them, and no call keeps anything.
+ *   - Token t of sequence s is row t % block of page block_table[s][t / block]; a page has `block` rows for every KV head.
+ *   - A page id outside 0 .. n_pages - 1 means that the block is absent: it is neither written nor attended to.  Any such
+ *     id but -1 that a call would use also sets *status.
+ * The calls need no handle; errors leave their text in qevict_last_error(NULL) of the calling thread.  They allocate
+ * nothing, do not synchronise and read lengths and tables on the device, so they can be captured. */
+typedef struct {
+  uint32_t struct_size;      /* sizeof(qevict_kv16_cache) */
+  int32_t device;
+  int32_t dtype;             /* QEVICT_DTYPE_* of the pages and of q, k, v, out */
+  int32_t n_seqs;
+  int32_t n_kv_heads;
+  int32_t head_dim;          /* 64 or 128 */
+  int32_t block;             /* 16, 32, 64 or 128 tokens */
+  int32_t max_blocks;        /* columns of block_table */
+  int32_t n_pages;           /* >= 1 */
+  int32_t reserved;          /* 0 */
+  void* k_pages;             /* device, channels contiguous, 16-byte aligned */
+  void* v_pages;
+  int64_t k_stride[3];       /* elements: page, head, token; multiples of 16 bytes */
+  int64_t v_stride[3];
+  const int32_t* block_table; /* device [n_seqs, max_blocks] */
+  int32_t* status;           /* device int32 or NULL */
+} qevict_kv16_cache;
+
+/* Appends tokens: token i of sequence s is row cu_new[s] + i of k, v and q (total_new rows; strides token, head) and becomes
+ * token start[s] + i of the cache.  cu_new: device int32 [n_seqs + 1], ascending, or NULL for one token per sequence (row
+ * s).  With a rotation the keys are stored rotated and, where q is given, q_out gets the rotated queries (q_out may be q);
+ * positions: device [n_axes][total_new], or NULL for the tokens' places in their sequences on every axis.  Without a rotation
+ * rows are stored (and queries copied) as they are.  Tokens past the table are dropped, a sequence whose rows do not lie
+ * in 0 .. total_new - 1 is left as it is; both set *status, as bounds that fall do.  A sequence with start < 0 is left as it is.
+ * Rows of no sequence are not read into a result, and their rows of q_out are not written.  No two tokens of a call may share
+ * a place. */
+typedef struct {
+  uint32_t struct_size;      /* sizeof(qevict_kv16_append_args) */
+  int32_t n_q_heads;         /* 0: no queries */
+  const qevict_kv16_cache* cache;
+  const qevict_rotation* rotation; /* host, or NULL */
+  int64_t total_new;
+  const int32_t* start;      /* device [n_seqs] */
+  const int32_t* cu_new;     /* device, or NULL */
+  const int32_t* positions;  /* device, or NULL */
+  int64_t axis_stride;
+  const void* k;             /* device */
+  const void* v;
+  const void* q;
+  void* q_out;
+  int64_t k_stride[2];
+  int64_t v_stride[2];
+  int64_t q_stride[2];
+  int64_t q_out_stride[2];
+} qevict_kv16_append_args;
+QEVICT_API qevict_status qevict_kv16_append(const qevict_kv16_append_args* args, void* stream);
+
 /* Tuning: force the number of KV splits per (unit, KV head) of the decode kernel (1..64); 0 restores
  * the built-in choice, which fills the GPU in whole waves.  Results do not depend on it beyond
  * floating-point summation order. */
@@ -542,7 +643,8 @@ QEVICT_API qevict_status qevict_kernel_timeline(qevict_handle h, int32_t max_rec
 QEVICT_API uint64_t qevict_launch_count(qevict_handle h);
 
 /* Text of the last error on this handle (never NULL).  With h == NULL: the calling thread's last failure of
- * qevict_create, qevict_workspace_bytes or one of the calls without a handle (qevict_prompt_*, qevict_kv8_*). */
+ * qevict_create, qevict_workspace_bytes or one of the calls without a handle (qevict_prompt_*, qevict_kv8_*, qevict_rope,
+ * qevict_kv16_*). */
 QEVICT_API const char* qevict_last_error(qevict_handle h);
 QEVICT_API const char* qevict_status_string(qevict_status s);
 /* Library version, "major.minor". */

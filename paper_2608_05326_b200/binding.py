@@ -98,6 +98,34 @@ class qevict_kv8_evict_args(C.Structure):
                                            "n_freed")])
 
 
+class qevict_rotation(C.Structure):
+    _fields_ = ([("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in ("n_pairs", "n_axes", "interleaved")] +
+                [("scale", C.c_double), ("inv_freq", C.c_double * 128), ("axis", C.c_uint8 * 128)])
+
+
+class qevict_rope_args(C.Structure):
+    _fields_ = ([("struct_size", C.c_uint32)] +
+                [(n, C.c_int32) for n in ("device", "dtype", "head_dim", "n_q_heads", "n_k_heads", "inverse", "reserved")] +
+                [("tokens", C.c_int64), ("rotation", C.c_void_p), ("positions", C.c_void_p), ("axis_stride", C.c_int64)] +
+                [(n, C.c_void_p) for n in ("q", "q_out", "k", "k_out")] +
+                [(n, C.c_int64 * 2) for n in ("q_stride", "q_out_stride", "k_stride", "k_out_stride")])
+
+
+class qevict_kv16_cache(C.Structure):
+    _fields_ = ([("struct_size", C.c_uint32)] +
+                [(n, C.c_int32) for n in ("device", "dtype", "n_seqs", "n_kv_heads", "head_dim", "block", "max_blocks", "n_pages",
+                                          "reserved")] +
+                [(n, C.c_void_p) for n in ("k_pages", "v_pages")] + [(n, C.c_int64 * 3) for n in ("k_stride", "v_stride")] +
+                [(n, C.c_void_p) for n in ("block_table", "status")])
+
+
+class qevict_kv16_append_args(C.Structure):
+    _fields_ = ([("struct_size", C.c_uint32), ("n_q_heads", C.c_int32), ("cache", C.c_void_p), ("rotation", C.c_void_p),
+                 ("total_new", C.c_int64)] + [(n, C.c_void_p) for n in ("start", "cu_new", "positions")] + [("axis_stride", C.c_int64)] +
+                [(n, C.c_void_p) for n in ("k", "v", "q", "q_out")] +
+                [(n, C.c_int64 * 2) for n in ("k_stride", "v_stride", "q_stride", "q_out_stride")])
+
+
 _lib = None
 
 _SIGNATURES = {
@@ -145,6 +173,8 @@ _SIGNATURES = {
     "qevict_kv8_attn": (C.c_int, [C.c_void_p, C.c_int32, C.c_float, C.c_void_p, C.c_void_p, C.c_int32,
                                   C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]),
     "qevict_kv8_evict": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "qevict_rope": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "qevict_kv16_append": (C.c_int, [C.c_void_p, C.c_void_p]),
     "qevict_export_q_page": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32] + [C.c_void_p] * 5),
 }
 
@@ -323,7 +353,7 @@ def qevict_kernel_time(h):
     return ms.value, n.value
 
 
-# --- calls without a cache handle: prompt attention, the 8-bit block-scaled cache ---------------------------------
+# --- calls without a cache handle: prompt attention, the 8-bit block-scaled cache, rotary positions, the 16-bit paged cache ---------------------------------
 # These are made once per layer and token, so what they cost on the host counts: argument structures are packed in one go
 # (struct.Struct in place of a ctypes structure filled field by field), a check that passes is one expression, and the
 # stream is read as a raw handle.
@@ -332,7 +362,13 @@ _CODES = {torch.int8: CODE_INT8, torch.float8_e4m3fn: CODE_E4M3}
 _PROMPT_PACK = struct.Struct("@I10if2q7P12qP")
 _KV8_PACK = struct.Struct("@I9i8P")
 _EVICT_PACK = struct.Struct("@I8i9P")
-for _pack, _cls in ((_PROMPT_PACK, qevict_prompt_args), (_KV8_PACK, qevict_kv8_cache), (_EVICT_PACK, qevict_kv8_evict_args)):
+_ROTATION_PACK = struct.Struct("@I3id128d128B")
+_ROPE_PACK = struct.Struct("@I7iq2Pq4P8q")
+_KV16_PACK = struct.Struct("@I9i2P6q2P")
+_APPEND16_PACK = struct.Struct("@Ii2Pq3Pq4P8q")
+for _pack, _cls in ((_PROMPT_PACK, qevict_prompt_args), (_KV8_PACK, qevict_kv8_cache), (_EVICT_PACK, qevict_kv8_evict_args),
+                    (_ROTATION_PACK, qevict_rotation), (_ROPE_PACK, qevict_rope_args), (_KV16_PACK, qevict_kv16_cache),
+                    (_APPEND16_PACK, qevict_kv16_append_args)):
     assert _pack.size == C.sizeof(_cls), _cls
 
 _i32, _f32, _u8 = torch.int32, torch.float32, torch.uint8
@@ -605,6 +641,176 @@ class Kv8Cache:
         if lse is None:
             return out if scores_out is None else (out, scores_out)
         return (out, lse) if scores_out is None else (out, lse, scores_out)
+
+
+class Rotation:
+    """Rotary positions of a model, laid out once: the frequency and the axis of every pair of channels.
+
+    inv_freq: one number per pair, of any sequence or tensor (read here); axes: the axis of every pair (default: one axis);
+    interleaved: pairs are (2p, 2p + 1), else (p, p + number of pairs); scale: factor of cosines and sines.
+    """
+
+    def __init__(self, inv_freq, axes=None, interleaved=False, scale=1.0):
+        try:
+            freq = [float(x) for x in inv_freq]
+            axis = [0] * len(freq) if axes is None else [operator.index(x) for x in axes]
+            scale = float(scale)
+        except (TypeError, ValueError) as e:
+            _refuse("inv_freq and axes must hold one number per pair (%s)" % e)
+        n = len(freq)
+        if len(axis) != n or not 0 < n <= 128:
+            _refuse("inv_freq and axes must hold one number for each of 1 to 128 pairs")
+        if not 0 <= min(axis) <= max(axis) < 8:
+            _refuse("axes must be 0 to 7")
+        self.n_pairs, self.n_axes, self.interleaved, self.scale = n, max(axis) + 1, bool(interleaved), scale
+        fill = [0] * (128 - n)
+        self._packed = C.create_string_buffer(_ROTATION_PACK.pack(C.sizeof(qevict_rotation), n, self.n_axes, self.interleaved, scale,
+                                                                  *freq, *fill, *axis, *fill))
+        self._address = C.addressof(self._packed)
+
+    @classmethod
+    def standard(cls, rotary_dim, base=10000.0, sections=None, interleaved=False, scale=1.0):
+        """Frequencies base^(-2p / rotary_dim); sections: how many pairs in a row belong to each axis (they add up to
+        rotary_dim / 2)."""
+        n = rotary_dim // 2
+        axes = None if sections is None else [a for a, m in enumerate(sections) for _ in range(m)]
+        if rotary_dim % 2 or (axes is not None and len(axes) != n):
+            _refuse("rotary_dim must be even and sections must add up to half of it")
+        return cls([float(base) ** (-2.0 * p / rotary_dim) for p in range(n)], axes, interleaved, scale)
+
+
+def _positions(positions, rotation, tokens, dev):
+    """Address and axis stride of positions, [tokens] or [n_axes, tokens] int32."""
+    if not isinstance(positions, torch.Tensor) or positions.dtype is not _i32 or positions.device != dev:
+        _refuse("positions must be an int32 tensor on %s" % dev)
+    shape, st, axes = positions.shape, positions.stride(), rotation.n_axes
+    if not (shape == (axes, tokens) or (axes == 1 and shape == (tokens,))) or (tokens > 1 and st[-1] != 1):
+        _refuse("positions must be [%d, %d], tokens contiguous" % (axes, tokens))
+    return positions.data_ptr(), st[0] if len(shape) == 2 else 0
+
+
+def _rows_like(t, name, dev, dtype, shape):
+    """Address and strides of rows [tokens, heads, d] of any strides that keep d contiguous."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.device != dev or len(t.shape) != 3 or \
+            any(want is not None and want != got for want, got in zip(shape, t.shape)) or t.stride(2) != 1:
+        _refuse("%s must be [tokens, heads, d] = %s %s on %s, d contiguous" % (name, tuple("any" if x is None else x for x in shape), dtype, dev))
+    st = t.stride()
+    return t.data_ptr(), st[:2]
+
+
+def qevict_rope(q, positions, rotation, k=None, out=None, k_out=None, inverse=False, stream=None):
+    """Rotates q [tokens, H, d] (and k [tokens, H_k, d]) to their positions, int32 [tokens] or [n_axes, tokens].  Returns out, or
+    (out, k_out) with k; either may be its input.  inverse: the transposed rotation -- the gradient of the forward one.  Any
+    strides that keep d contiguous and are multiples of 16 bytes.  No gradient is recorded."""
+    if stream is not None:
+        _check_stream(stream, _cuda(q, "q"))
+        with torch.cuda.stream(stream):
+            return qevict_rope(q, positions, rotation, k, out, k_out, inverse)
+    dev, dtype = _cuda(q, "q"), q.dtype
+    if dtype not in _DTYPES:
+        _refuse("q must be float16 or bfloat16")
+    if not isinstance(rotation, Rotation):
+        _refuse("rotation must be a Rotation")
+    p_q, s_q = _rows_like(q, "q", dev, dtype, (None, None, None))
+    n, hq, d = q.shape
+    p_pos, axis_stride = _positions(positions, rotation, n, dev)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    p_out, s_out = _rows_like(out, "out", dev, dtype, q.shape)
+    hk, p_k, s_k, p_ko, s_ko = 0, 0, (0, 0), 0, (0, 0)
+    if k is not None:
+        p_k, s_k = _rows_like(k, "k", dev, dtype, (n, None, d))
+        hk = k.shape[1]
+        if k_out is None:
+            k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+        p_ko, s_ko = _rows_like(k_out, "k_out", dev, dtype, k.shape)
+    elif k_out is not None:
+        _refuse("k_out without k")
+    args = _ROPE_PACK.pack(C.sizeof(qevict_rope_args), dev.index, _DTYPES[dtype], d, hq, hk, bool(inverse), 0, n, rotation._address, p_pos,
+                           axis_stride, p_q, p_out, p_k, p_ko, *s_q, *s_out, *s_k, *s_ko)
+    _check(lib().qevict_rope(args, _current_stream(dev)))
+    return out if k is None else (out, k_out)
+
+
+class Kv16Cache:
+    """View of a paged cache in 16 bits; the tensors stay the caller's.
+
+    k_pages, v_pages [n_pages, H_kv, block, d] float16 or bfloat16, of any strides (multiples of 16 bytes) that keep d contiguous;
+    block_table [n_seqs, max_blocks] int32; status: optional int32 tensor of one element that kernels set to a nonzero code
+    when a table or length is unusable or rows were dropped.
+    """
+
+    def __init__(self, k_pages, v_pages, block_table, status=None):
+        dev, dtype, shape, grid = _cuda(k_pages, "k_pages"), k_pages.dtype, k_pages.shape, block_table.shape
+        if dtype not in _DTYPES or len(shape) != 4 or len(grid) != 2:
+            _refuse("k_pages must be [n_pages, H_kv, block, d] float16 or bfloat16 and block_table [n_seqs, max_blocks]")
+        if v_pages.shape != shape or v_pages.dtype is not dtype or v_pages.device != dev or k_pages.stride(3) != 1 or v_pages.stride(3) != 1:
+            _refuse("k_pages and v_pages must have the same shape, type and device, the last dimension contiguous")
+        n_pages, h_kv, block, d = shape
+        n, mb = grid
+        self.device, self.dtype, self.n_seqs, self.max_blocks, self.block = dev, dtype, n, mb, block
+        self.n_pages, self.n_kv_heads, self.head_dim = n_pages, h_kv, d
+        self._view = C.create_string_buffer(_KV16_PACK.pack(
+            C.sizeof(qevict_kv16_cache), dev.index, _DTYPES[dtype], n, h_kv, d, block, mb, n_pages, 0, k_pages.data_ptr(), v_pages.data_ptr(),
+            *k_pages.stride()[:3], *v_pages.stride()[:3], _want(block_table, "block_table", dev, _i32),
+            0 if status is None else _want(status, "status", dev, _i32, (1,))))
+        self._address = C.addressof(self._view)
+        self._tensors = (k_pages, v_pages, block_table, status)
+
+    @classmethod
+    def allocate(cls, n_pages, n_seqs, max_blocks, n_kv_heads, head_dim, block, dtype=torch.bfloat16, device="cuda"):
+        """A cache with buffers of its own (an empty table; status word included): attributes k_pages, v_pages, block_table,
+        status."""
+        dev = torch.device(device)
+        if dev.index is None:
+            dev = torch.device(dev.type, torch.cuda.current_device())
+        shape = (n_pages, n_kv_heads, block, head_dim)
+        t = {"k_pages": torch.zeros(shape, dtype=dtype, device=dev), "v_pages": torch.zeros(shape, dtype=dtype, device=dev),
+             "block_table": torch.full((n_seqs, max_blocks), -1, dtype=_i32, device=dev),
+             "status": torch.zeros(1, dtype=_i32, device=dev)}
+        cache = cls(**t)
+        for name, x in t.items():
+            setattr(cache, name, x)
+        return cache
+
+    def append(self, k, v, start, cu_new=None, rotation=None, positions=None, q=None, q_out=None, stream=None):
+        """k, v [total, H_kv, d] (any strides that keep d contiguous): token i of sequence s is row cu_new[s] + i (without cu_new:
+        one token each, row s) and becomes token start[s] + i.  start < 0: the sequence is left as it is.  rotation: keys are
+        stored rotated; positions int32 [total] or [n_axes, total] (default: the tokens' places in their sequences).  q [total,
+        H_q, d]: rotated beside them into q_out (default: a new tensor; may be q), which is returned; its rows of no sequence
+        are not written."""
+        if stream is not None:
+            _check_stream(stream, self.device)
+            with torch.cuda.stream(stream):
+                return self.append(k, v, start, cu_new, rotation, positions, q, q_out)
+        n, dev, dtype, d = self.n_seqs, self.device, self.dtype, self.head_dim
+        p_k, s_k = _rows_like(k, "k", dev, dtype, (None, self.n_kv_heads, d))
+        total = k.shape[0]
+        p_v, s_v = _rows_like(v, "v", dev, dtype, (total, self.n_kv_heads, d))
+        p_start = _want(start, "start", dev, _i32, (n,))
+        p_cu = 0 if cu_new is None else _want(cu_new, "cu_new", dev, _i32, (n + 1,))
+        p_rot = p_pos = axis_stride = 0
+        if rotation is not None:
+            if not isinstance(rotation, Rotation):
+                _refuse("rotation must be a Rotation")
+            p_rot = rotation._address
+            if positions is not None:
+                p_pos, axis_stride = _positions(positions, rotation, total, dev)
+        elif positions is not None:
+            _refuse("positions without a rotation")
+        hq, p_q, s_q, p_qo, s_qo = 0, 0, (0, 0), 0, (0, 0)
+        if q is not None:
+            p_q, s_q = _rows_like(q, "q", dev, dtype, (total, None, d))
+            hq = q.shape[1]
+            if q_out is None:
+                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            p_qo, s_qo = _rows_like(q_out, "q_out", dev, dtype, q.shape)
+        elif q_out is not None:
+            _refuse("q_out without q")
+        args = _APPEND16_PACK.pack(C.sizeof(qevict_kv16_append_args), hq, self._address, p_rot, total, p_start, p_cu, p_pos, axis_stride,
+                                   p_k, p_v, p_q, p_qo, *s_k, *s_v, *s_q, *s_qo)
+        _check(lib().qevict_kv16_append(args, _current_stream(dev)))
+        return q_out
 
 
 KERNEL_NAMES = ("append", "decode_attn", "combine", "route", "migrate")
