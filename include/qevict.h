@@ -612,6 +612,35 @@ typedef struct {
 } qevict_kv16_append_args;
 QEVICT_API qevict_status qevict_kv16_append(const qevict_kv16_append_args* args, void* stream);
 
+/* Attention of the new tokens of every sequence, one or thousands, over the cache (lens[s] tokens, the new ones among them):
+ *     out[i, h] = sum_j softmax_j(scale * q[i, h] . k[j, h / G]) v[j, h / G],   lse[h, i] = ln sum_j exp(...)
+ * over the tokens j that are there and, with `causal`, j <= i + lens[s] - n_q[s] (the queries are the last n_q of lens tokens).
+ * A query that sees no token gets out = 0 and lse = -infinity.  q, out: [total_q] rows of n_q_heads heads (strides token, head),
+ * sequence s has rows cu_q[s] .. cu_q[s + 1] - 1 (device int32, ascending), or row s without cu_q; rows of no sequence are
+ * not written.  lse [n_q_heads, total_q].  max_q and max_len bound the lengths and size the launch; a sequence with more
+ * new tokens is cut to the first max_q, one with lens beyond max_len or the table to the smaller of them, rows outside 0 ..
+ * total_q - 1 are left out, bounds that fall are empty, and each sets *status, as a length < 0 does.  A key or value that is not
+ * finite spreads to every row of its sequence from 255 tokens before it on.  scratch: device, from
+ * qevict_kv16_attn_scratch_bytes for the same arguments; calls that may run at the same time need scratch of their own. */
+typedef struct {
+  uint32_t struct_size;      /* sizeof(qevict_kv16_attn_args) */
+  int32_t n_q_heads;         /* multiple of n_kv_heads */
+  int32_t max_q, max_len;
+  int32_t causal;            /* 0 or 1 */
+  float softmax_scale;       /* 0 => 1/sqrt(d); else 1e-30 .. 2e38 */
+  int64_t total_q;
+  const qevict_kv16_cache* cache;
+  const int32_t* lens;       /* device [n_seqs] */
+  const int32_t* cu_q;       /* device [n_seqs + 1], or NULL */
+  const void* q;             /* device */
+  void* out;
+  float* lse;                /* device, or NULL */
+  int64_t q_stride[2];
+  int64_t out_stride[2];
+} qevict_kv16_attn_args;
+QEVICT_API qevict_status qevict_kv16_attn_scratch_bytes(const qevict_kv16_attn_args* args, uint64_t* bytes);
+QEVICT_API qevict_status qevict_kv16_attn(const qevict_kv16_attn_args* args, void* scratch, uint64_t scratch_bytes, void* stream);
+
 /* Tuning: force the number of KV splits per (unit, KV head) of the decode kernel (1..64); 0 restores
  * the built-in choice, which fills the GPU in whole waves.  Results do not depend on it beyond
  * floating-point summation order. */

@@ -3,9 +3,15 @@
 import numpy as np
 
 
-def attention(q, k, v, causal=True, scale=None):
+def _visible(nq, nk, places, n_tokens):
+    """Key j is token places[j] of n_tokens, the queries are the last nq of them."""
+    places = np.arange(nk) if places is None else np.asarray(places)
+    return places[None] <= np.arange(nq)[:, None] + (nk if n_tokens is None else n_tokens) - nq
+
+
+def attention(q, k, v, causal=True, scale=None, places=None, n_tokens=None):
     """q [nq, Hq, d], k, v [nk, Hkv, d] -> out [nq, Hq, d], lse [Hq, nq], spread [nq, Hq, d] (probability-weighted |v|),
-    reach (largest scale * sum |q_c| |k_c|)."""
+    reach (largest scale * sum |q_c| |k_c|).  places, n_tokens: the keys are these tokens of n_tokens (default: all)."""
     q, k, v = (np.asarray(x, np.float64) for x in (q, k, v))
     nq, hq, d = q.shape
     nk, hkv = k.shape[0], k.shape[1]
@@ -20,7 +26,7 @@ def attention(q, k, v, causal=True, scale=None):
         x = scale * (q[:, h] @ k[:, g].T)
         reach = max(reach, float(scale * np.max(np.abs(q[:, h]) @ np.abs(k[:, g]).T)))
         if causal:
-            x = np.where(np.arange(nk)[None] <= np.arange(nq)[:, None] + nk - nq, x, -np.inf)
+            x = np.where(_visible(nq, nk, places, n_tokens), x, -np.inf)
         m = x.max(axis=1)
         ok = np.isfinite(m)
         p = np.exp(x - np.where(ok, m, 0.0)[:, None])

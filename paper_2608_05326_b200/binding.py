@@ -126,6 +126,13 @@ class qevict_kv16_append_args(C.Structure):
                 [(n, C.c_int64 * 2) for n in ("k_stride", "v_stride", "q_stride", "q_out_stride")])
 
 
+class qevict_kv16_attn_args(C.Structure):
+    _fields_ = ([("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in ("n_q_heads", "max_q", "max_len", "causal")] +
+                [("softmax_scale", C.c_float), ("total_q", C.c_int64)] +
+                [(n, C.c_void_p) for n in ("cache", "lens", "cu_q", "q", "out", "lse")] +
+                [(n, C.c_int64 * 2) for n in ("q_stride", "out_stride")])
+
+
 _lib = None
 
 _SIGNATURES = {
@@ -175,6 +182,8 @@ _SIGNATURES = {
     "qevict_kv8_evict": (C.c_int, [C.c_void_p, C.c_void_p]),
     "qevict_rope": (C.c_int, [C.c_void_p, C.c_void_p]),
     "qevict_kv16_append": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "qevict_kv16_attn_scratch_bytes": (C.c_int, [C.c_void_p, C.POINTER(C.c_uint64)]),
+    "qevict_kv16_attn": (C.c_int, [C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]),
     "qevict_export_q_page": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32] + [C.c_void_p] * 5),
 }
 
@@ -366,9 +375,10 @@ _ROTATION_PACK = struct.Struct("@I3id128d128B")
 _ROPE_PACK = struct.Struct("@I7iq2Pq4P8q")
 _KV16_PACK = struct.Struct("@I9i2P6q2P")
 _APPEND16_PACK = struct.Struct("@Ii2Pq3Pq4P8q")
+_ATTN16_PACK = struct.Struct("@I4ifq6P4q")
 for _pack, _cls in ((_PROMPT_PACK, qevict_prompt_args), (_KV8_PACK, qevict_kv8_cache), (_EVICT_PACK, qevict_kv8_evict_args),
                     (_ROTATION_PACK, qevict_rotation), (_ROPE_PACK, qevict_rope_args), (_KV16_PACK, qevict_kv16_cache),
-                    (_APPEND16_PACK, qevict_kv16_append_args)):
+                    (_APPEND16_PACK, qevict_kv16_append_args), (_ATTN16_PACK, qevict_kv16_attn_args)):
     assert _pack.size == C.sizeof(_cls), _cls
 
 _i32, _f32, _u8 = torch.int32, torch.float32, torch.uint8
@@ -811,6 +821,40 @@ class Kv16Cache:
                                    p_k, p_v, p_q, p_qo, *s_k, *s_v, *s_q, *s_qo)
         _check(lib().qevict_kv16_append(args, _current_stream(dev)))
         return q_out
+
+    def attn(self, q, lens, cu_q=None, max_q=None, max_len=None, causal=True, softmax_scale=0.0, out=None, return_lse=False, stream=None):
+        """Attention of the new tokens of every sequence over the cache, which holds lens[s] tokens of it, the new ones among them:
+        q [total, H_q, d] (any strides that keep d contiguous), rows cu_q[s] .. cu_q[s + 1] - 1 (without cu_q: one token each,
+        row s), the last of the lens[s] tokens; causal: each sees the tokens up to itself.  Returns out, or (out, lse [H_q,
+        total]); rows of no sequence are not written.  max_q, max_len: bounds of a sequence's new tokens and of lens, which size
+        the launch (default: all rows, what the table can hold).  No gradient is recorded."""
+        if stream is not None:
+            _check_stream(stream, self.device)
+            with torch.cuda.stream(stream):
+                return self.attn(q, lens, cu_q, max_q, max_len, causal, softmax_scale, out, return_lse)
+        n, dev, dtype = self.n_seqs, self.device, self.dtype
+        p_q, s_q = _rows_like(q, "q", dev, dtype, (None, None, self.head_dim))
+        total, hq = q.shape[0], q.shape[1]
+        p_lens = _want(lens, "lens", dev, _i32, (n,))
+        p_cu = 0 if cu_q is None else _want(cu_q, "cu_q", dev, _i32, (n + 1,))
+        if max_q is None:
+            max_q = total if p_cu else 1
+        if max_len is None:
+            max_len = self.max_blocks * self.block
+        if out is None:
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        p_out, s_out = _rows_like(out, "out", dev, dtype, q.shape)
+        lse = q.new_empty((hq, total), dtype=_f32) if return_lse else None
+        try:
+            args = _ATTN16_PACK.pack(C.sizeof(qevict_kv16_attn_args), hq, max_q, max_len, bool(causal), softmax_scale, total, self._address, p_lens,
+                                     p_cu, p_q, p_out, 0 if lse is None else lse.data_ptr(), *s_q, *s_out)
+        except (struct.error, OverflowError) as e:
+            _refuse("an argument does not fit its field (%s)" % e)
+        need, library = C.c_uint64(), lib()
+        _check(library.qevict_kv16_attn_scratch_bytes(args, C.byref(need)))
+        scratch = None if need.value == 0 else q.new_empty(need.value, dtype=_u8)
+        _check(library.qevict_kv16_attn(args, None if scratch is None else scratch.data_ptr(), need.value, _current_stream(dev)))
+        return (out, lse) if return_lse else out
 
 
 KERNEL_NAMES = ("append", "decode_attn", "combine", "route", "migrate")

@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 import torch
 
-from oracle import rotary as oracle
+from oracle import prompt, rotary as oracle
 from paper_2608_05326_b200 import binding
 
 HALF_STEP = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
@@ -319,3 +319,121 @@ def test_views_and_appends_of_the_binding_refuse_what_the_library_cannot_see():
                 lambda: cache.append(k[..., :32], k[..., :32], start)):
         with pytest.raises(binding.QEvictError):
             bad()
+
+
+# ---- attention -------------------------------------------------------------------------------------------------
+def _attn_args(view, **over):
+    a = binding.qevict_kv16_attn_args()
+    values = dict(struct_size=C.sizeof(a), n_q_heads=4, max_q=1, max_len=64, causal=1, softmax_scale=0.0, total_q=2, cache=C.addressof(view), lens=4096,
+                  q=4096, out=8192, q_stride=(256, 64), out_stride=(256, 64))
+    values.update(over)
+    return _fill(a, values)
+
+
+@pytest.mark.parametrize("over,status,word", VIEWS)
+def test_attention_refuses_unusable_views(over, status, word):
+    view, need = _view(**over), C.c_uint64()
+    _refused(binding.lib().qevict_kv16_attn(C.byref(_attn_args(view)), None, 0, None), status, word)
+    _refused(binding.lib().qevict_kv16_attn_scratch_bytes(C.byref(_attn_args(view)), C.byref(need)), status, word)
+
+
+@pytest.mark.parametrize("over,status,word", [
+    (dict(struct_size=8), 1, "struct_size"), (dict(cache=None), 1, "cache is NULL"), (dict(causal=2), 1, "causal"), (dict(max_q=-1), 1, "sizes"), (dict(max_len=-1), 1, "sizes"),
+    (dict(total_q=-1), 1, "sizes"), (dict(n_q_heads=3), 1, "multiple"), (dict(n_q_heads=0), 1, "multiple"), (dict(softmax_scale=-1.0), 1, "softmax_scale"),
+    (dict(softmax_scale=float("nan")), 1, "softmax_scale"), (dict(softmax_scale=3e38), 1, "softmax_scale"), (dict(max_q=2), 1, "without cu_q"), (dict(total_q=1), 1, "without cu_q"),
+    (dict(n_q_heads=2048), 4, "heads"), (dict(total_q=2 ** 31), 4, "tokens"), (dict(q=None), 1, "NULL"), (dict(out=None), 1, "NULL"), (dict(lens=None), 1, "NULL"),
+    (dict(q=4104), 1, "aligned"), (dict(lse=4098), 1, "aligned"), (dict(cu_q=4098), 1, "aligned"), (dict(q_stride=(250, 64)), 1, "strides"), (dict(out_stride=(256, 0)), 1, "strides"),
+])
+def test_attention_refuses_unusable_arguments(over, status, word):
+    view = _view()
+    _refused(binding.lib().qevict_kv16_attn(C.byref(_attn_args(view, **over)), None, 0, None), status, word)
+
+
+def test_attention_scratch_and_nothing_to_do():
+    lib, need, view = binding.lib(), C.c_uint64(1), _view(max_blocks=4096)
+    for over in (dict(total_q=0, cu_q=4096), dict(max_q=0)):
+        assert lib.qevict_kv16_attn(C.byref(_attn_args(view, **over)), None, 0, None) == 0
+    assert lib.qevict_kv16_attn(C.byref(_attn_args(_view(n_seqs=0, block_table=None))), None, 0, None) == 0
+    binding._check(lib.qevict_kv16_attn_scratch_bytes(C.byref(_attn_args(view, max_len=128)), C.byref(need)))
+    assert need.value == 0  # one tile of keys has no parts
+    long = _attn_args(view, max_len=65536)
+    binding._check(lib.qevict_kv16_attn_scratch_bytes(C.byref(long), C.byref(need)))
+    assert need.value > 0
+    assert lib.qevict_kv16_attn(C.byref(long), None, 0, None) == 3 and b"scratch" in lib.qevict_last_error(None)
+    assert lib.qevict_kv16_attn(C.byref(long), 4104, need.value, None) == 1 and b"aligned" in lib.qevict_last_error(None)
+    assert lib.qevict_kv16_attn_scratch_bytes(C.byref(long), None) == 1
+
+
+def _poison(pools, table, lens, block):
+    """Not-a-number wherever no token is: behind the lengths, in pages of nobody."""
+    pages = oracle.Pages([np.zeros((pools[0].shape[0], 1, block, 1))] * 2, table)
+    used = np.zeros((pools[0].shape[0], block), bool)
+    for s, n in enumerate(lens):
+        for b in range(-(-n // block)):
+            at = pages.place(s, b * block)
+            if at is not None:
+                used[at[0], :min(block, n - b * block)] = True
+    hide = torch.tensor(~used, device="cuda")[:, None, :, None]
+    for w, x in enumerate(pools):
+        x.masked_fill_(hide, float("nan") if w else float("inf"))
+
+
+def _check_seq(out, lse, q, k, v, n, places, causal, dtype, what, scale=None):
+    """out [nq, Hq, d], lse [Hq, nq] of one sequence of n tokens, of which `places` are there."""
+    ro, rl, spread, reach = prompt.attention(_np(q), k, v, causal, scale, places, n)
+    vmax = float(np.abs(v).max()) if v.size else 0.0
+    u = HALF_STEP[dtype]
+    tol = prompt.out_tolerance(ro, spread, vmax, k.shape[0], q.shape[-1], reach, u, u)
+    err = np.abs(_np(out) - ro)
+    assert (err <= tol).all(), (what, float((err / tol).max()), float(err.max()))
+    got, ok = _np(lse), np.isfinite(rl)
+    assert (np.isneginf(got) == np.isneginf(rl)).all(), what
+    assert (np.abs(got[ok] - rl[ok]) <= prompt.lse_tolerance(rl[ok], q.shape[-1], reach)).all(), what
+
+
+def _check_attn(out, lse, q, pools, table, lens, nq, causal, dtype, q_first=0, scale=None, only=None):
+    # (the pages as stored: what no token uses is not looked at)
+    pages, at = oracle.Pages([_np(x) for x in pools], table), q_first
+    for s, (m, n) in enumerate(zip(nq, lens)):
+        if only is None or s in only:
+            k, v, places = pages.rows(s, n)
+            _check_seq(out[at:at + m], lse[:, at:at + m], q[at:at + m], k, v, n, places, causal, dtype, "sequence %d (%d of %d)" % (s, m, n), scale)
+        at += m
+
+
+def _case(nq, lens, hq, hkv, d, block, dtype, seed, by_token=False, gain=1.0, extra=2, mb=None):
+    cache, pools, table, status = _cache(lens, hkv, d, block, dtype, seed, extra=extra, by_token=by_token)
+    if mb is not None:  # a wider table, with page ids behind the lengths that nothing may use
+        wide = torch.full((len(lens), mb), 1 << 30, dtype=torch.int32)
+        for s, n in enumerate(lens):
+            m = -(-n // block)
+            wide[s, :m] = torch.tensor(table[s, :m])
+        cache, table = binding.Kv16Cache(pools[0], pools[1], wide.cuda(), status), wide.numpy()
+    _poison(pools, table, lens, block)
+    return cache, pools, table, status, (_rows(sum(nq), hq, d, dtype, seed + 1) * gain).to(dtype)
+
+
+LENS = [
+    ([1], [1]), ([1], [128]), ([1], [129]), ([5], [5]), ([77], [77]), ([1], [300]), ([4], [1000]), ([33], [257]), ([300], [300]), ([129], [700]), ([260], [1500]),
+    ([5, 0, 130, 1, 255], [5, 64, 130, 0, 600]), ([1, 1, 1], [1, 640, 129]), ([3, 200], [131, 456]), ([130, 4], [2, 3]), ([3, 2], [0, 2]),
+]
+LAYOUTS = [
+    (torch.bfloat16, 32, 8, 128, 64, False), (torch.float16, 7, 1, 64, 16, True), (torch.bfloat16, 2, 2, 64, 128, False), (torch.float16, 28, 4, 128, 32, True),
+    (torch.bfloat16, 16, 1, 128, 16, False),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nq,lens", LENS)
+@pytest.mark.parametrize("dtype,hq,hkv,d,block,by_token", LAYOUTS)
+def test_attention_of_new_tokens(nq, lens, dtype, hq, hkv, d, block, by_token):
+    cache, pools, table, status, q = _case(nq, lens, hq, hkv, d, block, dtype, 40 + len(nq), by_token, mb=-(-max(lens) // block) + 3)
+    for causal in (True, False):
+        out, lse = cache.attn(q, _i32(lens), _cu(nq), max_q=max(nq), max_len=max(max(lens), 1), causal=causal, return_lse=True)
+        _check_attn(out, lse, q, pools, table, lens, nq, causal, dtype)
+        out, lse = cache.attn(q, _i32(lens), _cu(nq), causal=causal, return_lse=True)  # bounds from the shapes
+        _check_attn(out, lse, q, pools, table, lens, nq, causal, dtype)
+        if all(m == 1 for m in nq):
+            one, lse1 = cache.attn(q, _i32(lens), max_len=max(lens), causal=causal, return_lse=True)
+            _check_attn(one, lse1, q, pools, table, lens, nq, causal, dtype)
+    assert int(status) == 0
