@@ -9,14 +9,12 @@ namespace qevict {
 namespace {
 
 struct Plan {
-  int P, T;           // rows of a query tile: heads, tokens
-  int per_part;       // key tiles of a part
-  int pieces;         // parts of the longest sequence
-  bool pairs;         // whether there can be sequences with few queries and more than one key tile
-  bool compact;
-  long long pair_rows, rows;  // of the partial results
-  long long positions;        // of the grid
-  size_t o_bytes, bytes;
+  int P, T;       // rows of a query tile: heads, tokens
+  bool by_range;  // equal ranges, else whole items
+  bool cuts;      // an item may be shared
+  int slot_rows;
+  unsigned ctas;
+  size_t cut_bytes, o_bytes, bytes;
 };
 
 const char* attn_check(const qevict_kv16_attn_args* p, Kv16View* view, qevict_status* st) {
@@ -37,10 +35,8 @@ const char* attn_check(const qevict_kv16_attn_args* p, Kv16View* view, qevict_st
   return nullptr;
 }
 
-// Parts of the keys: the number that makes the call shortest by a model in steps (two tiles' products, about 2 us).  An item
-// costs its steps and some three more; items go to the SMs as these fall free, so the call takes the work of all items over the
-// SMs and about half an item for the uneven end, at least one item; and every part of the keys writes and reads its rows'
-// results in float32 once more.
+// Equal ranges of the work for all SMs; a call of many items (six for each SM, by its rows) hands out whole ones as SMs fall free,
+// longest first: CTAs that work on one head then walk its keys together, and the L2 serves most of them.
 Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
   Plan l = {};
   prompt_tile(p->n_q_heads / c.Hkv, &l.P, &l.T);
@@ -48,32 +44,44 @@ Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
   if (p->max_len < longest) longest = p->max_len;
   const long long max_q = p->max_q < p->total_q ? p->max_q : p->total_q;
   const long long rows = p->cu_q ? p->total_q : (p->total_q < c.n_seqs ? p->total_q : c.n_seqs);
-  const long long keys = (longest + TILE - 1) / TILE, groups = p->n_q_heads / l.P;
-  const long long tiles = prompt_tiles(false, c.n_seqs, max_q, rows, l.T) * groups;
-  const bool few = max_q <= l.T;  // every sequence has one tile of rows: a step takes two key tiles
-  l.pairs = keys > 1;
-  const double steps = few ? (keys + 1) / 2 : keys, sms = prompt_sms(p->cache->device);
-  const double merge = (double)rows * p->n_q_heads * c.D * 8.0 / 8e6 / 2.0;
-  double least = 0.0;
-  long long best = 1;
-  for (int s = 1; s <= 32 && (s == 1 || steps / s >= (few ? 1.0 : 4.0)); ++s) {
-    const double item = steps / s + 3.0, spread = tiles * s * item / sms + item / 2;
-    const double cost = (spread > item ? spread : item) + (s > 1 ? merge * s + 4.0 : 0.0);
-    if (s == 1 || cost < least) {
-      least = cost;
-      best = s;
-    }
+  const long long groups = p->n_q_heads / l.P, items = prompt_tiles(false, c.n_seqs, max_q, rows, l.T) * groups;
+  const int sms = prompt_sms(p->cache->device);
+  l.by_range = rows / (2 * l.T) * groups < 6 * sms;
+  if (!l.by_range) {
+    l.ctas = items <= (1ll << 28) ? (unsigned)items : 0u;
+    return l;
   }
-  l.per_part = (int)(keys > 0 ? (keys + best - 1) / best : 1);
-  l.pieces = (int)(keys > 0 ? (keys + l.per_part - 1) / l.per_part : 1);
-  l.rows = l.pieces > 1 && !few ? rows : 0;
-  l.compact = (long long)c.n_seqs * l.T < rows;
-  l.pair_rows = !l.pairs ? 0 : l.compact ? (long long)c.n_seqs * l.T : rows;
-  l.positions = tiles * l.pieces;
-  const long long partial = 2 * l.pieces * l.pair_rows + l.pieces * l.rows;
-  l.o_bytes = ((size_t)partial * p->n_q_heads * c.D * sizeof(float) + 255) & ~(size_t)255;
-  l.bytes = partial ? l.o_bytes + (size_t)partial * p->n_q_heads * sizeof(float) : 0;
+  const long long most = items * (KEY_COST * longest + ITEM_COST) / RANGE_LEAST + 1;
+  l.ctas = (unsigned)(most < sms ? most : sms);
+  l.cuts = longest > TILE && l.ctas > 1;
+  if (!l.cuts) return l;
+  l.slot_rows = max_q <= l.T ? TILE : 2 * TILE;
+  const size_t slots = 2 * (size_t)l.ctas * l.slot_rows;
+  l.cut_bytes = ((size_t)l.ctas * sizeof(PagedCut) + 255) & ~(size_t)255;
+  l.o_bytes = slots * c.D * sizeof(float);
+  l.bytes = l.cut_bytes + l.o_bytes + slots * sizeof(float);
   return l;
+}
+
+// A page's rows of a head by one copy of {64 channels, 8 tokens, d / 64 pieces, block / 8 groups}, which lands group by group with
+// a group's pieces side by side; heads are reached in pieces too.  Where a head's stride is no number of pieces, by a
+// copy for each 64 channels, which lands group by group.
+bool whole_pages(const qevict_kv16_cache* c) {
+  return c->n_kv_heads == 1 || (c->k_stride[1] % 64 == 0 && c->v_stride[1] % 64 == 0);
+}
+bool make_page_map(CUtensorMap* map, const qevict_kv16_cache* c, const void* base, const int64_t* stride, bool whole, int* head_step) {
+  const cuuint64_t d = c->head_dim, heads = c->n_kv_heads;
+  const int64_t head = heads > 1 ? stride[1] : (int64_t)d;
+  *head_step = whole ? (int)(head / 64) : 1;
+  if (head / 64 > 0x7fffffff / c->n_kv_heads) return false;
+  const cuuint64_t dims[5] = {whole ? 64 : d, 8, whole ? (heads - 1) * (head / 64) + d / 64 : heads, (cuuint64_t)c->block / 8, (cuuint64_t)c->n_pages};
+  const cuuint64_t st[4] = {(cuuint64_t)stride[2] * 2, (cuuint64_t)(whole ? 64 : head) * 2, (cuuint64_t)stride[2] * 16,
+                            (cuuint64_t)(c->n_pages > 1 ? stride[0] : (int64_t)d) * 2};
+  const cuuint32_t box[5] = {64, 8, whole ? (cuuint32_t)d / 64 : 1, (cuuint32_t)c->block / 8, 1}, el[5] = {1, 1, 1, 1, 1};
+  EncodeFn fn = encode_fn();
+  return fn && fn(map, c->dtype == QEVICT_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base),
+                  dims, st, box, el, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 const char* attn_check_pointers(const qevict_kv16_attn_args* p) {
@@ -91,13 +99,8 @@ cudaError_t launch_paged(const PromptArgs& a, const Plan& l, const CUtensorMap& 
   auto kernel = prompt_attn_kernel<T, D, true>;
   static std::atomic<uint64_t> done{0};
   cudaError_t e = once_per_device(done, device, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptSmem<D>::BYTES); });
-  if (e == cudaSuccess) e = launch_pdl(kernel, dim3((unsigned)l.positions), dim3(PROMPT_THREADS), PromptSmem<D>::BYTES, s, a, mq, mk, mv);
-  if (e == cudaSuccess && l.bytes > 0) {
-    // pairs alone: their rows, sequence by sequence; else all rows
-    const bool by_seq = l.rows == 0 && l.compact;
-    const long long rows = by_seq ? l.T : a.total_q;
-    e = launch_pdl(prompt_merge_kernel<T, D, true>, dim3((unsigned)((rows * a.Hq + 7) / 8), by_seq ? a.n_seqs : 1), dim3(256), 0, s, a, by_seq);
-  }
+  if (e == cudaSuccess) e = launch_pdl(kernel, dim3(l.ctas), dim3(PROMPT_THREADS), PromptSmem<D>::BYTES, s, a, mq, mk, mv);
+  if (e == cudaSuccess && l.cuts) e = launch_pdl(paged_merge_kernel<T, D>, dim3(l.slot_rows / 8, l.ctas), dim3(256), 0, s, a);
   return e;
 }
 
@@ -128,7 +131,7 @@ QEVICT_API qevict_status qevict_kv16_attn(const qevict_kv16_attn_args* p, void* 
   why = attn_check_pointers(p);
   if (why) return stateless_fail(QEVICT_ERR_INVALID_ARG, why);
   const Plan l = attn_plan(p, view);
-  if (l.positions > (1ll << 28)) return stateless_fail(QEVICT_ERR_UNSUPPORTED, "more than 2^28 work items in one call");
+  if (l.ctas == 0) return stateless_fail(QEVICT_ERR_UNSUPPORTED, "more than 2^28 work items in one call");
   if (l.bytes > 0 && (!scratch || scratch_bytes < l.bytes))
     return stateless_fail(QEVICT_ERR_NO_MEMORY, "scratch too small: see qevict_kv16_attn_scratch_bytes");
   if (l.bytes > 0 && misaligned16(scratch)) return stateless_fail(QEVICT_ERR_INVALID_ARG, "scratch must be 16-byte aligned");
@@ -139,18 +142,25 @@ QEVICT_API qevict_status qevict_kv16_attn(const qevict_kv16_attn_args* p, void* 
   a.max_q = (int)(p->max_q < p->total_q ? p->max_q : p->total_q);
   a.max_k = (int)(p->max_len < capacity ? p->max_len : capacity);
   a.causal = p->causal;
-  a.P = l.P; a.T = l.T; a.splits = l.pieces;
+  a.P = l.P; a.T = l.T; a.splits = 1;
   a.total_q = p->cu_q ? p->total_q : view.n_seqs;
   a.scale_log2 = (float)((p->softmax_scale > 0.f ? (double)p->softmax_scale : 1.0 / sqrt((double)view.D)) * 1.4426950408889634);
   a.out = p->out; a.lse = p->lse; a.q_bounds = p->cu_q; a.k_bounds = p->lens;
   a.lse_rows = p->total_q;
   a.out_stride[1] = p->out_stride[1]; a.out_stride[2] = p->out_stride[0];
-  a.part_o = static_cast<float*>(scratch);
-  a.part_lse = reinterpret_cast<float*>(static_cast<char*>(scratch) + l.o_bytes);
-  a.rows = l.rows; a.pair_rows = l.pair_rows; a.compact = l.compact;
+  if (l.cuts) {
+    char* base = static_cast<char*>(scratch);
+    a.cuts = reinterpret_cast<PagedCut*>(base);
+    a.part_o = reinterpret_cast<float*>(base + l.cut_bytes);
+    a.part_lse = reinterpret_cast<float*>(base + l.cut_bytes + l.o_bytes);
+  }
+  a.by_range = l.by_range; a.slot_rows = l.slot_rows;
   a.status = view.status;
   a.table = view.table; a.max_blocks = view.max_blocks; a.block_log2 = view.block_log2; a.n_pages = view.n_pages;
-  a.per_part = l.per_part;
+  const bool whole = whole_pages(c);
+  a.boxes = whole ? 1 : a.D / 64;
+  a.group_bytes = whole ? 16 * a.D : 1024;
+  a.half_bytes = whole ? 1024 : TILE * 128;
 #ifdef QEVICT_DEBUG_BOUNDS
   a.give_up_warp = -1;
   if (const char* e = getenv("QEVICT_CHECK_GIVE_UP")) sscanf(e, "%d:%d", &a.give_up_warp, &a.give_up_at);
@@ -161,8 +171,8 @@ QEVICT_API qevict_status qevict_kv16_attn(const qevict_kv16_attn_args* p, void* 
   CUtensorMap mq, mk, mv;
   const int64_t q_stride[3] = {0, p->q_stride[1], p->q_stride[0]};
   if (!make_map(&mq, c->dtype, p->q, a.D, p->total_q, a.Hq, 1, q_stride, a.T, a.P) ||
-      !make_map(&mk, c->dtype, c->k_pages, a.D, c->block, a.Hkv, c->n_pages, c->k_stride, c->block, 1) ||
-      !make_map(&mv, c->dtype, c->v_pages, a.D, c->block, a.Hkv, c->n_pages, c->v_stride, c->block, 1))
+      !make_page_map(&mk, c, c->k_pages, c->k_stride, whole, &a.head_step[0]) ||
+      !make_page_map(&mv, c, c->v_pages, c->v_stride, whole, &a.head_step[1]))
     return stateless_fail(QEVICT_ERR_CUDA, "a tensor map could not be made for q or the pages");
   cudaStream_t s = (cudaStream_t)stream;
   if (c->dtype == QEVICT_DTYPE_FP16)

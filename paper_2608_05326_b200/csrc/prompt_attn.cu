@@ -107,7 +107,7 @@ cudaError_t launch_prompt(const PromptArgs& a, const CUtensorMap& mq, const CUte
     e = launch_pdl(kernel, dim3((unsigned)(tiles * (a.Hq / a.P) * a.splits)), dim3(PROMPT_THREADS), PromptSmem<D>::BYTES, s, a, mq, mk, mv);
   if (e == cudaSuccess && a.splits > 1) {
     const unsigned ctas = (unsigned)(((long long)a.max_q * a.Hq + 7) / 8);
-    e = launch_pdl(prompt_merge_kernel<T, D, false>, dim3(ctas, a.n_seqs), dim3(256), 0, s, a, true);
+    e = launch_pdl(prompt_merge_kernel<T, D>, dim3(ctas, a.n_seqs), dim3(256), 0, s, a);
   }
   return e;
 }

@@ -49,6 +49,11 @@ constexpr int MMA_WARP = 16, LOAD_WARP = 17, ITEM_WARP = 18;
 constexpr int TILE = 128;           // query rows of a tile, keys of a tile
 constexpr float PROMPT_LAZY = 8.f;  // log2
 
+// An item whose keys the ranges of several CTAs share: it starts in the CTA that has this record and ends in the range of CTA `last`.
+struct PagedCut {
+  int valid, s, h0, r0, q0, nq, last, pair;
+};
+
 struct PromptArgs {
   int padded, n_seqs, Hq, Hkv, D, max_q, max_k, causal, splits;
   int P, T;  // a tile's rows: P query heads of one KV head, T tokens each
@@ -66,10 +71,13 @@ struct PromptArgs {
   // keys and values in pages (PAGED): a sequence's length is k_bounds[s], its rows of q are q_bounds' or, without them, row s
   const int32_t* table;  // [n_seqs][max_blocks]
   int max_blocks, block_log2, n_pages;
-  int per_part;          // key tiles of a work item at most
   long long lse_rows;    // rows of lse
-  int compact;           // partial results of pairs by sequence and row, T rows for each, else by row
-  long long pair_rows;   // rows of the partial results of pairs, which come first
+  int by_range;          // each CTA has an equal range of the call's work, else whole items as they fall free
+  int slot_rows;         // rows of a partial result
+  PagedCut* cuts;        // [CTAs]
+  int group_bytes, half_bytes;  // of K and V tiles in shared memory: from 8 keys to the next 8, from 64 channels to the next 64
+  int boxes;             // copies for each page: one, or one for each 64 channels
+  int head_step[2];      // keys, values: from head to head in the third coordinate
 #ifdef QEVICT_DEBUG_BOUNDS
   int give_up_warp, give_up_at;  // in every CTA this warp gives up at this wait of its (QEVICT_CHECK_GIVE_UP=warp:wait)
 #endif
@@ -135,6 +143,11 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, u
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
                ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(tok), "r"(head), "r"(seq) : "memory");
 }
+// a page's rows of a head: {channels, 8 tokens, 64-channel pieces of heads, groups of 8 tokens, pages}
+__device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int piece, int page) {
+  asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %4, %6}], [%2];"
+               ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(0), "r"(piece), "r"(page) : "memory");
+}
 __device__ __forceinline__ void commit_to(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
@@ -142,16 +155,16 @@ __device__ __forceinline__ void commit_to(uint32_t bar) {
 // offset, the high word (constant) the stride of 1024 bytes between groups of eight rows, version 1 and the swizzle.
 constexpr uint32_t DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
 __device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lbo) { return ((addr >> 4) & 0x3FFFu) | ((lbo >> 4) << 16); }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t acc) {
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t acc, uint32_t b_hi = DESC_HI) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}\n" ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(acc), "r"(DESC_HI)
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %6};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}\n" ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(acc), "r"(DESC_HI), "r"(b_hi)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t acc) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t acc, uint32_t b_hi = DESC_HI) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 db, {%2, %5};\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}\n" ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "r"(acc), "r"(DESC_HI)
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}\n" ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "r"(acc), "r"(b_hi)
       : "memory");
 }
 __device__ __forceinline__ void tm_ld32(uint32_t addr, float* v) {
@@ -221,7 +234,7 @@ template <int D> struct PromptSmem {
   static constexpr int HALF = TILE * 128;             // 64 channels of 128 rows
   static constexpr int TILE_BYTES = HALF * (D / 64);
   static constexpr int Q_OFF = 0, KV_OFF = 2 * TILE_BYTES, BAR_OFF = KV_OFF + STAGES * TILE_BYTES;
-  static constexpr int WORDS = 256, ITEMS = 320, ROWS = 576;  // behind the barriers: words, work items, row maxima
+  static constexpr int WORDS = 256, ITEMS = 320, ROWS = 592;  // behind the barriers: words, work items, row maxima
   static constexpr int BYTES = BAR_OFF + ROWS + 2048;
 };
 
@@ -242,28 +255,48 @@ template <bool PAGED> __device__ __forceinline__ bool seq_cut(const PromptArgs& 
          span_cut(a.k_bounds, PAGED || a.padded, s, a.max_k, a.total_k);
 }
 
-// Paged: the parts that a sequence's keys are cut into, and whether its queries are few.  Few queries (one tile) have both query
-// tiles of a CTA take the same rows, each one half of the part's key tiles: one's softmax then runs beside the other's
-// products as it does for two tiles of rows.
-__device__ __forceinline__ int paged_pieces(const PromptArgs& a, int keys) { return max(1, ((keys + TILE - 1) / TILE + a.per_part - 1) / a.per_part); }
+// Few queries (one tile of rows) have both query tiles of a CTA take the same rows, each one half of the key tiles: one's softmax
+// then runs beside the other's products as it does for two tiles of rows.
 __device__ __forceinline__ bool paged_pair(const PromptArgs& a, int nq, int keys) { return nq <= a.T && keys > TILE; }
-template <bool PAGED> __device__ __forceinline__ int pieces_of(const PromptArgs& a, int keys) { return PAGED ? paged_pieces(a, keys) : a.splits; }
-
-// Place of (part, row, head) among the partial results: paged ones of pairs come first, for two parts more per piece.
-__device__ __forceinline__ long long paged_place(const PromptArgs& a, bool pair, int part, int s, int row, long long prow, int hq) {
-  const long long r = pair ? part * a.pair_rows + (a.compact ? (long long)s * a.T + row : prow) : 2 * a.splits * a.pair_rows + part * a.rows + prow;
-  return r * a.Hq + hq;
-}
 
 // A work item: two tiles of T tokens of P heads of one sequence, or a part of their keys.
 struct PromptItem {
   int valid, h0, s, split, r0, q0, nq, k0, nk;  // h0: first query head, r0: first token
   int lo, n;       // key tiles of this item
   int nt0, nt1;    // end of the two query tiles' key tiles
-  int parts, pair, mid;  // paged: partial results of every row; both tiles have the same rows, the second one the key tiles lo .. mid - 1
+  // paged: both tiles have the same rows, the second one the key tiles lo .. mid - 1; where the results go, -1: to the output; key
+  // tiles of the CTA's items before
+  int pair, mid, slot, before;
   __device__ __forceinline__ int cnt(int w) const { return pair ? (w ? mid - lo : n - mid) : max(0, (w ? nt1 : nt0) - lo); }
   __device__ __forceinline__ bool dirty() const { return n > lo && n * TILE > nk; }  // the first tile reaches past the sequence
 };
+
+// Key tiles that an item's two query tiles see.
+__device__ __forceinline__ void item_tiles(const PromptArgs& a, PromptItem* it) {
+  int nt[2];
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    const int rw = it->r0 + w * a.T, last = min(rw + a.T, it->nq) - 1;
+    const int lim = rw >= it->nq ? 0 : (a.causal ? min(it->nk, last + it->nk - it->nq + 1) : it->nk);
+    nt[w] = lim > 0 ? (lim + TILE - 1) / TILE : 0;
+  }
+  it->lo = 0;
+  it->n = max(nt[0], nt[1]);
+  it->nt0 = nt[0];
+  it->nt1 = nt[1];
+}
+// What each query tile does of the item's key tiles lo .. n - 1.
+template <bool PAGED> __device__ __forceinline__ void item_streams(const PromptArgs& a, PromptItem* it) {
+  it->nt0 = min(it->nt0, it->n);
+  it->nt1 = min(it->nt1, it->n);
+  it->pair = PAGED && paged_pair(a, it->nq, it->nk);
+  it->mid = it->lo;
+  if (it->pair) {
+    it->mid = it->lo + (it->n - it->lo) / 2;
+    it->nt0 = it->n;
+    it->nt1 = it->mid;
+  }
+}
 
 // The item of grid position x, for a whole warp; not valid where x lies past the last sequence's.  Positions go by the
 // sequences' own lengths, so a batch of very different lengths has next to no empty positions, and by falling cost, so that the
@@ -273,10 +306,12 @@ struct PromptItem {
 // it), which is where the next one starts; positions mostly grow, but nothing promises it: a smaller one starts at the front.
 template <bool PAGED> __device__ __forceinline__ PromptItem item_of(const PromptArgs& a, int x, int lane, int* at, int* before) {
   PromptItem it;
-  const int t = x, step = 2 * a.T, groups = a.Hq / a.P;
-  it.split = 0;
+  const int t = x / a.splits, step = 2 * a.T, groups = a.Hq / a.P;
+  it.split = x - t * a.splits;
   it.h0 = 0;
   it.valid = 0;
+  it.slot = -1;
+  it.before = 0;
   it.s = 0;
   int mt = 0;
   if (t < *before) {
@@ -291,29 +326,22 @@ template <bool PAGED> __device__ __forceinline__ PromptItem item_of(const Prompt
       k_span<PAGED>(a, s, &first, &keys);
     }
     const int tiles = (n + step - 1) / step, base = (keys - n) / step, top = base + tiles;  // its levels: base .. top - 1
-    const int pieces = pieces_of<PAGED>(a, keys);
-    const int all = __reduce_add_sync(0xffffffffu, tiles * pieces) * groups, in = t - *before;
+    const int all = __reduce_add_sync(0xffffffffu, tiles) * groups, in = t - *before;
     if (in < all) {
       // the level: the largest L with more than `in` items on the levels from L on
-      auto from = [&](int level) { return __reduce_add_sync(0xffffffffu, min(tiles, max(0, top - level)) * pieces) * groups; };
+      auto from = [&](int level) { return __reduce_add_sync(0xffffffffu, min(tiles, max(0, top - level))) * groups; };
       int lo = __reduce_min_sync(0xffffffffu, tiles ? base : 0x7fffffff), hi = __reduce_max_sync(0xffffffffu, tiles ? top - 1 : -0x7fffffff);
       while (lo < hi) {
         const int mid = lo + ((hi - lo + 1) >> 1);
         if (from(mid) > in) lo = mid; else hi = mid - 1;
       }
-      int k = in - from(lo + 1), who;
+      const int k = in - from(lo + 1), nth = k / groups;
       uint32_t have = __ballot_sync(0xffffffffu, tiles > 0 && base <= lo && lo < top);
-      for (;; have &= have - 1) {
-        who = __ffs(have) - 1;
-        const int here = __shfl_sync(0xffffffffu, pieces, who) * groups;
-        if (k < here) break;
-        k -= here;
-      }
-      const int parts = __shfl_sync(0xffffffffu, pieces, who);
+      for (int i = 0; i < nth; ++i) have &= have - 1;
+      const int who = __ffs(have) - 1;
       it.valid = 1;
       it.s = *at + who;
-      it.h0 = k / parts * a.P;
-      it.split = k % parts;
+      it.h0 = (k - nth * groups) * a.P;
       mt = lo - __shfl_sync(0xffffffffu, base, who);
       break;
     }
@@ -323,33 +351,143 @@ template <bool PAGED> __device__ __forceinline__ PromptItem item_of(const Prompt
   if (!it.valid) return it;
   q_span<PAGED>(a, it.s, &it.q0, &it.nq);
   k_span<PAGED>(a, it.s, &it.k0, &it.nk);
-  const int pieces = pieces_of<PAGED>(a, it.nk);
-  int nt[2];
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    const int rw = it.r0 + w * a.T, last = min(rw + a.T, it.nq) - 1;
-    const int lim = rw >= it.nq ? 0 : (a.causal ? min(it.nk, last + it.nk - it.nq + 1) : it.nk);
-    nt[w] = lim > 0 ? (lim + TILE - 1) / TILE : 0;
-  }
-  it.lo = 0;
-  it.n = max(nt[0], nt[1]);
-  if (pieces > 1) {
-    const int per = (it.n + pieces - 1) / pieces;
+  item_tiles(a, &it);
+  if (a.splits > 1) {
+    const int per = (it.n + a.splits - 1) / a.splits;
     it.lo = min(it.n, it.split * per);
     it.n = min(it.n, it.lo + per);
   }
-  it.nt0 = min(nt[0], it.n);
-  it.nt1 = min(nt[1], it.n);
-  it.pair = PAGED && paged_pair(a, it.nq, it.nk);
-  it.parts = it.pair ? 2 * pieces : pieces;
-  it.mid = it.lo;
-  if (it.pair) {
-    it.mid = it.lo + (it.n - it.lo) / 2;
-    it.nt0 = it.n;
-    it.nt1 = it.mid;
-  }
+  item_streams<PAGED>(a, &it);
   return it;
 }
+
+// Paged calls with few items for the SMs: each CTA has an equal range of the call's work, whatever the lengths.
+//
+// The items stand in a row: sequence by sequence, heads in it, tiles of rows in these.  An item costs its visible keys (three
+// quarters for pairs, whose two tiles a step bandwidth bounds) and a constant; CTA c has what lies in [c, c + 1) * W of
+// the sum.  An end inside an item is moved to a key tile: an item has the CTAs that have tiles of it, and where these are
+// several, each writes a partial result.  The ranges are a function of the lengths alone.
+constexpr int ITEM_COST = 1024, KEY_COST = 4, KEY_COST_PAIR = 3, RANGE_LEAST = 1024;
+
+struct PagedSeq {
+  int q0, nq, nk, tiles, key_cost;
+  // visible keys of row tile t, and of all before it
+  __device__ __forceinline__ int keys(const PromptArgs& a, int t) const {
+    return !a.causal || t == tiles - 1 ? nk : max(0, nk - nq + (t + 1) * 2 * a.T);
+  }
+  __device__ __forceinline__ long long before(const PromptArgs& a, int t) const {
+    if (!a.causal) return (long long)t * nk;
+    const long long step = 2 * a.T, p = nk - nq, full = t < tiles ? t : tiles - 1;
+    long long u = p < 0 ? -p / step : 0;
+    if (u > full) u = full;
+    return (full - u) * p + step * (full * (full + 1) - u * (u + 1)) / 2 + (t < tiles ? 0 : nk);
+  }
+  __device__ __forceinline__ long long cost(const PromptArgs& a, int t) const { return (long long)key_cost * keys(a, t) + ITEM_COST; }
+  __device__ __forceinline__ long long cost_before(const PromptArgs& a, int t) const { return t > 0 ? key_cost * before(a, t) + (long long)t * ITEM_COST : 0; }
+};
+
+__device__ __forceinline__ PagedSeq paged_seq(const PromptArgs& a, int s) {
+  PagedSeq q = {0, 0, 0, 0, 0};
+  int k0;
+  if (s < a.n_seqs) {
+    q_span<true>(a, s, &q.q0, &q.nq);
+    k_span<true>(a, s, &k0, &q.nk);
+    q.tiles = (q.nq + 2 * a.T - 1) / (2 * a.T);
+    q.key_cost = paged_pair(a, q.nq, q.nk) ? KEY_COST_PAIR : KEY_COST;
+  }
+  return q;
+}
+
+struct PagedRange {
+  long long width, lo, hi, at;  // this CTA's part of the sum; start of the current item
+  int s, h, t;
+  PagedSeq seq;
+
+  __device__ __forceinline__ PagedRange(const PromptArgs& a, int lane) {
+    const int groups = a.Hq / a.P;
+    long long sum = 0;
+    for (int i = lane; i < a.n_seqs; i += 32) {
+      const PagedSeq q = paged_seq(a, i);
+      sum += q.cost_before(a, q.tiles) * groups;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    width = (sum + gridDim.x - 1) / gridDim.x;
+    if (width < RANGE_LEAST) width = RANGE_LEAST;
+    lo = blockIdx.x * width;
+    hi = lo + width < sum ? lo + width : sum;
+    s = a.n_seqs;
+    if (lo >= sum) return;
+    long long front = 0;  // cost of the sequences before
+    for (int i = 0; i < a.n_seqs; i += 32) {
+      const PagedSeq q = paged_seq(a, i + lane);
+      const long long mine = q.cost_before(a, q.tiles) * groups;
+      long long upto = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, front + upto > lo);
+      if (past) {
+        const int who = __ffs(past) - 1;
+        s = i + who;
+        front += __shfl_sync(0xffffffffu, upto - mine, who);
+        break;
+      }
+      front += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    seq = paged_seq(a, s);
+    const long long head = seq.cost_before(a, seq.tiles);
+    h = (int)((lo - front) / head);
+    front += h * head;
+    int t0 = 0, t1 = seq.tiles - 1;  // the last tile that starts at or before lo
+    while (t0 < t1) {
+      const int mid = (t0 + t1 + 1) >> 1;
+      if (front + seq.cost_before(a, mid) <= lo) t0 = mid; else t1 = mid - 1;
+    }
+    t = t0;
+    at = front + seq.cost_before(a, t);
+  }
+
+  // The next item of the range, its key tiles in it; false behind the last one.
+  __device__ __forceinline__ bool next(const PromptArgs& a, int lane, PromptItem* it) {
+    while (s < a.n_seqs && at < hi) {
+      const long long cost = seq.cost(a, t), end = at + cost;
+      it->valid = 1;
+      it->s = s; it->h0 = h * a.P; it->r0 = t * 2 * a.T;
+      it->q0 = seq.q0; it->nq = seq.nq; it->k0 = 0; it->nk = seq.nk;
+      it->split = 0;
+      item_tiles(a, it);
+      const int all = it->n;
+      const long long tile = (long long)seq.key_cost * TILE;
+      auto tiles_upto = [&](long long x) { return x <= at + ITEM_COST ? 0 : (int)((x - at - ITEM_COST) / tile); };
+      const int f0 = lo > at ? tiles_upto(lo) : 0;
+      const bool ends = end <= hi;
+      const int f1 = ends ? all : tiles_upto(hi);
+      it->lo = f0;
+      it->n = f1;
+      it->slot = f0 == 0 && ends ? -1 : 2 * (int)blockIdx.x + (f0 == 0);
+      if (f0 == 0 && f1 > 0 && !ends && lane == 0) {
+        const PagedCut c = {1, s, it->h0, it->r0, seq.q0, seq.nq, (int)((end - 1) / width), paged_pair(a, seq.nq, seq.nk)};
+        a.cuts[blockIdx.x] = c;
+      }
+      at = end;
+      if (++t == seq.tiles) {
+        t = 0;
+        if (++h == a.Hq / a.P) {
+          h = 0;
+          do { seq = paged_seq(a, ++s); } while (s < a.n_seqs && seq.tiles == 0);
+        }
+      }
+      if (f1 > f0 || (all == 0 && ends)) {
+        item_streams<true>(a, it);
+        return true;
+      }
+    }
+    return false;
+  }
+};
 
 template <class T, int D, bool PAGED>
 __global__ void __launch_bounds__(PROMPT_THREADS, 1)
@@ -372,6 +510,8 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
   PromptItem* items = reinterpret_cast<PromptItem*>(sm + SM::BAR_OFF + SM::ITEMS);
   static_assert(SM::ITEMS + sizeof(PromptItem) * 4 <= SM::ROWS, "two work items, and two that could not be handed out");
   if (smb & 1023u) {  // no tile would be where the products look for it
+    if (PAGED) pdl_prologue();
+    if (PAGED && a.cuts && tid == 0) a.cuts[blockIdx.x].valid = 0;
     kv8_record(a.status, CHECK_ALIGNMENT);
     return;
   }
@@ -436,7 +576,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       // Work items: the CTA's own grid position first, then positions that have not started, taken over one at a time
       // while the item before is in work.  (A grid of single-item CTAs pays for start, first loads and results of every
       // item with idle tensor cores: 12 packed prompts of up to 4001 tokens took 620 us.)
-      int x = blockIdx.x, y, z, put = 0, at = 0, before = 0;
+      int x = blockIdx.x, y, z, put = 0, at = 0, before = 0, k_tiles = 0;
       bool checks = false;  // whoever has position 0 (of its own or taken over) looks at the bounds
       auto item_at = [&] {
 #ifdef QEVICT_DEBUG_BOUNDS  // the checking build has its positions fall
@@ -445,6 +585,28 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         return item_of<PAGED>(a, x, lane, &at, &before);
 #endif
       };
+      auto hand_out = [&](const PromptItem& it) {
+        if (put >= 2) ok = wait_item(b_taken + 8 * (put & 1), (uint32_t)((put >> 1) - 1) & 1u);
+        if (ok && lane == 0) {
+          items[put & 1] = it;
+          bar_arrive(b_item + 8 * (put & 1));
+        } else if (!ok && lane == 0) {
+          items[2] = it;
+        }
+        ++put;
+      };
+      if (PAGED && a.by_range) {
+        checks = blockIdx.x == 0;
+        if (a.cuts && lane == 0) a.cuts[blockIdx.x].valid = 0;
+        PagedRange range(a, lane);
+        PromptItem it;
+        while (ok && range.next(a, lane, &it)) {
+          it.before = k_tiles;
+          k_tiles += it.n - it.lo;
+          hand_out(it);
+          __syncwarp();
+        }
+      } else
       for (uint32_t ask = 0;; ++ask) {
         if (lane == 0) {
           words[8] = ask + 1;
@@ -453,16 +615,13 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
                            smem_u32((void*)words)), "r"(b_next) : "memory");
         }
         checks = checks || x == 0;
-        const PromptItem it = item_at();
+        PromptItem it = item_at();
         if (it.valid) {
-          if (put >= 2) ok = wait_item(b_taken + 8 * (put & 1), (uint32_t)((put >> 1) - 1) & 1u);
-          if (ok && lane == 0) {
-            items[put & 1] = it;
-            bar_arrive(b_item + 8 * (put & 1));
-          } else if (!ok && lane == 0) {
-            items[2] = it;
+          if (PAGED) {
+            it.before = k_tiles;
+            k_tiles += it.n - it.lo;
           }
-          ++put;
+          hand_out(it);
         }
         __syncwarp();
         // (whatever has happened meanwhile: the answer is written to this CTA's memory)
@@ -498,7 +657,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
           if (seq_cut<PAGED>(a, s)) kv8_record(a.status, CHECK_LENGTH);
       }
     } else if (wid == LOAD_WARP) {
-      int slot = 0, q_turn = 0, issued = 0, k_tiles = 0;
+      int slot = 0, q_turn = 0, issued = 0;
       uint32_t phase = 0;
       while (const PromptItem* item = next_item()) {
         const PromptItem& it = *item;
@@ -520,9 +679,10 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         }
         int v_slot = 0;
         uint32_t v_phase = 0;
+        int k_tiles = it.before;
         bool clean = it.dirty(), v_seen = false;
-        // Paged: 32 page ids of each stream, one per lane, and the 32 below them on their way.  A block that is not there has the
-        // page after the last one: the copy then writes zeros.
+        // Paged: 32 page ids of each stream, one per lane, and the 32 below them on their way.  A block that is not there has a
+        // page behind the last one: the copy then writes zeros.
         const int per_log2 = 7 - a.block_log2;  // blocks of a tile
         const int blocks = PAGED ? (it.nk + (1 << a.block_log2) - 1) >> a.block_log2 : 0;
         int window[2] = {0, 0}, id[2] = {0, 0}, ahead[2] = {0, 0};
@@ -568,7 +728,9 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
               words[5] = issued + 1;
             }
             __syncwarp();
-            if (ok && x < D / 64) tma_load(dst + x * SM::HALF + (i << (a.block_log2 + 7)), value ? &mv : &mk, bar, x * 64, 0, hk, page);
+            if (ok && x < a.boxes)
+              tma_page(dst + x * SM::HALF + i * (a.group_bytes << (a.block_log2 - 3)), value ? &mv : &mk, bar, x * 64,
+                       hk * (value ? a.head_step[1] : a.head_step[0]), page);
             k_tiles += !value;
           } else if (ok && lane == 0) {
             bar_expect(bar, SM::TILE_BYTES);
@@ -586,10 +748,11 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
           ok = ok && wait(b_full + 8 * v_slot, v_phase);
           const int from = it.nk - (it.n - 1) * TILE, per = (TILE - from) * 8;
           if (ok) {
-            unsigned char* v0 = sm + SM::KV_OFF + v_slot * SM::TILE_BYTES + from * 128;
+            unsigned char* v0 = sm + SM::KV_OFF + v_slot * SM::TILE_BYTES;
             for (int k = lane; k < per * (D / 64); k += 32) {
-              const int x = k / per;
-              *reinterpret_cast<uint4*>(v0 + x * SM::HALF + (k - x * per) * 16) = make_uint4(0u, 0u, 0u, 0u);
+              const int x = k / per, row = from + ((k - x * per) >> 3), at = (k - x * per) & 7;
+              const int to = PAGED ? (row >> 3) * a.group_bytes + x * a.half_bytes + (row & 7) * 128 : row * 128 + x * SM::HALF;
+              *reinterpret_cast<uint4*>(v0 + to + at * 16) = make_uint4(0u, 0u, 0u, 0u);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
@@ -620,7 +783,9 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       const uint32_t base = (1u << 4) | (fmt << 7) | (fmt << 10) | ((128u >> 4) << 24);
       const uint32_t id_s = base | ((128u >> 3) << 17);                           // both operands K-major
       const uint32_t id_o = base | (1u << 16) | ((uint32_t)(D >> 3) << 17);       // V: channels contiguous (N-major)
-      const uint32_t q_lo = desc_lo(u_sm + SM::Q_OFF, 16), k_lo = desc_lo(u_sm + SM::KV_OFF, 16), v_lo = desc_lo(u_sm + SM::KV_OFF, SM::HALF);
+      const uint32_t q_lo = desc_lo(u_sm + SM::Q_OFF, 16), k_lo = desc_lo(u_sm + SM::KV_OFF, 16), v_lo = desc_lo(u_sm + SM::KV_OFF, PAGED ? (uint32_t)a.half_bytes : SM::HALF);
+      const uint32_t kv_hi = PAGED ? ((uint32_t)a.group_bytes >> 4) | (DESC_HI & ~0x3fffu) : DESC_HI;
+      const uint32_t k_half = PAGED ? (uint32_t)a.half_bytes : SM::HALF, v_step = PAGED ? (uint32_t)a.group_bytes * 2 : 2048u;
       const uint32_t ub = u_sm + SM::BAR_OFF, u_full = ub + 8, u_empty = u_full + 8 * NS, u_s = u_empty + 8 * NS, u_p = u_s + 16, u_o = u_p + 16;
       leader = elect_one();
       // Half of the products of S, a look at the other tile's P, the other half: the look's latency passes while the tensor
@@ -635,7 +800,10 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
 #pragma unroll
             for (int ks = part * (D / 32); ks < (part + 1) * (D / 32); ++ks) {
               const uint32_t o = ((uint32_t)(ks >> 2) * SM::HALF + (ks & 3) * 32) >> 4;
-              mma_ss(u_tm + w * 128, qa + o, ka + o, id_s, ks > 0);
+              if constexpr (PAGED)
+                mma_ss(u_tm + w * 128, qa + o, ka + (((uint32_t)(ks >> 2) * k_half + (ks & 3) * 32) >> 4), id_s, ks > 0, kv_hi);
+              else
+                mma_ss(u_tm + w * 128, qa + o, ka + o, id_s, ks > 0);
             }
             if (part == 1) commit_to(u_s + 8 * w);
           }
@@ -653,7 +821,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         if (leader) {
 #pragma unroll
           for (int ks = 0; ks < TILE / 16; ++ks)
-            mma_ts(u_tm + 256 + w * 128, u_tm + w * 128 + P_COL(ks >> 2, ks & 3), va + ks * (2048 >> 4), id_o, ks > 0 ? 1u : acc);
+            mma_ts(u_tm + 256 + w * 128, u_tm + w * 128 + P_COL(ks >> 2, ks & 3), va + ks * (v_step >> 4), id_o, ks > 0 ? 1u : acc, kv_hi);
         }
         __syncwarp();
       };
@@ -782,7 +950,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
     // also gives both the same answer to whether a wait of either's has run out, so that both leave at the same point.
     const int w = wid >> 3, half = (wid >> 2) & 1, r = (wid & 3) * 32 + lane;
     const int hl = r / a.T;  // head of this row; rows past P heads are not used
-    int tok = w * a.T + r - hl * a.T, k_tiles = 0;  // token
+    int tok = w * a.T + r - hl * a.T;  // token
     const uint32_t lane_base = (uint32_t)((wid & 3) * 32) << 16;
     const uint32_t ts = tmem + lane_base + w * 128, to = tmem + lane_base + 256 + w * 128 + half * (D / 2);
     float* xch = reinterpret_cast<float*>(sm + SM::BAR_OFF + SM::ROWS) + w * 2 * TILE + r;  // the two halves' values of a row
@@ -803,6 +971,12 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       if (PAGED) tok = (twin ? 0 : w * a.T) + r - hl * a.T;
       // keys that this row still sees from the tile's (this half's) first on; grows by a tile each time
       int left = (a.causal ? min(it.nk, it.r0 + tok + it.nk - it.nq + 1) : it.nk) - ((w ? it.nt1 : it.nt0) - 1) * TILE - half * (TILE / 2);
+      // (paged) place of this tile's number of absent blocks: the last 16 tiles' in the order of their copies, those of pairs in turn
+      int mask_at = 0, mask_step = 1;
+      if (PAGED) {
+        mask_at = it.before + (twin ? w : it.n - (w ? it.nt1 : it.nt0));
+        mask_step = twin ? 2 : 1;
+      }
       const bool mine = it.r0 + tok < it.nq && hl < a.P;  // rows of nobody hold anything, and have no say below
       float m = -INFINITY, l = 0.f;
       for (int i = cnt; i > 0; --i, left += TILE) {
@@ -820,8 +994,8 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
             for (int c = 0; c < TILE / 2; ++c) x[c] = c < left ? x[c] : -INFINITY;
           }
           if constexpr (PAGED) {
-            const int at = cnt - i, index = k_tiles + (twin ? 2 * at + w : it.n - (w ? it.nt1 : it.nt0) + at);
-            const uint32_t none = masks[index & 15];
+            const uint32_t none = masks[mask_at & 15];
+            mask_at += mask_step;
             if (none) {  // blocks that are not there, 16 keys at a time
 #pragma unroll
               for (int c = 0; c < TILE / 2; ++c)
@@ -882,7 +1056,6 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         l += s0 + s1;
       }
       if (!ok) break;
-      if (PAGED) k_tiles += it.n - it.lo;
       // results: the two halves' sums, half of the channels each
       if (cnt > 0) {
         ok = wait(b_o + 8 * w, o_phase);
@@ -892,14 +1065,67 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       xch[half * TILE] = l;
       meet();
       if (!ok) break;
+      if constexpr (PAGED) {
+        if (twin) {
+          // both tiles' results of the same rows: four warps share them, a quarter of the channels each
+          auto meet4 = [&] {
+            uint32_t all;
+            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}\n"
+                         : "=r"(all) : "r"((uint32_t)ok), "r"(9 + (wid & 3)) : "memory");
+            ok = all != 0;
+          };
+          float* both = reinterpret_cast<float*>(sm + SM::BAR_OFF + SM::ROWS) + r;
+          l = xch[0] + xch[TILE];
+          meet4();
+          xch[half * TILE] = half ? l : m;
+          meet4();
+          if (!ok) break;
+          tm_after();
+          const float m0 = both[0], m1 = both[2 * TILE], top = fmaxf(m0, m1);
+          const float f0 = top == -INFINITY ? 0.f : ex2p(m0 - top), f1 = top == -INFINITY ? 0.f : ex2p(m1 - top);
+          l = both[TILE] * f0 + both[3 * TILE] * f1;
+          const int row = it.r0 + tok, hq = it.h0 + hl, c0 = (2 * w + half) * (D / 4);
+          const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : top + log2f(l);
+          const long long prow = it.q0 + row, slot = (long long)it.slot * a.slot_rows + r;
+          if (mine && w == 0 && half == 0) {
+            if (it.slot >= 0) a.part_lse[slot] = lse2;
+            else if (a.lse) a.lse[hq * a.lse_rows + prow] = lse2 * 0.6931471805599453f;
+          }
+          T* out = static_cast<T*>(a.out) + prow * a.out_stride[2] + hq * a.out_stride[1] + c0;
+#pragma unroll 1
+          for (int c = 0; c < D / 4; c += 8) {
+            float o[8], o1[8];
+            tm_ld8(tmem + lane_base + 256 + c0 + c, o);
+            if (it.cnt(1) > 0) tm_ld8(tmem + lane_base + 384 + c0 + c, o1);
+            tm_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              o[k] *= f0;
+              if (it.cnt(1) > 0) o[k] += o1[k] * f1;
+              o[k] = l == 0.f ? 0.f : o[k] * inv;
+            }
+            if (!mine) continue;
+            if (it.slot >= 0) {
+              float4* po = reinterpret_cast<float4*>(a.part_o + slot * D + c0 + c);
+              po[0] = make_float4(o[0], o[1], o[2], o[3]);
+              po[1] = make_float4(o[4], o[5], o[6], o[7]);
+            } else {
+              *reinterpret_cast<uint4*>(out + c) = make_uint4(pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3]), pack2<T>(o[4], o[5]), pack2<T>(o[6], o[7]));
+            }
+          }
+          tm_before();
+          meet4();  // the next item's first products overwrite both
+          if (!ok) break;
+          continue;
+        }
+      }
       l = xch[0] + xch[TILE];
       const int row = it.r0 + tok, hq = it.h0 + hl;
       const float inv = l == 0.f ? 0.f : 1.f / l;
       const long long prow = a.padded ? (long long)it.s * a.max_q + row : (long long)it.q0 + row;
       const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
-      const bool partial = PAGED ? it.parts > 1 : a.splits > 1;
-      const long long place = PAGED ? paged_place(a, twin, twin ? 2 * it.split + w : it.split, it.s, row, prow, hq)
-                                    : ((long long)it.split * a.rows + prow) * a.Hq + hq;
+      const bool partial = PAGED ? it.slot >= 0 : a.splits > 1;
+      const long long place = PAGED ? (long long)it.slot * a.slot_rows + w * TILE + r : ((long long)it.split * a.rows + prow) * a.Hq + hq;
       if (mine && half == 0) {
         if (partial)
           a.part_lse[place] = lse2;
@@ -949,15 +1175,15 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       kv8_record(a.status, CHECK_COPY_TIMEOUT);
     }
     // The rows of the items that may not be finished become not-a-number, for callers who do not read the status: the two that
-    // were handed out last and the two that were not.
-    for (int n = 0; n < 4; ++n) {
-      const PromptItem& it = items[n];
-      for (int i = tid; it.valid && i < 2 * a.T * a.P; i += PROMPT_THREADS) {
-        const int row = it.r0 + i / a.P, hq = it.h0 + i % a.P;
+    // were handed out last and the two that were not.  Of a range, all.
+    auto lose = [&](const PromptItem& it, int first, int step) {
+      for (int i = first; it.valid && i < 2 * a.T * a.P; i += step) {
+        const int row = it.r0 + i / a.P, hl = i % a.P, hq = it.h0 + hl;
         if (row >= it.nq) break;
         const long long prow = a.padded ? (long long)it.s * a.max_q + row : (long long)it.q0 + row;
-        if (PAGED ? it.parts > 1 : a.splits > 1) {  // as a weight, it makes the merged row that
-          a.part_lse[PAGED ? paged_place(a, it.pair, it.pair ? 2 * it.split : it.split, it.s, row, prow, hq)
+        if (PAGED ? it.slot >= 0 : a.splits > 1) {  // as a weight, it makes the merged row that
+          const int w = (row - it.r0) / a.T;
+          a.part_lse[PAGED ? (long long)it.slot * a.slot_rows + w * TILE + hl * a.T + row - it.r0 - w * a.T
                            : ((long long)it.split * a.rows + prow) * a.Hq + hq] = NAN;
           continue;
         }
@@ -965,6 +1191,15 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         T* out = static_cast<T*>(a.out) + (a.padded ? it.s * a.out_stride[0] + row * a.out_stride[2] : prow * a.out_stride[2]) + hq * a.out_stride[1];
         for (int c = 0; c < D; ++c) out[c] = Tr<T>::from_float(NAN);
       }
+    };
+    if (PAGED && a.by_range) {
+      if (wid == ITEM_WARP) {
+        PagedRange range(a, lane);
+        PromptItem it;
+        while (range.next(a, lane, &it)) lose(it, lane, 32);
+      }
+    } else {
+      for (int n = 0; n < 4; ++n) lose(items[n], tid, PROMPT_THREADS);
     }
   }
   __syncthreads();
@@ -973,39 +1208,20 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
 
 // Joins the partial results of a split call: one warp per (row, head), a lane per part for the weights (at most 64 parts), then
 // per 2 or 4 channels.
-template <class T, int D, bool PAGED>
-__global__ void __launch_bounds__(256) prompt_merge_kernel(const PromptArgs a, const bool by_seq) {
+template <class T, int D>
+__global__ void __launch_bounds__(256) prompt_merge_kernel(const PromptArgs a) {
   constexpr int PER = D / 32;
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, s = blockIdx.y;
   pdl_prologue();
+  int q0, nq;
+  span_of(a.q_bounds, a.padded, s, a.max_q, a.total_q, &q0, &nq);
   const long long at = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  int s = blockIdx.y, row = (int)(at / a.Hq), q0, nq, splits = a.splits;
-  const int hq = (int)(at - (long long)row * a.Hq);
-  bool pair = false;
-  if constexpr (PAGED) {
-    // rows of all sequences, or (merging pairs alone) T rows for each
-    int k0, nk;
-    if (!by_seq) {
-      const int r = row;
-      if (r >= a.total_q) return;
-      s = sequence_of(a.q_bounds, a.n_seqs, r, a.total_q, lane, &q0);
-      if (s < 0) return;
-      row = r - q0;
-    }
-    q_span<PAGED>(a, s, &q0, &nq);
-    k_span<PAGED>(a, s, &k0, &nk);
-    pair = paged_pair(a, nq, nk);
-    splits = paged_pieces(a, nk) * (pair ? 2 : 1);
-    if (splits == 1) return;
-  } else {
-    q_span<PAGED>(a, s, &q0, &nq);
-  }
+  const int row = (int)(at / a.Hq), hq = (int)(at - (long long)row * a.Hq);
   if (row >= nq) return;
   const long long prow = a.padded ? (long long)s * a.max_q + row : (long long)q0 + row;
-  // of part 0; from part to part
-  const long long first = PAGED ? paged_place(a, pair, 0, s, row, prow, hq) : prow * a.Hq + hq, next = (PAGED && pair ? a.pair_rows : a.rows) * a.Hq;
-  float w0 = lane < splits ? a.part_lse[first + lane * next] : -INFINITY;
-  float w1 = lane + 32 < splits ? a.part_lse[first + (lane + 32) * next] : -INFINITY;
+  const long long first = prow * a.Hq + hq, next = a.rows * a.Hq;  // of part 0; from part to part
+  float w0 = lane < a.splits ? a.part_lse[first + lane * next] : -INFINITY;
+  float w1 = lane + 32 < a.splits ? a.part_lse[first + (lane + 32) * next] : -INFINITY;
   float M = fmaxf(w0, w1);
 #pragma unroll
   for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
@@ -1017,7 +1233,7 @@ __global__ void __launch_bounds__(256) prompt_merge_kernel(const PromptArgs a, c
   for (int o = 16; o; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
   float sum[PER] = {};
 #pragma unroll 4
-  for (int i = 0; i < splits; ++i) {
+  for (int i = 0; i < a.splits; ++i) {
     const float f = __shfl_sync(0xffffffffu, i < 32 ? w0 : w1, i & 31);
     const float* src = a.part_o + (first + i * next) * D + lane * PER;
     float v[PER];
@@ -1036,8 +1252,64 @@ __global__ void __launch_bounds__(256) prompt_merge_kernel(const PromptArgs a, c
   for (int k = 0; k < PER; k += 2)
     *reinterpret_cast<uint32_t*>(out + k) = L == 0.f ? 0u : pack2<T>(sum[k] / L, sum[k + 1] / L);
   if (lane == 0 && a.lse)
-    a.lse[a.padded ? ((long long)s * a.Hq + hq) * a.max_q + row : hq * (PAGED ? a.lse_rows : a.total_q) + prow] =
+    a.lse[a.padded ? ((long long)s * a.Hq + hq) * a.max_q + row : hq * a.total_q + prow] =
         L == 0.f ? -INFINITY : (Ms + log2f(L)) * 0.6931471805599453f;
+}
+
+// Paged: joins the partial results of the items that ranges share: blockIdx.y is the CTA in whose range such an item starts, one
+// warp per row of it.
+template <class T, int D>
+__global__ void __launch_bounds__(256) paged_merge_kernel(const PromptArgs a) {
+  constexpr int PER = D / 32;
+  const int lane = threadIdx.x & 31, i = blockIdx.x * 8 + (threadIdx.x >> 5), cta = blockIdx.y;
+  pdl_prologue();
+  const PagedCut c = a.cuts[cta];
+  const int w = i / TILE, r = i - w * TILE, hl = r / a.T, tok = w * a.T + r - hl * a.T;
+  if (!c.valid || hl >= a.P || c.r0 + tok >= c.nq || (c.pair && w)) return;
+  const int parts = c.last - cta + 1;
+  // part 0 ends its CTA's range, the others begin theirs
+  auto place = [&](int p) { return (long long)(2 * (cta + p) + (p == 0)) * a.slot_rows + i; };
+  float M = -INFINITY;
+  for (int p = lane; p < parts; p += 32) {
+    const float x = a.part_lse[place(p)];
+    M = x != x || M != M ? NAN : fmaxf(M, x);
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    const float x = __shfl_xor_sync(0xffffffffu, M, o);
+    M = x != x || M != M ? NAN : fmaxf(M, x);
+  }
+  const float Ms = M == -INFINITY ? 0.f : M;
+  float L = 0.f, sum[PER] = {};
+  for (int p0 = 0; p0 < parts; p0 += 32) {
+    const float weight = p0 + lane < parts ? ex2p(a.part_lse[place(p0 + lane)] - Ms) : 0.f;
+    L += weight;
+    const int n = min(32, parts - p0);
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) {
+      const float f = __shfl_sync(0xffffffffu, weight, p);
+      const float* src = a.part_o + place(p0 + p) * D + lane * PER;
+      float v[PER];
+      if (PER == 4) {
+        const float4 x = *reinterpret_cast<const float4*>(src);
+        v[0] = x.x; v[1] = x.y; v[2 % PER] = x.z; v[3 % PER] = x.w;
+      } else {
+        const float2 x = *reinterpret_cast<const float2*>(src);
+        v[0] = x.x; v[1] = x.y;
+      }
+#pragma unroll
+      for (int k = 0; k < PER; ++k) sum[k] += f * v[k];
+    }
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+  const long long prow = (long long)c.q0 + c.r0 + tok;
+  const int hq = c.h0 + hl;
+  T* out = static_cast<T*>(a.out) + prow * a.out_stride[2] + hq * a.out_stride[1] + lane * PER;
+#pragma unroll
+  for (int k = 0; k < PER; k += 2)
+    *reinterpret_cast<uint32_t*>(out + k) = L == 0.f ? 0u : pack2<T>(sum[k] / L, sum[k + 1] / L);
+  if (lane == 0 && a.lse) a.lse[hq * a.lse_rows + prow] = L == 0.f ? -INFINITY : (Ms + log2f(L)) * 0.6931471805599453f;
 }
 
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
