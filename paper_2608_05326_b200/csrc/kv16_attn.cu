@@ -2,7 +2,7 @@
 //
 // The kernel is the prompt attention's (prompt_attn.cuh) with keys and values by page: a tile of 128 keys is 1 to 8
 // pages, each copied by TMA from where the table says, page after page into the rows that they have in the tile.
-#include "prompt_attn.cuh"
+#include "kv16_few.cuh"
 
 namespace qevict {
 
@@ -10,6 +10,7 @@ namespace {
 
 struct Plan {
   int P, T;       // rows of a query tile: heads, tokens
+  int few;        // rows of a tile in steps of 16 where few_attn_kernel has the call, else 0
   bool by_range;  // equal ranges, else whole items
   bool cuts;      // an item may be shared
   int slot_rows;
@@ -35,6 +36,15 @@ const char* attn_check(const qevict_kv16_attn_args* p, Kv16View* view, qevict_st
   return nullptr;
 }
 
+Plan with_scratch(Plan l, const qevict_kv16_attn_args* p, const Kv16View& c) {
+  if (!l.cuts) return l;
+  const size_t slots = 2 * (size_t)l.ctas * l.slot_rows;
+  l.cut_bytes = ((size_t)l.ctas * sizeof(PagedCut) + 255) & ~(size_t)255;
+  l.o_bytes = slots * c.D * sizeof(float);
+  l.bytes = l.cut_bytes + l.o_bytes + slots * sizeof(float);
+  return l;
+}
+
 // Equal ranges of the work for all SMs; a call of many items (six for each SM, by its rows) hands out whole ones as SMs fall free,
 // longest first: CTAs that work on one head then walk its keys together, and the L2 serves most of them.
 Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
@@ -45,7 +55,18 @@ Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
   const long long max_q = p->max_q < p->total_q ? p->max_q : p->total_q;
   const long long rows = p->cu_q ? p->total_q : (p->total_q < c.n_seqs ? p->total_q : c.n_seqs);
   const long long groups = p->n_q_heads / l.P, items = prompt_tiles(false, c.n_seqs, max_q, rows, l.T) * groups;
-  const int sms = prompt_sms(p->cache->device);
+  const int sms = prompt_sms(p->cache->device), group = p->n_q_heads / c.Hkv;
+  if (group * max_q <= 32) {
+    l.few = group * max_q <= 16 ? 1 : 2;
+    l.P = group;
+    l.T = max_q > 0 ? (int)max_q : 1;
+    l.by_range = true;
+    const long long most = c.n_seqs * (long long)c.Hkv * (KEY_COST * longest + FEW_ITEM_COST) / FEW_RANGE_LEAST + 1, room = (long long)sms * (l.few == 1 ? 3 : 2);
+    l.ctas = (unsigned)(most < room ? most : room);
+    l.cuts = longest > FEW_KEYS && l.ctas > 1;
+    l.slot_rows = 16 * l.few;
+    return with_scratch(l, p, c);
+  }
   l.by_range = rows / (2 * l.T) * groups < 6 * sms;
   if (!l.by_range) {
     l.ctas = items <= (1ll << 28) ? (unsigned)items : 0u;
@@ -54,13 +75,8 @@ Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
   const long long most = items * (KEY_COST * longest + ITEM_COST) / RANGE_LEAST + 1;
   l.ctas = (unsigned)(most < sms ? most : sms);
   l.cuts = longest > TILE && l.ctas > 1;
-  if (!l.cuts) return l;
   l.slot_rows = max_q <= l.T ? TILE : 2 * TILE;
-  const size_t slots = 2 * (size_t)l.ctas * l.slot_rows;
-  l.cut_bytes = ((size_t)l.ctas * sizeof(PagedCut) + 255) & ~(size_t)255;
-  l.o_bytes = slots * c.D * sizeof(float);
-  l.bytes = l.cut_bytes + l.o_bytes + slots * sizeof(float);
-  return l;
+  return with_scratch(l, p, c);
 }
 
 // A page's rows of a head by one copy of {64 channels, 8 tokens, d / 64 pieces, block / 8 groups}, which lands group by group with
@@ -92,6 +108,19 @@ const char* attn_check_pointers(const qevict_kv16_attn_args* p) {
       bad_stride(p->out_stride[1], p->n_q_heads))
     return "strides must be positive multiples of 16 bytes";
   return nullptr;
+}
+
+template <class T, int D, int MT>
+cudaError_t launch_few(const PromptArgs& a, const Plan& l, const FewPages& g, int device, cudaStream_t s) {
+  auto kernel = few_attn_kernel<T, D, MT>;
+  static std::atomic<uint64_t> done{0};
+  cudaError_t e = once_per_device(done, device, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem<D, MT>()); });
+  if (e == cudaSuccess) e = launch_pdl(kernel, dim3(l.ctas), dim3(32 * FEW_WARPS), few_smem<D, MT>(), s, a, g);
+  if (e == cudaSuccess && l.cuts) e = launch_pdl(paged_merge_kernel<T, D>, dim3(l.slot_rows / 8, l.ctas), dim3(256), 0, s, a);
+  return e;
+}
+template <class T, int D> cudaError_t launch_few_rows(const PromptArgs& a, const Plan& l, const FewPages& g, int device, cudaStream_t s) {
+  return l.few == 1 ? launch_few<T, D, 1>(a, l, g, device, s) : launch_few<T, D, 2>(a, l, g, device, s);
 }
 
 template <class T, int D>
@@ -168,13 +197,28 @@ QEVICT_API qevict_status qevict_kv16_attn(const qevict_kv16_attn_args* p, void* 
   DeviceGuard guard(c->device);
   cudaError_t e = guard.err;
   if (e != cudaSuccess) return stateless_fail(QEVICT_ERR_CUDA, cudaGetErrorString(e));
+  cudaStream_t s = (cudaStream_t)stream;
+  if (l.few) {
+    FewPages g = {};
+    for (int w = 0; w < 2; ++w) {
+      g.pages[w] = view.pages[w];
+      for (int i = 0; i < 3; ++i) g.stride[w][i] = view.stride[w][i];
+      g.q_stride[w] = p->q_stride[w];
+    }
+    g.q = p->q;
+    if (c->dtype == QEVICT_DTYPE_FP16)
+      e = a.D == 128 ? launch_few_rows<__half, 128>(a, l, g, c->device, s) : launch_few_rows<__half, 64>(a, l, g, c->device, s);
+    else
+      e = a.D == 128 ? launch_few_rows<__nv_bfloat16, 128>(a, l, g, c->device, s) : launch_few_rows<__nv_bfloat16, 64>(a, l, g, c->device, s);
+    if (e != cudaSuccess) return stateless_fail(QEVICT_ERR_CUDA, cudaGetErrorString(e));
+    return QEVICT_OK;
+  }
   CUtensorMap mq, mk, mv;
   const int64_t q_stride[3] = {0, p->q_stride[1], p->q_stride[0]};
   if (!make_map(&mq, c->dtype, p->q, a.D, p->total_q, a.Hq, 1, q_stride, a.T, a.P) ||
       !make_page_map(&mk, c, c->k_pages, c->k_stride, whole, &a.head_step[0]) ||
       !make_page_map(&mv, c, c->v_pages, c->v_stride, whole, &a.head_step[1]))
     return stateless_fail(QEVICT_ERR_CUDA, "a tensor map could not be made for q or the pages");
-  cudaStream_t s = (cudaStream_t)stream;
   if (c->dtype == QEVICT_DTYPE_FP16)
     e = a.D == 128 ? launch_paged<__half, 128>(a, l, mq, mk, mv, c->device, s) : launch_paged<__half, 64>(a, l, mq, mk, mv, c->device, s);
   else

@@ -271,14 +271,14 @@ struct PromptItem {
   __device__ __forceinline__ bool dirty() const { return n > lo && n * TILE > nk; }  // the first tile reaches past the sequence
 };
 
-// Key tiles that an item's two query tiles see.
-__device__ __forceinline__ void item_tiles(const PromptArgs& a, PromptItem* it) {
+// Key tiles (of KT keys) that an item's two query tiles see.
+template <int KT = TILE> __device__ __forceinline__ void item_tiles(const PromptArgs& a, PromptItem* it) {
   int nt[2];
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
     const int rw = it->r0 + w * a.T, last = min(rw + a.T, it->nq) - 1;
     const int lim = rw >= it->nq ? 0 : (a.causal ? min(it->nk, last + it->nk - it->nq + 1) : it->nk);
-    nt[w] = lim > 0 ? (lim + TILE - 1) / TILE : 0;
+    nt[w] = lim > 0 ? (lim + KT - 1) / KT : 0;
   }
   it->lo = 0;
   it->n = max(nt[0], nt[1]);
@@ -382,8 +382,8 @@ struct PagedSeq {
     if (u > full) u = full;
     return (full - u) * p + step * (full * (full + 1) - u * (u + 1)) / 2 + (t < tiles ? 0 : nk);
   }
-  __device__ __forceinline__ long long cost(const PromptArgs& a, int t) const { return (long long)key_cost * keys(a, t) + ITEM_COST; }
-  __device__ __forceinline__ long long cost_before(const PromptArgs& a, int t) const { return t > 0 ? key_cost * before(a, t) + (long long)t * ITEM_COST : 0; }
+  template <int ITEM> __device__ __forceinline__ long long cost(const PromptArgs& a, int t) const { return (long long)key_cost * keys(a, t) + ITEM; }
+  template <int ITEM> __device__ __forceinline__ long long cost_before(const PromptArgs& a, int t) const { return t > 0 ? key_cost * before(a, t) + (long long)t * ITEM : 0; }
 };
 
 __device__ __forceinline__ PagedSeq paged_seq(const PromptArgs& a, int s) {
@@ -398,7 +398,11 @@ __device__ __forceinline__ PagedSeq paged_seq(const PromptArgs& a, int s) {
   return q;
 }
 
-struct PagedRange {
+// floor(x / y) for 0 <= x < 2^53: the quotient's distance from a whole number above it is at least 1 / y, more than it is rounded by
+__device__ __forceinline__ long long quotient(long long x, long long y) { return (long long)((double)x / (double)y); }
+
+// KT: keys of a tile; ITEM: what an item costs beside its keys; LEAST: least width of a range
+template <int KT, int ITEM = ITEM_COST, int LEAST = RANGE_LEAST> struct PagedRange {
   long long width, lo, hi, at;  // this CTA's part of the sum; start of the current item
   int s, h, t;
   PagedSeq seq;
@@ -408,12 +412,12 @@ struct PagedRange {
     long long sum = 0;
     for (int i = lane; i < a.n_seqs; i += 32) {
       const PagedSeq q = paged_seq(a, i);
-      sum += q.cost_before(a, q.tiles) * groups;
+      sum += q.template cost_before<ITEM>(a, q.tiles) * groups;
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    width = (sum + gridDim.x - 1) / gridDim.x;
-    if (width < RANGE_LEAST) width = RANGE_LEAST;
+    width = quotient(sum + gridDim.x - 1, gridDim.x);
+    if (width < LEAST) width = LEAST;
     lo = blockIdx.x * width;
     hi = lo + width < sum ? lo + width : sum;
     s = a.n_seqs;
@@ -421,7 +425,7 @@ struct PagedRange {
     long long front = 0;  // cost of the sequences before
     for (int i = 0; i < a.n_seqs; i += 32) {
       const PagedSeq q = paged_seq(a, i + lane);
-      const long long mine = q.cost_before(a, q.tiles) * groups;
+      const long long mine = q.template cost_before<ITEM>(a, q.tiles) * groups;
       long long upto = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -438,30 +442,29 @@ struct PagedRange {
       front += __shfl_sync(0xffffffffu, upto, 31);
     }
     seq = paged_seq(a, s);
-    const long long head = seq.cost_before(a, seq.tiles);
-    h = (int)((lo - front) / head);
+    const long long head = seq.template cost_before<ITEM>(a, seq.tiles);
+    h = (int)quotient(lo - front, head);
     front += h * head;
     int t0 = 0, t1 = seq.tiles - 1;  // the last tile that starts at or before lo
     while (t0 < t1) {
       const int mid = (t0 + t1 + 1) >> 1;
-      if (front + seq.cost_before(a, mid) <= lo) t0 = mid; else t1 = mid - 1;
+      if (front + seq.template cost_before<ITEM>(a, mid) <= lo) t0 = mid; else t1 = mid - 1;
     }
     t = t0;
-    at = front + seq.cost_before(a, t);
+    at = front + seq.template cost_before<ITEM>(a, t);
   }
 
   // The next item of the range, its key tiles in it; false behind the last one.
   __device__ __forceinline__ bool next(const PromptArgs& a, int lane, PromptItem* it) {
     while (s < a.n_seqs && at < hi) {
-      const long long cost = seq.cost(a, t), end = at + cost;
+      const long long cost = seq.template cost<ITEM>(a, t), end = at + cost;
       it->valid = 1;
       it->s = s; it->h0 = h * a.P; it->r0 = t * 2 * a.T;
       it->q0 = seq.q0; it->nq = seq.nq; it->k0 = 0; it->nk = seq.nk;
       it->split = 0;
-      item_tiles(a, it);
+      item_tiles<KT>(a, it);
       const int all = it->n;
-      const long long tile = (long long)seq.key_cost * TILE;
-      auto tiles_upto = [&](long long x) { return x <= at + ITEM_COST ? 0 : (int)((x - at - ITEM_COST) / tile); };
+      auto tiles_upto = [&](long long x) { return x <= at + ITEM ? 0 : (int)quotient(x - at - ITEM, seq.key_cost * KT); };
       const int f0 = lo > at ? tiles_upto(lo) : 0;
       const bool ends = end <= hi;
       const int f1 = ends ? all : tiles_upto(hi);
@@ -469,7 +472,7 @@ struct PagedRange {
       it->n = f1;
       it->slot = f0 == 0 && ends ? -1 : 2 * (int)blockIdx.x + (f0 == 0);
       if (f0 == 0 && f1 > 0 && !ends && lane == 0) {
-        const PagedCut c = {1, s, it->h0, it->r0, seq.q0, seq.nq, (int)((end - 1) / width), paged_pair(a, seq.nq, seq.nk)};
+        const PagedCut c = {1, s, it->h0, it->r0, seq.q0, seq.nq, (int)quotient(end - 1, width), paged_pair(a, seq.nq, seq.nk)};
         a.cuts[blockIdx.x] = c;
       }
       at = end;
@@ -598,7 +601,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       if (PAGED && a.by_range) {
         checks = blockIdx.x == 0;
         if (a.cuts && lane == 0) a.cuts[blockIdx.x].valid = 0;
-        PagedRange range(a, lane);
+        PagedRange<TILE> range(a, lane);
         PromptItem it;
         while (ok && range.next(a, lane, &it)) {
           it.before = k_tiles;
@@ -1194,7 +1197,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
     };
     if (PAGED && a.by_range) {
       if (wid == ITEM_WARP) {
-        PagedRange range(a, lane);
+        PagedRange<TILE> range(a, lane);
         PromptItem it;
         while (range.next(a, lane, &it)) lose(it, lane, 32);
       }
