@@ -8,9 +8,12 @@ namespace qevict {
 
 namespace {
 
+constexpr int FEW_CLUSTER_KEYS = 1024;
+
 struct Plan {
   int P, T;       // rows of a query tile: heads, tokens
-  int few;        // rows of a tile in steps of 16 where few_attn_kernel has the call, else 0
+  bool few;       // few_attn_kernel has the call
+  int ranks;      // CTAs of a cluster that has a sequence's KV head, else 0
   bool by_range;  // equal ranges, else whole items
   bool cuts;      // an item may be shared
   int slot_rows;
@@ -56,15 +59,20 @@ Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
   const long long rows = p->cu_q ? p->total_q : (p->total_q < c.n_seqs ? p->total_q : c.n_seqs);
   const long long groups = p->n_q_heads / l.P, items = prompt_tiles(false, c.n_seqs, max_q, rows, l.T) * groups;
   const int sms = prompt_sms(p->cache->device), group = p->n_q_heads / c.Hkv;
-  if (group * max_q <= 32) {
-    l.few = group * max_q <= 16 ? 1 : 2;
+  if (group * max_q <= FEW_ROWS) {
+    l.few = true;
     l.P = group;
     l.T = max_q > 0 ? (int)max_q : 1;
+    const long long room = (long long)sms * FEW_CTAS, units = c.n_seqs * (long long)c.Hkv;
+    // up to 16 CTAs for each unit where that fills no more than one wave and none has more than FEW_CLUSTER_KEYS keys
+    for (int ranks = 1; ranks <= 16; ranks *= 2)
+      if (units * ranks <= room && longest <= (long long)ranks * FEW_CLUSTER_KEYS && (ranks == 1 || ranks <= longest / (FEW_WARPS * FEW_KEYS))) l.ranks = ranks;
+    if (l.ranks) return l;
     l.by_range = true;
-    const long long most = c.n_seqs * (long long)c.Hkv * (KEY_COST * longest + FEW_ITEM_COST) / FEW_RANGE_LEAST + 1, room = (long long)sms * (l.few == 1 ? 3 : 2);
+    const long long most = units * (KEY_COST * longest + FEW_ITEM_COST) / FEW_RANGE_LEAST + 1;
     l.ctas = (unsigned)(most < room ? most : room);
     l.cuts = longest > FEW_KEYS && l.ctas > 1;
-    l.slot_rows = 16 * l.few;
+    l.slot_rows = FEW_ROWS;
     return with_scratch(l, p, c);
   }
   l.by_range = rows / (2 * l.T) * groups < 6 * sms;
@@ -110,19 +118,38 @@ const char* attn_check_pointers(const qevict_kv16_attn_args* p) {
   return nullptr;
 }
 
-template <class T, int D, int MT>
+template <class T, int D>
 cudaError_t launch_few(const PromptArgs& a, const Plan& l, const FewPages& g, int device, cudaStream_t s) {
-  auto kernel = few_attn_kernel<T, D, MT>;
+  if (l.ranks) {
+    auto kernel = few_attn_kernel<T, D, true>;
+    static std::atomic<uint64_t> done{0};
+    cudaError_t e = once_per_device(done, device, [&] {
+      const cudaError_t e0 = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem(D));
+      return e0 != cudaSuccess ? e0 : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    });
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(l.ranks * a.Hkv, a.n_seqs);
+    cfg.blockDim = dim3(32 * FEW_WARPS);
+    cfg.dynamicSmemBytes = few_smem(D);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = l.ranks;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, a, g);
+  }
+  auto kernel = few_attn_kernel<T, D, false>;
   static std::atomic<uint64_t> done{0};
-  cudaError_t e = once_per_device(done, device, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem<D, MT>()); });
-  if (e == cudaSuccess) e = launch_pdl(kernel, dim3(l.ctas), dim3(32 * FEW_WARPS), few_smem<D, MT>(), s, a, g);
+  cudaError_t e = once_per_device(done, device, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem(D)); });
+  if (e == cudaSuccess) e = launch_pdl(kernel, dim3(l.ctas), dim3(32 * FEW_WARPS), few_smem(D), s, a, g);
   if (e == cudaSuccess && l.cuts) e = launch_pdl(paged_merge_kernel<T, D>, dim3(l.slot_rows / 8, l.ctas), dim3(256), 0, s, a);
   return e;
 }
-template <class T, int D> cudaError_t launch_few_rows(const PromptArgs& a, const Plan& l, const FewPages& g, int device, cudaStream_t s) {
-  return l.few == 1 ? launch_few<T, D, 1>(a, l, g, device, s) : launch_few<T, D, 2>(a, l, g, device, s);
-}
-
 template <class T, int D>
 cudaError_t launch_paged(const PromptArgs& a, const Plan& l, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, int device, cudaStream_t s) {
   auto kernel = prompt_attn_kernel<T, D, true>;
@@ -160,7 +187,7 @@ QEVICT_API qevict_status qevict_kv16_attn(const qevict_kv16_attn_args* p, void* 
   why = attn_check_pointers(p);
   if (why) return stateless_fail(QEVICT_ERR_INVALID_ARG, why);
   const Plan l = attn_plan(p, view);
-  if (l.ctas == 0) return stateless_fail(QEVICT_ERR_UNSUPPORTED, "more than 2^28 work items in one call");
+  if (l.ctas == 0 && !l.ranks) return stateless_fail(QEVICT_ERR_UNSUPPORTED, "more than 2^28 work items in one call");
   if (l.bytes > 0 && (!scratch || scratch_bytes < l.bytes))
     return stateless_fail(QEVICT_ERR_NO_MEMORY, "scratch too small: see qevict_kv16_attn_scratch_bytes");
   if (l.bytes > 0 && misaligned16(scratch)) return stateless_fail(QEVICT_ERR_INVALID_ARG, "scratch must be 16-byte aligned");
@@ -207,9 +234,9 @@ QEVICT_API qevict_status qevict_kv16_attn(const qevict_kv16_attn_args* p, void* 
     }
     g.q = p->q;
     if (c->dtype == QEVICT_DTYPE_FP16)
-      e = a.D == 128 ? launch_few_rows<__half, 128>(a, l, g, c->device, s) : launch_few_rows<__half, 64>(a, l, g, c->device, s);
+      e = a.D == 128 ? launch_few<__half, 128>(a, l, g, c->device, s) : launch_few<__half, 64>(a, l, g, c->device, s);
     else
-      e = a.D == 128 ? launch_few_rows<__nv_bfloat16, 128>(a, l, g, c->device, s) : launch_few_rows<__nv_bfloat16, 64>(a, l, g, c->device, s);
+      e = a.D == 128 ? launch_few<__nv_bfloat16, 128>(a, l, g, c->device, s) : launch_few<__nv_bfloat16, 64>(a, l, g, c->device, s);
     if (e != cudaSuccess) return stateless_fail(QEVICT_ERR_CUDA, cudaGetErrorString(e));
     return QEVICT_OK;
   }

@@ -386,32 +386,44 @@ struct PagedSeq {
   template <int ITEM> __device__ __forceinline__ long long cost_before(const PromptArgs& a, int t) const { return t > 0 ? key_cost * before(a, t) + (long long)t * ITEM : 0; }
 };
 
-__device__ __forceinline__ PagedSeq paged_seq(const PromptArgs& a, int s) {
-  PagedSeq q = {0, 0, 0, 0, 0};
-  int k0;
-  if (s < a.n_seqs) {
-    q_span<true>(a, s, &q.q0, &q.nq);
-    k_span<true>(a, s, &k0, &q.nk);
-    q.tiles = (q.nq + 2 * a.T - 1) / (2 * a.T);
-    q.key_cost = paged_pair(a, q.nq, q.nk) ? KEY_COST_PAIR : KEY_COST;
-  }
-  return q;
+__device__ __forceinline__ PagedSeq paged_seq(const PromptArgs& a, int q0, int nq, int nk) {
+  return {q0, nq, nk, (nq + 2 * a.T - 1) / (2 * a.T), paged_pair(a, nq, nk) ? KEY_COST_PAIR : KEY_COST};
 }
 
 // floor(x / y) for 0 <= x < 2^53: the quotient's distance from a whole number above it is at least 1 / y, more than it is rounded by
-__device__ __forceinline__ long long quotient(long long x, long long y) { return (long long)((double)x / (double)y); }
+__device__ __forceinline__ long long quotient(long long x, long long y) {
+  if (((unsigned long long)x | (unsigned long long)y) >> 32 == 0) return (uint32_t)x / (uint32_t)y;
+  return (long long)((double)x / (double)y);
+}
 
 // KT: keys of a tile; ITEM: what an item costs beside its keys; LEAST: least width of a range
 template <int KT, int ITEM = ITEM_COST, int LEAST = RANGE_LEAST> struct PagedRange {
   long long width, lo, hi, at;  // this CTA's part of the sum; start of the current item
   int s, h, t;
   PagedSeq seq;
+  int lane_q0, lane_nq, lane_nk, first;  // the lane's sequence of 32, of which `first` is the first
+
+  __device__ __forceinline__ PagedSeq look(const PromptArgs& a, int s0, int lane) {
+    int k0;
+    lane_q0 = lane_nq = lane_nk = 0;
+    first = s0;
+    if (s0 + lane < a.n_seqs) {
+      q_span<true>(a, s0 + lane, &lane_q0, &lane_nq);
+      k_span<true>(a, s0 + lane, &k0, &lane_nk);
+    }
+    return paged_seq(a, lane_q0, lane_nq, lane_nk);
+  }
+  __device__ __forceinline__ PagedSeq sequence(const PromptArgs& a, int s, int lane) {  // of the whole warp
+    if (s >= first + 32) look(a, s & ~31, lane);
+    return paged_seq(a, __shfl_sync(0xffffffffu, lane_q0, s & 31), __shfl_sync(0xffffffffu, lane_nq, s & 31),
+                     __shfl_sync(0xffffffffu, lane_nk, s & 31));
+  }
 
   __device__ __forceinline__ PagedRange(const PromptArgs& a, int lane) {
     const int groups = a.Hq / a.P;
     long long sum = 0;
-    for (int i = lane; i < a.n_seqs; i += 32) {
-      const PagedSeq q = paged_seq(a, i);
+    for (int i = 0; i < a.n_seqs; i += 32) {
+      const PagedSeq q = look(a, i, lane);
       sum += q.template cost_before<ITEM>(a, q.tiles) * groups;
     }
 #pragma unroll
@@ -424,7 +436,7 @@ template <int KT, int ITEM = ITEM_COST, int LEAST = RANGE_LEAST> struct PagedRan
     if (lo >= sum) return;
     long long front = 0;  // cost of the sequences before
     for (int i = 0; i < a.n_seqs; i += 32) {
-      const PagedSeq q = paged_seq(a, i + lane);
+      const PagedSeq q = a.n_seqs > 32 ? look(a, i, lane) : paged_seq(a, lane_q0, lane_nq, lane_nk);
       const long long mine = q.template cost_before<ITEM>(a, q.tiles) * groups;
       long long upto = mine;
 #pragma unroll
@@ -441,7 +453,7 @@ template <int KT, int ITEM = ITEM_COST, int LEAST = RANGE_LEAST> struct PagedRan
       }
       front += __shfl_sync(0xffffffffu, upto, 31);
     }
-    seq = paged_seq(a, s);
+    seq = sequence(a, s, lane);
     const long long head = seq.template cost_before<ITEM>(a, seq.tiles);
     h = (int)quotient(lo - front, head);
     front += h * head;
@@ -455,7 +467,7 @@ template <int KT, int ITEM = ITEM_COST, int LEAST = RANGE_LEAST> struct PagedRan
   }
 
   // The next item of the range, its key tiles in it; false behind the last one.
-  __device__ __forceinline__ bool next(const PromptArgs& a, int lane, PromptItem* it) {
+  __device__ __forceinline__ bool next(const PromptArgs& a, int lane, bool writes, PromptItem* it) {
     while (s < a.n_seqs && at < hi) {
       const long long cost = seq.template cost<ITEM>(a, t), end = at + cost;
       it->valid = 1;
@@ -471,7 +483,7 @@ template <int KT, int ITEM = ITEM_COST, int LEAST = RANGE_LEAST> struct PagedRan
       it->lo = f0;
       it->n = f1;
       it->slot = f0 == 0 && ends ? -1 : 2 * (int)blockIdx.x + (f0 == 0);
-      if (f0 == 0 && f1 > 0 && !ends && lane == 0) {
+      if (f0 == 0 && f1 > 0 && !ends && writes) {
         const PagedCut c = {1, s, it->h0, it->r0, seq.q0, seq.nq, (int)quotient(end - 1, width), paged_pair(a, seq.nq, seq.nk)};
         a.cuts[blockIdx.x] = c;
       }
@@ -480,7 +492,9 @@ template <int KT, int ITEM = ITEM_COST, int LEAST = RANGE_LEAST> struct PagedRan
         t = 0;
         if (++h == a.Hq / a.P) {
           h = 0;
-          do { seq = paged_seq(a, ++s); } while (s < a.n_seqs && seq.tiles == 0);
+          do {
+            if (++s < a.n_seqs) seq = sequence(a, s, lane);
+          } while (s < a.n_seqs && seq.tiles == 0);
         }
       }
       if (f1 > f0 || (all == 0 && ends)) {
@@ -603,7 +617,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         if (a.cuts && lane == 0) a.cuts[blockIdx.x].valid = 0;
         PagedRange<TILE> range(a, lane);
         PromptItem it;
-        while (ok && range.next(a, lane, &it)) {
+        while (ok && range.next(a, lane, lane == 0, &it)) {
           it.before = k_tiles;
           k_tiles += it.n - it.lo;
           hand_out(it);
@@ -1199,7 +1213,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       if (wid == ITEM_WARP) {
         PagedRange<TILE> range(a, lane);
         PromptItem it;
-        while (range.next(a, lane, &it)) lose(it, lane, 32);
+        while (range.next(a, lane, lane == 0, &it)) lose(it, lane, 32);
       }
     } else {
       for (int n = 0; n < 4; ++n) lose(items[n], tid, PROMPT_THREADS);
