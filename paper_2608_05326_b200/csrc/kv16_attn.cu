@@ -2,6 +2,7 @@
 //
 // The kernel is the prompt attention's (prompt_attn.cuh) with keys and values by page: a tile of 128 keys is 1 to 8
 // pages, each copied by TMA from where the table says, page after page into the rows that they have in the tile.
+#include <stdlib.h>
 #include "kv16_few.cuh"
 
 namespace qevict {
@@ -59,17 +60,18 @@ Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
   const long long rows = p->cu_q ? p->total_q : (p->total_q < c.n_seqs ? p->total_q : c.n_seqs);
   const long long groups = p->n_q_heads / l.P, items = prompt_tiles(false, c.n_seqs, max_q, rows, l.T) * groups;
   const int sms = prompt_sms(p->cache->device), group = p->n_q_heads / c.Hkv;
-  if (group * max_q <= FEW_ROWS) {
+  const long long units = c.n_seqs * (long long)c.Hkv, steps = (longest + FEW_KEYS - 1) / FEW_KEYS + FEW_ITEM_COST;
+  if (group * max_q <= FEW_ROWS && units * steps < (1ll << 30)) {
     l.few = true;
     l.P = group;
     l.T = max_q > 0 ? (int)max_q : 1;
-    const long long room = (long long)sms * FEW_CTAS, units = c.n_seqs * (long long)c.Hkv;
+    const long long room = (long long)sms * FEW_CTAS;
     // up to 16 CTAs for each unit where that fills no more than one wave and none has more than FEW_CLUSTER_KEYS keys
     for (int ranks = 1; ranks <= 16; ranks *= 2)
       if (units * ranks <= room && longest <= (long long)ranks * FEW_CLUSTER_KEYS && (ranks == 1 || ranks <= longest / (FEW_WARPS * FEW_KEYS))) l.ranks = ranks;
     if (l.ranks) return l;
     l.by_range = true;
-    const long long most = units * (KEY_COST * longest + FEW_ITEM_COST) / FEW_RANGE_LEAST + 1;
+    const long long most = units * steps / FEW_RANGE_LEAST + 1;
     l.ctas = (unsigned)(most < room ? most : room);
     l.cuts = longest > FEW_KEYS && l.ctas > 1;
     l.slot_rows = FEW_ROWS;
@@ -118,13 +120,21 @@ const char* attn_check_pointers(const qevict_kv16_attn_args* p) {
   return nullptr;
 }
 
+// Shared memory for FEW_CTAS on an SM, the rest for the L1: a load on its way has its place there
+template <class K> cudaError_t few_attributes(K kernel, int smem) {
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  int pct = 45;
+  if (const char* x = getenv("QX")) pct = atoi(x);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, pct);
+}
+
 template <class T, int D>
 cudaError_t launch_few(const PromptArgs& a, const Plan& l, const FewPages& g, int device, cudaStream_t s) {
   if (l.ranks) {
     auto kernel = few_attn_kernel<T, D, true>;
     static std::atomic<uint64_t> done{0};
     cudaError_t e = once_per_device(done, device, [&] {
-      const cudaError_t e0 = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem(D));
+      const cudaError_t e0 = few_attributes(kernel, few_smem(D));
       return e0 != cudaSuccess ? e0 : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     });
     if (e != cudaSuccess) return e;
@@ -145,7 +155,7 @@ cudaError_t launch_few(const PromptArgs& a, const Plan& l, const FewPages& g, in
   }
   auto kernel = few_attn_kernel<T, D, false>;
   static std::atomic<uint64_t> done{0};
-  cudaError_t e = once_per_device(done, device, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem(D)); });
+  cudaError_t e = once_per_device(done, device, [&] { return few_attributes(kernel, few_smem(D)); });
   if (e == cudaSuccess) e = launch_pdl(kernel, dim3(l.ctas), dim3(32 * FEW_WARPS), few_smem(D), s, a, g);
   if (e == cudaSuccess && l.cuts) e = launch_pdl(paged_merge_kernel<T, D>, dim3(l.slot_rows / 8, l.ctas), dim3(256), 0, s, a);
   return e;

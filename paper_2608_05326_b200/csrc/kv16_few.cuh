@@ -10,8 +10,7 @@
 //   - A lane has 16 bytes of two neighbouring keys' values; byte permutes pair them, and the output's columns come in the order
 //     that this gives (channel 8 n + e is column n of step e).
 //   - Keys past the end and blocks that are not there are not read; their operands are zero and their logits masked.
-// How the keys are shared: a call with many keys gives each CTA an equal range of its work (PagedRange, 16 keys at a
-// time) and joins what ranges share in a second launch; a call that one wave of clusters holds gives each (sequence, KV
+// How the keys are shared: a call with many keys gives each CTA an equal range of its work (FewRange) and joins what ranges share in a second launch; a call that one wave of clusters holds gives each (sequence, KV
 // head) a cluster of CTAs, which join their sums through each other's shared memory.
 #pragma once
 
@@ -22,9 +21,9 @@ namespace qevict {
 namespace {
 
 constexpr int FEW_WARPS = 4, FEW_KEYS = 16;
-constexpr int FEW_ITEM_COST = 256, FEW_RANGE_LEAST = 512;
+constexpr int FEW_ITEM_COST = 5, FEW_RANGE_LEAST = 8;  // steps of 16 keys
 constexpr int FEW_ROWS = 16, FEW_CTAS = 3;  // of an SM: 168 registers a thread
-constexpr int few_smem(int D) { return (FEW_WARPS * (D + 8) + D) * FEW_ROWS * 4 + D / 32 * 1024 + (FEW_WARPS + 1) * FEW_ROWS * 8; }
+constexpr int few_smem(int D) { return (FEW_WARPS * 72 + D) * FEW_ROWS * 4 + D / 32 * 1024 + (FEW_WARPS + 1) * FEW_ROWS * 8; }
 
 __device__ __forceinline__ uint4 ld_page16(const void* p) {
   uint4 r;
@@ -56,13 +55,99 @@ struct FewPages {
   long long q_stride[2];  // token, head
 };
 
+// A CTA's equal range of the work: the sequences' KV heads stand in a row, each of its steps and FEW_ITEM_COST more.  An end inside a
+// KV head's constant is moved to its first step.  (The host sees to it that the sum fits 31 bits.)
+struct FewRange {
+  uint32_t width, lo, hi, at;  // this CTA's part of the sum; start of the current item
+  int s, h, q0, nq, nk;
+  int lane_q0, lane_nq, lane_nk, first;  // the lane's sequence of 32, of which `first` is the first
+
+  static __device__ __forceinline__ uint32_t cost(int nq, int nk) { return nq > 0 ? (nk + FEW_KEYS - 1) / FEW_KEYS + FEW_ITEM_COST : 0; }
+  __device__ __forceinline__ uint32_t look(const PromptArgs& a, int s0, int lane) {  // work of the lane's sequence
+    int k0;
+    lane_q0 = lane_nq = lane_nk = 0;
+    first = s0;
+    if (s0 + lane < a.n_seqs) {
+      q_span<true>(a, s0 + lane, &lane_q0, &lane_nq);
+      k_span<true>(a, s0 + lane, &k0, &lane_nk);
+    }
+    return cost(lane_nq, lane_nk) * a.Hkv;
+  }
+  __device__ __forceinline__ void sequence(const PromptArgs& a, int lane) {
+    if (s >= first + 32) look(a, s & ~31, lane);
+    q0 = __shfl_sync(0xffffffffu, lane_q0, s & 31);
+    nq = __shfl_sync(0xffffffffu, lane_nq, s & 31);
+    nk = __shfl_sync(0xffffffffu, lane_nk, s & 31);
+  }
+  __device__ __forceinline__ FewRange(const PromptArgs& a, int lane) {
+    uint32_t sum = 0, mine = 0;
+    for (int i = 0; i < a.n_seqs; i += 32) {
+      mine = look(a, i, lane);
+      sum += __reduce_add_sync(0xffffffffu, mine);
+    }
+    width = (sum + gridDim.x - 1) / gridDim.x;
+    if (width < FEW_RANGE_LEAST) width = FEW_RANGE_LEAST;
+    lo = blockIdx.x * width;
+    hi = min(lo + width, sum);
+    s = a.n_seqs;
+    if (lo >= sum) return;
+    uint32_t front = 0;  // work of the sequences before
+    for (int i = 0;; i += 32) {
+      if (a.n_seqs > 32) mine = look(a, i, lane);
+      uint32_t upto = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, front + upto > lo);
+      if (past) {
+        const int who = __ffs(past) - 1;
+        s = i + who;
+        front += __shfl_sync(0xffffffffu, upto - mine, who);
+        break;
+      }
+      front += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    sequence(a, lane);
+    h = (lo - front) / cost(nq, nk);
+    at = front + h * cost(nq, nk);
+  }
+  // The next item, its steps in the range; false behind the last one.
+  __device__ __forceinline__ bool next(const PromptArgs& a, int lane, bool writes, PromptItem* it) {
+    while (s < a.n_seqs && at < hi) {
+      const uint32_t end = at + cost(nq, nk);
+      const int all = (nk + FEW_KEYS - 1) / FEW_KEYS;
+      auto steps_upto = [&](uint32_t x) { return x <= at + FEW_ITEM_COST ? 0 : (int)(x - at - FEW_ITEM_COST); };
+      const bool ends = end <= hi;
+      it->s = s; it->h0 = h * a.P; it->q0 = q0; it->nq = nq; it->nk = nk;
+      it->lo = lo > at ? steps_upto(lo) : 0;
+      it->n = ends ? all : steps_upto(hi);
+      it->slot = it->lo == 0 && ends ? -1 : 2 * (int)blockIdx.x + (it->lo == 0);
+      if (it->lo == 0 && it->n > 0 && !ends && writes) {
+        const PagedCut c = {1, s, it->h0, 0, q0, nq, (int)((end - 1) / width), 0};
+        a.cuts[blockIdx.x] = c;
+      }
+      at = end;
+      if (++h == a.Hkv) {
+        h = 0;
+        do {
+          if (++s < a.n_seqs) sequence(a, lane);
+        } while (s < a.n_seqs && nq == 0);
+      }
+      if (it->n > it->lo || (all == 0 && ends)) return true;
+    }
+    return false;
+  }
+};
+
 // CLUSTER: blockIdx is (KV head * ranks + rank, sequence)
 template <class T, int D, bool CLUSTER>
 __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ FewPages g) {
   constexpr int J = D / 32;       // 16-byte pieces of a key in a lane
   constexpr int H = D / 64;       // of a value
   constexpr int N = D / 8;        // column steps of the output
-  constexpr int LINE = D + 8;     // floats from row to row of a warp's output
+  constexpr int LINE = 64 + 8;    // floats from row to row of a warp's output, 64 channels at a time
   extern __shared__ __align__(16) unsigned char few_sm[];
   auto os = reinterpret_cast<float (*)[FEW_ROWS][LINE]>(few_sm);                    // outputs: the warps', [FEW_WARPS]
   auto mine = reinterpret_cast<float (*)[D]>(os + FEW_WARPS);                       // the CTA's, [FEW_ROWS]
@@ -73,7 +158,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(cons
   if (!CLUSTER && a.cuts && tid == 0) a.cuts[blockIdx.x].valid = 0;
 
   // keys f0 * 16 .. f1 * 16 - 1 for the rows of one KV head
-  auto attend = [&](const PromptItem& it, int f0, int f1) {
+  auto attend = [&](const PromptItem& it, int f0, int f1, auto take) {
     const int hk = it.h0 / a.P;
     // pages of this warp's next 32 steps, one per lane
     const int blocks = (it.nk + (1 << a.block_log2) - 1) >> a.block_log2;
@@ -90,6 +175,19 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(cons
       return p;
     };
     int ids = fetch(0);
+    // queries, in the order of the operands; requested before the pages' rows, behind which they would wait
+    uint2 q[J / 2][2];
+#pragma unroll
+    for (int u = 0; u < J / 2; ++u) {
+      const int ju = warp + u * FEW_WARPS, ch = (c + 4 * (ju >> 1)) * 8 + (ju & 1) * 4;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = row + 8 * i, hl = r / a.T, tok = r - hl * a.T;
+        q[u][i] = make_uint2(0u, 0u);
+        if (hl < a.P && tok < it.nq)
+          q[u][i] = *reinterpret_cast<const uint2*>(static_cast<const T*>(g.q) + (long long)(it.q0 + tok) * g.q_stride[0] + (long long)(it.h0 + hl) * g.q_stride[1] + ch);
+      }
+    }
     // this lane's parts of the keys and values of a step; rows past the end are zero
     uint4 k[2][J], v[4][H];
     auto load_k = [&](int step, int page) {
@@ -117,19 +215,8 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(cons
       load_k(step, page);
       load_v(step, page);
     }
-    // queries, in the order of the operands
-    for (int e = tid; e < 2 * J * 32; e += 32 * FEW_WARPS) {
-      const int l = e & 31, ju = e >> 5, ch = ((l & 3) + 4 * (ju >> 1)) * 8 + (ju & 1) * 4;
-      uint2 q[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int r = (l >> 2) + 8 * i, hl = r / a.T, tok = r - hl * a.T;
-        q[i] = make_uint2(0u, 0u);
-        if (hl < a.P && tok < it.nq)
-          q[i] = *reinterpret_cast<const uint2*>(static_cast<const T*>(g.q) + (long long)(it.q0 + tok) * g.q_stride[0] + (long long)(it.h0 + hl) * g.q_stride[1] + ch);
-      }
-      qf[ju][l] = make_uint4(q[0].x, q[1].x, q[0].y, q[1].y);
-    }
+    for (int u = 0; u < J / 2; ++u) qf[warp + u * FEW_WARPS][lane] = make_uint4(q[u][0].x, q[u][1].x, q[u][0].y, q[u][1].y);
     // keys that the rows of this lane see, that every row sees
     const int all_see = a.causal ? it.nk - it.nq + 1 : it.nk;
     int sees[2];
@@ -216,33 +303,38 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(cons
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int r = row + 8 * i;
       float t = l[i];
       t += __shfl_xor_sync(0xffffffffu, t, 1);
       t += __shfl_xor_sync(0xffffffffu, t, 2);
       if (c == 0) {
-        ms[warp][r] = m[i];
-        ls[warp][r] = t;
+        ms[warp][row + 8 * i] = m[i];
+        ls[warp][row + 8 * i] = t;
       }
-#pragma unroll
-      for (int n = 0; n < N; ++n) *reinterpret_cast<float2*>(&os[warp][r][n * 8 + 2 * c]) = make_float2(o[n][2 * i], o[n][2 * i + 1]);
     }
-    __syncthreads();
-  };
-  // The warps' results, eight channels `n` of row r: reference, sum, output without the division.
-  auto join = [&](int r, int n, float* top, float* sum, float (&y)[8]) {
-    *top = ms[0][r];
+    // the warps' sums, 64 channels at a time: eight of row r to `take`, with the reference and the sum, before the division
 #pragma unroll
-    for (int w = 1; w < FEW_WARPS; ++w) *top = fmaxf(*top, ms[w][r]);
-    *sum = 0.f;
+    for (int h = 0; h < H; ++h) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = 0.f;
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int w = 0; w < FEW_WARPS; ++w) {
-      const float f = *top == -INFINITY ? 0.f : ex2p(ms[w][r] - *top);
-      *sum += f * ls[w][r];
+        for (int e = 0; e < 8; ++e)
+          *reinterpret_cast<float2*>(&os[warp][row + 8 * i][e * 8 + 2 * c]) = make_float2(o[h * 8 + e][2 * i], o[h * 8 + e][2 * i + 1]);
+      __syncthreads();
+      const int r = tid >> 3, n = tid & 7;
+      if (r / a.T < a.P && r % a.T < it.nq) {
+        float top = ms[0][r], sum = 0.f, y[8] = {};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] += f * os[w][r][(n >> 3) * 64 + i * 8 + (n & 7)];
+        for (int w = 1; w < FEW_WARPS; ++w) top = fmaxf(top, ms[w][r]);
+#pragma unroll
+        for (int w = 0; w < FEW_WARPS; ++w) {
+          const float f = top == -INFINITY ? 0.f : ex2p(ms[w][r] - top);
+          sum += f * ls[w][r];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] += f * os[w][r][i * 8 + n];
+        }
+        take(r, h * 8 + n, top, sum, y);
+      }
+      __syncthreads();
     }
   };
   auto result = [&](const PromptItem& it, int r, int n, float top, float sum, float (&y)[8]) {
@@ -262,7 +354,6 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(cons
       if (n == 0 && a.lse) a.lse[hq * a.lse_rows + prow] = lse2 * 0.6931471805599453f;
     }
   };
-  auto row_of = [&](const PromptItem& it, int r) { return r / a.T < a.P && r % a.T < it.nq; };
 
   if constexpr (CLUSTER) {
     uint32_t rank, ranks;
@@ -275,12 +366,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(cons
     k_span<true>(a, it.s, &k0, &it.nk);
     if (blockIdx.x == 0 && tid == 0 && a.status && seq_cut<true>(a, it.s)) kv8_record(a.status, CHECK_LENGTH);
     const int steps = (it.nk + FEW_KEYS - 1) / FEW_KEYS, per = (steps + ranks - 1) / ranks;
-    attend(it, min(steps, (int)rank * per), min(steps, (int)(rank + 1) * per));
-    for (int e = tid; e < FEW_ROWS * N; e += 32 * FEW_WARPS) {
-      const int r = e / N, n = e - r * N;
-      if (!row_of(it, r)) continue;
-      float top, sum, y[8];
-      join(r, n, &top, &sum, y);
+    attend(it, min(steps, (int)rank * per), min(steps, (int)(rank + 1) * per), [&](int r, int n, float top, float sum, float (&y)[8]) {
       float4* po = reinterpret_cast<float4*>(&mine[r][n * 8]);
       po[0] = make_float4(y[0], y[1], y[2], y[3]);
       po[1] = make_float4(y[4], y[5], y[6], y[7]);
@@ -288,11 +374,11 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(cons
         ms[FEW_WARPS][r] = top;
         ls[FEW_WARPS][r] = sum;
       }
-    }
+    });
     cluster_meet();
     for (int e = tid * (int)ranks + (int)rank; e < FEW_ROWS * N; e += 32 * FEW_WARPS * (int)ranks) {
       const int r = e / N, n = e - r * N;
-      if (!row_of(it, r)) continue;
+      if (r / a.T >= a.P || r % a.T >= it.nq) continue;
       const uint32_t at_m = smem_u32(&ms[FEW_WARPS][r]), at_l = smem_u32(&ls[FEW_WARPS][r]), at_o = smem_u32(&mine[r][n * 8]);
       float top = -INFINITY, sum = 0.f, y[8] = {};
       for (int k = 0; k < (int)ranks; ++k) {
@@ -312,19 +398,10 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(cons
     if (blockIdx.x == 0 && a.status)
       for (int s = tid; s < a.n_seqs; s += 32 * FEW_WARPS)
         if (seq_cut<true>(a, s)) kv8_record(a.status, CHECK_LENGTH);
-    PagedRange<FEW_KEYS, FEW_ITEM_COST, FEW_RANGE_LEAST> range(a, lane);
+    FewRange range(a, lane);
     PromptItem it;
-    while (range.next(a, lane, tid == 0, &it)) {
-      attend(it, it.lo, it.n);
-      for (int e = tid; e < FEW_ROWS * N; e += 32 * FEW_WARPS) {
-        const int r = e / N, n = e - r * N;
-        if (!row_of(it, r)) continue;
-        float top, sum, y[8];
-        join(r, n, &top, &sum, y);
-        result(it, r, n, top, sum, y);
-      }
-      __syncthreads();
-    }
+    while (range.next(a, lane, tid == 0, &it))
+      attend(it, it.lo, it.n, [&](int r, int n, float top, float sum, float (&y)[8]) { result(it, r, n, top, sum, y); });
   }
 }
 

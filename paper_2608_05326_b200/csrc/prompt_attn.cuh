@@ -271,14 +271,14 @@ struct PromptItem {
   __device__ __forceinline__ bool dirty() const { return n > lo && n * TILE > nk; }  // the first tile reaches past the sequence
 };
 
-// Key tiles (of KT keys) that an item's two query tiles see.
-template <int KT = TILE> __device__ __forceinline__ void item_tiles(const PromptArgs& a, PromptItem* it) {
+// Key tiles that an item's two query tiles see.
+__device__ __forceinline__ void item_tiles(const PromptArgs& a, PromptItem* it) {
   int nt[2];
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
     const int rw = it->r0 + w * a.T, last = min(rw + a.T, it->nq) - 1;
     const int lim = rw >= it->nq ? 0 : (a.causal ? min(it->nk, last + it->nk - it->nq + 1) : it->nk);
-    nt[w] = lim > 0 ? (lim + KT - 1) / KT : 0;
+    nt[w] = lim > 0 ? (lim + TILE - 1) / TILE : 0;
   }
   it->lo = 0;
   it->n = max(nt[0], nt[1]);
@@ -382,8 +382,8 @@ struct PagedSeq {
     if (u > full) u = full;
     return (full - u) * p + step * (full * (full + 1) - u * (u + 1)) / 2 + (t < tiles ? 0 : nk);
   }
-  template <int ITEM> __device__ __forceinline__ long long cost(const PromptArgs& a, int t) const { return (long long)key_cost * keys(a, t) + ITEM; }
-  template <int ITEM> __device__ __forceinline__ long long cost_before(const PromptArgs& a, int t) const { return t > 0 ? key_cost * before(a, t) + (long long)t * ITEM : 0; }
+  __device__ __forceinline__ long long cost(const PromptArgs& a, int t) const { return (long long)key_cost * keys(a, t) + ITEM_COST; }
+  __device__ __forceinline__ long long cost_before(const PromptArgs& a, int t) const { return t > 0 ? key_cost * before(a, t) + (long long)t * ITEM_COST : 0; }
 };
 
 __device__ __forceinline__ PagedSeq paged_seq(const PromptArgs& a, int q0, int nq, int nk) {
@@ -396,8 +396,7 @@ __device__ __forceinline__ long long quotient(long long x, long long y) {
   return (long long)((double)x / (double)y);
 }
 
-// KT: keys of a tile; ITEM: what an item costs beside its keys; LEAST: least width of a range
-template <int KT, int ITEM = ITEM_COST, int LEAST = RANGE_LEAST> struct PagedRange {
+struct PagedRange {
   long long width, lo, hi, at;  // this CTA's part of the sum; start of the current item
   int s, h, t;
   PagedSeq seq;
@@ -424,12 +423,12 @@ template <int KT, int ITEM = ITEM_COST, int LEAST = RANGE_LEAST> struct PagedRan
     long long sum = 0;
     for (int i = 0; i < a.n_seqs; i += 32) {
       const PagedSeq q = look(a, i, lane);
-      sum += q.template cost_before<ITEM>(a, q.tiles) * groups;
+      sum += q.cost_before(a, q.tiles) * groups;
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     width = quotient(sum + gridDim.x - 1, gridDim.x);
-    if (width < LEAST) width = LEAST;
+    if (width < RANGE_LEAST) width = RANGE_LEAST;
     lo = blockIdx.x * width;
     hi = lo + width < sum ? lo + width : sum;
     s = a.n_seqs;
@@ -437,7 +436,7 @@ template <int KT, int ITEM = ITEM_COST, int LEAST = RANGE_LEAST> struct PagedRan
     long long front = 0;  // cost of the sequences before
     for (int i = 0; i < a.n_seqs; i += 32) {
       const PagedSeq q = a.n_seqs > 32 ? look(a, i, lane) : paged_seq(a, lane_q0, lane_nq, lane_nk);
-      const long long mine = q.template cost_before<ITEM>(a, q.tiles) * groups;
+      const long long mine = q.cost_before(a, q.tiles) * groups;
       long long upto = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -454,29 +453,29 @@ template <int KT, int ITEM = ITEM_COST, int LEAST = RANGE_LEAST> struct PagedRan
       front += __shfl_sync(0xffffffffu, upto, 31);
     }
     seq = sequence(a, s, lane);
-    const long long head = seq.template cost_before<ITEM>(a, seq.tiles);
+    const long long head = seq.cost_before(a, seq.tiles);
     h = (int)quotient(lo - front, head);
     front += h * head;
     int t0 = 0, t1 = seq.tiles - 1;  // the last tile that starts at or before lo
     while (t0 < t1) {
       const int mid = (t0 + t1 + 1) >> 1;
-      if (front + seq.template cost_before<ITEM>(a, mid) <= lo) t0 = mid; else t1 = mid - 1;
+      if (front + seq.cost_before(a, mid) <= lo) t0 = mid; else t1 = mid - 1;
     }
     t = t0;
-    at = front + seq.template cost_before<ITEM>(a, t);
+    at = front + seq.cost_before(a, t);
   }
 
   // The next item of the range, its key tiles in it; false behind the last one.
   __device__ __forceinline__ bool next(const PromptArgs& a, int lane, bool writes, PromptItem* it) {
     while (s < a.n_seqs && at < hi) {
-      const long long cost = seq.template cost<ITEM>(a, t), end = at + cost;
+      const long long cost = seq.cost(a, t), end = at + cost;
       it->valid = 1;
       it->s = s; it->h0 = h * a.P; it->r0 = t * 2 * a.T;
       it->q0 = seq.q0; it->nq = seq.nq; it->k0 = 0; it->nk = seq.nk;
       it->split = 0;
-      item_tiles<KT>(a, it);
+      item_tiles(a, it);
       const int all = it->n;
-      auto tiles_upto = [&](long long x) { return x <= at + ITEM ? 0 : (int)quotient(x - at - ITEM, seq.key_cost * KT); };
+      auto tiles_upto = [&](long long x) { return x <= at + ITEM_COST ? 0 : (int)quotient(x - at - ITEM_COST, seq.key_cost * TILE); };
       const int f0 = lo > at ? tiles_upto(lo) : 0;
       const bool ends = end <= hi;
       const int f1 = ends ? all : tiles_upto(hi);
@@ -615,7 +614,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       if (PAGED && a.by_range) {
         checks = blockIdx.x == 0;
         if (a.cuts && lane == 0) a.cuts[blockIdx.x].valid = 0;
-        PagedRange<TILE> range(a, lane);
+        PagedRange range(a, lane);
         PromptItem it;
         while (ok && range.next(a, lane, lane == 0, &it)) {
           it.before = k_tiles;
@@ -1211,7 +1210,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
     };
     if (PAGED && a.by_range) {
       if (wid == ITEM_WARP) {
-        PagedRange<TILE> range(a, lane);
+        PagedRange range(a, lane);
         PromptItem it;
         while (range.next(a, lane, lane == 0, &it)) lose(it, lane, 32);
       }
