@@ -61,7 +61,7 @@ Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
   const long long groups = p->n_q_heads / l.P, items = prompt_tiles(false, c.n_seqs, max_q, rows, l.T) * groups;
   const int sms = prompt_sms(p->cache->device), group = p->n_q_heads / c.Hkv;
   const long long units = c.n_seqs * (long long)c.Hkv, steps = (longest + FEW_KEYS - 1) / FEW_KEYS + FEW_ITEM_COST;
-  if (group * max_q <= FEW_ROWS && units * steps < (1ll << 30)) {
+  if (!getenv("QT") && group * max_q <= FEW_ROWS && units * steps < (1ll << 30)) {
     l.few = true;
     l.P = group;
     l.T = max_q > 0 ? (int)max_q : 1;
@@ -77,7 +77,7 @@ Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
     l.slot_rows = FEW_ROWS;
     return with_scratch(l, p, c);
   }
-  l.by_range = rows / (2 * l.T) * groups < 6 * sms;
+  l.by_range = rows / (2 * l.T) * groups < 6 * sms && items * (KEY_COST * longest + ITEM_COST) < (1ll << 31);
   if (!l.by_range) {
     l.ctas = items <= (1ll << 28) ? (unsigned)items : 0u;
     return l;

@@ -367,6 +367,7 @@ template <bool PAGED> __device__ __forceinline__ PromptItem item_of(const Prompt
 // quarters for pairs, whose two tiles a step bandwidth bounds) and a constant; CTA c has what lies in [c, c + 1) * W of
 // the sum.  An end inside an item is moved to a key tile: an item has the CTAs that have tiles of it, and where these are
 // several, each writes a partial result.  The ranges are a function of the lengths alone.
+// (The host sees to it that the sum fits 31 bits.)
 constexpr int ITEM_COST = 1024, KEY_COST = 4, KEY_COST_PAIR = 3, RANGE_LEAST = 1024;
 
 struct PagedSeq {
@@ -375,29 +376,23 @@ struct PagedSeq {
   __device__ __forceinline__ int keys(const PromptArgs& a, int t) const {
     return !a.causal || t == tiles - 1 ? nk : max(0, nk - nq + (t + 1) * 2 * a.T);
   }
-  __device__ __forceinline__ long long before(const PromptArgs& a, int t) const {
-    if (!a.causal) return (long long)t * nk;
-    const long long step = 2 * a.T, p = nk - nq, full = t < tiles ? t : tiles - 1;
-    long long u = p < 0 ? -p / step : 0;
-    if (u > full) u = full;
-    return (full - u) * p + step * (full * (full + 1) - u * (u + 1)) / 2 + (t < tiles ? 0 : nk);
+  __device__ __forceinline__ uint32_t before(const PromptArgs& a, int t) const {
+    if (!a.causal) return (uint32_t)t * nk;
+    // full tiles of rows, of which the first u see nothing (modulo 2^32, in which the sum fits)
+    const uint32_t step = 2 * a.T, p = nk - nq, full = t < tiles ? t : tiles - 1;
+    const uint32_t u = nk < nq ? min(full, (uint32_t)(nq - nk) / step) : 0u;
+    return (full - u) * p + a.T * (full * (full + 1) - u * (u + 1)) + (t < tiles ? 0 : nk);
   }
-  __device__ __forceinline__ long long cost(const PromptArgs& a, int t) const { return (long long)key_cost * keys(a, t) + ITEM_COST; }
-  __device__ __forceinline__ long long cost_before(const PromptArgs& a, int t) const { return t > 0 ? key_cost * before(a, t) + (long long)t * ITEM_COST : 0; }
+  __device__ __forceinline__ uint32_t cost(const PromptArgs& a, int t) const { return key_cost * keys(a, t) + ITEM_COST; }
+  __device__ __forceinline__ uint32_t cost_before(const PromptArgs& a, int t) const { return t > 0 ? key_cost * before(a, t) + t * ITEM_COST : 0u; }
 };
 
 __device__ __forceinline__ PagedSeq paged_seq(const PromptArgs& a, int q0, int nq, int nk) {
   return {q0, nq, nk, (nq + 2 * a.T - 1) / (2 * a.T), paged_pair(a, nq, nk) ? KEY_COST_PAIR : KEY_COST};
 }
 
-// floor(x / y) for 0 <= x < 2^53: the quotient's distance from a whole number above it is at least 1 / y, more than it is rounded by
-__device__ __forceinline__ long long quotient(long long x, long long y) {
-  if (((unsigned long long)x | (unsigned long long)y) >> 32 == 0) return (uint32_t)x / (uint32_t)y;
-  return (long long)((double)x / (double)y);
-}
-
 struct PagedRange {
-  long long width, lo, hi, at;  // this CTA's part of the sum; start of the current item
+  uint32_t width, lo, hi, at;  // this CTA's part of the sum; start of the current item
   int s, h, t;
   PagedSeq seq;
   int lane_q0, lane_nq, lane_nk, first;  // the lane's sequence of 32, of which `first` is the first
@@ -420,27 +415,28 @@ struct PagedRange {
 
   __device__ __forceinline__ PagedRange(const PromptArgs& a, int lane) {
     const int groups = a.Hq / a.P;
-    long long sum = 0;
+    uint32_t sum = 0, mine = 0;
     for (int i = 0; i < a.n_seqs; i += 32) {
       const PagedSeq q = look(a, i, lane);
-      sum += q.cost_before(a, q.tiles) * groups;
+      mine = q.cost_before(a, q.tiles) * groups;
+      sum += __reduce_add_sync(0xffffffffu, mine);
     }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    width = quotient(sum + gridDim.x - 1, gridDim.x);
+    width = (sum + gridDim.x - 1) / gridDim.x;
     if (width < RANGE_LEAST) width = RANGE_LEAST;
     lo = blockIdx.x * width;
-    hi = lo + width < sum ? lo + width : sum;
+    hi = min(lo + width, sum);
     s = a.n_seqs;
     if (lo >= sum) return;
-    long long front = 0;  // cost of the sequences before
-    for (int i = 0; i < a.n_seqs; i += 32) {
-      const PagedSeq q = a.n_seqs > 32 ? look(a, i, lane) : paged_seq(a, lane_q0, lane_nq, lane_nk);
-      const long long mine = q.cost_before(a, q.tiles) * groups;
-      long long upto = mine;
+    uint32_t front = 0;  // cost of the sequences before
+    for (int i = 0;; i += 32) {
+      if (a.n_seqs > 32) {
+        const PagedSeq q = look(a, i, lane);
+        mine = q.cost_before(a, q.tiles) * groups;
+      }
+      uint32_t upto = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const long long x = __shfl_up_sync(0xffffffffu, upto, o);
+        const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
         if (lane >= o) upto += x;
       }
       const uint32_t past = __ballot_sync(0xffffffffu, front + upto > lo);
@@ -453,8 +449,8 @@ struct PagedRange {
       front += __shfl_sync(0xffffffffu, upto, 31);
     }
     seq = sequence(a, s, lane);
-    const long long head = seq.cost_before(a, seq.tiles);
-    h = (int)quotient(lo - front, head);
+    const uint32_t head = seq.cost_before(a, seq.tiles);
+    h = (lo - front) / head;
     front += h * head;
     int t0 = 0, t1 = seq.tiles - 1;  // the last tile that starts at or before lo
     while (t0 < t1) {
@@ -468,14 +464,14 @@ struct PagedRange {
   // The next item of the range, its key tiles in it; false behind the last one.
   __device__ __forceinline__ bool next(const PromptArgs& a, int lane, bool writes, PromptItem* it) {
     while (s < a.n_seqs && at < hi) {
-      const long long cost = seq.cost(a, t), end = at + cost;
+      const uint32_t end = at + seq.cost(a, t);
       it->valid = 1;
       it->s = s; it->h0 = h * a.P; it->r0 = t * 2 * a.T;
       it->q0 = seq.q0; it->nq = seq.nq; it->k0 = 0; it->nk = seq.nk;
       it->split = 0;
       item_tiles(a, it);
       const int all = it->n;
-      auto tiles_upto = [&](long long x) { return x <= at + ITEM_COST ? 0 : (int)quotient(x - at - ITEM_COST, seq.key_cost * TILE); };
+      auto tiles_upto = [&](uint32_t x) { return x <= at + ITEM_COST ? 0 : (int)((x - at - ITEM_COST) / (uint32_t)(seq.key_cost * TILE)); };
       const int f0 = lo > at ? tiles_upto(lo) : 0;
       const bool ends = end <= hi;
       const int f1 = ends ? all : tiles_upto(hi);
@@ -483,7 +479,7 @@ struct PagedRange {
       it->n = f1;
       it->slot = f0 == 0 && ends ? -1 : 2 * (int)blockIdx.x + (f0 == 0);
       if (f0 == 0 && f1 > 0 && !ends && writes) {
-        const PagedCut c = {1, s, it->h0, it->r0, seq.q0, seq.nq, (int)quotient(end - 1, width), paged_pair(a, seq.nq, seq.nk)};
+        const PagedCut c = {1, s, it->h0, it->r0, seq.q0, seq.nq, (int)((end - 1) / width), paged_pair(a, seq.nq, seq.nk)};
         a.cuts[blockIdx.x] = c;
       }
       at = end;
@@ -704,15 +700,12 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         int window[2] = {0, 0}, id[2] = {0, 0}, ahead[2] = {0, 0};
         auto fetch = [&](int win) {
           const int b = win * 32 + lane;
-          int p = a.n_pages;
-          if (win >= 0 && b < blocks) {
-            p = a.table[(size_t)it.s * a.max_blocks + b];
-            if (p < 0 || p >= a.n_pages) {
-              if (p != -1) kv8_record(a.status, CHECK_PAGE_ID);
-              p = a.n_pages;
-            }
-          }
-          return p;
+          return win >= 0 && b < blocks ? a.table[(size_t)it.s * a.max_blocks + b] : -1;
+        };
+        auto look = [&](int p) {  // a page id, or the place of none
+          if (p >= 0 && p < a.n_pages) return p;
+          if (p != -1) kv8_record(a.status, CHECK_PAGE_ID);
+          return a.n_pages;
         };
         if (PAGED) {
 #pragma unroll
@@ -723,6 +716,8 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
               ahead[w] = fetch(window[w] - 1);
             }
           }
+          id[0] = look(id[0]);
+          if (c1 > 0) id[1] = look(id[1]);
         }
         auto issue = [&](int w, bool value, int j) {  // the next slot of the ring: K or V of key tile j (of stream w)
           if (!ok) return;
@@ -732,7 +727,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
             const int first = j << per_log2;
             if ((first >> 5) != window[w]) {
               window[w] = first >> 5;
-              id[w] = ahead[w];
+              id[w] = look(ahead[w]);
               ahead[w] = fetch(window[w] - 1);
             }
             const uint32_t none = __ballot_sync(0xffffffffu, id[w] == a.n_pages && window[w] * 32 + lane < blocks);
@@ -987,12 +982,6 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       if (PAGED) tok = (twin ? 0 : w * a.T) + r - hl * a.T;
       // keys that this row still sees from the tile's (this half's) first on; grows by a tile each time
       int left = (a.causal ? min(it.nk, it.r0 + tok + it.nk - it.nq + 1) : it.nk) - ((w ? it.nt1 : it.nt0) - 1) * TILE - half * (TILE / 2);
-      // (paged) place of this tile's number of absent blocks: the last 16 tiles' in the order of their copies, those of pairs in turn
-      int mask_at = 0, mask_step = 1;
-      if (PAGED) {
-        mask_at = it.before + (twin ? w : it.n - (w ? it.nt1 : it.nt0));
-        mask_step = twin ? 2 : 1;
-      }
       const bool mine = it.r0 + tok < it.nq && hl < a.P;  // rows of nobody hold anything, and have no say below
       float m = -INFINITY, l = 0.f;
       for (int i = cnt; i > 0; --i, left += TILE) {
@@ -1010,8 +999,9 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
             for (int c = 0; c < TILE / 2; ++c) x[c] = c < left ? x[c] : -INFINITY;
           }
           if constexpr (PAGED) {
-            const uint32_t none = masks[mask_at & 15];
-            mask_at += mask_step;
+            // (read from the item each time: the registers are the logits')
+            const volatile PromptItem& v = it;
+            const uint32_t none = masks[(v.pair ? v.before + w + 2 * (cnt - i) : v.before + v.n - i - (w ? v.nt1 : v.nt0) + cnt) & 15];
             if (none) {  // blocks that are not there, 16 keys at a time
 #pragma unroll
               for (int c = 0; c < TILE / 2; ++c)
@@ -1109,25 +1099,29 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
           }
           T* out = static_cast<T*>(a.out) + prow * a.out_stride[2] + hq * a.out_stride[1] + c0;
 #pragma unroll 1
-          for (int c = 0; c < D / 4; c += 8) {
-            float o[8], o1[8];
-            tm_ld8(tmem + lane_base + 256 + c0 + c, o);
-            if (it.cnt(1) > 0) tm_ld8(tmem + lane_base + 384 + c0 + c, o1);
+          for (int c = 0; c < D / 4; c += 16) {
+            float o[16], o1[16];
+            tm_ld16(tmem + lane_base + 256 + c0 + c, o);
+            const bool two = it.cnt(1) > 0;
+            if (two) tm_ld16(tmem + lane_base + 384 + c0 + c, o1);
             tm_wait_ld();
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < 16; ++k) {
               o[k] *= f0;
-              if (it.cnt(1) > 0) o[k] += o1[k] * f1;
+              if (two) o[k] += o1[k] * f1;
               o[k] = l == 0.f ? 0.f : o[k] * inv;
             }
-            if (!mine) continue;
-            if (it.slot >= 0) {
-              float4* po = reinterpret_cast<float4*>(a.part_o + slot * D + c0 + c);
-              po[0] = make_float4(o[0], o[1], o[2], o[3]);
-              po[1] = make_float4(o[4], o[5], o[6], o[7]);
-            } else {
-              *reinterpret_cast<uint4*>(out + c) = make_uint4(pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3]), pack2<T>(o[4], o[5]), pack2<T>(o[6], o[7]));
+            if (mine && it.slot >= 0) {
+#pragma unroll
+              for (int k = 0; k < 16; k += 4)
+                *reinterpret_cast<float4*>(a.part_o + slot * D + c0 + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+            } else if (mine) {
+#pragma unroll
+              for (int k = 0; k < 16; k += 8)
+                *reinterpret_cast<uint4*>(out + c + k) =
+                    make_uint4(pack2<T>(o[k], o[k + 1]), pack2<T>(o[k + 2], o[k + 3]), pack2<T>(o[k + 4], o[k + 5]), pack2<T>(o[k + 6], o[k + 7]));
             }
+            __syncwarp();
           }
           tm_before();
           meet4();  // the next item's first products overwrite both
