@@ -2,19 +2,17 @@
 //
 // The kernel is the prompt attention's (prompt_attn.cuh) with keys and values by page: a tile of 128 keys is 1 to 8
 // pages, each copied by TMA from where the table says, page after page into the rows that they have in the tile.
-#include <stdlib.h>
 #include "kv16_few.cuh"
 
 namespace qevict {
 
 namespace {
 
-constexpr int FEW_CLUSTER_KEYS = 1024;
+constexpr int FEW_CLUSTER_KEYS = 1024;  // of a CTA
 
 struct Plan {
   int P, T;       // rows of a query tile: heads, tokens
-  bool few;       // few_attn_kernel has the call
-  int ranks;      // CTAs of a cluster that has a sequence's KV head, else 0
+  int ranks;      // few_attn_kernel has the call, with clusters of as many CTAs, else 0
   bool by_range;  // equal ranges, else whole items
   bool cuts;      // an item may be shared
   int slot_rows;
@@ -60,22 +58,17 @@ Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
   const long long rows = p->cu_q ? p->total_q : (p->total_q < c.n_seqs ? p->total_q : c.n_seqs);
   const long long groups = p->n_q_heads / l.P, items = prompt_tiles(false, c.n_seqs, max_q, rows, l.T) * groups;
   const int sms = prompt_sms(p->cache->device), group = p->n_q_heads / c.Hkv;
-  const long long units = c.n_seqs * (long long)c.Hkv, steps = (longest + FEW_KEYS - 1) / FEW_KEYS + FEW_ITEM_COST;
-  if (!getenv("QT") && group * max_q <= FEW_ROWS && units * steps < (1ll << 30)) {
-    l.few = true;
-    l.P = group;
-    l.T = max_q > 0 ? (int)max_q : 1;
-    const long long room = (long long)sms * FEW_CTAS;
-    // up to 16 CTAs for each unit where that fills no more than one wave and none has more than FEW_CLUSTER_KEYS keys
-    for (int ranks = 1; ranks <= 16; ranks *= 2)
-      if (units * ranks <= room && longest <= (long long)ranks * FEW_CLUSTER_KEYS && (ranks == 1 || ranks <= longest / (FEW_WARPS * FEW_KEYS))) l.ranks = ranks;
-    if (l.ranks) return l;
-    l.by_range = true;
-    const long long most = units * steps / FEW_RANGE_LEAST + 1;
-    l.ctas = (unsigned)(most < room ? most : room);
-    l.cuts = longest > FEW_KEYS && l.ctas > 1;
-    l.slot_rows = FEW_ROWS;
-    return with_scratch(l, p, c);
+  if (group * max_q <= FEW_ROWS) {
+    // clusters as large as one wave holds, four steps of keys for each CTA at least
+    const long long room = (long long)sms * FEW_CTAS, units = c.n_seqs * (long long)c.Hkv;
+    int ranks = 1;
+    while (ranks < 16 && units * ranks * 2 <= room && ranks * 2 * FEW_WARPS * FEW_KEYS <= longest) ranks *= 2;
+    if (longest <= (long long)ranks * FEW_CLUSTER_KEYS && units * longest <= room * FEW_CLUSTER_KEYS) {
+      l.ranks = ranks;
+      l.P = group;
+      l.T = max_q > 0 ? (int)max_q : 1;
+      return l;
+    }
   }
   l.by_range = rows / (2 * l.T) * groups < 6 * sms && items * (KEY_COST * longest + ITEM_COST) < (1ll << 31);
   if (!l.by_range) {
@@ -120,46 +113,32 @@ const char* attn_check_pointers(const qevict_kv16_attn_args* p) {
   return nullptr;
 }
 
-// Shared memory for FEW_CTAS on an SM, the rest for the L1: a load on its way has its place there
-template <class K> cudaError_t few_attributes(K kernel, int smem) {
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  int pct = 45;
-  if (const char* x = getenv("QX")) pct = atoi(x);
-  return e != cudaSuccess ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, pct);
-}
-
 template <class T, int D>
 cudaError_t launch_few(const PromptArgs& a, const Plan& l, const FewPages& g, int device, cudaStream_t s) {
-  if (l.ranks) {
-    auto kernel = few_attn_kernel<T, D, true>;
-    static std::atomic<uint64_t> done{0};
-    cudaError_t e = once_per_device(done, device, [&] {
-      const cudaError_t e0 = few_attributes(kernel, few_smem(D));
-      return e0 != cudaSuccess ? e0 : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    });
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(l.ranks * a.Hkv, a.n_seqs);
-    cfg.blockDim = dim3(32 * FEW_WARPS);
-    cfg.dynamicSmemBytes = few_smem(D);
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = l.ranks;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, a, g);
-  }
-  auto kernel = few_attn_kernel<T, D, false>;
+  auto kernel = few_attn_kernel<T, D>;
   static std::atomic<uint64_t> done{0};
-  cudaError_t e = once_per_device(done, device, [&] { return few_attributes(kernel, few_smem(D)); });
-  if (e == cudaSuccess) e = launch_pdl(kernel, dim3(l.ctas), dim3(32 * FEW_WARPS), few_smem(D), s, a, g);
-  if (e == cudaSuccess && l.cuts) e = launch_pdl(paged_merge_kernel<T, D>, dim3(l.slot_rows / 8, l.ctas), dim3(256), 0, s, a);
-  return e;
+  cudaError_t e = once_per_device(done, device, [&] {
+    cudaError_t e0 = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem(D));
+    if (e0 == cudaSuccess) e0 = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 45);  // FEW_CTAS fit; the rest is L1
+    return e0 != cudaSuccess ? e0 : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  });
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(l.ranks * a.Hkv, a.n_seqs);
+  cfg.blockDim = dim3(32 * FEW_WARPS);
+  cfg.dynamicSmemBytes = few_smem(D);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = l.ranks;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, a, g);
 }
+
 template <class T, int D>
 cudaError_t launch_paged(const PromptArgs& a, const Plan& l, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, int device, cudaStream_t s) {
   auto kernel = prompt_attn_kernel<T, D, true>;
@@ -235,7 +214,7 @@ QEVICT_API qevict_status qevict_kv16_attn(const qevict_kv16_attn_args* p, void* 
   cudaError_t e = guard.err;
   if (e != cudaSuccess) return stateless_fail(QEVICT_ERR_CUDA, cudaGetErrorString(e));
   cudaStream_t s = (cudaStream_t)stream;
-  if (l.few) {
+  if (l.ranks) {
     FewPages g = {};
     for (int w = 0; w < 2; ++w) {
       g.pages[w] = view.pages[w];

@@ -1,17 +1,22 @@
-// Attention of few new tokens (a step of decoding, drafts) over the 16-bit paged cache.
+// Attention of few new tokens over few cached ones (a step of decoding, drafts) in the 16-bit paged cache: calls for which latency
+// counts.
 //
 //     S = Q K^T,  P = 2^(S * scale * log2 e - m),  O += P V
 //
-// The rows are the tokens of all heads that share a KV head, at most 16 of them, so keys and values are read once and
-// bandwidth bounds it.  The four warps of a CTA take 16 keys in turn, straight from global memory into the registers that the
-// products want them in, the next ones on their way while these are in work, and join their sums through shared memory in the end.
+// The rows are the tokens of all heads that share a KV head, at most 16 of them.  A cluster of up to 16 CTAs has a (sequence, KV
+// head); the four warps of a CTA take 16 of its keys in turn, straight from global memory into the registers that the
+// products want them in, the next ones on their way while these are in work.  The warps join their sums through shared memory, the
+// CTAs through each other's: one launch, and no scratch.
 //   - mma.m16n8k16 contracts over channels in any order, so a lane takes 16 bytes of a key as the operands of two steps (elements
 //     0, 1 | 2, 3 and 4, 5 | 6, 7), and the queries are laid out to match.
 //   - A lane has 16 bytes of two neighbouring keys' values; byte permutes pair them, and the output's columns come in the order
 //     that this gives (channel 8 n + e is column n of step e).
 //   - Keys past the end and blocks that are not there are not read; their operands are zero and their logits masked.
-// How the keys are shared: a call with many keys gives each CTA an equal range of its work (FewRange) and joins what ranges share in a second launch; a call that one wave of clusters holds gives each (sequence, KV
-// head) a cluster of CTAs, which join their sums through each other's shared memory.
+// Measured beside the kernel for tiles of rows (equal ranges, two launches), 32 / 8 heads of 128, one token for each of n sequences:
+// n = 1, 128 tokens 5.3 us (14.1), 2001 tokens 9.4 us (17.8), 8001: 18.4 us (22.9), 16001: 28.7 us (30.1), 32001: 57 us (44); n = 16,
+// 1001: 18.6 us (26.4), 2001: 33.8 us (40.7), 4001: 60.8 us (61.8).  It takes calls with up to FEW_CLUSTER_KEYS keys for each
+// CTA of one wave; beyond, its loads reach 5.2 TB/s where copies of whole pages reach 6.3.  Loads on their way have their place in the L1, so shared memory is kept
+// small (64 sequences of 2049 tokens: 145 us with all of it, 105 us with 45 %).
 #pragma once
 
 #include "prompt_attn.cuh"
@@ -21,7 +26,6 @@ namespace qevict {
 namespace {
 
 constexpr int FEW_WARPS = 4, FEW_KEYS = 16;
-constexpr int FEW_ITEM_COST = 5, FEW_RANGE_LEAST = 8;  // steps of 16 keys
 constexpr int FEW_ROWS = 16, FEW_CTAS = 3;  // of an SM: 168 registers a thread
 constexpr int few_smem(int D) { return (FEW_WARPS * 72 + D) * FEW_ROWS * 4 + D / 32 * 1024 + (FEW_WARPS + 1) * FEW_ROWS * 8; }
 
@@ -55,94 +59,8 @@ struct FewPages {
   long long q_stride[2];  // token, head
 };
 
-// A CTA's equal range of the work: the sequences' KV heads stand in a row, each of its steps and FEW_ITEM_COST more.  An end inside a
-// KV head's constant is moved to its first step.  (The host sees to it that the sum fits 31 bits.)
-struct FewRange {
-  uint32_t width, lo, hi, at;  // this CTA's part of the sum; start of the current item
-  int s, h, q0, nq, nk;
-  int lane_q0, lane_nq, lane_nk, first;  // the lane's sequence of 32, of which `first` is the first
-
-  static __device__ __forceinline__ uint32_t cost(int nq, int nk) { return nq > 0 ? (nk + FEW_KEYS - 1) / FEW_KEYS + FEW_ITEM_COST : 0; }
-  __device__ __forceinline__ uint32_t look(const PromptArgs& a, int s0, int lane) {  // work of the lane's sequence
-    int k0;
-    lane_q0 = lane_nq = lane_nk = 0;
-    first = s0;
-    if (s0 + lane < a.n_seqs) {
-      q_span<true>(a, s0 + lane, &lane_q0, &lane_nq);
-      k_span<true>(a, s0 + lane, &k0, &lane_nk);
-    }
-    return cost(lane_nq, lane_nk) * a.Hkv;
-  }
-  __device__ __forceinline__ void sequence(const PromptArgs& a, int lane) {
-    if (s >= first + 32) look(a, s & ~31, lane);
-    q0 = __shfl_sync(0xffffffffu, lane_q0, s & 31);
-    nq = __shfl_sync(0xffffffffu, lane_nq, s & 31);
-    nk = __shfl_sync(0xffffffffu, lane_nk, s & 31);
-  }
-  __device__ __forceinline__ FewRange(const PromptArgs& a, int lane) {
-    uint32_t sum = 0, mine = 0;
-    for (int i = 0; i < a.n_seqs; i += 32) {
-      mine = look(a, i, lane);
-      sum += __reduce_add_sync(0xffffffffu, mine);
-    }
-    width = (sum + gridDim.x - 1) / gridDim.x;
-    if (width < FEW_RANGE_LEAST) width = FEW_RANGE_LEAST;
-    lo = blockIdx.x * width;
-    hi = min(lo + width, sum);
-    s = a.n_seqs;
-    if (lo >= sum) return;
-    uint32_t front = 0;  // work of the sequences before
-    for (int i = 0;; i += 32) {
-      if (a.n_seqs > 32) mine = look(a, i, lane);
-      uint32_t upto = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += x;
-      }
-      const uint32_t past = __ballot_sync(0xffffffffu, front + upto > lo);
-      if (past) {
-        const int who = __ffs(past) - 1;
-        s = i + who;
-        front += __shfl_sync(0xffffffffu, upto - mine, who);
-        break;
-      }
-      front += __shfl_sync(0xffffffffu, upto, 31);
-    }
-    sequence(a, lane);
-    h = (lo - front) / cost(nq, nk);
-    at = front + h * cost(nq, nk);
-  }
-  // The next item, its steps in the range; false behind the last one.
-  __device__ __forceinline__ bool next(const PromptArgs& a, int lane, bool writes, PromptItem* it) {
-    while (s < a.n_seqs && at < hi) {
-      const uint32_t end = at + cost(nq, nk);
-      const int all = (nk + FEW_KEYS - 1) / FEW_KEYS;
-      auto steps_upto = [&](uint32_t x) { return x <= at + FEW_ITEM_COST ? 0 : (int)(x - at - FEW_ITEM_COST); };
-      const bool ends = end <= hi;
-      it->s = s; it->h0 = h * a.P; it->q0 = q0; it->nq = nq; it->nk = nk;
-      it->lo = lo > at ? steps_upto(lo) : 0;
-      it->n = ends ? all : steps_upto(hi);
-      it->slot = it->lo == 0 && ends ? -1 : 2 * (int)blockIdx.x + (it->lo == 0);
-      if (it->lo == 0 && it->n > 0 && !ends && writes) {
-        const PagedCut c = {1, s, it->h0, 0, q0, nq, (int)((end - 1) / width), 0};
-        a.cuts[blockIdx.x] = c;
-      }
-      at = end;
-      if (++h == a.Hkv) {
-        h = 0;
-        do {
-          if (++s < a.n_seqs) sequence(a, lane);
-        } while (s < a.n_seqs && nq == 0);
-      }
-      if (it->n > it->lo || (all == 0 && ends)) return true;
-    }
-    return false;
-  }
-};
-
-// CLUSTER: blockIdx is (KV head * ranks + rank, sequence)
-template <class T, int D, bool CLUSTER>
+// blockIdx is (KV head * ranks + rank, sequence)
+template <class T, int D>
 __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ FewPages g) {
   constexpr int J = D / 32;       // 16-byte pieces of a key in a lane
   constexpr int H = D / 64;       // of a value
@@ -155,7 +73,6 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(cons
   auto ms = reinterpret_cast<float (*)[FEW_ROWS]>(qf + 2 * J), ls = ms + FEW_WARPS + 1;  // references and sums: the warps', the CTA's
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = lane >> 2, c = lane & 3;
   pdl_prologue();
-  if (!CLUSTER && a.cuts && tid == 0) a.cuts[blockIdx.x].valid = 0;
 
   // keys f0 * 16 .. f1 * 16 - 1 for the rows of one KV head
   auto attend = [&](const PromptItem& it, int f0, int f1, auto take) {
@@ -342,67 +259,50 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(cons
     const float inv = sum == 0.f ? 0.f : 1.f / sum, lse2 = sum == 0.f ? -INFINITY : top + log2f(sum);
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = sum == 0.f ? 0.f : y[i] * inv;
-    const long long prow = it.q0 + tok, slot = (long long)it.slot * a.slot_rows + r;
-    if (!CLUSTER && it.slot >= 0) {
-      float4* po = reinterpret_cast<float4*>(a.part_o + slot * D + n * 8);
-      po[0] = make_float4(y[0], y[1], y[2], y[3]);
-      po[1] = make_float4(y[4], y[5], y[6], y[7]);
-      if (n == 0) a.part_lse[slot] = lse2;
-    } else {
-      *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + prow * a.out_stride[2] + hq * a.out_stride[1] + n * 8) =
-          make_uint4(pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3]), pack2<T>(y[4], y[5]), pack2<T>(y[6], y[7]));
-      if (n == 0 && a.lse) a.lse[hq * a.lse_rows + prow] = lse2 * 0.6931471805599453f;
-    }
+    const long long prow = it.q0 + tok;
+    *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + prow * a.out_stride[2] + hq * a.out_stride[1] + n * 8) =
+        make_uint4(pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3]), pack2<T>(y[4], y[5]), pack2<T>(y[6], y[7]));
+    if (n == 0 && a.lse) a.lse[hq * a.lse_rows + prow] = lse2 * 0.6931471805599453f;
   };
 
-  if constexpr (CLUSTER) {
-    uint32_t rank, ranks;
-    asm("mov.u32 %0, %%cluster_ctarank;\nmov.u32 %1, %%cluster_nctarank;" : "=r"(rank), "=r"(ranks));
-    PromptItem it;
-    it.s = blockIdx.y;
-    it.h0 = blockIdx.x / ranks * a.P;
-    int k0;
-    q_span<true>(a, it.s, &it.q0, &it.nq);
-    k_span<true>(a, it.s, &k0, &it.nk);
-    if (blockIdx.x == 0 && tid == 0 && a.status && seq_cut<true>(a, it.s)) kv8_record(a.status, CHECK_LENGTH);
-    const int steps = (it.nk + FEW_KEYS - 1) / FEW_KEYS, per = (steps + ranks - 1) / ranks;
-    attend(it, min(steps, (int)rank * per), min(steps, (int)(rank + 1) * per), [&](int r, int n, float top, float sum, float (&y)[8]) {
-      float4* po = reinterpret_cast<float4*>(&mine[r][n * 8]);
-      po[0] = make_float4(y[0], y[1], y[2], y[3]);
-      po[1] = make_float4(y[4], y[5], y[6], y[7]);
-      if (n == 0) {
-        ms[FEW_WARPS][r] = top;
-        ls[FEW_WARPS][r] = sum;
-      }
-    });
-    cluster_meet();
-    for (int e = tid * (int)ranks + (int)rank; e < FEW_ROWS * N; e += 32 * FEW_WARPS * (int)ranks) {
-      const int r = e / N, n = e - r * N;
-      if (r / a.T >= a.P || r % a.T >= it.nq) continue;
-      const uint32_t at_m = smem_u32(&ms[FEW_WARPS][r]), at_l = smem_u32(&ls[FEW_WARPS][r]), at_o = smem_u32(&mine[r][n * 8]);
-      float top = -INFINITY, sum = 0.f, y[8] = {};
-      for (int k = 0; k < (int)ranks; ++k) {
-        const float mk = peer_float(at_m, k), lk = peer_float(at_l, k);
-        const float4 y0 = peer_float4(at_o, k), y1 = peer_float4(at_o + 16, k);
-        const float t = fmaxf(top, mk), f0 = t == -INFINITY ? 0.f : ex2p(top - t), f1 = t == -INFINITY ? 0.f : ex2p(mk - t);
-        const float z[8] = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
-        sum = sum * f0 + lk * f1;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = y[i] * f0 + z[i] * f1;
-        top = t;
-      }
-      result(it, r, n, top, sum, y);
+  uint32_t rank, ranks;
+  asm("mov.u32 %0, %%cluster_ctarank;\nmov.u32 %1, %%cluster_nctarank;" : "=r"(rank), "=r"(ranks));
+  PromptItem it;
+  it.s = blockIdx.y;
+  it.h0 = blockIdx.x / ranks * a.P;
+  int k0;
+  q_span<true>(a, it.s, &it.q0, &it.nq);
+  k_span<true>(a, it.s, &k0, &it.nk);
+  if (blockIdx.x == 0 && tid == 0 && a.status && seq_cut<true>(a, it.s)) kv8_record(a.status, CHECK_LENGTH);
+  const int steps = (it.nk + FEW_KEYS - 1) / FEW_KEYS, per = (steps + ranks - 1) / ranks;
+  attend(it, min(steps, (int)rank * per), min(steps, (int)(rank + 1) * per), [&](int r, int n, float top, float sum, float (&y)[8]) {
+    float4* po = reinterpret_cast<float4*>(&mine[r][n * 8]);
+    po[0] = make_float4(y[0], y[1], y[2], y[3]);
+    po[1] = make_float4(y[4], y[5], y[6], y[7]);
+    if (n == 0) {
+      ms[FEW_WARPS][r] = top;
+      ls[FEW_WARPS][r] = sum;
     }
-    cluster_meet();  // the others have read this CTA's
-  } else {
-    if (blockIdx.x == 0 && a.status)
-      for (int s = tid; s < a.n_seqs; s += 32 * FEW_WARPS)
-        if (seq_cut<true>(a, s)) kv8_record(a.status, CHECK_LENGTH);
-    FewRange range(a, lane);
-    PromptItem it;
-    while (range.next(a, lane, tid == 0, &it))
-      attend(it, it.lo, it.n, [&](int r, int n, float top, float sum, float (&y)[8]) { result(it, r, n, top, sum, y); });
+  });
+  cluster_meet();
+  for (int e = tid * (int)ranks + (int)rank; e < FEW_ROWS * N; e += 32 * FEW_WARPS * (int)ranks) {
+    const int r = e / N, n = e - r * N;
+    if (r / a.T >= a.P || r % a.T >= it.nq) continue;
+    const uint32_t at_m = smem_u32(&ms[FEW_WARPS][r]), at_l = smem_u32(&ls[FEW_WARPS][r]), at_o = smem_u32(&mine[r][n * 8]);
+    float top = -INFINITY, sum = 0.f, y[8] = {};
+    for (int k = 0; k < (int)ranks; ++k) {
+      const float mk = peer_float(at_m, k), lk = peer_float(at_l, k);
+      const float4 y0 = peer_float4(at_o, k), y1 = peer_float4(at_o + 16, k);
+      const float t = fmaxf(top, mk), f0 = t == -INFINITY ? 0.f : ex2p(top - t), f1 = t == -INFINITY ? 0.f : ex2p(mk - t);
+      const float z[8] = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
+      sum = sum * f0 + lk * f1;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = y[i] * f0 + z[i] * f1;
+      top = t;
+    }
+    result(it, r, n, top, sum, y);
   }
+  cluster_meet();  // the others have read this CTA's
 }
 
 }  // namespace
