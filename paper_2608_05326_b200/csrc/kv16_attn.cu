@@ -188,6 +188,7 @@ QEVICT_API qevict_status qevict_kv16_attn(const qevict_kv16_attn_args* p, void* 
   a.max_k = (int)(p->max_len < capacity ? p->max_len : capacity);
   a.causal = p->causal;
   a.P = l.P; a.T = l.T; a.splits = 1;
+  a.groups = a.Hq / a.P; a.inv_step = 1.0 / (2 * a.T);
   a.total_q = p->cu_q ? p->total_q : view.n_seqs;
   a.scale_log2 = (float)((p->softmax_scale > 0.f ? (double)p->softmax_scale : 1.0 / sqrt((double)view.D)) * 1.4426950408889634);
   a.out = p->out; a.lse = p->lse; a.q_bounds = p->cu_q; a.k_bounds = p->lens;

@@ -72,6 +72,8 @@ struct PromptArgs {
   const int32_t* table;  // [n_seqs][max_blocks]
   int max_blocks, block_log2, n_pages;
   long long lse_rows;    // rows of lse
+  double inv_step;       // 1 / (2 T)
+  int groups;            // Hq / P
   int by_range;          // each CTA has an equal range of the call's work, else whole items as they fall free
   int slot_rows;         // rows of a partial result
   PagedCut* cuts;        // [CTAs]
@@ -370,6 +372,15 @@ template <bool PAGED> __device__ __forceinline__ PromptItem item_of(const Prompt
 // (The host sees to it that the sum fits 31 bits.)
 constexpr int ITEM_COST = 1024, KEY_COST = 4, KEY_COST_PAIR = 3, RANGE_LEAST = 1024;
 
+// (What runs before the first copy runs once, from instructions that are fetched as they come: some 50 cycles for each, so its
+// divisions are worth replacing.)
+// x / y where that is below 2^20: the float quotient is off by less than one
+__device__ __forceinline__ uint32_t small_quotient(uint32_t x, uint32_t y) {
+  uint32_t q = (uint32_t)__fdividef((float)x, (float)y);
+  if (q * y > x) --q;
+  if (x - q * y >= y) ++q;
+  return q;
+}
 struct PagedSeq {
   int q0, nq, nk, tiles, key_cost;
   // visible keys of row tile t, and of all before it
@@ -388,12 +399,14 @@ struct PagedSeq {
 };
 
 __device__ __forceinline__ PagedSeq paged_seq(const PromptArgs& a, int q0, int nq, int nk) {
-  return {q0, nq, nk, (nq + 2 * a.T - 1) / (2 * a.T), paged_pair(a, nq, nk) ? KEY_COST_PAIR : KEY_COST};
+  // (x + 1/2) / step is at least 1 / (2 step) from a whole number, far more than it is rounded by
+  return {q0, nq, nk, (int)((nq + 2 * a.T - 0.5) * a.inv_step), paged_pair(a, nq, nk) ? KEY_COST_PAIR : KEY_COST};
 }
 
 struct PagedRange {
   uint32_t width, lo, hi, at;  // this CTA's part of the sum; start of the current item
   int s, h, t;
+  bool begun;  // the current item has been given
   PagedSeq seq;
   int lane_q0, lane_nq, lane_nk, first;  // the lane's sequence of 32, of which `first` is the first
 
@@ -414,20 +427,23 @@ struct PagedRange {
   }
 
   __device__ __forceinline__ PagedRange(const PromptArgs& a, int lane) {
-    const int groups = a.Hq / a.P;
+    const int groups = a.groups;
     uint32_t sum = 0, mine = 0;
+#pragma unroll 1
     for (int i = 0; i < a.n_seqs; i += 32) {
       const PagedSeq q = look(a, i, lane);
       mine = q.cost_before(a, q.tiles) * groups;
       sum += __reduce_add_sync(0xffffffffu, mine);
     }
     width = (sum + gridDim.x - 1) / gridDim.x;
+    begun = false;
     if (width < RANGE_LEAST) width = RANGE_LEAST;
     lo = blockIdx.x * width;
     hi = min(lo + width, sum);
     s = a.n_seqs;
     if (lo >= sum) return;
     uint32_t front = 0;  // cost of the sequences before
+#pragma unroll 1
     for (int i = 0;; i += 32) {
       if (a.n_seqs > 32) {
         const PagedSeq q = look(a, i, lane);
@@ -450,9 +466,10 @@ struct PagedRange {
     }
     seq = sequence(a, s, lane);
     const uint32_t head = seq.cost_before(a, seq.tiles);
-    h = (lo - front) / head;
+    h = small_quotient(lo - front, head);
     front += h * head;
     int t0 = 0, t1 = seq.tiles - 1;  // the last tile that starts at or before lo
+#pragma unroll 1
     while (t0 < t1) {
       const int mid = (t0 + t1 + 1) >> 1;
       if (front + seq.cost_before(a, mid) <= lo) t0 = mid; else t1 = mid - 1;
@@ -463,7 +480,22 @@ struct PagedRange {
 
   // The next item of the range, its key tiles in it; false behind the last one.
   __device__ __forceinline__ bool next(const PromptArgs& a, int lane, bool writes, PromptItem* it) {
-    while (s < a.n_seqs && at < hi) {
+#pragma unroll 1
+    while (true) {
+      if (begun) {
+        at += seq.cost(a, t);
+        if (++t == seq.tiles) {
+          t = 0;
+          if (++h == a.groups) {
+            h = 0;
+            do {
+              if (++s < a.n_seqs) seq = sequence(a, s, lane);
+            } while (s < a.n_seqs && seq.tiles == 0);
+          }
+        }
+      }
+      begun = true;
+      if (s >= a.n_seqs || at >= hi) return false;
       const uint32_t end = at + seq.cost(a, t);
       it->valid = 1;
       it->s = s; it->h0 = h * a.P; it->r0 = t * 2 * a.T;
@@ -471,33 +503,24 @@ struct PagedRange {
       it->split = 0;
       item_tiles(a, it);
       const int all = it->n;
-      auto tiles_upto = [&](uint32_t x) { return x <= at + ITEM_COST ? 0 : (int)((x - at - ITEM_COST) / (uint32_t)(seq.key_cost * TILE)); };
-      const int f0 = lo > at ? tiles_upto(lo) : 0;
+      auto tiles_upto = [&](uint32_t x) {
+        if (x <= at + ITEM_COST) return 0;
+        x -= at + ITEM_COST;
+        return (int)(seq.key_cost == KEY_COST ? x / (KEY_COST * TILE) : x / (KEY_COST_PAIR * TILE));
+      };
       const bool ends = end <= hi;
-      const int f1 = ends ? all : tiles_upto(hi);
-      it->lo = f0;
-      it->n = f1;
-      it->slot = f0 == 0 && ends ? -1 : 2 * (int)blockIdx.x + (f0 == 0);
-      if (f0 == 0 && f1 > 0 && !ends && writes) {
-        const PagedCut c = {1, s, it->h0, it->r0, seq.q0, seq.nq, (int)((end - 1) / width), paged_pair(a, seq.nq, seq.nk)};
+      it->lo = lo > at ? tiles_upto(lo) : 0;
+      it->n = ends ? all : tiles_upto(hi);
+      it->slot = it->lo == 0 && ends ? -1 : 2 * (int)blockIdx.x + (it->lo == 0);
+      if (it->lo == 0 && it->n > 0 && !ends && writes) {
+        const PagedCut c = {1, s, it->h0, it->r0, seq.q0, seq.nq, (int)small_quotient(end - 1, width), seq.key_cost == KEY_COST_PAIR};
         a.cuts[blockIdx.x] = c;
       }
-      at = end;
-      if (++t == seq.tiles) {
-        t = 0;
-        if (++h == a.Hq / a.P) {
-          h = 0;
-          do {
-            if (++s < a.n_seqs) seq = sequence(a, s, lane);
-          } while (s < a.n_seqs && seq.tiles == 0);
-        }
-      }
-      if (f1 > f0 || (all == 0 && ends)) {
+      if (it->n > it->lo || (all == 0 && ends)) {
         item_streams<true>(a, it);
         return true;
       }
     }
-    return false;
   }
 };
 
