@@ -699,13 +699,18 @@ def _positions(positions, rotation, tokens, dev):
     return positions.data_ptr(), st[0] if len(shape) == 2 else 0
 
 
-def _rows_like(t, name, dev, dtype, shape):
+def _rows_like(t, name, dev, dtype, n=None, heads=None, d=None):
     """Address and strides of rows [tokens, heads, d] of any strides that keep d contiguous."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.device != dev or len(t.shape) != 3 or \
-            any(want is not None and want != got for want, got in zip(shape, t.shape)) or t.stride(2) != 1:
-        _refuse("%s must be [tokens, heads, d] = %s %s on %s, d contiguous" % (name, tuple("any" if x is None else x for x in shape), dtype, dev))
-    st = t.stride()
-    return t.data_ptr(), st[:2]
+    try:
+        if t.dtype is dtype and t.device == dev:
+            a, b, c = t.shape
+            st = t.stride()
+            if (n is None or a == n) and (heads is None or b == heads) and (d is None or c == d) and st[2] == 1:
+                return t.data_ptr(), st[0], st[1]
+    except (AttributeError, ValueError):
+        pass
+    _refuse("%s must be [tokens, heads, d] = [%s] %s on %s, d contiguous" %
+            (name, ", ".join("any" if x is None else str(x) for x in (n, heads, d)), dtype, dev))
 
 
 def qevict_rope(q, positions, rotation, k=None, out=None, k_out=None, inverse=False, stream=None):
@@ -721,19 +726,19 @@ def qevict_rope(q, positions, rotation, k=None, out=None, k_out=None, inverse=Fa
         _refuse("q must be float16 or bfloat16")
     if not isinstance(rotation, Rotation):
         _refuse("rotation must be a Rotation")
-    p_q, s_q = _rows_like(q, "q", dev, dtype, (None, None, None))
+    p_q, *s_q = _rows_like(q, "q", dev, dtype)
     n, hq, d = q.shape
     p_pos, axis_stride = _positions(positions, rotation, n, dev)
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    p_out, s_out = _rows_like(out, "out", dev, dtype, q.shape)
+        out = q.new_empty((n, hq, d))
+    p_out, *s_out = _rows_like(out, "out", dev, dtype, n, hq, d)
     hk, p_k, s_k, p_ko, s_ko = 0, 0, (0, 0), 0, (0, 0)
     if k is not None:
-        p_k, s_k = _rows_like(k, "k", dev, dtype, (n, None, d))
+        p_k, *s_k = _rows_like(k, "k", dev, dtype, n, None, d)
         hk = k.shape[1]
         if k_out is None:
-            k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
-        p_ko, s_ko = _rows_like(k_out, "k_out", dev, dtype, k.shape)
+            k_out = q.new_empty((n, hk, d))
+        p_ko, *s_ko = _rows_like(k_out, "k_out", dev, dtype, n, hk, d)
     elif k_out is not None:
         _refuse("k_out without k")
     args = _ROPE_PACK.pack(C.sizeof(qevict_rope_args), dev.index, _DTYPES[dtype], d, hq, hk, bool(inverse), 0, n, rotation._address, p_pos,
@@ -794,9 +799,9 @@ class Kv16Cache:
             with torch.cuda.stream(stream):
                 return self.append(k, v, start, cu_new, rotation, positions, q, q_out)
         n, dev, dtype, d = self.n_seqs, self.device, self.dtype, self.head_dim
-        p_k, s_k = _rows_like(k, "k", dev, dtype, (None, self.n_kv_heads, d))
+        p_k, *s_k = _rows_like(k, "k", dev, dtype, None, self.n_kv_heads, d)
         total = k.shape[0]
-        p_v, s_v = _rows_like(v, "v", dev, dtype, (total, self.n_kv_heads, d))
+        p_v, *s_v = _rows_like(v, "v", dev, dtype, total, self.n_kv_heads, d)
         p_start = _want(start, "start", dev, _i32, (n,))
         p_cu = 0 if cu_new is None else _want(cu_new, "cu_new", dev, _i32, (n + 1,))
         p_rot = p_pos = axis_stride = 0
@@ -810,11 +815,11 @@ class Kv16Cache:
             _refuse("positions without a rotation")
         hq, p_q, s_q, p_qo, s_qo = 0, 0, (0, 0), 0, (0, 0)
         if q is not None:
-            p_q, s_q = _rows_like(q, "q", dev, dtype, (total, None, d))
+            p_q, *s_q = _rows_like(q, "q", dev, dtype, total, None, d)
             hq = q.shape[1]
             if q_out is None:
-                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-            p_qo, s_qo = _rows_like(q_out, "q_out", dev, dtype, q.shape)
+                q_out = q.new_empty((total, hq, d))
+            p_qo, *s_qo = _rows_like(q_out, "q_out", dev, dtype, total, hq, d)
         elif q_out is not None:
             _refuse("q_out without q")
         args = _APPEND16_PACK.pack(C.sizeof(qevict_kv16_append_args), hq, self._address, p_rot, total, p_start, p_cu, p_pos, axis_stride,
@@ -833,8 +838,8 @@ class Kv16Cache:
             with torch.cuda.stream(stream):
                 return self.attn(q, lens, cu_q, max_q, max_len, causal, softmax_scale, out, return_lse)
         n, dev, dtype = self.n_seqs, self.device, self.dtype
-        p_q, s_q = _rows_like(q, "q", dev, dtype, (None, None, self.head_dim))
-        total, hq = q.shape[0], q.shape[1]
+        p_q, *s_q = _rows_like(q, "q", dev, dtype, None, None, self.head_dim)
+        total, hq, d = q.shape
         p_lens = _want(lens, "lens", dev, _i32, (n,))
         p_cu = 0 if cu_q is None else _want(cu_q, "cu_q", dev, _i32, (n + 1,))
         if max_q is None:
@@ -842,8 +847,8 @@ class Kv16Cache:
         if max_len is None:
             max_len = self.max_blocks * self.block
         if out is None:
-            out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        p_out, s_out = _rows_like(out, "out", dev, dtype, q.shape)
+            out = q.new_empty((total, hq, d))
+        p_out, *s_out = _rows_like(out, "out", dev, dtype, total, hq, d)
         lse = q.new_empty((hq, total), dtype=_f32) if return_lse else None
         try:
             args = _ATTN16_PACK.pack(C.sizeof(qevict_kv16_attn_args), hq, max_q, max_len, bool(causal), softmax_scale, total, self._address, p_lens,

@@ -437,3 +437,427 @@ def test_attention_of_new_tokens(nq, lens, dtype, hq, hkv, d, block, by_token):
             one, lse1 = cache.attn(q, _i32(lens), max_len=max(lens), causal=causal, return_lse=True)
             _check_attn(one, lse1, q, pools, table, lens, nq, causal, dtype)
     assert int(status) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,hq,hkv,d,block", [
+    (torch.bfloat16, 28, 4, 128, 64), (torch.float16, 16, 1, 128, 32), (torch.bfloat16, 8, 8, 64, 16), (torch.float16, 40, 1, 64, 128), (torch.bfloat16, 37, 1, 128, 16),
+    (torch.float16, 64, 2, 64, 64), (torch.bfloat16, 6, 3, 128, 128),
+])
+@pytest.mark.parametrize("nq,lens", [([1, 1], [900, 77]), ([2, 2], [1500, 130]), ([5, 3], [700, 4]), ([16, 17], [2000, 300]), ([150], [1111])])
+def test_head_layouts(dtype, hq, hkv, d, block, nq, lens):
+    cache, pools, table, status, q = _case(nq, lens, hq, hkv, d, block, dtype, 50)
+    out, lse = cache.attn(q, _i32(lens), _cu(nq), max_q=max(nq), max_len=max(lens), return_lse=True)
+    _check_attn(out, lse, q, pools, table, lens, nq, True, dtype)
+    assert int(status) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gain", [0.02, 8.0])
+@pytest.mark.parametrize("nq,lens", [([1, 3], [700, 1300]), ([200], [900])])
+def test_flat_and_sharp_distributions(gain, nq, lens):
+    cache, pools, table, _, q = _case(nq, lens, 4, 2, 128, 32, torch.bfloat16, 51, gain=gain)
+    out, lse = cache.attn(q, _i32(lens), _cu(nq), return_lse=True)
+    _check_attn(out, lse, q, pools, table, lens, nq, True, torch.bfloat16)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nq", [1, 40, 500])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_logits_that_grow_along_the_keys_move_the_reference(nq, sign):
+    n, hkv, d, block, dtype = 3000, 1, 128, 16, torch.float16
+    cache, pools, table, _, q = _case([nq], [n], 2, hkv, d, block, dtype, 52)
+    slope = sign * torch.linspace(-3, 3, n, device="cuda")
+    for t in range(0, n, block):
+        page = int(table[0, t // block])
+        m = min(block, n - t)
+        pools[0][page, 0, :m] = (pools[0][page, 0, :m].float() * 0.1 + slope[t:t + m, None]).to(dtype)
+    q = (q.float() * 0.1 + 1.0).to(dtype)
+    out, lse = cache.attn(q, _i32([n]), _cu([nq]), max_q=nq, return_lse=True)
+    _check_attn(out, lse, q, pools, table, [n], [nq], True, dtype)
+
+
+@pytest.mark.gpu
+def test_an_own_softmax_scale():
+    for nq in (1, 60):
+        cache, pools, table, _, q = _case([nq], [500], 4, 2, 64, 16, torch.float16, 53)
+        out, lse = cache.attn(q, _i32([500]), _cu([nq]), softmax_scale=0.37, return_lse=True)
+        _check_attn(out, lse, q, pools, table, [500], [nq], True, torch.float16, scale=0.37)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nq,lens", [([1], [9000]), ([1, 1, 1], [40000, 130, 5000]), ([7], [30000]), ([1, 40, 3], [20000, 6001, 90]), ([300, 1], [9000, 30000])])
+@pytest.mark.parametrize("dtype,hq,hkv,d,block", [(torch.bfloat16, 4, 2, 128, 64), (torch.float16, 7, 1, 64, 16)])
+def test_long_contexts_are_shared_by_many_thread_blocks(nq, lens, dtype, hq, hkv, d, block):
+    cache, pools, table, _, q = _case(nq, lens, hq, hkv, d, block, dtype, 54)
+    args = dict(cu_q=_cu(nq), max_q=max(nq), max_len=max(lens), return_lse=True)
+    for causal in (True, False):
+        out, lse = cache.attn(q, _i32(lens), causal=causal, **args)
+        _check_attn(out, lse, q, pools, table, lens, nq, causal, dtype)
+    again, lse2 = cache.attn(q, _i32(lens), causal=False, **args)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+def _fill_pages(pools, table, s, k, v, block):
+    """Puts keys and values [n, H, d] of sequence s into its pages."""
+    for w, x in enumerate((k, v)):
+        for t in range(0, x.shape[0], block):
+            m = min(block, x.shape[0] - t)
+            pools[w][int(table[s, t // block]), :, :m] = x[t:t + m].transpose(0, 1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nq,nk,hq,hkv,d,dtype,block", [
+    (1, 16000, 4, 2, 128, torch.bfloat16, 64), (2, 70000, 4, 2, 128, torch.bfloat16, 64), (1, 70000, 7, 1, 64, torch.float16, 16), (40, 24001, 4, 1, 128, torch.float16, 32),
+    (300, 9000, 2, 1, 64, torch.bfloat16, 128),
+])
+def test_shared_keys_lose_and_exchange_no_part(nq, nk, hq, hkv, d, dtype, block):
+    from test_prompt_attn import _check_rms, _part_keys
+
+    g = torch.Generator().manual_seed(71)
+    q, v = torch.randn((nq, hq, d), generator=g).to(dtype).cuda(), torch.randn((nk, hkv, d), generator=g).to(dtype).cuda()
+    k = _part_keys(nk, hkv, d, 16, dtype, g).cuda()
+    cache, pools, table, _ = _cache([nk], hkv, d, block, dtype, 72)
+    _fill_pages(pools, table, 0, k, v, block)
+    _check_rms(cache.attn(q, _i32([nk]), _cu([nq]), max_q=nq, max_len=nk), q, k, v, True, dtype, 16)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("block", [16, 32, 64, 128])
+@pytest.mark.parametrize("nq,lens", [([1, 1, 1, 1], [1000, 600, 40, 2500]), ([9, 30, 2, 1], [1000, 600, 40, 2500]), ([300], [1500])])
+def test_blocks_that_are_not_there_are_not_attended_to(nq, lens, block):
+    hq, hkv, d, dtype = 4, 2, 128, torch.bfloat16
+    cache, pools, table, status, q = _case(nq, lens, hq, hkv, d, block, dtype, 55)
+    rng = np.random.default_rng(block)
+    for holes in (0.2, 0.9, 1.0):
+        gaps = np.where(rng.random(table.shape) < holes, -1, table).astype(np.int32)
+        gaps[0, :1] = table[0, :1]  # (a sequence that keeps its first block alone)
+        view = binding.Kv16Cache(pools[0], pools[1], torch.tensor(gaps, device="cuda"), status)
+        for max_len in (max(lens), 100000):
+            if max_len > gaps.shape[1] * block:
+                max_len = gaps.shape[1] * block
+            out, lse = view.attn(q, _i32(lens), _cu(nq), max_q=max(nq), max_len=max_len, return_lse=True)
+            _check_attn(out, lse, q, pools, gaps, lens, nq, True, dtype)
+    assert int(status) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nq,n", [(1, 500), (1, 50000), (200, 2000)])
+@pytest.mark.parametrize("wrong", [-2, -2 ** 31, 2 ** 31 - 1, None])
+def test_impossible_pages_are_absent_and_said(nq, n, wrong):
+    hq, hkv, d, block, dtype = 4, 2, 64, 32, torch.float16
+    cache, pools, table, status, q = _case([nq], [n], hq, hkv, d, block, dtype, 56)
+    table = table.copy()
+    table[0, 3] = table[0, -1] = pools[0].shape[0] if wrong is None else wrong
+    view = binding.Kv16Cache(pools[0], pools[1], torch.tensor(table, device="cuda"), status)
+    out, lse = view.attn(q, _i32([n]), _cu([nq]), max_q=nq, return_lse=True)
+    _check_attn(out, lse, q, pools, table, [n], [nq], True, dtype)
+    assert int(status) == 10
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nq,lens", [([4, 1], [70, 9]), ([70, 9], [70, 9]), ([3, 1], [41000, 900])])
+def test_what_lies_outside_the_sequences_is_neither_used_nor_written(nq, lens):
+    hq, hkv, d, block, dtype = 4, 2, 128, 32, torch.bfloat16
+    cache, pools, table, status, _ = _case(nq, lens, hq, hkv, d, block, dtype, 57)
+    q = _rows(5 + sum(nq) + 50, hq, d, dtype, 58)
+    q[:5], q[5 + sum(nq):] = float("nan"), float("inf")
+    out, before = torch.full_like(q, 3.0), [x.clone() for x in pools]
+    got, lse = cache.attn(q, _i32(lens), _cu(nq, 5), max_q=max(nq), max_len=max(lens), out=out, return_lse=True)
+    assert got is out
+    _check_attn(out, lse, q, pools, table, lens, nq, True, dtype, 5)
+    a, b = 5, 5 + sum(nq)
+    assert (out[:a] == 3).all() and (out[b:] == 3).all() and int(status) == 0
+    assert all(torch.equal(x.view(torch.int16), y.view(torch.int16)) for x, y in zip(pools, before))
+    one = cache.attn(q[:7], _i32(lens), out=out[:7])  # without bounds: one token each, rows of nobody behind
+    assert (one[2:5] == 3).all()
+
+
+@pytest.mark.gpu
+def test_a_sequence_has_the_same_bits_whatever_values_are_next_to_it():
+    hq, hkv, d, block, dtype = 6, 2, 128, 16, torch.bfloat16
+    for nq, lens in (([1, 1, 1], [900, 16, 4000]), ([37, 3, 150], [900, 16, 4000]), ([2, 1, 1], [900, 16, 60000])):
+        cache, pools, table, _, q = _case(nq, lens, hq, hkv, d, block, dtype, 59, gain=4.0)
+        args = dict(cu_q=_cu(nq), max_q=max(nq), max_len=max(lens), return_lse=True)
+        alone = cache.attn(q, _i32(lens), **args)
+        for fill in (1e4, float("nan"), float("inf")):
+            q2 = q.clone()
+            q2[nq[0]:nq[0] + nq[1]] = fill
+            for x in pools:
+                x[int(table[1, 0])] = fill
+            out, lse = cache.attn(q2, _i32(lens), **args)
+            for a, b in ((0, nq[0]), (nq[0] + nq[1], sum(nq))):
+                assert torch.equal(out[a:b], alone[0][a:b]) and torch.equal(lse[:, a:b], alone[1][:, a:b])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("max_q,max_len,lens,cu,rows,code", [
+    (4, 600, [600, 90], [0, 4, 6], 6, 0), (3, 600, [600, 90], [0, 4, 6], 6, 11), (4, 599, [600, 90], [0, 4, 6], 6, 11), (4, 600, [-1, 90], [0, 4, 6], 6, 11),
+    (4, 600, [600, 90], [0, 4, 3], 6, 11), (4, 600, [600, 90], [0, 4, 8], 6, 11), (4, 600, [600, 90], [-2, 4, 6], 6, 11), (4, 10 ** 6, [10 ** 6, 90], [0, 4, 6], 6, 11),
+    (2 ** 31 - 1025, 2 ** 31 - 1, [600, 90], [0, 4, 6], 6, 0),
+])
+def test_lengths_and_bounds_that_are_cut_set_the_status(max_q, max_len, lens, cu, rows, code):
+    hq, hkv, d, block, dtype = 2, 1, 64, 16, torch.float16
+    for more in (1, 40):  # few rows, and tiles of them
+        true = [608, 96]
+        cache, pools, table, status = _cache(true, hkv, d, block, dtype, 60)
+        n_rows = rows * more
+        q = _rows(n_rows, hq, d, dtype, 61)
+        bounds = [c * more for c in cu]
+        mq = max_q * more if max_q < 1000 else max_q
+        out, lse = cache.attn(q, _i32(lens), _i32(bounds), max_q=mq, max_len=max_len, out=torch.full_like(q, 3.0), return_lse=True)
+        assert int(status) == code, int(status)
+        cap = min(table.shape[1] * block, max_len)
+        pages = oracle.Pages([_np(x) for x in pools], table)
+        for s in range(2):
+            a, b = max(0, min(bounds[s], n_rows)), min(bounds[s + 1], n_rows)
+            if b <= a or (code and s == 1 and cu[1] > cu[2]):
+                continue
+            m, n = min(b - a, mq), max(0, min(lens[s], cap))
+            k, v, places = pages.rows(s, n)
+            _check_seq(out[a:a + m], lse[:, a:a + m], q[a:a + m], k, v, n, places, True, dtype, (more, s))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_seqs", [33, 700])
+@pytest.mark.parametrize("most", [1, 3, 90])
+def test_many_sequences(n_seqs, most):
+    hq, hkv, d, block, dtype = 4, 2, 64, 16, torch.bfloat16
+    rng = np.random.default_rng(n_seqs + most)
+    nq = rng.integers(0, most + 1, n_seqs)
+    lens = nq + rng.integers(0, 200, n_seqs)
+    lens[5], nq[7], lens[9] = 3000, most, 0
+    cache, pools, table, status, q = _case(list(nq), list(lens), hq, hkv, d, block, dtype, 62)
+    out, lse = cache.attn(q, _i32(lens), _cu(nq), max_q=most, max_len=int(max(lens)), return_lse=True)
+    _check_attn(out, lse, q, pools, table, [int(x) for x in lens], [int(x) for x in nq], True, dtype)
+    assert int(status) == 0
+
+
+@pytest.mark.gpu
+def test_as_many_sequences_as_a_call_takes():
+    n, hq, hkv, d, block, dtype = 65535, 2, 1, 64, 16, torch.float16
+    g = torch.Generator().manual_seed(63)
+    pools = [torch.randn((50, hkv, block, d), generator=g).to(dtype).cuda() for _ in range(2)]
+    table = torch.randint(0, 50, (n, 2), generator=g, dtype=torch.int32)
+    lens = torch.randint(0, 33, (n,), generator=g, dtype=torch.int32)
+    q = _rows(n, hq, d, dtype, 64)
+    cache = binding.Kv16Cache(pools[0], pools[1], table.cuda())
+    out, lse = cache.attn(q, lens.cuda(), return_lse=True)
+    pages = oracle.Pages([_np(x) for x in pools], table.numpy())
+    for s in (0, 1, 31, 32, 40000, 65533, 65534):
+        k, v, places = pages.rows(s, int(lens[s]))
+        _check_seq(out[s:s + 1], lse[:, s:s + 1], q[s:s + 1], k, v, int(lens[s]), places, True, dtype, s)
+    empty = (lens == 0).cuda()
+    assert not out[empty].any() and torch.isneginf(lse[:, empty]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nq", [1, 50])
+def test_pages_past_2_to_the_31_elements(nq):
+    hq, hkv, d, block, dtype = 16, 8, 128, 128, torch.float16
+    n_pages = (1 << 31) // (hkv * d * block) + 40
+    pools = [torch.zeros((n_pages, hkv, block, d), dtype=dtype, device="cuda") for _ in range(2)]
+    table = np.array([[n_pages - 1, 0, n_pages - 30, n_pages - 2]], np.int32)
+    for x in pools:
+        for p in table[0]:
+            x[int(p)] = _rows(hkv * block, 1, d, dtype, int(p) % 97)[:, 0].view(hkv, block, d)
+    cache = binding.Kv16Cache(pools[0], pools[1], torch.tensor(table, device="cuda"))
+    q = _rows(nq, hq, d, dtype, 65)
+    out, lse = cache.attn(q, _i32([500]), _cu([nq]), max_q=nq, return_lse=True)
+    small = [torch.stack([x[int(p)] for p in table[0]]) for x in pools]
+    _check_attn(out, lse, q, small, np.arange(4)[None], [500], [nq], True, dtype)
+
+
+def _strided(how, n_pages, hkv, block, d, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    shapes = {"pairs": (n_pages, 2, hkv, block, d), "by token": (n_pages, block, hkv, d), "padded heads": (n_pages, block, hkv, d + 8), "padded rows": (n_pages, hkv, block, d + 8),
+              "heads first": (hkv, n_pages, block, d)}
+    pools = [torch.randn(shapes[how], generator=g).to(dtype).cuda() for _ in range(1 if how == "pairs" else 2)]
+    if how == "pairs":
+        return [pools[0][:, 0], pools[0][:, 1]]
+    if how == "heads first":
+        return [x.transpose(0, 1) for x in pools]
+    if how == "padded rows":
+        return [x[..., :d] for x in pools]
+    return [x[..., :d].transpose(1, 2) for x in pools]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("how", ["pairs", "by token", "padded heads", "padded rows", "heads first"])
+@pytest.mark.parametrize("nq", [2, 90])
+@pytest.mark.parametrize("d,block,dtype", [(128, 16, torch.bfloat16), (64, 128, torch.float16)])
+def test_strides_of_the_pages(how, nq, d, block, dtype):
+    hq, hkv, n = 6, 3, 700
+    n_pages = -(-n // block) + 3
+    pools = _strided(how, n_pages, hkv, block, d, dtype, 66)
+    before = [x.clone() for x in pools]
+    table = np.random.default_rng(67).permutation(n_pages)[None, :-(-n // block)].astype(np.int32)
+    cache = binding.Kv16Cache(pools[0], pools[1], torch.tensor(table, device="cuda"))
+    k, v = _rows(nq, hkv, d, dtype, 68), _rows(nq, hkv, d, dtype, 69)
+    cache.append(k, v, _i32([n - nq]), cu_new=_cu([nq]))
+    _check_append(cache, pools, table, before, k, v, [n - nq], [nq], [0], _np(k), np.zeros(k.shape))
+    wide = _rows(nq, hq + 2, d + 8, dtype, 70)
+    q, out = wide[:, 1:hq + 1, 8:], torch.empty((hq, nq, d), dtype=dtype, device="cuda").transpose(0, 1)
+    got, lse = cache.attn(q, _i32([n]), _cu([nq]), out=out, return_lse=True)
+    assert got is out
+    _check_attn(out, lse, q, pools, table, [n], [nq], True, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nq,lens", [([2, 1], [700, 90]), ([1, 3], [60000, 90]), ([333, 90], [333, 900]), ([3000], [3100])])
+def test_the_output_may_take_the_place_of_the_queries(nq, lens):
+    cache, _, _, _, q = _case(nq, lens, 8, 2, 128, 64, torch.bfloat16, 73)
+    args = dict(cu_q=_cu(nq), max_q=max(nq), max_len=max(lens))
+    want = cache.attn(q, _i32(lens), **args)
+    got = cache.attn(q, _i32(lens), out=q, **args)
+    assert got is q and torch.equal(q, want)
+
+
+@pytest.mark.gpu
+def test_many_work_items_are_handed_out_whole():
+    # more than six items for each SM: 32 heads of their own KV head
+    nq, lens, hq, d, dtype = [4100], [4500], 32, 64, torch.float16
+    cache, pools, table, _, q = _case(nq, lens, hq, hq, d, 128, dtype, 74)
+    out, lse = cache.attn(q, _i32(lens), _cu(nq), return_lse=True)
+    rows = [torch.cat([x[int(p)] for p in table[0]], dim=1)[:, :lens[0]].transpose(0, 1) for x in pools]
+    for h in (0, 17, 31):
+        _check_seq(out[:, h:h + 1], lse[h:h + 1], q[:, h:h + 1], _np(rows[0][:, h:h + 1]), _np(rows[1][:, h:h + 1]), lens[0], None, True, dtype, h)
+
+
+# ---- the operators together ------------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,hq,hkv,d,block,n_axes", [(torch.bfloat16, 8, 2, 128, 16, 1), (torch.float16, 6, 3, 64, 64, 3)])
+def test_prompts_in_pieces_then_drafts_then_tokens(dtype, hq, hkv, d, block, n_axes):
+    """Two sequences as a server takes them, against the attention of whole prompts over keys rotated by themselves."""
+    rotation, _ = _spec(d // 2, n_axes)
+    total = [410, 300]
+    qkv = [[_rows(n, h, d, dtype, 80 + s) for h in (hq, hkv, hkv)] for s, n in enumerate(total)]
+    pos = [_i32(np.random.default_rng(s).integers(0, 9999, (n_axes, n))) if n_axes > 1 else _i32(np.arange(n))[None] for s, n in enumerate(total)]
+    whole = []
+    for (q, k, v), p, n in zip(qkv, pos, total):
+        rq, rk = binding.qevict_rope(q, p, rotation, k=k)
+        whole.append((binding.qevict_prompt_attn(rq, rk, v, _cu([n]), return_lse=True), rq, rk, v))
+    cache = binding.Kv16Cache.allocate(80, 2, 32, hkv, d, block, dtype)
+    cache.block_table.copy_(torch.randperm(80, generator=torch.Generator().manual_seed(1))[:64].view(2, 32).to(torch.int32))
+    at = [0, 0]
+    out = [torch.zeros_like(x[0]) for x in qkv]
+    for step in ([200, 90], [150, 200], [5, 3], [1, 0], [0, 1], [4, 6], [50, 0]):
+        take = [slice(a, a + m) for a, m in zip(at, step)]
+        q, k, v = (torch.cat([x[i][t] for x, t in zip(qkv, take)]) for i in range(3))
+        start, cu = _i32(at), _cu(step)
+        p = torch.cat([x[:, t] for x, t in zip(pos, take)], dim=1) if n_axes > 1 else None
+        rq = cache.append(k, v, start, cu_new=cu, rotation=rotation, positions=p, q=q)
+        got = cache.attn(rq, start + cu.diff(), cu_q=cu, max_q=max(step))
+        for s, part in enumerate(got.split(step)):
+            out[s][take[s]] = part
+        at = [a + m for a, m in zip(at, step)]
+    assert at == total and int(cache.status) == 0
+    for s, ((_, lse), rq, rk, v) in enumerate(whole):
+        _check_seq(out[s], lse, rq, _np(rk), _np(v), total[s], None, True, dtype, s)
+    # a draft that is not accepted: the sequence is cut back and goes on
+    again = cache.attn(whole[0][1][190:200].contiguous(), _i32([200, 0]), cu_q=_cu([10, 0]))
+    want = prompt.attention(_np(whole[0][1][190:200]), _np(whole[0][2][:200]), _np(whole[0][3][:200]), True)
+    tol = prompt.out_tolerance(want[0], want[2], float(whole[0][3].abs().max()), 200, d, want[3], HALF_STEP[dtype], HALF_STEP[dtype])
+    assert (np.abs(_np(again) - want[0]) <= tol).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nq,room", [(1, 600), (1, 40000), (30, 600)])
+def test_captured_with_the_lengths_advanced_inside(nq, room):
+    hq, hkv, d, block, dtype, n = 4, 2, 128, 64, torch.bfloat16, 2
+    rotation, _ = _spec(64)
+    cache, pools, table, status = _cache([room] * n, hkv, d, block, dtype, 90)
+    q, k, v = (_rows(n * nq, h, d, dtype, 91 + i) for i, h in enumerate((hq, hkv, hkv)))
+    first = [100, room - 10 * nq]
+    lens, cu = _i32(first), _cu([nq] * n)
+    graphs, outs = [], []
+    for _ in range(2):  # two graphs of the same step
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            rq = cache.append(k, v, lens, cu_new=cu, rotation=rotation, q=q)
+            lens += nq
+            outs.append(cache.attn(rq, lens, cu_q=cu, max_q=nq, max_len=room, return_lse=True))
+        graphs.append((graph, rq))
+    for step in range(4):
+        k.copy_(_rows(n * nq, hkv, d, dtype, 95 + step))
+        graph, rq = graphs[step % 2]
+        graph.replay()
+        out, lse = outs[step % 2]
+        _check_attn(out, lse, rq, pools, table, [f + (step + 1) * nq for f in first], [nq] * n, True, dtype)
+    assert int(status) == 0
+
+
+@pytest.mark.gpu
+def test_two_calls_at_once_and_on_another_stream():
+    cases = [_case(nq, lens, 8, 2, 128, 32, torch.bfloat16, 100 + i) for i, (nq, lens) in enumerate((([1, 2], [30000, 700]), ([500], [2000]), ([1], [300])))]
+    calls = [(c[0], c[4], _i32(lens), _cu(nq)) for c, (nq, lens) in zip(cases, (([1, 2], [30000, 700]), ([500], [2000]), ([1], [300])))]
+    want = [c.attn(q, lens, cu) for c, q, lens, cu in calls]
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for s, (c, q, lens, cu) in zip(streams, calls):
+            got.append(c.attn(q, lens, cu, stream=s))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.gpu
+def test_the_first_call_of_a_process_may_be_captured():
+    import os
+    import subprocess
+    import sys
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = """
+import torch
+from paper_2608_05326_b200 import binding
+cache = binding.Kv16Cache.allocate(70, 1, 64, 2, 64, 128, torch.float16)
+cache.block_table.copy_(torch.arange(64, dtype=torch.int32)[None])
+g = torch.Generator().manual_seed(1)
+k, v = (torch.randn((1300, 2, 64), generator=g).half().cuda() for _ in range(2))
+q = torch.randn((1300, 4, 64), generator=g).half().cuda()
+rotation = binding.Rotation.standard(64)
+start, lens, cu = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0], [1300], [0, 1300]))
+few = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    rq = cache.append(k, v, start, cu_new=cu, rotation=rotation, q=q)
+    out = cache.attn(rq, lens, cu_q=cu)
+    last = cache.attn(rq[-1:], lens, cu_q=few, max_q=1, max_len=1300)
+graph.replay()
+again = cache.attn(rq, lens, cu_q=cu)
+one = cache.attn(rq[-1:], lens, cu_q=few, max_q=1, max_len=1300)
+assert torch.equal(out, again) and torch.equal(last, one) and out.abs().sum() > 0
+print("captured")
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=root, timeout=600)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stdout[-1000:] + r.stderr[-3000:]
+
+
+@pytest.mark.gpu
+def test_nothing_to_attend_to_and_nothing_to_do():
+    cache, pools, table, status = _cache([64, 64], 2, 64, 16, torch.float16, 110)
+    q = _rows(40, 4, 64, torch.float16, 111)
+    for cu, mq in (([0, 1, 2], 1), ([0, 20, 40], 20)):
+        rows = cu[-1]
+        out, lse = cache.attn(q[:rows], _i32([0, 0]), _i32(cu), max_q=mq, return_lse=True)
+        assert not out.any() and torch.isneginf(lse).all()
+    for args in (dict(cu_q=_i32([0, 0, 0])), dict(max_q=0, cu_q=_i32([0, 20, 40]))):
+        out = cache.attn(q, _i32([64, 64]), out=torch.full_like(q, 3.0), **args)
+        assert (out == 3).all()
+    out = cache.attn(q[:2], _i32([64, 64]), max_len=0)
+    assert not out.any() and int(status) == 11
+    assert cache.attn(q[:0], _i32([64, 64]), cu_q=_i32([0, 0, 0])).shape == (0, 4, 64)
+
+
+@pytest.mark.gpu
+def test_attention_of_the_binding_refuses_what_the_library_cannot_see():
+    cache = binding.Kv16Cache.allocate(4, 2, 2, 2, 64, 16, torch.float16)
+    q, lens, cu = _rows(2, 4, 64, torch.float16, 2), _i32([0, 0]), _i32([0, 1, 2])
+    for bad in (lambda: cache.attn(q.float(), lens), lambda: cache.attn(q[0], lens), lambda: cache.attn(q[..., :32], lens), lambda: cache.attn(q, lens[:1]),
+                lambda: cache.attn(q, lens.long()), lambda: cache.attn(q, lens, cu_q=lens), lambda: cache.attn(q, lens, out=q[:1]), lambda: cache.attn(q, lens, out=q.bfloat16()),
+                lambda: cache.attn(q, lens, max_q=2 ** 40), lambda: cache.attn(q, lens, max_len="a"), lambda: cache.attn(q, lens, max_q=2), lambda: cache.attn(q[:1], lens),
+                lambda: cache.attn(q, lens, cu_q=cu, softmax_scale=-1.0), lambda: cache.attn(q[:, :3], lens), lambda: cache.attn(q.transpose(1, 2), lens)):
+        with pytest.raises(binding.QEvictError):
+            bad()
