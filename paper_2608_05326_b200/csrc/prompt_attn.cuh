@@ -236,7 +236,7 @@ template <int D> struct PromptSmem {
   static constexpr int HALF = TILE * 128;             // 64 channels of 128 rows
   static constexpr int TILE_BYTES = HALF * (D / 64);
   static constexpr int Q_OFF = 0, KV_OFF = 2 * TILE_BYTES, BAR_OFF = KV_OFF + STAGES * TILE_BYTES;
-  static constexpr int WORDS = 256, ITEMS = 320, ROWS = 592;  // behind the barriers: words, work items, row maxima
+  static constexpr int WORDS = 320, ITEMS = 384, ROWS = 656;  // behind the barriers: words, work items, row maxima
   static constexpr int BYTES = BAR_OFF + ROWS + 2048;
 };
 
@@ -444,7 +444,7 @@ struct PagedRange {
     if (lo >= sum) return;
     uint32_t front = 0;  // cost of the sequences before
 #pragma unroll 1
-    for (int i = 0;; i += 32) {
+    for (int i = 0; i < a.n_seqs; i += 32) {
       if (a.n_seqs > 32) {
         const PagedSeq q = look(a, i, lane);
         mine = q.cost_before(a, q.tiles) * groups;
@@ -534,10 +534,11 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const uint32_t smb = smem_u32(sm), bars = smb + SM::BAR_OFF;
   // barriers: Q full / empty; ring full / empty; S ready, P ready, O ready of both tiles; value tail zeroed; work items
-  // full / empty (two places); answer to the request for the next one; products done after a failure
+  // full / empty (two places); answer to the request for the next one; products done after a failure; (paged) the four warps
+  // that share rows of a pair
   const uint32_t b_q = bars, b_full = bars + 8, b_empty = b_full + 8 * NS, b_s = b_empty + 8 * NS, b_p = b_s + 16, b_o = b_p + 16,
                  b_clean = b_o + 16, b_qe = b_clean + 8, b_item = b_qe + 8, b_taken = b_item + 16, b_next = b_taken + 16,
-                 b_done = b_next + 8;
+                 b_done = b_next + 8, b_quad = b_done + 8;
   // (paged) words 9 .. 12: a byte for each of the last 16 key tiles, bit i: its i-th block is absent
   // words: 0 .. 3 the answer; 4 tensor memory; 5 loads of K and V issued; 6 a wait has given up; 7 loads of Q; 8 requests for items
   volatile uint32_t* words = reinterpret_cast<volatile uint32_t*>(sm + SM::BAR_OFF + SM::WORDS);
@@ -568,6 +569,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
     bar_init(b_clean, 1);
     bar_init(b_next, 1);
     bar_init(b_done, 1);
+    for (int i = 0; i < 4; ++i) bar_init(b_quad + 8 * i, 4);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     for (int i = 5; i < 9; ++i) words[i] = 0;
     for (int i = 0; i < 4; ++i) items[i].valid = 0;
@@ -994,7 +996,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
                    : "=r"(both) : "r"((uint32_t)ok), "r"(1 + w * 4 + (wid & 3)) : "memory");
       ok = both != 0;
     };
-    uint32_t s_phase = 0, o_phase = 0;
+    uint32_t s_phase = 0, o_phase = 0, quad_phase = 0;
     while (true) {
       const PromptItem* item = next_item();
       meet();
@@ -1096,20 +1098,24 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       if (!ok) break;
       if constexpr (PAGED) {
         if (twin) {
-          // both tiles' results of the same rows: four warps share them, a quarter of the channels each
+          // Both tiles' results of the same rows: four warps share them, a quarter of the channels each.  They meet at a barrier with a
+          // bounded wait, which ends too when another tile's warps have given up; the two that share a tile then agree.
           auto meet4 = [&] {
-            uint32_t all;
-            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}\n"
-                         : "=r"(all) : "r"((uint32_t)ok), "r"(9 + (wid & 3)) : "memory");
-            ok = all != 0;
+            tm_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(b_quad + 8 * (wid & 3));
+            ok = ok && wait_item(b_quad + 8 * (wid & 3), quad_phase);
+            quad_phase ^= 1u;
+            tm_after();
+            meet();
           };
           float* both = reinterpret_cast<float*>(sm + SM::BAR_OFF + SM::ROWS) + r;
           l = xch[0] + xch[TILE];
           meet4();
+          if (!ok) break;
           xch[half * TILE] = half ? l : m;
           meet4();
           if (!ok) break;
-          tm_after();
           const float m0 = both[0], m1 = both[2 * TILE], top = fmaxf(m0, m1);
           const float f0 = top == -INFINITY ? 0.f : ex2p(m0 - top), f1 = top == -INFINITY ? 0.f : ex2p(m1 - top);
           l = both[TILE] * f0 + both[3 * TILE] * f1;
@@ -1146,7 +1152,6 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
             }
             __syncwarp();
           }
-          tm_before();
           meet4();  // the next item's first products overwrite both
           if (!ok) break;
           continue;
