@@ -75,7 +75,7 @@ struct PromptArgs {
   double inv_step;       // 1 / (2 T)
   int groups;            // Hq / P
   int by_range;          // each CTA has an equal range of the call's work, else whole items as they fall free
-  int slot_rows;         // rows of a partial result
+  int slot_rows;         // rows of a partial result: [slot][D / 4][slot_rows][4], a warp's rows side by side
   PagedCut* cuts;        // [CTAs]
   int group_bytes, half_bytes;  // of K and V tiles in shared memory: from 8 keys to the next 8, from 64 channels to the next 64
   int boxes;             // copies for each page: one, or one for each 64 channels
@@ -524,6 +524,12 @@ struct PagedRange {
   }
 };
 
+// Four channels from c on of row r of a partial result.  (Rows of D channels side by side had a warp write 32 pieces of 16 bytes at a
+// time: 25 to 33 thousand cycles for the results of an item.)
+template <int D> __device__ __forceinline__ float4* part_at(const PromptArgs& a, int slot, int c, int r) {
+  return reinterpret_cast<float4*>(a.part_o) + ((long long)slot * (D / 4) + (c >> 2)) * a.slot_rows + r;
+}
+
 template <class T, int D, bool PAGED>
 __global__ void __launch_bounds__(PROMPT_THREADS, 1)
     prompt_attn_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
@@ -702,21 +708,9 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         const bool pair = PAGED && it.pair;
         const int c0 = pair ? it.cnt(0) : it.n - it.lo, c1 = pair ? it.cnt(1) : 0;  // key tiles of the (two) streams
         if (c0 == 0) continue;
-        if (q_turn > 0) ok = wait_item(b_qe, (uint32_t)(q_turn - 1) & 1u);
-        ++q_turn;
-        if (ok && lane == 0) {
-          const int two = (it.cnt(0) > 0) + (!pair && it.cnt(1) > 0);
-          bar_expect(b_q, (uint32_t)two * (uint32_t)(a.T * a.P * D * 2));
-#pragma unroll
-          for (int w = 0; w < 2; ++w)
-            if (it.cnt(w) > 0 && !(pair && w))
-              for (int x = 0; x < D / 64; ++x)
-                tma_load(smb + SM::Q_OFF + w * SM::TILE_BYTES + x * SM::HALF, &mq, b_q, x * 64, it.q0 + it.r0 + w * a.T, it.h0, cs);
-          words[7] = (uint32_t)q_turn;
-        }
+        int k_tiles = it.before;
         int v_slot = 0;
         uint32_t v_phase = 0;
-        int k_tiles = it.before;
         bool clean = it.dirty(), v_seen = false;
         // Paged: 32 page ids of each stream, one per lane, and the 32 below them on their way.  A block that is not there has a
         // page behind the last one: the copy then writes zeros.
@@ -796,8 +790,21 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
           }
           __syncwarp();
         };
-        // K, V of the last tile, K, V of the one before, ...; those of two streams in turn, in the order of their products
+        // K, V of the last tile, K, V of the one before, ...; those of two streams in turn, in the order of their products.  (The
+        // queries' place is free when the last item's last S is done: its first keys need not wait for that.)
         issue(0, false, it.n - 1);
+        if (q_turn > 0) ok = wait_item(b_qe, (uint32_t)(q_turn - 1) & 1u);
+        ++q_turn;
+        if (ok && lane == 0) {
+          const int two = (it.cnt(0) > 0) + (!pair && it.cnt(1) > 0);
+          bar_expect(b_q, (uint32_t)two * (uint32_t)(a.T * a.P * D * 2));
+#pragma unroll
+          for (int w = 0; w < 2; ++w)
+            if (it.cnt(w) > 0 && !(pair && w))
+              for (int x = 0; x < D / 64; ++x)
+                tma_load(smb + SM::Q_OFF + w * SM::TILE_BYTES + x * SM::HALF, &mq, b_q, x * 64, it.q0 + it.r0 + w * a.T, it.h0, cs);
+          words[7] = (uint32_t)q_turn;
+        }
         if (c1 > 0) issue(1, false, it.mid - 1);
         for (int i = 0; i < c0 && ok; ++i) {
           issue(0, true, it.n - 1 - i);
@@ -1143,7 +1150,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
             if (mine && it.slot >= 0) {
 #pragma unroll
               for (int k = 0; k < 16; k += 4)
-                *reinterpret_cast<float4*>(a.part_o + slot * D + c0 + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                *part_at<D>(a, it.slot, c0 + c + k, r) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
             } else if (mine) {
 #pragma unroll
               for (int k = 0; k < 16; k += 8)
@@ -1185,7 +1192,9 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         if (!mine) continue;
         if (partial) {
 #pragma unroll
-          for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4*>(po + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+          for (int k = 0; k < 16; k += 4)
+            *(PAGED ? part_at<D>(a, it.slot, half * (D / 2) + c + k, w * TILE + r) : reinterpret_cast<float4*>(po + c + k)) =
+                make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
         } else {
 #pragma unroll
           for (int k = 0; k < 16; k += 8)
@@ -1294,60 +1303,40 @@ __global__ void __launch_bounds__(256) prompt_merge_kernel(const PromptArgs a) {
         L == 0.f ? -INFINITY : (Ms + log2f(L)) * 0.6931471805599453f;
 }
 
-// Paged: joins the partial results of the items that ranges share: blockIdx.y is the CTA in whose range such an item starts, one
-// warp per row of it.
+// Paged: joins the partial results of the items that ranges share: blockIdx.y is the CTA in whose range such an item starts, a
+// lane per row of 32, a warp per eight channels.
 template <class T, int D>
-__global__ void __launch_bounds__(256) paged_merge_kernel(const PromptArgs a) {
-  constexpr int PER = D / 32;
-  const int lane = threadIdx.x & 31, i = blockIdx.x * 8 + (threadIdx.x >> 5), cta = blockIdx.y;
+__global__ void __launch_bounds__(D * 4) paged_merge_kernel(const PromptArgs a) {
+  const int i = blockIdx.x * 32 + (threadIdx.x & 31), c8 = (threadIdx.x >> 5) * 8, cta = blockIdx.y;
   pdl_prologue();
   const PagedCut c = a.cuts[cta];
   const int w = i / TILE, r = i - w * TILE, hl = r / a.T, tok = w * a.T + r - hl * a.T;
   if (!c.valid || hl >= a.P || c.r0 + tok >= c.nq || (c.pair && w)) return;
   const int parts = c.last - cta + 1;
   // part 0 ends its CTA's range, the others begin theirs
-  auto place = [&](int p) { return (long long)(2 * (cta + p) + (p == 0)) * a.slot_rows + i; };
-  float M = -INFINITY;
-  for (int p = lane; p < parts; p += 32) {
-    const float x = a.part_lse[place(p)];
-    M = x != x || M != M ? NAN : fmaxf(M, x);
-  }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    const float x = __shfl_xor_sync(0xffffffffu, M, o);
-    M = x != x || M != M ? NAN : fmaxf(M, x);
-  }
-  const float Ms = M == -INFINITY ? 0.f : M;
-  float L = 0.f, sum[PER] = {};
-  for (int p0 = 0; p0 < parts; p0 += 32) {
-    const float weight = p0 + lane < parts ? ex2p(a.part_lse[place(p0 + lane)] - Ms) : 0.f;
-    L += weight;
-    const int n = min(32, parts - p0);
+  auto slot = [&](int p) { return 2 * (cta + p) + (p == 0); };
+  float top = -INFINITY, sum = 0.f, y[8] = {};
+  bool bad = false;
 #pragma unroll 4
-    for (int p = 0; p < n; ++p) {
-      const float f = __shfl_sync(0xffffffffu, weight, p);
-      const float* src = a.part_o + place(p0 + p) * D + lane * PER;
-      float v[PER];
-      if (PER == 4) {
-        const float4 x = *reinterpret_cast<const float4*>(src);
-        v[0] = x.x; v[1] = x.y; v[2 % PER] = x.z; v[3 % PER] = x.w;
-      } else {
-        const float2 x = *reinterpret_cast<const float2*>(src);
-        v[0] = x.x; v[1] = x.y;
-      }
+  for (int p = 0; p < parts; ++p) {
+    const float x = a.part_lse[(long long)slot(p) * a.slot_rows + i];
+    const float4 v0 = *part_at<D>(a, slot(p), c8, i), v1 = *part_at<D>(a, slot(p), c8 + 4, i);
+    bad = bad || x != x;  // the part was given up
+    const float t = fmaxf(top, x), f0 = t == -INFINITY ? 0.f : ex2p(top - t), f1 = t == -INFINITY ? 0.f : ex2p(x - t);
+    const float v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+    sum = sum * f0 + f1;
 #pragma unroll
-      for (int k = 0; k < PER; ++k) sum[k] += f * v[k];
-    }
+    for (int k = 0; k < 8; ++k) y[k] = y[k] * f0 + f1 * v[k];
+    top = t;
   }
+  const float inv = bad ? NAN : sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-  for (int o = 16; o; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+  for (int k = 0; k < 8; ++k) y[k] = sum == 0.f && !bad ? 0.f : y[k] * inv;
   const long long prow = (long long)c.q0 + c.r0 + tok;
   const int hq = c.h0 + hl;
-  T* out = static_cast<T*>(a.out) + prow * a.out_stride[2] + hq * a.out_stride[1] + lane * PER;
-#pragma unroll
-  for (int k = 0; k < PER; k += 2)
-    *reinterpret_cast<uint32_t*>(out + k) = L == 0.f ? 0u : pack2<T>(sum[k] / L, sum[k + 1] / L);
-  if (lane == 0 && a.lse) a.lse[hq * a.lse_rows + prow] = L == 0.f ? -INFINITY : (Ms + log2f(L)) * 0.6931471805599453f;
+  *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + prow * a.out_stride[2] + hq * a.out_stride[1] + c8) =
+      make_uint4(pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3]), pack2<T>(y[4], y[5]), pack2<T>(y[6], y[7]));
+  if (c8 == 0 && a.lse) a.lse[hq * a.lse_rows + prow] = bad ? NAN : sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
