@@ -708,6 +708,21 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         const bool pair = PAGED && it.pair;
         const int c0 = pair ? it.cnt(0) : it.n - it.lo, c1 = pair ? it.cnt(1) : 0;  // key tiles of the (two) streams
         if (c0 == 0) continue;
+        auto load_q = [&] {
+          if (q_turn > 0) ok = wait_item(b_qe, (uint32_t)(q_turn - 1) & 1u);
+          ++q_turn;
+          if (ok && lane == 0) {
+            const int two = (it.cnt(0) > 0) + (!pair && it.cnt(1) > 0);
+            bar_expect(b_q, (uint32_t)two * (uint32_t)(a.T * a.P * D * 2));
+#pragma unroll
+            for (int w = 0; w < 2; ++w)
+              if (it.cnt(w) > 0 && !(pair && w))
+                for (int x = 0; x < D / 64; ++x)
+                  tma_load(smb + SM::Q_OFF + w * SM::TILE_BYTES + x * SM::HALF, &mq, b_q, x * 64, it.q0 + it.r0 + w * a.T, it.h0, cs);
+            words[7] = (uint32_t)q_turn;
+          }
+        };
+        if (!PAGED) load_q();
         int k_tiles = it.before;
         int v_slot = 0;
         uint32_t v_phase = 0;
@@ -793,18 +808,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         // K, V of the last tile, K, V of the one before, ...; those of two streams in turn, in the order of their products.  (The
         // queries' place is free when the last item's last S is done: its first keys need not wait for that.)
         issue(0, false, it.n - 1);
-        if (q_turn > 0) ok = wait_item(b_qe, (uint32_t)(q_turn - 1) & 1u);
-        ++q_turn;
-        if (ok && lane == 0) {
-          const int two = (it.cnt(0) > 0) + (!pair && it.cnt(1) > 0);
-          bar_expect(b_q, (uint32_t)two * (uint32_t)(a.T * a.P * D * 2));
-#pragma unroll
-          for (int w = 0; w < 2; ++w)
-            if (it.cnt(w) > 0 && !(pair && w))
-              for (int x = 0; x < D / 64; ++x)
-                tma_load(smb + SM::Q_OFF + w * SM::TILE_BYTES + x * SM::HALF, &mq, b_q, x * 64, it.q0 + it.r0 + w * a.T, it.h0, cs);
-          words[7] = (uint32_t)q_turn;
-        }
+        if (PAGED) load_q();
         if (c1 > 0) issue(1, false, it.mid - 1);
         for (int i = 0; i < c0 && ok; ++i) {
           issue(0, true, it.n - 1 - i);
@@ -992,10 +996,26 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
     // Two threads to a row: 64 keys of every tile each.  The two warps that share rows meet at a barrier of their own, which
     // also gives both the same answer to whether a wait of either's has run out, so that both leave at the same point.
     const int w = wid >> 3, half = (wid >> 2) & 1, r = (wid & 3) * 32 + lane;
-    const int hl = r / a.T;  // head of this row; rows past P heads are not used
-    int tok = w * a.T + r - hl * a.T;  // token
     const uint32_t lane_base = (uint32_t)((wid & 3) * 32) << 16;
     const uint32_t ts = tmem + lane_base + w * 128, to = tmem + lane_base + 256 + w * 128 + half * (D / 2);
+    // What a row needs once for each item is made anew each time, from a thread index that the compiler cannot keep: the registers are
+    // the logits', and what waits for its turn in local memory comes from the L2 (shared memory leaves the L1 little).
+    struct Row {
+      int w, half, r, hl, row;  // tile, half of the keys and channels, row of the tile, head and token
+      bool mine;                // rows of nobody hold anything, and have no say below
+    };
+    auto row_of = [&](const PromptItem& it) {
+      uint32_t t;
+      asm volatile("mov.u32 %0, %%tid.x;" : "=r"(t));
+      Row x;
+      x.w = t >> 8;
+      x.half = (t >> 7) & 1;
+      x.r = t & 127;
+      x.hl = x.r / a.T;
+      x.row = it.r0 + (PAGED && it.pair ? 0 : x.w * a.T) + x.r - x.hl * a.T;
+      x.mine = x.row < it.nq && x.hl < a.P;
+      return x;
+    };
     float* xch = reinterpret_cast<float*>(sm + SM::BAR_OFF + SM::ROWS) + w * 2 * TILE + r;  // the two halves' values of a row
     auto meet = [&] {
       uint32_t both;
@@ -1004,17 +1024,31 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       ok = both != 0;
     };
     uint32_t s_phase = 0, o_phase = 0, quad_phase = 0;
+    // The four warps that share a pair's rows meet at a barrier with a bounded wait, which ends too when another tile's warps have given
+    // up; the two that share a tile then agree.
+    auto meet4 = [&] {
+      tm_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(b_quad + 8 * (wid & 3));
+      ok = ok && wait_item(b_quad + 8 * (wid & 3), quad_phase);
+      quad_phase ^= 1u;
+      tm_after();
+      meet();
+      return ok;
+    };
     while (true) {
       const PromptItem* item = next_item();
       meet();
       if (!ok || !item) break;
       const PromptItem& it = *item;
       const int cnt = it.cnt(w);
-      const bool twin = PAGED && it.pair;
-      if (PAGED) tok = (twin ? 0 : w * a.T) + r - hl * a.T;
-      // keys that this row still sees from the tile's (this half's) first on; grows by a tile each time
-      int left = (a.causal ? min(it.nk, it.r0 + tok + it.nk - it.nq + 1) : it.nk) - ((w ? it.nt1 : it.nt0) - 1) * TILE - half * (TILE / 2);
-      const bool mine = it.r0 + tok < it.nq && hl < a.P;  // rows of nobody hold anything, and have no say below
+      int left;  // keys that this row still sees from the tile's (this half's) first on; grows by a tile each time
+      bool mine;
+      {
+        const Row x = row_of(it);
+        left = (a.causal ? min(it.nk, x.row + it.nk - it.nq + 1) : it.nk) - ((w ? it.nt1 : it.nt0) - 1) * TILE - half * (TILE / 2);
+        mine = x.mine;
+      }
       float m = -INFINITY, l = 0.f;
       for (int i = cnt; i > 0; --i, left += TILE) {
         // S(j) stands for P V of the tile before too: a commit waits for everything its thread has issued before
@@ -1103,106 +1137,88 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
       xch[half * TILE] = l;
       meet();
       if (!ok) break;
+      l = xch[0] + xch[TILE];
+      float f0 = 1.f, f1 = 0.f;  // factors of the outputs
       if constexpr (PAGED) {
-        if (twin) {
-          // Both tiles' results of the same rows: four warps share them, a quarter of the channels each.  They meet at a barrier with a
-          // bounded wait, which ends too when another tile's warps have given up; the two that share a tile then agree.
-          auto meet4 = [&] {
-            tm_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(b_quad + 8 * (wid & 3));
-            ok = ok && wait_item(b_quad + 8 * (wid & 3), quad_phase);
-            quad_phase ^= 1u;
-            tm_after();
-            meet();
-          };
-          float* both = reinterpret_cast<float*>(sm + SM::BAR_OFF + SM::ROWS) + r;
-          l = xch[0] + xch[TILE];
-          meet4();
-          if (!ok) break;
+        if (it.pair) {
+          // both tiles' sums of the same rows: four warps share them, a quarter of the channels each
+          if (!(ok = meet4())) break;
           xch[half * TILE] = half ? l : m;
-          meet4();
-          if (!ok) break;
-          const float m0 = both[0], m1 = both[2 * TILE], top = fmaxf(m0, m1);
-          const float f0 = top == -INFINITY ? 0.f : ex2p(m0 - top), f1 = top == -INFINITY ? 0.f : ex2p(m1 - top);
+          if (!(ok = meet4())) break;
+          const float* both = xch - w * 2 * TILE;
+          const float m0 = both[0], m1 = both[2 * TILE];
+          m = fmaxf(m0, m1);
+          f0 = m == -INFINITY ? 0.f : ex2p(m0 - m);
+          f1 = m == -INFINITY ? 0.f : ex2p(m1 - m);
           l = both[TILE] * f0 + both[3 * TILE] * f1;
-          const int row = it.r0 + tok, hq = it.h0 + hl, c0 = (2 * w + half) * (D / 4);
-          const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : top + log2f(l);
-          const long long prow = it.q0 + row, slot = (long long)it.slot * a.slot_rows + r;
-          if (mine && w == 0 && half == 0) {
-            if (it.slot >= 0) a.part_lse[slot] = lse2;
-            else if (a.lse) a.lse[hq * a.lse_rows + prow] = lse2 * 0.6931471805599453f;
-          }
-          T* out = static_cast<T*>(a.out) + prow * a.out_stride[2] + hq * a.out_stride[1] + c0;
+        }
+      }
+      {
+        const Row x = row_of(it);
+        const bool pair = PAGED && it.pair, partial = PAGED ? it.slot >= 0 : a.splits > 1, none = l == 0.f;
+        const int hq = it.h0 + x.hl, c0 = pair ? (2 * x.w + x.half) * (D / 4) : x.half * (D / 2);
+        const long long prow = a.padded ? (long long)it.s * a.max_q + x.row : (long long)it.q0 + x.row;
+        const long long place = PAGED ? (long long)it.slot * a.slot_rows + (pair ? 0 : x.w * TILE) + x.r : ((long long)it.split * a.rows + prow) * a.Hq + hq;
+        const float lse2 = none ? -INFINITY : m + log2f(l), inv = none ? 0.f : 1.f / l;
+        if (x.mine && c0 == 0) {
+          if (partial)
+            a.part_lse[place] = lse2;
+          else if (a.lse)
+            a.lse[a.padded ? ((long long)it.s * a.Hq + hq) * a.max_q + x.row : hq * (PAGED ? a.lse_rows : a.total_q) + prow] = lse2 * 0.6931471805599453f;
+        }
+        f0 *= inv;
+        f1 *= inv;
+        const bool first = pair || cnt > 0, second = pair && it.cnt(1) > 0;  // tiles with products (warp-uniform)
+        const uint32_t from = words[4] + (uint32_t)((x.r & 96) << 16) + 256 + (pair ? 0 : x.w * 128) + c0;
+        // where 16 bytes of the row go, and from one such piece to the next
+        unsigned char* to_row;
+        long long step = 16;
+        if (!partial) {
+          to_row = reinterpret_cast<unsigned char*>(static_cast<T*>(a.out) + (a.padded ? it.s * a.out_stride[0] + x.row * a.out_stride[2] : prow * a.out_stride[2]) +
+                                                    hq * a.out_stride[1] + c0);
+        } else if (PAGED) {
+          to_row = reinterpret_cast<unsigned char*>(part_at<D>(a, it.slot, c0, (pair ? 0 : x.w * TILE) + x.r));
+          step = 16ll * a.slot_rows;
+        } else {
+          to_row = reinterpret_cast<unsigned char*>(a.part_o + place * D + c0);
+        }
 #pragma unroll 1
-          for (int c = 0; c < D / 4; c += 16) {
-            float o[16], o1[16];
-            tm_ld16(tmem + lane_base + 256 + c0 + c, o);
-            const bool two = it.cnt(1) > 0;
-            if (two) tm_ld16(tmem + lane_base + 384 + c0 + c, o1);
-            tm_wait_ld();
+        for (int c = 0; c < (pair ? D / 4 : D / 2); c += 16) {
+          float o[16];
+          if (first) {
+            tm_ld16(from + c, o);
+            if (PAGED && second) {
+              float o1[16];
+              tm_ld16(from + 128 + c, o1);
+              tm_wait_ld();
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              o[k] *= f0;
-              if (two) o[k] += o1[k] * f1;
-              o[k] = l == 0.f ? 0.f : o[k] * inv;
+              for (int k = 0; k < 16; ++k) o[k] = o[k] * f0 + o1[k] * f1;
+            } else {
+              tm_wait_ld();
+#pragma unroll
+              for (int k = 0; k < 16; ++k) o[k] *= f0;
             }
-            if (mine && it.slot >= 0) {
+          }
+          if (x.mine) {
 #pragma unroll
-              for (int k = 0; k < 16; k += 4)
-                *part_at<D>(a, it.slot, c0 + c + k, r) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-            } else if (mine) {
+            for (int k = 0; k < 16; ++k) o[k] = none ? 0.f : o[k];
+            if (partial) {
+#pragma unroll
+              for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4*>(to_row + (k >> 2) * step) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+              to_row += 4 * step;
+            } else {
 #pragma unroll
               for (int k = 0; k < 16; k += 8)
-                *reinterpret_cast<uint4*>(out + c + k) =
-                    make_uint4(pack2<T>(o[k], o[k + 1]), pack2<T>(o[k + 2], o[k + 3]), pack2<T>(o[k + 4], o[k + 5]), pack2<T>(o[k + 6], o[k + 7]));
+                *reinterpret_cast<uint4*>(to_row + 2 * k) = make_uint4(pack2<T>(o[k], o[k + 1]), pack2<T>(o[k + 2], o[k + 3]), pack2<T>(o[k + 4], o[k + 5]), pack2<T>(o[k + 6], o[k + 7]));
+              to_row += 32;
             }
-            __syncwarp();
           }
-          meet4();  // the next item's first products overwrite both
-          if (!ok) break;
-          continue;
+          __syncwarp();
+        }
+        if constexpr (PAGED) {
+          if (pair && !(ok = meet4())) break;  // the next item's first products overwrite both
         }
       }
-      l = xch[0] + xch[TILE];
-      const int row = it.r0 + tok, hq = it.h0 + hl;
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      const long long prow = a.padded ? (long long)it.s * a.max_q + row : (long long)it.q0 + row;
-      const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
-      const bool partial = PAGED ? it.slot >= 0 : a.splits > 1;
-      const long long place = PAGED ? (long long)it.slot * a.slot_rows + w * TILE + r : ((long long)it.split * a.rows + prow) * a.Hq + hq;
-      if (mine && half == 0) {
-        if (partial)
-          a.part_lse[place] = lse2;
-        else if (a.lse)
-          a.lse[a.padded ? ((long long)it.s * a.Hq + hq) * a.max_q + row : hq * (PAGED ? a.lse_rows : a.total_q) + prow] = lse2 * 0.6931471805599453f;
-      }
-      T* out = static_cast<T*>(a.out) + (a.padded ? it.s * a.out_stride[0] + row * a.out_stride[2] : prow * a.out_stride[2]) +
-               hq * a.out_stride[1] + half * (D / 2);
-      float* po = a.part_o + place * D + half * (D / 2);
-#pragma unroll 1
-      for (int c = 0; c < D / 2; c += 16) {
-        float o[16];
-        if (cnt > 0) {  // warp-uniform
-          tm_ld16(to + c, o);
-          tm_wait_ld();
-        }
-#pragma unroll
-        for (int k = 0; k < 16; ++k) o[k] = l == 0.f ? 0.f : o[k] * inv;
-        if (!mine) continue;
-        if (partial) {
-#pragma unroll
-          for (int k = 0; k < 16; k += 4)
-            *(PAGED ? part_at<D>(a, it.slot, half * (D / 2) + c + k, w * TILE + r) : reinterpret_cast<float4*>(po + c + k)) =
-                make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-        } else {
-#pragma unroll
-          for (int k = 0; k < 16; k += 8)
-            *reinterpret_cast<uint4*>(out + c + k) =
-                make_uint4(pack2<T>(o[k], o[k + 1]), pack2<T>(o[k + 2], o[k + 3]), pack2<T>(o[k + 4], o[k + 5]), pack2<T>(o[k + 6], o[k + 7]));
-        }
-      }
-      __syncwarp();
     }
   }
   tm_before();
