@@ -70,12 +70,12 @@ Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
       return l;
     }
   }
-  l.by_range = rows / (2 * l.T) * groups < 6 * sms && items * (KEY_COST * longest + ITEM_COST) < (1ll << 31);
+  l.by_range = rows / (2 * l.T) * groups < 6 * sms && items * (KEY_COST * longest + ITEM_COST_PAIR) < (1ll << 31);
   if (!l.by_range) {
     l.ctas = items <= (1ll << 28) ? (unsigned)items : 0u;
     return l;
   }
-  const long long most = items * (KEY_COST * longest + ITEM_COST) / RANGE_LEAST + 1;
+  const long long most = items * (KEY_COST * longest + ITEM_COST_PAIR) / RANGE_LEAST + 1;
   l.ctas = (unsigned)(most < sms ? most : sms);
   l.cuts = longest > TILE && l.ctas > 1;
   l.slot_rows = max_q <= l.T ? TILE : 2 * TILE;

@@ -366,11 +366,12 @@ template <bool PAGED> __device__ __forceinline__ PromptItem item_of(const Prompt
 // Paged calls with few items for the SMs: each CTA has an equal range of the call's work, whatever the lengths.
 //
 // The items stand in a row: sequence by sequence, heads in it, tiles of rows in these.  An item costs its visible keys (three
-// quarters for pairs, whose two tiles a step bandwidth bounds) and a constant; CTA c has what lies in [c, c + 1) * W of
+// quarters for pairs, whose two tiles a step bandwidth bounds) and a constant (8200 cycles of 3800 for a tile of keys; pairs,
+// which drain the copies, 16500 of 2000); CTA c has what lies in [c, c + 1) * W of
 // the sum.  An end inside an item is moved to a key tile: an item has the CTAs that have tiles of it, and where these are
 // several, each writes a partial result.  The ranges are a function of the lengths alone.
 // (The host sees to it that the sum fits 31 bits.)
-constexpr int ITEM_COST = 1024, KEY_COST = 4, KEY_COST_PAIR = 3, RANGE_LEAST = 1024;
+constexpr int ITEM_COST = 1024, KEY_COST = 4, ITEM_COST_PAIR = 3200, KEY_COST_PAIR = 3, RANGE_LEAST = 1024;
 
 // (What runs before the first copy runs once, from instructions that are fetched as they come: some 50 cycles for each, so its
 // divisions are worth replacing.)
@@ -394,8 +395,9 @@ struct PagedSeq {
     const uint32_t u = nk < nq ? min(full, (uint32_t)(nq - nk) / step) : 0u;
     return (full - u) * p + a.T * (full * (full + 1) - u * (u + 1)) + (t < tiles ? 0 : nk);
   }
-  __device__ __forceinline__ uint32_t cost(const PromptArgs& a, int t) const { return key_cost * keys(a, t) + ITEM_COST; }
-  __device__ __forceinline__ uint32_t cost_before(const PromptArgs& a, int t) const { return t > 0 ? key_cost * before(a, t) + t * ITEM_COST : 0u; }
+  __device__ __forceinline__ uint32_t item_cost() const { return key_cost == KEY_COST ? ITEM_COST : ITEM_COST_PAIR; }
+  __device__ __forceinline__ uint32_t cost(const PromptArgs& a, int t) const { return key_cost * keys(a, t) + item_cost(); }
+  __device__ __forceinline__ uint32_t cost_before(const PromptArgs& a, int t) const { return t > 0 ? key_cost * before(a, t) + t * item_cost() : 0u; }
 };
 
 __device__ __forceinline__ PagedSeq paged_seq(const PromptArgs& a, int q0, int nq, int nk) {
@@ -504,8 +506,8 @@ struct PagedRange {
       item_tiles(a, it);
       const int all = it->n;
       auto tiles_upto = [&](uint32_t x) {
-        if (x <= at + ITEM_COST) return 0;
-        x -= at + ITEM_COST;
+        if (x <= at + seq.item_cost()) return 0;
+        x -= at + seq.item_cost();
         return (int)(seq.key_cost == KEY_COST ? x / (KEY_COST * TILE) : x / (KEY_COST_PAIR * TILE));
       };
       const bool ends = end <= hi;
