@@ -12,7 +12,8 @@ constexpr int FEW_CLUSTER_KEYS = 1024;  // of a CTA
 
 struct Plan {
   int P, T;       // rows of a query tile: heads, tokens
-  int ranks;      // few_attn_kernel has the call, with clusters of as many CTAs, else 0
+  bool few;       // few_attn_kernel has the call
+  int ranks;      // with clusters of as many CTAs, else 0
   bool by_range;  // equal ranges, else whole items
   bool cuts;      // an item may be shared
   int slot_rows;
@@ -58,17 +59,25 @@ Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
   const long long rows = p->cu_q ? p->total_q : (p->total_q < c.n_seqs ? p->total_q : c.n_seqs);
   const long long groups = p->n_q_heads / l.P, items = prompt_tiles(false, c.n_seqs, max_q, rows, l.T) * groups;
   const int sms = prompt_sms(p->cache->device), group = p->n_q_heads / c.Hkv;
-  if (group * max_q <= FEW_ROWS) {
+  const long long units = c.n_seqs * (long long)c.Hkv, steps = (longest + FEW_KEYS - 1) / FEW_KEYS + FEW_ITEM_COST;
+  if (group * max_q <= FEW_ROWS && units * steps < (1ll << 30)) {
+    l.few = true;
+    l.P = group;
+    l.T = max_q > 0 ? (int)max_q : 1;
     // clusters as large as one wave holds, four steps of keys for each CTA at least
-    const long long room = (long long)sms * FEW_CTAS, units = c.n_seqs * (long long)c.Hkv;
+    const long long room = (long long)sms * FEW_CTAS;
     int ranks = 1;
     while (ranks < 16 && units * ranks * 2 <= room && ranks * 2 * FEW_WARPS * FEW_KEYS <= longest) ranks *= 2;
     if (longest <= (long long)ranks * FEW_CLUSTER_KEYS && units * longest <= room * FEW_CLUSTER_KEYS) {
       l.ranks = ranks;
-      l.P = group;
-      l.T = max_q > 0 ? (int)max_q : 1;
       return l;
     }
+    const long long most = units * steps / FEW_RANGE_LEAST + 1;
+    l.by_range = true;
+    l.ctas = (unsigned)(most < room ? most : room);
+    l.cuts = longest > FEW_KEYS && l.ctas > 1;
+    l.slot_rows = FEW_SLOT_ROWS;
+    return with_scratch(l, p, c);
   }
   l.by_range = rows / (2 * l.T) * groups < 6 * sms && items * (KEY_COST * longest + ITEM_COST_PAIR) < (1ll << 31);
   if (!l.by_range) {
@@ -113,13 +122,26 @@ const char* attn_check_pointers(const qevict_kv16_attn_args* p) {
   return nullptr;
 }
 
+template <class K> cudaError_t few_attributes(K kernel, int smem) {
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 45);  // FEW_CTAS fit; the rest is L1
+  return e;
+}
+
 template <class T, int D>
 cudaError_t launch_few(const PromptArgs& a, const Plan& l, const FewPages& g, int device, cudaStream_t s) {
-  auto kernel = few_attn_kernel<T, D>;
+  if (!l.ranks) {
+    auto kernel = few_attn_kernel<T, D, false>;
+    static std::atomic<uint64_t> done{0};
+    cudaError_t e = once_per_device(done, device, [&] { return few_attributes(kernel, few_smem(D)); });
+    if (e == cudaSuccess) e = launch_pdl(kernel, dim3(l.ctas), dim3(32 * FEW_WARPS), few_smem(D), s, a, g);
+    if (e == cudaSuccess && l.cuts) e = launch_pdl(paged_merge_kernel<T, D>, dim3(l.slot_rows / 32, l.ctas), dim3(D * 4), 0, s, a);
+    return e;
+  }
+  auto kernel = few_attn_kernel<T, D, true>;
   static std::atomic<uint64_t> done{0};
-  cudaError_t e = once_per_device(done, device, [&] {
-    cudaError_t e0 = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem(D));
-    if (e0 == cudaSuccess) e0 = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 45);  // FEW_CTAS fit; the rest is L1
+  const cudaError_t e = once_per_device(done, device, [&] {
+    const cudaError_t e0 = few_attributes(kernel, few_smem(D));
     return e0 != cudaSuccess ? e0 : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   });
   if (e != cudaSuccess) return e;
@@ -176,7 +198,7 @@ QEVICT_API qevict_status qevict_kv16_attn(const qevict_kv16_attn_args* p, void* 
   why = attn_check_pointers(p);
   if (why) return stateless_fail(QEVICT_ERR_INVALID_ARG, why);
   const Plan l = attn_plan(p, view);
-  if (l.ctas == 0 && !l.ranks) return stateless_fail(QEVICT_ERR_UNSUPPORTED, "more than 2^28 work items in one call");
+  if (l.ctas == 0 && !l.few) return stateless_fail(QEVICT_ERR_UNSUPPORTED, "more than 2^28 work items in one call");
   if (l.bytes > 0 && (!scratch || scratch_bytes < l.bytes))
     return stateless_fail(QEVICT_ERR_NO_MEMORY, "scratch too small: see qevict_kv16_attn_scratch_bytes");
   if (l.bytes > 0 && misaligned16(scratch)) return stateless_fail(QEVICT_ERR_INVALID_ARG, "scratch must be 16-byte aligned");
@@ -215,7 +237,7 @@ QEVICT_API qevict_status qevict_kv16_attn(const qevict_kv16_attn_args* p, void* 
   cudaError_t e = guard.err;
   if (e != cudaSuccess) return stateless_fail(QEVICT_ERR_CUDA, cudaGetErrorString(e));
   cudaStream_t s = (cudaStream_t)stream;
-  if (l.ranks) {
+  if (l.few) {
     FewPages g = {};
     for (int w = 0; w < 2; ++w) {
       g.pages[w] = view.pages[w];

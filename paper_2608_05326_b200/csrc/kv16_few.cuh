@@ -1,22 +1,25 @@
-// Attention of few new tokens over few cached ones (a step of decoding, drafts) in the 16-bit paged cache: calls for which latency
-// counts.
+// Attention of few new tokens (a step of decoding, drafts) over the 16-bit paged cache.
 //
 //     S = Q K^T,  P = 2^(S * scale * log2 e - m),  O += P V
 //
-// The rows are the tokens of all heads that share a KV head, at most 16 of them.  A cluster of up to 16 CTAs has a (sequence, KV
-// head); the four warps of a CTA take 16 of its keys in turn, straight from global memory into the registers that the
-// products want them in, the next ones on their way while these are in work.  The warps join their sums through shared memory, the
-// CTAs through each other's: one launch, and no scratch.
+// The rows are the tokens of all heads that share a KV head, at most 16 of them, so keys and values are read once and
+// bandwidth bounds it, or the latency of a short call.  The four warps of a CTA take 16 keys in turn, straight from global memory
+// into the registers that the products want them in, the next ones on their way while these are in work, and join their sums
+// through shared memory in the end.
 //   - mma.m16n8k16 contracts over channels in any order, so a lane takes 16 bytes of a key as the operands of two steps (elements
 //     0, 1 | 2, 3 and 4, 5 | 6, 7), and the queries are laid out to match.
 //   - A lane has 16 bytes of two neighbouring keys' values; byte permutes pair them, and the output's columns come in the order
 //     that this gives (channel 8 n + e is column n of step e).
 //   - Keys past the end and blocks that are not there are not read; their operands are zero and their logits masked.
-// Measured beside the kernel for tiles of rows (equal ranges, two launches), 32 / 8 heads of 128, one token for each of n sequences:
-// n = 1, 128 tokens 5.3 us (14.1), 2001 tokens 9.4 us (17.8), 8001: 18.4 us (22.9), 16001: 28.7 us (30.1), 32001: 57 us (44); n = 16,
-// 1001: 18.6 us (26.4), 2001: 33.8 us (40.7), 4001: 60.8 us (61.8).  It takes calls with up to FEW_CLUSTER_KEYS keys for each
-// CTA of one wave; beyond, its loads reach 5.2 TB/s where copies of whole pages reach 6.3.  Loads on their way have their place in the L1, so shared memory is kept
-// small (64 sequences of 2049 tokens: 145 us with all of it, 105 us with 45 %).
+// How the keys are shared: a call with up to FEW_CLUSTER_KEYS keys for each CTA of one wave gives a (sequence, KV head) a cluster of
+// up to 16 CTAs, which join their sums through each other's shared memory (one launch, no scratch); any other gives each CTA an equal
+// range of its work (FewRange) and joins what ranges share in a second launch.
+// Measured (32 / 8 heads of 128, one token for each of n sequences, graph replays; beside it the kernel for tiles of rows, which takes
+// 16 rows as 128): n = 1, 128 tokens 5.3 us (14.1), 2048 tokens 9.2 us (17.8), 8000: 18.4 us (22.9); n = 16, 2000: 33.8 us (40.7).  Ranges,
+// call after call: n = 64, 2048 tokens 105 us (124), 8 x 65536 tokens of 28 / 4 heads 200 us (5.4 TB/s; 230): short runs take 190 us
+// either way, but here the power limit leaves 1.75 GHz where tensor memory products of 128 rows leave 1.57.
+// Loads on their way have their place in the L1, so shared memory is kept small: with all of it 8 x 65536 tokens took 270 us; through a
+// ring in shared memory (cp.async) 231 us.
 #pragma once
 
 #include "prompt_attn.cuh"
@@ -26,7 +29,8 @@ namespace qevict {
 namespace {
 
 constexpr int FEW_WARPS = 4, FEW_KEYS = 16;
-constexpr int FEW_ROWS = 16, FEW_CTAS = 3;  // of an SM: 168 registers a thread
+constexpr int FEW_ITEM_COST = 5, FEW_RANGE_LEAST = 8;  // steps of 16 keys
+constexpr int FEW_ROWS = 16, FEW_SLOT_ROWS = 32, FEW_CTAS = 3;  // of an SM: 168 registers a thread
 constexpr int few_smem(int D) { return (FEW_WARPS * 72 + D) * FEW_ROWS * 4 + D / 32 * 1024 + (FEW_WARPS + 1) * FEW_ROWS * 8; }
 
 __device__ __forceinline__ uint4 ld_page16(const void* p) {
@@ -59,8 +63,96 @@ struct FewPages {
   long long q_stride[2];  // token, head
 };
 
-// blockIdx is (KV head * ranks + rank, sequence)
-template <class T, int D>
+// A CTA's equal range of the work: the sequences' KV heads stand in a row, each of its steps and FEW_ITEM_COST more.  An end inside a
+// KV head's constant is moved to its first step.  (The host sees to it that the sum fits 31 bits.)
+struct FewRange {
+  uint32_t width, lo, hi, at;  // this CTA's part of the sum; start of the current item
+  int s, h, q0, nq, nk;
+  int lane_q0, lane_nq, lane_nk, first;  // the lane's sequence of 32, of which `first` is the first
+
+  static __device__ __forceinline__ uint32_t cost(int nq, int nk) { return nq > 0 ? (nk + FEW_KEYS - 1) / FEW_KEYS + FEW_ITEM_COST : 0; }
+  __device__ __forceinline__ uint32_t look(const PromptArgs& a, int s0, int lane) {  // work of the lane's sequence
+    int k0;
+    lane_q0 = lane_nq = lane_nk = 0;
+    first = s0;
+    if (s0 + lane < a.n_seqs) {
+      q_span<true>(a, s0 + lane, &lane_q0, &lane_nq);
+      k_span<true>(a, s0 + lane, &k0, &lane_nk);
+    }
+    return cost(lane_nq, lane_nk) * a.Hkv;
+  }
+  __device__ __forceinline__ void sequence(const PromptArgs& a, int lane) {
+    if (s >= first + 32) look(a, s & ~31, lane);
+    q0 = __shfl_sync(0xffffffffu, lane_q0, s & 31);
+    nq = __shfl_sync(0xffffffffu, lane_nq, s & 31);
+    nk = __shfl_sync(0xffffffffu, lane_nk, s & 31);
+  }
+  __device__ __forceinline__ FewRange(const PromptArgs& a, int lane) {
+    uint32_t sum = 0, mine = 0;
+    for (int i = 0; i < a.n_seqs; i += 32) {
+      mine = look(a, i, lane);
+      sum += __reduce_add_sync(0xffffffffu, mine);
+    }
+    width = (sum + gridDim.x - 1) / gridDim.x;
+    if (width < FEW_RANGE_LEAST) width = FEW_RANGE_LEAST;
+    lo = blockIdx.x * width;
+    hi = min(lo + width, sum);
+    s = a.n_seqs;
+    if (lo >= sum) return;
+    uint32_t front = 0;  // work of the sequences before
+#pragma unroll 1
+    for (int i = 0; i < a.n_seqs; i += 32) {
+      if (a.n_seqs > 32) mine = look(a, i, lane);
+      uint32_t upto = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, front + upto > lo);
+      if (past) {
+        const int who = __ffs(past) - 1;
+        s = i + who;
+        front += __shfl_sync(0xffffffffu, upto - mine, who);
+        break;
+      }
+      front += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    sequence(a, lane);
+    h = small_quotient(lo - front, cost(nq, nk));
+    at = front + h * cost(nq, nk);
+  }
+  // The next item, its steps in the range; false behind the last one.
+  __device__ __forceinline__ bool next(const PromptArgs& a, int lane, bool writes, PromptItem* it) {
+#pragma unroll 1
+    while (s < a.n_seqs && at < hi) {
+      const uint32_t end = at + cost(nq, nk);
+      const int all = (nk + FEW_KEYS - 1) / FEW_KEYS;
+      auto steps_upto = [&](uint32_t x) { return x <= at + FEW_ITEM_COST ? 0 : (int)(x - at - FEW_ITEM_COST); };
+      const bool ends = end <= hi;
+      it->s = s; it->h0 = h * a.P; it->q0 = q0; it->nq = nq; it->nk = nk;
+      it->lo = lo > at ? steps_upto(lo) : 0;
+      it->n = ends ? all : steps_upto(hi);
+      it->slot = it->lo == 0 && ends ? -1 : 2 * (int)blockIdx.x + (it->lo == 0);
+      if (it->lo == 0 && it->n > 0 && !ends && writes) {
+        const PagedCut c = {1, s, it->h0, 0, q0, nq, (int)small_quotient(end - 1, width), 0};
+        a.cuts[blockIdx.x] = c;
+      }
+      at = end;
+      if (++h == a.Hkv) {
+        h = 0;
+        do {
+          if (++s < a.n_seqs) sequence(a, lane);
+        } while (s < a.n_seqs && nq == 0);
+      }
+      if (it->n > it->lo || (all == 0 && ends)) return true;
+    }
+    return false;
+  }
+};
+
+// CLUSTER: blockIdx is (KV head * ranks + rank, sequence)
+template <class T, int D, bool CLUSTER>
 __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ FewPages g) {
   constexpr int J = D / 32;       // 16-byte pieces of a key in a lane
   constexpr int H = D / 64;       // of a value
@@ -73,6 +165,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(cons
   auto ms = reinterpret_cast<float (*)[FEW_ROWS]>(qf + 2 * J), ls = ms + FEW_WARPS + 1;  // references and sums: the warps', the CTA's
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = lane >> 2, c = lane & 3;
   pdl_prologue();
+  if (!CLUSTER && a.cuts && tid == 0) a.cuts[blockIdx.x].valid = 0;
 
   // keys f0 * 16 .. f1 * 16 - 1 for the rows of one KV head
   auto attend = [&](const PromptItem& it, int f0, int f1, auto take) {
@@ -260,11 +353,27 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(cons
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = sum == 0.f ? 0.f : y[i] * inv;
     const long long prow = it.q0 + tok;
+    if (!CLUSTER && it.slot >= 0) {
+      *part_at<D>(a, it.slot, n * 8, r) = make_float4(y[0], y[1], y[2], y[3]);
+      *part_at<D>(a, it.slot, n * 8 + 4, r) = make_float4(y[4], y[5], y[6], y[7]);
+      if (n == 0) a.part_lse[(long long)it.slot * a.slot_rows + r] = lse2;
+      return;
+    }
     *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + prow * a.out_stride[2] + hq * a.out_stride[1] + n * 8) =
         make_uint4(pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3]), pack2<T>(y[4], y[5]), pack2<T>(y[6], y[7]));
     if (n == 0 && a.lse) a.lse[hq * a.lse_rows + prow] = lse2 * 0.6931471805599453f;
   };
 
+  if constexpr (!CLUSTER) {
+    if (blockIdx.x == 0 && a.status)
+      for (int s = tid; s < a.n_seqs; s += 32 * FEW_WARPS)
+        if (seq_cut<true>(a, s)) kv8_record(a.status, CHECK_LENGTH);
+    FewRange range(a, lane);
+    PromptItem it;
+    while (range.next(a, lane, tid == 0, &it))
+      attend(it, it.lo, it.n, [&](int r, int n, float top, float sum, float (&y)[8]) { result(it, r, n, top, sum, y); });
+    return;
+  }
   uint32_t rank, ranks;
   asm("mov.u32 %0, %%cluster_ctarank;\nmov.u32 %1, %%cluster_nctarank;" : "=r"(rank), "=r"(ranks));
   PromptItem it;
