@@ -135,7 +135,7 @@ cudaError_t launch_few(const PromptArgs& a, const Plan& l, const FewPages& g, in
     static std::atomic<uint64_t> done{0};
     cudaError_t e = once_per_device(done, device, [&] { return few_attributes(kernel, few_smem(D)); });
     if (e == cudaSuccess) e = launch_pdl(kernel, dim3(l.ctas), dim3(32 * FEW_WARPS), few_smem(D), s, a, g);
-    if (e == cudaSuccess && l.cuts) e = launch_pdl(paged_merge_kernel<T, D>, dim3(l.slot_rows / 32, l.ctas), dim3(D * 4), 0, s, a);
+    if (e == cudaSuccess && l.cuts) e = launch_pdl(paged_merge_kernel<T, D>, dim3(l.slot_rows / 32, l.ctas, D / 64), dim3(32 * MERGE_WARPS), 0, s, a);
     return e;
   }
   auto kernel = few_attn_kernel<T, D, true>;
@@ -167,7 +167,7 @@ cudaError_t launch_paged(const PromptArgs& a, const Plan& l, const CUtensorMap& 
   static std::atomic<uint64_t> done{0};
   cudaError_t e = once_per_device(done, device, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptSmem<D>::BYTES); });
   if (e == cudaSuccess) e = launch_pdl(kernel, dim3(l.ctas), dim3(PROMPT_THREADS), PromptSmem<D>::BYTES, s, a, mq, mk, mv);
-  if (e == cudaSuccess && l.cuts) e = launch_pdl(paged_merge_kernel<T, D>, dim3(l.slot_rows / 32, l.ctas), dim3(D * 4), 0, s, a);
+  if (e == cudaSuccess && l.cuts) e = launch_pdl(paged_merge_kernel<T, D>, dim3(l.slot_rows / 32, l.ctas, D / 64), dim3(32 * MERGE_WARPS), 0, s, a);
   return e;
 }
 

@@ -1321,40 +1321,58 @@ __global__ void __launch_bounds__(256) prompt_merge_kernel(const PromptArgs a) {
         L == 0.f ? -INFINITY : (Ms + log2f(L)) * 0.6931471805599453f;
 }
 
-// Paged: joins the partial results of the items that ranges share: blockIdx.y is the CTA in whose range such an item starts, a
-// lane per row of 32, a warp per eight channels.
+// Paged: joins the partial results of the items that ranges share: blockIdx.y is the CTA in whose range such an item starts, a lane
+// per row of 32, a warp per four channels of 64.  The warps look for the largest reference together, and many parts' rows are
+// requested at a time (one long sequence may have 60 parts: one after the other they took 13 us).
+constexpr int MERGE_WARPS = 16;
 template <class T, int D>
-__global__ void __launch_bounds__(D * 4) paged_merge_kernel(const PromptArgs a) {
-  const int i = blockIdx.x * 32 + (threadIdx.x & 31), c8 = (threadIdx.x >> 5) * 8, cta = blockIdx.y;
+__global__ void __launch_bounds__(32 * MERGE_WARPS) paged_merge_kernel(const PromptArgs a) {
+  __shared__ float red[MERGE_WARPS][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane, c4 = blockIdx.z * 64 + warp * 4, cta = blockIdx.y;
   pdl_prologue();
   const PagedCut c = a.cuts[cta];
+  if (!c.valid) return;  // the whole CTA leaves
   const int w = i / TILE, r = i - w * TILE, hl = r / a.T, tok = w * a.T + r - hl * a.T;
-  if (!c.valid || hl >= a.P || c.r0 + tok >= c.nq || (c.pair && w)) return;
+  const bool mine = hl < a.P && c.r0 + tok < c.nq && !(c.pair && w);
   const int parts = c.last - cta + 1;
   // part 0 ends its CTA's range, the others begin theirs
   auto slot = [&](int p) { return 2 * (cta + p) + (p == 0); };
-  float top = -INFINITY, sum = 0.f, y[8] = {};
-  bool bad = false;
-#pragma unroll 4
-  for (int p = 0; p < parts; ++p) {
-    const float x = a.part_lse[(long long)slot(p) * a.slot_rows + i];
-    const float4 v0 = *part_at<D>(a, slot(p), c8, i), v1 = *part_at<D>(a, slot(p), c8 + 4, i);
-    bad = bad || x != x;  // the part was given up
-    const float t = fmaxf(top, x), f0 = t == -INFINITY ? 0.f : ex2p(top - t), f1 = t == -INFINITY ? 0.f : ex2p(x - t);
-    const float v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
-    sum = sum * f0 + f1;
+  auto lse_of = [&](int p) { return a.part_lse[(long long)slot(p) * a.slot_rows + i]; };
+  float top = -INFINITY;
+  if (mine)
+    for (int p = warp; p < parts; p += MERGE_WARPS) {
+      const float x = lse_of(p);
+      top = x != x || top != top ? NAN : fmaxf(top, x);  // not a number: the part was given up
+    }
+  red[warp][lane] = top;
+  __syncthreads();
+  if (!mine) return;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) y[k] = y[k] * f0 + f1 * v[k];
-    top = t;
+  for (int k = 0; k < MERGE_WARPS; ++k) {
+    const float x = red[k][lane];
+    top = x != x || top != top ? NAN : fmaxf(top, x);
   }
-  const float inv = bad ? NAN : sum == 0.f ? 0.f : 1.f / sum;
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f, y[4] = {};
+#pragma unroll 8
+  for (int p = 0; p < parts; ++p) {
+    const float f = ex2p(lse_of(p) - ref);
+    const float4 v = *part_at<D>(a, slot(p), c4, i);
+    sum += f;
+    y[0] += f * v.x;
+    y[1] += f * v.y;
+    y[2] += f * v.z;
+    y[3] += f * v.w;
+  }
+  const bool none = sum == 0.f;
+  const float inv = none ? 0.f : 1.f / sum;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) y[k] = sum == 0.f && !bad ? 0.f : y[k] * inv;
+  for (int k = 0; k < 4; ++k) y[k] = none ? 0.f : y[k] * inv;
   const long long prow = (long long)c.q0 + c.r0 + tok;
   const int hq = c.h0 + hl;
-  *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + prow * a.out_stride[2] + hq * a.out_stride[1] + c8) =
-      make_uint4(pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3]), pack2<T>(y[4], y[5]), pack2<T>(y[6], y[7]));
-  if (c8 == 0 && a.lse) a.lse[hq * a.lse_rows + prow] = bad ? NAN : sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+  *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + prow * a.out_stride[2] + hq * a.out_stride[1] + c4) =
+      make_uint2(pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3]));
+  if (c4 == 0 && a.lse) a.lse[hq * a.lse_rows + prow] = none ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
 }
 
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
