@@ -587,8 +587,8 @@ typedef struct {
  * token start[s] + i of the cache.  cu_new: device int32 [n_seqs + 1], ascending, or NULL for one token per sequence (row
  * s).  With a rotation the keys are stored rotated and, where q is given, q_out gets the rotated queries (q_out may be q);
  * positions: device [n_axes][total_new], or NULL for the tokens' places in their sequences on every axis.  Without a rotation
- * rows are stored (and queries copied) as they are.  Tokens past the table are dropped, a sequence whose rows do not lie
- * in 0 .. total_new - 1 is left as it is; both set *status, as bounds that fall do.  A sequence with start < 0 is left as it is.
+ * rows are stored (and queries copied) as they are.  Tokens past the table are dropped (their queries are rotated all the same), a
+ * sequence whose rows do not lie in 0 .. total_new - 1 is left as it is; both set *status, as bounds that fall do.  A sequence with start < 0 is left as it is.
  * Rows of no sequence are not read into a result, and their rows of q_out are not written.  No two tokens of a call may share
  * a place. */
 typedef struct {
@@ -617,11 +617,13 @@ QEVICT_API qevict_status qevict_kv16_append(const qevict_kv16_append_args* args,
  * over the tokens j that are there and, with `causal`, j <= i + lens[s] - n_q[s] (the queries are the last n_q of lens tokens).
  * A query that sees no token gets out = 0 and lse = -infinity.  q, out: [total_q] rows of n_q_heads heads (strides token, head),
  * sequence s has rows cu_q[s] .. cu_q[s + 1] - 1 (device int32, ascending), or row s without cu_q; rows of no sequence are
- * not written.  lse [n_q_heads, total_q].  max_q and max_len bound the lengths and size the launch; a sequence with more
+ * not written.  out may be q (same strides).  lse [n_q_heads, total_q].  max_q and max_len bound the lengths and size the launch; a sequence with more
  * new tokens is cut to the first max_q, one with lens beyond max_len or the table to the smaller of them, rows outside 0 ..
  * total_q - 1 are left out, bounds that fall are empty, and each sets *status, as a length < 0 does.  A key or value that is not
  * finite spreads to every row of its sequence from 255 tokens before it on.  scratch: device, from
- * qevict_kv16_attn_scratch_bytes for the same arguments; calls that may run at the same time need scratch of their own. */
+ * qevict_kv16_attn_scratch_bytes for the same arguments; calls that may run at the same time need scratch of their own.  How the
+ * keys are shared among thread blocks, and with it the order of the float32 sums, follows from all lengths of the call; the same
+ * call gives the same bits.  The rows of a call that gave up (*status) are not-a-number where they have no result. */
 typedef struct {
   uint32_t struct_size;      /* sizeof(qevict_kv16_attn_args) */
   int32_t n_q_heads;         /* multiple of n_kv_heads */

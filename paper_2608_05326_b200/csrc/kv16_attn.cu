@@ -1,7 +1,8 @@
 // Attention of new tokens over the 16-bit paged cache: checks of the arguments, plan, launch.
 //
-// The kernel is the prompt attention's (prompt_attn.cuh) with keys and values by page: a tile of 128 keys is 1 to 8
-// pages, each copied by TMA from where the table says, page after page into the rows that they have in the tile.
+// Up to 16 rows for a KV head (a token or a draft for the heads that share it): kv16_few.cuh.  More: the prompt attention's kernel
+// (prompt_attn.cuh) with keys and values by page: a tile of 128 keys is 1 to 8 pages, each copied by TMA from where the
+// table says, page after page into the rows that they have in the tile.
 #include "kv16_few.cuh"
 
 namespace qevict {
@@ -119,6 +120,8 @@ const char* attn_check_pointers(const qevict_kv16_attn_args* p) {
   if (bad_stride(p->q_stride[0], p->total_q) || bad_stride(p->q_stride[1], p->n_q_heads) || bad_stride(p->out_stride[0], p->total_q) ||
       bad_stride(p->out_stride[1], p->n_q_heads))
     return "strides must be positive multiples of 16 bytes";
+  if (p->q == p->out && ((p->total_q > 1 && p->q_stride[0] != p->out_stride[0]) || (p->n_q_heads > 1 && p->q_stride[1] != p->out_stride[1])))
+    return "an output in its input's place must have its strides";
   return nullptr;
 }
 

@@ -343,6 +343,7 @@ def test_attention_refuses_unusable_views(over, status, word):
     (dict(softmax_scale=float("nan")), 1, "softmax_scale"), (dict(softmax_scale=3e38), 1, "softmax_scale"), (dict(max_q=2), 1, "without cu_q"), (dict(total_q=1), 1, "without cu_q"),
     (dict(n_q_heads=2048), 4, "heads"), (dict(total_q=2 ** 31), 4, "tokens"), (dict(q=None), 1, "NULL"), (dict(out=None), 1, "NULL"), (dict(lens=None), 1, "NULL"),
     (dict(q=4104), 1, "aligned"), (dict(lse=4098), 1, "aligned"), (dict(cu_q=4098), 1, "aligned"), (dict(q_stride=(250, 64)), 1, "strides"), (dict(out_stride=(256, 0)), 1, "strides"),
+    (dict(out=4096, out_stride=(512, 64)), 1, "its strides"),
 ])
 def test_attention_refuses_unusable_arguments(over, status, word):
     view = _view()
