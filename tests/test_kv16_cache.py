@@ -716,13 +716,16 @@ def test_the_output_may_take_the_place_of_the_queries(nq, lens):
 
 @pytest.mark.gpu
 def test_many_work_items_are_handed_out_whole():
-    # more than six items for each SM: 64 heads of their own KV head
-    nq, lens, hq, d, dtype = [4100], [4500], 64, 64, torch.float16
+    # more than six items for each SM: 64 heads of their own KV head; sequences with one tile of rows among them
+    nq, lens, hq, d, dtype = [4100, 1, 3, 128], [4500, 3000, 100, 700], 64, 64, torch.float16
     cache, pools, table, _, q = _case(nq, lens, hq, hq, d, 128, dtype, 74)
     out, lse = cache.attn(q, _i32(lens), _cu(nq), return_lse=True)
-    rows = [torch.cat([x[int(p)] for p in table[0]], dim=1)[:, :lens[0]].transpose(0, 1) for x in pools]
-    for h in (0, 17, 63):
-        _check_seq(out[:, h:h + 1], lse[h:h + 1], q[:, h:h + 1], _np(rows[0][:, h:h + 1]), _np(rows[1][:, h:h + 1]), lens[0], None, True, dtype, h)
+    at = 0
+    for s, (m, n) in enumerate(zip(nq, lens)):
+        rows = [torch.cat([x[int(p)] for p in table[s, :-(-n // 128)]], dim=1)[:, :n].transpose(0, 1) for x in pools]
+        for h in (0, 17, 63):
+            _check_seq(out[at:at + m, h:h + 1], lse[h:h + 1, at:at + m], q[at:at + m, h:h + 1], _np(rows[0][:, h:h + 1]), _np(rows[1][:, h:h + 1]), n, None, True, dtype, (s, h))
+        at += m
 
 
 # ---- the operators together ------------------------------------------------------------------------------------
