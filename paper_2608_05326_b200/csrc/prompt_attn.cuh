@@ -376,7 +376,8 @@ template <bool PAGED> __device__ __forceinline__ PromptItem item_of(const Prompt
 //
 // The items stand in a row: sequence by sequence, heads in it, tiles of rows in these.  An item costs its visible keys (three
 // quarters for pairs, whose two tiles a step bandwidth bounds) and a constant (8200 cycles of 3800 for a tile of keys; pairs,
-// which drain the copies, 16500 of 2000); CTA c has what lies in [c, c + 1) * W of
+// which drain the copies, 16500 of 2000).  (A piece of 2048 tokens between 31 single ones 668 us; pairs' keys at three sevenths 785 us,
+// at seven and eleven eighths 688 and 727 us.)  CTA c has what lies in [c, c + 1) * W of
 // the sum.  An end inside an item is moved to a key tile: an item has the CTAs that have tiles of it, and where these are
 // several, each writes a partial result.  The ranges are a function of the lengths alone.
 // (The host sees to it that the sum fits 31 bits.)
