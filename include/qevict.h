@@ -619,7 +619,8 @@ QEVICT_API qevict_status qevict_kv16_append(const qevict_kv16_append_args* args,
  * sequence s has rows cu_q[s] .. cu_q[s + 1] - 1 (device int32, ascending), or row s without cu_q; rows of no sequence are
  * not written.  out may be q (same strides).  lse [n_q_heads, total_q].  max_q and max_len bound the lengths and size the launch; a sequence with more
  * new tokens is cut to the first max_q, one with lens beyond max_len or the table to the smaller of them, rows outside 0 ..
- * total_q - 1 are left out, bounds that fall are empty, and each sets *status, as a length < 0 does.  A key or value that is not
+ * total_q - 1 are left out, bounds that fall are empty, and each sets *status, as a length < 0 does (rows that such bounds give to
+ * several sequences get the result of any of them, or none).  A key or value that is not
  * finite spreads to every row of its sequence from 255 tokens before it on.  scratch: device, from
  * qevict_kv16_attn_scratch_bytes for the same arguments; calls that may run at the same time need scratch of their own.  How the
  * keys are shared among thread blocks, and with it the order of the float32 sums, follows from all lengths of the call; the same

@@ -80,7 +80,7 @@ Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
     l.slot_rows = FEW_SLOT_ROWS;
     return with_scratch(l, p, c);
   }
-  l.by_range = rows / (2 * l.T) * groups < 6 * sms && items * (KEY_COST * longest + ITEM_COST_PAIR) < (1ll << 31);
+  l.by_range = rows / (2 * l.T) * groups < 6 * sms;
   if (!l.by_range) {
     l.ctas = items <= (1ll << 28) ? (unsigned)items : 0u;
     return l;

@@ -379,14 +379,15 @@ template <bool PAGED> __device__ __forceinline__ PromptItem item_of(const Prompt
 // which drain the copies, 16500 of 2000).  (A piece of 2048 tokens between 31 single ones 668 us; pairs' keys at three sevenths 785 us,
 // at seven and eleven eighths 688 and 727 us.)  CTA c has what lies in [c, c + 1) * W of
 // the sum.  An end inside an item is moved to a key tile: an item has the CTAs that have tiles of it, and where these are
-// several, each writes a partial result.  The ranges are a function of the lengths alone.
-// (The host sees to it that the sum fits 31 bits.)
+// several, each writes a partial result.  The ranges are a function of the lengths alone.  The sum is held in 64 bits: bounds that
+// fall and rise give many sequences the same rows, so no bound on the rows keeps it within 32 (an item that crossed the end of a
+// sum that had wrapped named a CTA behind the last, whose results the join then read behind the scratch).
 constexpr int ITEM_COST = 1024, KEY_COST = 4, ITEM_COST_PAIR = 3200, KEY_COST_PAIR = 3, RANGE_LEAST = 1024;
 
 // (What runs before the first copy runs once, from instructions that are fetched as they come: some 50 cycles for each, so its
 // divisions are worth replacing.)
 // x / y where that is below 2^20: the float quotient is off by less than one
-__device__ __forceinline__ uint32_t small_quotient(uint32_t x, uint32_t y) {
+template <class U> __device__ __forceinline__ uint32_t small_quotient(U x, U y) {
   uint32_t q = (uint32_t)__fdividef((float)x, (float)y);
   if (q * y > x) --q;
   if (x - q * y >= y) ++q;
@@ -398,16 +399,15 @@ struct PagedSeq {
   __device__ __forceinline__ int keys(const PromptArgs& a, int t) const {
     return !a.causal || t == tiles - 1 ? nk : max(0, nk - nq + (t + 1) * 2 * a.T);
   }
-  __device__ __forceinline__ uint32_t before(const PromptArgs& a, int t) const {
-    if (!a.causal) return (uint32_t)t * nk;
-    // full tiles of rows, of which the first u see nothing (modulo 2^32, in which the sum fits)
-    const uint32_t step = 2 * a.T, p = nk - nq, full = t < tiles ? t : tiles - 1;
-    const uint32_t u = nk < nq ? min(full, (uint32_t)(nq - nk) / step) : 0u;
-    return (full - u) * p + a.T * (full * (full + 1) - u * (u + 1)) + (t < tiles ? 0 : nk);
+  __device__ __forceinline__ long long before(const PromptArgs& a, int t) const {
+    if (!a.causal) return (long long)t * nk;
+    // full tiles of rows, of which the first u see nothing (fewer than 2^10 in a call of ranges)
+    const int step = 2 * a.T, full = t < tiles ? t : tiles - 1, u = nk < nq ? min(full, (nq - nk) / step) : 0;
+    return (long long)(full - u) * (nk - nq) + a.T * (full * (full + 1) - u * (u + 1)) + (t < tiles ? 0 : nk);
   }
   __device__ __forceinline__ uint32_t item_cost() const { return key_cost == KEY_COST ? ITEM_COST : ITEM_COST_PAIR; }
-  __device__ __forceinline__ uint32_t cost(const PromptArgs& a, int t) const { return key_cost * keys(a, t) + item_cost(); }
-  __device__ __forceinline__ uint32_t cost_before(const PromptArgs& a, int t) const { return t > 0 ? key_cost * before(a, t) + t * item_cost() : 0u; }
+  __device__ __forceinline__ uint64_t cost(const PromptArgs& a, int t) const { return (uint64_t)key_cost * (uint32_t)keys(a, t) + item_cost(); }
+  __device__ __forceinline__ uint64_t cost_before(const PromptArgs& a, int t) const { return t > 0 ? key_cost * (uint64_t)before(a, t) + t * item_cost() : 0ull; }
 };
 
 __device__ __forceinline__ PagedSeq paged_seq(const PromptArgs& a, int q0, int nq, int nk) {
@@ -416,7 +416,7 @@ __device__ __forceinline__ PagedSeq paged_seq(const PromptArgs& a, int q0, int n
 }
 
 struct PagedRange {
-  uint32_t width, lo, hi, at;  // this CTA's part of the sum; start of the current item
+  uint64_t width, lo, hi, at;  // this CTA's part of the sum; start of the current item
   int s, h, t;
   bool begun;  // the current item has been given
   PagedSeq seq;
@@ -440,31 +440,32 @@ struct PagedRange {
 
   __device__ __forceinline__ PagedRange(const PromptArgs& a, int lane) {
     const int groups = a.groups;
-    uint32_t sum = 0, mine = 0;
+    uint64_t sum = 0, mine = 0;
 #pragma unroll 1
     for (int i = 0; i < a.n_seqs; i += 32) {
       const PagedSeq q = look(a, i, lane);
       mine = q.cost_before(a, q.tiles) * groups;
-      sum += __reduce_add_sync(0xffffffffu, mine);
+      // (a sequence's work is below 2^44: in a call of ranges fewer than 2^11 items of 2^33 at most)
+      sum += __reduce_add_sync(0xffffffffu, (uint32_t)mine & 0xffffffu) + ((uint64_t)__reduce_add_sync(0xffffffffu, (uint32_t)(mine >> 24)) << 24);
     }
-    width = (sum + gridDim.x - 1) / gridDim.x;
+    width = sum >> 31 ? (sum + gridDim.x - 1) / gridDim.x : ((uint32_t)sum + gridDim.x - 1) / gridDim.x;
     begun = false;
     if (width < RANGE_LEAST) width = RANGE_LEAST;
     lo = blockIdx.x * width;
     hi = min(lo + width, sum);
     s = a.n_seqs;
     if (lo >= sum) return;
-    uint32_t front = 0;  // cost of the sequences before
+    uint64_t front = 0;  // cost of the sequences before
 #pragma unroll 1
     for (int i = 0; i < a.n_seqs; i += 32) {
       if (a.n_seqs > 32) {
         const PagedSeq q = look(a, i, lane);
         mine = q.cost_before(a, q.tiles) * groups;
       }
-      uint32_t upto = mine;
+      uint64_t upto = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+        const uint64_t x = __shfl_up_sync(0xffffffffu, upto, o);
         if (lane >= o) upto += x;
       }
       const uint32_t past = __ballot_sync(0xffffffffu, front + upto > lo);
@@ -477,7 +478,7 @@ struct PagedRange {
       front += __shfl_sync(0xffffffffu, upto, 31);
     }
     seq = sequence(a, s, lane);
-    const uint32_t head = seq.cost_before(a, seq.tiles);
+    const uint64_t head = seq.cost_before(a, seq.tiles);
     h = small_quotient(lo - front, head);
     front += h * head;
     int t0 = 0, t1 = seq.tiles - 1;  // the last tile that starts at or before lo
@@ -508,17 +509,17 @@ struct PagedRange {
       }
       begun = true;
       if (s >= a.n_seqs || at >= hi) return false;
-      const uint32_t end = at + seq.cost(a, t);
+      const uint64_t end = at + seq.cost(a, t);
       it->valid = 1;
       it->s = s; it->h0 = h * a.P; it->r0 = t * 2 * a.T;
       it->q0 = seq.q0; it->nq = seq.nq; it->k0 = 0; it->nk = seq.nk;
       it->split = 0;
       item_tiles(a, it);
       const int all = it->n;
-      auto tiles_upto = [&](uint32_t x) {
+      auto tiles_upto = [&](uint64_t x) {
         if (x <= at + seq.item_cost()) return 0;
-        x -= at + seq.item_cost();
-        return (int)(seq.key_cost == KEY_COST ? x / (KEY_COST * TILE) : x / (KEY_COST_PAIR * TILE));
+        const uint32_t rows = (uint32_t)((x - at - seq.item_cost()) / TILE);
+        return (int)(seq.key_cost == KEY_COST ? rows / KEY_COST : rows / KEY_COST_PAIR);
       };
       const bool ends = end <= hi;
       it->lo = lo > at ? tiles_upto(lo) : 0;

@@ -865,3 +865,29 @@ def test_attention_of_the_binding_refuses_what_the_library_cannot_see():
                 lambda: cache.attn(q, lens, cu_q=cu, softmax_scale=-1.0), lambda: cache.attn(q[:, :3], lens), lambda: cache.attn(q.transpose(1, 2), lens)):
         with pytest.raises(binding.QEvictError):
             bad()
+
+
+# ---- bounds that fall and rise ---------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_seqs,total,n,causal", [(200, 4096, 40000, False), (64, 4096, 140000, True), (9, 700, 5000, True)])
+def test_bounds_that_give_many_sequences_the_same_rows(n_seqs, total, n, causal):
+    # 0, total, 0, total, ...: every second sequence falls and is empty, every other one has all rows.  Their work together passes 2^32 of
+    # the units in which it is shared out, although the rows of the call alone would not (the last case: both fit).  All have the
+    # same pages, so whichever of them a row's result is from, it is the same but for its sums' order.
+    hq, hkv, d, block, dtype = 32, 8, 64, 128, torch.bfloat16
+    blocks = -(-n // block)
+    pools = [torch.randn((blocks, hkv, block, d), generator=torch.Generator().manual_seed(120 + w)).to(dtype).cuda() for w in range(2)]
+    table = torch.randperm(blocks, generator=torch.Generator().manual_seed(122)).to(torch.int32)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    cache = binding.Kv16Cache(pools[0], pools[1], table[None].repeat(n_seqs, 1).cuda(), status)
+    q = _rows(total + 1, hq, d, dtype, 123)
+    cu = [total * (i % 2) for i in range(n_seqs + 1)]
+    out, lse = cache.attn(q, _i32([n] * n_seqs), _i32(cu), max_q=total, max_len=n, causal=causal, out=torch.full_like(q, 3.0), return_lse=True)
+    assert int(status) == 11
+    assert (out[total:] == 3).all()
+    k, v = ((x[table.long().cuda()].transpose(0, 1).reshape(hkv, -1, d)[:, :n].transpose(0, 1)) for x in pools)
+    for row in (0, 1, total // 3, total // 2 + 5, total - 1):
+        for g in (0, 5):
+            h, seen = slice(g * 4, g * 4 + 4), n - total + row + 1 if causal else n
+            _check_seq(out[row:row + 1, h], lse[h, row:row + 1], q[row:row + 1, h], _np(k[:seen, g:g + 1]), _np(v[:seen, g:g + 1]), seen, None, False, dtype, (row, g))
+    assert out.isfinite().all() and lse[:, :total].isfinite().all()
