@@ -10,6 +10,8 @@ namespace qevict {
 namespace {
 
 constexpr int FEW_CLUSTER_KEYS = 1024;  // of a CTA
+// Whole items: item_of adds up those of 32 sequences in 32 bits, each of which may have all rows of the call where bounds fall and rise.
+constexpr long long MOST_ITEMS = 1ll << 24;
 
 struct Plan {
   int P, T;       // rows of a query tile: heads, tokens
@@ -82,7 +84,7 @@ Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
   }
   l.by_range = rows / (2 * l.T) * groups < 6 * sms;
   if (!l.by_range) {
-    l.ctas = items <= (1ll << 28) ? (unsigned)items : 0u;
+    l.ctas = items <= MOST_ITEMS ? (unsigned)items : 0u;
     return l;
   }
   const long long most = items * (KEY_COST * longest + ITEM_COST_PAIR) / RANGE_LEAST + 1;
@@ -201,7 +203,7 @@ QEVICT_API qevict_status qevict_kv16_attn(const qevict_kv16_attn_args* p, void* 
   why = attn_check_pointers(p);
   if (why) return stateless_fail(QEVICT_ERR_INVALID_ARG, why);
   const Plan l = attn_plan(p, view);
-  if (l.ctas == 0 && !l.few) return stateless_fail(QEVICT_ERR_UNSUPPORTED, "more than 2^28 work items in one call");
+  if (l.ctas == 0 && !l.few) return stateless_fail(QEVICT_ERR_UNSUPPORTED, "more than 2^24 work items in one call");
   if (l.bytes > 0 && (!scratch || scratch_bytes < l.bytes))
     return stateless_fail(QEVICT_ERR_NO_MEMORY, "scratch too small: see qevict_kv16_attn_scratch_bytes");
   if (l.bytes > 0 && misaligned16(scratch)) return stateless_fail(QEVICT_ERR_INVALID_ARG, "scratch must be 16-byte aligned");

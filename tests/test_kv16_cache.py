@@ -891,3 +891,11 @@ def test_bounds_that_give_many_sequences_the_same_rows(n_seqs, total, n, causal)
             h, seen = slice(g * 4, g * 4 + 4), n - total + row + 1 if causal else n
             _check_seq(out[row:row + 1, h], lse[h, row:row + 1], q[row:row + 1, h], _np(k[:seen, g:g + 1]), _np(v[:seen, g:g + 1]), seen, None, False, dtype, (row, g))
     assert out.isfinite().all() and lse[:, :total].isfinite().all()
+
+
+def test_more_work_items_than_a_search_can_add_up_are_refused():
+    # 32 sequences may each have all rows of the call where bounds fall and rise: their items together have to stay below 2^31
+    view = _view(n_kv_heads=32, k_stride=(32768, 1024, 64), v_stride=(32768, 1024, 64), max_blocks=4096)
+    for total, status in ((1 << 27, 4), (1 << 30, 4), ((1 << 31) - 1025, 4)):
+        args = _attn_args(view, n_q_heads=32, total_q=total, max_q=total, max_len=65536, cu_q=4096, q_stride=(2048, 64), out_stride=(2048, 64))
+        _refused(binding.lib().qevict_kv16_attn(C.byref(args), None, 0, None), status, "2^24 work items")
