@@ -46,7 +46,8 @@ def logit_error(d, reach):
 
 def out_tolerance(out, spread, vmax, n_keys, d, reach, u_out, u_prob):
     """u_out: half a step of the output type; u_prob: of the type in which probabilities enter the product (fp16 has an
-    absolute floor of 2^-25 of the row's reference, which is at most the row's sum)."""
+    absolute floor of 2^-25 of the row's reference, which is at most the row's sum, where the reference is the largest logit;
+    the kernels set it 2^7 lower and are within 2^-32)."""
     rel = logit_error(d, reach)
     return u_out * np.abs(out) * 1.01 + (u_prob + rel) * spread * 1.01 + n_keys * 2.0 ** -25 * vmax + 1e-30
 

@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(cons
           float t = fmaxf(fmaxf(x[0][2 * i], x[0][2 * i + 1]), fmaxf(x[1][2 * i], x[1][2 * i + 1]));
           t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
           t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
-          top[i] = t * a.scale_log2;
+          top[i] = t * a.scale_log2 - P_UP<T>;
           moves = moves || top[i] > m[i] + PROMPT_LAZY;
         }
         if (__any_sync(0xffffffffu, moves)) {  // each row by its own logits: what else is in the tile has no say
@@ -285,6 +285,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, FEW_CTAS) few_attn_kernel(cons
             }
           }
         }
+        // P enters the product in the type of the values, half a step off each (prompt_attn.cuh says why m is where it is)
         uint32_t p[4];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {

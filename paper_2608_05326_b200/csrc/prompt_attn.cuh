@@ -11,8 +11,11 @@
 //   - S (128 x 128 fp32) and O (128 x d fp32) of both tiles fill the 512 columns of tensor memory.  P goes back over S
 //     in 16 bits and is the A operand of the second product from there.
 //   - While one tile's warps are in their softmax, the tensor cores work on the other tile's products.
-//   - The reference exponent m of a row moves only when a logit exceeds it by 2^8 (then O is rescaled in tensor
-//     memory); P is at most 2^8, sums are float32.
+//   - The reference exponent m of a row moves only when a logit exceeds by 2^8 the largest one that it was set by (then O is
+//     rescaled in tensor memory); sums are float32.  P is rounded to the type of the values, with which it enters the product:
+//     half a step each.  In fp16 m stands 2^7 below the largest logit (P_UP), so that P fills the type's range up to 2^15 and is
+//     lost below 2^-32 of the largest probability: with m at the largest logit 65536 keys at 2^-25 of it stayed in the sum and
+//     vanished from the product, 0.2 % of the row.
 // What bounds it: at d = 128 a key tile costs both query tiles 2048 tensor-core cycles at best; with both operands of S in
 // shared memory the products alone take about 2750 (8 KB of operands for 64 cycles of products, at 128 bytes a cycle, and
 // the copies write through the same port), and a step takes about 3600 with the softmax behind it.  Measured, call after
@@ -57,6 +60,9 @@ constexpr int PROMPT_THREADS = 640;  // four softmax warpgroups, one for product
 constexpr int MMA_WARP = 16, LOAD_WARP = 17, ITEM_WARP = 18;
 constexpr int TILE = 128;           // query rows of a tile, keys of a tile
 constexpr float PROMPT_LAZY = 8.f;  // log2
+// How far below a row's largest logit its reference is set (log2); P is at most 2^(P_UP + PROMPT_LAZY).
+template <class T> constexpr float P_UP = 0.f;  // bf16 has the range of float32
+template <> constexpr float P_UP<__half> = 7.f;
 
 // An item whose keys the ranges of several CTAs share: it starts in the CTA that has this record and ends in the range of CTA `last`.
 struct PagedCut {
@@ -1098,7 +1104,7 @@ __global__ void __launch_bounds__(PROMPT_THREADS, 1)
         }
         meet();
         if (!ok) break;
-        const float top_x = fmaxf(xch[0], xch[TILE]) * a.scale_log2;
+        const float top_x = fmaxf(xch[0], xch[TILE]) * a.scale_log2 - P_UP<T>;
         if (__any_sync(0xffffffffu, mine && top_x > m + PROMPT_LAZY)) {
           const float m_new = fmaxf(m, top_x);
           const float f = m_new == m ? 1.f : ex2p(m - m_new);

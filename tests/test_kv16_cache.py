@@ -899,3 +899,59 @@ def test_more_work_items_than_a_search_can_add_up_are_refused():
     for total, status in ((1 << 27, 4), (1 << 30, 4), ((1 << 31) - 1025, 4)):
         args = _attn_args(view, n_q_heads=32, total_q=total, max_q=total, max_len=65536, cu_q=4096, q_stride=(2048, 64), out_stride=(2048, 64))
         _refused(binding.lib().qevict_kv16_attn(C.byref(args), None, 0, None), status, "2^24 work items")
+
+
+# ---- one sharp key and a long flat tail ------------------------------------------------------------------------
+def _tail_keys(n, sinks, hkv, d, dtype, seed):
+    """Every query (ones) has the logit 1.5625 d scale at the sinks, whose values are 0, and next to none elsewhere, where the values are
+    about 1: with d = 128 a probability of 2^-25.5 of a sink's, with d = 64 and the scale of 128 doubled the same."""
+    g = torch.Generator().manual_seed(seed)
+    k, v = torch.randn((n, hkv, d), generator=g) * 0.01, 1.0 + 0.1 * torch.randn((n, hkv, d), generator=g)
+    k[sinks], v[sinks] = 1.5625, 0.0
+    return k.to(dtype).cuda(), v.to(dtype).cuda()
+
+
+def _check_tail(out, lse, k, v, scale, dtype):
+    """out [rows, Hq, d], lse [Hq, rows]: every row is a query of ones over all keys.
+
+    A probability enters the product in 16 bits: half a step off, and in fp16, where the reference stands 2^7 below the
+    largest logit, off by at most half the smallest subnormal, 2^-25, of 2^7 times the largest probability: 2^-32 of it.  bf16 has
+    no such floor."""
+    hq, d, hkv, n = out.shape[1], out.shape[2], k.shape[1], k.shape[0]
+    wo, wl, spread, reach = prompt.attention(np.ones((1, hq, d)), _np(k), _np(v), False, scale)
+    u = HALF_STEP[dtype]
+    rel, floor = prompt.logit_error(d, reach), 2.0 ** -32 if dtype is torch.float16 else 0.0
+    top = 1.0 / float(np.exp(wl[0, 0] - 1.5625 * d * scale))  # a sink's probability, the largest
+    tol = 1.01 * u * np.abs(wo) + 1.01 * (u + rel) * spread + 1.01 * n * floor * top * float(v.double().abs().max()) + SMALLEST[dtype] / 2
+    err = (out.double() - torch.tensor(wo, device=out.device)).abs() / torch.tensor(tol, device=out.device)
+    assert float(err.max()) <= 1.0, float(err.max())
+    assert ((lse.double() - torch.tensor(wl, device=out.device)).abs() <= torch.tensor(prompt.lse_tolerance(wl, d, reach), device=out.device)).all()
+    assert hq % hkv == 0 and float((1.01 * u * np.abs(wo)).max()) < float(tol.max()) < 0.05 * float(np.abs(wo).max())  # the tail is seen
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("nq,n_seqs,n,sinks", [
+    (1, 3, 8000, [0, 16, 32, 48]),        # clusters: 16 keys for each of four warps in turn, the sinks before the tail
+    (1, 222, 40000, [0, 16, 32, 48]),     # equal ranges
+    (4, 111, 40000, [0, 16, 32, 48]),
+    (30, 74, 40000, [20000, 39999]),      # pairs: the last tile first, one half of the keys each
+    (100, 37, 40000, [39999]),            # tiles of rows
+    (4096, 2, 40000, [39999]),
+])
+def test_a_long_flat_tail_under_a_sharp_key_is_not_lost(nq, n_seqs, n, sinks, d, dtype):
+    hq, hkv, block = 8, 2, 128
+    scale = 128 ** -0.5 * (2.0 if d == 64 else 1.0)
+    k, v = _tail_keys(n, sinks, hkv, d, dtype, 130)
+    blocks = -(-n // block)
+    pools = [torch.zeros((blocks, hkv, block, d), dtype=dtype, device="cuda") for _ in range(2)]
+    for x, y in zip(pools, (k, v)):
+        x.copy_(torch.nn.functional.pad(y, (0, 0, 0, 0, 0, blocks * block - n)).view(blocks, block, hkv, d).transpose(1, 2))
+    cache = binding.Kv16Cache(pools[0], pools[1], torch.arange(blocks, dtype=torch.int32, device="cuda")[None].repeat(n_seqs, 1))
+    q = torch.ones((n_seqs * nq, hq, d), dtype=dtype, device="cuda")
+    out, lse = cache.attn(q, _i32([n] * n_seqs), _cu([nq] * n_seqs), max_q=nq, causal=False, softmax_scale=scale, return_lse=True)
+    _check_tail(out, lse, k, v, scale, dtype)
+    if nq == 4096:  # the same kernel over keys side by side
+        out, lse = binding.qevict_prompt_attn(q[:8192].contiguous(), k, v, _i32([0, 8192]), _i32([0, n]), causal=False, softmax_scale=scale, return_lse=True)
+        _check_tail(out, lse, k, v, scale, dtype)
