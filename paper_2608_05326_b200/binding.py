@@ -713,15 +713,47 @@ def _rows_like(t, name, dev, dtype, n=None, heads=None, d=None):
             (name, ", ".join("any" if x is None else str(x) for x in (n, heads, d)), dtype, dev))
 
 
+class _Rope(torch.autograd.Function):
+    """The rotation with its gradient, which is the transposed rotation of the outputs' gradients."""
+
+    @staticmethod
+    def forward(ctx, q, k, positions, rotation, inverse):
+        out = qevict_rope(q, positions, rotation, k, inverse=inverse)
+        ctx.save_for_backward(positions)
+        ctx.rotation, ctx.inverse = rotation, inverse
+        ctx.set_materialize_grads(False)
+        if k is not None:
+            ctx.mark_non_differentiable(*(y for x, y in zip((q, k), out) if not x.requires_grad))
+        return out
+
+    @staticmethod
+    def backward(ctx, *grads):
+        # (a gradient may be expanded, or start anywhere: then a copy)
+        grads = [g if g is None or (g.stride(2) == 1 and not g.data_ptr() % 16 and all(n < 2 or (st > 0 and not st % 8) for n, st in zip(g.shape[:2], g.stride())))
+                 else g.clone(memory_format=torch.contiguous_format) for g in grads]
+        given = [i for i, g in enumerate(grads) if g is not None and ctx.needs_input_grad[i]]
+        result = [None] * 5
+        if given:
+            turned = qevict_rope(grads[given[0]], ctx.saved_tensors[0], ctx.rotation, grads[1] if len(given) == 2 else None, inverse=not ctx.inverse)
+            for i, x in zip(given, turned if len(given) == 2 else (turned,)):
+                result[i] = x
+        return tuple(result)
+
+
 def qevict_rope(q, positions, rotation, k=None, out=None, k_out=None, inverse=False, stream=None):
     """Rotates q [tokens, H, d] (and k [tokens, H_k, d]) to their positions, int32 [tokens] or [n_axes, tokens].  Returns out, or
     (out, k_out) with k; either may be its input.  inverse: the transposed rotation -- the gradient of the forward one.  Any
-    strides that keep d contiguous and are multiples of 16 bytes.  No gradient is recorded."""
+    strides that keep d contiguous and are multiples of 16 bytes.  Gradients with respect to q and k are recorded where autograd asks
+    for them; out and k_out cannot be given then."""
     if stream is not None:
         _check_stream(stream, _cuda(q, "q"))
         with torch.cuda.stream(stream):
             return qevict_rope(q, positions, rotation, k, out, k_out, inverse)
     dev, dtype = _cuda(q, "q"), q.dtype
+    if torch.is_grad_enabled() and any(isinstance(x, torch.Tensor) and x.requires_grad for x in (q, k, out, k_out)):
+        if out is not None or k_out is not None:
+            _refuse("out and k_out hold no history: q, k, out and k_out must not require a gradient there (or call under torch.no_grad)")
+        return _Rope.apply(q, k, positions, rotation, bool(inverse))
     if dtype not in _DTYPES:
         _refuse("q must be float16 or bfloat16")
     if not isinstance(rotation, Rotation):
@@ -793,7 +825,7 @@ class Kv16Cache:
         one token each, row s) and becomes token start[s] + i.  start < 0: the sequence is left as it is.  rotation: keys are
         stored rotated; positions int32 [total] or [n_axes, total] (default: the tokens' places in their sequences).  q [total,
         H_q, d]: rotated beside them into q_out (default: a new tensor; may be q), which is returned; its rows of no sequence
-        are not written."""
+        are not written.  No gradient is recorded."""
         if stream is not None:
             _check_stream(stream, self.device)
             with torch.cuda.stream(stream):

@@ -238,3 +238,125 @@ def test_bindings_refuse_what_the_library_cannot_see():
         with pytest.raises(binding.QEvictError):
             bad()
     assert binding.qevict_rope(q[:0], pos[:, :0], rotation).shape == (0, 2, 64)
+
+
+# ---- gradients -------------------------------------------------------------------------------------------------
+def _leaves(tokens, hq, hk, d, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    return [torch.randn((tokens, h, d), generator=g).to(dtype).cuda().requires_grad_() for h in (hq, hk)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,dtype,d,n_pairs,interleaved,n_axes,inverse", [
+    (1, torch.bfloat16, 128, 64, False, 1, False), (77, torch.float16, 64, 16, True, 1, False), (500, torch.bfloat16, 128, 40, False, 3, True), (0, torch.float16, 64, 32, False, 1, False),
+])
+def test_gradients_reach_queries_and_keys(tokens, dtype, d, n_pairs, interleaved, n_axes, inverse):
+    rotation, spec = _rot(n_pairs, n_axes, interleaved, 21, 1.25)
+    q, k = _leaves(tokens, 6, 2, d, dtype, 22)
+    wq, wk = (x.detach().flip(-1) + 1 for x in (q, k))
+    pos = torch.randint(0, 9999, (n_axes, tokens), generator=torch.Generator().manual_seed(23), dtype=torch.int32).cuda()
+    oq, ok = binding.qevict_rope(q, pos, rotation, k=k, inverse=inverse)
+    plain = binding.qevict_rope(q.detach(), pos, rotation, k=k.detach(), inverse=inverse)
+    assert torch.equal(oq, plain[0]) and torch.equal(ok, plain[1]) and not plain[0].requires_grad
+    torch.autograd.backward([oq, ok], [wq, wk])
+    for got, w in ((q.grad, wq), (k.grad, wk)):
+        _check(got, w, _np(pos), spec, not inverse)
+    # one of them alone, with and without the other
+    for part in (0, 1):
+        q2, k2 = (x.detach().requires_grad_(i == part) for i, x in enumerate((q, k)))
+        both = binding.qevict_rope(q2, pos, rotation, k=k2, inverse=inverse)
+        assert [x.requires_grad for x in both] == [part == 0, part == 1]
+        both[part].backward((wq, wk)[part])
+        assert torch.equal((q2, k2)[part].grad, (q, k)[part].grad) and (q2, k2)[1 - part].grad is None
+        alone = (q, k)[part].detach().requires_grad_()
+        binding.qevict_rope(alone, pos, rotation, inverse=inverse).backward((wq, wk)[part])
+        assert torch.equal(alone.grad, (q, k)[part].grad)
+    # a loss that sees one of two outputs: the other has no gradient
+    q3, k3 = (x.detach().requires_grad_() for x in (q, k))
+    binding.qevict_rope(q3, pos, rotation, k=k3, inverse=inverse)[1].backward(wk)
+    assert q3.grad is None and torch.equal(k3.grad, k.grad)
+
+
+@pytest.mark.gpu
+def test_gradients_by_differences_and_of_the_gradient():
+    # the map is linear, so a step of any size from 0 is its derivative, but for roundings: <w, R (x + e) - R x> against <grad, e>
+    rotation, spec = _rot(24, 1, False, 24)
+    x = _leaves(40, 3, 1, 64, torch.float16, 25)[0]
+    at = x.detach()
+    pos = torch.arange(40, dtype=torch.int32, device="cuda") * 7
+    w, e = (torch.randn_like(x).detach() for _ in range(2))
+    (grad,) = torch.autograd.grad(binding.qevict_rope(x, pos, rotation), x, w)
+    moved = binding.qevict_rope(at + e, pos, rotation).double() - binding.qevict_rope(at, pos, rotation).double()
+    left, right = (w.double() * moved).sum(), (grad.double() * ((at + e).double() - at.double())).sum()
+    # three roundings of at most half a step: of both images, weighted with w, and of the gradient, weighted with the step
+    size = sum(float((a.double().norm(dim=-1) * b.double().norm(dim=-1)).sum()) for a, b in ((w, at + e), (w, at), (w, (at + e).double() - at.double())))
+    assert abs(float(left - right)) <= 2.0 ** -11 * 2 ** 0.5 * 1.01 * size
+    # gradients of gradients: <grad(w), u> as a function of w has the gradient R u
+    v = w.clone().requires_grad_()
+    (first,) = torch.autograd.grad(binding.qevict_rope(x, pos, rotation), x, v, create_graph=True)
+    (second,) = torch.autograd.grad(first, v, e)
+    assert torch.equal(second, binding.qevict_rope(e, pos, rotation))
+
+
+@pytest.mark.gpu
+def test_gradients_of_any_strides_and_streams():
+    rotation, _ = _rot(32, 1, True, 26)
+    pos = torch.arange(50, dtype=torch.int32, device="cuda")
+    q = _leaves(50, 4, 1, 64, torch.bfloat16, 27)[0]
+    for make in (lambda y: y.sum(), lambda y: y[:, 1].sum(), lambda y: (y.transpose(0, 1).reshape(4, -1) * torch.arange(4, device="cuda", dtype=y.dtype)[:, None]).sum(),
+                 lambda y: (y.transpose(1, 2) * 2).sum(), lambda y: y[..., 1:].sum()):
+        (want_g,) = torch.autograd.grad(make((z := binding.qevict_rope(q.detach(), pos, rotation).requires_grad_())), z)
+        want = binding.qevict_rope(want_g.contiguous(), pos, rotation, inverse=True)
+        (got,) = torch.autograd.grad(make(binding.qevict_rope(q, pos, rotation)), q)
+        assert torch.equal(got, want)
+    wide = torch.randn((50, 4 * 64 + 4), dtype=torch.bfloat16, device="cuda")  # a gradient that starts off the 16 bytes
+    off = wide[:, 4:].view(50, 4, 64)
+    (got,) = torch.autograd.grad(binding.qevict_rope(q, pos, rotation), q, off)
+    assert torch.equal(got, binding.qevict_rope(off.contiguous(), pos, rotation, inverse=True))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    y = binding.qevict_rope(q, pos, rotation, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    (got,) = torch.autograd.grad(y, q, torch.ones_like(y))
+    torch.cuda.synchronize()
+    assert torch.equal(got, binding.qevict_rope(torch.ones_like(q).detach(), pos, rotation, inverse=True))
+
+
+@pytest.mark.gpu
+def test_gradients_in_a_captured_step():
+    rotation, spec = _rot(32, 1, False, 28)
+    q = _leaves(60, 4, 1, 64, torch.float16, 29)[0]
+    pos = torch.arange(60, dtype=torch.int32, device="cuda")
+    w = torch.randn_like(q).detach()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.autograd.grad(binding.qevict_rope(q, pos, rotation), q, w)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        (grad,) = torch.autograd.grad(binding.qevict_rope(q, pos, rotation), q, w)
+    for _ in range(2):
+        w.copy_(torch.randn_like(w))
+        graph.replay()
+        _check(grad, w, pos.cpu().numpy(), spec, True)
+
+
+@pytest.mark.gpu
+def test_a_gradient_is_not_lost_in_given_outputs():
+    rotation, _ = _rot(32, 1, False, 30)
+    q, k = _leaves(5, 2, 2, 64, torch.float16, 31)
+    pos, plain = torch.arange(5, dtype=torch.int32, device="cuda"), q.detach()
+    for bad in (lambda: binding.qevict_rope(q, pos, rotation, out=plain), lambda: binding.qevict_rope(plain, pos, rotation, k=k, k_out=plain),
+                lambda: binding.qevict_rope(plain, pos, rotation, k=k, out=plain), lambda: binding.qevict_rope(plain, pos, rotation, out=q)):
+        with pytest.raises(binding.QEvictError, match="gradient"):
+            bad()
+    with torch.no_grad():
+        out = torch.empty_like(plain)
+        assert binding.qevict_rope(q, pos, rotation, out=out) is out and not out.requires_grad
+        assert not binding.qevict_rope(q, pos, rotation).requires_grad
+    assert binding.qevict_rope(plain, pos, rotation, out=out) is out
+    y = binding.qevict_rope(q, pos, rotation)
+    pos += 1  # what the gradient needs is not the same any more
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
