@@ -51,6 +51,60 @@ Plan with_scratch(Plan l, const qevict_kv16_attn_args* p, const Kv16View& c) {
   return l;
 }
 
+template <class K> cudaError_t few_attributes(K kernel, int smem) {
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 45);  // FEW_CTAS fit; the rest is L1
+  return e;
+}
+template <class T, int D> cudaError_t few_cluster_attributes(int device) {
+  static std::atomic<uint64_t> done{0};
+  return once_per_device(done, device, [] {
+    auto kernel = few_attn_kernel<T, D, true>;
+    const cudaError_t e = few_attributes(kernel, few_smem(D));
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  });
+}
+void few_cluster_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attr, int D, int ranks, dim3 grid, cudaStream_t s) {
+  cfg->gridDim = grid;
+  cfg->blockDim = dim3(32 * FEW_WARPS);
+  cfg->dynamicSmemBytes = few_smem(D);
+  cfg->stream = s;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ranks;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg->attrs = attr;
+  cfg->numAttrs = 2;
+}
+
+// The largest cluster that the device holds, asked once for the instance that takes most of it: 16 thread blocks on a whole one; a part
+// of one may have fewer SMs side by side, and a launch of more is an error.
+int few_most_ranks(int device) {
+#ifdef QEVICT_DEBUG_BOUNDS
+  if (const char* e = getenv("QEVICT_CHECK_CLUSTER")) return atoi(e);  // the checking build can be told of a smaller one
+#endif
+  static std::atomic<int> known[64];
+  if (device >= 64) return 1;
+  int most = known[device].load(std::memory_order_relaxed);
+  if (most > 0) return most;
+  DeviceGuard guard(device);
+  if (guard.err != cudaSuccess || few_cluster_attributes<__nv_bfloat16, 128>(device) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return 16;  // (no device: the size of the scratch is asked for elsewhere; the launch says so)
+  }
+  for (most = 16; most > 1; most /= 2) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    few_cluster_config(&cfg, attr, 128, most, dim3(most), nullptr);
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, few_attn_kernel<__nv_bfloat16, 128, true>, &cfg) == cudaSuccess && n > 0) break;
+    (void)cudaGetLastError();
+  }
+  known[device].store(most, std::memory_order_relaxed);
+  return most;
+}
+
 // Equal ranges of the work for all SMs; a call of many items (six for each SM, by its rows) hands out whole ones as SMs fall free,
 // longest first: CTAs that work on one head then walk its keys together, and the L2 serves most of them.
 Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
@@ -69,8 +123,9 @@ Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
     l.T = max_q > 0 ? (int)max_q : 1;
     // clusters as large as one wave holds, four steps of keys for each CTA at least
     const long long room = (long long)sms * FEW_CTAS;
+    const int most_ranks = few_most_ranks(p->cache->device);
     int ranks = 1;
-    while (ranks < 16 && units * ranks * 2 <= room && ranks * 2 * FEW_WARPS * FEW_KEYS <= longest) ranks *= 2;
+    while (ranks < most_ranks && units * ranks * 2 <= room && ranks * 2 * FEW_WARPS * FEW_KEYS <= longest) ranks *= 2;
     if (longest <= (long long)ranks * FEW_CLUSTER_KEYS && units * longest <= room * FEW_CLUSTER_KEYS) {
       l.ranks = ranks;
       return l;
@@ -127,12 +182,6 @@ const char* attn_check_pointers(const qevict_kv16_attn_args* p) {
   return nullptr;
 }
 
-template <class K> cudaError_t few_attributes(K kernel, int smem) {
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 45);  // FEW_CTAS fit; the rest is L1
-  return e;
-}
-
 template <class T, int D>
 cudaError_t launch_few(const PromptArgs& a, const Plan& l, const FewPages& g, int device, cudaStream_t s) {
   if (!l.ranks) {
@@ -143,27 +192,12 @@ cudaError_t launch_few(const PromptArgs& a, const Plan& l, const FewPages& g, in
     if (e == cudaSuccess && l.cuts) e = launch_pdl(paged_merge_kernel<T, D>, dim3(l.slot_rows / 32, l.ctas, D / 64), dim3(32 * MERGE_WARPS), 0, s, a);
     return e;
   }
-  auto kernel = few_attn_kernel<T, D, true>;
-  static std::atomic<uint64_t> done{0};
-  const cudaError_t e = once_per_device(done, device, [&] {
-    const cudaError_t e0 = few_attributes(kernel, few_smem(D));
-    return e0 != cudaSuccess ? e0 : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-  });
+  const cudaError_t e = few_cluster_attributes<T, D>(device);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(l.ranks * a.Hkv, a.n_seqs);
-  cfg.blockDim = dim3(32 * FEW_WARPS);
-  cfg.dynamicSmemBytes = few_smem(D);
-  cfg.stream = s;
   cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = l.ranks;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kernel, a, g);
+  few_cluster_config(&cfg, attr, D, l.ranks, dim3(l.ranks * a.Hkv, a.n_seqs), s);
+  return cudaLaunchKernelEx(&cfg, few_attn_kernel<T, D, true>, a, g);
 }
 
 template <class T, int D>

@@ -96,3 +96,34 @@ def test_a_wait_that_gives_up_leaves_results_or_not_a_number():
     thread block leaves, its other warps leave with it and soon, and each row and head holds its result, or not-a-number."""
     r = _run(_GIVE_UP)
     assert r.returncode == 0 and "gave up" in r.stdout, r.stdout[-1500:] + r.stderr[-3000:]
+
+
+_CLUSTERS = """
+    import os
+    import torch
+    from paper_2608_05326_b200 import binding, build
+    build.build(variant="check")
+    import test_kv16_cache as t
+
+    for most in (1, 2, 4, 8):
+        os.environ["QEVICT_CHECK_CLUSTER"] = str(most)
+        for nq, lens, hq, hkv, d, dtype in (([1], [2048], 32, 8, 128, torch.bfloat16), ([1, 2, 1], [8000, 1, 700], 8, 2, 64, torch.float16), ([3], [16000], 4, 1, 128, torch.float16),
+                                            ([4], [900], 4, 1, 128, torch.bfloat16)):
+            cache, pools, table, status, q = t._case(nq, lens, hq, hkv, d, 64, dtype, 140)
+            out, lse = cache.attn(q, t._i32(lens), t._cu(nq), max_q=max(nq), max_len=max(lens), return_lse=True)
+            t._check_attn(out, lse, q, pools, table, lens, nq, True, dtype)
+            assert int(status) == 0
+            os.environ["QEVICT_CHECK_CLUSTER"] = "16"  # what a whole device holds: the same results but for their sums' order
+            whole = cache.attn(q, t._i32(lens), t._cu(nq), max_q=max(nq), max_len=max(lens), return_lse=True)
+            t._check_attn(whole[0], whole[1], q, pools, table, lens, nq, True, dtype)
+            del os.environ["QEVICT_CHECK_CLUSTER"]  # the device's own answer
+            own = cache.attn(q, t._i32(lens), t._cu(nq), max_q=max(nq), max_len=max(lens), return_lse=True)
+            assert torch.equal(own[0], whole[0]) and torch.equal(own[1], whole[1])
+            os.environ["QEVICT_CHECK_CLUSTER"] = str(most)
+    print("clusters")
+"""
+
+
+def test_a_device_that_holds_no_large_clusters_takes_smaller_ones_or_ranges():
+    r = _run(_CLUSTERS)
+    assert r.returncode == 0 and "clusters" in r.stdout, r.stdout[-1500:] + r.stderr[-3000:]
