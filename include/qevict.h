@@ -386,8 +386,9 @@ QEVICT_API qevict_status qevict_import_state(qevict_handle h, int32_t layer, int
  * k, v [n_seqs, n_kv_heads, max_k, d] (the layout of qevict_prefill_assign), lse [n_seqs, n_q_heads, max_q];
  * bounds are device int32 [n_seqs] lengths, or NULL for max_q / max_k everywhere.  max_q and max_k bound the
  * lengths; a longer sequence is cut to them, one that reaches outside the rows to these, one whose bounds fall is
- * empty; each sets *status.  A key or value that is not finite spreads to every row of the
- * sequence from 255 tokens before it on (nothing outside the sequence is affected). */
+ * empty; each sets *status (n_q and n_k are then what is left: a cut sequence's rows are masked as the last of its cut keys).
+ * A key or value that is not finite spreads to every row of the sequence from 255 tokens before it on (nothing outside the
+ * sequence is affected). */
 enum { QEVICT_LAYOUT_PACKED = 0, QEVICT_LAYOUT_PADDED = 1 };
 typedef struct {
   uint32_t struct_size;      /* sizeof(qevict_prompt_args) */
@@ -588,9 +589,9 @@ typedef struct {
  * s).  With a rotation the keys are stored rotated and, where q is given, q_out gets the rotated queries (q_out may be q);
  * positions: device [n_axes][total_new], or NULL for the tokens' places in their sequences on every axis.  Without a rotation
  * rows are stored (and queries copied) as they are.  Tokens past the table are dropped (their queries are rotated all the same), a
- * sequence whose rows do not lie in 0 .. total_new - 1 is left as it is; both set *status, as bounds that fall do.  A sequence with start < 0 is left as it is.
- * Rows of no sequence are not read into a result, and their rows of q_out are not written.  No two tokens of a call may share
- * a place. */
+ * sequence whose rows do not lie in 0 .. total_new - 1 is left as it is; both set *status, as bounds that fall do.  A sequence with
+ * start < 0 is left as it is, its rows of q_out too.  Rows of no sequence are not read into a result, and their rows of q_out are
+ * not written.  No two tokens of a call may share a place. */
 typedef struct {
   uint32_t struct_size;      /* sizeof(qevict_kv16_append_args) */
   int32_t n_q_heads;         /* 0: no queries */
@@ -617,10 +618,12 @@ QEVICT_API qevict_status qevict_kv16_append(const qevict_kv16_append_args* args,
  * over the tokens j that are there and, with `causal`, j <= i + lens[s] - n_q[s] (the queries are the last n_q of lens tokens).
  * A query that sees no token gets out = 0 and lse = -infinity.  q, out: [total_q] rows of n_q_heads heads (strides token, head),
  * sequence s has rows cu_q[s] .. cu_q[s + 1] - 1 (device int32, ascending), or row s without cu_q; rows of no sequence are
- * not written.  out may be q (same strides).  lse [n_q_heads, total_q].  max_q and max_len bound the lengths and size the launch; a sequence with more
- * new tokens is cut to the first max_q, one with lens beyond max_len or the table to the smaller of them, rows outside 0 ..
+ * not written.  out may be q (same strides).  lse [n_q_heads, total_q].  max_q and max_len bound the lengths and size the launch; a
+ * sequence with more new tokens is cut to the first max_q, one with lens beyond max_len or the table to the smaller of them, rows outside 0 ..
  * total_q - 1 are left out, bounds that fall are empty, and each sets *status, as a length < 0 does (rows that such bounds give to
- * several sequences get the result of any of them, or none).  A key or value that is not
+ * several sequences get the result of any of them, or none).  n_q[s] and lens[s] are then what is left: a cut sequence's rows are masked
+ * as the last ones of its cut length.  max_len may be any bound, the table's for a captured step, but the closer it is the better the
+ * plan: it decides whether a short call takes one launch or two and how many thread blocks share it.  A key or value that is not
  * finite spreads to every row of its sequence from 255 tokens before it on.  scratch: device, from
  * qevict_kv16_attn_scratch_bytes for the same arguments; calls that may run at the same time need scratch of their own.  How the
  * keys are shared among thread blocks, and with it the order of the float32 sums, follows from all lengths of the call; the same

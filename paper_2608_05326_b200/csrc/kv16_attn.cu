@@ -106,7 +106,10 @@ int few_most_ranks(int device) {
 }
 
 // Equal ranges of the work for all SMs; a call of many items (six for each SM, by its rows) hands out whole ones as SMs fall free,
-// longest first: CTAs that work on one head then walk its keys together, and the L2 serves most of them.
+// longest first: CTAs that work on one head then walk its keys together, and the L2 serves most of them.  Both sides, best graph replays,
+// 32 / 8 heads of 128: 4 prompts of 2048 (7 items for each SM) whole 179 us, ranges 215; 8192 behind 57344 (7) 6.6 and 7.2 ms; 16384 alone
+// (14) 1.83 and 1.99 ms; 4096 behind 57344 (3.5) 3.57 and 3.43 ms; 2048 (1.7) 1.75 and 1.63 ms.  The rows do not say how unlike the
+// items are: a prompt of 8192 beside one token with 131072 takes 1.39 ms in whole items, 8 of which last beyond all others, 0.67 in ranges.
 Plan attn_plan(const qevict_kv16_attn_args* p, const Kv16View& c) {
   Plan l = {};
   prompt_tile(p->n_q_heads / c.Hkv, &l.P, &l.T);

@@ -15,9 +15,11 @@
 // up to 16 CTAs, which join their sums through each other's shared memory (one launch, no scratch); any other gives each CTA an equal
 // range of its work (FewRange) and joins what ranges share in a second launch.
 // Measured (32 / 8 heads of 128, one token for each of n sequences, graph replays; beside it the kernel for tiles of rows, which takes
-// 16 rows as 128): n = 1, 128 tokens 5.3 us (14.1), 2048 tokens 9.2 us (17.8), 8000: 18.4 us (22.9); n = 16, 2000: 33.8 us (40.7).  Ranges,
-// call after call: n = 64, 2048 tokens 105 us (124), 8 x 65536 tokens of 28 / 4 heads 200 us (5.4 TB/s; 230): short runs take 190 us
-// either way, but here the power limit leaves 1.75 GHz where tensor memory products of 128 rows leave 1.57.
+// 16 rows as 128): n = 1, 128 tokens 5.5 us (14.1), 2048 tokens 9.2 us (17.8), 8000: 17.5 to 18.4 us (22.9); n = 16, 2000: 34.3 us (40.7).
+// Ranges, call after call: n = 64, 2048 tokens 109 us (124), 8 x 65536 tokens of 28 / 4 heads 195 to 205 us (5.2 to 5.5 TB/s; 230): short
+// runs take 193 us either way, but here the power limit leaves 1.75 GHz where tensor memory products of 128 rows leave 1.57.
+// The rest of P behind its rounding as a second product takes the error against 64 bits from 2.0e-3 to 1.6e-3 in bf16 (the output's own
+// rounding) and costs 5 to 6 % (8 x 65536 193 -> 204 us): left out, as in the kernel for tiles.
 // Loads on their way have their place in the L1, so shared memory is kept small: with all of it 8 x 65536 tokens took 270 us; through a
 // ring in shared memory (cp.async) 231 us.
 #pragma once

@@ -19,11 +19,10 @@
 // What bounds it: at d = 128 a key tile costs both query tiles 2048 tensor-core cycles at best; with both operands of S in
 // shared memory the products alone take about 2750 (8 KB of operands for 64 cycles of products, at 128 bytes a cycle, and
 // the copies write through the same port), and a step takes about 3600 with the softmax behind it.  Measured, call after
-// call: causal 32768 tokens x 32 heads 7.97 ms (1103 TFLOP/s, 0.78 of the measured sustained rate; the power limit holds it there:
-// single calls of a cool card take 6.9 to 7.4 ms); 12 packed prompts of up to 4001 tokens 594 us (849 TFLOP/s), the best of graph
-// replays 497 to 512 us; d = 64: 16384 tokens x 32 heads 1.57 ms (702 TFLOP/s: half the products for the same exponentials).
-// Shares of the
-// exponentials as polynomials on the FMA units were slower at every share (1/2 to 1/16): what the softmax waits for is
+// call: causal 32768 tokens x 32 heads 7.82 to 7.97 ms (1103 to 1125 TFLOP/s, 0.8 of the measured sustained rate; the power limit holds
+// it there: single calls of a cool card take 6.8 to 7.4 ms); 12 packed prompts of up to 4001 tokens 572 to 594 us (849 to 882 TFLOP/s),
+// the best of graph replays 494 to 512 us; d = 64: 16384 tokens x 32 heads 1.57 ms (702 TFLOP/s: half the products for the same
+// exponentials).  Shares of the exponentials as polynomials on the FMA units were slower at every share (1/2 to 1/16): what the softmax waits for is
 // issue and hand-over, not the exponential unit.
 //
 // Few query rows (one token, a short piece behind a long prefix): the keys are split over several CTAs whose partial
@@ -31,12 +30,14 @@
 //
 // PAGED: keys and values come by page, one copy for each page of a head (a box of {64 channels, 8 tokens, d / 64 pieces, groups}: the
 // pieces of eight keys land side by side, which the products' descriptors follow); copies of 64 channels of a page took 276 us
-// where these take 214, pages of 16 tokens, 8 x 65536 tokens.  Calls with fewer than six items for each SM give every CTA an
+// where these took 214, pages of 16 tokens, 8 x 65536 tokens.  Calls with fewer than six items for each SM give every CTA an
 // equal range of the work (PagedRange) and join what ranges share in paged_merge_kernel; others hand out whole items as above.
 // A sequence with one tile of rows has both query tiles take the same rows and half of the keys each.  Measured, 32 / 8 heads of
-// 128, call after call: 8192 tokens behind 57344 7.7 ms (1075 TFLOP/s), pieces of up to 701 tokens behind up to 24000 of four prompts
-// 473 us (920 TFLOP/s; 403 us, 1078 TFLOP/s before the power limit), drafts of up to 5 tokens of 16 users with up to 32768
-// 187 us (5.0 TB/s; 166 us).
+// 128, call after call on several cards (single calls of a cool one): 8192 tokens behind 57344 7.70 to 7.79 ms, 1060 to 1071 TFLOP/s (6.6);
+// pieces of up to 701 tokens behind up to 24000 of four prompts 480 to 490 us, 888 to 906 TFLOP/s (415); drafts of up to 5 tokens of 16
+// users with up to 32768 178 to 188 us, 5.0 to 5.3 TB/s (165).  Registers: of the 476 bytes that the compiler reports
+// as spilled at d = 128 (832 loaded) 290 (530) go with the item warp's search for its range, which runs beside the products in 32
+// registers: without that search it reports 184 (300), and 28 (24) for the kernel without pages.
 //
 // Keys past the sequence's end are masked by selection, so what lies there (another sequence, padding, NaN) never
 // enters; value rows past the end are zeroed in shared memory before the product reads them, since 0 * NaN is NaN.
@@ -382,9 +383,10 @@ template <bool PAGED> __device__ __forceinline__ PromptItem item_of(const Prompt
 //
 // The items stand in a row: sequence by sequence, heads in it, tiles of rows in these.  An item costs its visible keys (three
 // quarters for pairs, whose two tiles a step bandwidth bounds) and a constant (8200 cycles of 3800 for a tile of keys; pairs,
-// which drain the copies, 16500 of 2000).  (A piece of 2048 tokens between 31 single ones 668 us; pairs' keys at three sevenths 785 us,
-// at seven and eleven eighths 688 and 727 us.)  CTA c has what lies in [c, c + 1) * W of
-// the sum.  An end inside an item is moved to a key tile: an item has the CTAs that have tiles of it, and where these are
+// which drain the copies, 16500 of 2000).  Pairs' keys at two, three
+// and four quarters, graph replays: a piece of 2048 tokens between 31 single ones 707, 703, 731 us (heads of 64: 636, 609, 653); drafts of
+// 16 users 245, 241, 269; of 64 users with 2048 tokens each 122, 121, 120; a piece of 300 between 8 single ones 193, 235, 287.  CTA c has
+// what lies in [c, c + 1) * W of the sum.  An end inside an item is moved to a key tile: an item has the CTAs that have tiles of it, and where these are
 // several, each writes a partial result.  The ranges are a function of the lengths alone.  The sum is held in 64 bits: bounds that
 // fall and rise give many sequences the same rows, so no bound on the rows keeps it within 32 (an item that crossed the end of a
 // sum that had wrapped named a CTA behind the last, whose results the join then read behind the scratch).
