@@ -45,11 +45,13 @@ def logit_error(d, reach):
 
 
 def out_tolerance(out, spread, vmax, n_keys, d, reach, u_out, u_prob):
-    """u_out: half a step of the output type; u_prob: of the type in which probabilities enter the product (fp16 has an
-    absolute floor of 2^-25 of the row's reference, which is at most the row's sum, where the reference is the largest logit;
-    the kernels set it 2^7 lower and are within 2^-32)."""
+    """u_out: half a step of the output type; u_prob: of the type in which probabilities enter the product.  fp16 has an absolute
+    floor of 2^-25 of the row's reference, which is at most the row's sum, where the reference is the largest logit (the kernels
+    for 16-bit keys set it 2^7 lower and are within 2^-32).  bf16 has the range of float32 and no such floor: what is left is the
+    float32 sum of n_keys products, a rounding of 2^-24 of the sum of magnitudes for each."""
     rel = logit_error(d, reach)
-    return u_out * np.abs(out) * 1.01 + (u_prob + rel) * spread * 1.01 + n_keys * 2.0 ** -25 * vmax + 1e-30
+    rest = n_keys * (2.0 ** -25 * vmax if u_prob < 2.0 ** -9 else 2.0 ** -24 * spread)
+    return u_out * np.abs(out) * 1.01 + (u_prob + rel) * spread * 1.01 + rest + 1e-30
 
 
 def lse_tolerance(lse, d, reach):
