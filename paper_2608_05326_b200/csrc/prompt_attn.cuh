@@ -22,8 +22,8 @@
 // call: causal 32768 tokens x 32 heads 7.82 to 7.97 ms (1103 to 1125 TFLOP/s, 0.8 of the measured sustained rate; the power limit holds
 // it there: single calls of a cool card take 6.8 to 7.4 ms); 12 packed prompts of up to 4001 tokens 572 to 594 us (849 to 882 TFLOP/s),
 // the best of graph replays 494 to 512 us; d = 64: 16384 tokens x 32 heads 1.57 ms (702 TFLOP/s: half the products for the same
-// exponentials).  Shares of the exponentials as polynomials on the FMA units were slower at every share (1/2 to 1/16): what the softmax waits for is
-// issue and hand-over, not the exponential unit.
+// exponentials).  Shares of the exponentials as polynomials on the FMA units were slower at every share (1/2 to 1/16): what the
+// softmax waits for is issue and hand-over, not the exponential unit.
 //
 // Few query rows (one token, a short piece behind a long prefix): the keys are split over several CTAs whose partial
 // outputs prompt_merge_kernel joins.
@@ -383,13 +383,13 @@ template <bool PAGED> __device__ __forceinline__ PromptItem item_of(const Prompt
 //
 // The items stand in a row: sequence by sequence, heads in it, tiles of rows in these.  An item costs its visible keys (three
 // quarters for pairs, whose two tiles a step bandwidth bounds) and a constant (8200 cycles of 3800 for a tile of keys; pairs,
-// which drain the copies, 16500 of 2000).  Pairs' keys at two, three
-// and four quarters, graph replays: a piece of 2048 tokens between 31 single ones 707, 703, 731 us (heads of 64: 636, 609, 653); drafts of
-// 16 users 245, 241, 269; of 64 users with 2048 tokens each 122, 121, 120; a piece of 300 between 8 single ones 193, 235, 287.  CTA c has
-// what lies in [c, c + 1) * W of the sum.  An end inside an item is moved to a key tile: an item has the CTAs that have tiles of it, and where these are
-// several, each writes a partial result.  The ranges are a function of the lengths alone.  The sum is held in 64 bits: bounds that
-// fall and rise give many sequences the same rows, so no bound on the rows keeps it within 32 (an item that crossed the end of a
-// sum that had wrapped named a CTA behind the last, whose results the join then read behind the scratch).
+// which drain the copies, 16500 of 2000).  Pairs' keys at two, three and four quarters, graph replays: a piece of 2048 tokens between 31
+// single ones 707, 703, 731 us (heads of 64: 636, 609, 653); drafts of 16 users 245, 241, 269; of 64 users with 2048 tokens each 122,
+// 121, 120; a piece of 300 between 8 single ones 193, 235, 287.  CTA c has what lies in [c, c + 1) * W of the sum.  An end inside an
+// item is moved to a key tile: an item has the CTAs that have tiles of it, and where these are several, each writes a partial result.
+// The ranges are a function of the lengths alone.  The sum is held in 64 bits: bounds that fall and rise give many sequences the same
+// rows, so no bound on the rows keeps it within 32 (an item that crossed the end of a sum that had wrapped named a CTA behind the
+// last, whose results the join then read behind the scratch).
 constexpr int ITEM_COST = 1024, KEY_COST = 4, ITEM_COST_PAIR = 3200, KEY_COST_PAIR = 3, RANGE_LEAST = 1024;
 
 // (What runs before the first copy runs once, from instructions that are fetched as they come: some 50 cycles for each, so its
